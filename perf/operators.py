@@ -1,0 +1,499 @@
+"""The measured calls of the label-scoring and 8-bit cache operators: what a
+streaming recogniser computes around its decoder when it asks how sure it was,
+aligns a transcript, or runs a neural language model beside the n-gram LMs.
+
+  scores  ``label_scores``: log probabilities of given labels, entropy and the
+          top alternatives of rows of logits in memory
+  joint   ``joint_label_scores``: the same from the joint network's input rows
+          and output weights, the logits staying on the chip
+  append  ``KV8Cache.append`` and ``KV8Cache.read``: new keys and values into a
+          paged 8-bit cache, and the touched blocks' values back
+  attend  ``KV8Cache.attend``: attention over that cache, causal, with a
+          sliding window and first tokens that stay visible
+
+Everything but a cache's handle is the same for both forms; the handle holds
+the state's own tensors.
+"""
+import math
+import random
+import types
+
+import torch
+
+own = False
+
+DEV = "cuda"
+LEAST, MOST = 2.0 ** -32, 2.0 ** 60  # magnitudes that a block's scale covers
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+# ---------------------------------------------------------------- the cases
+
+def _scores(name, n, C, ld, dtype, m, k, temp):
+    return dict(name=name, kind="scores", n=n, C=C, ld=ld, dtype=dtype, m=m, k=k, temp=temp)
+
+
+def _joint(name, n, H, C, m, k, temp=1.0):
+    return dict(name=name, kind="joint", n=n, H=H, C=C, m=m, k=k, temp=temp)
+
+
+def _append(name, n, new, past, heads, dim, block, dtype):
+    return dict(name=name, kind="append", n=n, new=new, past=past, heads=heads, dim=dim, block=block, dtype=dtype)
+
+
+def _attend(name, n, new, past, heads, kv, dim, block, window, sinks, dtype):
+    return dict(name=name, kind="attend", n=n, new=new, past=past, heads=heads, kv=kv, dim=dim, block=block,
+                window=window, sinks=sinks, dtype=dtype)
+
+
+def listed():
+    return [
+        # one live stream asks how sure its last label was (V = 1024 and blank): latency
+        _scores("scores 1 x 1025", 1, 1025, 1025, "fp32", 1, 4, 1.0),
+        # a wide sub-word vocabulary of a neural LM, a batch of hypotheses, rows of a padded buffer
+        _scores("scores 96 x 131073 bf16", 96, 131073, 131080, "bf16", 1, 8, 0.8),
+        # the lattices of a batch of utterances (V = 4096 and blank): label and blank at each node
+        _scores("scores 16384 x 4097", 16384, 4097, 4097, "fp32", 2, 5, 1.0),
+        # the small joint network (V = 256, H = 320) for a few streams
+        _joint("joint 7 x 320 x 257", 7, 320, 257, 1, 3),
+        # one utterance's lattice, small model, an odd number of nodes
+        _joint("joint 1001 x 640 x 1025", 1001, 640, 1025, 2, 4),
+        # a batch of utterances on the large model: alignment of training or rescored transcripts
+        _joint("joint 16384 x 1024 x 4097", 16384, 1024, 4097, 2, 5),
+        # one new token for each hypothesis of a full server
+        _append("append 256 x 1", 256, 1, 1500, 8, 64, 32, "bf16"),
+        # prompts of a few hypotheses, ragged
+        _append("append 6 x 4000", 6, 4000, 0, 8, 128, 64, "bf16"),
+        # one hypothesis, one token, a short context: latency
+        _attend("attend 1 x 1 past 777", 1, 1, 777, 8, 8, 64, 16, 0, 0, "bf16"),
+        # single tokens over long ragged contexts, shared key and value heads
+        _attend("attend 64 x 1 past 16000", 64, 1, 16000, 32, 8, 128, 32, 0, 0, "bf16"),
+        # a 1040 ms chunk of an endless stream: a window, and first tokens that stay
+        _attend("attend 96 x 13 window 512", 96, 13, 5000, 8, 8, 128, 16, 512, 4, "fp16"),
+        # ragged prompts after a shared context
+        _attend("attend 4 x 4000 past 2000", 4, 4000, 2000, 16, 4, 128, 64, 0, 0, "bf16"),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["scores", "joint", "append", "attend", "attend"])
+    if kind == "scores":
+        C = _log_int(rng, 2, 200_000)
+        n = _log_int(rng, 1, min(16384, max(2, 60_000_000 // C)))
+        c = _scores("", n, C, C + rng.choice([0, 0, 3, 8]), rng.choice(["fp32", "bf16", "fp16"]), rng.randint(0, 3),
+                    rng.randint(0, 8), rng.choice([1.0, 1.0, 0.7, 1.5]))
+    elif kind == "joint":
+        H, C = 64 * rng.randint(1, 16), _log_int(rng, 17, 4097)
+        c = _joint("", _log_int(rng, 1, 16384), H, C, rng.randint(0, 3), rng.randint(0, 8), rng.choice([1.0, 1.0, 0.7]))
+    elif kind == "append":
+        heads, dim, block = rng.choice([1, 2, 5, 8]), rng.choice([64, 128]), rng.choice([16, 32, 64])
+        if rng.random() < 0.5:  # a few tokens a sequence, at any length
+            c = _append("", _log_int(rng, 1, 256), rng.randint(1, block), _log_int(rng, 1, 3000), heads, dim, block, "bf16")
+        else:  # prompts
+            c = _append("", _log_int(rng, 1, 8), _log_int(rng, 65, 3500), 0, heads, dim, block, rng.choice(["bf16", "fp16"]))
+    else:
+        kv = rng.choice([1, 2, 4, 8])
+        heads, dim, block = kv * rng.choice([1, 1, 2, 3, 4, 8]), rng.choice([64, 128]), rng.choice([16, 32, 64])
+        new = rng.choice([1, 1, rng.randint(2, 32), _log_int(rng, 33, 2500)])
+        past = _log_int(rng, 1, 12000 if new < 33 else 3500)
+        n = _log_int(rng, 1, 96 if new == 1 else 48 if new < 33 else 3)
+        if new == 1:  # the caches of all sequences stay below the largest listed case's
+            past = min(past, 64 * 16000 * 1024 // (n * kv * dim))
+        elif new < 33:  # ... and the products
+            past = min(past, max(64, 400_000_000 // (n * new * heads)))
+        window = rng.choice([0, 0, _log_int(rng, 1, 2000)])
+        c = _attend("", n, new, past, heads, kv, dim, block, window, rng.choice([0, 4, 17]) if window else 0,
+                    rng.choice(["bf16", "fp16"]))
+    del c["name"]
+    return c
+
+
+# ---------------------------------------------------------------- inputs
+
+def _rng(seed):
+    return torch.Generator(device=DEV).manual_seed(int(seed))
+
+
+def _lengths(case):
+    """(tokens before the call, new tokens) of each sequence: ragged, and the
+    same at every seed (a case's work is known without its inputs)."""
+    r = random.Random(case["n"] * 7919 + case["new"] * 31 + case["past"])
+    if case["n"] == 1:
+        return [case["past"]], [case["new"]]
+    new = [case["new"] if case["new"] < 33 else max(1, int(case["new"] * r.uniform(0.5, 1.0))) for _ in range(case["n"])]
+    return [int(case["past"] * r.uniform(0.3, 1.0)) for _ in range(case["n"])], new
+
+
+def _int(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def _starts(counts):
+    return torch.cumsum(torch.tensor([0] + list(counts)), 0).to(torch.int32).to(DEV)
+
+
+def _heads_like(g, *shape):
+    """Keys or values: each head with its own spread, a few channels wide."""
+    x = torch.randn(shape, generator=g, device=DEV)
+    x *= torch.exp2(torch.rand(shape[-2], 1, generator=g, device=DEV) * 2 - 1)
+    return x * (1 + 3 * (torch.rand(shape[-1], generator=g, device=DEV) < 0.05))
+
+
+def _labels(g, n, m, C):
+    """Given labels; one in sixteen is absent (-1)."""
+    lab = torch.randint(0, C, (n, m), generator=g, device=DEV, dtype=torch.int32)
+    return torch.where(torch.rand((n, m), generator=g, device=DEV) < 1 / 16, -1, lab).to(torch.int32)
+
+
+def prepare(case, seed):
+    g = _rng(seed)
+    kind = case["kind"]
+    s = types.SimpleNamespace(kind=kind, case=case)
+    if kind == "scores":
+        n, C = case["n"], case["C"]
+        buf = torch.randn((n, case["ld"]), generator=g, device=DEV) * 3
+        s.x = buf.to(TYPES[case["dtype"]])[:, :C]
+        # labels that a grammar or a phrase list rules out
+        s.x[:, torch.rand(C, generator=g, device=DEV) < 0.02] = -math.inf
+        s.labels = _labels(g, n, case["m"], C)
+    elif kind == "joint":
+        n, H, C = case["n"], case["H"], case["C"]
+        # activations and weights spread as the synthetic models', on a grid on which every
+        # sum is exact in 32 bits: equal logits are equal whatever the order of their sums
+        a = torch.relu(torch.randn((n, H), generator=g, device=DEV) * math.sqrt(2)).clamp(max=7.75)
+        w = torch.randn((C, H), generator=g, device=DEV).clamp(-4, 4) * 3 / math.sqrt(H)
+        grid = 2.0 ** round(math.log2(3 / math.sqrt(H)) - 5)
+        s.A = (torch.round(a * 16) / 16).to(torch.bfloat16)
+        s.Wt = (torch.round(w / grid) * grid).to(torch.bfloat16)
+        s.labels = _labels(g, n, case["m"], C)
+    else:
+        _prepare_cache(s, case, g)
+    return s
+
+
+def _prepare_cache(s, case, g):
+    append = case["kind"] == "append"
+    dt = TYPES[case["dtype"]]
+    kv, dim, block, n = case["heads"] if append else case["kv"], case["dim"], case["block"], case["n"]
+    past, new = _lengths(case)
+    if append and case["new"] > block:  # a prompt starts on a block
+        past = [p // block * block for p in past]
+    lens = [p + c for p, c in zip(past, new)]
+    s.max_new, s.max_len, s.rows = max(new), max(lens), sum(new)
+    s.window, s.sinks = case.get("window", 0), case.get("sinks", 0)
+    # the block table: blocks that no query sees any more were given back (-1); block 0 stays free
+    width = -(-s.max_len // block)
+    first = [(max(0, p - s.window + 1) if s.window else 0) // block for p in past]
+    keep = [[b * block < s.sinks or f <= b < -(-e // block) for b in range(width)] for f, e in zip(first, lens)]
+    keep = torch.tensor(keep)
+    total = int(keep.sum())
+    ids = torch.randperm(total, generator=g, device=DEV).to(torch.int32) + 1
+    table = torch.full((n, width), -1, dtype=torch.int32, device=DEV)
+    table[keep.to(DEV)] = ids
+    # sequences sit in slots of their own, in another order than the call's
+    s.slots = torch.randperm(n, generator=g, device=DEV).to(torch.int32)
+    s.table = torch.empty_like(table)
+    s.table[s.slots.long()] = table
+    s.lens = torch.empty(n, dtype=torch.int32, device=DEV)
+    s.lens[s.slots.long()] = _int(lens)
+    s.starts = _starts(new)
+    s.n_blocks = total + 1
+    mk = lambda: _heads_like(g, s.n_blocks, block, kv, dim).to(dt).transpose(1, 2)  # noqa: E731
+    if append:
+        s.k8, s.v8 = (torch.zeros((s.n_blocks, kv, block, dim), dtype=torch.int8, device=DEV) for _ in range(2))
+        s.ks, s.vs = (torch.ones((s.n_blocks, kv), device=DEV) for _ in range(2))
+        s.kt, s.vt = (_heads_like(g, n, 2, block, kv, dim).to(dt).transpose(2, 3).contiguous() for _ in range(2))
+        s.k, s.v = (_heads_like(g, s.rows, kv, dim).to(dt) for _ in range(2))
+        s.touched = [e - p // block * block for p, e in zip(past, lens)]  # tokens of the touched blocks
+        s.read_starts, s.read_rows = _starts(s.touched), sum(s.touched)
+    else:
+        s.k8, s.ks = _quantised(mk().float())
+        s.v8, s.vs = _quantised(mk().float())
+        s.kt, s.vt = (torch.zeros((n, 2, kv, block, dim), dtype=dt, device=DEV) for _ in range(2))
+        s.q = torch.randn((s.rows, case["heads"], dim), generator=g, device=DEV).to(dt)
+        s.scale = 1 / math.sqrt(dim)
+    s.cache = None
+    if own:
+        import paper_2609_14991_gb300 as tsd
+
+        s.cache = tsd.KV8Cache(s.k8, s.v8, s.ks, s.vs, s.kt, s.vt)
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(s):
+    if own:
+        return _run_own(s)
+    return {"scores": _plain_scores, "joint": _plain_joint, "append": _plain_append, "attend": _plain_attend}[s.kind](s)
+
+
+def _run_own(s):
+    import paper_2609_14991_gb300 as tsd
+
+    c = s.case
+    if s.kind == "scores":
+        return _answer(tsd.label_scores(s.x, s.labels, k=c["k"], temperature=c["temp"]))
+    if s.kind == "joint":
+        return _answer(tsd.joint_label_scores(s.A, s.Wt, s.labels, k=c["k"], temperature=c["temp"]))
+    if s.kind == "append":
+        s.cache.append(s.k, s.v, s.table, s.lens, starts=s.starts, slots=s.slots, max_new=s.max_new)
+        k, v = s.cache.read(s.table, s.lens, s.read_rows, starts=s.read_starts, slots=s.slots)
+        return {"k": k, "v": v, "k_scale": s.ks, "v_scale": s.vs, "k_tail": s.kt, "v_tail": s.vt}
+    return s.cache.attend(s.q, s.table, s.lens, starts=s.starts, slots=s.slots, scale=s.scale, window=s.window,
+                          sinks=s.sinks, max_new=s.max_new, max_len=s.max_len)
+
+
+def _answer(r):
+    return {"logp": r.logp, "entropy": r.entropy, "alt_labels": r.alt_labels, "alt_logp": r.alt_logp}
+
+
+def _order_keys(x):
+    """int64 keys that order fp32 values, equal ones by descending index."""
+    b = x.view(torch.int32).to(torch.int64)
+    b = torch.where(b < 0, -(b & 0x7FFFFFFF), b)  # -0 and 0 alike
+    return (b << 32) + (x.shape[1] - 1 - torch.arange(x.shape[1], device=x.device))
+
+
+def _plain_rows(x, labels, k, temp):
+    """The scores of fp32 logits, row by row."""
+    y = x / temp
+    top = y.amax(1, keepdim=True)
+    d = y - top
+    e = torch.exp(d)
+    total = e.sum(1, keepdim=True)
+    log_total = torch.log(total)
+    logp = torch.where(labels < 0, 0.0, torch.gather(d, 1, labels.clamp(min=0).long()) - log_total)
+    entropy = log_total[:, 0] - torch.where(e > 0, e * d, 0.0).sum(1) / total[:, 0]
+    kk = min(k, x.shape[1])
+    at = torch.topk(_order_keys(x), kk, dim=1).indices
+    if kk < k:
+        at = torch.nn.functional.pad(at, (0, k - kk))
+    alt = torch.gather(d, 1, at) - log_total
+    alt[:, kk:] = -math.inf
+    return {"logp": logp, "entropy": entropy, "alt_labels": torch.where(alt == -math.inf, -1, at).to(torch.int32),
+            "alt_logp": alt}
+
+
+def _plain_scores(s):
+    return _plain_rows(s.x.float().contiguous(), s.labels, s.case["k"], s.case["temp"])
+
+
+def _plain_joint(s):
+    return _plain_rows(s.A.float() @ s.Wt.float().t(), s.labels, s.case["k"], s.case["temp"])
+
+
+def _quantised(x):
+    """8-bit integers and scales of blocks [.., heads, block, dim] (fp32)."""
+    top = x.abs().amax((-2, -1))
+    scale = torch.clamp(top, min=LEAST) * (1 / 127)  # one product in 32 bits
+    scale = torch.where(top <= MOST, scale, math.nan)
+    # in 64 bits: quotients next to a half
+    q = torch.round(x.double() / scale[..., None, None].double()).clamp(-127, 127)
+    return torch.nan_to_num(q).to(torch.int8), scale
+
+
+def _plain_append(s):
+    c, block = s.case, s.case["block"]
+    slots = s.slots.long()
+    end = s.lens[slots].long()
+    cnt = (s.starts[1:] - s.starts[:-1]).long()
+    base = (end - cnt) // block  # first touched block
+    nb = (block - 1 + s.max_new + block - 1) // block
+    pos = base[:, None] * block + torch.arange(nb * block, device=DEV)
+    live = pos < end[:, None]
+    fresh = pos >= (end - cnt)[:, None]
+    row = (s.starts[:-1, None] + pos - (end - cnt)[:, None]).clamp(0, s.rows - 1)
+    blk = base[:, None] + torch.arange(nb, device=DEV)
+    wanted = blk * block < end[:, None]
+    ids = torch.where(wanted, torch.gather(s.table[slots], 1, blk.clamp(max=s.table.shape[1] - 1)), 0).long()
+    got = []
+    for new, x8, xs, tail in ((s.k, s.k8, s.ks, s.kt), (s.v, s.v8, s.vs, s.vt)):
+        old = tail[slots[:, None], (pos // block) % 2, :, pos % block]
+        x = torch.where(live[..., None, None], torch.where(fresh[..., None, None], new[row], old), 0).float()
+        x = x.view(len(slots), nb, block, *x.shape[2:]).transpose(2, 3)  # [n, nb, heads, block, dim]
+        q, sc = _quantised(x)
+        x8[ids] = torch.where(wanted[..., None, None, None], q, x8[0])
+        xs[ids] = torch.where(wanted[..., None], sc, xs[0])
+        # originals of the new tokens in the last block and the one before it
+        at = end[:, None] - 1 - torch.arange(2 * block, device=DEV)
+        at = torch.where((at >= (end - cnt)[:, None]) & (at // block >= ((end - 1) // block - 1)[:, None]), at,
+                         (end - 1)[:, None])
+        tail[slots[:, None], (at // block) % 2, :, at % block] = new[s.starts[:-1, None] + at - (end - cnt)[:, None]]
+        # the touched blocks' values, packed
+        r = torch.arange(s.read_rows, device=DEV)
+        i = torch.searchsorted(s.read_starts[1:], r, right=True)
+        p = r - s.read_starts[i] + (end - (s.read_starts[1:] - s.read_starts[:-1]))[i]
+        b = s.table[slots[i], p // block].long()
+        got.append(x8[b, :, p % block].float() * xs[b][..., None])
+    return {"k": got[0], "v": got[1], "k_scale": s.ks, "v_scale": s.vs, "k_tail": s.kt, "v_tail": s.vt}
+
+
+def _plain_attend(s):
+    c, block = s.case, s.case["block"]
+    slots = s.slots.long()
+    end = s.lens[slots].long()
+    cnt = (s.starts[1:] - s.starts[:-1]).long()
+    n, kv, g, dim = c["n"], c["kv"], c["heads"] // c["kv"], c["dim"]
+    first = (end - cnt - s.window + 1).clamp(min=0) if s.window else torch.zeros_like(end)
+    span = min(s.max_len, s.window + s.max_new - 1) if s.window else s.max_len
+    j = torch.arange(s.sinks + span, device=DEV)
+    key = torch.where(j < s.sinks, j, first[:, None] + j - s.sinks)  # [n, J]
+    seen = torch.where(j < s.sinks, j < first[:, None], key < end[:, None])
+    key_b = key.clamp(max=s.table.shape[1] * block - 1)
+    b = torch.gather(s.table[slots], 1, key_b // block).clamp(min=0).long()
+    k = s.k8[b, :, key_b % block].float() * s.ks[b][..., None]  # [n, J, kv, dim]
+    v = s.v8[b, :, key_b % block].float() * s.vs[b][..., None]
+    t = torch.arange(s.max_new, device=DEV)
+    row = (s.starts[:-1, None] + t).clamp(max=s.rows - 1)
+    q = s.q[row].float().view(n, s.max_new, kv, g, dim).permute(0, 2, 3, 1, 4).reshape(n, kv, g * s.max_new, dim)
+    att = (q * s.scale) @ k.permute(0, 2, 3, 1)
+    pos = (end - cnt)[:, None] + t
+    see = seen[:, None] & (key[:, None] <= pos[..., None])
+    if s.window:
+        see &= (key[:, None] < s.sinks) | (key[:, None] > pos[..., None] - s.window)
+    att = att.view(n, kv, g, s.max_new, -1).masked_fill_(~see[:, None, None], -math.inf)
+    att -= att.amax(-1, keepdim=True).clamp(min=-3e38)
+    att = att.exp_()
+    att /= att.sum(-1, keepdim=True)
+    out = att.view(n, kv, g * s.max_new, -1) @ v.transpose(1, 2)
+    out = out.view(n, kv, g, s.max_new, dim).permute(0, 3, 1, 2, 4).reshape(n, s.max_new, kv * g, dim)
+    r = torch.arange(s.rows, device=DEV)
+    i = torch.searchsorted(s.starts[1:], r, right=True)
+    return out[i, r - s.starts[i]].to(s.q.dtype)
+
+
+# ---------------------------------------------------------------- what a pass cannot do without
+
+def _visible_pairs(p, c, window, sinks):
+    """(query, key) pairs of a sequence with p tokens before c new ones."""
+    if not window:
+        return c * p + c * (c + 1) // 2
+    t = 0
+    for pos in range(p, p + c):
+        lo = max(0, pos - window + 1)
+        t += pos - lo + 1 + min(sinks, lo)
+    return t
+
+
+def work(case):
+    kind = case["kind"]
+    if kind in ("scores", "joint"):
+        n, m, k, C = case["n"], case["m"], case["k"], case["C"]
+        out = n * (8 * m + 4 + 8 * k)
+        if kind == "scores":
+            return {"bytes": n * C * (4 if case["dtype"] == "fp32" else 2) + out, "flops": 4 * n * C}
+        return {"bytes": 2 * (n + C) * case["H"] + out, "flops": 2 * n * C * case["H"]}
+    past, new = _lengths(case)
+    dim, block = case["dim"], case["block"]
+    if kind == "append":
+        heads = case["heads"]
+        if case["new"] > block:
+            past = [p // block * block for p in past]
+        old = sum(p % block for p in past)
+        touched = sum(p % block + c for p, c in zip(past, new))
+        kept = sum(min(c, block + (p + c - 1) % block + 1) for p, c in zip(past, new))
+        # originals in (new, and those of the open blocks), 8 bits out, values out, originals kept
+        per = 2 * (sum(new) + old) + touched + 4 * touched + 2 * kept
+        return {"bytes": 2 * heads * dim * per, "flops": 4 * heads * dim * touched}
+    w, sk = case["window"], case["sinks"]
+    keys = pairs = 0
+    for p, c in zip(past, new):
+        lo = max(0, p - w + 1) if w else 0
+        keys += p + c - lo + min(sk, lo)
+        pairs += _visible_pairs(p, c, w, sk)
+    return {"bytes": 2 * keys * case["kv"] * dim + 4 * sum(new) * case["heads"] * dim, "flops": 4 * dim * case["heads"] * pairs}
+
+
+# ---------------------------------------------------------------- the definition in 64 bits
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "scores":
+        return _exact_rows(lambda a, b: s.x[a:b].double(), s.labels, case)
+    if kind == "joint":
+        w = s.Wt.double().t().contiguous()
+        return _exact_rows(lambda a, b: s.A[a:b].double() @ w, s.labels, case)
+    return _exact_append(s, case) if kind == "append" else _exact_attend(s, case)
+
+
+def _exact_rows(rows, labels, case):
+    n, m, k, C, temp = case["n"], case["m"], case["k"], case["C"], case["temp"]
+    step = max(1, (1 << 27) // C)
+    out = {"logp": [], "entropy": [], "alt_labels": [], "alt_logp": []}
+    for a in range(0, n, step):
+        x = rows(a, min(n, a + step))
+        lp = torch.log_softmax(x / temp, 1)
+        p = lp.exp()
+        out["entropy"].append(-torch.nan_to_num(p * lp, nan=0.0).sum(1))
+        lab = labels[a:a + step].long()
+        given = torch.take_along_dim(lp, lab.clamp(min=0), 1)
+        out["logp"].append(torch.where(lab < 0, torch.zeros_like(given), given))
+        order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+        lp = torch.take_along_dim(lp, order, 1)
+        pad = (0, k - order.shape[1])
+        lp = torch.nn.functional.pad(lp, pad, value=-math.inf)
+        order = torch.nn.functional.pad(order, pad, value=-1)
+        out["alt_labels"].append(torch.where(torch.isinf(lp), torch.full_like(order, -1), order).to(torch.int32))
+        out["alt_logp"].append(lp)
+    return {name: torch.cat(v) for name, v in out.items()}
+
+
+def _exact_append(s, case):
+    block = case["block"]
+    past, new = _lengths(case)
+    if case["new"] > block:
+        past = [p // block * block for p in past]
+    ks, vs = s.ks.clone(), s.vs.clone()
+    tails = [s.kt.clone(), s.vt.clone()]
+    got = [[], []]
+    slots, at = s.slots.tolist(), 0
+    table = s.table.tolist()
+    for i, slot in enumerate(slots):
+        p, c = past[i], new[i]
+        b0 = p // block
+        for w, (src, sc) in enumerate(((s.k, ks), (s.v, vs))):
+            old = tails[w][slot, b0 % 2, :, :p % block].transpose(0, 1)
+            x = torch.cat([old, src[at:at + c]]).double()  # [tokens, heads, dim] from block b0 on
+            whole = torch.nn.functional.pad(x, (0, 0, 0, 0, 0, -len(x) % block)).view(-1, block, *x.shape[1:])
+            top = whole.abs().amax((1, 3))
+            step = (top.clamp(min=LEAST).float() * (1 / 127)).double()
+            vals = torch.round(whole / step[:, None, :, None]) * step[:, None, :, None]
+            got[w].append(vals.reshape(-1, *x.shape[1:])[:len(x)])
+            sc[torch.tensor(table[slot][b0:b0 + len(whole)], device=DEV)] = step.float()
+            last = (p + c - 1) // block
+            for b in {max(b0, last - 1), last}:  # originals of the new tokens in the last two blocks
+                lo, hi = max(p, b * block), min(p + c, (b + 1) * block)
+                tails[w][slot, b % 2, :, lo - b * block:hi - b * block] = src[at + lo - p:at + hi - p].transpose(0, 1)
+        at += c
+    return {"k": torch.cat(got[0]), "v": torch.cat(got[1]), "k_scale": ks.double(), "v_scale": vs.double(),
+            "k_tail": tails[0].double(), "v_tail": tails[1].double()}
+
+
+def _exact_attend(s, case):
+    block, g = case["block"], case["heads"] // case["kv"]
+    past, new = _lengths(case)
+    slots, table, at, outs = s.slots.tolist(), s.table, 0, []
+    for i, slot in enumerate(slots):
+        p, c = past[i], new[i]
+        key = torch.arange(p + c, device=DEV)
+        if s.window:
+            key = key[(key < s.sinks) | (key > p - s.window)]
+        b = table[slot, key // block].long()
+        see = key[None] <= torch.arange(p, p + c, device=DEV)[:, None]
+        if s.window:
+            see &= (key[None] < s.sinks) | (torch.arange(p, p + c, device=DEV)[:, None] - key[None] < s.window)
+        out = torch.empty((c, case["heads"], case["dim"]), dtype=torch.float64, device=DEV)
+        for h in range(case["kv"]):
+            k = s.k8[b, h, key % block].double() * s.ks[b, h, None].double()
+            v = s.v8[b, h, key % block].double() * s.vs[b, h, None].double()
+            for j in range(h * g, (h + 1) * g):
+                a = torch.where(see, s.q[at:at + c, j].double() @ k.t() / math.sqrt(case["dim"]), -math.inf)
+                out[:, j] = torch.softmax(a, 1) @ v
+        outs.append(out)
+        at += c
+    return torch.cat(outs)
