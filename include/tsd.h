@@ -568,6 +568,142 @@ TSD_API tsd_status tsd_encoder_gemm_flops(const tsd_encoder* enc, int32_t n, int
  * [1, max_streams] x [1, max_chunk]. */
 TSD_API tsd_status tsd_encoder_launches_per_chunk(const tsd_encoder* enc, int32_t n, int32_t C, int64_t* launches);
 
+/* ------------------------------------------------------------------------
+ * Scores of labels (no counterpart in the paper: the numbers a caller needs
+ * around the decode -- how sure the model was of a label, what else it
+ * considered, how well a given transcript fits).
+ *
+ * For each of n rows of C logits x and a temperature T, with y = x / T and
+ * lse = log sum_i exp(y_i):
+ *   logp        float [n][m]: y_l - lse of each given label l = labels[row][j]
+ *               (int32 [n][m]); label -1 stands for none and gives 0, any
+ *               other label outside [0, C) gives NaN.  0 <= m <= 8;
+ *   entropy     float [n] (NULL: not computed): -sum_i p_i log p_i in nats,
+ *               p = exp(y - lse);
+ *   alt_labels, alt_logp  int32 and float [n][k]: the k largest logits'
+ *               labels in descending order (equal ones by ascending label)
+ *               and their y - lse.  0 <= k <= 8.
+ * A logit of -inf masks its label: probability 0, never an alternative
+ * (alternatives that do not exist are label -1 with -inf).  In a row whose
+ * labels are all masked every log probability is -inf and the entropy 0.  A
+ * row with a NaN or +inf logit has NaN scores and entropy, and alternatives
+ * -1 with NaN.  All sums are fp32.
+ * All pointers are device memory; asynchronous on cuda_stream; nothing is
+ * allocated, so the calls can be captured into a graph. */
+
+/* Element types of the operators below. */
+#define TSD_F32 0
+#define TSD_BF16 1
+#define TSD_F16 2
+
+/* From logits in memory: n rows of C elements of type dtype, row_stride
+ * elements apart (any alignment of the element type).  1 <= n <= 2^30,
+ * 1 <= C <= 262144, row_stride >= C (or n = 1), temperature > 0 and finite.  A
+ * row's results are the same bits whatever else is in the call. */
+TSD_API tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits, int32_t dtype, int64_t row_stride,
+                                    float temperature, int32_t m, const int32_t* labels, int32_t k, float* logp,
+                                    float* entropy, int32_t* alt_labels, float* alt_logp, void* cuda_stream);
+
+/* From a joint network's input rows: x = A[row] . Wt[label] (bf16 in, fp32
+ * accumulate on the tensor cores); the logits are not stored.
+ *   A   bf16 [n][H], rows a_stride elements apart;
+ *   Wt  bf16 [C][H] (W_out label-major), rows w_stride elements apart;
+ * both 16-byte aligned with strides a multiple of 8.  H a multiple of 64 in
+ * [64, 8192], 1 <= n <= 2^24, 1 <= C <= 262144.  workspace: device memory of
+ * at least tsd_joint_label_scores_workspace() bytes, 16-byte aligned, used
+ * only by this call's kernels (calls that may overlap need one each).
+ * TSD_EINVAL if it is too small. */
+TSD_API tsd_status tsd_joint_label_scores_workspace(int32_t n, int32_t H, int32_t C, int32_t m, int32_t k,
+                                                    int64_t* bytes);
+TSD_API tsd_status tsd_joint_label_scores(int32_t n, int32_t H, int32_t C, const void* A_bf16, int64_t a_stride,
+                                          const void* Wt_bf16, int64_t w_stride, float temperature, int32_t m,
+                                          const int32_t* labels, int32_t k, float* logp, float* entropy,
+                                          int32_t* alt_labels, float* alt_logp, void* workspace,
+                                          int64_t workspace_bytes, void* cuda_stream);
+
+/* ------------------------------------------------------------------------
+ * Attention over a paged cache held in 8 bits (a neural LM or an attention
+ * decoder beside the n-gram LMs; the paper has no counterpart).
+ *
+ * The cache of one layer: blocks of `block` tokens, each with one scale per
+ * head for its keys and one for its values.  All memory is the caller's.
+ *   k, v             int8 [n_blocks][kv_heads][block][dim]
+ *   k_scale, v_scale float [n_blocks][kv_heads]; a stored q stands for q * scale
+ *   k_tail, v_tail   dtype [n_slots][2][kv_heads][block][dim]: the unrounded
+ *                    keys and values of a slot's last token's block b and of the
+ *                    block before it, at [slot][b % 2]
+ * A block and head's scale is a * (1/127) (one fp32 product with the rounded
+ * reciprocal), a the largest magnitude among its tokens, at least 2^-32;
+ * q = x / scale, the exact quotient rounded to nearest even.  While a block is filling it is
+ * rounded again from the unrounded tokens, so what a sequence's blocks hold does not depend
+ * on how its tokens were split into calls.  A block and head with a NaN, an
+ * infinity or a magnitude above 2^60 gets scale NaN: every query that sees
+ * one of its tokens has a NaN result for the heads that read it. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  void *k_tail, *v_tail;
+  int32_t dtype;    /* TSD_BF16 or TSD_F16: tails, new keys and values, queries, results */
+  int32_t n_blocks; /* blocks of the pool */
+  int32_t kv_heads; /* 1..1024 */
+  int32_t block;    /* tokens per block: 16, 32 or 64 */
+  int32_t dim;      /* head dimension: 64 or 128 */
+  int32_t n_slots;  /* sequence slots */
+} tsd_kv8;
+
+/* The sequences of a call (device arrays).  Sequence i of n lives in slot
+ * s = slots[i] (slots NULL: s = i); it holds lens[s] tokens, those of this
+ * call included; token p is in block table[s][p / block].  Rows
+ * starts[i] .. starts[i+1] of the call's row arrays are its last tokens, in
+ * order (starts NULL: one row each; rows = n).  Rows behind the last
+ * sequence's are not read or written.  A sequence whose slot, length or rows
+ * are out of range (lens[s] > table_width * block, more rows than tokens, rows
+ * outside [0, rows)) is not appended, and its rows inside [0, rows) read or
+ * attend as NaN.  A block id outside [0, n_blocks) is not written and reads
+ * as NaN; ids of blocks that no query sees are not read, so blocks that left
+ * a window can be given back. */
+typedef struct {
+  int32_t n;            /* 1..65535 */
+  const int32_t* slots;  /* [n] or NULL */
+  const int32_t* lens;   /* [n_slots] */
+  const int32_t* table;  /* [n_slots][table_width] */
+  int32_t table_width;
+  const int32_t* starts; /* [n + 1] or NULL */
+  int32_t rows;          /* rows of the row arrays, 1..2^22 */
+  int32_t max_new;       /* most rows of a sequence, and most tokens of one: both only */
+  int32_t max_len;       /* size launches (0: unknown); results do not depend on them being right */
+} tsd_kv8_batch;
+
+/* Appends the rows of keys and values (kv_heads x dim each; row and head
+ * strides in elements, a multiple of 8, 16-byte aligned).  lens counts the new tokens already.
+ * Slots are distinct, and no block is another sequence's in the same call. */
+TSD_API tsd_status tsd_kv8_append(const tsd_kv8* cache, const tsd_kv8_batch* batch, const void* k, int64_t k_row,
+                                  int64_t k_head, const void* v, int64_t v_row, int64_t v_head, void* cuda_stream);
+
+/* The values that the cache holds for the rows' tokens: k_out, v_out float
+ * [rows][kv_heads][dim], 16-byte aligned. */
+TSD_API tsd_status tsd_kv8_read(const tsd_kv8* cache, const tsd_kv8_batch* batch, float* k_out, float* v_out,
+                                void* cuda_stream);
+
+/* Causal attention of the rows' queries over their sequences' cached tokens:
+ * with k, v the values that the cache holds,
+ *   out[row][h] = sum_j p_j v_j,  p = softmax_j(scale * q[row][h] . k_j)
+ * over the tokens j that token pos sees: j <= pos, and with window > 0 only
+ * j > pos - window or j < sinks (the first `sinks` tokens stay visible).
+ * heads: query heads, a multiple of kv_heads, at most 64 per kv head and 1024; query
+ * head h reads kv head h / (heads / kv_heads).  q and out: row and head
+ * strides in elements, a multiple of 8, 16-byte aligned; out may not overlap q.
+ * Products take fp16 operands (queries scaled by a power of two per row, the
+ * 8-bit integers as they are, probabilities rounded to fp16) and accumulate in
+ * fp32, as do the softmax's statistics.  workspace: device memory of at least
+ * tsd_kv8_attend_workspace() bytes (may be 0), 16-byte aligned, for this call alone. */
+TSD_API tsd_status tsd_kv8_attend_workspace(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads,
+                                            int32_t window, int32_t sinks, int64_t* bytes);
+TSD_API tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads, const void* q,
+                                  int64_t q_row, int64_t q_head, float scale, int32_t window, int32_t sinks, void* out,
+                                  int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
+                                  void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -62,6 +62,17 @@ class EncoderLayerC(ctypes.Structure):
     _fields_ = [(n, _vp) for n in _ENC_LAYER_FIELDS]
 
 
+class KV8C(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("k_tail", _vp), ("v_tail", _vp),
+                ("dtype", _i32), ("n_blocks", _i32), ("kv_heads", _i32), ("block", _i32), ("dim", _i32),
+                ("n_slots", _i32)]
+
+
+class KV8BatchC(ctypes.Structure):
+    _fields_ = [("n", _i32), ("slots", _vp), ("lens", _vp), ("table", _vp), ("table_width", _i32), ("starts", _vp),
+                ("rows", _i32), ("max_new", _i32), ("max_len", _i32)]
+
+
 SIGNATURES = {
     "tsd_last_error": ([], ctypes.c_char_p),
     "tsd_version": ([], ctypes.c_char_p),
@@ -114,6 +125,15 @@ SIGNATURES = {
     "tsd_encoder_timing": ([_vp, _vp, _vp, _i32, _i32], _i32),
     "tsd_encoder_gemm_flops": ([_vp, _i32, _i32, _P(ctypes.c_double)], _i32),
     "tsd_encoder_launches_per_chunk": ([_vp, _i32, _i32, _P(_i64)], _i32),
+    "tsd_label_scores": ([_i32, _i32, _vp, _i32, _i64, _f32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp], _i32),
+    "tsd_joint_label_scores_workspace": ([_i32, _i32, _i32, _i32, _i32, _P(_i64)], _i32),
+    "tsd_joint_label_scores": ([_i32, _i32, _i32, _vp, _i64, _vp, _i64, _f32, _i32, _vp, _i32, _vp, _vp, _vp, _vp, _vp,
+                                _i64, _vp], _i32),
+    "tsd_kv8_append": ([_P(KV8C), _P(KV8BatchC), _vp, _i64, _i64, _vp, _i64, _i64, _vp], _i32),
+    "tsd_kv8_read": ([_P(KV8C), _P(KV8BatchC), _vp, _vp, _vp], _i32),
+    "tsd_kv8_attend_workspace": ([_P(KV8C), _P(KV8BatchC), _i32, _i32, _i32, _P(_i64)], _i32),
+    "tsd_kv8_attend": ([_P(KV8C), _P(KV8BatchC), _i32, _vp, _i64, _i64, _f32, _i32, _i32, _vp, _i64, _i64, _vp, _i64,
+                        _vp], _i32),
 }
 
 _lib = None
@@ -632,3 +652,299 @@ class Encoder:
         x = _i64()
         _check(lib().tsd_encoder_launches_per_chunk(self.h, int(n), int(C), ctypes.byref(x)))
         return x.value
+
+
+# ---------------------------------------------------------------- scores of labels
+
+def _dtype_code(t) -> int:
+    """The library's number of a tensor's element type; -1 for others."""
+    import torch
+
+    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype, -1)
+
+
+def _device_tensor(who, name, t, dev):
+    if not t.is_cuda or t.device.index != dev:
+        raise ValueError(f"{who}: {name} must be a CUDA tensor on the current device")
+
+
+class _On:
+    """Allocates on the stream that a call runs on (None: the current one), so
+    that the caching allocator does not hand the memory on too early."""
+
+    def __init__(self, stream):
+        self.ctx = None
+        if stream is not None:
+            import torch
+
+            self.ctx = torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *a):
+        if self.ctx is not None:
+            self.ctx.__exit__(*a)
+
+
+class LabelScores:
+    """logp [n, m], entropy [n] (float32), alt_labels [n, k] (int32) and
+    alt_logp [n, k] (float32) of one call."""
+
+    __slots__ = ("logp", "entropy", "alt_labels", "alt_logp")
+
+    def __init__(self, logp, entropy, alt_labels, alt_logp):
+        self.logp, self.entropy, self.alt_labels, self.alt_logp = logp, entropy, alt_labels, alt_logp
+
+
+def _label_args(who, n, labels, k, out, dev, stream):
+    """(labels, m, LabelScores): the given labels checked, the outputs checked or allocated."""
+    import torch
+
+    m = 0
+    if labels is not None:
+        if labels.dtype != torch.int32 or labels.dim() not in (1, 2) or labels.shape[0] != n:
+            raise ValueError(f"{who}: labels must be int32 [{n}] or [{n}, m]")
+        _device_tensor(who, "labels", labels, dev)
+        if not labels.is_contiguous():
+            raise ValueError(f"{who}: labels must be contiguous")
+        m = labels.shape[1] if labels.dim() == 2 else 1
+    if not 0 <= k <= 8 or m > 8:
+        raise ValueError(f"{who}: at most 8 given labels and 8 alternatives")
+    shape = (n,) if labels is not None and labels.dim() == 1 else (n, m)
+    if out is None:
+        with _On(stream):
+            f = torch.empty(n * (m + 1 + 2 * k), dtype=torch.float32, device=torch.device("cuda", dev))
+        # one allocation, four parts
+        a, b, c = n * m, n * (m + 1), n * (m + 1 + k)
+        out = LabelScores(f[:a].view(shape), f[a:b], f[b:c].view(torch.int32).view(n, k), f[c:].view(n, k))
+    else:
+        for name, t, dt, want in (("logp", out.logp, torch.float32, shape), ("entropy", out.entropy, torch.float32, (n,)),
+                                  ("alt_labels", out.alt_labels, torch.int32, (n, k)),
+                                  ("alt_logp", out.alt_logp, torch.float32, (n, k))):
+            if t.dtype != dt or tuple(t.shape) != want or not t.is_contiguous():
+                raise ValueError(f"{who}: out.{name} must be contiguous {dt} {list(want)}")
+            _device_tensor(who, f"out.{name}", t, dev)
+    return m, out
+
+
+def label_scores(logits, labels=None, k: int = 0, temperature: float = 1.0, out: Optional[LabelScores] = None,
+                 stream=None) -> LabelScores:
+    """Log probabilities of given labels, entropy and the k most likely labels
+    of rows of logits (``tsd_label_scores``).  logits: cuda float32, bfloat16 or
+    float16 [n, C], any row stride; -inf masks a label.  labels: cuda int32 [n]
+    or [n, m], -1 for none."""
+    import torch
+
+    who = "label_scores"
+    if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
+        raise ValueError(f"{who}: logits must be [n, C]")
+    code = _dtype_code(logits)
+    if code < 0:
+        raise ValueError(f"{who}: logits must be float32, bfloat16 or float16")
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    _device_tensor(who, "logits", logits, dev)
+    n, C = logits.shape
+    if (C > 1 and logits.stride(1) != 1) or (n > 1 and logits.stride(0) < C):
+        raise ValueError(f"{who}: a row's logits must be adjacent and rows must not overlap")
+    m, out = _label_args(who, n, labels, k, out, dev, stream)
+    _check(lib().tsd_label_scores(n, C, logits.data_ptr(), code, logits.stride(0), temperature, m,
+                                  labels.data_ptr() if m else None, k, out.logp.data_ptr() if m else None,
+                                  out.entropy.data_ptr(), out.alt_labels.data_ptr() if k else None,
+                                  out.alt_logp.data_ptr() if k else None, _stream(stream)))
+    return out
+
+
+def joint_label_scores(A, Wt, labels=None, k: int = 0, temperature: float = 1.0, out: Optional[LabelScores] = None,
+                       stream=None) -> LabelScores:
+    """The same of the logits A . Wt^T, which stay on the chip
+    (``tsd_joint_label_scores``): A cuda bf16 [n, H], the joint network's input
+    rows; Wt cuda bf16 (or int16 bit patterns) [C, H], W_out label-major.  Row
+    strides a multiple of 8, H of 64."""
+    import torch
+
+    who = "joint_label_scores"
+    if A.dim() != 2 or A.dtype != torch.bfloat16 or A.shape[0] < 1:
+        raise ValueError(f"{who}: A must be bf16 [n, H]")
+    n, H = A.shape
+    if Wt.dim() != 2 or Wt.dtype not in (torch.bfloat16, torch.int16) or Wt.shape[1] != H or Wt.shape[0] < 1:
+        raise ValueError(f"{who}: Wt must be bf16 [C, H] with H = {H}")
+    C = Wt.shape[0]
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for name, t in (("A", A), ("Wt", Wt)):
+        _device_tensor(who, name, t, dev)
+        if t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < H):
+            raise ValueError(f"{who}: a row of {name} must be adjacent and rows must not overlap")
+    m, out = _label_args(who, n, labels, k, out, dev, stream)
+    need = _i64()
+    L = lib()
+    _check(L.tsd_joint_label_scores_workspace(n, H, C, m, k, ctypes.byref(need)))
+    with _On(stream):
+        ws = torch.empty(need.value, dtype=torch.uint8, device=A.device)
+    _check(L.tsd_joint_label_scores(n, H, C, A.data_ptr(), A.stride(0), Wt.data_ptr(), Wt.stride(0), temperature, m,
+                                    labels.data_ptr() if m else None, k, out.logp.data_ptr() if m else None,
+                                    out.entropy.data_ptr(), out.alt_labels.data_ptr() if k else None,
+                                    out.alt_logp.data_ptr() if k else None, ws.data_ptr(), need.value,
+                                    _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- the 8-bit cache
+
+class KV8Cache:
+    """One layer's paged cache of keys and values in 8 bits (``tsd_kv8``), over
+    tensors of the caller's (``KV8Cache.empty`` makes them):
+
+      k, v              int8 [n_blocks, kv_heads, block, dim]
+      k_scale, v_scale  float32 [n_blocks, kv_heads]
+      k_tail, v_tail    bf16 or fp16 [n_slots, 2, kv_heads, block, dim]: the
+                        unrounded tokens of each slot's last two blocks
+
+    The calls take the same arrays: table int32 [n_slots, width] (block ids),
+    lens int32 [n_slots] (tokens, the call's own included), slots int32 [n] (the
+    sequences; None: slots 0 .. n-1) and starts int32 [n + 1] (their rows; None:
+    one row each).  max_new and max_len bound a sequence's rows and tokens; they
+    size launches only.  Everything is read on the device, so a call captured
+    into a graph can be replayed with other lengths, tables and rows."""
+
+    def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail):
+        import torch
+
+        if k.dim() != 4 or k.dtype != torch.int8:
+            raise ValueError("KV8Cache: k must be int8 [n_blocks, kv_heads, block, dim]")
+        n_blocks, heads, block, dim = k.shape
+        code = _dtype_code(k_tail)
+        if code not in (1, 2) or k_tail.dim() != 5 or k_tail.shape[1:] != (2, heads, block, dim):
+            raise ValueError(f"KV8Cache: k_tail must be bf16 or fp16 [n_slots, 2, {heads}, {block}, {dim}]")
+        if block not in (16, 32, 64) or dim not in (64, 128):
+            raise ValueError("KV8Cache: block is 16, 32 or 64 and dim 64 or 128")
+        n_slots = k_tail.shape[0]
+        named = {"k": (k, k), "v": (v, k), "k_scale": (k_scale, None), "v_scale": (v_scale, None),
+                 "k_tail": (k_tail, k_tail), "v_tail": (v_tail, k_tail)}
+        for name, (t, like) in named.items():
+            if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+                raise ValueError(f"KV8Cache: {name} must be {like.dtype} {list(like.shape)}")
+            if like is None and (t.dtype != torch.float32 or tuple(t.shape) != (n_blocks, heads)):
+                raise ValueError(f"KV8Cache: {name} must be float32 [{n_blocks}, {heads}]")
+            if not t.is_cuda or t.device != k.device:
+                raise ValueError(f"KV8Cache: {name} must be a CUDA tensor on k's device")
+            if not t.is_contiguous():
+                raise ValueError(f"KV8Cache: {name} must be contiguous")
+        self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail = k, v, k_scale, v_scale, k_tail, v_tail
+        self.dtype, self.device = k_tail.dtype, k.device
+        self.n_blocks, self.kv_heads, self.block, self.dim, self.n_slots = n_blocks, heads, block, dim, n_slots
+        self._c = KV8C(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(),
+                       v_tail.data_ptr(), code, n_blocks, heads, block, dim, n_slots)
+
+    @classmethod
+    def empty(cls, n_blocks: int, n_slots: int, kv_heads: int, dim: int, block: int = 32, dtype=None, device=None):
+        """A cache over new tensors (zeros, scales 1) on the current device."""
+        import torch
+
+        dtype = dtype or torch.bfloat16
+        device = device or torch.device("cuda", torch.cuda.current_device())
+        z = lambda *s, dt: torch.zeros(s, dtype=dt, device=device)  # noqa: E731
+        one = lambda: torch.ones((n_blocks, kv_heads), dtype=torch.float32, device=device)  # noqa: E731
+        return cls(z(n_blocks, kv_heads, block, dim, dt=torch.int8), z(n_blocks, kv_heads, block, dim, dt=torch.int8),
+                   one(), one(), z(n_slots, 2, kv_heads, block, dim, dt=dtype),
+                   z(n_slots, 2, kv_heads, block, dim, dt=dtype))
+
+    def _batch(self, who, table, lens, starts, slots, rows, max_new, max_len):
+        import torch
+
+        i32 = torch.int32
+        if torch.cuda.current_device() != self.device.index:
+            raise ValueError(f"{who}: the cache is on another device than the current one")
+        if table.dtype != i32 or table.dim() != 2 or table.shape[0] != self.n_slots or not table.is_contiguous():
+            raise ValueError(f"{who}: table must be contiguous int32 [{self.n_slots}, width]")
+        if lens.dtype != i32 or lens.dim() != 1 or lens.shape[0] != self.n_slots or not lens.is_contiguous():
+            raise ValueError(f"{who}: lens must be contiguous int32 [{self.n_slots}]")
+        n = None
+        if slots is not None:
+            if slots.dtype != i32 or slots.dim() != 1 or not slots.is_contiguous():
+                raise ValueError(f"{who}: slots must be contiguous int32 [n]")
+            n = slots.shape[0]
+        if starts is not None:
+            if starts.dtype != i32 or starts.dim() != 1 or not starts.is_contiguous() or starts.shape[0] < 2:
+                raise ValueError(f"{who}: starts must be contiguous int32 [n + 1]")
+            if n is not None and starts.shape[0] != n + 1:
+                raise ValueError(f"{who}: starts must have {n + 1} entries")
+            n = starts.shape[0] - 1
+        if n is None:
+            n = rows
+        for t in (table, lens, slots, starts):
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{who}: table, lens, slots and starts must be on the cache's device")
+        return KV8BatchC(n, slots.data_ptr() if slots is not None else None, lens.data_ptr(), table.data_ptr(),
+                         table.shape[1], starts.data_ptr() if starts is not None else None, rows, max_new or 0,
+                         max_len or 0)
+
+    def _rows(self, who, name, t, heads=None):
+        if t.dim() != 3 or t.dtype != self.dtype or t.shape[2] != self.dim or (heads and t.shape[1] != heads):
+            raise ValueError(f"{who}: {name} must be {self.dtype} [rows, {heads or 'heads'}, {self.dim}]")
+        if t.device != self.device:
+            raise ValueError(f"{who}: {name} must be on the cache's device")
+        if t.stride(2) != 1:
+            raise ValueError(f"{who}: {name}'s last dimension must be adjacent")
+
+    def append(self, k, v, table, lens, starts=None, slots=None, max_new: Optional[int] = None, stream=None):
+        """Appends rows of keys and values [rows, kv_heads, dim] (``tsd_kv8_append``)."""
+        who = "KV8Cache.append"
+        self._rows(who, "k", k, self.kv_heads)
+        self._rows(who, "v", v, self.kv_heads)
+        if k.shape != v.shape:
+            raise ValueError(f"{who}: k and v must have the same rows")
+        b = self._batch(who, table, lens, starts, slots, k.shape[0], max_new, None)
+        _check(lib().tsd_kv8_append(ctypes.byref(self._c), ctypes.byref(b), k.data_ptr(), k.stride(0), k.stride(1),
+                                    v.data_ptr(), v.stride(0), v.stride(1), _stream(stream)))
+
+    def read(self, table, lens, rows: int, starts=None, slots=None, out=None, stream=None):
+        """(k, v) float32 [rows, kv_heads, dim]: the values held for the rows'
+        tokens (``tsd_kv8_read``)."""
+        import torch
+
+        who = "KV8Cache.read"
+        b = self._batch(who, table, lens, starts, slots, rows, None, None)
+        shape = (rows, self.kv_heads, self.dim)
+        if out is None:
+            with _On(stream):
+                out = (torch.empty(shape, dtype=torch.float32, device=self.device),
+                       torch.empty(shape, dtype=torch.float32, device=self.device))
+        for t in out:
+            if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                raise ValueError(f"{who}: out must be two contiguous float32 {list(shape)} on the cache's device")
+        _check(lib().tsd_kv8_read(ctypes.byref(self._c), ctypes.byref(b), out[0].data_ptr(), out[1].data_ptr(),
+                                  _stream(stream)))
+        return out
+
+    def attend(self, q, table, lens, starts=None, slots=None, scale: Optional[float] = None, window: int = 0,
+               sinks: int = 0, out=None, max_new: Optional[int] = None, max_len: Optional[int] = None, stream=None):
+        """Causal attention of queries [rows, heads, dim] over the cached tokens
+        (``tsd_kv8_attend``): window > 0 limits a token's sight to the last
+        `window` tokens and the first `sinks`.  scale: 1 / sqrt(dim) if None."""
+        import torch
+
+        who = "KV8Cache.attend"
+        self._rows(who, "q", q)
+        rows, heads = q.shape[0], q.shape[1]
+        b = self._batch(who, table, lens, starts, slots, rows, max_new, max_len)
+        L = lib()
+        need = _i64()
+        _check(L.tsd_kv8_attend_workspace(ctypes.byref(self._c), ctypes.byref(b), heads, window, sinks,
+                                          ctypes.byref(need)))
+        ws = None
+        if out is None or need.value:
+            with _On(stream):
+                if out is None:
+                    out = torch.empty((rows, heads, self.dim), dtype=self.dtype, device=self.device)
+                if need.value:
+                    ws = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        self._rows(who, "out", out, heads)
+        if out.shape[0] != rows:
+            raise ValueError(f"{who}: out must have {rows} rows")
+        _check(L.tsd_kv8_attend(ctypes.byref(self._c), ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
+                                self.dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
+                                out.stride(0), out.stride(1), ws.data_ptr() if ws is not None else None, need.value,
+                                _stream(stream)))
+        return out

@@ -1,0 +1,534 @@
+// Attention over the 8-bit paged cache with few query rows per key head: single
+// tokens and short chunks (tsd.h: tsd_kv8_attend).
+//
+// The rows of a sequence and key head are its new tokens times the query heads
+// that share the head (row = token * group + head of the group).  16 rows are one
+// tile of mma.sync.m16n8k16 (fp16 in, fp32 out): the keys and values are
+// read once for all of them.  Four warps of a CTA share the work as MW row
+// tiles x 4 / MW key groups; a long context is split over CTAs too
+// (partial results in the workspace, joined by k_kv8_join).
+//
+// Mathematics, per row: with integers k_j, v_j, scales a_b, c_b of key j's block b and
+// the row's factor f (queries are scaled by f, a power of two, into fp16),
+//   s_j = (q f . k_j) (scale log2(e) a_b / f) + log2(c_b),   m = max_j s_j,
+//   out = sum_j 2^(s_j - m) v_j  /  sum_j 2^(s_j - m) / c_b,
+// so a value's scale is an addend of the exponent and the integers go into the
+// products as they are (exact in fp16, as is every query within 2^28 of its
+// row's largest).  Probabilities are rounded to fp16 (half a step 2^-12), as
+// multiples of 2^(m - 7): down to 2^-31 of the largest they are not flushed.  The maximum
+// follows only when a score passes it by more than 2^8, which fp16 still holds:
+// most tiles need no exchange between lanes.
+//
+// Layout: a tile is 16 tokens of one block and head, 16 x dim contiguous
+// bytes: one untiled bulk copy for its keys and one for its values into a ring of
+// stages per key group.  A product over the head dimension may take the
+// dimensions in any order, and so may one over keys: lane (g, t) of a warp takes 16
+// consecutive bytes of key g as its part of four k-steps, and 16 consecutive
+// dimensions of keys 2t, 2t+1, 2t+8, 2t+9 as its part of 16 column tiles, so
+// nothing is transposed.  Integers become fp16 by placing the byte (offset by 128)
+// in the mantissa of 1024 and subtracting 1152: both exact.
+#include <algorithm>
+
+#include "kv8_attend.h"
+#include "tc_common.cuh"
+
+namespace tsd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 16;  // keys per tile
+
+template <int DIM, int MW>
+struct RowsShape {
+  static constexpr int kKeyGroups = 4 / MW;
+  static constexpr int kStages = MW == 1 ? 4 : 8;
+  static constexpr int kStageBytes = 2 * kTile * DIM;
+  static constexpr int kRing = kKeyGroups * kStages * kStageBytes;
+  static constexpr int kOutStride = DIM + 4;
+  static constexpr int kOut = 64 * kOutStride * 4;  // four warps' 16 rows
+  static constexpr int kBarOff = kRing > kOut ? kRing : kOut;
+  static constexpr int kSmem = kBarOff + kKeyGroups * kStages * 16 + 64 * 8;
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+template <bool BF16>
+__device__ __forceinline__ float wide16(uint32_t u) {
+  if (BF16) return __uint_as_float(u << 16);
+  return __half2float(__ushort_as_half((unsigned short)u));
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+  if (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The key tiles that rows at positions pos0 .. pos1 see: first those of the
+// sinks before the window, then the window's.
+struct KeyTiles {
+  int sink, from, total;  // sink tiles 0 .. sink-1, then tiles from, from + 1, ..
+  __device__ __forceinline__ int token(int j) const { return kTile * (j < sink ? j : from + j - sink); }
+};
+__device__ __forceinline__ KeyTiles key_tiles(int pos0, int pos1, int window, int sinks) {
+  const int first = window > 0 ? max(0, pos0 - window + 1) : 0;
+  KeyTiles k;
+  k.sink = (min(sinks, first) + kTile - 1) / kTile;
+  k.from = max(k.sink, first / kTile);
+  k.total = k.sink + pos1 / kTile + 1 - k.from;
+  return k;
+}
+
+template <bool BF16, int DIM, int MW>
+__global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Attend a) {
+  using S = RowsShape<DIM, MW>;
+  constexpr int KW = S::kKeyGroups, ST = S::kStages;
+  constexpr int kSteps = DIM / 16;  // k-steps of the scores' product
+  constexpr int kCols = DIM / 8;    // column tiles of the values' product
+  extern __shared__ __align__(128) unsigned char smem[];
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBarOff);
+  float2* s_ml = reinterpret_cast<float2*>(bars + 2 * KW * ST);  // [64] (max, sum) of the warps' rows
+  float* s_out = reinterpret_cast<float*>(smem);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int mw = warp % MW, kg = warp / MW;
+  const int head = blockIdx.y % a.c.kv_heads, mt0 = blockIdx.y / a.c.kv_heads, mts = gridDim.y / a.c.kv_heads;
+  const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
+  const int rows = q.count * a.group;
+  if (mt0 * 16 * MW >= rows) return;
+  uint64_t* full = bars + kg * ST;
+  uint64_t* empty = bars + KW * ST + kg * ST;
+  unsigned char* ring = smem + kg * ST * S::kStageBytes;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < KW * ST; ++i) {
+      mbar_init(bars + i, 1);
+      mbar_init(bars + KW * ST + i, MW);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  int it0 = 0;  // tiles that this key group has taken so far (the ring's position)
+  bool dead = false;  // a wait of this CTA ran out: NaN for its rows from there on
+
+  for (int mt = mt0; mt * 16 * MW < rows; mt += mts) {
+    const int r0 = mt * 16 * MW + mw * 16;  // this warp's first row
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    float o[kCols][4];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+
+    if (q.ok && !dead) {
+      const int before = q.len - q.count;
+      const int last_row = min(rows, (mt + 1) * 16 * MW) - 1;
+      const KeyTiles tiles = key_tiles(before + mt * 16 * MW / a.group, before + last_row / a.group, a.window, a.sinks);
+      const int lo = (int)((int64_t)tiles.total * blockIdx.x / gridDim.x), hi = (int)((int64_t)tiles.total * (blockIdx.x + 1) / gridDim.x);
+      const int n = hi - lo > kg ? (hi - lo - kg + KW - 1) / KW : 0;  // this key group's tiles lo + kg + i KW
+      // the queries' fragments
+      uint32_t qf[kSteps][4];
+      float rc[2];
+      int pos[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int r = r0 + g + 8 * h, tok = r / a.group;
+        pos[h] = before + min(tok, q.count - 1);
+        uint2 w[kSteps];
+        float top = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          w[kk] = make_uint2(0, 0);
+          if (r < rows)
+            w[kk] = __ldg(reinterpret_cast<const uint2*>(a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + r % a.group) * a.q_head +
+                                                         64 * (kk >> 2) + 16 * t + 4 * (kk & 3)));
+        }
+        bool odd = false;  // a NaN, which the maximum would pass over
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          const float x0 = fabsf(wide16<BF16>(w[kk].x & 0xffffu)), x1 = fabsf(wide16<BF16>(w[kk].x >> 16));
+          const float x2 = fabsf(wide16<BF16>(w[kk].y & 0xffffu)), x3 = fabsf(wide16<BF16>(w[kk].y >> 16));
+          top = fmaxf(fmaxf(top, fmaxf(x0, x1)), fmaxf(x2, x3));
+          odd = odd || !(x0 + x1 + x2 + x3 <= INFINITY);
+        }
+        top = odd ? INFINITY : top;
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // f brings the row's largest magnitude into [2^14, 2^15)
+        const int ex = (int)(__float_as_uint(top) >> 23);
+        const bool fine = ex < 255;
+        const int fe = fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127;
+        const float f = __uint_as_float((uint32_t)fe << 23);
+        rc[h] = fine ? a.scale * kLog2e / f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          qf[kk][h] = narrow2<false>(wide16<BF16>(w[kk].x & 0xffffu) * f, wide16<BF16>(w[kk].x >> 16) * f);
+          qf[kk][2 + h] = narrow2<false>(wide16<BF16>(w[kk].y & 0xffffu) * f, wide16<BF16>(w[kk].y >> 16) * f);
+        }
+      }
+      // positions that every row of this warp sees
+      const int all_to = before + min(r0, rows - 1) / a.group;                                             // the first row's
+      const int all_from = a.window > 0 ? before + min(r0 + 15, rows - 1) / a.group - a.window + 1 : 0;  // the last row's window
+
+      const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
+      const auto block_of = [&](int i) {  // of the key group's tile i; -1 outside the pool
+        const int id = __ldg(table + tiles.token(lo + kg + i * KW) / a.c.block);
+        return id < a.c.n_blocks ? id : -1;
+      };
+      int ids = 0;  // lane j: the block of issued tile (i & ~31) + j
+      const auto issue = [&](int i) {
+        if ((i & 31) == 0) ids = i + lane < n ? block_of(i + lane) : -1;
+        const int id = __shfl_sync(0xffffffffu, ids, i & 31);
+        if (lane == 0) {
+          const int at = it0 + i, st = at % ST;
+          // a wait that runs out leaves a stage that nothing is copied into: its consumers' waits run out too
+          if (at < ST || mbar_wait(empty + st, (uint32_t)(at / ST - 1) & 1u)) {
+            if (id >= 0) {
+              const size_t off = (((size_t)id * a.c.kv_heads + head) * a.c.block + tiles.token(lo + kg + i * KW) % a.c.block) * DIM;
+              mbar_expect_tx(full + st, S::kStageBytes);
+              bulk_g2s(ring + st * S::kStageBytes, static_cast<const int8_t*>(a.c.k) + off, kTile * DIM, full + st);
+              bulk_g2s(ring + st * S::kStageBytes + kTile * DIM, static_cast<const int8_t*>(a.c.v) + off, kTile * DIM, full + st);
+            } else {
+              mbar_arrive(full + st);
+            }
+          }
+        }
+        __syncwarp();
+      };
+      if (mw == 0)
+        for (int i = 0; i < min(n, ST - 1); ++i) issue(i);
+      float a_b = 0.f, lc_b = 0.f, ic_b = 0.f;  // lane j: scales of tile (i & ~31) + j
+      bool expired = false;
+      for (int i = 0; i < n; ++i) {
+        if ((i & 31) == 0) {
+          const int id = i + lane < n ? block_of(i + lane) : -1;
+          const float nan = __uint_as_float(0x7fc00000u);
+          a_b = id >= 0 ? __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head) : nan;
+          const float c = id >= 0 ? __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head) : nan;
+          const float cs = c == 0.f ? 0x1p-80f : c;  // a scale of 0 stands for values of 0, of their weight all the same
+          lc_b = log2f(cs);
+          ic_b = 1.f / cs;
+        }
+        if (mw == 0 && i + ST - 1 < n) issue(i + ST - 1);
+        const int at = it0 + i, st = at % ST;
+        if (!mbar_wait(full + st, (uint32_t)(at / ST) & 1u)) {
+          // what is still in flight lands before anything reuses the ring
+          for (int j = at + 1; j < min(it0 + n, at + ST); ++j) mbar_wait(full + j % ST, (uint32_t)(j / ST) & 1u);
+          expired = true;
+          break;
+        }
+        const unsigned char* kt = ring + st * S::kStageBytes;
+        const unsigned char* vt = kt + kTile * DIM;
+        // scores: two column tiles of eight keys
+        float s[2][4];
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+          for (int u = 0; u < DIM / 64; ++u) {
+            const uint4 x = *reinterpret_cast<const uint4*>(kt + (nt * 8 + g) * DIM + 64 * u + 16 * t);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t y = w[j] ^ 0x80808080u;
+              mma16816(s[nt], qf[4 * u + j], int_half2(__byte_perm(y, 0x64646464u, 0x4140)), int_half2(__byte_perm(y, 0x64646464u, 0x4342)));
+            }
+          }
+        }
+        const int tok0 = tiles.token(lo + kg + i * KW);
+        const float ab = __shfl_sync(0xffffffffu, a_b, i & 31), lc = __shfl_sync(0xffffffffu, lc_b, i & 31), ic = __shfl_sync(0xffffffffu, ic_b, i & 31);
+        float top[2] = {-INFINITY, -INFINITY};
+        const bool whole = tok0 + kTile - 1 <= all_to && (tok0 >= all_from || tok0 + kTile <= a.sinks);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float c = rc[h] * ab;
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float v = fmaf(s[nt][2 * h + e], c, lc);
+              if (!whole) {
+                const int key = tok0 + nt * 8 + 2 * t + e;
+                const bool see = key <= pos[h] && (a.window <= 0 || key > pos[h] - a.window || key < a.sinks);
+                v = see ? v : -INFINITY;
+              }
+              s[nt][2 * h + e] = v;
+              top[h] = fmaxf(top[h], v);
+            }
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float x = fmaxf(m[h], top[h]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            const float w = x == m[h] ? 1.f : ex2_approx(m[h] - x);
+            m[h] = x;
+            l[h] *= w;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+              o[j][2 * h] *= w;
+              o[j][2 * h + 1] *= w;
+            }
+          }
+        }
+        uint32_t p[4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float ref = m[h] == -INFINITY ? 0.f : m[h] - 7.f;
+          float sum = 0.f;
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            const float x = ex2_approx(s[nt][2 * h] - ref), y = ex2_approx(s[nt][2 * h + 1] - ref);
+            sum += x + y;
+            p[2 * nt + h] = narrow2<false>(x, y);
+          }
+          if (sum != 0.f) l[h] = fmaf(sum, ic, l[h]);  // a block that the row does not see may have a NaN scale
+        }
+        // values: keys 2t, 2t+1, 2t+8, 2t+9 of 16 (8) dimensions
+        constexpr int kW = DIM / 32;  // words per key
+        uint32_t v[4][kW];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const unsigned char* src = vt + (2 * t + (j & 1) + 8 * (j >> 1)) * DIM + (DIM / 8) * g;
+          if constexpr (DIM == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(src);
+            v[j][0] = x.x, v[j][1] = x.y, v[j][2] = x.z, v[j][3] = x.w;
+          } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(src);
+            v[j][0] = x.x, v[j][1] = x.y;
+          }
+        }
+        // the stage has been read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty + st);
+#pragma unroll
+        for (int w = 0; w < kW; ++w) {
+          const uint32_t x0 = v[0][w] ^ 0x80808080u, x1 = v[1][w] ^ 0x80808080u, y0 = v[2][w] ^ 0x80808080u, y1 = v[3][w] ^ 0x80808080u;
+          const uint32_t xl = __byte_perm(x0, x1, 0x5140), xh = __byte_perm(x0, x1, 0x7362);
+          const uint32_t yl = __byte_perm(y0, y1, 0x5140), yh = __byte_perm(y0, y1, 0x7362);
+          mma16816(o[4 * w], p, int_half2(__byte_perm(xl, 0x64646464u, 0x4140)), int_half2(__byte_perm(yl, 0x64646464u, 0x4140)));
+          mma16816(o[4 * w + 1], p, int_half2(__byte_perm(xl, 0x64646464u, 0x4342)), int_half2(__byte_perm(yl, 0x64646464u, 0x4342)));
+          mma16816(o[4 * w + 2], p, int_half2(__byte_perm(xh, 0x64646464u, 0x4140)), int_half2(__byte_perm(yh, 0x64646464u, 0x4140)));
+          mma16816(o[4 * w + 3], p, int_half2(__byte_perm(xh, 0x64646464u, 0x4342)), int_half2(__byte_perm(yh, 0x64646464u, 0x4342)));
+        }
+      }
+      dead = __any_sync(0xffffffffu, expired);
+      if (dead) {  // the rows say NaN
+        l[0] = l[1] = __uint_as_float(0x7fc00000u);
+        m[0] = m[1] = 0.f;
+      }
+      it0 += n;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
+        l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
+      }
+    } else if (kg == 0 && (dead || blockIdx.x == 0)) {
+      m[0] = m[1] = 0.f;
+      l[0] = l[1] = __uint_as_float(0x7fc00000u);
+    }
+
+    // join the key groups through shared memory (the ring's: every stage has been read)
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = warp * 16 + g + 8 * h;
+      if (t == 0) s_ml[r] = make_float2(m[h], l[h]);
+      // column tile j, column c: dimension c (DIM / 8) + j; this lane has columns 2t and 2t + 1
+      float* dst = s_out + r * S::kOutStride + (DIM / 4) * t;
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int j = 0; j < kCols; j += 4)
+          *reinterpret_cast<float4*>(dst + e * kCols + j) = make_float4(o[j][2 * h + e], o[j + 1][2 * h + e], o[j + 2][2 * h + e], o[j + 3][2 * h + e]);
+    }
+    __syncthreads();
+    constexpr int kOct = DIM / 8;
+    for (int e = threadIdx.x; e < 16 * MW * kOct; e += 128) {
+      const int row = e / kOct, col = 8 * (e % kOct), r = mt * 16 * MW + row;
+      if (r >= rows) break;
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * 16 * MW + row].x);
+      float acc[8] = {}, sum = 0.f;
+#pragma unroll
+      for (int k = 0; k < KW; ++k) {
+        const float2 ml = s_ml[k * 16 * MW + row];
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;
+        const float w = ml.x == -INFINITY ? 1.f : ex2_approx(ml.x - top);
+        sum = fmaf(w, ml.y, sum);
+        const float* src = s_out + (k * 16 * MW + row) * S::kOutStride + col;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, src[j], acc[j]);
+      }
+      const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
+      if (gridDim.x == 1) {
+        const float inv = 1.f / sum;
+        uint4 y;
+        y.x = narrow2<BF16>(acc[0] * inv, acc[1] * inv);
+        y.y = narrow2<BF16>(acc[2] * inv, acc[3] * inv);
+        y.z = narrow2<BF16>(acc[4] * inv, acc[5] * inv);
+        y.w = narrow2<BF16>(acc[6] * inv, acc[7] * inv);
+        *reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + col) = y;
+      } else {
+        const size_t at = ((size_t)blockIdx.x * a.b.rows + tok) * a.heads + h;
+        float4* dst = reinterpret_cast<float4*>(a.part + at * DIM + col);
+        dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+        if (col == 0) a.part_ml[at] = make_float2(top, sum);
+      }
+    }
+    fence_async_smem();
+    dead = __syncthreads_or(dead);  // then the ring is written again
+  }
+}
+
+// Joins the splits' partial results: one warp per row and query head, lane = DIM / 32 dimensions.
+template <bool BF16, int DIM>
+__global__ void __launch_bounds__(128) k_kv8_join(const __grid_constant__ Kv8Attend a, int splits) {
+  const size_t at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const size_t items = (size_t)a.b.rows * a.heads;
+  if (at >= items) return;
+  const int tok = (int)(at / a.heads), h = (int)(at % a.heads);
+  if (a.b.starts && (tok < __ldg(a.b.starts) || tok >= __ldg(a.b.starts + a.b.n))) return;
+  float top = -INFINITY;
+  for (int s = lane; s < splits; s += 32) top = fmaxf(top, a.part_ml[s * items + at].x);
+#pragma unroll
+  for (int i = 16; i; i >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, i));
+  constexpr int kN = DIM / 32;
+  float acc[kN] = {}, sum = 0.f;
+  for (int s = 0; s < splits; ++s) {
+    const float2 ml = a.part_ml[s * items + at];
+    if (ml.x == -INFINITY && ml.y == 0.f) continue;
+    const float w = ml.x == -INFINITY ? 1.f : ex2_approx(ml.x - top);
+    sum = fmaf(w, ml.y, sum);
+    const float* src = a.part + (s * items + at) * DIM + kN * lane;
+#pragma unroll
+    for (int j = 0; j < kN; ++j) acc[j] = fmaf(w, src[j], acc[j]);
+  }
+  const float inv = 1.f / sum;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + kN * lane);
+#pragma unroll
+  for (int j = 0; j < kN; j += 2) dst[j / 2] = narrow2<BF16>(acc[j] * inv, acc[j + 1] * inv);
+}
+
+template <bool BF16, int DIM, int MW>
+cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t s) {
+  using S = RowsShape<DIM, MW>;
+  static const cudaError_t e = cudaFuncSetAttribute(k_kv8_rows<BF16, DIM, MW>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return e;
+  k_kv8_rows<BF16, DIM, MW><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, S::kSmem, s>>>(a);
+  return cudaGetLastError();
+}
+
+template <bool BF16, int DIM>
+cudaError_t launch_mw(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
+  cudaError_t e = p.mw == 1 ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
+                : p.mw == 2 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
+                            : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
+  if (e == cudaSuccess && p.splits > 1) {
+    const size_t items = (size_t)a.b.rows * a.heads;
+    k_kv8_join<BF16, DIM><<<(unsigned)((items + 3) / 4), 128, 0, s>>>(a, p.splits);
+    e = cudaGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int window, int sinks, int sms) {
+  Kv8RowsPlan p;
+  const int group = heads / c.kv_heads;
+  const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
+  const int64_t rows = (int64_t)most * group;
+  p.mw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int64_t mtiles = (rows + 16 * p.mw - 1) / (16 * p.mw);
+  p.mtiles = (int)std::min<int64_t>(mtiles, std::max(1, 65535 / c.kv_heads));
+  const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);
+  const int64_t keys = window > 0 ? std::min<int64_t>(cap, (int64_t)window + sinks + most) : cap;
+  const int64_t tiles = (keys + kTile - 1) / kTile;
+  // CTAs wanted: three per SM and a few rounds of them, so that ragged lengths even out; each with two tiles at least
+  // per warp
+  const int64_t units = (int64_t)b.n * c.kv_heads * p.mtiles;
+  const int64_t want = ((int64_t)sms * 6 + units - 1) / units;
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, tiles / (2 * 4 / p.mw), 64}));
+  p.bytes = p.splits > 1 ? (int64_t)p.splits * b.rows * heads * (c.dim + 2) * 4 : 0;
+  return p;
+}
+
+cudaError_t kv8_rows_launch(Kv8Attend a, const Kv8RowsPlan& p, void* workspace, cudaStream_t s) {
+  a.part = static_cast<float*>(workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part + (p.splits > 1 ? (size_t)p.splits * a.b.rows * a.heads * a.c.dim : 0));
+  const bool bf = a.c.dtype == TSD_BF16;
+  if (a.c.dim == 64) return bf ? launch_mw<true, 64>(a, p, s) : launch_mw<false, 64>(a, p, s);
+  return bf ? launch_mw<true, 128>(a, p, s) : launch_mw<false, 128>(a, p, s);
+}
+
+}  // namespace tsd
+
+using namespace tsd;
+
+static tsd_status attend_check(const char* who, const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads, int32_t window, int32_t sinks) {
+  if (tsd_status st = kv8_check(who, cache, batch)) return st;
+  if (heads < 1 || heads % cache->kv_heads || heads / cache->kv_heads > 64)
+    return fail(TSD_EINVAL, "%s: heads=%d must be 1..64 times kv_heads=%d", who, heads, cache->kv_heads);
+  if (heads > 1024) return fail(TSD_EINVAL, "%s: heads=%d above 1024", who, heads);
+  if (window < 0 || sinks < 0) return fail(TSD_EINVAL, "%s: negative window=%d or sinks=%d", who, window, sinks);
+  return TSD_OK;
+}
+
+static tsd_status device_sms(int* sms) {
+  int dev = 0;
+  TSD_CUDA(cudaGetDevice(&dev));
+  TSD_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  return TSD_OK;
+}
+
+extern "C" tsd_status tsd_kv8_attend_workspace(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads,
+                                               int32_t window, int32_t sinks, int64_t* bytes) {
+  clear_error();
+  if (!bytes) return fail(TSD_EINVAL, "tsd_kv8_attend_workspace: NULL argument");
+  if (tsd_status st = attend_check("tsd_kv8_attend_workspace", cache, batch, heads, window, sinks)) return st;
+  int sms = 0;
+  if (tsd_status st = device_sms(&sms)) return st;
+  *bytes = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms).bytes;
+  return TSD_OK;
+}
+
+extern "C" tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads, const void* q,
+                                     int64_t q_row, int64_t q_head, float scale, int32_t window, int32_t sinks, void* out,
+                                     int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
+                                     void* cuda_stream) {
+  clear_error();
+  if (tsd_status st = attend_check("tsd_kv8_attend", cache, batch, heads, window, sinks)) return st;
+  if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "q", q, q_row, q_head)) return st;
+  if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "out", out, out_row, out_head)) return st;
+  int sms = 0;
+  if (tsd_status st = device_sms(&sms)) return st;
+  const Kv8RowsPlan p = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms);
+  if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
+    return fail(TSD_EINVAL, "tsd_kv8_attend: workspace of %lld bytes, %lld needed (16-byte aligned)", (long long)workspace_bytes, (long long)p.bytes);
+  Kv8Attend a{};
+  a.c = *cache;
+  a.b = *batch;
+  a.q = static_cast<const uint16_t*>(q);
+  a.out = static_cast<uint16_t*>(out);
+  a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
+  a.heads = heads;
+  a.group = heads / cache->kv_heads;
+  a.window = window;
+  a.sinks = sinks;
+  a.scale = scale;
+  TSD_CUDA(kv8_rows_launch(a, p, workspace, static_cast<cudaStream_t>(cuda_stream)));
+  return TSD_OK;
+}

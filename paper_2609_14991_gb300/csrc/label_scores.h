@@ -1,0 +1,67 @@
+// Scores of labels: what its two forms (scores.cu, joint_scores.cu) share.
+#pragma once
+
+#include "internal.h"
+
+namespace tsd {
+
+constexpr int kMaxGiven = 8;  // given labels per row
+constexpr int kMaxAlt = 8;    // alternatives per row
+
+struct LabelArgs {
+  int m, k;
+  const int32_t* labels;
+  float *logp, *entropy;
+  int32_t* alt_labels;
+  float* alt_logp;
+  float inv_temp;
+};
+
+// A row's sums: m its largest logit, S = sum 2^d, E = sum 2^d d with d =
+// (x - m) log2(e) / T (m = 0 in the exponents of a row without finite logits).
+struct RowSums {
+  float m, S, E;
+  // NaN or +inf among the logits: the sums are NaN, as inf - inf is
+  __device__ __forceinline__ bool odd() const { return !(S >= 0.f) || m == INFINITY; }
+};
+
+// max that keeps NaN
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// y - lse of a logit of the row
+__device__ __forceinline__ float label_logp(const RowSums& r, float inv_temp, float x) {
+  if (r.odd()) return __uint_as_float(0x7fc00000u);
+  if (r.m == -INFINITY) return x == -INFINITY ? x : __uint_as_float(0x7fc00000u);
+  return (x - r.m) * inv_temp - logf(r.S);
+}
+
+// The given labels' scores and the entropy, by one warp; logit(l): the row's
+// logit of label l >= 0 (NaN outside its labels).
+template <class F>
+__device__ __forceinline__ void label_finish(const LabelArgs& a, int64_t row, const RowSums& r, int lane, F logit) {
+  if (lane < a.m) {
+    const int l = a.labels[row * a.m + lane];
+    float y = __uint_as_float(0x7fc00000u);
+    if (l == -1) y = 0.f;
+    else if (l >= 0) y = label_logp(r, a.inv_temp, logit(l));
+    a.logp[row * a.m + lane] = y;
+  }
+  if (lane == 0 && a.entropy)
+    a.entropy[row] = r.odd() ? __uint_as_float(0x7fc00000u) : r.m == -INFINITY ? 0.f : fmaxf(0.f, logf(r.S) - 0.693147180559945f * (r.E / r.S));
+}
+
+// Alternative j: the logit and label found (-inf: none).
+__device__ __forceinline__ void label_alternative(const LabelArgs& a, int64_t row, int j, const RowSums& r, float x, int label) {
+  const bool none = r.odd() || !(x > -INFINITY);
+  a.alt_labels[row * a.k + j] = none ? -1 : label;
+  a.alt_logp[row * a.k + j] = r.odd() ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : label_logp(r, a.inv_temp, x);
+}
+
+tsd_status label_check(const char* who, int32_t n, int32_t most_n, int32_t C, float temperature, int32_t m,
+                       const int32_t* labels, int32_t k, const float* logp, const int32_t* alt_labels, const float* alt_logp);
+
+}  // namespace tsd
