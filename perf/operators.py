@@ -220,6 +220,7 @@ def _prepare_cache(s, case, g):
     if own:
         import paper_2609_14991_gb300 as tsd
 
+        s.k8, s.v8 = s.k8.contiguous(), s.v8.contiguous()  # the cache's own layout
         s.cache = tsd.KV8Cache(s.k8, s.v8, s.ks, s.vs, s.kt, s.vt)
 
 
