@@ -656,41 +656,62 @@ class Encoder:
 
 # ---------------------------------------------------------------- scores of labels
 
+# What a short call spends on the host is mostly attribute look-ups and small
+# tensors: the calls below fetch each once, make their outputs in one allocation
+# and remember a shape's workspace size.
+
+_DTYPE = None  # element type -> the library's number
+
+
 def _dtype_code(t) -> int:
     """The library's number of a tensor's element type; -1 for others."""
+    global _DTYPE
+    if _DTYPE is None:
+        import torch
+
+        _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+    return _DTYPE.get(t.dtype, -1)
+
+
+def _on_current(who, name, t):
+    """The current device's index, which t has to be on."""
     import torch
 
-    return {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype, -1)
-
-
-def _device_tensor(who, name, t, dev):
-    if not t.is_cuda or t.device.index != dev:
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
         raise ValueError(f"{who}: {name} must be a CUDA tensor on the current device")
+    return dev
 
 
-class _On:
-    """Allocates on the stream that a call runs on (None: the current one), so
-    that the caching allocator does not hand the memory on too early."""
+def _raw_stream(stream, dev) -> int:
+    import torch
 
-    def __init__(self, stream):
-        self.ctx = None
-        if stream is not None:
-            import torch
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
-            self.ctx = torch.cuda.stream(stream)
 
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+def _empty(n, dtype, dev, stream):
+    """n elements that the caching allocator gives out for the call's stream."""
+    import torch
 
-    def __exit__(self, *a):
-        if self.ctx is not None:
-            self.ctx.__exit__(*a)
+    if stream is None:
+        return torch.empty(n, dtype=dtype, device=dev)
+    with torch.cuda.stream(stream):
+        return torch.empty(n, dtype=dtype, device=dev)
+
+
+_sizes = {}  # workspace bytes by call shape
+
+
+def _remember(key, bytes_):
+    if len(_sizes) > 4096:
+        _sizes.clear()
+    _sizes[key] = bytes_
+    return bytes_
 
 
 class LabelScores:
-    """logp [n, m], entropy [n] (float32), alt_labels [n, k] (int32) and
-    alt_logp [n, k] (float32) of one call."""
+    """Results of one call: logp [n, m] (or [n]), entropy [n], alt_logp [n, k]
+    (float32) and alt_labels [n, k] (int32)."""
 
     __slots__ = ("logp", "entropy", "alt_labels", "alt_logp")
 
@@ -699,34 +720,48 @@ class LabelScores:
 
 
 def _label_args(who, n, labels, k, out, dev, stream):
-    """(labels, m, LabelScores): the given labels checked, the outputs checked or allocated."""
+    """(m, LabelScores, addresses of labels, logp, entropy, alt_labels,
+    alt_logp): the given labels checked, the outputs checked or allocated."""
     import torch
 
-    m = 0
+    m, shape, lp = 0, (n, 0), None
     if labels is not None:
-        if labels.dtype != torch.int32 or labels.dim() not in (1, 2) or labels.shape[0] != n:
+        shape = tuple(labels.shape)
+        if labels.dtype != torch.int32 or len(shape) not in (1, 2) or shape[0] != n:
             raise ValueError(f"{who}: labels must be int32 [{n}] or [{n}, m]")
-        _device_tensor(who, "labels", labels, dev)
+        if labels.get_device() != dev:
+            raise ValueError(f"{who}: labels must be a CUDA tensor on the current device")
         if not labels.is_contiguous():
             raise ValueError(f"{who}: labels must be contiguous")
-        m = labels.shape[1] if labels.dim() == 2 else 1
+        m = shape[1] if len(shape) == 2 else 1
+        lp = labels.data_ptr() if m else None
     if not 0 <= k <= 8 or m > 8:
         raise ValueError(f"{who}: at most 8 given labels and 8 alternatives")
-    shape = (n,) if labels is not None and labels.dim() == 1 else (n, m)
     if out is None:
-        with _On(stream):
-            f = torch.empty(n * (m + 1 + 2 * k), dtype=torch.float32, device=torch.device("cuda", dev))
-        # one allocation, four parts
-        a, b, c = n * m, n * (m + 1), n * (m + 1 + k)
-        out = LabelScores(f[:a].view(shape), f[a:b], f[b:c].view(torch.int32).view(n, k), f[c:].view(n, k))
-    else:
-        for name, t, dt, want in (("logp", out.logp, torch.float32, shape), ("entropy", out.entropy, torch.float32, (n,)),
-                                  ("alt_labels", out.alt_labels, torch.int32, (n, k)),
-                                  ("alt_logp", out.alt_logp, torch.float32, (n, k))):
-            if t.dtype != dt or tuple(t.shape) != want or not t.is_contiguous():
-                raise ValueError(f"{who}: out.{name} must be contiguous {dt} {list(want)}")
-            _device_tensor(who, f"out.{name}", t, dev)
-    return m, out
+        # one buffer: logp, entropy, the alternatives' scores and labels
+        buf = _empty(n * (m + 1 + 2 * k), torch.float32, dev, stream)
+        p, at = buf.data_ptr(), n * (m + 1)
+        part = buf.as_strided
+        res = LabelScores(part(shape, (m, 1) if len(shape) == 2 else (1,), 0), part((n,), (1,), n * m),
+                          buf.view(torch.int32).as_strided((n, k), (k, 1), at + n * k), part((n, k), (k, 1), at))
+        return m, res, lp, p if m else None, p + 4 * n * m, p + 4 * (at + n * k) if k else None, p + 4 * at if k else None
+    for name, t, dt, want in (("logp", out.logp, torch.float32, shape), ("entropy", out.entropy, torch.float32, (n,)),
+                              ("alt_labels", out.alt_labels, torch.int32, (n, k)),
+                              ("alt_logp", out.alt_logp, torch.float32, (n, k))):
+        if t.dtype != dt or tuple(t.shape) != want or not t.is_contiguous():
+            raise ValueError(f"{who}: out.{name} must be contiguous {dt} {list(want)}")
+        if t.get_device() != dev:
+            raise ValueError(f"{who}: out.{name} must be a CUDA tensor on the current device")
+    return (m, out, lp, out.logp.data_ptr() if m else None, out.entropy.data_ptr(),
+            out.alt_labels.data_ptr() if k else None, out.alt_logp.data_ptr() if k else None)
+
+
+def _row_stride(who, name, t, shape):
+    """The distance of a matrix's rows, each of which is adjacent."""
+    s0, s1 = t.stride()
+    if (s1 != 1 and shape[1] > 1) or (s0 < shape[1] and shape[0] > 1):
+        raise ValueError(f"{who}: a row of {name} must be adjacent and rows must not overlap")
+    return s0
 
 
 def label_scores(logits, labels=None, k: int = 0, temperature: float = 1.0, out: Optional[LabelScores] = None,
@@ -735,25 +770,21 @@ def label_scores(logits, labels=None, k: int = 0, temperature: float = 1.0, out:
     of rows of logits (``tsd_label_scores``).  logits: cuda float32, bfloat16 or
     float16 [n, C], any row stride; -inf masks a label.  labels: cuda int32 [n]
     or [n, m], -1 for none."""
-    import torch
-
     who = "label_scores"
-    if logits.dim() != 2 or logits.shape[0] < 1 or logits.shape[1] < 1:
+    shape = logits.shape
+    if len(shape) != 2 or shape[0] < 1 or shape[1] < 1:
         raise ValueError(f"{who}: logits must be [n, C]")
     code = _dtype_code(logits)
     if code < 0:
         raise ValueError(f"{who}: logits must be float32, bfloat16 or float16")
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    _device_tensor(who, "logits", logits, dev)
-    n, C = logits.shape
-    if (C > 1 and logits.stride(1) != 1) or (n > 1 and logits.stride(0) < C):
-        raise ValueError(f"{who}: a row's logits must be adjacent and rows must not overlap")
-    m, out = _label_args(who, n, labels, k, out, dev, stream)
-    _check(lib().tsd_label_scores(n, C, logits.data_ptr(), code, logits.stride(0), temperature, m,
-                                  labels.data_ptr() if m else None, k, out.logp.data_ptr() if m else None,
-                                  out.entropy.data_ptr(), out.alt_labels.data_ptr() if k else None,
-                                  out.alt_logp.data_ptr() if k else None, _stream(stream)))
-    return out
+    dev = _on_current(who, "logits", logits)
+    ld = _row_stride(who, "logits", logits, shape)
+    m, res, lab, logp, ent, alt, altp = _label_args(who, shape[0], labels, k, out, dev, stream)
+    st = lib().tsd_label_scores(shape[0], shape[1], logits.data_ptr(), code, ld, temperature, m, lab, k, logp, ent, alt,
+                                altp, _raw_stream(stream, dev))
+    if st:
+        _check(st)
+    return res
 
 
 def joint_label_scores(A, Wt, labels=None, k: int = 0, temperature: float = 1.0, out: Optional[LabelScores] = None,
@@ -765,29 +796,31 @@ def joint_label_scores(A, Wt, labels=None, k: int = 0, temperature: float = 1.0,
     import torch
 
     who = "joint_label_scores"
-    if A.dim() != 2 or A.dtype != torch.bfloat16 or A.shape[0] < 1:
+    sa, sw = A.shape, Wt.shape
+    if len(sa) != 2 or A.dtype != torch.bfloat16 or sa[0] < 1:
         raise ValueError(f"{who}: A must be bf16 [n, H]")
-    n, H = A.shape
-    if Wt.dim() != 2 or Wt.dtype not in (torch.bfloat16, torch.int16) or Wt.shape[1] != H or Wt.shape[0] < 1:
+    n, H = sa
+    if len(sw) != 2 or Wt.dtype not in (torch.bfloat16, torch.int16) or sw[1] != H or sw[0] < 1:
         raise ValueError(f"{who}: Wt must be bf16 [C, H] with H = {H}")
-    C = Wt.shape[0]
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for name, t in (("A", A), ("Wt", Wt)):
-        _device_tensor(who, name, t, dev)
-        if t.stride(1) != 1 or (t.shape[0] > 1 and t.stride(0) < H):
-            raise ValueError(f"{who}: a row of {name} must be adjacent and rows must not overlap")
-    m, out = _label_args(who, n, labels, k, out, dev, stream)
-    need = _i64()
+    C = sw[0]
+    dev = _on_current(who, "A", A)
+    if Wt.get_device() != dev:
+        raise ValueError(f"{who}: Wt must be a CUDA tensor on the current device")
+    lda, ldw = _row_stride(who, "A", A, sa), _row_stride(who, "Wt", Wt, sw)
+    m, res, lab, logp, ent, alt, altp = _label_args(who, n, labels, k, out, dev, stream)
     L = lib()
-    _check(L.tsd_joint_label_scores_workspace(n, H, C, m, k, ctypes.byref(need)))
-    with _On(stream):
-        ws = torch.empty(need.value, dtype=torch.uint8, device=A.device)
-    _check(L.tsd_joint_label_scores(n, H, C, A.data_ptr(), A.stride(0), Wt.data_ptr(), Wt.stride(0), temperature, m,
-                                    labels.data_ptr() if m else None, k, out.logp.data_ptr() if m else None,
-                                    out.entropy.data_ptr(), out.alt_labels.data_ptr() if k else None,
-                                    out.alt_logp.data_ptr() if k else None, ws.data_ptr(), need.value,
-                                    _stream(stream)))
-    return out
+    key = (dev, n, H, C, m, k)
+    need = _sizes.get(key)
+    if need is None:
+        b = _i64()
+        _check(L.tsd_joint_label_scores_workspace(n, H, C, m, k, ctypes.byref(b)))
+        need = _remember(key, b.value)
+    ws = _empty(need, torch.uint8, dev, stream)
+    st = L.tsd_joint_label_scores(n, H, C, A.data_ptr(), lda, Wt.data_ptr(), ldw, temperature, m, lab, k, logp, ent, alt,
+                                  altp, ws.data_ptr(), need, _raw_stream(stream, dev))
+    if st:
+        _check(st)
+    return res
 
 
 # ---------------------------------------------------------------- the 8-bit cache
@@ -834,8 +867,10 @@ class KV8Cache:
         self.k, self.v, self.k_scale, self.v_scale, self.k_tail, self.v_tail = k, v, k_scale, v_scale, k_tail, v_tail
         self.dtype, self.device = k_tail.dtype, k.device
         self.n_blocks, self.kv_heads, self.block, self.dim, self.n_slots = n_blocks, heads, block, dim, n_slots
+        self._dev = k.get_device()
         self._c = KV8C(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k_tail.data_ptr(),
                        v_tail.data_ptr(), code, n_blocks, heads, block, dim, n_slots)
+        self._pc = ctypes.byref(self._c)
 
     @classmethod
     def empty(cls, n_blocks: int, n_slots: int, kv_heads: int, dim: int, block: int = 32, dtype=None, device=None):
@@ -853,51 +888,54 @@ class KV8Cache:
     def _batch(self, who, table, lens, starts, slots, rows, max_new, max_len):
         import torch
 
-        i32 = torch.int32
-        if torch.cuda.current_device() != self.device.index:
+        i32, dev = torch.int32, self._dev
+        if torch.cuda.current_device() != dev:
             raise ValueError(f"{who}: the cache is on another device than the current one")
-        if table.dtype != i32 or table.dim() != 2 or table.shape[0] != self.n_slots or not table.is_contiguous():
-            raise ValueError(f"{who}: table must be contiguous int32 [{self.n_slots}, width]")
-        if lens.dtype != i32 or lens.dim() != 1 or lens.shape[0] != self.n_slots or not lens.is_contiguous():
-            raise ValueError(f"{who}: lens must be contiguous int32 [{self.n_slots}]")
-        n = None
+        ts, n_slots = table.shape, self.n_slots
+        if table.dtype != i32 or len(ts) != 2 or ts[0] != n_slots or not table.is_contiguous():
+            raise ValueError(f"{who}: table must be contiguous int32 [{n_slots}, width]")
+        if lens.dtype != i32 or lens.shape != (n_slots,) or not lens.is_contiguous():
+            raise ValueError(f"{who}: lens must be contiguous int32 [{n_slots}]")
+        n, ps, pt = rows, None, None
         if slots is not None:
             if slots.dtype != i32 or slots.dim() != 1 or not slots.is_contiguous():
                 raise ValueError(f"{who}: slots must be contiguous int32 [n]")
-            n = slots.shape[0]
+            n, ps = slots.shape[0], slots.data_ptr()
         if starts is not None:
             if starts.dtype != i32 or starts.dim() != 1 or not starts.is_contiguous() or starts.shape[0] < 2:
                 raise ValueError(f"{who}: starts must be contiguous int32 [n + 1]")
-            if n is not None and starts.shape[0] != n + 1:
+            if slots is not None and starts.shape[0] != n + 1:
                 raise ValueError(f"{who}: starts must have {n + 1} entries")
-            n = starts.shape[0] - 1
-        if n is None:
-            n = rows
-        for t in (table, lens, slots, starts):
-            if t is not None and t.device != self.device:
-                raise ValueError(f"{who}: table, lens, slots and starts must be on the cache's device")
-        return KV8BatchC(n, slots.data_ptr() if slots is not None else None, lens.data_ptr(), table.data_ptr(),
-                         table.shape[1], starts.data_ptr() if starts is not None else None, rows, max_new or 0,
-                         max_len or 0)
+            n, pt = starts.shape[0] - 1, starts.data_ptr()
+        if (table.get_device() != dev or lens.get_device() != dev or (ps is not None and slots.get_device() != dev)
+                or (pt is not None and starts.get_device() != dev)):
+            raise ValueError(f"{who}: table, lens, slots and starts must be on the cache's device")
+        return KV8BatchC(n, ps, lens.data_ptr(), table.data_ptr(), ts[1], pt, rows, max_new or 0, max_len or 0)
 
     def _rows(self, who, name, t, heads=None):
-        if t.dim() != 3 or t.dtype != self.dtype or t.shape[2] != self.dim or (heads and t.shape[1] != heads):
-            raise ValueError(f"{who}: {name} must be {self.dtype} [rows, {heads or 'heads'}, {self.dim}]")
-        if t.device != self.device:
+        """(rows, heads, distance of rows, distance of heads) of [rows, heads, dim]."""
+        s = t.shape
+        if len(s) != 3 or t.dtype != self.dtype or s[2] != self.dim or (heads is not None and s[1] != heads):
+            raise ValueError(f"{who}: {name} must be {self.dtype} [rows, {'heads' if heads is None else heads}, {self.dim}]")
+        if t.get_device() != self._dev:
             raise ValueError(f"{who}: {name} must be on the cache's device")
-        if t.stride(2) != 1:
+        d = t.stride()
+        if d[2] != 1:
             raise ValueError(f"{who}: {name}'s last dimension must be adjacent")
+        return s[0], s[1], d[0], d[1]
 
     def append(self, k, v, table, lens, starts=None, slots=None, max_new: Optional[int] = None, stream=None):
         """Appends rows of keys and values [rows, kv_heads, dim] (``tsd_kv8_append``)."""
         who = "KV8Cache.append"
-        self._rows(who, "k", k, self.kv_heads)
-        self._rows(who, "v", v, self.kv_heads)
-        if k.shape != v.shape:
+        rows, _, kr, kh = self._rows(who, "k", k, self.kv_heads)
+        rows_v, _, vr, vh = self._rows(who, "v", v, self.kv_heads)
+        if rows != rows_v:
             raise ValueError(f"{who}: k and v must have the same rows")
-        b = self._batch(who, table, lens, starts, slots, k.shape[0], max_new, None)
-        _check(lib().tsd_kv8_append(ctypes.byref(self._c), ctypes.byref(b), k.data_ptr(), k.stride(0), k.stride(1),
-                                    v.data_ptr(), v.stride(0), v.stride(1), _stream(stream)))
+        b = self._batch(who, table, lens, starts, slots, rows, max_new, None)
+        st = lib().tsd_kv8_append(self._pc, ctypes.byref(b), k.data_ptr(), kr, kh, v.data_ptr(), vr, vh,
+                                  _raw_stream(stream, self._dev))
+        if st:
+            _check(st)
 
     def read(self, table, lens, rows: int, starts=None, slots=None, out=None, stream=None):
         """(k, v) float32 [rows, kv_heads, dim]: the values held for the rows'
@@ -908,14 +946,14 @@ class KV8Cache:
         b = self._batch(who, table, lens, starts, slots, rows, None, None)
         shape = (rows, self.kv_heads, self.dim)
         if out is None:
-            with _On(stream):
-                out = (torch.empty(shape, dtype=torch.float32, device=self.device),
-                       torch.empty(shape, dtype=torch.float32, device=self.device))
+            out = _empty(shape, torch.float32, self._dev, stream), _empty(shape, torch.float32, self._dev, stream)
         for t in out:
-            if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+            if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous() or t.get_device() != self._dev:
                 raise ValueError(f"{who}: out must be two contiguous float32 {list(shape)} on the cache's device")
-        _check(lib().tsd_kv8_read(ctypes.byref(self._c), ctypes.byref(b), out[0].data_ptr(), out[1].data_ptr(),
-                                  _stream(stream)))
+        st = lib().tsd_kv8_read(self._pc, ctypes.byref(b), out[0].data_ptr(), out[1].data_ptr(),
+                                _raw_stream(stream, self._dev))
+        if st:
+            _check(st)
         return out
 
     def attend(self, q, table, lens, starts=None, slots=None, scale: Optional[float] = None, window: int = 0,
@@ -926,25 +964,30 @@ class KV8Cache:
         import torch
 
         who = "KV8Cache.attend"
-        self._rows(who, "q", q)
-        rows, heads = q.shape[0], q.shape[1]
+        rows, heads, qr, qh = self._rows(who, "q", q)
         b = self._batch(who, table, lens, starts, slots, rows, max_new, max_len)
+        pb = ctypes.byref(b)
         L = lib()
-        need = _i64()
-        _check(L.tsd_kv8_attend_workspace(ctypes.byref(self._c), ctypes.byref(b), heads, window, sinks,
-                                          ctypes.byref(need)))
+        dev = self._dev
+        key = (dev, self.dim, self.kv_heads, self.block, b.n, rows, heads, b.table_width, max_new, max_len, window, sinks)
+        need = _sizes.get(key)
+        if need is None:
+            x = _i64()
+            _check(L.tsd_kv8_attend_workspace(self._pc, pb, heads, window, sinks, ctypes.byref(x)))
+            need = _remember(key, x.value)
         ws = None
-        if out is None or need.value:
-            with _On(stream):
-                if out is None:
-                    out = torch.empty((rows, heads, self.dim), dtype=self.dtype, device=self.device)
-                if need.value:
-                    ws = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-        self._rows(who, "out", out, heads)
-        if out.shape[0] != rows:
-            raise ValueError(f"{who}: out must have {rows} rows")
-        _check(L.tsd_kv8_attend(ctypes.byref(self._c), ctypes.byref(b), heads, q.data_ptr(), q.stride(0), q.stride(1),
-                                self.dim ** -0.5 if scale is None else scale, window, sinks, out.data_ptr(),
-                                out.stride(0), out.stride(1), ws.data_ptr() if ws is not None else None, need.value,
-                                _stream(stream)))
+        if need:
+            ws = _empty(need, torch.uint8, dev, stream)
+        if out is None:
+            out = _empty((rows, heads, self.dim), self.dtype, dev, stream)
+            orow, oh = heads * self.dim, self.dim
+        else:
+            orows, _, orow, oh = self._rows(who, "out", out, heads)
+            if orows != rows:
+                raise ValueError(f"{who}: out must have {rows} rows")
+        st = L.tsd_kv8_attend(self._pc, pb, heads, q.data_ptr(), qr, qh, self.dim ** -0.5 if scale is None else scale,
+                              window, sinks, out.data_ptr(), orow, oh, ws.data_ptr() if ws is not None else None, need,
+                              _raw_stream(stream, dev))
+        if st:
+            _check(st)
         return out

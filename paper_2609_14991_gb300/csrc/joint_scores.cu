@@ -1,7 +1,10 @@
 // Scores of labels from a joint network's input rows (tsd.h:
-// tsd_joint_label_scores): the product A . Wt^T on the tensor cores with the
-// scores' sums, the given labels' logits and the best labels taken in its
-// epilogue; logits never leave the SM.
+// tsd_joint_label_scores): the product A . Wt^T on the tensor cores.  From two
+// 256 x 256 tiles per pair of SMs on, the scores' sums, the given labels' logits
+// and the best labels are taken in its epilogue and no logit leaves the SM.
+// Smaller calls store their logits (at most 40 MB, which stay in L2) and scores.cu's kernel
+// follows: the epilogue's code runs once per tile there, and fetching it takes longer
+// than running it (1001 x 640 x 1025 with 4 alternatives: 23.4 us fused).
 //
 // Mathematics: scores.cu's, with a running maximum m per row: when it grows to m',
 // w = 2^((m - m') c), S := w S, E := w (E + (m - m') c S).
@@ -14,10 +17,13 @@
 // mod 2, warps 2-17 take tile i - 1 (thread = row; the four warps of a TMEM
 // lane quadrant take a quarter of the columns each).
 //
-// The best labels: a thread keeps its best in order in registers, and logits
-// above its last one go to a small buffer in shared memory first (three
-// instructions each, only where one of eight neighbours passes in some
-// lane); the buffer is sorted in when one of the warp's fills.
+// The best labels: a thread keeps the K largest maxima of its groups of eight
+// logits (two min/max instructions per place and group, no branch).  After
+// each tile the four threads of a row show one another theirs: the K-th
+// largest of all is a bound that K of the row's logits reach and hardly more.
+// Only then are the tile's logits read again, and those that reach the bound put
+// with their labels into a buffer in shared memory, unordered; a full buffer
+// drops what the bound has passed since.  The row tile's end orders what is left.
 #include <cuda.h>
 
 #include <algorithm>
@@ -34,7 +40,10 @@ using namespace tc;
 
 constexpr int kEpiWarps = 16;
 constexpr int kThreads = 64 + 32 * kEpiWarps;
-constexpr int kBuf = 16;  // candidates per thread between sorts
+// Candidates per thread: what an ordering leaves, four more, and as much again as
+// keeps a full buffer rare (K 8: 9059 orderings a call with 12, hardly any with 16).
+template <int K>
+constexpr int kBufOf = K <= 0 ? 0 : K + 8;
 
 struct JointScoreArgs {
   LabelArgs o;
@@ -43,8 +52,11 @@ struct JointScoreArgs {
   int tiles;       // row tiles x label tiles
   int workers;     // CTAs or pairs
   int segs;        // most partial results per row
+  float* logits;   // small calls: [n][ld]
+  int ld;
   float* given;    // [n][m] the given labels' logits
-  float* part;     // [n][segs][3 + 2 K]: m, S, E, logits, labels
+  float4* part;    // [n][segs] partial results: m, S, E and the number of candidates
+  float2* cand;    // [n][segs][4 K] logits and labels that may be among the row's best
 };
 
 // the worker whose range of tiles holds tile t (worker p has tiles p T / P .. (p + 1) T / P)
@@ -52,52 +64,181 @@ __host__ __device__ __forceinline__ int worker_of(int64_t t, int64_t tiles, int6
   return (int)(((t + 1) * workers - 1) / tiles);
 }
 
-template <int BN, bool PAIR>
+// K: the most alternatives, or kStore: logits are stored
+constexpr int kStore = -1;
+
+template <int BN, bool PAIR, int K>
 struct ScoreShape {
   static constexpr int kABytes = kBM * kBK * 2;
   static constexpr int kBRows = PAIR ? BN / 2 : BN;
   static constexpr int kStageBytes = kABytes + kBRows * kBK * 2;
   static constexpr int kParts = BN / 32 < 4 ? BN / 32 : 4;  // warps of a lane quadrant with work
   static constexpr int kCols = BN / kParts;                 // columns of a warp
+  static constexpr int kBuf = kBufOf<K>;
   static constexpr int kBufBytes = kEpiWarps * 32 * kBuf * 8;
-  static constexpr int kFit = (227 * 1024 - 1024 - 512 - kBufBytes) / kStageBytes;
+  static constexpr int kShownBytes = K < 0 ? 0 : 4 * 128 * (K > 4 ? K : 4) * 4;  // per part and row of the CTA
+  static constexpr int kFit = (227 * 1024 - 1024 - 512 - kBufBytes - kShownBytes) / kStageBytes;
   static constexpr int kStages = kFit < 12 ? kFit : 12;
   static constexpr int kBufOff = kStages * kStageBytes;
-  static constexpr int kBarOff = kBufOff + kBufBytes;
+  static constexpr int kShownOff = kBufOff + kBufBytes;
+  static constexpr int kBarOff = kShownOff + kShownBytes;
   static constexpr int kSmem = kBarOff + 512 + 1024;
   static_assert((2 * kStages + 5) * 8 + 4 <= 512, "barrier area");
   static_assert(kSmem <= 227 * 1024 && kStages >= 4, "shared memory per CTA");
-  static_assert(kBufBytes >= kEpiWarps * 32 * (3 + 2 * kMaxAlt) * 4, "the parts' results pass through the buffer");
 };
 
-template <int K>
-struct Best {
-  float v[K > 0 ? K : 1];
-  int i[K > 0 ? K : 1];
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int j = 0; j < K; ++j) {
-      v[j] = -INFINITY;
-      i[j] = 0x7fffffff;
-    }
-  }
-  // in descending order, equal logits by label
-  __device__ __forceinline__ void insert(float y, int label) {
-#pragma unroll
-    for (int j = K - 1; j >= 0; --j) {
-      const bool here = y > v[j] || (y == v[j] && label < i[j]);
-      const bool above = j > 0 && (y > v[j - 1] || (y == v[j - 1] && label < i[j - 1]));
-      v[j] = here ? (above ? v[j - 1] : y) : v[j];
-      i[j] = here ? (above ? i[j - 1] : label) : i[j];
-    }
-  }
+constexpr float kLowest = -3.402823466e38f;  // finite: masked logits (-inf) stay below it
+
+// the next float above a finite one
+__device__ __forceinline__ float above(float x) {
+  int o = __float_as_int(x + 0.f);
+  o = (o ^ ((o >> 31) & 0x7fffffff)) + 1;
+  return __int_as_float(o ^ ((o >> 31) & 0x7fffffff));
+}
+
+// Makes room in a warp's buffers: what the bound has passed goes; where that
+// leaves more than `full` (many logits reach it), all but the K best of this part, and the
+// gate rises above the last of them.  A part's labels ascend in its buffer, so of equal
+// logits the first are the better ones, and a later one is not among its best.
+// Not inlined: rare, and called from many places.
+struct Room {
+  int cnt;
+  float gate;
 };
+template <int K>
+__device__ __noinline__ Room make_room(float2* buf, int cnt, float bound, float gate, int full) {
+  const auto keep = [&](auto stays) {
+    int to = 0;
+    const int most = __reduce_max_sync(0xffffffffu, cnt);
+#pragma unroll 1
+    for (int j = 0; j < most; ++j) {
+      const float2 y = buf[j * 32];
+      if (j < cnt && stays(y.x)) {
+        buf[to * 32] = y;
+        ++to;
+      }
+    }
+    cnt = to;
+  };
+  keep([&](float y) { return y >= bound; });
+  if (__any_sync(0xffffffffu, cnt > full)) {
+    float best[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) best[i] = -INFINITY;
+    int most = __reduce_max_sync(0xffffffffu, cnt);
+#pragma unroll 1
+    for (int j = 0; j < most; ++j) {
+      float y = j < cnt ? buf[j * 32].x : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const float hi = fmaxf(best[i], y);
+        y = fminf(best[i], y);
+        best[i] = hi;
+      }
+    }
+    const float last = best[K - 1];  // -inf in a lane with fewer: all stay
+    int equal = 0;                   // places for logits equal to the last
+#pragma unroll
+    for (int i = 0; i < K; ++i) equal += best[i] == last;
+    keep([&](float y) { return y > last || (y == last && equal-- > 0); });
+    if (last > -INFINITY) gate = fmaxf(gate, above(last));
+  }
+  return {cnt, gate};
+}
+
+// Puts those of 32 logits (labels from c0 on; maxima of eight each in top) that
+// reach the gate into the buffers.
+template <int K>
+__device__ __forceinline__ void push32(const float (&v)[32], const float* top, int c0, float2* buf, int& cnt, float bound, float& gate) {
+  constexpr int kBuf = kBufOf<K>;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    if (__any_sync(0xffffffffu, top[g] >= gate)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (j % 4 == 0 && __any_sync(0xffffffffu, cnt > kBuf - 4)) {
+          const Room r = make_room<K>(buf, cnt, bound, gate, kBuf - 4);
+          cnt = r.cnt;
+          gate = r.gate;
+        }
+        if (v[8 * g + j] >= gate) {
+          buf[cnt * 32] = make_float2(v[8 * g + j], __int_as_float(c0 + 8 * g + j));
+          ++cnt;
+        }
+      }
+    }
+  }
+}
+
+// The larger half of two lists in descending order (a[i] against b[K-1-i]), in order again.
+template <int K>
+__device__ __forceinline__ void merge_top(float (&a)[K], const float (&b)[K]) {
+#pragma unroll
+  for (int i = 0; i < K; ++i) a[i] = fmaxf(a[i], b[K - 1 - i]);
+#pragma unroll
+  for (int d = K / 2; d > 0; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < K; ++i)
+      if (!(i & d)) {
+        const float hi = fmaxf(a[i], a[i + d]), lo = fminf(a[i], a[i + d]);
+        a[i] = hi;
+        a[i + d] = lo;
+      }
+}
+
+// Enters N group maxima (8 or 4) into the list of the K largest.
+template <int K, int N>
+__device__ __forceinline__ void enter(float (&kept)[K], const float (&groups)[N]) {
+  constexpr int M = N > K ? N : K;
+  float x[M];
+#pragma unroll
+  for (int i = 0; i < M; ++i) x[i] = i < N ? groups[i] : -INFINITY;
+  // bitonic sort, descending
+#pragma unroll
+  for (int w = 2; w <= M; w <<= 1)
+#pragma unroll
+    for (int d = w / 2; d > 0; d >>= 1)
+#pragma unroll
+      for (int i = 0; i < M; ++i)
+        if (!(i & d)) {
+          const float hi = fmaxf(x[i], x[i + d]), lo = fminf(x[i], x[i + d]);
+          const bool down = (i & w) == 0;
+          x[i] = down ? hi : lo;
+          x[i + d] = down ? lo : hi;
+        }
+  float b[K];
+#pragma unroll
+  for (int i = 0; i < K; ++i) b[i] = x[i];
+  merge_top<K>(kept, b);
+}
+
+// The K-th largest of the parts' lists ([part][K / 4][128], this thread's row).
+template <int K, int PARTS>
+__device__ __forceinline__ float row_bound(const float4* shown) {
+  float a[PARTS][K];
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+    for (int j = 0; j < K; j += 4) {
+      float4 x;  // another warp may be writing it
+      asm volatile("ld.volatile.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(smem_u32(shown + (p * (K / 4) + j / 4) * 128)));
+      a[p][j] = x.x, a[p][j + 1] = x.y, a[p][j + 2] = x.z, a[p][j + 3] = x.w;
+    }
+  if constexpr (PARTS == 4) {
+    merge_top<K>(a[0], a[1]);
+    merge_top<K>(a[2], a[3]);
+  }
+  float least = INFINITY;
+#pragma unroll
+  for (int i = 0; i < K; ++i) least = fminf(least, fmaxf(a[0][i], a[PARTS / 2][K - 1 - i]));
+  return least;
+}
 
 template <int BN, bool PAIR, int K>
 __global__ void __launch_bounds__(kThreads, 1)
     k_joint_scores(const __grid_constant__ JointScoreArgs a, const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB) {
-  using S = ScoreShape<BN, PAIR>;
-  constexpr int kStages = S::kStages;
+  using S = ScoreShape<BN, PAIR, K>;
+  constexpr int kStages = S::kStages, kBuf = S::kBuf;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarOff);
@@ -213,46 +354,51 @@ __global__ void __launch_bounds__(kThreads, 1)
     const float c = a.o.inv_temp * kLog2e;
     const uint64_t cc = pair_of(c, c);
     float m = -INFINITY, s = 0.f, e = 0.f;
-    Best<K> best;
-    best.clear();
+    float bound = kLowest;  // K logits of the row reach it
+    float gate = kLowest;   // what a later logit of this part has to reach: the bound, or more after a full ordering
+    // the K largest of each part's group maxima so far, in order: [part][K / 4][128]
+    float4* shown = reinterpret_cast<float4*>(smem + S::kShownOff) + q * 32 + lane;
+    const auto bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + q) : "memory"); };  // the quadrant's four warps
     int cnt = 0, tl = 0;
-    bool ok = true;
-    const auto sort_in = [&]() {
-      const int most = __reduce_max_sync(0xffffffffu, cnt);
-      for (int j = 0; j < most; ++j)
-        if (j < cnt) {
-          const float2 y = buf[j * 32];
-          best.insert(y.x, __float_as_int(y.y));
-        }
-      cnt = 0;
-    };
+    bool ok = true, opening = true;
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int j = 0; j < K; j += 4) shown[(part * (K / 4) + j / 4) * 128] = make_float4(kLowest, kLowest, kLowest, kLowest);
+    }
     for (int t = first; t < last; ++t, ++tl) {
       const int ab = tl & 1;
       const int mt = t / a.Nt, row = mt * kTM + rank * kBM + q * 32 + lane, n0 = t % a.Nt * BN;
       // also the warps without columns: none hands a tile back before it is there
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(accf + ab, (uint32_t)(tl >> 1) & 1u));
-      if (ok && part < S::kParts && row - lane < a.n) {
-        fence_after();
-        int given[kMaxGiven];
+      const bool live = ok && part < S::kParts && row - lane < a.n;
+      float groups[S::kCols / 8];  // maxima of eight logits each
 #pragma unroll
-        for (int j = 0; j < kMaxGiven; ++j) given[j] = j < a.o.m && row < a.n ? __ldg(a.o.labels + (int64_t)row * a.o.m + j) : -1;
-#pragma unroll 1
+      for (int g = 0; g < S::kCols / 8; ++g) groups[g] = -INFINITY;
+      if (live) {
+        fence_after();
+#pragma unroll
         for (int h = 0; h < S::kCols / 32; ++h) {
           const int c0 = n0 + part * S::kCols + 32 * h;
           if (c0 >= a.C) break;
           float v[32];
           __syncwarp();
           tmem_ld32(tmem + (uint32_t)(ab * BN + part * S::kCols + 32 * h) + ((uint32_t)(q * 32) << 16), v);
+          if constexpr (K == kStore) {  // past the last label too: rows are padded to whole 32s
+            float4* to = reinterpret_cast<float4*>(a.logits + (int64_t)row * a.ld + c0);
+            if (row < a.n) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) to[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+            }
+            continue;
+          }
           if (c0 + 32 > a.C) {  // past the last label
 #pragma unroll
             for (int j = 0; j < 32; ++j)
               if (c0 + j >= a.C) v[j] = -INFINITY;
           }
           // given labels among these
-#pragma unroll
-          for (int j = 0; j < kMaxGiven; ++j) {
-            if (j >= a.o.m) break;
-            const int at = given[j] - c0;
+          for (int j = 0; j < a.o.m; ++j) {
+            const int at = (row < a.n ? __ldg(a.o.labels + (int64_t)row * a.o.m + j) : -1) - c0;
             const bool here = at >= 0 && at < 32;
             if (__any_sync(0xffffffffu, here)) {
               float x = 0.f;
@@ -261,8 +407,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (here) a.given[(int64_t)row * a.o.m + j] = x;
             }
           }
-          // eighths' and the whole's maxima
-          float top[4];
+          // the groups' and the whole's maxima
+          float* top = groups + 4 * h;
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             top[g] = fmaxf(fmaxf(fmaxf(v[8 * g], v[8 * g + 1]), fmaxf(v[8 * g + 2], v[8 * g + 3])),
@@ -296,26 +442,48 @@ __global__ void __launch_bounds__(kThreads, 1)
           unpair(e2, x0, x1);
           e += x0 + x1;
           if constexpr (K > 0) {
-            float bound = best.v[K - 1];
-            if (__any_sync(0xffffffffu, all > bound)) {
-#pragma unroll
-              for (int g = 0; g < 4; ++g) {
-                if (__any_sync(0xffffffffu, top[g] > bound)) {
-                  if (__any_sync(0xffffffffu, cnt > kBuf - 8)) {
-                    sort_in();
-                    bound = best.v[K - 1];
-                  }
-#pragma unroll
-                  for (int j = 0; j < 8; ++j)
-                    if (v[8 * g + j] > bound) {
-                      buf[cnt * 32] = make_float2(v[8 * g + j], __int_as_float(c0 + 8 * g + j));
-                      ++cnt;
-                    }
-                }
-              }
-            }
+            if (!opening) push32<K>(v, top, c0, buf, cnt, bound, gate);
           }
         }
+      }
+      if constexpr (K > 0) {
+        // the part's maxima, the row's bound, and the logits that reach it
+        float widest = groups[0];
+#pragma unroll
+        for (int g = 1; g < S::kCols / 8; ++g) widest = fmaxf(widest, groups[g]);
+        if (__any_sync(0xffffffffu, widest > bound)) {
+          float kept[K];
+#pragma unroll
+          for (int j = 0; j < K; j += 4) {
+            const float4 x = shown[(part * (K / 4) + j / 4) * 128];
+            kept[j] = x.x, kept[j + 1] = x.y, kept[j + 2] = x.z, kept[j + 3] = x.w;
+          }
+          enter<K, S::kCols / 8>(kept, groups);
+#pragma unroll
+          for (int j = 0; j < K; j += 4) shown[(part * (K / 4) + j / 4) * 128] = make_float4(kept[j], kept[j + 1], kept[j + 2], kept[j + 3]);
+        }
+        // in step on a row tile's first tile; later the others' lists may be a tile old, or half
+        // of each: every entry only grows, so the bound, which serves the next tile, holds all the same
+        if (opening) bar();
+        bound = fmaxf(bound, row_bound<K, S::kParts>(shown));
+        gate = fmaxf(gate, bound);
+        if (live && opening) {  // the first tile's logits again, now that there is a bound
+#pragma unroll
+          for (int h = 0; h < S::kCols / 32; ++h) {
+            const int c0 = n0 + part * S::kCols + 32 * h;
+            if (c0 >= a.C) break;
+            float v[32];
+            __syncwarp();
+            tmem_ld32(tmem + (uint32_t)(ab * BN + part * S::kCols + 32 * h) + ((uint32_t)(q * 32) << 16), v);
+            if (c0 + 32 > a.C) {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (c0 + j >= a.C) v[j] = -INFINITY;
+            }
+            push32<K>(v, groups + 4 * h, c0, buf, cnt, bound, gate);
+          }
+        }
+        opening = false;
       }
       // this warp's reads of the accumulator are done: hand it back
       fence_before();
@@ -325,60 +493,58 @@ __global__ void __launch_bounds__(kThreads, 1)
         else
           asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(smem_u32(acce + ab), 0)) : "memory");
       }
+      if (K == kStore) continue;
       if (t + 1 == last || (t + 1) / a.Nt != mt) {
         // the row tile's last tile here: join the parts of each row and leave the result
-        if constexpr (K > 0) {
-          sort_in();
-        }
         if (!ok) s = __uint_as_float(0x7fc00000u);
-        constexpr int kF = 3 + 2 * K;
-        float* parts = reinterpret_cast<float*>(quadrant) + lane;  // [part][kF][32]
-        const auto bar = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(1 + q) : "memory"); };
-        bar();  // the quadrant's four warps: every buffer has been read ...
-        if constexpr (S::kParts > 1) {
-          if (part > 0 && part < S::kParts) {
-            float* f = parts + part * kF * 32;
-            f[0] = m, f[32] = s, f[64] = e;
-#pragma unroll
-            for (int j = 0; j < K; ++j) {
-              f[(3 + j) * 32] = best.v[j];
-              f[(3 + K + j) * 32] = __int_as_float(best.i[j]);
-            }
-          }
+        const int seg = worker - worker_of((int64_t)mt * a.Nt, a.tiles, a.workers);
+        const int64_t at = (int64_t)row * a.segs + seg;
+        if constexpr (K > 0) {
+          bar();  // every part's last list is there
+          bound = row_bound<K, S::kParts>(shown);
+          cnt = make_room<K>(buf, cnt, bound, gate, 4 * K / S::kParts).cnt;
+          bar();  // the lists have been read: the sums take their place
         }
+        float4* sums = reinterpret_cast<float4*>(smem + S::kShownOff) + q * 32 + lane;  // [part][128] m, S, E, candidates
+        sums[part * 128] = make_float4(m, s, e, __int_as_float(cnt));
         bar();
-        if (part == 0) {
-#pragma unroll 1
-          for (int p = 1; p < S::kParts; ++p) {
-            const float* f = parts + p * kF * 32;
-            const float om = f[0];
-            float os = f[32], oe = f[64];
-            const float to = fmaxf(m, om);
-            const float d0 = m == -INFINITY ? 0.f : (m - to) * c, w0 = ex2_approx(d0);
-            const float d1 = om == -INFINITY ? 0.f : (om - to) * c, w1 = ex2_approx(d1);
-            e = w0 * fmaf(d0, s, e) + w1 * fmaf(d1, os, oe);
-            s = w0 * s + w1 * os;
-            m = to;
-#pragma unroll 1
-            for (int j = 0; j < K; ++j) best.insert(f[(3 + j) * 32], __float_as_int(f[(3 + K + j) * 32]));
-          }
-          if (row < a.n) {
-            const int seg = worker - worker_of((int64_t)mt * a.Nt, a.tiles, a.workers);
-            float* f = a.part + ((int64_t)row * a.segs + seg) * kF;
-            f[0] = m, f[1] = s, f[2] = e;
+        float4 of[S::kParts];
+        int all = 0, mine = 0;  // candidates of the row, and of the parts before this one
 #pragma unroll
-            for (int j = 0; j < K; ++j) {
-              f[3 + j] = best.v[j];
-              f[3 + K + j] = __int_as_float(best.i[j]);
-            }
-          }
+        for (int p = 0; p < S::kParts; ++p) {
+          of[p] = sums[p * 128];
+          if (p < part) mine += __float_as_int(of[p].w);
+          all += __float_as_int(of[p].w);
         }
-        bar();  // ... and the results, before the buffers are written again
+        if constexpr (K > 0) {
+          if (row < a.n)
+            for (int i = 0; i < cnt; ++i) a.cand[at * (4 * K) + mine + i] = buf[i * 32];
+        }
+        if (part == 0 && row < a.n) {
+#pragma unroll
+          for (int p = 1; p < S::kParts; ++p) {
+            const float to = fmaxf(m, of[p].x);
+            const float d0 = m == -INFINITY ? 0.f : (m - to) * c, w0 = ex2_approx(d0);
+            const float d1 = of[p].x == -INFINITY ? 0.f : (of[p].x - to) * c, w1 = ex2_approx(d1);
+            e = w0 * fmaf(d0, s, e) + w1 * fmaf(d1, of[p].y, of[p].z);
+            s = w0 * s + w1 * of[p].y;
+            m = to;
+          }
+          a.part[at] = make_float4(m, s, e, __int_as_float(all));
+        }
+        bar();  // before the buffers and the lists are written again
         m = -INFINITY, s = 0.f, e = 0.f;
-        best.clear();
+        cnt = 0;
+        bound = gate = kLowest;
+        opening = true;
+        if constexpr (K > 0) {
+#pragma unroll
+          for (int j = 0; j < K; j += 4) shown[(part * (K / 4) + j / 4) * 128] = make_float4(kLowest, kLowest, kLowest, kLowest);
+        }
       }
     }
   }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   fence_before();
   __syncthreads();
   if constexpr (PAIR)  // neither CTA leaves while the other may still signal it or read its operands
@@ -392,39 +558,94 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-// Eight lanes per row join its partial results and write the scores.
-template <int K>
-__global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant__ JointScoreArgs a, int rows_per_tile) {
-  const int64_t row = (int64_t)blockIdx.x * 16 + threadIdx.x / 8;
-  const int l = threadIdx.x & 7;
+// L lanes per row (8 or 32) join its partial results and write the scores.  A
+// lane takes every fourth candidate of its partial results, with no load
+// waiting for another but where a result has more than eight.  The K largest
+// values come from lists in registers, as above; the candidates that reach
+// the last of them, hardly more than K, are placed by counting better ones.
+constexpr int kJoinCap = 32;
+template <int K, int L>
+__global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant__ JointScoreArgs a, int rows_per_tile, int cap) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr int kRows = 128 / L;
+  __shared__ float2 s_list[kRows][K > 0 ? kJoinCap : 1];
+  __shared__ int s_count[kRows];
+  const int slot = threadIdx.x / L;
+  const int64_t row = (int64_t)blockIdx.x * kRows + slot;
+  const int l = threadIdx.x & (L - 1);
   const bool live = row < a.n;
-  constexpr int kF = 3 + 2 * K;
   const int mt = (int)((live ? row : 0) / rows_per_tile);
   const int w0 = worker_of((int64_t)mt * a.Nt, a.tiles, a.workers), w1 = worker_of((int64_t)(mt + 1) * a.Nt - 1, a.tiles, a.workers);
   const int segs = live ? w1 - w0 + 1 : 0;
-  const float* part = a.part + row * a.segs * kF;
-  const auto widest = [](float x) {
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-    return x;
-  };
-  const auto total = [](float x) {
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-  };
+  const float4* part = a.part + row * a.segs;
+  const float2* cand = a.cand + row * a.segs * cap;
   const float c = a.o.inv_temp * kLog2e;
-  float m = -INFINITY;
-  for (int i = l; i < segs; i += 8) m = fmaxf(m, part[i * kF]);
-  m = widest(m);
-  float s = 0.f, e = 0.f;
-  for (int i = l; i < segs; i += 8) {
-    const float pm = part[i * kF], ps = part[i * kF + 1], pe = part[i * kF + 2];
-    const float d = pm == -INFINITY ? 0.f : (pm - m) * c, w = ex2_approx(d);
-    s += w * ps;
-    e += w * fmaf(d, ps, pe);
+  if (l == 0) s_count[slot] = 0;
+  // sums, of each partial result by one lane; values, by all
+  float m = -INFINITY, s = 0.f, e = 0.f;
+  float best[K > 0 ? K : 1];
+#pragma unroll
+  for (int i = 0; i < K; ++i) best[i] = kLowest;
+  const auto enter_one = [&](float y) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+      const float hi = fmaxf(best[i], y);
+      y = fminf(best[i], y);
+      best[i] = hi;
+    }
+  };
+  const auto join = [&](float om, float os, float oe) {
+    const float to = fmaxf(m, om);
+    const float d0 = m == -INFINITY ? 0.f : (m - to) * c, x0 = ex2_approx(d0);
+    const float d1 = om == -INFINITY ? 0.f : (om - to) * c, x1 = ex2_approx(d1);
+    e = x0 * fmaf(d0, s, e) + x1 * fmaf(d1, os, oe);
+    s = x0 * s + x1 * os;
+    m = to;
+  };
+  // f(candidate) for each of this lane's
+  const auto each = [&](auto f) {
+    for (int u = l; u < segs * 4; u += L) {
+      const float4 p = part[u >> 2];
+      const float2* x = cand + (int64_t)(u >> 2) * cap;
+      float2 y0, y1;
+      if (K > 0) y0 = x[u & 3], y1 = x[(u & 3) + 4];  // within the result's places, filled or not
+      f(p, u, true);
+      if constexpr (K > 0) {
+        const int n = __float_as_int(p.w);
+        if ((u & 3) < n) f(y0);
+        if ((u & 3) + 4 < n) f(y1);
+        for (int j = (u & 3) + 8; j < n; j += 4) f(x[j]);
+      }
+    }
+  };
+  struct First {
+    decltype(join)& add;
+    decltype(enter_one)& enter;
+    __device__ void operator()(const float4& p, int u, bool) {
+      if ((u & 3) == 0) add(p.x, p.y, p.z);
+    }
+    __device__ void operator()(const float2& y) { enter(y.x); }
+  };
+  each(First{join, enter_one});
+#pragma unroll
+  for (int o = 1; o < L; o <<= 1) {
+    const float om = __shfl_xor_sync(0xffffffffu, m, o), os = __shfl_xor_sync(0xffffffffu, s, o), oe = __shfl_xor_sync(0xffffffffu, e, o);
+    // in the same order in both lanes: one result for the row
+    if (l & o) {
+      const float tm = m, ts = s, te = e;
+      m = om, s = os, e = oe;
+      join(tm, ts, te);
+    } else {
+      join(om, os, oe);
+    }
+    if constexpr (K > 0) {
+      float b[K];
+#pragma unroll
+      for (int i = 0; i < K; ++i) b[i] = __shfl_xor_sync(0xffffffffu, best[i], o);
+      merge_top<K>(best, b);
+    }
   }
-  const RowSums sums{m, total(s), total(e)};
+  const RowSums sums{m, s, e};
   if (live) {
     label_finish(a.o, row, sums, l, [&](int label) {
       if (label >= a.C) return __uint_as_float(0x7fc00000u);
@@ -432,60 +653,104 @@ __global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant
     });
   }
   if constexpr (K > 0) {
-    float pv = INFINITY;
-    int pi = -1;
-    for (int r = 0; r < a.o.k; ++r) {
-      float bv = -INFINITY;
-      int bi = 0x7fffffff;
-      for (int i = l; i < segs * K; i += 8) {
-        const float* f = part + (i / K) * kF + 3 + i % K;
-        const float y = f[0];
-        const int label = __float_as_int(f[K]);
-        const bool after = y < pv || (y == pv && label > pi);
-        if (after && (y > bv || (y == bv && label < bi))) bv = y, bi = label;
+    const float bound = best[K - 1];
+    struct Second {
+      float bound;
+      int* count;
+      float2* list;
+      __device__ void operator()(const float4&, int, bool) {}
+      __device__ void operator()(const float2& y) {
+        if (y.x >= bound) {
+          const int at = atomicAdd(count, 1);
+          if (at < kJoinCap) list[at] = y;
+        }
       }
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) {
-        const float y = __shfl_xor_sync(0xffffffffu, bv, o);
-        const int label = __shfl_xor_sync(0xffffffffu, bi, o);
-        if (y > bv || (y == bv && label < bi)) bv = y, bi = label;
+    };
+    __syncwarp();
+    each(Second{bound, &s_count[slot], s_list[slot]});
+    __syncwarp();
+    const int n = s_count[slot];
+    if (!live) return;
+    if (n <= kJoinCap) {
+      for (int i = l; i < n; i += L) {
+        const float2 y = s_list[slot][i];
+        const int label = __float_as_int(y.y);
+        int place = 0;
+        for (int j = 0; j < n; ++j) {
+          const float2 z = s_list[slot][j];
+          place += z.x > y.x || (z.x == y.x && __float_as_int(z.y) < label) ? 1 : 0;
+        }
+        if (place < a.o.k) label_alternative(a.o, row, place, sums, y.x, label);
       }
-      if (live && l == 0) label_alternative(a.o, row, r, sums, bv, bi);
-      pv = bv;
-      pi = bi;
+      for (int j = n + l; j < a.o.k; j += L) label_alternative(a.o, row, j, sums, -INFINITY, -1);
+    } else if (l == 0) {  // many equal logits: one lane looks for the next one k times
+      float pv = INFINITY;
+      int pi = -1;
+      for (int r = 0; r < a.o.k; ++r) {
+        float bv = -INFINITY;
+        int bi = 0x7fffffff;
+        for (int u = 0; u < segs; ++u)
+          for (int j = 0; j < __float_as_int(part[u].w); ++j) {
+            const float2 y = cand[(int64_t)u * cap + j];
+            const int label = __float_as_int(y.y);
+            const bool after = y.x < pv || (y.x == pv && label > pi);
+            if (after && (y.x > bv || (y.x == bv && label < bi))) bv = y.x, bi = label;
+          }
+        label_alternative(a.o, row, r, sums, bv, bi);
+        pv = bv;
+        pi = bi;
+      }
     }
   }
 }
 
 struct ScorePlan {
-  bool pair;
-  int bn, tm, Nt, tiles, workers, segs, K;
+  bool store, pair;  // logits stored; pairs of CTAs
+  int bn, tm, Nt, tiles, workers, segs, K, ld;
   int64_t given, bytes;  // offset of the partial results, size of the workspace
 };
 
-// The tile shape: pairs of 256 x 256 once they fill the SMs; below, 128 x 128 and 128 x 64
-// tiles put more SMs on the operands.
 ScorePlan score_plan(int n, int H, int C, int m, int k, int sms) {
-  ScorePlan p;
+  ScorePlan p{};
   const auto tiles_of = [&](int tm, int bn) { return (int64_t)((n + tm - 1) / tm) * ((C + bn - 1) / bn); };
-  p.pair = tiles_of(256, 256) >= sms / 2;
-  p.bn = p.pair ? 256 : tiles_of(128, 128) >= sms ? 128 : 64;
+  p.store = tiles_of(256, 256) < 2 * (sms / 2);
+  p.pair = !p.store;
+  p.bn = 256;
+  if (p.store) {
+    // rounds of tiles times a k-block's clocks: its MMAs, or its operands at 64 bytes
+    // per clock and SM
+    const auto cost = [&](int tm, int bn, int slots, double mma, double rows) {
+      const int64_t t = tiles_of(tm, bn);
+      return (double)((t + slots - 1) / slots) * (H / kBK) * std::max(mma, rows * 128 / 64) + 12 * bn;
+    };
+    double best = cost(256, 256, sms / 2, 516, 256);
+    p.pair = true;
+    for (int bn : {128, 64}) {
+      const double x = cost(128, bn, sms, bn == 128 ? 260 : 196, 128 + bn);
+      if (x < best) best = x, p.bn = bn, p.pair = false;
+    }
+  }
   p.tm = p.pair ? 256 : 128;
   p.Nt = (C + p.bn - 1) / p.bn;
   p.tiles = (int)tiles_of(p.tm, p.bn);
   p.workers = std::min(p.tiles, p.pair ? sms / 2 : sms);
+  if (p.store) {
+    p.ld = (C + 31) / 32 * 32;
+    p.bytes = (int64_t)n * p.ld * 4;
+    return p;
+  }
   const int each = p.tiles / p.workers;  // fewest tiles of a worker
   p.segs = std::min(p.Nt, (p.Nt - 2 + each) / each + 1);
   p.K = k == 0 ? 0 : k <= 4 ? 4 : kMaxAlt;
   p.given = ((int64_t)n * m * 4 + 15) / 16 * 16;
-  p.bytes = p.given + (int64_t)n * p.segs * (3 + 2 * p.K) * 4;
+  p.bytes = p.given + (int64_t)n * p.segs * (16 + 4 * p.K * 8);
   return p;
 }
 
 template <int BN, bool PAIR, int K>
-cudaError_t launch_shape(const ScorePlan& p, const JointScoreArgs& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
-  using S = ScoreShape<BN, PAIR>;
-  cudaError_t e = cudaFuncSetAttribute(k_joint_scores<BN, PAIR, K>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+cudaError_t launch_tiles(const ScorePlan& p, const JointScoreArgs& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+  using S = ScoreShape<BN, PAIR, K>;
+  cudaError_t e = smem_opt_in<k_joint_scores<BN, PAIR, K>>(S::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(PAIR ? 2 * p.workers : p.workers));
@@ -498,17 +763,32 @@ cudaError_t launch_shape(const ScorePlan& p, const JointScoreArgs& a, const CUte
   at.val.clusterDim.y = at.val.clusterDim.z = 1;
   cfg.attrs = &at;
   cfg.numAttrs = PAIR ? 1 : 0;
-  e = cudaLaunchKernelEx(&cfg, k_joint_scores<BN, PAIR, K>, a, tmA, tmB);
-  if (e != cudaSuccess) return e;
-  k_joint_scores_join<K><<<(unsigned)((a.n + 15) / 16), 128, 0, s>>>(a, p.tm);
-  return cudaGetLastError();
+  return cudaLaunchKernelEx(&cfg, k_joint_scores<BN, PAIR, K>, a, tmA, tmB);
 }
 
 template <int K>
-cudaError_t launch_k(const ScorePlan& p, const JointScoreArgs& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
-  if (p.pair) return launch_shape<256, true, K>(p, a, tmA, tmB, s);
-  if (p.bn == 128) return launch_shape<128, false, K>(p, a, tmA, tmB, s);
-  return launch_shape<64, false, K>(p, a, tmA, tmB, s);
+cudaError_t launch_fused(const ScorePlan& p, const JointScoreArgs& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+  const cudaError_t e = launch_tiles<256, true, K>(p, a, tmA, tmB, s);
+  if (e != cudaSuccess) return e;
+  // few partial results per row: eight lanes; more (few rows, many labels): a warp
+  const bool wide = p.segs > 4;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(wide ? (a.n + 3) / 4 : (a.n + 15) / 16));
+  cfg.blockDim = dim3(128);
+  cfg.stream = s;
+  cudaLaunchAttribute pdl{};
+  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &pdl;
+  cfg.numAttrs = 1;
+  return wide ? cudaLaunchKernelEx(&cfg, k_joint_scores_join<K, 32>, a, p.tm, 4 * K) : cudaLaunchKernelEx(&cfg, k_joint_scores_join<K, 8>, a, p.tm, 4 * K);
+}
+
+cudaError_t launch_stored(const ScorePlan& p, const JointScoreArgs& a, const CUtensorMap& tmA, const CUtensorMap& tmB, cudaStream_t s) {
+  const cudaError_t e = p.pair        ? launch_tiles<256, true, kStore>(p, a, tmA, tmB, s)
+                        : p.bn == 128 ? launch_tiles<128, false, kStore>(p, a, tmA, tmB, s)
+                                      : launch_tiles<64, false, kStore>(p, a, tmA, tmB, s);
+  return e == cudaSuccess ? label_rows_launch(a.o, a.logits, TSD_F32, a.ld, a.n, a.C, true, s) : e;
 }
 
 tsd_status check(const char* who, int32_t n, int32_t H, int32_t C) {
@@ -531,9 +811,8 @@ extern "C" tsd_status tsd_joint_label_scores_workspace(int32_t n, int32_t H, int
   if (!bytes) return fail(TSD_EINVAL, "%s: NULL argument", who);
   if (tsd_status st = check(who, n, H, C)) return st;
   if (m < 0 || m > kMaxGiven || k < 0 || k > kMaxAlt) return fail(TSD_EINVAL, "%s: m=%d or k=%d outside [0, 8]", who, m, k);
-  int dev = 0, sms = 0;
-  TSD_CUDA(cudaGetDevice(&dev));
-  TSD_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  int sms = 0;
+  TSD_CUDA(device_sms(&sms));
   *bytes = score_plan(n, H, C, m, k, sms).bytes;
   return TSD_OK;
 }
@@ -554,9 +833,8 @@ extern "C" tsd_status tsd_joint_label_scores(int32_t n, int32_t H, int32_t C, co
     return fail(TSD_EINVAL, "%s: strides %lld, %lld must be multiples of 8, at least H=%d", who, (long long)a_stride, (long long)w_stride, H);
   if (reinterpret_cast<uintptr_t>(A_bf16) % 16 || reinterpret_cast<uintptr_t>(Wt_bf16) % 16)
     return fail(TSD_EINVAL, "%s: A and Wt must be 16-byte aligned", who);
-  int dev = 0, sms = 0;
-  TSD_CUDA(cudaGetDevice(&dev));
-  TSD_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  int sms = 0;
+  TSD_CUDA(device_sms(&sms));
   const ScorePlan p = score_plan(n, H, C, m, k, sms);
   if (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16)
     return fail(TSD_EINVAL, "%s: workspace of %lld bytes, %lld needed (16-byte aligned)", who, (long long)workspace_bytes, (long long)p.bytes);
@@ -564,9 +842,19 @@ extern "C" tsd_status tsd_joint_label_scores(int32_t n, int32_t H, int32_t C, co
   if (!make_map(&tmA, A_bf16, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, n, kBK, kBM, CU_TENSOR_MAP_SWIZZLE_128B, a_stride) ||
       !make_map(&tmB, Wt_bf16, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, C, kBK, p.pair ? p.bn / 2 : p.bn, CU_TENSOR_MAP_SWIZZLE_128B, w_stride))
     return fail(TSD_ECUDA, "%s: cuTensorMapEncodeTiled failed", who);
-  JointScoreArgs a{{m, k, labels, logp, entropy, alt_labels, alt_logp, 1.f / temperature}, n, H, C, p.Nt, p.tiles, p.workers, p.segs,
-                   static_cast<float*>(workspace), reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + p.given)};
+  JointScoreArgs a{};
+  a.o = {m, k, labels, logp, entropy, alt_labels, alt_logp, 1.f / temperature};
+  a.n = n, a.H = H, a.C = C;
+  a.Nt = p.Nt, a.tiles = p.tiles, a.workers = p.workers, a.segs = p.segs;
+  a.logits = static_cast<float*>(workspace);
+  a.ld = p.ld;
+  a.given = static_cast<float*>(workspace);
+  a.part = reinterpret_cast<float4*>(static_cast<unsigned char*>(workspace) + p.given);
+  a.cand = reinterpret_cast<float2*>(a.part + (int64_t)n * p.segs);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  TSD_CUDA(p.K == 0 ? launch_k<0>(p, a, tmA, tmB, s) : p.K == 4 ? launch_k<4>(p, a, tmA, tmB, s) : launch_k<8>(p, a, tmA, tmB, s));
+  TSD_CUDA(p.store ? launch_stored(p, a, tmA, tmB, s)
+           : p.K == 0 ? launch_fused<0>(p, a, tmA, tmB, s)
+           : p.K == 4 ? launch_fused<4>(p, a, tmA, tmB, s)
+                      : launch_fused<kMaxAlt>(p, a, tmA, tmB, s));
   return TSD_OK;
 }

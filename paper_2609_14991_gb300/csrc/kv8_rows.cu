@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(128) k_kv8_join(const __grid_constant__ Kv8Att
 template <bool BF16, int DIM, int MW>
 cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t s) {
   using S = RowsShape<DIM, MW>;
-  static const cudaError_t e = cudaFuncSetAttribute(k_kv8_rows<BF16, DIM, MW>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  const cudaError_t e = smem_opt_in<k_kv8_rows<BF16, DIM, MW>>(S::kSmem);
   if (e != cudaSuccess) return e;
   k_kv8_rows<BF16, DIM, MW><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, S::kSmem, s>>>(a);
   return cudaGetLastError();
@@ -487,20 +487,13 @@ static tsd_status attend_check(const char* who, const tsd_kv8* cache, const tsd_
   return TSD_OK;
 }
 
-static tsd_status device_sms(int* sms) {
-  int dev = 0;
-  TSD_CUDA(cudaGetDevice(&dev));
-  TSD_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
-  return TSD_OK;
-}
-
 extern "C" tsd_status tsd_kv8_attend_workspace(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads,
                                                int32_t window, int32_t sinks, int64_t* bytes) {
   clear_error();
   if (!bytes) return fail(TSD_EINVAL, "tsd_kv8_attend_workspace: NULL argument");
   if (tsd_status st = attend_check("tsd_kv8_attend_workspace", cache, batch, heads, window, sinks)) return st;
   int sms = 0;
-  if (tsd_status st = device_sms(&sms)) return st;
+  TSD_CUDA(device_sms(&sms));
   *bytes = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms).bytes;
   return TSD_OK;
 }
@@ -514,7 +507,7 @@ extern "C" tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* 
   if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "q", q, q_row, q_head)) return st;
   if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "out", out, out_row, out_head)) return st;
   int sms = 0;
-  if (tsd_status st = device_sms(&sms)) return st;
+  TSD_CUDA(device_sms(&sms));
   const Kv8RowsPlan p = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms);
   if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
     return fail(TSD_EINVAL, "tsd_kv8_attend: workspace of %lld bytes, %lld needed (16-byte aligned)", (long long)workspace_bytes, (long long)p.bytes);

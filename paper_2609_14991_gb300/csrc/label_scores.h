@@ -1,4 +1,4 @@
-// Scores of labels: what its two forms (scores.cu, joint_scores.cu) share.
+// Scores of labels: what its two operators (scores.cu, joint_scores.cu) share.
 #pragma once
 
 #include "internal.h"
@@ -60,6 +60,10 @@ __device__ __forceinline__ void label_alternative(const LabelArgs& a, int64_t ro
   a.alt_labels[row * a.k + j] = none ? -1 : label;
   a.alt_logp[row * a.k + j] = r.odd() ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : label_logp(r, a.inv_temp, x);
 }
+
+// The scores of n rows of logits in memory (scores.cu), ld elements apart; after: once
+// the kernel before it in the stream, launched to allow that, is done.
+cudaError_t label_rows_launch(const LabelArgs& o, const void* x, int dtype, int64_t ld, int n, int C, bool after, cudaStream_t s);
 
 tsd_status label_check(const char* who, int32_t n, int32_t most_n, int32_t C, float temperature, int32_t m,
                        const int32_t* labels, int32_t k, const float* logp, const int32_t* alt_labels, const float* alt_logp);

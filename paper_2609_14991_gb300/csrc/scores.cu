@@ -8,9 +8,9 @@
 // x_i - m is formed first (exact or rounded once), so a row's offset costs no
 // precision.  A row stays in registers (32 or 64 logits per thread): 32 to 512 threads
 // per row, above 16384 logits a cluster of 2 to 8 CTAs of 512 that exchange
-// through distributed shared memory.  The k largest: the threads form groups (8 to 128 of
-// them); the k-th largest of the groups' maxima is a bound that at least
-// k logits reach and few pass, so only those few are gathered and ordered.  If more
+// through distributed shared memory.  The k largest: the threads form 16 groups (per CTA), the
+// groups 8 classes (4 where k <= 4); the least of the classes' maxima is a bound that at least
+// k logits reach and few pass (about 22 of random ones for 8), so only those are gathered and ordered.  If more
 // than the gathering holds reach it (many equal logits), k rounds of a maximum over
 // the whole row take its place.
 #include <cooperative_groups.h>
@@ -35,20 +35,21 @@ struct RowsArgs {
   int n, C;
 };
 
-constexpr int kCap = 256;       // logits gathered per row (and CTA)
-constexpr int kGroupsMax = 16;  // groups per CTA
+constexpr int kCap = 256;    // logits gathered per row
+constexpr int kGroups = 16;  // groups of a CTA's threads (of a row's, where a warp takes one)
 
-// What the CTAs of a row's cluster show one another.
+// A row's shared memory.  In a cluster every CTA writes its groups' maxima
+// into each CTA's and its sums into the first CTA's; the first one fetches the
+// logits gathered by the others.
+template <int CS>
 struct RowShared {
-  float top[kGroupsMax];  // groups' maxima
-  float2 sums[16];        // warps' S and E
-  float cv[kCap];         // gathered logits and their labels
+  float top[kGroups * CS];  // groups' maxima
+  float2 sums[16 * CS];     // warps' S and E
+  float cv[kCap];           // gathered logits and their labels
   int ci[kCap];
-  int count;
+  int count;         // this CTA's logits that reach the bound
   float best_v[16];  // warps' best of a round over the whole row
   int best_i[16];
-  float pick_v;
-  int pick_i;
 };
 
 template <typename T>
@@ -97,18 +98,18 @@ template <typename T, int G, int CS, int E>
 __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_constant__ RowsArgs a) {
   constexpr int VE = 16 / sizeof(T), NV = E / VE;
   constexpr int kWarps = G / 32;
-  constexpr int kPerWarp = kWarps >= 16 ? 1 : (16 / kWarps < 8 ? 16 / kWarps : 8);  // groups in a warp
-  constexpr int kGroups = kPerWarp * kWarps;
+  constexpr int kLanes = G / kGroups;  // threads of a group
   constexpr int kRows = G == 32 ? 4 : 1;
-  constexpr int kKeys = (kGroups * CS + 31) / 32;  // groups' maxima per lane
-  __shared__ RowShared s_rows[kRows];
+  constexpr int kSub = E < 8 ? E : 8;  // logits whose maximum is kept for the gathering
+  __shared__ RowShared<CS> s_rows[kRows];
   const int warp_in_cta = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slot = G == 32 ? warp_in_cta : 0, warp = G == 32 ? 0 : warp_in_cta;
   const int64_t row = (int64_t)(blockIdx.x / CS) * kRows + slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // stored logits of joint rows: the product before
   if (row >= a.n) return;  // a whole warp (G 32) or none: the grid has n CTAs or clusters
   const int rank = CS > 1 ? (int)(blockIdx.x % CS) : 0;
-  RowShared& sh = s_rows[slot];
-  const auto peer = [&](int r) -> RowShared* {
+  RowShared<CS>& sh = s_rows[slot];
+  const auto peer = [&](int r) -> RowShared<CS>* {
     if constexpr (CS > 1) return cg::this_cluster().map_shared_rank(&sh, r);
     else return &sh;
   };
@@ -120,6 +121,8 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
     if constexpr (CS > 1) cg::this_cluster().sync();
     else sync_cta();
   };
+  // the cluster's CTAs have started before one writes to another (waited for below)
+  if constexpr (CS > 1) cg::this_cluster().barrier_arrive();
   const int t = warp * 32 + lane, rt = rank * G + t;
   const T* x = static_cast<const T*>(a.x) + row * a.ld;
   const int C = a.C, k = a.o.k;
@@ -133,12 +136,13 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int j = rt + i * G * CS;
+      w[i] = make_uint4(0, 0, 0, 0);
       if (j < nvec) w[i] = __ldcs(reinterpret_cast<const uint4*>(x + lead) + j);
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       unpack<T>(w[i], v + i * VE);
-      if (rt + i * G * CS >= nvec) {
+      if ((i + 1) * G * CS > nvec && rt + i * G * CS >= nvec) {  // the first test is the row's: most vectors skip the second
 #pragma unroll
         for (int j = 0; j < VE; ++j) v[i * VE + j] = -INFINITY;
       }
@@ -148,42 +152,44 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
   const float xv = xi >= 0 ? to_float(x[xi]) : -INFINITY;
   const auto label_of = [&](int e) { return lead + (rt + e / VE * G * CS) * VE + e % VE; };
 
-  // the groups' maxima, the row's, and the bound of the k largest
+  // maxima: of eight logits each, the thread's, the groups'
+  float sub[E / kSub];
+#pragma unroll
+  for (int i = 0; i < E / kSub; ++i) {
+    sub[i] = v[i * kSub];
+#pragma unroll
+    for (int j = 1; j < kSub; ++j) sub[i] = fmaxf(sub[i], v[i * kSub + j]);
+  }
   float mine = xv;
 #pragma unroll
-  for (int e = 0; e < E; ++e) mine = fmaxf(mine, v[e]);
+  for (int i = 0; i < E / kSub; ++i) mine = fmaxf(mine, sub[i]);
+  if (!(mine >= -INFINITY)) mine = INFINITY;  // NaN alone: the sums say so
   float gm = mine;
 #pragma unroll
-  for (int o = 1; o < 32 / kPerWarp; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
-  if (lane % (32 / kPerWarp) == 0) sh.top[warp * kPerWarp + lane / (32 / kPerWarp)] = gm;
+  for (int o = 1; o < kLanes; o <<= 1) gm = fmaxf(gm, __shfl_xor_sync(0xffffffffu, gm, o));
+  constexpr int kHeld = 32 / kLanes;  // groups of a warp
+  if constexpr (CS == 1) {
+    if (lane % kLanes == 0) sh.top[warp * kHeld + lane / kLanes] = gm;
+  } else {
+    // lane r of the warp (one group) writes to CTA r
+    static_assert(CS == 1 || kLanes == 32, "a warp is a group");
+    cg::this_cluster().barrier_wait();
+    if (lane < CS) peer(lane)->top[rank * kGroups + warp] = gm;
+  }
   if (t == 0) sh.count = 0;
   sync_row();
-  int keys[kKeys];
+  // The row's maximum, and a bound that k logits reach: the groups in 8 (or 4)
+  // classes, the least of the classes' maxima.
+  constexpr int kKeys = CS > 1 ? kGroups * CS / 32 : 1;
+  int key = order_of(sh.top[lane % (kGroups * CS)]);
 #pragma unroll
-  for (int i = 0; i < kKeys; ++i) {
-    const int j = lane + 32 * i;
-    keys[i] = j < kGroups * CS ? order_of(peer(j / kGroups)->top[j % kGroups]) : INT32_MIN;
-  }
-  float m = 0.f, bound = 0.f;
-  for (int r = 0; r < max(k, 1); ++r) {
-    int best = keys[0];
-#pragma unroll
-    for (int i = 1; i < kKeys; ++i) best = max(best, keys[i]);
-    const int top = __reduce_max_sync(0xffffffffu, best);
-    bound = value_of(top);
-    if (r == 0) m = bound;
-    // one holder gives it up
-    const bool holder = lane == __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
-    bool open = holder;
-#pragma unroll
-    for (int i = 0; i < kKeys; ++i)
-      if (open && keys[i] == top) {
-        keys[i] = INT32_MIN;
-        open = false;
-      }
-    if (top == INT32_MIN) break;
-  }
-  if (!(bound >= -INFINITY)) bound = -INFINITY;  // fewer groups than k
+  for (int i = 1; i < kKeys; ++i) key = max(key, order_of(sh.top[lane + 32 * i]));
+  const float m = value_of(__reduce_max_sync(0xffffffffu, key));
+  key = max(key, __shfl_xor_sync(0xffffffffu, key, 8));
+  if (CS > 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, 16));
+  if (k <= 4) key = max(key, __shfl_xor_sync(0xffffffffu, key, 4));
+  if (k == 1) key = max(key, max(__shfl_xor_sync(0xffffffffu, key, 1), __shfl_xor_sync(0xffffffffu, key, 2)));
+  const float bound = value_of(__reduce_min_sync(0xffffffffu, key));
 
   // sums: in pairs, a masked logit's exponent held finite (its term is 0 all the same)
   const float ms = m == -INFINITY ? 0.f : m, c = a.o.inv_temp * kLog2e;
@@ -214,46 +220,92 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
     S += __shfl_xor_sync(0xffffffffu, S, o);
     E2 += __shfl_xor_sync(0xffffffffu, E2, o);
   }
-  if (lane == 0) sh.sums[warp] = make_float2(S, E2);
+  if (lane == 0) peer(0)->sums[rank * kWarps + warp] = make_float2(S, E2);
 
-  // gather what reaches the bound
+  // gather what reaches the bound; a list that has run over is not counted on
+  constexpr int kMine = kCap / CS;
   if (k > 0 && mine >= bound && mine > -INFINITY) {
     const auto take = [&](float y, int label) {
-      const int at = atomicAdd(&sh.count, 1);
-      if (at < kCap) {
-        sh.cv[at] = y;
-        sh.ci[at] = label;
+      if (y >= bound && y > -INFINITY) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < kMine) {
+          sh.cv[at] = y;
+          sh.ci[at] = label;
+        }
       }
     };
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (v[e] >= bound && v[e] > -INFINITY) take(v[e], label_of(e));
-    if (xv >= bound && xv > -INFINITY) take(xv, xi);
+    for (int i = 0; i < E / kSub; ++i)
+      if (sub[i] >= bound && *(volatile int*)&sh.count <= kMine) {
+#pragma unroll
+        for (int j = 0; j < kSub; ++j) take(v[i * kSub + j], label_of(i * kSub + j));
+      }
+    take(xv, xi);
   }
   sync_row();
 
-  S = E2 = 0.f;
-  bool over = false;
-  for (int r = 0; r < CS; ++r) {
-    const RowShared* p = peer(r);
-    const float2 y = lane < kWarps ? p->sums[lane] : make_float2(0.f, 0.f);
-    S += y.x;
-    E2 += y.y;
-    over = over || p->count > kCap;
-  }
+  int count = sh.count;
+  bool over = count > kMine;
+  if constexpr (CS > 1) {
+    if (rank == 0) {
+      int theirs[CS];
 #pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    S += __shfl_xor_sync(0xffffffffu, S, o);
-    E2 += __shfl_xor_sync(0xffffffffu, E2, o);
+      for (int r = 1; r < CS; ++r) theirs[r] = peer(r)->count;
+#pragma unroll
+      for (int r = 1; r < CS; ++r) over = over || theirs[r] > kMine;
+      if (!over) {  // kMine <= 128 threads copy a list
+        static_assert(kMine <= G, "a thread per gathered logit");
+#pragma unroll
+        for (int r = 1; r < CS; ++r) {
+          if (t < theirs[r]) {
+            sh.cv[count + t] = peer(r)->cv[t];
+            sh.ci[count + t] = peer(r)->ci[t];
+          }
+          count += theirs[r];
+        }
+      }
+    }
+    cg::this_cluster().sync();  // the others' memory has been read
   }
-  const RowSums sums{m, S, E2};
-  if (rank == 0 && warp == 0) {
+  if (rank != 0 || (!over && warp != 0)) return;
+  RowSums sums{m, 0.f, 0.f};
+  if (warp == 0) {
+#pragma unroll
+    for (int i = 0; i < (kWarps * CS + 31) / 32; ++i) {
+      const float2 y = lane + 32 * i < kWarps * CS ? sh.sums[lane + 32 * i] : make_float2(0.f, 0.f);
+      sums.S += y.x;
+      sums.E += y.y;
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      sums.S += __shfl_xor_sync(0xffffffffu, sums.S, o);
+      sums.E += __shfl_xor_sync(0xffffffffu, sums.E, o);
+    }
     label_finish(a.o, row, sums, lane, [&](int l) { return l < C ? to_float(x[l]) : __uint_as_float(0x7fc00000u); });
   }
 
   // the k best in order
   float pv = INFINITY;
   int pi = -1;
+  if (!over) {
+    const float y0 = lane < count ? sh.cv[lane] : -INFINITY;
+    const int i0 = lane < count ? sh.ci[lane] : 0x7fffffff;
+    for (int r = 0; r < k; ++r) {
+      const bool open = before(pv, pi, y0, i0);
+      float bv = open ? y0 : -INFINITY;
+      int bi = open ? i0 : 0x7fffffff;
+      for (int i = lane + 32; i < count; i += 32) {
+        const float y = sh.cv[i];
+        const int l = sh.ci[i];
+        if (before(pv, pi, y, l) && before(y, l, bv, bi)) bv = y, bi = l;
+      }
+      warp_best(bv, bi);
+      if (lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
+      pv = bv;
+      pi = bi;
+    }
+    return;
+  }
   for (int r = 0; r < k; ++r) {
     float bv = -INFINITY;
     int bi = 0x7fffffff;
@@ -263,80 +315,80 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
         bi = i;
       }
     };
-    if (!over) {
-      if (rank != 0 || warp != 0) break;
-      for (int q = 0; q < CS; ++q) {
-        const RowShared* p = peer(q);
-        for (int i = lane; i < p->count; i += 32) look(p->cv[i], p->ci[i]);
-      }
-      warp_best(bv, bi);
-    } else {
+    if constexpr (CS == 1) {
 #pragma unroll
       for (int e = 0; e < E; ++e) look(v[e], label_of(e));
       if (xi >= 0) look(xv, xi);
-      warp_best(bv, bi);
-      if (lane == 0) {
-        sh.best_v[warp] = bv;
-        sh.best_i[warp] = bi;
-      }
-      sync_row();
-      bv = -INFINITY;
-      bi = 0x7fffffff;
-      for (int q = 0; q < CS; ++q) {
-        const RowShared* p = peer(q);
-        const float y = lane < kWarps ? p->best_v[lane] : -INFINITY;
-        const int i = lane < kWarps ? p->best_i[lane] : 0x7fffffff;
-        if (before(y, i, bv, bi)) {
-          bv = y;
-          bi = i;
-        }
-      }
-      warp_best(bv, bi);
-      sync_row();  // before the next round's are written
+    } else {  // the first CTA alone, from memory
+      for (int i = t; i < C; i += G) look(to_float(x[i]), i);
     }
-    if (rank == 0 && warp == 0 && lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
+    warp_best(bv, bi);
+    if (lane == 0) {
+      sh.best_v[warp] = bv;
+      sh.best_i[warp] = bi;
+    }
+    sync_cta();
+    bv = lane < kWarps ? sh.best_v[lane] : -INFINITY;
+    bi = lane < kWarps ? sh.best_i[lane] : 0x7fffffff;
+    warp_best(bv, bi);
+    sync_cta();  // before the next round's are written
+    if (t == 0) label_alternative(a.o, row, r, sums, bv, bi);
     pv = bv;
     pi = bi;
   }
-  if constexpr (CS > 1) cg::this_cluster().sync();  // no CTA leaves while its memory is read
 }
 
 template <typename T, int G, int CS, int E>
-cudaError_t launch(const RowsArgs& a, cudaStream_t s) {
+cudaError_t launch(const RowsArgs& a, bool after, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
   constexpr int kRows = G == 32 ? 4 : 1;
   cfg.gridDim = dim3((unsigned)(((int64_t)a.n + kRows - 1) / kRows * CS));
   cfg.blockDim = dim3(G == 32 ? 128 : G);
   cfg.stream = s;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = CS;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = CS > 1 ? 1 : 0;
+  cudaLaunchAttribute at[2];
+  int n = 0;
+  if (CS > 1) {
+    at[n].id = cudaLaunchAttributeClusterDimension;
+    at[n].val.clusterDim.x = CS;
+    at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  if (after) {
+    at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  cfg.attrs = at;
+  cfg.numAttrs = (unsigned)n;
   return cudaLaunchKernelEx(&cfg, k_label_rows<T, G, CS, E>, a);
 }
 
 // The fewest threads that hold a row in 32 registers each (64 above 8 x 512 x 32; 8 for
 // rows of a few vectors, where 32 would be mostly empty).
 template <typename T>
-cudaError_t launch_type(const RowsArgs& a, cudaStream_t s) {
+cudaError_t launch_type(const RowsArgs& a, bool after, cudaStream_t s) {
   const int vecs = a.C / (16 / (int)sizeof(T)) + 1;  // most whole vectors, with one of the ends
   const int per = 32 / (16 / (int)sizeof(T));        // vectors per thread
-  if (vecs <= 32 * per / 4) return launch<T, 32, 1, 8>(a, s);
-  if (a.C / (16 / (int)sizeof(T)) <= 32 * per) return launch<T, 32, 1, 32>(a, s);
+  if (vecs <= 32 * per / 4) return launch<T, 32, 1, 8>(a, after, s);
+  if (a.C / (16 / (int)sizeof(T)) <= 32 * per) return launch<T, 32, 1, 32>(a, after, s);
   const int v = a.C / (16 / (int)sizeof(T));
-  if (v <= 64 * per) return launch<T, 64, 1, 32>(a, s);
-  if (v <= 128 * per) return launch<T, 128, 1, 32>(a, s);
-  if (v <= 256 * per) return launch<T, 256, 1, 32>(a, s);
-  if (v <= 512 * per) return launch<T, 512, 1, 32>(a, s);
-  if (v <= 1024 * per) return launch<T, 512, 2, 32>(a, s);
-  if (v <= 2048 * per) return launch<T, 512, 4, 32>(a, s);
-  if (v <= 4096 * per) return launch<T, 512, 8, 32>(a, s);
-  return launch<T, 512, 8, 64>(a, s);
+  if (v <= 64 * per) return launch<T, 64, 1, 32>(a, after, s);
+  if (v <= 128 * per) return launch<T, 128, 1, 32>(a, after, s);
+  if (v <= 256 * per) return launch<T, 256, 1, 32>(a, after, s);
+  if (v <= 512 * per) return launch<T, 512, 1, 32>(a, after, s);
+  if (v <= 1024 * per) return launch<T, 512, 2, 32>(a, after, s);
+  if (v <= 2048 * per) return launch<T, 512, 4, 32>(a, after, s);
+  if (v <= 4096 * per) return launch<T, 512, 8, 32>(a, after, s);
+  return launch<T, 512, 8, 64>(a, after, s);
 }
 
 }  // namespace
+
+cudaError_t label_rows_launch(const LabelArgs& o, const void* x, int dtype, int64_t ld, int n, int C, bool after, cudaStream_t s) {
+  const RowsArgs a{o, x, n > 1 ? ld : 0, n, C};
+  return dtype == TSD_F32    ? launch_type<float>(a, after, s)
+         : dtype == TSD_BF16 ? launch_type<__nv_bfloat16>(a, after, s)
+                             : launch_type<__half>(a, after, s);
+}
 
 tsd_status label_check(const char* who, int32_t n, int32_t most_n, int32_t C, float temperature, int32_t m,
                        const int32_t* labels, int32_t k, const float* logp, const int32_t* alt_labels, const float* alt_logp) {
@@ -365,8 +417,7 @@ extern "C" tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits,
   if (dtype != TSD_F32 && dtype != TSD_BF16 && dtype != TSD_F16) return fail(TSD_EINVAL, "%s: unknown dtype %d", who, dtype);
   if (n > 1 && row_stride < C) return fail(TSD_EINVAL, "%s: row_stride=%lld below C=%d", who, (long long)row_stride, C);
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == TSD_F32 ? 4 : 2)) return fail(TSD_EINVAL, "%s: logits not aligned to their type", who);
-  RowsArgs a{{m, k, labels, logp, entropy, alt_labels, alt_logp, 1.f / temperature}, logits, n > 1 ? row_stride : 0, n, C};
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  TSD_CUDA(dtype == TSD_F32 ? launch_type<float>(a, s) : dtype == TSD_BF16 ? launch_type<__nv_bfloat16>(a, s) : launch_type<__half>(a, s));
+  const LabelArgs o{m, k, labels, logp, entropy, alt_labels, alt_logp, 1.f / temperature};
+  TSD_CUDA(label_rows_launch(o, logits, dtype, row_stride, n, C, false, static_cast<cudaStream_t>(cuda_stream)));
   return TSD_OK;
 }

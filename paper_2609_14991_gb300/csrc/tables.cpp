@@ -65,6 +65,19 @@ namespace {
 std::atomic<int32_t> g_fail_alloc{0};  // allocations left before the injected failure (0: off)
 }  // namespace
 
+cudaError_t device_sms(int* sms) {
+  static std::atomic<int> known[64];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  *sms = dev < 64 ? known[dev].load() : 0;
+  if (*sms == 0) {
+    e = cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess && dev < 64) known[dev].store(*sms);
+  }
+  return e;
+}
+
 bool alloc_hook_fires() {
   int32_t n = g_fail_alloc.load();
   while (n > 0) {

@@ -170,10 +170,12 @@ def test_joint_sizes(n, H, C):
     check_joint(n, H, C, 2, 4, seed=n + C)
 
 
-@pytest.mark.parametrize("n,C", [(300, 2000), (1300, 1025), (2500, 2049), (5000, 1000), (2000, 4097)])
+@pytest.mark.parametrize("n,C", [(300, 2000), (1300, 1025), (2500, 2049), (5000, 1000), (2000, 4097), (2600, 4097),
+                                 (9001, 1025), (20000, 513), (40000, 60), (129, 40001)])
 def test_joint_tile_shapes(n, C):
-    """Calls in 128 x 64, 128 x 128 and paired 256 x 256 tiles, one row tile over several workers and several row
-    tiles over one: every row against the 64-bit sums, the labels exactly."""
+    """Calls that store their logits (128 x 64, 128 x 128 and paired tiles) and calls that do not, one row tile over
+    several workers (up to all of them) and several row tiles over one: every row against the 64-bit sums, the
+    labels exactly."""
     A, W = joint_inputs(n, 128, C, n)
     lab = given(n, 2, C, n)
     for k in (0, 3, 8):
@@ -197,24 +199,52 @@ def test_joint_strides():
 
 
 def test_joint_ties_and_equal_rows():
-    """All weights equal: every logit equal, the lowest labels in order; a label outside the row."""
-    n, H, C = 130, 64, 1000
-    A, W = joint_inputs(n, H, C, 1)
-    W = W[:1].repeat(C, 1).contiguous()
-    lab = torch.tensor([[C]] * n, dtype=torch.int32, device=DEV)
-    got = tsd.joint_label_scores(A, W, lab, k=8)
+    """All weights equal: every logit equal, the lowest labels in order; a label outside the row.  Then few
+    distinct weights, so that every logit occurs many times, in runs and scattered, and ascending ones, so
+    that every logit is the best so far."""
+    for n, C in ((130, 1000), (130, 40000), (5000, 2100)):
+        H = 64
+        A, W1 = joint_inputs(n, H, C, 1)
+        W = W1[:1].repeat(C, 1).contiguous()
+        lab = torch.tensor([[C]] * n, dtype=torch.int32, device=DEV)
+        for k in (3, 8):
+            got = tsd.joint_label_scores(A, W, lab, k=k)
+            assert torch.equal(got.alt_labels.cpu(), torch.arange(k, dtype=torch.int32).repeat(n, 1))
+            # all logits are the largest, so every sum counts exact ones
+            assert float((got.alt_logp + math.log(C)).abs().max()) < 1e-5
+            assert float((got.entropy - math.log(C)).abs().max()) < 2e-5
+            assert torch.isnan(got.logp).all()
+        g = torch.Generator().manual_seed(3)
+        for order in (torch.arange(C) // 37 % 23, torch.randint(0, 23, (C,), generator=g), torch.arange(C) * 23 // C):
+            order = order.to(DEV)
+            W = (W1[:23].sort(0).values[order] if order[0] == 0 and order[-1] == 22 else W1[:23][order]).contiguous()
+            got = tsd.joint_label_scores(A, W, None, k=8)
+            x = A.double() @ W.double().t()
+            want = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :8].to(torch.int32)
+            assert torch.equal(got.alt_labels, want), (n, C)
+
+
+def test_joint_ascending_logits():
+    """Every later label is better: the buffers of candidates run full again and again."""
+    n, H, C = 700, 64, 20000
+    A = torch.zeros(n, H, dtype=torch.bfloat16, device=DEV)
+    A[:, 0], A[:, 1] = 1, 1
+    i = torch.arange(C)
+    W = torch.zeros(C, H)
+    W[:, 0], W[:, 1] = i // 128, (i % 128) / 128  # bf16 holds both parts, fp32 their sum
+    got = tsd.joint_label_scores(A, W.to(torch.bfloat16).to(DEV), None, k=8)
+    assert torch.equal(got.alt_labels.cpu(), torch.arange(C - 1, C - 9, -1, dtype=torch.int32).repeat(n, 1))
+    got = tsd.joint_label_scores(A, W.flip(0).to(torch.bfloat16).to(DEV), None, k=8)
     assert torch.equal(got.alt_labels.cpu(), torch.arange(8, dtype=torch.int32).repeat(n, 1))
-    assert float((got.alt_logp + math.log(C)).abs().max()) < 1e-5
-    assert float((got.entropy - math.log(C)).abs().max()) < 2e-5
-    assert torch.isnan(got.logp).all()
 
 
-def test_joint_non_finite_rows():
-    A, W = joint_inputs(260, 64, 300, 2)
+@pytest.mark.parametrize("n,C", [(260, 300), (260, 30000)])
+def test_joint_non_finite_rows(n, C):
+    A, W = joint_inputs(n, 64, C, 2)
     A[3, 5] = math.nan
     A[200, 0] = math.inf
-    got = tsd.joint_label_scores(A, W, torch.zeros(260, dtype=torch.int32, device=DEV), k=2)
-    bad = torch.zeros(260, dtype=torch.bool)
+    got = tsd.joint_label_scores(A, W, torch.zeros(n, dtype=torch.int32, device=DEV), k=2)
+    bad = torch.zeros(n, dtype=torch.bool)
     bad[3] = bad[200] = True
     assert torch.equal(torch.isnan(got.logp).cpu(), bad) and torch.equal(torch.isnan(got.entropy).cpu(), bad)
     assert torch.equal((got.alt_labels == -1).all(1).cpu(), bad) and torch.equal(torch.isnan(got.alt_logp).all(1).cpu(), bad)
