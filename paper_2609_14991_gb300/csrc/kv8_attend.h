@@ -25,12 +25,68 @@ __device__ __forceinline__ uint32_t int_half2(uint32_t x) {
   return r;
 }
 
+template <bool BF16>
+__device__ __forceinline__ float wide16(uint32_t u) {
+  if (BF16) return __uint_as_float(u << 16);
+  return __half2float(__ushort_as_half((unsigned short)u));
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t narrow2(float a, float b) {
+  if (BF16) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+constexpr int kKv8Unit = 16;  // tokens that are sure to share a block
+
+// The key tiles that rows at positions pos0 .. pos1 see: first those of the
+// sinks before the window, then the window's.
+struct KeyTiles {
+  int sink, from, total;  // sink tiles 0 .. sink-1, then tiles from, from + 1, ..
+  __device__ __forceinline__ int token(int j) const { return kKv8Unit * (j < sink ? j : from + j - sink); }
+};
+__device__ __forceinline__ KeyTiles key_tiles(int pos0, int pos1, int window, int sinks) {
+  const int first = window > 0 ? max(0, pos0 - window + 1) : 0;
+  KeyTiles k;
+  k.sink = (min(sinks, first) + kKv8Unit - 1) / kKv8Unit;
+  k.from = max(k.sink, first / kKv8Unit);
+  k.total = k.sink + pos1 / kKv8Unit + 1 - k.from;
+  return k;
+}
+
+// The power of two that brings a row's largest magnitude into [2^14, 2^15) (2^126 at
+// most); fine: false for NaN and infinity.
+struct QueryScale {
+  float f;
+  bool fine;
+};
+__device__ __forceinline__ QueryScale query_scale(float top) {
+  const int ex = (int)(__float_as_uint(top) >> 23);
+  const bool fine = ex < 255;
+  return {__uint_as_float((uint32_t)(fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127) << 23), fine};
+}
+
 // Few rows per key head (kv8_rows.cu): row tiles of 16 x mw, the keys over `splits` CTAs.
 struct Kv8RowsPlan {
   int mw = 1, mtiles = 1, splits = 1;
   int64_t bytes = 0;  // workspace
 };
 Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int window, int sinks, int sms);
-cudaError_t kv8_rows_launch(Kv8Attend a, const Kv8RowsPlan& p, void* workspace, cudaStream_t s);
+cudaError_t kv8_rows_launch(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s);
+
+// Many (kv8_tiles.cu): row tiles of 256.  false: kv8_rows.cu is the better one.
+struct Kv8TilesPlan {
+  int mtiles = 0, splits = 1;
+  int64_t bytes = 0;
+};
+bool kv8_tiles_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int window, int sinks, int sms, Kv8TilesPlan* p);
+cudaError_t kv8_tiles_launch(const Kv8Attend& a, const Kv8TilesPlan& p, cudaStream_t s);
+
+// Joins the splits' partial results (kv8_rows.cu).
+cudaError_t kv8_join_launch(const Kv8Attend& a, int splits, cudaStream_t s);
 
 }  // namespace tsd

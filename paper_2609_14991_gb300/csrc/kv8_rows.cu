@@ -38,7 +38,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int kTile = 16;  // keys per tile
+constexpr int kTile = kKv8Unit;  // keys per tile
 
 template <int DIM, int MW>
 struct RowsShape {
@@ -56,37 +56,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-template <bool BF16>
-__device__ __forceinline__ float wide16(uint32_t u) {
-  if (BF16) return __uint_as_float(u << 16);
-  return __half2float(__ushort_as_half((unsigned short)u));
-}
-
-template <bool BF16>
-__device__ __forceinline__ uint32_t narrow2(float a, float b) {
-  if (BF16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-
-// The key tiles that rows at positions pos0 .. pos1 see: first those of the
-// sinks before the window, then the window's.
-struct KeyTiles {
-  int sink, from, total;  // sink tiles 0 .. sink-1, then tiles from, from + 1, ..
-  __device__ __forceinline__ int token(int j) const { return kTile * (j < sink ? j : from + j - sink); }
-};
-__device__ __forceinline__ KeyTiles key_tiles(int pos0, int pos1, int window, int sinks) {
-  const int first = window > 0 ? max(0, pos0 - window + 1) : 0;
-  KeyTiles k;
-  k.sink = (min(sinks, first) + kTile - 1) / kTile;
-  k.from = max(k.sink, first / kTile);
-  k.total = k.sink + pos1 / kTile + 1 - k.from;
-  return k;
 }
 
 template <bool BF16, int DIM, int MW>
@@ -162,12 +131,9 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
         top = odd ? INFINITY : top;
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // f brings the row's largest magnitude into [2^14, 2^15)
-        const int ex = (int)(__float_as_uint(top) >> 23);
-        const bool fine = ex < 255;
-        const int fe = fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127;
-        const float f = __uint_as_float((uint32_t)fe << 23);
-        rc[h] = fine ? a.scale * kLog2e / f : __uint_as_float(0x7fc00000u);
+        const QueryScale qs = query_scale(top);
+        const float f = qs.f;
+        rc[h] = qs.fine ? a.scale * kLog2e / f : __uint_as_float(0x7fc00000u);
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
           qf[kk][h] = narrow2<false>(wide16<BF16>(w[kk].x & 0xffffu) * f, wide16<BF16>(w[kk].x >> 16) * f);
@@ -433,15 +399,16 @@ cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t
 
 template <bool BF16, int DIM>
 cudaError_t launch_mw(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
-  cudaError_t e = p.mw == 1 ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
-                : p.mw == 2 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
-                            : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
-  if (e == cudaSuccess && p.splits > 1) {
-    const size_t items = (size_t)a.b.rows * a.heads;
-    k_kv8_join<BF16, DIM><<<(unsigned)((items + 3) / 4), 128, 0, s>>>(a, p.splits);
-    e = cudaGetLastError();
-  }
-  return e;
+  return p.mw == 1   ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
+         : p.mw == 2 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
+                     : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
+}
+
+template <bool BF16, int DIM>
+cudaError_t launch_join(const Kv8Attend& a, int splits, cudaStream_t s) {
+  const size_t items = (size_t)a.b.rows * a.heads;
+  k_kv8_join<BF16, DIM><<<(unsigned)((items + 3) / 4), 128, 0, s>>>(a, splits);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -466,62 +433,17 @@ Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, i
   return p;
 }
 
-cudaError_t kv8_rows_launch(Kv8Attend a, const Kv8RowsPlan& p, void* workspace, cudaStream_t s) {
-  a.part = static_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(a.part + (p.splits > 1 ? (size_t)p.splits * a.b.rows * a.heads * a.c.dim : 0));
+cudaError_t kv8_join_launch(const Kv8Attend& a, int splits, cudaStream_t s) {
   const bool bf = a.c.dtype == TSD_BF16;
-  if (a.c.dim == 64) return bf ? launch_mw<true, 64>(a, p, s) : launch_mw<false, 64>(a, p, s);
-  return bf ? launch_mw<true, 128>(a, p, s) : launch_mw<false, 128>(a, p, s);
+  if (a.c.dim == 64) return bf ? launch_join<true, 64>(a, splits, s) : launch_join<false, 64>(a, splits, s);
+  return bf ? launch_join<true, 128>(a, splits, s) : launch_join<false, 128>(a, splits, s);
+}
+
+cudaError_t kv8_rows_launch(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
+  const bool bf = a.c.dtype == TSD_BF16;
+  const cudaError_t e = a.c.dim == 64 ? (bf ? launch_mw<true, 64>(a, p, s) : launch_mw<false, 64>(a, p, s))
+                                      : (bf ? launch_mw<true, 128>(a, p, s) : launch_mw<false, 128>(a, p, s));
+  return e == cudaSuccess && p.splits > 1 ? kv8_join_launch(a, p.splits, s) : e;
 }
 
 }  // namespace tsd
-
-using namespace tsd;
-
-static tsd_status attend_check(const char* who, const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads, int32_t window, int32_t sinks) {
-  if (tsd_status st = kv8_check(who, cache, batch)) return st;
-  if (heads < 1 || heads % cache->kv_heads || heads / cache->kv_heads > 64)
-    return fail(TSD_EINVAL, "%s: heads=%d must be 1..64 times kv_heads=%d", who, heads, cache->kv_heads);
-  if (heads > 1024) return fail(TSD_EINVAL, "%s: heads=%d above 1024", who, heads);
-  if (window < 0 || sinks < 0) return fail(TSD_EINVAL, "%s: negative window=%d or sinks=%d", who, window, sinks);
-  return TSD_OK;
-}
-
-extern "C" tsd_status tsd_kv8_attend_workspace(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads,
-                                               int32_t window, int32_t sinks, int64_t* bytes) {
-  clear_error();
-  if (!bytes) return fail(TSD_EINVAL, "tsd_kv8_attend_workspace: NULL argument");
-  if (tsd_status st = attend_check("tsd_kv8_attend_workspace", cache, batch, heads, window, sinks)) return st;
-  int sms = 0;
-  TSD_CUDA(device_sms(&sms));
-  *bytes = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms).bytes;
-  return TSD_OK;
-}
-
-extern "C" tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads, const void* q,
-                                     int64_t q_row, int64_t q_head, float scale, int32_t window, int32_t sinks, void* out,
-                                     int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
-                                     void* cuda_stream) {
-  clear_error();
-  if (tsd_status st = attend_check("tsd_kv8_attend", cache, batch, heads, window, sinks)) return st;
-  if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "q", q, q_row, q_head)) return st;
-  if (tsd_status st = kv8_check_rows("tsd_kv8_attend", "out", out, out_row, out_head)) return st;
-  int sms = 0;
-  TSD_CUDA(device_sms(&sms));
-  const Kv8RowsPlan p = kv8_rows_plan(*cache, *batch, heads, window, sinks, sms);
-  if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
-    return fail(TSD_EINVAL, "tsd_kv8_attend: workspace of %lld bytes, %lld needed (16-byte aligned)", (long long)workspace_bytes, (long long)p.bytes);
-  Kv8Attend a{};
-  a.c = *cache;
-  a.b = *batch;
-  a.q = static_cast<const uint16_t*>(q);
-  a.out = static_cast<uint16_t*>(out);
-  a.q_row = q_row, a.q_head = q_head, a.out_row = out_row, a.out_head = out_head;
-  a.heads = heads;
-  a.group = heads / cache->kv_heads;
-  a.window = window;
-  a.sinks = sinks;
-  a.scale = scale;
-  TSD_CUDA(kv8_rows_launch(a, p, workspace, static_cast<cudaStream_t>(cuda_stream)));
-  return TSD_OK;
-}

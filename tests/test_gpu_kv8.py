@@ -167,6 +167,54 @@ def test_prompts():
         b.check_attend(counts, heads, window=window, sinks=5 if window else 0)
 
 
+@pytest.mark.parametrize("dim,dtype", [(64, torch.bfloat16), (128, torch.float16)])
+@pytest.mark.parametrize("heads,kv,counts,past,window,sinks", [
+    (1, 1, [100, 128, 129], [0, 1, 15], 0, 0),        # one row tile, whole and not
+    (1, 1, [256, 257, 385], [16, 0, 100], 0, 0),      # two, and the first of the next pair
+    (3, 1, [97, 171, 0], [300, 5, 40], 0, 0),         # a group that does not divide a tile
+    (4, 2, [200, 33, 130], [0, 700, 64], 0, 0),
+    (2, 1, [300, 64, 150], [20, 400, 129], 50, 0),    # windows inside a tile, across tiles, with sinks
+    (2, 2, [150, 260, 128], [200, 333, 1000], 200, 4),
+    (8, 1, [40, 13, 100], [600, 20, 0], 17, 33),
+    (64, 1, [7, 2, 9], [1000, 0, 90], 0, 0),
+])
+def test_row_tiles(heads, kv, counts, past, window, sinks, dim, dtype):
+    """Prompts in tiles of 128 rows and 128 keys; also with hints that split their keys over CTAs, and
+    hints too small, so that a CTA takes several row tiles."""
+    b = Batch(tsd, [p + c for p, c in zip(past, counts)], kv, 16 if window else 64, dim, dtype, seed=heads + dim)
+    b.append(past)
+    b.append(counts)
+    b.check_held()
+    for kw in (dict(max_new=max(counts)), dict(max_new=96, max_len=64)):
+        b.check_attend(counts, heads, window=window, sinks=sinks, **kw)
+
+
+def test_row_tiles_of_spoilt_rows_and_blocks():
+    """NaN reaches the rows that see it in the tiled form too, and a bad sequence is all NaN."""
+    b = Batch(tsd, [400, 300], 1, 16, 64, seed=3)
+    k, v = b.rows(700, 1), b.rows(700, 1)
+    v[100, 0, 2] = math.nan  # block 6 of sequence 0
+    b.append([400, 300], k=k, v=v)
+    a = b.args([400, 300])
+    q = b.rows(700, 2)
+    q[250, 1, 0] = math.inf
+    out = b.cache.attend(q, window=120, sinks=3, max_new=400, **a)
+    pos = torch.arange(400)
+    bad = torch.zeros(700, 2, dtype=torch.bool)
+    bad[:400][(pos >= 96) & (pos - 119 <= 111)] = True
+    bad[250, 1] = True
+    assert torch.equal(torch.isnan(out).all(2).cpu(), bad) and torch.equal(torch.isnan(out).any(2).cpu(), bad)
+    t = b.table.clone()
+    t[b.slots[1], 2] = b.cache.n_blocks
+    out = b.cache.attend(q[400:], max_new=300, **{**a, "table": t, "slots": a["slots"][1:].contiguous(),
+                                                  "starts": torch.tensor([0, 300], dtype=torch.int32, device="cuda")})
+    assert bool(torch.isnan(out[32:]).all()) and not bool(torch.isnan(out[:32]).any())
+    lens = a["lens"].clone()
+    lens[b.slots[1]] = 299
+    out2 = b.cache.attend(q, window=120, sinks=3, max_new=400, **{**a, "lens": lens})
+    assert bool(torch.isnan(out2[400:]).all()) and torch.equal(torch.isnan(out2[:400]).all(2).cpu(), bad[:400])
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 def test_long_contexts_over_several_ctas(dim):
     """Contexts split over CTAs and joined; the largest value at the far end, and scores of a wide range."""
