@@ -644,7 +644,7 @@ typedef struct {
   float *k_scale, *v_scale;
   void *k_tail, *v_tail;
   int32_t dtype;    /* TSD_BF16 or TSD_F16: tails, new keys and values, queries, results */
-  int32_t n_blocks; /* blocks of the pool */
+  int32_t n_blocks; /* blocks of the pool; n_blocks * kv_heads * block below 2^32 - 64 */
   int32_t kv_heads; /* 1..1024 */
   int32_t block;    /* tokens per block: 16, 32 or 64 */
   int32_t dim;      /* head dimension: 64 or 128 */

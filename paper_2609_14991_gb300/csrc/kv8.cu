@@ -203,6 +203,8 @@ tsd_status kv8_check(const char* who, const tsd_kv8* c, const tsd_kv8_batch* b) 
   if (c->dim != 64 && c->dim != 128) return fail(TSD_EINVAL, "%s: dim=%d is not 64 or 128", who, c->dim);
   if (c->kv_heads < 1 || c->kv_heads > 1024) return fail(TSD_EINVAL, "%s: kv_heads=%d outside [1, 1024]", who, c->kv_heads);
   if (c->n_blocks < 1 || c->n_slots < 1) return fail(TSD_EINVAL, "%s: n_blocks=%d and n_slots=%d must be positive", who, c->n_blocks, c->n_slots);
+  if ((int64_t)c->n_blocks * c->kv_heads * c->block > UINT32_MAX - 64)
+    return fail(TSD_EINVAL, "%s: n_blocks=%d x kv_heads=%d x block=%d above 2^32 rows", who, c->n_blocks, c->kv_heads, c->block);
   if (!b->lens || !b->table) return fail(TSD_EINVAL, "%s: NULL lens or table", who);
   if (b->n < 1 || b->n > 65535) return fail(TSD_EINVAL, "%s: n=%d outside [1, 65535]", who, b->n);
   if (b->table_width < 1 || (int64_t)b->table_width * c->block > INT32_MAX - 64)

@@ -4,22 +4,27 @@
 // The mathematics is kv8_rows.cu's; the products run on tcgen05 (fp16 in, fp32
 // accumulate in TMEM).  A CTA takes 256 rows of a sequence and key head (row =
 // token * group + head of the group) as two tiles of 128, and the keys they see in
-// tiles of 128:
+// tiles of 128, 64 at a time:
 //   warps 0-7   softmax: a thread is a row (warps 0-3 tile 0, 4-7 tile 1), so its
-//               maximum, sum and masks need no exchange.  Reads its scores from TMEM,
+//               maximum, sum and masks need no exchange.  Reads its 64 scores from TMEM,
 //               leaves probabilities (fp16) in their place as the values'
 //               product's A operand;
-//   warps 8-11  turn the integers of the next key tile into fp16 in shared memory
-//               (128-byte swizzle), once for both row tiles and all heads of a group;
-//   warp 12     issues the MMAs: while one tile's softmax runs, the other tile's
-//               products do.
-// Keys are the K-major B operand of the scores; the same layout of the values is read as
-// an MN-major B operand, so neither is transposed.  A tile's accumulator is rescaled in
-// TMEM only when a row's maximum grows by more than 2^8.
+//   warps 8-15  turn the integers of the next key tile into fp16 in shared memory
+//               (128-byte swizzle; warps 8-11 keys, 12-15 values), once for both row
+//               tiles and all heads of a group;
+//   warp 16     issues the MMAs.
+// Registers go to where they are used (setmaxnreg): 152 for softmax, 64 for conversion.
+// Each row tile has two score buffers of 64 keys: the scores of step i + 2 are computed
+// as soon as the values' product of step i has read its probabilities, so the softmax
+// never waits for a product that waits for it.  (With one buffer of 128 keys a tile's
+// softmax, 3700 clocks, and its products, 1600, took turns.)  Keys are the K-major B
+// operand of the scores; the same layout of the values is read as an MN-major B
+// operand, so neither is transposed.  The accumulator is rescaled in TMEM only when a row's maximum
+// grows by more than 2^8.
 //
-// What bounds it at dim 128: per key tile and CTA the MMAs take 2080 clocks, the
-// hardware's 2^x 2048 (256 x 128 of them at 16 per clock), beside 1400 issue slots per
-// scheduler for scores, probabilities and conversions.
+// What bounds it at dim 128, per 128 keys: the MMAs take 2600 clocks (49 for 128 x 64 x
+// 16, whose operands come from shared memory at 128 bytes per clock, 65 for 128 x 128 x
+// 16 with A in TMEM), the hardware's 2^x 2048 (256 x 128 at 16 per clock).
 #include <algorithm>
 #include <climits>
 
@@ -35,8 +40,14 @@ using namespace tc;
 constexpr int kUnit = kKv8Unit;
 constexpr int kKeys = 128;            // keys per tile
 constexpr int kUnits = kKeys / kUnit;
-constexpr int kSoftWarps = 8, kConvWarps = 4;
-constexpr int kThreads = 32 * (kSoftWarps + kConvWarps + 1);
+constexpr int kStep = 64;             // keys per step
+constexpr int kStepUnits = kStep / kUnit;
+constexpr int kSoftWarps = 8, kConvWarps = 4;  // softmax; conversion of keys, and as many of values
+constexpr int kMmaWarp = kSoftWarps + 2 * kConvWarps;
+constexpr int kThreads = 32 * (kMmaWarp + 4);  // whole warpgroups: three warps of the last have no work
+constexpr int kSoftRegs = 152, kConvRegs = 64, kMmaRegs = 40;
+constexpr int kLaunchRegs = 96;  // per thread, what the launch has to bring
+static_assert(32 * kSoftWarps * kSoftRegs + 64 * kConvWarps * kConvRegs + 128 * kMmaRegs <= kThreads * kLaunchRegs, "register split");
 
 template <int DIM>
 struct TilesShape {
@@ -47,7 +58,7 @@ struct TilesShape {
   static constexpr int kV = 4 * kTileBytes;             // two stages
   static constexpr int kBar = 6 * kTileBytes;
   static constexpr int kSmem = kBar + 256 + 1024;
-  static constexpr int kO = 256;  // TMEM: scores of the tiles at 0 and 128, accumulators from here
+  static constexpr int kO = 256;  // TMEM: the row tiles' two score buffers at 0, 64 and 128, 192; accumulators from here
 };
 
 // fp16 operands, fp32 accumulate; bTrans: B is MN-major
@@ -79,6 +90,29 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
       : "memory");
 }
 
+// 64 consecutive columns of this warp's 32 lanes.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -96,19 +130,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBar);
   uint64_t *k_full = bars, *k_empty = bars + 2, *v_full = bars + 4, *v_empty = bars + 6;  // [2] stages
-  uint64_t *s_full = bars + 8, *p_full = bars + 10, *o_full = bars + 12;                    // [2] row tiles
-  uint64_t *q_full = bars + 14, *drain = bars + 15;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 16);
+  uint64_t *s_full = bars + 8, *p_full = bars + 12;  // [row tile][buffer]
+  uint64_t *o_done = bars + 16, *o_full = bars + 18;  // [2] row tiles: a step's values' product, the last one's
+  uint64_t *q_full = bars + 20, *drain = bars + 21;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
+  volatile int* lost = reinterpret_cast<volatile int*>(bars + 23);  // a wait ran out
 
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
-  const int head = blockIdx.y % a.c.kv_heads, split = blockIdx.y / a.c.kv_heads, splits = gridDim.y / a.c.kv_heads;
+  const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.y);
+  const int head = blockIdx.x % a.c.kv_heads, split = blockIdx.x / a.c.kv_heads, splits = gridDim.x / a.c.kv_heads;
   const int rows = q.count * a.group;
   const int mts = (rows + 255) / 256;
-  if ((int)blockIdx.x >= mts) return;
+  if ((int)blockIdx.z >= mts) return;
 
-  const auto say_nan = [&](int row0) {
-    for (int e = threadIdx.x; e < 256 * (DIM / 8); e += kThreads) {
+  const auto say_nan = [&](int row0, int threads) {
+    for (int e = threadIdx.x; e < 256 * (DIM / 8); e += threads) {
       const int r = row0 + e / (DIM / 8), col = 8 * (e % (DIM / 8));
       if (r >= rows) break;
       const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
@@ -120,7 +156,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     }
   };
   if (!q.ok) {
-    for (int mt = blockIdx.x; mt < mts; mt += gridDim.x) say_nan(mt * 256);
+    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) say_nan(mt * 256, kThreads);
     return;
   }
 
@@ -130,15 +166,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
       mbar_init(v_full + i, kConvWarps);
       mbar_init(k_empty + i, 1);
       mbar_init(v_empty + i, 1);
+      mbar_init(o_done + i, 1);
+      mbar_init(o_full + i, 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);
-      mbar_init(o_full + i, 1);
     }
     mbar_init(q_full, kSoftWarps);
     mbar_init(drain, 1);
+    *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kSoftWarps + kConvWarps) {
+  if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -146,24 +186,54 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-
   const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
   const int before = q.len - q.count;
-  // the barriers' positions: key tiles so far (of row tile 0, of row tile 1), row tiles, and those with keys
-  int at0 = 0, at1 = 0, mi = 0, done0 = 0, done1 = 0;
-  bool dead = false;  // a wait ran out: NaN from there on
-  for (int mt = blockIdx.x; mt < mts; mt += gridDim.x, ++mi) {
-    // the later rows see the most keys: they go first
-    const int row0 = (mts - 1 - mt) * 256;
-    const bool two = rows - row0 > 128;
-    const KeyTiles units = key_tiles(before + row0 / a.group, before + (min(rows, row0 + 256) - 1) / a.group, a.window, a.sinks);
-    const int all = (units.total + kUnits - 1) / kUnits;
-    const int lo = (int)((int64_t)all * split / splits), n = (int)((int64_t)all * (split + 1) / splits) - lo;
+  const int shift = __ffs(a.c.block) - 1;  // tokens per block: 16, 32 or 64
+  // a row tile of 256 and its share of the keys
+  struct Part {
+    int row0, lo, n, steps;  // first row; first key tile, key tiles and steps
+    bool two;
+    KeyTiles units;
+  };
+  const auto part_of = [&](int mt) {
+    Part p;
+    p.row0 = (mts - 1 - mt) * 256;  // the later rows see the most keys: they go first, of all heads and sequences
+    p.two = rows - p.row0 > 128;
+    p.units = key_tiles(before + p.row0 / a.group, before + (min(rows, p.row0 + 256) - 1) / a.group, a.window, a.sinks);
+    const int all = (p.units.total + kUnits - 1) / kUnits;
+    p.lo = (int)((int64_t)all * split / splits);
+    p.n = (int)((int64_t)all * (split + 1) / splits) - p.lo;
+    p.steps = (min(p.units.total, (p.lo + p.n) * kUnits) - p.lo * kUnits + kStepUnits - 1) / kStepUnits;
+    return p;
+  };
+  // Every role walks the row tiles by itself (each has registers of its own number); between
+  // two of them all meet.  False once a wait has run out anywhere: the rows from
+  // there on say NaN.
+  const auto meet = [&](bool dead) {
+    if (dead) *lost = 1;
+    asm volatile("bar.sync 1, %0;" ::"n"(32 * (kMmaWarp + 1)) : "memory");
+    return *lost == 0;
+  };
 
-    if (dead) {
-      say_nan(row0);
-    } else if (warp < kSoftWarps) {
-      const int tile = warp >> 2, r = row0 + threadIdx.x;
+  if (warp > kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    return;
+  }
+  if (warp < kSoftWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int tile = warp >> 2;
+    int at0 = 0, done = 0;  // the barriers' positions: steps and row tiles with steps so far
+    int mt = blockIdx.z;
+    for (bool fine = true; mt < mts; mt += gridDim.z) {
+      const Part pt = part_of(mt);
+      const int row0 = pt.row0, lo = pt.lo, n = pt.n, steps = pt.steps;
+      const KeyTiles& units = pt.units;
+      if (!fine) {
+        say_nan(row0, 32 * kSoftWarps);
+        continue;
+      }
+      bool dead = false;
+      const int r = row0 + threadIdx.x;
       const bool live = r < rows;
       const int tok = min(r, rows - 1) / a.group, pos = before + tok;
       // the row's queries as fp16, scaled by f into [2^14, 2^15)
@@ -183,8 +253,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
             odd = odd || !(x + y <= INFINITY);
           }
         }
+        // (a negative scale's sign too, so that a larger product is a larger score)
         const QueryScale qs = query_scale(odd ? INFINITY : top);
-        rc = qs.fine ? a.scale * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
+        rc = qs.fine ? fabsf(a.scale) * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
+        const float f = a.scale < 0.f ? -qs.f : qs.f;
         // the last row tile's products have read the rows before these: its accumulators were waited for
         const int rr = threadIdx.x & 127;
         unsigned char* dst = smem + S::kQ + tile * S::kTileBytes + rr * 128;
@@ -194,14 +266,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           const uint32_t u[4] = {w.x, w.y, w.z, w.w};
           uint32_t y[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) y[j] = narrow2<false>(wide16<BF16>(u[j] & 0xffffu) * qs.f, wide16<BF16>(u[j] >> 16) * qs.f);
+          for (int j = 0; j < 4; ++j) y[j] = narrow2<false>(wide16<BF16>(u[j] & 0xffffu) * f, wide16<BF16>(u[j] >> 16) * f);
           *reinterpret_cast<uint4*>(dst + (i >> 3) * S::kHalf + (((i & 7) ^ (rr & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
         }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(q_full);
       }
-      if (tile == 0 || two) {
+      if (tile == 0 || pt.two) {
         const uint32_t st = tmem + (uint32_t)(tile * 128) + ((uint32_t)((warp & 3) * 32) << 16);  // scores, then probabilities
         const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
         // positions that every row of the warp sees
@@ -209,110 +281,125 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         const int all_to = before + min(wr, rows - 1) / a.group;
         const int all_from = a.window > 0 ? before + min(wr + 31, rows - 1) / a.group - a.window + 1 : 0;
         float m = -INFINITY, l = 0.f;
-        // lane u < 8: scales of the next key tile's unit u
         const float nan = __uint_as_float(0x7fc00000u);
-        float na = nan, nc = nan;
-        const auto fetch = [&](int j) {
+        // lane u < 8: the scales of the next key tile's unit u, and the block of the one after's: no
+        // load waits for another
+        const auto block_of = [&](int j) {
           const int u = (lo + j) * kUnits + lane;
+          return lane < kUnits && u < units.total && j < n ? __ldg(table + (units.token(u) >> shift)) : -1;
+        };
+        float na = nan, nc = nan;
+        const auto fetch = [&](int id) {
           na = nc = nan;
-          if (lane < kUnits && u < units.total) {
-            const int id = __ldg(table + units.token(u) / a.c.block);
-            if (id >= 0 && id < a.c.n_blocks) {
-              na = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
-              nc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
-            }
+          if (id >= 0 && id < a.c.n_blocks) {
+            na = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
+            nc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
           }
         };
-        if (n > 0) fetch(0);
-        for (int j = 0; j < n; ++j) {
-          const float ua = na, uc = nc == 0.f ? 0x1p-80f : nc;
-          const float ul = log2f(uc), ui = 1.f / uc;
-          if (j + 1 < n) fetch(j + 1);
-          if (!mbar_wait(s_full + tile, (uint32_t)((tile ? at1 : at0) + j) & 1u)) {
+        fetch(block_of(0));
+        int id1 = block_of(1);
+        float ua = nan, ul = nan, ui = nan;
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+          if ((i & 1) == 0) {  // a key tile's scales
+            const float uc = nc == 0.f ? 0x1p-80f : nc;
+            ua = na;
+            ul = log2f(uc);
+            ui = 1.f / uc;
+            fetch(id1);
+            id1 = block_of((i >> 1) + 2);
+          }
+          const int at = at0 + i, buf = at & 1;
+          if (!__all_sync(0xffffffffu, mbar_wait(s_full + 2 * tile + buf, (uint32_t)(at >> 1) & 1u))) {
             dead = true;
             break;
           }
           fence_after();
-          const int u0 = (lo + j) * kUnits;
-          const int t_lo = units.token(u0), t_hi = units.token(min(u0 + kUnits, units.total) - 1) + kUnit - 1;
-          const bool whole = u0 + kUnits <= units.total && t_hi <= all_to && (t_lo >= all_from || t_hi < a.sinks);
-          // s' of a unit's 16 scores, masked
-          const auto scores = [&](const float* v, int u, float* s) {
-            const float c = rc * __shfl_sync(0xffffffffu, ua, u), lc = __shfl_sync(0xffffffffu, ul, u);
+          const uint32_t sb = st + (uint32_t)(buf * kStep);
+          uint32_t raw[kStep];
+          tmem_ld64(sb, raw);
+          float v[kStep];
 #pragma unroll
-            for (int i = 0; i < kUnit; ++i) s[i] = fmaf(v[i], c, lc);
-            if (!whole) {
-              const int t0 = units.token(u0 + u);
-              const int lim = u0 + u < units.total ? pos - t0 : -1;  // the row sees the unit's keys up to here
-              const int from = a.window > 0 && lim >= 0 ? lim - a.window : INT_MIN, sk = a.sinks - t0;
+          for (int e = 0; e < kStep; ++e) v[e] = __uint_as_float(raw[e]);
+          const int u0 = lo * kUnits + i * kStepUnits, w0 = kStepUnits * (i & 1);  // the step's first unit; in its tile
+          const int t_lo = units.token(u0), t_hi = units.token(min(u0 + kStepUnits, units.total) - 1) + kUnit - 1;
+          const bool whole = u0 + kStepUnits <= units.total && t_hi <= all_to && (t_lo >= all_from || t_hi < a.sinks);
+          // a unit's products, masked where a row does not see all of the step
+          const auto mask = [&](float* x, int u) {
+            const int t0 = units.token(u0 + u);
+            const int lim = u0 + u < units.total ? pos - t0 : -1;  // the row sees the unit's keys up to here
+            const int from = a.window > 0 && lim >= 0 ? lim - a.window : INT_MIN, sk = a.sinks - t0;
 #pragma unroll
-              for (int i = 0; i < kUnit; ++i)
-                if (!(i <= lim && (i > from || i < sk))) s[i] = -INFINITY;
-            }
+            for (int e = 0; e < kUnit; ++e)
+              if (!(e <= lim && (e > from || e < sk))) x[e] = -INFINITY;
           };
-          float top = -INFINITY;
+          float c[kStepUnits], lc[kStepUnits], top = -INFINITY;
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            float v[32], s[16];
-            tmem_ld32(st + 32 * ch, v);
+          for (int u = 0; u < kStepUnits; ++u) {
+            c[u] = rc * __shfl_sync(0xffffffffu, ua, w0 + u);
+            lc[u] = __shfl_sync(0xffffffffu, ul, w0 + u);
+            if (!whole) mask(v + kUnit * u, u);
+            float x = v[kUnit * u];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              scores(v + 16 * h, 2 * ch + h, s);
-#pragma unroll
-              for (int i = 0; i < kUnit; ++i) top = fmaxf(top, s[i]);
-            }
+            for (int e = 1; e < kUnit; ++e) x = fmaxf(x, v[kUnit * u + e]);
+            if (x > -INFINITY) top = fmaxf(top, fmaf(x, c[u], lc[u]));  // c >= 0: the largest product has the largest score
           }
           if (__any_sync(0xffffffffu, top > m + 8.f)) {
             const float x = fmaxf(m, top);
             const float w = x == m ? 1.f : ex2_approx(m - x);
             m = x;
             l *= w;
-            if (j > 0) {  // the values' products so far are done: the scores came after them
+            if (i > 0) {  // the accumulator, once the last step's values are in it (those before are: this step's scores came after them)
+              if (!__all_sync(0xffffffffu, mbar_wait(o_done + tile, (uint32_t)(at - 1) & 1u))) {
+                dead = true;
+                break;
+              }
+              fence_after();
+#pragma unroll 1
+              for (int ch = 0; ch < DIM / 16; ++ch) {
+                float y[16];
+                tmem_ld16(ot + 16 * ch, y);
+                uint32_t z[16];
 #pragma unroll
-              for (int ch = 0; ch < DIM / 32; ++ch) {
-                float v[32];
-                tmem_ld32(ot + 32 * ch, v);
-                uint32_t y[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) y[i] = __float_as_uint(v[i] * w);
-                tmem_st16(ot + 32 * ch, y);
-                tmem_st16(ot + 32 * ch + 16, y + 16);
+                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(y[e] * w);
+                tmem_st16(ot + 16 * ch, z);
               }
             }
           }
           const float ref = m == -INFINITY ? 0.f : m - 7.f;
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            float v[32];
-            tmem_ld32(st + 32 * ch, v);
-            uint32_t y[16];
+          for (int u = 0; u < kStepUnits; ++u) {
+            float* x = v + kUnit * u;
+            const float lr = lc[u] - ref, ic = __shfl_sync(0xffffffffu, ui, w0 + u);
+            const uint64_t c2 = pair_of(c[u], c[u]), l2 = pair_of(lr, lr);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float s[16];
-              scores(v + 16 * h, 2 * ch + h, s);
-              const float ic = __shfl_sync(0xffffffffu, ui, 2 * ch + h);
-              float sum = 0.f;
+            for (int e = 0; e < kUnit; e += 2) unpair(fma2(pair_of(x[e], x[e + 1]), c2, l2), x[e], x[e + 1]);
+            if (!whole) mask(x, u);
+            uint32_t y[kUnit / 2];
+            uint64_t sum = 0;
 #pragma unroll
-              for (int i = 0; i < kUnit; i += 2) {
-                const float p0 = ex2_approx(s[i] - ref), p1 = ex2_approx(s[i + 1] - ref);
-                sum += p0 + p1;
-                y[8 * h + i / 2] = narrow2<false>(p0, p1);
-              }
-              if (sum != 0.f) l = fmaf(sum, ic, l);  // a unit that the row does not see may have a NaN scale
+            for (int e = 0; e < kUnit; e += 2) {
+              const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
+              sum = add2(sum, pair_of(p0, p1));
+              y[e / 2] = narrow2<false>(p0, p1);
             }
-            tmem_st16(st + 16 * ch, y);
+            float s0, s1;
+            unpair(sum, s0, s1);
+            s0 += s1;
+            if (s0 != 0.f) l = fmaf(s0, ic, l);  // a unit that the row does not see may have a NaN scale
+            tmem_st8(sb + 8 * u, y);
           }
           tmem_st_wait();
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + tile);
+          if (lane == 0) mbar_arrive(p_full + 2 * tile + buf);
         }
-        if (n > 0 && !dead && !mbar_wait(o_full + tile, (uint32_t)(tile ? done1 : done0) & 1u)) dead = true;
+        if (steps > 0 && !dead && !mbar_wait(o_full + tile, (uint32_t)done & 1u)) dead = true;
         fence_after();
         if (__any_sync(0xffffffffu, dead)) l = nan;
         // a row's results: its own contiguous DIM values
         const int h = head * a.group + min(r, rows - 1) % a.group;
-        const size_t at = ((size_t)split * a.b.rows + q.row0 + tok) * a.heads + h;
+        const size_t item = ((size_t)split * a.b.rows + q.row0 + tok) * a.heads + h;
         const float inv = 1.f / l;
 #pragma unroll
         for (int ch = 0; ch < DIM / 32; ++ch) {
@@ -327,115 +414,135 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
               dst[i] = make_uint4(narrow2<BF16>(v[8 * i] * inv, v[8 * i + 1] * inv), narrow2<BF16>(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
                                   narrow2<BF16>(v[8 * i + 4] * inv, v[8 * i + 5] * inv), narrow2<BF16>(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
           } else if (n > 0) {
-            float4* dst = reinterpret_cast<float4*>(a.part + at * DIM + 32 * ch);
+            float4* dst = reinterpret_cast<float4*>(a.part + item * DIM + 32 * ch);
 #pragma unroll
             for (int i = 0; i < 8; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           }
         }
-        if (splits > 1 && live) a.part_ml[at] = make_float2(m, l);
-        fence_before();
+        if (splits > 1 && live) a.part_ml[item] = make_float2(m, l);
+        at0 += steps;
+        done += steps > 0;
       }
-    } else if (warp < kSoftWarps + kConvWarps) {
+      fence_before();
+      fine = meet(dead);
+    }
+  } else if (warp < kMmaWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvRegs));
+    int at0 = 0;
+    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
+      const Part pt = part_of(mt);
+      const int lo = pt.lo, n = pt.n;
+      const KeyTiles& units = pt.units;
+      bool dead = false;
       // integers to fp16: instruction i of a tile takes 16 keys, four per warp, eight (four) lanes each
       constexpr int kLanes = DIM / 16, kPer = 32 / kLanes;  // lanes per key, keys per warp and instruction
       constexpr int kInst = kKeys / (kConvWarps * kPer);
-      const int cw = warp - kSoftWarps, key = cw * kPer + lane / kLanes, part = lane % kLanes;
-      for (int j = 0; j < n && !dead; ++j) {
-        const int at = at0 + j, s = at & 1;
-        // lane u < 8: unit u's block and first row in it
-        int id = -1, row = 0;
+      const bool vals = warp >= kSoftWarps + kConvWarps;
+      const int cw = (warp - kSoftWarps) % kConvWarps, key = cw * kPer + lane / kLanes, part = lane % kLanes;
+      // lane u < 8: the block of tile j's unit u (-1: none), and its first row in the pool (kNone)
+      constexpr uint32_t kNone = 0xffffffffu;
+      const auto block_of = [&](int j) {
         const int u = (lo + j) * kUnits + lane;
-        if (lane < kUnits && u < units.total) {
-          const int t0 = units.token(u);
-          id = __ldg(table + t0 / a.c.block);
-          if (id >= a.c.n_blocks) id = -1;
-          row = t0 % a.c.block;
+        return lane < kUnits && u < units.total && j < n ? __ldg(table + (units.token(u) >> shift)) : -1;
+      };
+      const auto row_of = [&](int j, int id) {
+        return id >= 0 && id < a.c.n_blocks ? ((uint32_t)id * a.c.kv_heads + head) * a.c.block + (units.token((lo + j) * kUnits + lane) & (a.c.block - 1)) : kNone;
+      };
+      const uint32_t in_unit = key % kUnit;
+      const unsigned char* base = static_cast<const unsigned char*>(vals ? a.c.v : a.c.k) + 16 * part;  // this lane's 16 bytes of row 0
+      const auto load = [&](uint32_t where, int i) {
+        const uint32_t row = __shfl_sync(0xffffffffu, where, (i * kConvWarps * kPer + key) / kUnit);
+        return row != kNone ? __ldg(reinterpret_cast<const uint4*>(base + (size_t)(row + in_unit) * DIM)) : make_uint4(0, 0, 0, 0);
+      };
+      uint64_t *full = vals ? v_full : k_full, *empty = vals ? v_empty : k_empty;
+      unsigned char* stages = smem + (vals ? S::kV : S::kK) + (part >> 2) * S::kHalf;
+      const int c0 = 2 * (part & 3);
+      const bool swap = part >> 2;  // these lanes write their two chunks in the other order (bank conflicts)
+      uint4 x[kInst];  // a tile's loads take the registers of the tile before it as they are freed
+      uint32_t next = row_of(0, block_of(0));
+#pragma unroll
+      for (int i = 0; i < kInst; ++i) x[i] = load(next, i);
+      next = row_of(1, block_of(1));
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int at = at0 + j, id = block_of(j + 2);
+        if (at >= 2 && !mbar_wait(empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
+          dead = true;
+          break;
         }
+        unsigned char* dst = stages + (at & 1) * S::kTileBytes;
 #pragma unroll
-        for (int which = 0; which < 2; ++which) {
-          const int8_t* base = static_cast<const int8_t*>(which ? a.c.v : a.c.k);
-          uint4 x[kInst];
-#pragma unroll
-          for (int i = 0; i < kInst; ++i) {
-            const int r = i * kConvWarps * kPer + key;
-            const int rid = __shfl_sync(0xffffffffu, id, r / kUnit), rrow = __shfl_sync(0xffffffffu, row, r / kUnit);
-            x[i] = make_uint4(0, 0, 0, 0);
-            if (rid >= 0)
-              x[i] = __ldg(reinterpret_cast<const uint4*>(base + (((size_t)rid * a.c.kv_heads + head) * a.c.block + rrow + r % kUnit) * DIM) + part);
-          }
-          uint64_t* empty = (which ? v_empty : k_empty) + s;
-          if (at >= 2 && !mbar_wait(empty, (uint32_t)((at >> 1) - 1) & 1u)) {
-            dead = true;
-            break;
-          }
-          unsigned char* dst = smem + (which ? S::kV : S::kK) + s * S::kTileBytes + (part >> 2) * S::kHalf;
-#pragma unroll
-          for (int i = 0; i < kInst; ++i) {
-            const int r = i * kConvWarps * kPer + key;
-            const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
-            uint32_t y[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              y[2 * e] = int_half2(__byte_perm(w[e], 0x64646464u, 0x4140));
-              y[2 * e + 1] = int_half2(__byte_perm(w[e], 0x64646464u, 0x4342));
-            }
-            // two 16-byte chunks; the lanes of the second half of a key write theirs in the other order (bank conflicts)
-            const int c0 = 2 * (part & 3);
-            const uint4 y0 = make_uint4(y[0], y[1], y[2], y[3]), y1 = make_uint4(y[4], y[5], y[6], y[7]);
-            const bool swap = part >> 2;
-            *reinterpret_cast<uint4*>(dst + r * 128 + (((c0 + (swap ? 1 : 0)) ^ (r & 7)) << 4)) = swap ? y1 : y0;
-            *reinterpret_cast<uint4*>(dst + r * 128 + (((c0 + (swap ? 0 : 1)) ^ (r & 7)) << 4)) = swap ? y0 : y1;
-          }
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive((which ? v_full : k_full) + s);
+        for (int i = 0; i < kInst; ++i) {
+          const int r = i * kConvWarps * kPer + key;
+          const uint32_t w[4] = {x[i].x ^ 0x80808080u, x[i].y ^ 0x80808080u, x[i].z ^ 0x80808080u, x[i].w ^ 0x80808080u};
+          x[i] = load(next, i);
+          // chunks of eight: the first and the second half of the 16 bytes
+          const uint32_t a0 = swap ? w[2] : w[0], a1 = swap ? w[3] : w[1], b0 = swap ? w[0] : w[2], b1 = swap ? w[1] : w[3];
+          const auto lo2 = [](uint32_t v) { return int_half2(__byte_perm(v, 0x64646464u, 0x4140)); };
+          const auto hi2 = [](uint32_t v) { return int_half2(__byte_perm(v, 0x64646464u, 0x4342)); };
+          *reinterpret_cast<uint4*>(dst + r * 128 + (((c0 + (swap ? 1 : 0)) ^ (r & 7)) << 4)) = make_uint4(lo2(a0), hi2(a0), lo2(a1), hi2(a1));
+          *reinterpret_cast<uint4*>(dst + r * 128 + (((c0 + (swap ? 0 : 1)) ^ (r & 7)) << 4)) = make_uint4(lo2(b0), hi2(b0), lo2(b1), hi2(b1));
         }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full + (at & 1));
+        next = row_of(j + 2, id);
       }
-    } else {
-     if (elect()) {
+      at0 += n;
+      if (!meet(dead)) break;
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    int at0 = 0, tile_at[2] = {0, 0}, mi = 0;  // key tiles, steps of the row tiles, row tiles
+    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z, ++mi) {
+      const Part pt = part_of(mt);
+      const int steps = pt.steps, tiles = pt.two ? 2 : 1;
+      bool dead = false;
+      if (elect()) {
       bool ok = mbar_wait(q_full, (uint32_t)mi & 1u);
       const uint32_t sq = smem_u32(smem + S::kQ), sk = smem_u32(smem + S::kK), sv = smem_u32(smem + S::kV);
-      const auto scores = [&](int tile, int at) {
-        const uint32_t qa = sq + tile * S::kTileBytes, kb = sk + (at & 1) * S::kTileBytes;
+      // step i's products; a key tile's stage is free once its last step's of all row tiles are done
+      const auto scores = [&](int t, int i) {
+        const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
+        const uint32_t qa = sq + t * S::kTileBytes, kb = sk + stage * S::kTileBytes + (i & 1) * (kStep * 128);
 #pragma unroll
         for (int kk = 0; kk < DIM / 16; ++kk)
-          mma_f16_ss(tmem + tile * 128, sw128_desc(qa + (kk >> 2) * S::kHalf) + 2 * (kk & 3), sw128_desc(kb + (kk >> 2) * S::kHalf) + 2 * (kk & 3),
-                     idesc_f16(128, kKeys, false), kk > 0);
-        mma_commit(s_full + tile);
+          mma_f16_ss(tmem + t * 128 + buf * kStep, sw128_desc(qa + (kk >> 2) * S::kHalf) + 2 * (kk & 3), sw128_desc(kb + (kk >> 2) * S::kHalf) + 2 * (kk & 3),
+                     idesc_f16(128, kStep, false), kk > 0);
+        mma_commit(s_full + 2 * t + buf);
+        if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(k_empty + stage);
       };
-      const auto values = [&](int tile, int at, bool acc) {
-        const uint32_t vb = sv + (at & 1) * S::kTileBytes;
+      const auto values = [&](int t, int i) {
+        const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
+        const uint32_t vb = sv + stage * S::kTileBytes + (i & 1) * (kStep * 128);
 #pragma unroll
-        for (int kk = 0; kk < kKeys / 16; ++kk)
-          mma_f16_ts(tmem + S::kO + tile * DIM, tmem + tile * 128 + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true),
-                     acc || kk > 0);
+        for (int kk = 0; kk < kStep / 16; ++kk)
+          mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + buf * kStep + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true),
+                     i > 0 || kk > 0);
+        mma_commit(o_done + t);
+        if (i == steps - 1) mma_commit(o_full + t);
+        if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(v_empty + stage);
       };
-      const int tiles = two ? 2 : 1;
-      if (ok && n > 0) {
-        ok = mbar_wait(k_full + (at0 & 1), (uint32_t)(at0 >> 1) & 1u);
-        if (ok) {
-          fence_after();
-          for (int t = 0; t < tiles; ++t) scores(t, at0);
-          mma_commit(k_empty + (at0 & 1));
-        }
-      }
-      for (int j = 0; j < n && ok; ++j) {
-        const int at = at0 + j;
-        ok = mbar_wait(v_full + (at & 1), (uint32_t)(at >> 1) & 1u);
+      const auto have = [&](uint64_t* full, int i) {
+        const int at = at0 + (i >> 1);
+        const bool there = mbar_wait(full + (at & 1), (uint32_t)(at >> 1) & 1u);
+        fence_after();
+        return there;
+      };
+      if (ok && steps > 0) ok = have(k_full, 0);
+      for (int i = 0; i < min(2, steps) && ok; ++i)
+        for (int t = 0; t < tiles; ++t) scores(t, i);
+      for (int i = 0; i < steps && ok; ++i) {
+        if ((i & 1) == 0) ok = have(v_full, i);
         for (int t = 0; t < tiles && ok; ++t) {
-          ok = mbar_wait(p_full + t, (uint32_t)((t ? at1 : at0) + j) & 1u);
+          const int at = tile_at[t] + i;
+          ok = mbar_wait(p_full + 2 * t + (at & 1), (uint32_t)(at >> 1) & 1u);
           if (!ok) break;
           fence_after();
-          values(t, at, j > 0);
-          if (t == tiles - 1) mma_commit(v_empty + (at & 1));
-          if (j + 1 < n) {
-            ok = t > 0 || mbar_wait(k_full + ((at + 1) & 1), (uint32_t)((at + 1) >> 1) & 1u);
-            if (!ok) break;
-            fence_after();
-            scores(t, at + 1);
-            if (t == tiles - 1) mma_commit(k_empty + ((at + 1) & 1));
-          } else {
-            mma_commit(o_full + t);
+          values(t, i);
+          if (i + 2 < steps) {
+            if (t == 0 && (i & 1) == 0) ok = have(k_full, i + 2);
+            if (ok) scores(t, i + 2);
           }
         }
       }
@@ -444,27 +551,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         mbar_wait(drain, 0);
         dead = true;
       }
-     }
-     __syncwarp();
+      }
+      __syncwarp();
+      at0 += pt.n;
+      tile_at[0] += steps;
+      if (pt.two) tile_at[1] += steps;
+      fence_before();
+      if (!meet(__any_sync(0xffffffffu, dead))) break;
+      fence_after();
     }
-    at0 += n;
-    done0 += n > 0;
-    if (two) at1 += n, done1 += n > 0;
-    // every role is done with this row tile before the next one's queries
-    fence_before();
-    dead = __syncthreads_or(dead);
     fence_after();
-  }
-  if (warp == kSoftWarps + kConvWarps)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
 }
 
 template <bool BF16, int DIM>
 cudaError_t launch(const Kv8Attend& a, const Kv8TilesPlan& p, cudaStream_t s) {
   using S = TilesShape<DIM>;
+  static const bool enough = [] {  // setmaxnreg waits for registers that the launch did not bring
+    cudaFuncAttributes at{};
+    return cudaFuncGetAttributes(&at, k_kv8_tiles<BF16, DIM>) == cudaSuccess && at.numRegs >= kLaunchRegs;
+  }();
+  if (!enough) return cudaErrorLaunchOutOfResources;
   const cudaError_t e = smem_opt_in<k_kv8_tiles<BF16, DIM>>(S::kSmem);
   if (e != cudaSuccess) return e;
-  k_kv8_tiles<BF16, DIM><<<dim3(p.mtiles, a.c.kv_heads * p.splits, a.b.n), kThreads, S::kSmem, s>>>(a);
+  k_kv8_tiles<BF16, DIM><<<dim3(a.c.kv_heads * p.splits, a.b.n, p.mtiles), kThreads, S::kSmem, s>>>(a);
   return cudaGetLastError();
 }
 
@@ -474,7 +585,7 @@ bool kv8_tiles_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int win
   const int group = heads / c.kv_heads;
   const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
   if ((int64_t)most * group < 96) return false;
-  p->mtiles = (int)(((int64_t)most * group + 255) / 256);
+  p->mtiles = (int)std::min<int64_t>(((int64_t)most * group + 255) / 256, 65535);
   const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, (int64_t)window + sinks + most) : cap;
   // few row tiles: the keys over several CTAs too, four key tiles each at least
