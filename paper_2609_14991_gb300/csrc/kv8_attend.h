@@ -70,7 +70,8 @@ __device__ __forceinline__ QueryScale query_scale(float top) {
   return {__uint_as_float((uint32_t)(fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127) << 23), fine};
 }
 
-// Few rows per key head (kv8_rows.cu): row tiles of 16 x mw, the keys over `splits` CTAs.
+// Few rows per key head (kv8_rows.cu): row tiles of 16 x mw (mw 0: of 8), the keys over
+// `splits` CTAs.
 struct Kv8RowsPlan {
   int mw = 1, mtiles = 1, splits = 1;
   int64_t bytes = 0;  // workspace

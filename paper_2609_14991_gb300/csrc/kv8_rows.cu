@@ -2,11 +2,14 @@
 // tokens and short chunks (tsd.h: tsd_kv8_attend).
 //
 // The rows of a sequence and key head are its new tokens times the query heads
-// that share the head (row = token * group + head of the group).  16 rows are one
-// tile of mma.sync.m16n8k16 (fp16 in, fp32 out): the keys and values are
-// read once for all of them.  Four warps of a CTA share the work as MW row
-// tiles x 4 / MW key groups; a long context is split over CTAs too
-// (partial results in the workspace, joined by k_kv8_join).
+// that share the head (row = token * group + head of the group).  The products are
+// mma.sync.m16n8k16 (fp16 in, fp32 out): tcgen05 takes 64 or 128 rows, and these are
+// few.  Up to eight rows (k_kv8_eight) are the eight columns: scores are keys x
+// rows, results dimensions x rows, so no product is spent on rows that are not
+// there.  More (k_kv8_rows) are row tiles of 16.  The keys and values are read once
+// for all rows of a CTA, whose four warps share the work as MW row tiles x 4 / MW key groups; a
+// long context is split over CTAs too (partial results in the workspace, joined by
+// k_kv8_join).
 //
 // Mathematics, per row: with integers k_j, v_j, scales a_b, c_b of key j's block b and
 // the row's factor f (queries are scaled by f, a power of two, into fp16),
@@ -56,6 +59,41 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Joins a row's results of the CTA's `parts` key groups (maximum and sum ml_step apart,
+// eight of its dimensions from col on acc_step apart) and writes them, or this
+// split's share.
+template <bool BF16, int DIM>
+__device__ __forceinline__ void emit_row(const Kv8Attend& a, const Kv8Seq& q, int r, int head, int col, const float2* ml, int ml_step, const float* src,
+                                         int acc_step, int parts) {
+  float top = -INFINITY;
+  for (int k = 0; k < parts; ++k) top = fmaxf(top, ml[k * ml_step].x);
+  float acc[8] = {}, sum = 0.f;
+  for (int k = 0; k < parts; ++k) {
+    const float2 x = ml[k * ml_step];
+    if (x.x == -INFINITY && x.y == 0.f) continue;
+    const float w = x.x == -INFINITY ? 1.f : ex2_approx(x.x - top);
+    sum = fmaf(w, x.y, sum);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, src[k * acc_step + j], acc[j]);
+  }
+  const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
+  if (gridDim.x == 1) {
+    const float inv = 1.f / sum;
+    uint4 y;
+    y.x = narrow2<BF16>(acc[0] * inv, acc[1] * inv);
+    y.y = narrow2<BF16>(acc[2] * inv, acc[3] * inv);
+    y.z = narrow2<BF16>(acc[4] * inv, acc[5] * inv);
+    y.w = narrow2<BF16>(acc[6] * inv, acc[7] * inv);
+    *reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + col) = y;
+  } else {
+    const size_t at = ((size_t)blockIdx.x * a.b.rows + tok) * a.heads + h;
+    float4* dst = reinterpret_cast<float4*>(a.part + at * DIM + col);
+    dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    if (col == 0) a.part_ml[at] = make_float2(top, sum);
+  }
 }
 
 template <bool BF16, int DIM, int MW>
@@ -145,8 +183,9 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
       const int all_from = a.window > 0 ? before + min(r0 + 15, rows - 1) / a.group - a.window + 1 : 0;  // the last row's window
 
       const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
+      const int shift = __ffs(a.c.block) - 1;
       const auto block_of = [&](int i) {  // of the key group's tile i; -1 outside the pool
-        const int id = __ldg(table + tiles.token(lo + kg + i * KW) / a.c.block);
+        const int id = __ldg(table + (tiles.token(lo + kg + i * KW) >> shift));
         return id < a.c.n_blocks ? id : -1;
       };
       int ids = 0;  // lane j: the block of issued tile (i & ~31) + j
@@ -158,7 +197,7 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
           // a wait that runs out leaves a stage that nothing is copied into: its consumers' waits run out too
           if (at < ST || mbar_wait(empty + st, (uint32_t)(at / ST - 1) & 1u)) {
             if (id >= 0) {
-              const size_t off = (((size_t)id * a.c.kv_heads + head) * a.c.block + tiles.token(lo + kg + i * KW) % a.c.block) * DIM;
+              const size_t off = (((size_t)id * a.c.kv_heads + head) * a.c.block + (tiles.token(lo + kg + i * KW) & (a.c.block - 1))) * DIM;
               mbar_expect_tx(full + st, S::kStageBytes);
               bulk_g2s(ring + st * S::kStageBytes, static_cast<const int8_t*>(a.c.k) + off, kTile * DIM, full + st);
               bulk_g2s(ring + st * S::kStageBytes + kTile * DIM, static_cast<const int8_t*>(a.c.v) + off, kTile * DIM, full + st);
@@ -303,6 +342,7 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
       l[0] = l[1] = __uint_as_float(0x7fc00000u);
     }
 
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // join the key groups through shared memory (the ring's: every stage has been read)
     __syncthreads();
 #pragma unroll
@@ -322,45 +362,296 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
     for (int e = threadIdx.x; e < 16 * MW * kOct; e += 128) {
       const int row = e / kOct, col = 8 * (e % kOct), r = mt * 16 * MW + row;
       if (r >= rows) break;
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < KW; ++k) top = fmaxf(top, s_ml[k * 16 * MW + row].x);
-      float acc[8] = {}, sum = 0.f;
-#pragma unroll
-      for (int k = 0; k < KW; ++k) {
-        const float2 ml = s_ml[k * 16 * MW + row];
-        if (ml.x == -INFINITY && ml.y == 0.f) continue;
-        const float w = ml.x == -INFINITY ? 1.f : ex2_approx(ml.x - top);
-        sum = fmaf(w, ml.y, sum);
-        const float* src = s_out + (k * 16 * MW + row) * S::kOutStride + col;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) acc[j] = fmaf(w, src[j], acc[j]);
-      }
-      const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
-      if (gridDim.x == 1) {
-        const float inv = 1.f / sum;
-        uint4 y;
-        y.x = narrow2<BF16>(acc[0] * inv, acc[1] * inv);
-        y.y = narrow2<BF16>(acc[2] * inv, acc[3] * inv);
-        y.z = narrow2<BF16>(acc[4] * inv, acc[5] * inv);
-        y.w = narrow2<BF16>(acc[6] * inv, acc[7] * inv);
-        *reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + col) = y;
-      } else {
-        const size_t at = ((size_t)blockIdx.x * a.b.rows + tok) * a.heads + h;
-        float4* dst = reinterpret_cast<float4*>(a.part + at * DIM + col);
-        dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-        dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-        if (col == 0) a.part_ml[at] = make_float2(top, sum);
-      }
+      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, 16 * MW, s_out + row * S::kOutStride + col, 16 * MW * S::kOutStride, KW);
     }
     fence_async_smem();
     dead = __syncthreads_or(dead);  // then the ring is written again
   }
 }
 
+// Up to eight rows per CTA (more: in turns).  Each warp takes every fourth stage of
+// two 16-key units, which it copies into a ring of its own.
+template <int DIM>
+struct EightShape {
+  static constexpr int kStages = 2;
+  static constexpr int kUnitBytes = 2 * kTile * DIM;       // keys, then values
+  static constexpr int kRing = 4 * kStages * 2 * kUnitBytes;
+  static constexpr int kOutStride = DIM + 4;
+  static constexpr int kBarOff = kRing;
+  static constexpr int kSmem = kBarOff + 4 * kStages * 8 + 32 * 8;
+  static_assert(4 * 8 * kOutStride * 4 <= kRing, "the warps' results pass through the ring");
+};
+
+// The transpose of an 8 x 8 matrix of 16-bit elements spread over a warp.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
+template <bool BF16, int DIM>
+__global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv8Attend a) {
+  using S = EightShape<DIM>;
+  constexpr int ST = S::kStages;
+  constexpr int kSteps = DIM / 16, kTiles = DIM / 16;  // k-steps of the scores; 16-dimension tiles of the results
+  extern __shared__ __align__(128) unsigned char smem[];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarOff) + warp * ST;
+  float2* s_ml = reinterpret_cast<float2*>(smem + S::kBarOff + 4 * ST * 8);  // [4 warps][8 rows] maximum, sum
+  float* s_out = reinterpret_cast<float*>(smem);
+  unsigned char* ring = smem + warp * ST * 2 * S::kUnitBytes;
+  const int head = blockIdx.y % a.c.kv_heads, mt0 = blockIdx.y / a.c.kv_heads, mts = gridDim.y / a.c.kv_heads;
+  const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
+  const int rows = q.count * a.group;
+  if (mt0 * 8 >= rows) return;
+  if (lane < ST) mbar_init(full + lane, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+  const int shift = __ffs(a.c.block) - 1;
+  int it0 = 0;        // stages of this warp so far
+  bool dead = false;  // a wait of this CTA ran out: NaN for its rows from there on
+
+  for (int mt = mt0; mt * 8 < rows; mt += mts) {
+    const int r0 = mt * 8;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // rows 2t, 2t + 1
+    float o[kTiles][4];
+#pragma unroll
+    for (int j = 0; j < kTiles; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    if (q.ok && !dead) {
+      const int before = q.len - q.count;
+      const KeyTiles units = key_tiles(before + r0 / a.group, before + (min(rows, r0 + 8) - 1) / a.group, a.window, a.sinks);
+      const int all = (units.total + 1) / 2;
+      const int lo = (int)((int64_t)all * blockIdx.x / gridDim.x), hi = (int)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
+      const int n = hi - lo > warp ? (hi - lo - warp + 3) / 4 : 0;  // this warp's stages lo + warp + 4 i
+      const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
+      // unit u of stage i in the list of units
+      const auto unit_at = [&](int i, int u) { return 2 * (lo + warp + 4 * i) + u; };
+      const auto block_of = [&](int v) {
+        const int id = v < units.total ? __ldg(table + (units.token(v) >> shift)) : -1;
+        return id < a.c.n_blocks ? id : -1;
+      };
+      int ids = -1;  // lane 2 j + u: the block of unit u of stage (i & ~15) + j
+      const auto issue = [&](int i) {
+        if ((i & 15) == 0) ids = i + (lane >> 1) < n ? block_of(unit_at(i + (lane >> 1), lane & 1)) : -1;
+        const int id0 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15)), id1 = __shfl_sync(0xffffffffu, ids, 2 * (i & 15) + 1);
+        const int st = (it0 + i) % ST;
+        if (lane == 0) {
+          const uint32_t bytes = ((id0 >= 0) + (id1 >= 0)) * S::kUnitBytes;
+          if (bytes) mbar_expect_tx(full + st, bytes);
+          else mbar_arrive(full + st);
+        }
+        __syncwarp();
+        // lanes 0 .. 3: keys and values of the two units
+        const int id = lane & 2 ? id1 : id0;
+        if (lane < 4 && id >= 0) {
+          const size_t off = (((size_t)id * a.c.kv_heads + head) * a.c.block + (units.token(unit_at(i, lane >> 1)) & (a.c.block - 1))) * DIM;
+          bulk_g2s(ring + st * 2 * S::kUnitBytes + (lane >> 1) * S::kUnitBytes + (lane & 1) * kTile * DIM,
+                   static_cast<const int8_t*>(lane & 1 ? a.c.v : a.c.k) + off, kTile * DIM, full + st);
+        }
+        __syncwarp();
+      };
+      for (int i = 0; i < min(n, ST); ++i) issue(i);
+
+      // the queries' fragments: row g's, scaled by f
+      uint32_t qf[kSteps][2];
+      float rc[2];
+      int pos[2];
+      {
+        const int r = r0 + g, tok = r / a.group;
+        uint2 w[kSteps];
+        float top = 0.f;
+        bool odd = false;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          w[kk] = make_uint2(0, 0);
+          if (r < rows)
+            w[kk] = __ldg(reinterpret_cast<const uint2*>(a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + r % a.group) * a.q_head +
+                                                         64 * (kk >> 2) + 16 * t + 4 * (kk & 3)));
+        }
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          const float x0 = fabsf(wide16<BF16>(w[kk].x & 0xffffu)), x1 = fabsf(wide16<BF16>(w[kk].x >> 16));
+          const float x2 = fabsf(wide16<BF16>(w[kk].y & 0xffffu)), x3 = fabsf(wide16<BF16>(w[kk].y >> 16));
+          top = fmaxf(fmaxf(top, fmaxf(x0, x1)), fmaxf(x2, x3));
+          odd = odd || !(x0 + x1 + x2 + x3 <= INFINITY);
+        }
+        top = odd ? INFINITY : top;
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const QueryScale qs = query_scale(top);
+        const float c = qs.fine ? a.scale * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) {
+          qf[kk][0] = narrow2<false>(wide16<BF16>(w[kk].x & 0xffffu) * qs.f, wide16<BF16>(w[kk].x >> 16) * qs.f);
+          qf[kk][1] = narrow2<false>(wide16<BF16>(w[kk].y & 0xffffu) * qs.f, wide16<BF16>(w[kk].y >> 16) * qs.f);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          rc[h] = __shfl_sync(0xffffffffu, c, 8 * t + 4 * h);
+          pos[h] = before + min(r0 + 2 * t + h, rows - 1) / a.group;
+        }
+      }
+      // positions that every row sees
+      const int all_to = before + r0 / a.group;
+      const int all_from = a.window > 0 ? before + (min(rows, r0 + 8) - 1) / a.group - a.window + 1 : 0;
+
+      float a_b = 0.f, lc_b = 0.f, ic_b = 0.f;  // lane 2 j + u: scales of unit u of stage (i & ~15) + j
+      bool expired = false;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        if ((i & 15) == 0) {
+          const int id = i + (lane >> 1) < n ? block_of(unit_at(i + (lane >> 1), lane & 1)) : -1;
+          const float nan = __uint_as_float(0x7fc00000u);
+          a_b = id >= 0 ? __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head) : nan;
+          const float c = id >= 0 ? __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head) : nan;
+          const float cs = c == 0.f ? 0x1p-80f : c;  // a scale of 0 stands for values of 0, of their weight all the same
+          lc_b = log2f(cs);
+          ic_b = 1.f / cs;
+        }
+        const int at = it0 + i, st = at % ST;
+        if (!__all_sync(0xffffffffu, mbar_wait(full + st, (uint32_t)(at / ST) & 1u))) {
+          for (int j = at + 1; j < min(it0 + n, at + ST); ++j) mbar_wait(full + j % ST, (uint32_t)(j / ST) & 1u);
+          expired = true;
+          break;
+        }
+        const unsigned char* stage = ring + st * 2 * S::kUnitBytes;
+        float s[2][4];  // keys g, g + 8 x rows 2t, 2t + 1
+        float top[2] = {-INFINITY, -INFINITY}, ic[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
+          const unsigned char* kt = stage + u * S::kUnitBytes + g * DIM + 16 * t;
+#pragma unroll
+          for (int v = 0; v < DIM / 64; ++v) {
+            const uint4 x = *reinterpret_cast<const uint4*>(kt + 64 * v), y = *reinterpret_cast<const uint4*>(kt + 8 * DIM + 64 * v);
+            const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              const uint32_t xx = xw[w] ^ 0x80808080u, yy = yw[w] ^ 0x80808080u;
+              const uint32_t f[4] = {int_half2(__byte_perm(xx, 0x64646464u, 0x4140)), int_half2(__byte_perm(yy, 0x64646464u, 0x4140)),
+                                     int_half2(__byte_perm(xx, 0x64646464u, 0x4342)), int_half2(__byte_perm(yy, 0x64646464u, 0x4342))};
+              mma16816(s[u], f, qf[4 * v + w][0], qf[4 * v + w][1]);
+            }
+          }
+          const int from = 2 * (i & 15) + u;
+          const float ab = __shfl_sync(0xffffffffu, a_b, from), lc = __shfl_sync(0xffffffffu, lc_b, from);
+          ic[u] = __shfl_sync(0xffffffffu, ic_b, from);
+          const int vu = unit_at(i, u), tok0 = units.token(vu);
+          const bool whole = vu < units.total && tok0 + kTile - 1 <= all_to && (tok0 >= all_from || tok0 + kTile <= a.sinks);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int h = e & 1;
+            float x = fmaf(s[u][e], rc[h] * ab, lc);
+            if (!whole) {
+              const int key = tok0 + g + 8 * (e >> 1);
+              const bool see = vu < units.total && key <= pos[h] && (a.window <= 0 || key > pos[h] - a.window || key < a.sinks);
+              x = see ? x : -INFINITY;
+            }
+            s[u][e] = x;
+            top[h] = fmaxf(top[h], x);
+          }
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float x = fmaxf(m[h], top[h]);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+            const float w = x == m[h] ? 1.f : ex2_approx(m[h] - x);
+            m[h] = x;
+            l[h] *= w;
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) {
+              o[j][h] *= w;
+              o[j][2 + h] *= w;
+            }
+          }
+        }
+        const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0] - 7.f, m[1] == -INFINITY ? 0.f : m[1] - 7.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float p[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = ex2_approx(s[u][e] - ref[e & 1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float sum = p[h] + p[2 + h];
+            if (sum != 0.f) l[h] = fmaf(sum, ic[u], l[h]);  // a unit that the row does not see may have a NaN scale
+          }
+          const uint32_t b0 = transpose8(narrow2<false>(p[0], p[1])), b1 = transpose8(narrow2<false>(p[2], p[3]));
+          // values: keys 2t, 2t+1, 2t+8, 2t+9 of 16 (8) dimensions
+          constexpr int kW = DIM / 32;  // words per key
+          const unsigned char* vt = stage + u * S::kUnitBytes + kTile * DIM + 2 * t * DIM + (DIM / 8) * g;
+          uint32_t v[4][kW];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const unsigned char* src = vt + ((j & 1) + 8 * (j >> 1)) * DIM;
+            if constexpr (DIM == 128) {
+              const uint4 x = *reinterpret_cast<const uint4*>(src);
+              v[j][0] = x.x, v[j][1] = x.y, v[j][2] = x.z, v[j][3] = x.w;
+            } else {
+              const uint2 x = *reinterpret_cast<const uint2*>(src);
+              v[j][0] = x.x, v[j][1] = x.y;
+            }
+          }
+#pragma unroll
+          for (int w = 0; w < kW; ++w) {
+            const uint32_t x0 = v[0][w] ^ 0x80808080u, x1 = v[1][w] ^ 0x80808080u, y0 = v[2][w] ^ 0x80808080u, y1 = v[3][w] ^ 0x80808080u;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {  // dimensions 4 w + 2 half, and the next
+              const uint32_t x = __byte_perm(x0, x1, half ? 0x7362 : 0x5140), y = __byte_perm(y0, y1, half ? 0x7362 : 0x5140);
+              const uint32_t f[4] = {int_half2(__byte_perm(x, 0x64646464u, 0x4140)), int_half2(__byte_perm(x, 0x64646464u, 0x4342)),
+                                     int_half2(__byte_perm(y, 0x64646464u, 0x4140)), int_half2(__byte_perm(y, 0x64646464u, 0x4342))};
+              mma16816(o[2 * w + half], f, b0, b1);
+            }
+          }
+        }
+        __syncwarp();  // the stage has been read
+        if (i + ST < n) issue(i + ST);
+      }
+      dead = expired;
+      if (dead) {
+        l[0] = l[1] = __uint_as_float(0x7fc00000u);
+        m[0] = m[1] = 0.f;
+      }
+      it0 += n;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], d);
+    } else if (warp == 0 && (dead || blockIdx.x == 0)) {
+      m[0] = m[1] = 0.f;
+      l[0] = l[1] = __uint_as_float(0x7fc00000u);
+    }
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // join the warps through shared memory (the rings': every stage has been read)
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (g == 0) s_ml[warp * 8 + 2 * t + h] = make_float2(m[h], l[h]);
+      float* dst = s_out + (warp * 8 + 2 * t + h) * S::kOutStride + (DIM / 8) * g;
+#pragma unroll
+      for (int j = 0; j < kTiles; j += 2)
+        *reinterpret_cast<float4*>(dst + 2 * j) = make_float4(o[j][h], o[j][2 + h], o[j + 1][h], o[j + 1][2 + h]);
+    }
+    __syncthreads();
+    constexpr int kOct = DIM / 8;
+    for (int e = threadIdx.x; e < 8 * kOct; e += 128) {
+      const int row = e / kOct, col = 8 * (e % kOct), r = r0 + row;
+      if (r >= rows) break;
+      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, 8, s_out + row * S::kOutStride + col, 8 * S::kOutStride, 4);
+    }
+    fence_async_smem();
+    dead = __syncthreads_or(dead);  // then the rings are written again
+  }
+}
+
 // Joins the splits' partial results: one warp per row and query head, lane = DIM / 32 dimensions.
 template <bool BF16, int DIM>
 __global__ void __launch_bounds__(128) k_kv8_join(const __grid_constant__ Kv8Attend a, int splits) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const size_t at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
   const size_t items = (size_t)a.b.rows * a.heads;
@@ -398,8 +689,17 @@ cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t
 }
 
 template <bool BF16, int DIM>
+cudaError_t launch_eight(const Kv8Attend& a, int splits, int mtiles, cudaStream_t s) {
+  const cudaError_t e = smem_opt_in<k_kv8_eight<BF16, DIM>>(EightShape<DIM>::kSmem);
+  if (e != cudaSuccess) return e;
+  k_kv8_eight<BF16, DIM><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, EightShape<DIM>::kSmem, s>>>(a);
+  return cudaGetLastError();
+}
+
+template <bool BF16, int DIM>
 cudaError_t launch_mw(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
-  return p.mw == 1   ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
+  return p.mw == 0   ? launch_eight<BF16, DIM>(a, p.splits, p.mtiles, s)
+         : p.mw == 1 ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
          : p.mw == 2 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
                      : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
 }
@@ -407,8 +707,16 @@ cudaError_t launch_mw(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) 
 template <bool BF16, int DIM>
 cudaError_t launch_join(const Kv8Attend& a, int splits, cudaStream_t s) {
   const size_t items = (size_t)a.b.rows * a.heads;
-  k_kv8_join<BF16, DIM><<<(unsigned)((items + 3) / 4), 128, 0, s>>>(a, splits);
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((items + 3) / 4));
+  cfg.blockDim = dim3(128);
+  cfg.stream = s;
+  cudaLaunchAttribute pdl{};
+  pdl.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &pdl;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k_kv8_join<BF16, DIM>, a, splits);
 }
 
 }  // namespace
@@ -418,17 +726,17 @@ Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, i
   const int group = heads / c.kv_heads;
   const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
   const int64_t rows = (int64_t)most * group;
-  p.mw = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const int64_t mtiles = (rows + 16 * p.mw - 1) / (16 * p.mw);
+  p.mw = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  const int per = p.mw ? 16 * p.mw : 8;
+  const int64_t mtiles = (rows + per - 1) / per;
   p.mtiles = (int)std::min<int64_t>(mtiles, std::max(1, 65535 / c.kv_heads));
   const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, (int64_t)window + sinks + most) : cap;
-  const int64_t tiles = (keys + kTile - 1) / kTile;
-  // CTAs wanted: three per SM and a few rounds of them, so that ragged lengths even out; each with two tiles at least
-  // per warp
+  // CTAs wanted: two rounds of three per SM, so that ragged lengths even out, in shares of at
+  // least 1024 keys; where there are fewer sequences and heads than SMs, of 128
   const int64_t units = (int64_t)b.n * c.kv_heads * p.mtiles;
   const int64_t want = ((int64_t)sms * 6 + units - 1) / units;
-  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, tiles / (2 * 4 / p.mw), 64}));
+  p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys / (units < sms ? 128 : 1024), 64}));
   p.bytes = p.splits > 1 ? (int64_t)p.splits * b.rows * heads * (c.dim + 2) * 4 : 0;
   return p;
 }
