@@ -70,10 +70,10 @@ __device__ __forceinline__ QueryScale query_scale(float top) {
   return {__uint_as_float((uint32_t)(fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127) << 23), fine};
 }
 
-// Few rows per key head (kv8_rows.cu): row tiles of 16 x mw (mw 0: of 8), the keys over
-// `splits` CTAs.
+// Few rows per key head (kv8_rows.cu): row tiles of 8, 16 (two or four warps), 32 or 64, the
+// keys over `splits` CTAs.
 struct Kv8RowsPlan {
-  int mw = 1, mtiles = 1, splits = 1;
+  int rows = 8, warps = 4, mtiles = 1, splits = 1;
   int64_t bytes = 0;  // workspace
 };
 Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int window, int sinks, int sms);

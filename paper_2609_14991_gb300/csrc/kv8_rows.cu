@@ -4,9 +4,9 @@
 // The rows of a sequence and key head are its new tokens times the query heads
 // that share the head (row = token * group + head of the group).  The products are
 // mma.sync.m16n8k16 (fp16 in, fp32 out): tcgen05 takes 64 or 128 rows, and these are
-// few.  Up to eight rows (k_kv8_eight) are the eight columns: scores are keys x
-// rows, results dimensions x rows, so no product is spent on rows that are not
-// there.  More (k_kv8_rows) are row tiles of 16.  The keys and values are read once
+// few.  Up to 16 rows (k_kv8_eight) are one or two column tiles of eight: scores are
+// keys x rows, results dimensions x rows, so few products are spent on rows that are
+// not there.  More (k_kv8_rows) are row tiles of 16.  The keys and values are read once
 // for all rows of a CTA, whose four warps share the work as MW row tiles x 4 / MW key groups; a
 // long context is split over CTAs too (partial results in the workspace, joined by
 // k_kv8_join).
@@ -369,17 +369,19 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
   }
 }
 
-// Up to eight rows per CTA (more: in turns).  Each warp takes every fourth stage of
-// two 16-key units, which it copies into a ring of its own.
-template <int DIM>
+// Up to 8 NT rows per CTA of W warps (more rows: in turns).  Each warp takes every W-th
+// stage of two 16-key units, which it copies into a ring of its own.
+template <int DIM, int NT, int W>
 struct EightShape {
   static constexpr int kStages = 2;
   static constexpr int kUnitBytes = 2 * kTile * DIM;       // keys, then values
-  static constexpr int kRing = 4 * kStages * 2 * kUnitBytes;
+  static constexpr int kRing = W * kStages * 2 * kUnitBytes;
   static constexpr int kOutStride = DIM + 4;
-  static constexpr int kBarOff = kRing;
-  static constexpr int kSmem = kBarOff + 4 * kStages * 8 + 32 * 8;
-  static_assert(4 * 8 * kOutStride * 4 <= kRing, "the warps' results pass through the ring");
+  static constexpr int kQStride = DIM + 8;  // fp16 queries, padded
+  static constexpr int kQOff = kRing;
+  static constexpr int kBarOff = kQOff + 8 * NT * (kQStride * 2 + 8);
+  static constexpr int kSmem = kBarOff + W * kStages * 8 + W * 8 * NT * 8;
+  static_assert(W * 8 * NT * kOutStride * 4 <= kRing, "the warps' results pass through the ring");
 };
 
 // The transpose of an 8 x 8 matrix of 16-bit elements spread over a warp.
@@ -389,21 +391,23 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
   return y;
 }
 
-template <bool BF16, int DIM>
-__global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv8Attend a) {
-  using S = EightShape<DIM>;
+template <bool BF16, int DIM, int NT, int W>
+__global__ void __launch_bounds__(32 * W, 12 / W) k_kv8_eight(const __grid_constant__ Kv8Attend a) {
+  using S = EightShape<DIM, NT, W>;
   constexpr int ST = S::kStages;
-  constexpr int kSteps = DIM / 16, kTiles = DIM / 16;  // k-steps of the scores; 16-dimension tiles of the results
+  constexpr int kSteps = DIM / 16, kTiles = DIM / 16, kRows = 8 * NT;  // k-steps of the scores; 16-dimension tiles of the results
   extern __shared__ __align__(128) unsigned char smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + S::kBarOff) + warp * ST;
-  float2* s_ml = reinterpret_cast<float2*>(smem + S::kBarOff + 4 * ST * 8);  // [4 warps][8 rows] maximum, sum
+  float2* s_ml = reinterpret_cast<float2*>(smem + S::kBarOff + W * ST * 8);  // [warp][row] maximum, sum
   float* s_out = reinterpret_cast<float*>(smem);
   unsigned char* ring = smem + warp * ST * 2 * S::kUnitBytes;
+  uint16_t* s_q = reinterpret_cast<uint16_t*>(smem + S::kQOff);               // [rows][kQStride]
+  float* s_rc = reinterpret_cast<float*>(smem + S::kQOff + kRows * S::kQStride * 2);  // [rows]
   const int head = blockIdx.y % a.c.kv_heads, mt0 = blockIdx.y / a.c.kv_heads, mts = gridDim.y / a.c.kv_heads;
   const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
   const int rows = q.count * a.group;
-  if (mt0 * 8 >= rows) return;
+  if (mt0 * kRows >= rows) return;
   if (lane < ST) mbar_init(full + lane, 1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncwarp();
@@ -411,21 +415,26 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
   int it0 = 0;        // stages of this warp so far
   bool dead = false;  // a wait of this CTA ran out: NaN for its rows from there on
 
-  for (int mt = mt0; mt * 8 < rows; mt += mts) {
-    const int r0 = mt * 8;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // rows 2t, 2t + 1
-    float o[kTiles][4];
+  for (int mt = mt0; mt * kRows < rows; mt += mts) {
+    const int r0 = mt * kRows;
+    float m[NT][2], l[NT][2];  // rows 8 c + 2t, 8 c + 2t + 1
+    float o[NT][kTiles][4];
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+    for (int c = 0; c < NT; ++c) {
+      m[c][0] = m[c][1] = -INFINITY;
+      l[c][0] = l[c][1] = 0.f;
+#pragma unroll
+      for (int j = 0; j < kTiles; ++j) o[c][j][0] = o[c][j][1] = o[c][j][2] = o[c][j][3] = 0.f;
+    }
     if (q.ok && !dead) {
       const int before = q.len - q.count;
-      const KeyTiles units = key_tiles(before + r0 / a.group, before + (min(rows, r0 + 8) - 1) / a.group, a.window, a.sinks);
+      const KeyTiles units = key_tiles(before + r0 / a.group, before + (min(rows, r0 + kRows) - 1) / a.group, a.window, a.sinks);
       const int all = (units.total + 1) / 2;
       const int lo = (int)((int64_t)all * blockIdx.x / gridDim.x), hi = (int)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
-      const int n = hi - lo > warp ? (hi - lo - warp + 3) / 4 : 0;  // this warp's stages lo + warp + 4 i
+      const int n = hi - lo > warp ? (hi - lo - warp + W - 1) / W : 0;  // this warp's stages lo + warp + W i
       const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
       // unit u of stage i in the list of units
-      const auto unit_at = [&](int i, int u) { return 2 * (lo + warp + 4 * i) + u; };
+      const auto unit_at = [&](int i, int u) { return 2 * (lo + warp + W * i) + u; };
       const auto block_of = [&](int v) {
         const int id = v < units.total ? __ldg(table + (units.token(v) >> shift)) : -1;
         return id < a.c.n_blocks ? id : -1;
@@ -452,48 +461,55 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
       };
       for (int i = 0; i < min(n, ST); ++i) issue(i);
 
-      // the queries' fragments: row g's, scaled by f
-      uint32_t qf[kSteps][2];
-      float rc[2];
-      int pos[2];
+      // the queries as fp16, scaled by f: each thread its part of a row, then the warps' fragments
       {
-        const int r = r0 + g, tok = r / a.group;
-        uint2 w[kSteps];
+        constexpr int kPer = 32 * W / kRows, kQuads = DIM / kPer / 4;  // threads per row, groups of four elements per thread
+        const int row = threadIdx.x / kPer, part = threadIdx.x % kPer, r = r0 + row, tok = r / a.group;
+        uint2 w[kQuads];
         float top = 0.f;
         bool odd = false;
+        const uint16_t* src = a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + r - tok * a.group) * a.q_head + 4 * part;
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-          w[kk] = make_uint2(0, 0);
-          if (r < rows)
-            w[kk] = __ldg(reinterpret_cast<const uint2*>(a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + r % a.group) * a.q_head +
-                                                         64 * (kk >> 2) + 16 * t + 4 * (kk & 3)));
-        }
+        for (int k = 0; k < kQuads; ++k) w[k] = r < rows ? __ldg(reinterpret_cast<const uint2*>(src + 4 * kPer * k)) : make_uint2(0, 0);
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk) {
-          const float x0 = fabsf(wide16<BF16>(w[kk].x & 0xffffu)), x1 = fabsf(wide16<BF16>(w[kk].x >> 16));
-          const float x2 = fabsf(wide16<BF16>(w[kk].y & 0xffffu)), x3 = fabsf(wide16<BF16>(w[kk].y >> 16));
+        for (int k = 0; k < kQuads; ++k) {
+          const float x0 = fabsf(wide16<BF16>(w[k].x & 0xffffu)), x1 = fabsf(wide16<BF16>(w[k].x >> 16));
+          const float x2 = fabsf(wide16<BF16>(w[k].y & 0xffffu)), x3 = fabsf(wide16<BF16>(w[k].y >> 16));
           top = fmaxf(fmaxf(top, fmaxf(x0, x1)), fmaxf(x2, x3));
           odd = odd || !(x0 + x1 + x2 + x3 <= INFINITY);
         }
         top = odd ? INFINITY : top;
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+#pragma unroll
+        for (int d = 1; d < kPer; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
         const QueryScale qs = query_scale(top);
-        const float c = qs.fine ? a.scale * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
+        if (part == 0) s_rc[row] = qs.fine ? a.scale * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int k = 0; k < kQuads; ++k)
+          *reinterpret_cast<uint2*>(s_q + row * S::kQStride + 4 * (part + kPer * k)) =
+              make_uint2(narrow2<false>(wide16<BF16>(w[k].x & 0xffffu) * qs.f, wide16<BF16>(w[k].x >> 16) * qs.f),
+                         narrow2<false>(wide16<BF16>(w[k].y & 0xffffu) * qs.f, wide16<BF16>(w[k].y >> 16) * qs.f));
+      }
+      __syncthreads();
+      uint32_t qf[NT][kSteps][2];  // rows 8 c + g
+      float rc[NT][2];
+      int pos[NT][2];
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
-          qf[kk][0] = narrow2<false>(wide16<BF16>(w[kk].x & 0xffffu) * qs.f, wide16<BF16>(w[kk].x >> 16) * qs.f);
-          qf[kk][1] = narrow2<false>(wide16<BF16>(w[kk].y & 0xffffu) * qs.f, wide16<BF16>(w[kk].y >> 16) * qs.f);
+          const uint2 w = *reinterpret_cast<const uint2*>(s_q + (8 * c + g) * S::kQStride + 64 * (kk >> 2) + 16 * t + 4 * (kk & 3));
+          qf[c][kk][0] = w.x;
+          qf[c][kk][1] = w.y;
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          rc[h] = __shfl_sync(0xffffffffu, c, 8 * t + 4 * h);
-          pos[h] = before + min(r0 + 2 * t + h, rows - 1) / a.group;
+          rc[c][h] = s_rc[8 * c + 2 * t + h];
+          pos[c][h] = before + min(r0 + 8 * c + 2 * t + h, rows - 1) / a.group;
         }
       }
       // positions that every row sees
       const int all_to = before + r0 / a.group;
-      const int all_from = a.window > 0 ? before + (min(rows, r0 + 8) - 1) / a.group - a.window + 1 : 0;
+      const int all_from = a.window > 0 ? before + (min(rows, r0 + kRows) - 1) / a.group - a.window + 1 : 0;
 
       float a_b = 0.f, lc_b = 0.f, ic_b = 0.f;  // lane 2 j + u: scales of unit u of stage (i & ~15) + j
       bool expired = false;
@@ -515,11 +531,14 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
           break;
         }
         const unsigned char* stage = ring + st * 2 * S::kUnitBytes;
-        float s[2][4];  // keys g, g + 8 x rows 2t, 2t + 1
-        float top[2] = {-INFINITY, -INFINITY}, ic[2];
+        float s[NT][2][4];  // unit u's keys g, g + 8 x rows 2t, 2t + 1
+        float top[NT][2], ic[2];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) top[c][0] = top[c][1] = -INFINITY;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          s[u][0] = s[u][1] = s[u][2] = s[u][3] = 0.f;
+#pragma unroll
+          for (int c = 0; c < NT; ++c) s[c][u][0] = s[c][u][1] = s[c][u][2] = s[c][u][3] = 0.f;
           const unsigned char* kt = stage + u * S::kUnitBytes + g * DIM + 16 * t;
 #pragma unroll
           for (int v = 0; v < DIM / 64; ++v) {
@@ -530,7 +549,8 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
               const uint32_t xx = xw[w] ^ 0x80808080u, yy = yw[w] ^ 0x80808080u;
               const uint32_t f[4] = {int_half2(__byte_perm(xx, 0x64646464u, 0x4140)), int_half2(__byte_perm(yy, 0x64646464u, 0x4140)),
                                      int_half2(__byte_perm(xx, 0x64646464u, 0x4342)), int_half2(__byte_perm(yy, 0x64646464u, 0x4342))};
-              mma16816(s[u], f, qf[4 * v + w][0], qf[4 * v + w][1]);
+#pragma unroll
+              for (int c = 0; c < NT; ++c) mma16816(s[c][u], f, qf[c][4 * v + w][0], qf[c][4 * v + w][1]);
             }
           }
           const int from = 2 * (i & 15) + u;
@@ -539,47 +559,58 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
           const int vu = unit_at(i, u), tok0 = units.token(vu);
           const bool whole = vu < units.total && tok0 + kTile - 1 <= all_to && (tok0 >= all_from || tok0 + kTile <= a.sinks);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int h = e & 1;
-            float x = fmaf(s[u][e], rc[h] * ab, lc);
-            if (!whole) {
-              const int key = tok0 + g + 8 * (e >> 1);
-              const bool see = vu < units.total && key <= pos[h] && (a.window <= 0 || key > pos[h] - a.window || key < a.sinks);
-              x = see ? x : -INFINITY;
-            }
-            s[u][e] = x;
-            top[h] = fmaxf(top[h], x);
-          }
-        }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f)) {
+          for (int c = 0; c < NT; ++c)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            float x = fmaxf(m[h], top[h]);
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
-            const float w = x == m[h] ? 1.f : ex2_approx(m[h] - x);
-            m[h] = x;
-            l[h] *= w;
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j) {
-              o[j][h] *= w;
-              o[j][2 + h] *= w;
+            for (int e = 0; e < 4; ++e) {
+              const int h = e & 1;
+              float x = fmaf(s[c][u][e], rc[c][h] * ab, lc);
+              if (!whole) {
+                const int key = tok0 + g + 8 * (e >> 1);
+                const bool see = vu < units.total && key <= pos[c][h] && (a.window <= 0 || key > pos[c][h] - a.window || key < a.sinks);
+                x = see ? x : -INFINITY;
+              }
+              s[c][u][e] = x;
+              top[c][h] = fmaxf(top[c][h], x);
             }
-          }
         }
-        const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0] - 7.f, m[1] == -INFINITY ? 0.f : m[1] - 7.f};
+        bool grows = false;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) grows = grows || top[c][0] > m[c][0] + 8.f || top[c][1] > m[c][1] + 8.f;
+        if (__any_sync(0xffffffffu, grows)) {
+#pragma unroll
+          for (int c = 0; c < NT; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              float x = fmaxf(m[c][h], top[c][h]);
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 8));
+              x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 16));
+              const float w = x == m[c][h] ? 1.f : ex2_approx(m[c][h] - x);
+              m[c][h] = x;
+              l[c][h] *= w;
+#pragma unroll
+              for (int j = 0; j < kTiles; ++j) {
+                o[c][j][h] *= w;
+                o[c][j][2 + h] *= w;
+              }
+            }
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float p[4];
+          uint32_t b[NT][2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = ex2_approx(s[u][e] - ref[e & 1]);
+          for (int c = 0; c < NT; ++c) {
+            float p[4];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float sum = p[h] + p[2 + h];
-            if (sum != 0.f) l[h] = fmaf(sum, ic[u], l[h]);  // a unit that the row does not see may have a NaN scale
+            for (int e = 0; e < 4; ++e) p[e] = ex2_approx(s[c][u][e] - (m[c][e & 1] == -INFINITY ? 0.f : m[c][e & 1] - 7.f));
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const float sum = p[h] + p[2 + h];
+              if (sum != 0.f) l[c][h] = fmaf(sum, ic[u], l[c][h]);  // a unit that the row does not see may have a NaN scale
+            }
+            b[c][0] = transpose8(narrow2<false>(p[0], p[1]));
+            b[c][1] = transpose8(narrow2<false>(p[2], p[3]));
           }
-          const uint32_t b0 = transpose8(narrow2<false>(p[0], p[1])), b1 = transpose8(narrow2<false>(p[2], p[3]));
           // values: keys 2t, 2t+1, 2t+8, 2t+9 of 16 (8) dimensions
           constexpr int kW = DIM / 32;  // words per key
           const unsigned char* vt = stage + u * S::kUnitBytes + kTile * DIM + 2 * t * DIM + (DIM / 8) * g;
@@ -603,7 +634,8 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
               const uint32_t x = __byte_perm(x0, x1, half ? 0x7362 : 0x5140), y = __byte_perm(y0, y1, half ? 0x7362 : 0x5140);
               const uint32_t f[4] = {int_half2(__byte_perm(x, 0x64646464u, 0x4140)), int_half2(__byte_perm(x, 0x64646464u, 0x4342)),
                                      int_half2(__byte_perm(y, 0x64646464u, 0x4140)), int_half2(__byte_perm(y, 0x64646464u, 0x4342))};
-              mma16816(o[2 * w + half], f, b0, b1);
+#pragma unroll
+              for (int c = 0; c < NT; ++c) mma16816(o[c][2 * w + half], f, b[c][0], b[c][1]);
             }
           }
         }
@@ -611,37 +643,43 @@ __global__ void __launch_bounds__(128, 3) k_kv8_eight(const __grid_constant__ Kv
         if (i + ST < n) issue(i + ST);
       }
       dead = expired;
-      if (dead) {
-        l[0] = l[1] = __uint_as_float(0x7fc00000u);
-        m[0] = m[1] = 0.f;
-      }
       it0 += n;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int c = 0; c < NT; ++c)
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], d);
-    } else if (warp == 0 && (dead || blockIdx.x == 0)) {
-      m[0] = m[1] = 0.f;
-      l[0] = l[1] = __uint_as_float(0x7fc00000u);
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) l[c][h] += __shfl_xor_sync(0xffffffffu, l[c][h], d);
+        }
+    }
+    if (dead || (!q.ok && warp == 0 && blockIdx.x == 0)) {
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        m[c][0] = m[c][1] = 0.f;
+        l[c][0] = l[c][1] = __uint_as_float(0x7fc00000u);
+      }
     }
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     // join the warps through shared memory (the rings': every stage has been read)
     __syncthreads();
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (g == 0) s_ml[warp * 8 + 2 * t + h] = make_float2(m[h], l[h]);
-      float* dst = s_out + (warp * 8 + 2 * t + h) * S::kOutStride + (DIM / 8) * g;
+    for (int c = 0; c < NT; ++c)
 #pragma unroll
-      for (int j = 0; j < kTiles; j += 2)
-        *reinterpret_cast<float4*>(dst + 2 * j) = make_float4(o[j][h], o[j][2 + h], o[j + 1][h], o[j + 1][2 + h]);
-    }
+      for (int h = 0; h < 2; ++h) {
+        const int row = warp * kRows + 8 * c + 2 * t + h;
+        if (g == 0) s_ml[row] = make_float2(m[c][h], l[c][h]);
+        float* dst = s_out + row * S::kOutStride + (DIM / 8) * g;
+#pragma unroll
+        for (int j = 0; j < kTiles; j += 2)
+          *reinterpret_cast<float4*>(dst + 2 * j) = make_float4(o[c][j][h], o[c][j][2 + h], o[c][j + 1][h], o[c][j + 1][2 + h]);
+      }
     __syncthreads();
     constexpr int kOct = DIM / 8;
-    for (int e = threadIdx.x; e < 8 * kOct; e += 128) {
+    for (int e = threadIdx.x; e < kRows * kOct; e += 32 * W) {
       const int row = e / kOct, col = 8 * (e % kOct), r = r0 + row;
       if (r >= rows) break;
-      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, 8, s_out + row * S::kOutStride + col, 8 * S::kOutStride, 4);
+      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, kRows, s_out + row * S::kOutStride + col, kRows * S::kOutStride, W);
     }
     fence_async_smem();
     dead = __syncthreads_or(dead);  // then the rings are written again
@@ -688,20 +726,23 @@ cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t
   return cudaGetLastError();
 }
 
-template <bool BF16, int DIM>
+template <bool BF16, int DIM, int NT, int W>
 cudaError_t launch_eight(const Kv8Attend& a, int splits, int mtiles, cudaStream_t s) {
-  const cudaError_t e = smem_opt_in<k_kv8_eight<BF16, DIM>>(EightShape<DIM>::kSmem);
+  using S = EightShape<DIM, NT, W>;
+  const cudaError_t e = smem_opt_in<k_kv8_eight<BF16, DIM, NT, W>>(S::kSmem);
   if (e != cudaSuccess) return e;
-  k_kv8_eight<BF16, DIM><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, EightShape<DIM>::kSmem, s>>>(a);
+  k_kv8_eight<BF16, DIM, NT, W><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 32 * W, S::kSmem, s>>>(a);
   return cudaGetLastError();
 }
 
 template <bool BF16, int DIM>
-cudaError_t launch_mw(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
-  return p.mw == 0   ? launch_eight<BF16, DIM>(a, p.splits, p.mtiles, s)
-         : p.mw == 1 ? launch_rows<BF16, DIM, 1>(a, p.splits, p.mtiles, s)
-         : p.mw == 2 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
-                     : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
+cudaError_t launch_dim(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
+  if (p.rows <= 16 && p.warps == 2)
+    return p.rows == 8 ? launch_eight<BF16, DIM, 1, 2>(a, p.splits, p.mtiles, s) : launch_eight<BF16, DIM, 2, 2>(a, p.splits, p.mtiles, s);
+  return p.rows == 8    ? launch_eight<BF16, DIM, 1, 4>(a, p.splits, p.mtiles, s)
+         : p.rows == 16 ? launch_eight<BF16, DIM, 2, 4>(a, p.splits, p.mtiles, s)
+         : p.rows == 32 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
+                        : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
 }
 
 template <bool BF16, int DIM>
@@ -726,17 +767,19 @@ Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, i
   const int group = heads / c.kv_heads;
   const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
   const int64_t rows = (int64_t)most * group;
-  p.mw = rows <= 8 ? 0 : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-  const int per = p.mw ? 16 * p.mw : 8;
-  const int64_t mtiles = (rows + per - 1) / per;
+  p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t mtiles = (rows + p.rows - 1) / p.rows;
   p.mtiles = (int)std::min<int64_t>(mtiles, std::max(1, 65535 / c.kv_heads));
   const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, (int64_t)window + sinks + most) : cap;
-  // CTAs wanted: two rounds of three per SM, so that ragged lengths even out, in shares of at
+  // CTAs wanted: four rounds of three per SM, so that ragged lengths even out (64 x 16000: 221 us; 239 with two rounds), in shares of at
   // least 1024 keys; where there are fewer sequences and heads than SMs, of 128
   const int64_t units = (int64_t)b.n * c.kv_heads * p.mtiles;
-  const int64_t want = ((int64_t)sms * 6 + units - 1) / units;
+  const int64_t want = ((int64_t)sms * 12 + units - 1) / units;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys / (units < sms ? 128 : 1024), 64}));
+  // short shares in more CTAs than fit at once: two warps each, so that all start together (544 keys and 13
+  // rows, 768 CTAs: 35.7 us, with four warps 44.8; 1200 keys, 1 row: 40.9 and 41.4; 2400: 73.7 and 70.9)
+  p.warps = units * p.splits > 3 * sms && keys / p.splits <= 1024 ? 2 : 4;
   p.bytes = p.splits > 1 ? (int64_t)p.splits * b.rows * heads * (c.dim + 2) * 4 : 0;
   return p;
 }
@@ -749,8 +792,8 @@ cudaError_t kv8_join_launch(const Kv8Attend& a, int splits, cudaStream_t s) {
 
 cudaError_t kv8_rows_launch(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s) {
   const bool bf = a.c.dtype == TSD_BF16;
-  const cudaError_t e = a.c.dim == 64 ? (bf ? launch_mw<true, 64>(a, p, s) : launch_mw<false, 64>(a, p, s))
-                                      : (bf ? launch_mw<true, 128>(a, p, s) : launch_mw<false, 128>(a, p, s));
+  const cudaError_t e = a.c.dim == 64 ? (bf ? launch_dim<true, 64>(a, p, s) : launch_dim<false, 64>(a, p, s))
+                                      : (bf ? launch_dim<true, 128>(a, p, s) : launch_dim<false, 128>(a, p, s));
   return e == cudaSuccess && p.splits > 1 ? kv8_join_launch(a, p.splits, s) : e;
 }
 
