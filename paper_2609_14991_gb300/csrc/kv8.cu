@@ -10,6 +10,7 @@
 #include <climits>
 
 #include "kv8.h"
+#include "tc_common.cuh"
 
 namespace tsd {
 
@@ -31,36 +32,63 @@ __device__ __forceinline__ float wide(uint32_t u) {
   return __half2float(__ushort_as_half((unsigned short)u));
 }
 
-// x / s rounded to the nearest integer, ties to even, of the exact quotient
-// (s > 0, |x / s| below 128).  r is off by less than 2^-15, so only a quotient that
-// near to a half needs the exact side: the sign of x - h s, which a fused
-// multiply-add has right.
-__device__ __forceinline__ int round_quotient(float x, float s, float inv) {
-  const float r = x * inv;
+// Eight quotients x / s rounded to nearest even, as bytes (|x / s| below 127.5, s >
+// 2^-40).  r = x (1 / s) is off by less than 2^-15; adding 1.5 * 2^23 leaves its nearest
+// integer in the low bits.  Only a quotient that near to a half needs more: the exact side
+// is the sign of x - h s, which a fused multiply-add has right.
+constexpr float kMagic = 12582912.f;
+__device__ __forceinline__ float beside_half(float x, float s, float r) {
   float q = rintf(r);
   const float d = r - q;
-  if (fabsf(fabsf(d) - 0.5f) < 0x1p-14f) {
+  if (fabsf(d) > 0.5f - 0x1p-14f) {
     const float h = d > 0.f ? q + 0.5f : q - 0.5f;
     const float rem = fmaf(-h, s, x);
     q = rem > 0.f ? h + 0.5f : rem < 0.f ? h - 0.5f : rintf(h);
   }
-  return (int)fminf(fmaxf(q, -127.f), 127.f);
+  return q + kMagic;
+}
+__device__ __forceinline__ uint2 round8(const float (&x)[8], float s, float inv) {
+  const uint64_t v2 = tc::pair_of(inv, inv), up = tc::pair_of(kMagic, kMagic), down = tc::pair_of(-kMagic, -kMagic);
+  float m[8], far = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; j += 2) {
+    const uint64_t r = tc::mul2(tc::pair_of(x[j], x[j + 1]), v2), t = tc::add2(r, up);
+    float q0, q1, r0, r1;
+    tc::unpair(t, m[j], m[j + 1]);
+    tc::unpair(tc::add2(t, down), q0, q1);
+    tc::unpair(r, r0, r1);
+    far = fmaxf(far, fmaxf(fabsf(r0 - q0), fabsf(r1 - q1)));
+  }
+  if (far > 0.5f - 0x1p-14f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m[j] = beside_half(x[j], s, x[j] * inv);
+  }
+  const auto bytes = [](float a, float b, float c, float d) {
+    return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040), __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
+  };
+  return make_uint2(bytes(m[0], m[1], m[2], m[3]), bytes(m[4], m[5], m[6], m[7]));
 }
 
-// One CTA per touched block, head, and keys or values.  Each thread holds
-// BLOCK * DIM / 128 elements as packed 16-bit vectors: one read, the largest
+// A touched block, head, and keys or values is one unit: 64 elements per thread
+// (32 in the smallest blocks), so a unit is a warp, two or four, and CTAs of 128 threads hold 4, 2 or 1.  A
+// thread holds its elements as packed 16-bit vectors: one read, the largest
 // magnitude from the patterns (they order as integers without the sign, NaN
 // and infinity above every number), one write.  Bound by memory: 2 bytes in, 1 out
-// per element; the largest case holds 64 elements a thread.
+// per element.
 template <bool BF16, int BLOCK, int DIM>
-__global__ void __launch_bounds__(kThreads) k_kv8_append(const __grid_constant__ AppendArgs a) {
-  constexpr int kVecs = BLOCK * DIM / 8 / kThreads;  // 8-element vectors per thread
+__global__ void __launch_bounds__(kThreads, 8) k_kv8_append(const __grid_constant__ AppendArgs a) {
+  constexpr int T = BLOCK * DIM / 64 < 32 ? 32 : BLOCK * DIM / 64;  // threads per unit
+  constexpr int kVecs = BLOCK * DIM / 8 / T;                        // 8-element vectors per thread
   constexpr int kCols = DIM / 8;
   __shared__ uint32_t s_top[kThreads / 32];
-  const int t = threadIdx.x;
-  const int head = blockIdx.y >> 1, which = blockIdx.y & 1;
+  const int u = threadIdx.x / T, t = threadIdx.x % T, unit = blockIdx.y * (kThreads / T) + u;
   const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
-  if (!q.ok || q.count == 0) return;
+  if (!q.ok || q.count == 0 || unit >= 2 * a.c.kv_heads) return;  // whole units
+  const auto sync = [&]() {
+    if constexpr (T == 32) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + u), "n"(T) : "memory");
+  };
+  const int head = unit >> 1, which = unit & 1;
   const int start = q.len - q.count;  // first new token
   const int b0 = start / BLOCK, b1 = (q.len - 1) / BLOCK;
   const uint16_t* src = (which ? a.src[1] : a.src[0]) + head * (which ? a.head[1] : a.head[0]);
@@ -70,51 +98,57 @@ __global__ void __launch_bounds__(kThreads) k_kv8_append(const __grid_constant__
     return tail + ((((size_t)q.slot * 2 + (b & 1)) * a.c.kv_heads + head) * BLOCK + tok) * DIM + col * 8;
   };
   for (int b = b0 + (int)blockIdx.x; b <= b1; b += gridDim.x) {
+    const int id = __ldg(a.b.table + (size_t)q.slot * a.b.table_width + b);
     uint4 x[kVecs];
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
-      const int e = t + i * kThreads, tok = e / kCols, col = e % kCols;
+      const int e = t + i * T, tok = e / kCols, col = e % kCols;
       const int pos = b * BLOCK + tok;
       x[i] = make_uint4(0, 0, 0, 0);
       if (pos < start) x[i] = *reinterpret_cast<const uint4*>(tail_at(b, tok, col));
       else if (pos < q.len)
         x[i] = __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(q.row0 + pos - start) * stride + col * 8));
+    }
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
       const uint32_t m = 0x7fff7fffu;
       top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & m, x[i].y & m), __vmaxu2(x[i].z & m, x[i].w & m)));
     }
-    top = max(top & 0xffffu, top >> 16);
-    top = __reduce_max_sync(0xffffffffu, top);
-    __syncthreads();  // the last block's use of s_top, and (first block) its reads of the tail
-    if ((t & 31) == 0) s_top[t >> 5] = top;
-    __syncthreads();
-    top = max(max(s_top[0], s_top[1]), max(s_top[2], s_top[3]));
+    top = __reduce_max_sync(0xffffffffu, max(top & 0xffffu, top >> 16));
+    sync();  // the last block's use of s_top, and (first block) its reads of the tail
+    if constexpr (T > 32) {
+      if ((t & 31) == 0) s_top[threadIdx.x >> 5] = top;
+      sync();
+      const uint32_t* mine = s_top + u * (T / 32);
+#pragma unroll
+      for (int i = 0; i < T / 32; ++i) top = max(top, mine[i]);
+    }
     const float big = wide<BF16>(top);
     const bool fine = big <= kKv8Most;  // false for NaN and infinity
     const float s = fmaxf(big, kKv8Least) * (1.f / 127.f), inv = 1.f / s;
-    const int id = __ldg(a.b.table + (size_t)q.slot * a.b.table_width + b);
     if (id >= 0 && id < a.c.n_blocks) {
       int8_t* out = static_cast<int8_t*>(which ? a.c.v : a.c.k) + ((size_t)id * a.c.kv_heads + head) * BLOCK * DIM;
 #pragma unroll
       for (int i = 0; i < kVecs; ++i) {
+        if (b * BLOCK + (t + i * T) / kCols >= q.len) break;  // not yet tokens: left as they are
         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        uint32_t y[2] = {0, 0};
+        uint2 y = make_uint2(0, 0);
         if (fine) {
+          float v[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int v = round_quotient(wide<BF16>((w[j / 2] >> (16 * (j & 1))) & 0xffffu), s, inv);
-            y[j / 4] |= (uint32_t)(v & 0xff) << (8 * (j & 3));
-          }
+          for (int j = 0; j < 4; ++j) v[2 * j] = wide<BF16>(w[j] & 0xffffu), v[2 * j + 1] = BF16 ? __uint_as_float(w[j] & 0xffff0000u) : wide<BF16>(w[j] >> 16);
+          y = round8(v, s, inv);
         }
-        *reinterpret_cast<uint2*>(out + (size_t)(t + i * kThreads) * 8) = make_uint2(y[0], y[1]);
+        *reinterpret_cast<uint2*>(out + (size_t)(t + i * T) * 8) = y;
       }
       if (t == 0) (which ? a.c.v_scale : a.c.k_scale)[(size_t)id * a.c.kv_heads + head] = fine ? s : __uint_as_float(0x7fc00000u);
     }
     if (b == b0) {
-      // originals of the new tokens in the last two blocks: written by the CTA that has
+      // originals of the new tokens in the last two blocks: written by the unit that has
       // read the old ones (all of its threads have, above), in rows that no other reads
       const int from = max(start, (b1 - 1) * BLOCK);
-      for (int e = t; e < (q.len - from) * kCols; e += kThreads) {
+      for (int e = t; e < (q.len - from) * kCols; e += T) {
         const int pos = from + e / kCols, col = e % kCols;
         *reinterpret_cast<uint4*>(tail_at(pos / BLOCK, pos % BLOCK, col)) =
             __ldg(reinterpret_cast<const uint4*>(src + (int64_t)(q.row0 + pos - start) * stride + col * 8));
@@ -123,17 +157,19 @@ __global__ void __launch_bounds__(kThreads) k_kv8_append(const __grid_constant__
   }
 }
 
-// The sequence that holds row r: the last i with starts[i] <= r.
-__device__ __forceinline__ int seq_of(const tsd_kv8_batch& b, int r) {
+// The sequence that holds a warp's row r: the last i with starts[i] <= r; -1: none.  Each
+// round takes 32 probes at once.
+__device__ __forceinline__ int seq_of(const tsd_kv8_batch& b, int r, int lane) {
   if (!b.starts) return r < b.n ? r : -1;
-  int lo = 0, hi = b.n;  // starts[lo] <= r < starts[hi], where both hold
-  if (r < __ldg(b.starts) || r >= __ldg(b.starts + b.n)) return -1;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (__ldg(b.starts + mid) <= r) lo = mid;
-    else hi = mid;
-  }
-  return lo;
+  int lo = 0, hi = b.n + 1;  // starts[lo] <= r < starts[hi], where both hold
+  do {
+    const int step = (hi - lo + 31) / 32, at = lo + step * lane;
+    const unsigned below = __ballot_sync(0xffffffffu, at < hi && __ldg(b.starts + at) <= r);
+    if (!below) return -1;
+    lo += step * (31 - __clz(below));
+    hi = min(lo + step, hi);
+  } while (hi - lo > 1);
+  return lo < b.n ? lo : -1;
 }
 
 // One warp per row: its keys and values, all heads.  Bound by the writes (4 bytes an element).
@@ -142,7 +178,7 @@ __global__ void __launch_bounds__(256) k_kv8_read(const __grid_constant__ tsd_kv
                                                   float* k_out, float* v_out) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (r >= b.rows) return;
-  const int i = seq_of(b, r);
+  const int i = seq_of(b, r, lane);
   if (i < 0) return;  // behind the last sequence
   const Kv8Seq q = kv8_seq(c, b, i);
   if (r < q.row0 || r >= q.row0 + q.count) return;
@@ -177,17 +213,24 @@ __global__ void __launch_bounds__(256) k_kv8_read(const __grid_constant__ tsd_kv
   }
 }
 
-template <bool BF16, int BLOCK>
+template <bool BF16, int BLOCK, int DIM>
 void launch_append(const AppendArgs& a, dim3 grid, cudaStream_t s) {
-  if (a.c.dim == 64) k_kv8_append<BF16, BLOCK, 64><<<grid, kThreads, 0, s>>>(a);
-  else k_kv8_append<BF16, BLOCK, 128><<<grid, kThreads, 0, s>>>(a);
+  constexpr int T = BLOCK * DIM / 64 < 32 ? 32 : BLOCK * DIM / 64, kUnits = kThreads / T;
+  grid.y = (2 * a.c.kv_heads + kUnits - 1) / kUnits;
+  k_kv8_append<BF16, BLOCK, DIM><<<grid, kThreads, 0, s>>>(a);
+}
+
+template <bool BF16, int BLOCK>
+void launch_append_dim(const AppendArgs& a, dim3 grid, cudaStream_t s) {
+  if (a.c.dim == 64) launch_append<BF16, BLOCK, 64>(a, grid, s);
+  else launch_append<BF16, BLOCK, 128>(a, grid, s);
 }
 
 template <bool BF16>
 void launch_append_type(const AppendArgs& a, dim3 grid, cudaStream_t s) {
-  if (a.c.block == 16) launch_append<BF16, 16>(a, grid, s);
-  else if (a.c.block == 32) launch_append<BF16, 32>(a, grid, s);
-  else launch_append<BF16, 64>(a, grid, s);
+  if (a.c.block == 16) launch_append_dim<BF16, 16>(a, grid, s);
+  else if (a.c.block == 32) launch_append_dim<BF16, 32>(a, grid, s);
+  else launch_append_dim<BF16, 64>(a, grid, s);
 }
 
 }  // namespace
@@ -237,7 +280,7 @@ extern "C" tsd_status tsd_kv8_append(const tsd_kv8* cache, const tsd_kv8_batch* 
   AppendArgs a{*cache, *batch, {static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v)}, {k_row, v_row}, {k_head, v_head}};
   const int most = batch->max_new ? (batch->max_new < batch->rows ? batch->max_new : batch->rows) : batch->rows;
   const int64_t blocks = ((int64_t)most + 2 * cache->block - 2) / cache->block;
-  const dim3 grid((unsigned)blocks, 2 * cache->kv_heads, batch->n);
+  const dim3 grid((unsigned)blocks, 1, batch->n);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (cache->dtype == TSD_BF16) launch_append_type<true>(a, grid, s);
   else launch_append_type<false>(a, grid, s);
