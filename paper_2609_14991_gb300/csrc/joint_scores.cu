@@ -581,6 +581,9 @@ __global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant
   const float2* cand = a.cand + row * a.segs * cap;
   const float c = a.o.inv_temp * kLog2e;
   if (l == 0) s_count[slot] = 0;
+  // the given labels and their logits
+  const int label = live && l < a.o.m ? __ldg(a.o.labels + row * a.o.m + l) : -1;
+  const float x = label >= 0 && label < a.C ? a.given[row * a.o.m + l] : 0.f;
   // sums, of each partial result by one lane; values, by all
   float m = -INFINITY, s = 0.f, e = 0.f;
   float best[K > 0 ? K : 1];
@@ -645,12 +648,10 @@ __global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant
       merge_top<K>(best, b);
     }
   }
-  const RowSums sums{m, s, e};
+  const RowScore sums(RowSums{m, s, e});
   if (live) {
-    label_finish(a.o, row, sums, l, [&](int label) {
-      if (label >= a.C) return __uint_as_float(0x7fc00000u);
-      return a.given[row * a.o.m + l];
-    });
+    if (l < a.o.m) a.o.logp[row * a.o.m + l] = label_given(a.o, sums, label, label < a.C ? x : __uint_as_float(0x7fc00000u));
+    if (l == 0 && a.o.entropy) a.o.entropy[row] = sums.entropy;
   }
   if constexpr (K > 0) {
     const float bound = best[K - 1];

@@ -21,8 +21,6 @@ struct LabelArgs {
 // (x - m) log2(e) / T (m = 0 in the exponents of a row without finite logits).
 struct RowSums {
   float m, S, E;
-  // NaN or +inf among the logits: the sums are NaN, as inf - inf is
-  __device__ __forceinline__ bool odd() const { return !(S >= 0.f) || m == INFINITY; }
 };
 
 // max that keeps NaN
@@ -32,33 +30,34 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
-// y - lse of a logit of the row
-__device__ __forceinline__ float label_logp(const RowSums& r, float inv_temp, float x) {
-  if (r.odd()) return __uint_as_float(0x7fc00000u);
-  if (r.m == -INFINITY) return x == -INFINITY ? x : __uint_as_float(0x7fc00000u);
-  return (x - r.m) * inv_temp - logf(r.S);
-}
-
-// The given labels' scores and the entropy, by one warp; logit(l): the row's
-// logit of label l >= 0 (NaN outside its labels).
-template <class F>
-__device__ __forceinline__ void label_finish(const LabelArgs& a, int64_t row, const RowSums& r, int lane, F logit) {
-  if (lane < a.m) {
-    const int l = a.labels[row * a.m + lane];
-    float y = __uint_as_float(0x7fc00000u);
-    if (l == -1) y = 0.f;
-    else if (l >= 0) y = label_logp(r, a.inv_temp, logit(l));
-    a.logp[row * a.m + lane] = y;
+// What a row's scores are made of.
+struct RowScore {
+  float m, ln_s, entropy;
+  bool odd;  // NaN or +inf among the logits: the sums are NaN, as inf - inf is
+  __device__ __forceinline__ explicit RowScore(const RowSums& r) {
+    m = r.m;
+    ln_s = logf(r.S);
+    odd = !(r.S >= 0.f) || r.m == INFINITY;
+    entropy = odd ? __uint_as_float(0x7fc00000u) : m == -INFINITY ? 0.f : fmaxf(0.f, ln_s - 0.693147180559945f * (r.E / r.S));
   }
-  if (lane == 0 && a.entropy)
-    a.entropy[row] = r.odd() ? __uint_as_float(0x7fc00000u) : r.m == -INFINITY ? 0.f : fmaxf(0.f, logf(r.S) - 0.693147180559945f * (r.E / r.S));
+  // y - lse of a logit of the row
+  __device__ __forceinline__ float logp(float inv_temp, float x) const {
+    if (odd) return __uint_as_float(0x7fc00000u);
+    if (m == -INFINITY) return x == -INFINITY ? x : __uint_as_float(0x7fc00000u);
+    return (x - m) * inv_temp - ln_s;
+  }
+};
+
+// The score of given label l with logit x (NaN outside the row).
+__device__ __forceinline__ float label_given(const LabelArgs& a, const RowScore& r, int l, float x) {
+  return l == -1 ? 0.f : l >= 0 ? r.logp(a.inv_temp, x) : __uint_as_float(0x7fc00000u);
 }
 
 // Alternative j: the logit and label found (-inf: none).
-__device__ __forceinline__ void label_alternative(const LabelArgs& a, int64_t row, int j, const RowSums& r, float x, int label) {
-  const bool none = r.odd() || !(x > -INFINITY);
+__device__ __forceinline__ void label_alternative(const LabelArgs& a, int64_t row, int j, const RowScore& r, float x, int label) {
+  const bool none = r.odd || !(x > -INFINITY);
   a.alt_labels[row * a.k + j] = none ? -1 : label;
-  a.alt_logp[row * a.k + j] = r.odd() ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : label_logp(r, a.inv_temp, x);
+  a.alt_logp[row * a.k + j] = r.odd ? __uint_as_float(0x7fc00000u) : none ? -INFINITY : r.logp(a.inv_temp, x);
 }
 
 // The scores of n rows of logits in memory (scores.cu), ld elements apart; after: once

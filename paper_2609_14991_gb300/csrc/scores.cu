@@ -8,9 +8,10 @@
 // x_i - m is formed first (exact or rounded once), so a row's offset costs no
 // precision.  A row stays in registers (32 or 64 logits per thread): 32 to 512 threads
 // per row, above 16384 logits a cluster of 2 to 8 CTAs of 512 that exchange
-// through distributed shared memory.  The k largest: the threads form 16 groups (per CTA), the
-// groups 8 classes (4 where k <= 4); the least of the classes' maxima is a bound that at least
-// k logits reach and few pass (about 22 of random ones for 8), so only those are gathered and ordered.  If more
+// through distributed shared memory.  The k largest: the threads form 16 groups (per CTA); the
+// k-th largest of the groups' maxima is a bound that at least k logits reach and few pass
+// (about 11 of random ones for 8; the least of eight classes' maxima let 22 pass, which took 1.4 times as long in all).  Threads that hold one
+// leave it with its seven neighbours; one warp picks and orders.  If more
 // than the gathering holds reach it (many equal logits), k rounds of a maximum over
 // the whole row take its place.
 #include <cooperative_groups.h>
@@ -35,19 +36,22 @@ struct RowsArgs {
   int n, C;
 };
 
-constexpr int kCap = 256;    // logits gathered per row
+constexpr int kCap = 64;     // logits that the last step takes
 constexpr int kGroups = 16;  // groups of a CTA's threads (of a row's, where a warp takes one)
 
 // A row's shared memory.  In a cluster every CTA writes its groups' maxima
 // into each CTA's and its sums into the first CTA's; the first one fetches the
-// logits gathered by the others.
+// eights gathered by the others.
 template <int CS>
 struct RowShared {
-  float top[kGroups * CS];  // groups' maxima
-  float2 sums[16 * CS];     // warps' S and E
-  float cv[kCap];           // gathered logits and their labels
+  static constexpr int kEights = CS == 1 ? 64 : 128;  // gathered per row
+  float top[kGroups * CS];                            // groups' maxima
+  float2 sums[16 * CS];                               // warps' S and E
+  float4 eight[kEights][2];                           // eight logits of a thread, one of which reaches the bound
+  int code[kEights];                                  // whose and which; below 0: a single logit's label, ~label
+  float cv[kCap];                                     // the logits that reach it, and their labels
   int ci[kCap];
-  int count;         // this CTA's logits that reach the bound
+  int count;         // this CTA's eights
   float best_v[16];  // warps' best of a round over the whole row
   int best_i[16];
 };
@@ -95,12 +99,12 @@ __device__ __forceinline__ void warp_best(float& v, int& i) {
 }
 
 template <typename T, int G, int CS, int E>
-__global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 32 ? 128 : G)) k_label_rows(const __grid_constant__ RowsArgs a) {
   constexpr int VE = 16 / sizeof(T), NV = E / VE;
   constexpr int kWarps = G / 32;
   constexpr int kLanes = G / kGroups;  // threads of a group
   constexpr int kRows = G == 32 ? 4 : 1;
-  constexpr int kSub = E < 8 ? E : 8;  // logits whose maximum is kept for the gathering
+  constexpr int kEights = E / 8;  // a thread's logits in eights
   __shared__ RowShared<CS> s_rows[kRows];
   const int warp_in_cta = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slot = G == 32 ? warp_in_cta : 0, warp = G == 32 ? 0 : warp_in_cta;
@@ -148,21 +152,28 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
       }
     }
   }
+  // the given labels' logits, on their way early
+  int given = -1;
+  float given_x = __uint_as_float(0x7fc00000u);
+  if (rt < a.o.m) {
+    given = __ldg(a.o.labels + row * a.o.m + rt);
+    if (given >= 0 && given < C) given_x = to_float(x[given]);
+  }
   const int xi = rt < lead ? rt : rt < lead + tail ? nvec * VE + rt : -1;
   const float xv = xi >= 0 ? to_float(x[xi]) : -INFINITY;
   const auto label_of = [&](int e) { return lead + (rt + e / VE * G * CS) * VE + e % VE; };
 
   // maxima: of eight logits each, the thread's, the groups'
-  float sub[E / kSub];
+  float sub[kEights];
 #pragma unroll
-  for (int i = 0; i < E / kSub; ++i) {
-    sub[i] = v[i * kSub];
+  for (int i = 0; i < kEights; ++i) {
+    sub[i] = v[i * 8];
 #pragma unroll
-    for (int j = 1; j < kSub; ++j) sub[i] = fmaxf(sub[i], v[i * kSub + j]);
+    for (int j = 1; j < 8; ++j) sub[i] = fmaxf(sub[i], v[i * 8 + j]);
   }
   float mine = xv;
 #pragma unroll
-  for (int i = 0; i < E / kSub; ++i) mine = fmaxf(mine, sub[i]);
+  for (int i = 0; i < kEights; ++i) mine = fmaxf(mine, sub[i]);
   if (!(mine >= -INFINITY)) mine = INFINITY;  // NaN alone: the sums say so
   float gm = mine;
 #pragma unroll
@@ -178,18 +189,24 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
   }
   if (t == 0) sh.count = 0;
   sync_row();
-  // The row's maximum, and a bound that k logits reach: the groups in 8 (or 4)
-  // classes, the least of the classes' maxima.
-  constexpr int kKeys = CS > 1 ? kGroups * CS / 32 : 1;
+  // The row's maximum, and the k-th largest of the groups' maxima: a lane's place is the
+  // number of larger ones (in a cluster of 32 classes of groups).
+  constexpr int kClasses = CS > 1 ? 32 : kGroups;
   int key = order_of(sh.top[lane % (kGroups * CS)]);
 #pragma unroll
-  for (int i = 1; i < kKeys; ++i) key = max(key, order_of(sh.top[lane + 32 * i]));
+  for (int i = 1; i < kGroups * CS / 32; ++i) key = max(key, order_of(sh.top[lane + 32 * i]));
   const float m = value_of(__reduce_max_sync(0xffffffffu, key));
-  key = max(key, __shfl_xor_sync(0xffffffffu, key, 8));
-  if (CS > 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, 16));
-  if (k <= 4) key = max(key, __shfl_xor_sync(0xffffffffu, key, 4));
-  if (k == 1) key = max(key, max(__shfl_xor_sync(0xffffffffu, key, 1), __shfl_xor_sync(0xffffffffu, key, 2)));
-  const float bound = value_of(__reduce_min_sync(0xffffffffu, key));
+  float bound = -INFINITY;
+  if (k > 0) {
+    int place = 0;
+#pragma unroll
+    for (int d = 1; d < kClasses; ++d) {
+      const int other = __shfl_xor_sync(0xffffffffu, key, d);
+      // of equal ones the lower lane's comes first: this one has d's highest bit where the partner is lower
+      place += other > key || (other == key && (lane & (1 << (31 - __clz(d)))) != 0) ? 1 : 0;
+    }
+    bound = value_of(__shfl_sync(0xffffffffu, key, __ffs(__ballot_sync(0xffffffffu, place == k - 1)) - 1));
+  }
 
   // sums: in pairs, a masked logit's exponent held finite (its term is 0 all the same)
   const float ms = m == -INFINITY ? 0.f : m, c = a.o.inv_temp * kLog2e;
@@ -222,25 +239,27 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
   }
   if (lane == 0) peer(0)->sums[rank * kWarps + warp] = make_float2(S, E2);
 
-  // gather what reaches the bound; a list that has run over is not counted on
-  constexpr int kMine = kCap / CS;
+  // gather the eights with a logit that reaches the bound
+  constexpr int kMine = RowShared<CS>::kEights / CS;
   if (k > 0 && mine >= bound && mine > -INFINITY) {
-    const auto take = [&](float y, int label) {
-      if (y >= bound && y > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < kEights; ++i)
+      if (sub[i] >= bound) {
         const int at = atomicAdd(&sh.count, 1);
         if (at < kMine) {
-          sh.cv[at] = y;
-          sh.ci[at] = label;
+          sh.eight[at][0] = make_float4(v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3]);
+          sh.eight[at][1] = make_float4(v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]);
+          sh.code[at] = rt * kEights + i;
         }
       }
-    };
-#pragma unroll
-    for (int i = 0; i < E / kSub; ++i)
-      if (sub[i] >= bound && *(volatile int*)&sh.count <= kMine) {
-#pragma unroll
-        for (int j = 0; j < kSub; ++j) take(v[i * kSub + j], label_of(i * kSub + j));
+    if (xv >= bound && xi >= 0) {
+      const int at = atomicAdd(&sh.count, 1);
+      if (at < kMine) {
+        sh.eight[at][0] = make_float4(xv, -INFINITY, -INFINITY, -INFINITY);
+        sh.eight[at][1] = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        sh.code[at] = ~xi;
       }
-    take(xv, xi);
+    }
   }
   sync_row();
 
@@ -253,59 +272,111 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
       for (int r = 1; r < CS; ++r) theirs[r] = peer(r)->count;
 #pragma unroll
       for (int r = 1; r < CS; ++r) over = over || theirs[r] > kMine;
-      if (!over) {  // kMine <= 128 threads copy a list
-        static_assert(kMine <= G, "a thread per gathered logit");
+      if (!over) {
+        static_assert(kMine <= G, "a thread per gathered eight");
 #pragma unroll
         for (int r = 1; r < CS; ++r) {
           if (t < theirs[r]) {
-            sh.cv[count + t] = peer(r)->cv[t];
-            sh.ci[count + t] = peer(r)->ci[t];
+            sh.eight[count + t][0] = peer(r)->eight[t][0];
+            sh.eight[count + t][1] = peer(r)->eight[t][1];
+            sh.code[count + t] = peer(r)->code[t];
           }
           count += theirs[r];
         }
       }
     }
     cg::this_cluster().sync();  // the others' memory has been read
+    if (rank != 0) return;
   }
-  if (rank != 0 || (!over && warp != 0)) return;
-  RowSums sums{m, 0.f, 0.f};
-  if (warp == 0) {
+  if (!over && warp != 0) return;
+  RowSums total{m, 0.f, 0.f};
+  if constexpr (kWarps == 1) {
+    total.S = S;
+    total.E = E2;
+  } else if (warp == 0) {
 #pragma unroll
     for (int i = 0; i < (kWarps * CS + 31) / 32; ++i) {
       const float2 y = lane + 32 * i < kWarps * CS ? sh.sums[lane + 32 * i] : make_float2(0.f, 0.f);
-      sums.S += y.x;
-      sums.E += y.y;
+      total.S += y.x;
+      total.E += y.y;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
-      sums.S += __shfl_xor_sync(0xffffffffu, sums.S, o);
-      sums.E += __shfl_xor_sync(0xffffffffu, sums.E, o);
+      total.S += __shfl_xor_sync(0xffffffffu, total.S, o);
+      total.E += __shfl_xor_sync(0xffffffffu, total.E, o);
     }
-    label_finish(a.o, row, sums, lane, [&](int l) { return l < C ? to_float(x[l]) : __uint_as_float(0x7fc00000u); });
   }
+  const RowScore sums(total);
+  if (t < a.o.m) a.o.logp[row * a.o.m + t] = label_given(a.o, sums, given, given_x);
+  if (t == 0 && a.o.entropy) a.o.entropy[row] = sums.entropy;
 
   // the k best in order
+  if (!over) {
+    if (k == 0) return;
+    // the gathered eights' logits that reach the bound, with their labels
+    int found = 0;
+    for (int base = 0; base < count; base += 32) {
+      const int at = base + lane;
+      float y[8];
+      int code = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = -INFINITY;
+      if (at < count) {
+        const float4 x0 = sh.eight[at][0], x1 = sh.eight[at][1];
+        y[0] = x0.x, y[1] = x0.y, y[2] = x0.z, y[3] = x0.w, y[4] = x1.x, y[5] = x1.y, y[6] = x1.z, y[7] = x1.w;
+        code = sh.code[at];
+      }
+      const int first = code % kEights * 8, owner = code / kEights;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool in = y[j] >= bound && y[j] > -INFINITY;
+        const unsigned who = __ballot_sync(0xffffffffu, in);
+        if (in) {
+          const int to = found + __popc(who & ((1u << lane) - 1)), e = first + j;
+          if (to < kCap) {
+            sh.cv[to] = y[j];
+            sh.ci[to] = code < 0 ? ~code : lead + (owner + e / VE * G * CS) * VE + e % VE;
+          }
+        }
+        found += __popc(who);
+      }
+    }
+    __syncwarp();
+    if (found <= 32) {  // a logit's place is the number of better ones
+      const float y0 = lane < found ? sh.cv[lane] : -INFINITY;
+      const int i0 = lane < found ? sh.ci[lane] : 0x7fffffff;
+      int place = 0;
+#pragma unroll 4
+      for (int j = 0; j < found; ++j) place += before(__shfl_sync(0xffffffffu, y0, j), __shfl_sync(0xffffffffu, i0, j), y0, i0) ? 1 : 0;
+      if (lane < found && place < k) label_alternative(a.o, row, place, sums, y0, i0);
+      if (lane >= found && lane < k) label_alternative(a.o, row, lane, sums, -INFINITY, -1);  // fewer than k
+      return;
+    }
+    over = found > kCap;
+    if (!over) {
+      float pv = INFINITY;
+      int pi = -1;
+      for (int r = 0; r < k; ++r) {
+        float bv = -INFINITY;
+        int bi = 0x7fffffff;
+        for (int i = lane; i < found; i += 32) {
+          const float y = sh.cv[i];
+          const int l = sh.ci[i];
+          if (before(pv, pi, y, l) && before(y, l, bv, bi)) bv = y, bi = l;
+        }
+        warp_best(bv, bi);
+        if (lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
+        pv = bv;
+        pi = bi;
+      }
+      return;
+    }
+  }
+  // Many equal logits: a maximum over the whole row per round, by all threads where the
+  // eights had no room, by one warp from memory where their logits had none.
+  const bool alone = count <= kMine;
   float pv = INFINITY;
   int pi = -1;
-  if (!over) {
-    const float y0 = lane < count ? sh.cv[lane] : -INFINITY;
-    const int i0 = lane < count ? sh.ci[lane] : 0x7fffffff;
-    for (int r = 0; r < k; ++r) {
-      const bool open = before(pv, pi, y0, i0);
-      float bv = open ? y0 : -INFINITY;
-      int bi = open ? i0 : 0x7fffffff;
-      for (int i = lane + 32; i < count; i += 32) {
-        const float y = sh.cv[i];
-        const int l = sh.ci[i];
-        if (before(pv, pi, y, l) && before(y, l, bv, bi)) bv = y, bi = l;
-      }
-      warp_best(bv, bi);
-      if (lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
-      pv = bv;
-      pi = bi;
-    }
-    return;
-  }
   for (int r = 0; r < k; ++r) {
     float bv = -INFINITY;
     int bi = 0x7fffffff;
@@ -315,23 +386,25 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G) k_label_rows(const __grid_c
         bi = i;
       }
     };
-    if constexpr (CS == 1) {
+    if (CS > 1 || alone) {  // the first CTA, or its first warp
+      for (int i = t; i < C; i += alone ? 32 : G) look(to_float(x[i]), i);
+    } else {
 #pragma unroll
       for (int e = 0; e < E; ++e) look(v[e], label_of(e));
       if (xi >= 0) look(xv, xi);
-    } else {  // the first CTA alone, from memory
-      for (int i = t; i < C; i += G) look(to_float(x[i]), i);
     }
     warp_best(bv, bi);
-    if (lane == 0) {
-      sh.best_v[warp] = bv;
-      sh.best_i[warp] = bi;
+    if (!alone) {
+      if (lane == 0) {
+        sh.best_v[warp] = bv;
+        sh.best_i[warp] = bi;
+      }
+      sync_cta();
+      bv = lane < kWarps ? sh.best_v[lane] : -INFINITY;
+      bi = lane < kWarps ? sh.best_i[lane] : 0x7fffffff;
+      warp_best(bv, bi);
+      sync_cta();  // before the next round's are written
     }
-    sync_cta();
-    bv = lane < kWarps ? sh.best_v[lane] : -INFINITY;
-    bi = lane < kWarps ? sh.best_i[lane] : 0x7fffffff;
-    warp_best(bv, bi);
-    sync_cta();  // before the next round's are written
     if (t == 0) label_alternative(a.o, row, r, sums, bv, bi);
     pv = bv;
     pi = bi;
