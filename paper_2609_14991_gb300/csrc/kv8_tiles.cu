@@ -13,14 +13,14 @@
 //               (128-byte swizzle; warps 8-11 keys, 12-15 values), once for both row
 //               tiles and all heads of a group;
 //   warp 16     issues the MMAs.
-// Registers go to where they are used (setmaxnreg): 152 for softmax, 64 for conversion.
+// Registers go to where they are used (setmaxnreg): 136 for softmax, 72 for conversion.
 // Each row tile has two score buffers of 64 keys: the scores of step i + 2 are computed
 // as soon as the values' product of step i has read its probabilities, so the softmax
 // never waits for a product that waits for it.  (With one buffer of 128 keys a tile's
 // softmax, 3700 clocks, and its products, 1600, took turns.)  Keys are the K-major B
 // operand of the scores; the same layout of the values is read as an MN-major B
-// operand, so neither is transposed.  The accumulator is rescaled in TMEM only when a row's maximum
-// grows by more than 2^8.
+// operand, so neither is transposed.  The maximum is looked for, and the accumulator rescaled in
+// TMEM, only in steps whose probabilities outgrow fp16.
 //
 // What bounds it at dim 128, per 128 keys: the MMAs take 2600 clocks (49 for 128 x 64 x
 // 16, whose operands come from shared memory at 128 bytes per clock, 65 for 128 x 128 x
@@ -45,7 +45,7 @@ constexpr int kStepUnits = kStep / kUnit;
 constexpr int kSoftWarps = 8, kConvWarps = 4;  // softmax; conversion of keys, and as many of values
 constexpr int kMmaWarp = kSoftWarps + 2 * kConvWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 4);  // whole warpgroups: three warps of the last have no work
-constexpr int kSoftRegs = 152, kConvRegs = 64, kMmaRegs = 40;
+constexpr int kSoftRegs = 136, kConvRegs = 72, kMmaRegs = 48;
 constexpr int kLaunchRegs = 96;  // per thread, what the launch has to bring
 static_assert(32 * kSoftWarps * kSoftRegs + 64 * kConvWarps * kConvRegs + 128 * kMmaRegs <= kThreads * kLaunchRegs, "register split");
 
@@ -90,23 +90,6 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
       : "memory");
 }
 
-// 64 consecutive columns of this warp's 32 lanes.
-__device__ __forceinline__ void tmem_ld64(uint32_t taddr, uint32_t (&r)[64]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
-      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, %48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
-        "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
-        "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
-        "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
-        "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
-      : "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
@@ -316,11 +299,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           }
           fence_after();
           const uint32_t sb = st + (uint32_t)(buf * kStep);
-          uint32_t raw[kStep];
-          tmem_ld64(sb, raw);
-          float v[kStep];
-#pragma unroll
-          for (int e = 0; e < kStep; ++e) v[e] = __uint_as_float(raw[e]);
           const int u0 = lo * kUnits + i * kStepUnits, w0 = kStepUnits * (i & 1);  // the step's first unit; in its tile
           const int t_lo = units.token(u0), t_hi = units.token(min(u0 + kStepUnits, units.total) - 1) + kUnit - 1;
           const bool whole = u0 + kStepUnits <= units.total && t_hi <= all_to && (t_lo >= all_from || t_hi < a.sinks);
@@ -333,62 +311,88 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
             for (int e = 0; e < kUnit; ++e)
               if (!(e <= lim && (e > from || e < sk))) x[e] = -INFINITY;
           };
-          float c[kStepUnits], lc[kStepUnits], top = -INFINITY;
-#pragma unroll
-          for (int u = 0; u < kStepUnits; ++u) {
-            c[u] = rc * __shfl_sync(0xffffffffu, ua, w0 + u);
-            lc[u] = __shfl_sync(0xffffffffu, ul, w0 + u);
-            if (!whole) mask(v + kUnit * u, u);
-            float x = v[kUnit * u];
-#pragma unroll
-            for (int e = 1; e < kUnit; ++e) x = fmaxf(x, v[kUnit * u + e]);
-            if (x > -INFINITY) top = fmaxf(top, fmaf(x, c[u], lc[u]));  // c >= 0: the largest product has the largest score
-          }
-          if (__any_sync(0xffffffffu, top > m + 8.f)) {
-            const float x = fmaxf(m, top);
-            const float w = x == m ? 1.f : ex2_approx(m - x);
-            m = x;
-            l *= w;
-            if (i > 0) {  // the accumulator, once the last step's values are in it (those before are: this step's scores came after them)
-              if (!__all_sync(0xffffffffu, mbar_wait(o_done + tile, (uint32_t)(at - 1) & 1u))) {
-                dead = true;
-                break;
-              }
-              fence_after();
+          // Probabilities relative to the maximum so far, without looking for this step's:
+          // one that a score has outgrown shows in the sum, and the step is taken again from
+          // its scores, which the probabilities have not replaced yet.  (Sums up to 2^15:
+          // no probability then reaches fp16's largest.)
+          uint32_t y[kStep / 2];
+          float more;
+          bool look = i == 0;
 #pragma unroll 1
-              for (int ch = 0; ch < DIM / 16; ++ch) {
-                float y[16];
-                tmem_ld16(ot + 16 * ch, y);
-                uint32_t z[16];
+          while (true) {
+            if (look) {
+              float top = -INFINITY;
+#pragma unroll 1
+              for (int h = 0; h < 2; ++h) {
+                float v[32];
+                tmem_ld32(sb + 32 * h, v);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(y[e] * w);
-                tmem_st16(ot + 16 * ch, z);
+                for (int u = 0; u < 2; ++u) {
+                  const float c = rc * __shfl_sync(0xffffffffu, ua, w0 + 2 * h + u), lc = __shfl_sync(0xffffffffu, ul, w0 + 2 * h + u);
+                  if (!whole) mask(v + kUnit * u, 2 * h + u);
+                  float x = v[kUnit * u];
+#pragma unroll
+                  for (int e = 1; e < kUnit; ++e) x = fmaxf(x, v[kUnit * u + e]);
+                  if (x > -INFINITY) top = fmaxf(top, fmaf(x, c, lc));  // c >= 0: the largest product has the largest score
+                }
+              }
+              const float x = fmaxf(m, top);
+              const float w = x == m ? 1.f : ex2_approx(m - x);
+              m = x;
+              l *= w;
+              if (i > 0) {  // the accumulator, once the last step's values are in it (those before are: this step's scores came after them)
+                if (!__all_sync(0xffffffffu, mbar_wait(o_done + tile, (uint32_t)(at - 1) & 1u))) {
+                  dead = true;
+                  break;
+                }
+                fence_after();
+#pragma unroll 1
+                for (int ch = 0; ch < DIM / 16; ++ch) {
+                  float o[16];
+                  tmem_ld16(ot + 16 * ch, o);
+                  uint32_t z[16];
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * w);
+                  tmem_st16(ot + 16 * ch, z);
+                }
               }
             }
-          }
-          const float ref = m == -INFINITY ? 0.f : m - 7.f;
+            const float ref = m == -INFINITY ? 0.f : m - 7.f;
+            more = 0.f;
+            float whole_sum = 0.f;
 #pragma unroll
-          for (int u = 0; u < kStepUnits; ++u) {
-            float* x = v + kUnit * u;
-            const float lr = lc[u] - ref, ic = __shfl_sync(0xffffffffu, ui, w0 + u);
-            const uint64_t c2 = pair_of(c[u], c[u]), l2 = pair_of(lr, lr);
+            for (int h = 0; h < 2; ++h) {
+              float v[32];
+              tmem_ld32(sb + 32 * h, v);
 #pragma unroll
-            for (int e = 0; e < kUnit; e += 2) unpair(fma2(pair_of(x[e], x[e + 1]), c2, l2), x[e], x[e + 1]);
-            if (!whole) mask(x, u);
-            uint32_t y[kUnit / 2];
-            uint64_t sum = 0;
+              for (int u = 2 * h; u < 2 * h + 2; ++u) {
+                float* x = v + kUnit * (u & 1);
+                const float c = rc * __shfl_sync(0xffffffffu, ua, w0 + u), lr = __shfl_sync(0xffffffffu, ul, w0 + u) - ref, ic = __shfl_sync(0xffffffffu, ui, w0 + u);
+                const uint64_t c2 = pair_of(c, c), l2 = pair_of(lr, lr);
 #pragma unroll
-            for (int e = 0; e < kUnit; e += 2) {
-              const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
-              sum = add2(sum, pair_of(p0, p1));
-              y[e / 2] = narrow2<false>(p0, p1);
+                for (int e = 0; e < kUnit; e += 2) unpair(fma2(pair_of(x[e], x[e + 1]), c2, l2), x[e], x[e + 1]);
+                if (!whole) mask(x, u);
+                uint64_t sum = 0;
+#pragma unroll
+                for (int e = 0; e < kUnit; e += 2) {
+                  const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
+                  sum = add2(sum, pair_of(p0, p1));
+                  y[8 * u + e / 2] = narrow2<false>(p0, p1);
+                }
+                float s0, s1;
+                unpair(sum, s0, s1);
+                s0 += s1;
+                whole_sum += s0;
+                if (s0 != 0.f) more = fmaf(s0, ic, more);  // a unit that the row does not see may have a NaN scale
+              }
             }
-            float s0, s1;
-            unpair(sum, s0, s1);
-            s0 += s1;
-            if (s0 != 0.f) l = fmaf(s0, ic, l);  // a unit that the row does not see may have a NaN scale
-            tmem_st8(sb + 8 * u, y);
+            if (look || !__any_sync(0xffffffffu, whole_sum > 32768.f)) break;
+            look = true;
           }
+          if (dead) break;
+          l += more;
+#pragma unroll
+          for (int u = 0; u < kStepUnits; ++u) tmem_st8(sb + 8 * u, y + 8 * u);
           tmem_st_wait();
           fence_before();
           __syncwarp();
