@@ -13,7 +13,7 @@
 //               (128-byte swizzle; warps 8-11 keys, 12-15 values), once for both row
 //               tiles and all heads of a group;
 //   warp 16     issues the MMAs.
-// Registers go to where they are used (setmaxnreg): 136 for softmax, 72 for conversion.
+// Registers go to where they are used (setmaxnreg): 144 for softmax, 72 for conversion.
 // Each row tile has two score buffers of 64 keys: the scores of step i + 2 are computed
 // as soon as the values' product of step i has read its probabilities, so the softmax
 // never waits for a product that waits for it.  (With one buffer of 128 keys a tile's
@@ -45,7 +45,7 @@ constexpr int kStepUnits = kStep / kUnit;
 constexpr int kSoftWarps = 8, kConvWarps = 4;  // softmax; conversion of keys, and as many of values
 constexpr int kMmaWarp = kSoftWarps + 2 * kConvWarps;
 constexpr int kThreads = 32 * (kMmaWarp + 4);  // whole warpgroups: three warps of the last have no work
-constexpr int kSoftRegs = 136, kConvRegs = 72, kMmaRegs = 48;
+constexpr int kSoftRegs = 144, kConvRegs = 72, kMmaRegs = 48;
 constexpr int kLaunchRegs = 96;  // per thread, what the launch has to bring
 static_assert(32 * kSoftWarps * kSoftRegs + 64 * kConvWarps * kConvRegs + 128 * kMmaRegs <= kThreads * kLaunchRegs, "register split");
 
@@ -90,6 +90,25 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
       : "memory");
 }
 
+// 32 columns, on their way until tmem_ld_wait (which waits for all of the thread's loads).
+__device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+      : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+        "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+        "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+        "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               :
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
@@ -292,14 +311,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
             fetch(id1);
             id1 = block_of((i >> 1) + 2);
           }
-          const int at = at0 + i, buf = at & 1;
+          const int at = at0 + i, buf = at & 1, w0 = kStepUnits * (i & 1);  // the step's first unit in its tile
+          float c[kStepUnits], lc[kStepUnits], ic[kStepUnits];
+#pragma unroll
+          for (int u = 0; u < kStepUnits; ++u) {
+            c[u] = rc * __shfl_sync(0xffffffffu, ua, w0 + u);
+            lc[u] = __shfl_sync(0xffffffffu, ul, w0 + u);
+            ic[u] = __shfl_sync(0xffffffffu, ui, w0 + u);
+          }
           if (!__all_sync(0xffffffffu, mbar_wait(s_full + 2 * tile + buf, (uint32_t)(at >> 1) & 1u))) {
             dead = true;
             break;
           }
           fence_after();
           const uint32_t sb = st + (uint32_t)(buf * kStep);
-          const int u0 = lo * kUnits + i * kStepUnits, w0 = kStepUnits * (i & 1);  // the step's first unit; in its tile
+          const int u0 = lo * kUnits + i * kStepUnits;  // the step's first unit
           const int t_lo = units.token(u0), t_hi = units.token(min(u0 + kStepUnits, units.total) - 1) + kUnit - 1;
           const bool whole = u0 + kStepUnits <= units.total && t_hi <= all_to && (t_lo >= all_from || t_hi < a.sinks);
           // a unit's products, masked where a row does not see all of the step
@@ -322,18 +348,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           while (true) {
             if (look) {
               float top = -INFINITY;
-#pragma unroll 1
+#pragma unroll
               for (int h = 0; h < 2; ++h) {
                 float v[32];
                 tmem_ld32(sb + 32 * h, v);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                  const float c = rc * __shfl_sync(0xffffffffu, ua, w0 + 2 * h + u), lc = __shfl_sync(0xffffffffu, ul, w0 + 2 * h + u);
                   if (!whole) mask(v + kUnit * u, 2 * h + u);
                   float x = v[kUnit * u];
 #pragma unroll
                   for (int e = 1; e < kUnit; ++e) x = fmaxf(x, v[kUnit * u + e]);
-                  if (x > -INFINITY) top = fmaxf(top, fmaf(x, c, lc));  // c >= 0: the largest product has the largest score
+                  if (x > -INFINITY) top = fmaxf(top, fmaf(x, c[2 * h + u], lc[2 * h + u]));  // c >= 0: the largest product has the largest score
                 }
               }
               const float x = fmaxf(m, top);
@@ -360,17 +385,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
             const float ref = m == -INFINITY ? 0.f : m - 7.f;
             more = 0.f;
             float whole_sum = 0.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              float v[32];
-              tmem_ld32(sb + 32 * h, v);
+            const auto half = [&](const uint32_t (&raw)[32], int h) {
 #pragma unroll
               for (int u = 2 * h; u < 2 * h + 2; ++u) {
-                float* x = v + kUnit * (u & 1);
-                const float c = rc * __shfl_sync(0xffffffffu, ua, w0 + u), lr = __shfl_sync(0xffffffffu, ul, w0 + u) - ref, ic = __shfl_sync(0xffffffffu, ui, w0 + u);
-                const uint64_t c2 = pair_of(c, c), l2 = pair_of(lr, lr);
+                float x[kUnit];
+                const float lr = lc[u] - ref;
+                const uint64_t c2 = pair_of(c[u], c[u]), l2 = pair_of(lr, lr);
 #pragma unroll
-                for (int e = 0; e < kUnit; e += 2) unpair(fma2(pair_of(x[e], x[e + 1]), c2, l2), x[e], x[e + 1]);
+                for (int e = 0; e < kUnit; e += 2)
+                  unpair(fma2(pair_of(__uint_as_float(raw[kUnit * (u & 1) + e]), __uint_as_float(raw[kUnit * (u & 1) + e + 1])), c2, l2), x[e], x[e + 1]);
                 if (!whole) mask(x, u);
                 uint64_t sum = 0;
 #pragma unroll
@@ -383,9 +406,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
                 unpair(sum, s0, s1);
                 s0 += s1;
                 whole_sum += s0;
-                if (s0 != 0.f) more = fmaf(s0, ic, more);  // a unit that the row does not see may have a NaN scale
+                if (s0 != 0.f) more = fmaf(s0, ic[u], more);  // a unit that the row does not see may have a NaN scale
               }
-            }
+            };
+            uint32_t r0[32], r1[32];
+            tmem_ld32_begin(sb, r0);
+            tmem_ld_wait(r0);
+            half(r0, 0);
+            tmem_ld32_begin(sb + 32, r1);
+            tmem_ld_wait(r1);
+            half(r1, 1);
             if (look || !__any_sync(0xffffffffu, whole_sum > 32768.f)) break;
             look = true;
           }
