@@ -109,10 +109,19 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
                :
                : "memory");
 }
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+      "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+      "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+      "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
@@ -282,6 +291,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         const int wr = row0 + (threadIdx.x & ~31);
         const int all_to = before + min(wr, rows - 1) / a.group;
         const int all_from = a.window > 0 ? before + min(wr + 31, rows - 1) / a.group - a.window + 1 : 0;
+        // ... and the units of the list, past the sinks, that hold nothing else
+        const int seen_from = max(units.sink, (max(all_from, 0) + kUnit - 1) / kUnit - units.from + units.sink);
+        const int seen_to = min(units.total, (all_to + 1) / kUnit - units.from + units.sink);
         float m = -INFINITY, l = 0.f;
         const float nan = __uint_as_float(0x7fc00000u);
         // lane u < 8: the scales of the next key tile's unit u, and the block of the one after's: no
@@ -306,8 +318,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           if ((i & 1) == 0) {  // a key tile's scales
             const float uc = nc == 0.f ? 0x1p-80f : nc;
             ua = na;
-            ul = log2f(uc);
-            ui = 1.f / uc;
+            ul = lg2_approx(uc);  // 2^-22 of the value: 2^-17 at a scale of 2^-32, an fp16 weight rounds by 2^-11
+            ui = rcp_approx(uc);
             fetch(id1);
             id1 = block_of((i >> 1) + 2);
           }
@@ -326,8 +338,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           fence_after();
           const uint32_t sb = st + (uint32_t)(buf * kStep);
           const int u0 = lo * kUnits + i * kStepUnits;  // the step's first unit
-          const int t_lo = units.token(u0), t_hi = units.token(min(u0 + kStepUnits, units.total) - 1) + kUnit - 1;
-          const bool whole = u0 + kStepUnits <= units.total && t_hi <= all_to && (t_lo >= all_from || t_hi < a.sinks);
+          const bool whole = u0 >= seen_from && u0 + kStepUnits <= seen_to;
           // a unit's products, masked where a row does not see all of the step
           const auto mask = [&](float* x, int u) {
             const int t0 = units.token(u0 + u);
@@ -421,8 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           }
           if (dead) break;
           l += more;
-#pragma unroll
-          for (int u = 0; u < kStepUnits; ++u) tmem_st8(sb + 8 * u, y + 8 * u);
+          tmem_st32(sb, y);
           tmem_st_wait();
           fence_before();
           __syncwarp();
