@@ -17,7 +17,7 @@
 //   out = sum_j 2^(s_j - m) v_j  /  sum_j 2^(s_j - m) / c_b,
 // so a value's scale is an addend of the exponent and the integers go into the
 // products as they are (exact in fp16, as is every query within 2^28 of its
-// row's largest).  Probabilities are rounded to fp16 (half a step 2^-12), as
+// row's largest).  Probabilities are rounded to fp16 (half a step 2^-11), as
 // multiples of 2^(m - 7): down to 2^-31 of the largest they are not flushed.  The maximum
 // follows only when a score passes it by more than 2^8, which fp16 still holds:
 // most tiles need no exchange between lanes.
@@ -46,7 +46,7 @@ constexpr int kTile = kKv8Unit;  // keys per tile
 template <int DIM, int MW>
 struct RowsShape {
   static constexpr int kKeyGroups = 4 / MW;
-  static constexpr int kStages = MW == 1 ? 4 : 8;
+  static constexpr int kStages = 8;
   static constexpr int kStageBytes = 2 * kTile * DIM;
   static constexpr int kRing = kKeyGroups * kStages * kStageBytes;
   static constexpr int kOutStride = DIM + 4;

@@ -123,10 +123,11 @@ class Batch:
     def check_attend(self, counts, heads, window=0, sinks=0, scale=None, q=None, **kw):
         """Attention of counts[i] last tokens of each sequence against fp64.
 
-        Bounds: each probability is rounded to fp16 (half a step is 2^-12 of it)
-        and carries the fp32 error of its exponent (below 2^-15 for scores below
-        2^6), so a result is off by at most (2^-12 + 2^-14) sum p |v|, twice that
-        with the sum of the probabilities; then half a step of the result's type."""
+        Bounds: each probability is rounded to fp16 (half a step is 2^-11 of it)
+        for the products, and not for the sum that divides them; in both it carries
+        the error of its exponent and of 2^x, 2^-14 together for scores below 2^6.
+        So a result is off by at most (2^-11 + 2 * 2^-14) sum p |v|; then half a
+        step of the result's type."""
         q = self.rows(max(1, sum(counts)), heads) if q is None else q
         scale = self.dim ** -0.5 if scale is None else scale
         out = self.cache.attend(q, **self.args(counts), window=window, sinks=sinks, scale=scale, **kw)

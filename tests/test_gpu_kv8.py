@@ -229,6 +229,45 @@ def test_long_contexts_over_several_ctas(dim):
     b.check_attend([3, 0, 2], 2, window=3000, sinks=4)
 
 
+@pytest.mark.parametrize("heads,count", [(1, 1), (12, 1), (1, 20), (5, 11)])
+def test_long_contexts_of_other_row_counts(heads, count):
+    """One and two column tiles of eight rows, row tiles of 32 and 64, each over several CTAs."""
+    b = Batch(tsd, [3000 + count, 700], 1, 16, 64, seed=heads)
+    b.append([3000, 700 - count])
+    b.append([count, count])
+    for kw in (dict(), dict(max_new=count, max_len=3000 + count)):
+        b.check_attend([count, count], heads, **kw)
+
+
+def test_many_short_contexts():
+    """More sequences and key heads than the GPU runs CTAs at once."""
+    lens = [1 + (37 * i) % 90 for i in range(260)]
+    b = Batch(tsd, lens, 2, 16, 64, seed=4)
+    b.append(lens)
+    for heads in (2, 4, 20):
+        b.check_attend([1] * len(lens), heads, max_len=90)
+
+
+@pytest.mark.parametrize("counts,heads", [([1, 1], 2), ([9, 20], 4), ([50, 30], 1), ([300, 140], 2)])
+def test_scores_that_grow(counts, heads):
+    """Scores (below 44) that rise along the keys, by jumps inside a tile too, and fall again: the
+    running maximum moves many times.  Negative scales turn rises into falls."""
+    past = [400, 90]
+    b = Batch(tsd, [p + c for p, c in zip(past, counts)], 1, 16, 64, seed=heads)
+    n = sum(past) + sum(counts)
+    t = torch.arange(n) % (n // 3)
+    along = 0.25 * (t / 40 + 4 * (t % 97 > 50) + 0.3 * torch.randn(n, generator=b.g)).clamp(-12, 12)
+    k = (along[:, None, None] * torch.ones(64)).to(b.dtype).cuda()
+    b.append(past, k=k[:sum(past)])
+    b.append(counts, k=k[sum(past):])
+    q = (1 + 0.2 * b.rows(sum(counts), heads)).to(b.dtype)
+    top = 0.125 * float(q.double().sum(2).abs().max()) * float(k.abs().max())
+    assert top < 44
+    for scale in (0.125, -0.125):
+        b.check_attend(counts, heads, q=q, scale=scale)
+    b.check_attend(counts, heads, q=q, scale=0.0)
+
+
 def test_values_of_very_different_scales():
     """Blocks of values between 2^-20 and 2^20, the small ones with the larger weights too, and blocks of zeros."""
     for seed in range(3):
