@@ -42,7 +42,7 @@
 #include <algorithm>
 
 #include "encoder.h"
-#include "tc_common.cuh"
+#include "tc_pair.cuh"
 
 namespace tsd {
 

@@ -3,7 +3,6 @@
 
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <cstdint>
 #include <string>
 #include <vector>
@@ -40,21 +39,6 @@ tsd_status cuda_fail(cudaError_t e, const char* what);
     cudaError_t _e = (call);                                 \
     if (_e != cudaSuccess) return ::tsd::cuda_fail(_e, #call); \
   } while (0)
-
-// Lets a kernel take that much dynamic shared memory; asked of the runtime once per device.
-template <auto KERNEL>
-cudaError_t smem_opt_in(int bytes) {
-  static std::atomic<uint64_t> done{0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || (dev < 64 && (done.load() >> dev & 1))) return e;
-  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && dev < 64) done.fetch_or(uint64_t(1) << dev);
-  return e;
-}
-
-// The current device's SMs.
-cudaError_t device_sms(int* sms);
 
 // True if the test hook (tsd_debug_fail_alloc) makes this allocation fail.
 bool alloc_hook_fires();

@@ -30,7 +30,8 @@
 
 #include "internal.h"
 #include "label_scores.h"
-#include "tc_common.cuh"
+#include "launch.h"
+#include "tc_pair.cuh"
 
 namespace tsd {
 
@@ -840,8 +841,8 @@ extern "C" tsd_status tsd_joint_label_scores(int32_t n, int32_t H, int32_t C, co
   if (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16)
     return fail(TSD_EINVAL, "%s: workspace of %lld bytes, %lld needed (16-byte aligned)", who, (long long)workspace_bytes, (long long)p.bytes);
   CUtensorMap tmA, tmB;
-  if (!make_map(&tmA, A_bf16, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, n, kBK, kBM, CU_TENSOR_MAP_SWIZZLE_128B, a_stride) ||
-      !make_map(&tmB, Wt_bf16, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, H, C, kBK, p.pair ? p.bn / 2 : p.bn, CU_TENSOR_MAP_SWIZZLE_128B, w_stride))
+  if (!make_strided_map(&tmA, A_bf16, H, n, a_stride, kBK, kBM) ||
+      !make_strided_map(&tmB, Wt_bf16, H, C, w_stride, kBK, p.pair ? p.bn / 2 : p.bn))
     return fail(TSD_ECUDA, "%s: cuTensorMapEncodeTiled failed", who);
   JointScoreArgs a{};
   a.o = {m, k, labels, logp, entropy, alt_labels, alt_logp, 1.f / temperature};

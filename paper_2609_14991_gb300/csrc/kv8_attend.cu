@@ -1,5 +1,6 @@
 // Attention over the 8-bit paged cache: the entry points (tsd.h: tsd_kv8_attend).
 #include "kv8_attend.h"
+#include "launch.h"
 
 using namespace tsd;
 

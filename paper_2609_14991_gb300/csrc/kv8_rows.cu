@@ -33,6 +33,7 @@
 #include <algorithm>
 
 #include "kv8_attend.h"
+#include "launch.h"
 #include "tc_common.cuh"
 
 namespace tsd {

@@ -29,6 +29,7 @@
 #include <climits>
 
 #include "kv8_attend.h"
+#include "launch.h"
 #include "tc_common.cuh"
 
 namespace tsd {

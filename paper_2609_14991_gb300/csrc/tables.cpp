@@ -14,6 +14,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "internal.h"
+#include "launch.h"
 
 namespace tsd {
 
