@@ -45,7 +45,8 @@ constexpr int kStep = 64;             // keys per step
 constexpr int kStepUnits = kStep / kUnit;
 constexpr int kSoftWarps = 8, kConvWarps = 4;  // softmax; conversion of keys, and as many of values
 constexpr int kMmaWarp = kSoftWarps + 2 * kConvWarps;
-constexpr int kThreads = 32 * (kMmaWarp + 4);  // whole warpgroups: three warps of the last have no work
+constexpr int kScaleWarp = kMmaWarp + 1;
+constexpr int kThreads = 32 * (kMmaWarp + 4);  // whole warpgroups: two warps of the last have no work
 constexpr int kSoftRegs = 144, kConvRegs = 72, kMmaRegs = 48;
 constexpr int kLaunchRegs = 96;  // per thread, what the launch has to bring
 static_assert(32 * kSoftWarps * kSoftRegs + 64 * kConvWarps * kConvRegs + 128 * kMmaRegs <= kThreads * kLaunchRegs, "register split");
@@ -58,7 +59,8 @@ struct TilesShape {
   static constexpr int kK = 2 * kTileBytes;             // two stages
   static constexpr int kV = 4 * kTileBytes;             // two stages
   static constexpr int kBar = 6 * kTileBytes;
-  static constexpr int kSmem = kBar + 256 + 1024;
+  static constexpr int kScales = kBar + 256;  // [stage][3][kUnits]: a key tile's key scales, log2 and reciprocal of its value scales
+  static constexpr int kSmem = kScales + 2 * 3 * kUnits * 4 + 1024;
   static constexpr int kO = 256;  // TMEM: the row tiles' two score buffers at 0, 64 and 128, 192; accumulators from here
 };
 
@@ -91,24 +93,20 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
       : "memory");
 }
 
-// 32 columns, on their way until tmem_ld_wait (which waits for all of the thread's loads).
-__device__ __forceinline__ void tmem_ld32_begin(uint32_t taddr, uint32_t (&r)[32]) {
+// 16 columns, on their way until tmem_ld16_wait (which waits for all of the thread's loads).
+__device__ __forceinline__ void tmem_ld16_begin(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr));
 }
-__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16_wait(uint32_t (&r)[16]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;"
       : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-        "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
-        "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
-        "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               :
-               : "memory");
+        "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+      :
+      : "memory");
 }
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
   asm volatile(
@@ -146,8 +144,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
   uint64_t *o_done = bars + 16, *o_full = bars + 18;  // [2] row tiles: a step's values' product, the last one's
   uint64_t *q_full = bars + 20, *drain = bars + 21;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 22);
-  volatile int* lost = reinterpret_cast<volatile int*>(bars + 23);  // a wait ran out
 
+  float* scales = reinterpret_cast<float*>(smem + S::kScales);
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.y);
   const int head = blockIdx.x % a.c.kv_heads, split = blockIdx.x / a.c.kv_heads, splits = gridDim.x / a.c.kv_heads;
@@ -155,27 +153,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
   const int mts = (rows + 255) / 256;
   if ((int)blockIdx.z >= mts) return;
 
-  const auto say_nan = [&](int row0, int threads) {
-    for (int e = threadIdx.x; e < 256 * (DIM / 8); e += threads) {
-      const int r = row0 + e / (DIM / 8), col = 8 * (e % (DIM / 8));
-      if (r >= rows) break;
-      const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
-      const uint32_t nan2 = BF16 ? 0x7fc07fc0u : 0x7e007e00u;
-      if (splits == 1)
-        *reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + col) = make_uint4(nan2, nan2, nan2, nan2);
-      else if (col == 0)
-        a.part_ml[((size_t)split * a.b.rows + tok) * a.heads + h] = make_float2(0.f, __uint_as_float(0x7fc00000u));
+  // row r says NaN
+  const auto say_nan = [&](int r) {
+    if (r >= rows) return;
+    const int tok = q.row0 + r / a.group, h = head * a.group + r % a.group;
+    const uint32_t nan2 = BF16 ? 0x7fc07fc0u : 0x7e007e00u;
+    if (splits == 1) {
+      uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head);
+      for (int i = 0; i < DIM / 8; ++i) dst[i] = make_uint4(nan2, nan2, nan2, nan2);
+    } else {
+      a.part_ml[((size_t)split * a.b.rows + tok) * a.heads + h] = make_float2(0.f, __uint_as_float(0x7fc00000u));
     }
   };
   if (!q.ok) {
-    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) say_nan(mt * 256, kThreads);
+    if (threadIdx.x < 256)
+      for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) say_nan(mt * 256 + threadIdx.x);
     return;
   }
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i, kConvWarps);
-      mbar_init(v_full + i, kConvWarps);
+      mbar_init(v_full + i, kConvWarps + 1);
       mbar_init(k_empty + i, 1);
       mbar_init(v_empty + i, 1);
       mbar_init(o_done + i, 1);
@@ -187,7 +186,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     }
     mbar_init(q_full, kSoftWarps);
     mbar_init(drain, 1);
-    *lost = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -218,46 +216,46 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     p.steps = (min(p.units.total, (p.lo + p.n) * kUnits) - p.lo * kUnits + kStepUnits - 1) / kStepUnits;
     return p;
   };
-  // Every role walks the row tiles by itself (each has registers of its own number); between
-  // two of them all meet.  False once a wait has run out anywhere: the rows from
+  // Every role walks the row tiles by itself (each has registers of its own number), so the
+  // next one's keys and values are converted while the softmax ends this one.  A wait
+  // that runs out ends its role; the others' waits on it run out in turn, and the rows from
   // there on say NaN.
-  const auto meet = [&](bool dead) {
-    if (dead) *lost = 1;
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * (kMmaWarp + 1)) : "memory");
-    return *lost == 0;
-  };
-
-  if (warp > kMmaWarp) {
+  if (warp > kScaleWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
     return;
   }
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int tile = warp >> 2;
-    int at0 = 0, done = 0;  // the barriers' positions: steps and row tiles with steps so far
+    int at0 = 0, kt0 = 0, done = 0;  // the barriers' positions: steps, key tiles and row tiles with steps so far
     int mt = blockIdx.z;
+    // (a warp of a row tile that has no rows must not arrive for the next one's queries early)
+    const auto row_tile_end = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftWarps) : "memory"); };
     for (bool fine = true; mt < mts; mt += gridDim.z) {
       const Part pt = part_of(mt);
       const int row0 = pt.row0, lo = pt.lo, n = pt.n, steps = pt.steps;
       const KeyTiles& units = pt.units;
+      const int r = row0 + threadIdx.x;
       if (!fine) {
-        say_nan(row0, 32 * kSoftWarps);
+        say_nan(r);
+        row_tile_end();
         continue;
       }
       bool dead = false;
-      const int r = row0 + threadIdx.x;
       const bool live = r < rows;
       const int tok = min(r, rows - 1) / a.group, pos = before + tok;
       // the row's queries as fp16, scaled by f into [2^14, 2^15)
-      float rc;
-      {
+      float rc = 0.f;
+      if (steps > 0) {
         float top = 0.f;
         bool odd = false;
         const uint16_t* src = a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + min(r, rows - 1) % a.group) * a.q_head;
-#pragma unroll 8
+        uint4 w[DIM / 8];
+#pragma unroll
+        for (int i = 0; i < DIM / 8; ++i) w[i] = live ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
         for (int i = 0; i < DIM / 8; ++i) {
-          const uint4 w = live ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+          const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const float x = fabsf(wide16<BF16>(u[j] & 0xffffu)), y = fabsf(wide16<BF16>(u[j] >> 16));
@@ -272,10 +270,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         // the last row tile's products have read the rows before these: its accumulators were waited for
         const int rr = threadIdx.x & 127;
         unsigned char* dst = smem + S::kQ + tile * S::kTileBytes + rr * 128;
-#pragma unroll 4
+#pragma unroll
         for (int i = 0; i < DIM / 8; ++i) {
-          const uint4 w = live ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
-          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+          const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
           uint32_t y[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = narrow2<false>(wide16<BF16>(u[j] & 0xffffu) * f, wide16<BF16>(u[j] >> 16) * f);
@@ -297,40 +294,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         const int seen_to = min(units.total, (all_to + 1) / kUnit - units.from + units.sink);
         float m = -INFINITY, l = 0.f;
         const float nan = __uint_as_float(0x7fc00000u);
-        // lane u < 8: the scales of the next key tile's unit u, and the block of the one after's: no
-        // load waits for another
-        const auto block_of = [&](int j) {
-          const int u = (lo + j) * kUnits + lane;
-          return lane < kUnits && u < units.total && j < n ? __ldg(table + (units.token(u) >> shift)) : -1;
-        };
-        float na = nan, nc = nan;
-        const auto fetch = [&](int id) {
-          na = nc = nan;
-          if (id >= 0 && id < a.c.n_blocks) {
-            na = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
-            nc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
-          }
-        };
-        fetch(block_of(0));
-        int id1 = block_of(1);
-        float ua = nan, ul = nan, ui = nan;
 #pragma unroll 1
         for (int i = 0; i < steps; ++i) {
-          if ((i & 1) == 0) {  // a key tile's scales
-            const float uc = nc == 0.f ? 0x1p-80f : nc;
-            ua = na;
-            ul = lg2_approx(uc);  // 2^-22 of the value: 2^-17 at a scale of 2^-32, an fp16 weight rounds by 2^-11
-            ui = rcp_approx(uc);
-            fetch(id1);
-            id1 = block_of((i >> 1) + 2);
-          }
-          const int at = at0 + i, buf = at & 1, w0 = kStepUnits * (i & 1);  // the step's first unit in its tile
-          float c[kStepUnits], lc[kStepUnits], ic[kStepUnits];
-#pragma unroll
-          for (int u = 0; u < kStepUnits; ++u) {
-            c[u] = rc * __shfl_sync(0xffffffffu, ua, w0 + u);
-            lc[u] = __shfl_sync(0xffffffffu, ul, w0 + u);
-            ic[u] = __shfl_sync(0xffffffffu, ui, w0 + u);
+          const int at = at0 + i, buf = at & 1, kt = kt0 + (i >> 1);
+          // a key tile's scales, with its values
+          if ((i & 1) == 0 && !__all_sync(0xffffffffu, mbar_wait(v_full + (kt & 1), (uint32_t)(kt >> 1) & 1u))) {
+            dead = true;
+            break;
           }
           if (!__all_sync(0xffffffffu, mbar_wait(s_full + 2 * tile + buf, (uint32_t)(at >> 1) & 1u))) {
             dead = true;
@@ -338,6 +308,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           }
           fence_after();
           const uint32_t sb = st + (uint32_t)(buf * kStep);
+          float c[kStepUnits], lc[kStepUnits], ic[kStepUnits];
+          {
+            const float* from = scales + 3 * kUnits * (kt & 1) + kStepUnits * (i & 1);
+            const float4 x = *reinterpret_cast<const float4*>(from), y = *reinterpret_cast<const float4*>(from + kUnits), z = *reinterpret_cast<const float4*>(from + 2 * kUnits);
+            c[0] = rc * x.x, c[1] = rc * x.y, c[2] = rc * x.z, c[3] = rc * x.w;
+            lc[0] = y.x, lc[1] = y.y, lc[2] = y.z, lc[3] = y.w;
+            ic[0] = z.x, ic[1] = z.y, ic[2] = z.z, ic[3] = z.w;
+          }
           const int u0 = lo * kUnits + i * kStepUnits;  // the step's first unit
           const bool whole = u0 >= seen_from && u0 + kStepUnits <= seen_to;
           // a unit's products, masked where a row does not see all of the step
@@ -397,15 +375,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
             const float ref = m == -INFINITY ? 0.f : m - 7.f;
             more = 0.f;
             float whole_sum = 0.f;
-            const auto half = [&](const uint32_t (&raw)[32], int h) {
-#pragma unroll
-              for (int u = 2 * h; u < 2 * h + 2; ++u) {
+            const auto unit = [&](const uint32_t (&raw)[kUnit], int u) {
                 float x[kUnit];
                 const float lr = lc[u] - ref;
                 const uint64_t c2 = pair_of(c[u], c[u]), l2 = pair_of(lr, lr);
 #pragma unroll
                 for (int e = 0; e < kUnit; e += 2)
-                  unpair(fma2(pair_of(__uint_as_float(raw[kUnit * (u & 1) + e]), __uint_as_float(raw[kUnit * (u & 1) + e + 1])), c2, l2), x[e], x[e + 1]);
+                  unpair(fma2(pair_of(__uint_as_float(raw[e]), __uint_as_float(raw[e + 1])), c2, l2), x[e], x[e + 1]);
                 if (!whole) mask(x, u);
                 uint64_t sum = 0;
 #pragma unroll
@@ -419,15 +395,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
                 s0 += s1;
                 whole_sum += s0;
                 if (s0 != 0.f) more = fmaf(s0, ic[u], more);  // a unit that the row does not see may have a NaN scale
-              }
             };
-            uint32_t r0[32], r1[32];
-            tmem_ld32_begin(sb, r0);
-            tmem_ld_wait(r0);
-            half(r0, 0);
-            tmem_ld32_begin(sb + 32, r1);
-            tmem_ld_wait(r1);
-            half(r1, 1);
+            uint32_t raw[2][kUnit];  // a unit's scores are on their way while the one before is worked on
+            tmem_ld16_begin(sb, raw[0]);
+#pragma unroll
+            for (int u = 0; u < kStepUnits; ++u) {
+              tmem_ld16_wait(raw[u & 1]);
+              if (u + 1 < kStepUnits) tmem_ld16_begin(sb + kUnit * (u + 1), raw[(u + 1) & 1]);
+              unit(raw[u & 1], u);
+            }
             if (look || !__any_sync(0xffffffffu, whole_sum > 32768.f)) break;
             look = true;
           }
@@ -468,9 +444,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         at0 += steps;
         done += steps > 0;
       }
+      kt0 += n;
       fence_before();
-      fine = meet(dead);
+      fine = !__any_sync(0xffffffffu, dead);
+      row_tile_end();
     }
+    asm volatile("bar.arrive 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");
   } else if (warp < kMmaWarp) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kConvRegs));
     int at0 = 0;
@@ -534,14 +513,59 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         next = row_of(j + 2, id);
       }
       at0 += n;
-      if (!meet(dead)) break;
+      if (__any_sync(0xffffffffu, dead)) break;
+    }
+  } else if (warp == kScaleWarp) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
+    int at0 = 0;
+    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
+      const Part pt = part_of(mt);
+      const int lo = pt.lo, n = pt.n;
+      bool dead = false;
+      // lane u < 8: unit u of the tile: its scales, loaded a tile ahead, from the block read two ahead
+      const auto block_of = [&](int j) {
+        const int u = (lo + j) * kUnits + lane;
+        return lane < kUnits && u < pt.units.total && j < n ? __ldg(table + (pt.units.token(u) >> shift)) : -1;
+      };
+      float ka, vc;
+      const auto fetch = [&](int id) {
+        ka = vc = __uint_as_float(0x7fc00000u);
+        if (id >= 0 && id < a.c.n_blocks) {
+          ka = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
+          vc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
+        }
+      };
+      fetch(block_of(0));
+      int id1 = block_of(1);
+#pragma unroll 1
+      for (int j = 0; j < n; ++j) {
+        const int at = at0 + j;
+        if (at >= 2 && !mbar_wait(v_empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
+          dead = true;
+          break;
+        }
+        const float y = vc == 0.f ? 0x1p-80f : vc;
+        float* to = scales + 3 * kUnits * (at & 1) + lane;
+        if (lane < kUnits) {
+          to[0] = ka;
+          to[kUnits] = lg2_approx(y);  // 2^-22 of the value: 2^-17 at a scale of 2^-32, an fp16 weight rounds by 2^-11
+          to[2 * kUnits] = rcp_approx(y);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(v_full + (at & 1));
+        fetch(id1);
+        id1 = block_of(j + 2);
+      }
+      at0 += n;
+      if (__any_sync(0xffffffffu, dead)) break;
     }
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    int at0 = 0, tile_at[2] = {0, 0}, mi = 0;  // key tiles, steps of the row tiles, row tiles
-    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z, ++mi) {
+    int at0 = 0, tile_at[2] = {0, 0}, mi = 0;  // key tiles, steps of the row tiles, row tiles with steps
+    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
       const Part pt = part_of(mt);
       const int steps = pt.steps, tiles = pt.two ? 2 : 1;
+      if (steps == 0) continue;
       bool dead = false;
       if (elect()) {
       bool ok = mbar_wait(q_full, (uint32_t)mi & 1u);
@@ -574,7 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         fence_after();
         return there;
       };
-      if (ok && steps > 0) ok = have(k_full, 0);
+      if (ok) ok = have(k_full, 0);
       for (int i = 0; i < min(2, steps) && ok; ++i)
         for (int t = 0; t < tiles; ++t) scores(t, i);
       for (int i = 0; i < steps && ok; ++i) {
@@ -598,13 +622,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
       }
       }
       __syncwarp();
+      ++mi;
       at0 += pt.n;
       tile_at[0] += steps;
       if (pt.two) tile_at[1] += steps;
-      fence_before();
-      if (!meet(__any_sync(0xffffffffu, dead))) break;
-      fence_after();
+      if (__any_sync(0xffffffffu, dead)) break;
     }
+    asm volatile("bar.sync 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");  // the accumulators have been read
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
