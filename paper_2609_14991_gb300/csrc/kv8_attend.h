@@ -58,6 +58,18 @@ __device__ __forceinline__ KeyTiles key_tiles(int pos0, int pos1, int window, in
   return k;
 }
 
+// Where share i of `parts` even shares of `all` begins.
+__device__ __forceinline__ int share_from(int all, int i, int parts) {
+  const int each = all / parts;
+  return i * each + min(i, all - each * parts);
+}
+
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // The power of two that brings a row's largest magnitude into [2^14, 2^15) (2^126 at
 // most); fine: false for NaN and infinity.
 struct QueryScale {

@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
       const int before = q.len - q.count;
       const int last_row = min(rows, (mt + 1) * 16 * MW) - 1;
       const KeyTiles tiles = key_tiles(before + mt * 16 * MW / a.group, before + last_row / a.group, a.window, a.sinks);
-      const int lo = (int)((int64_t)tiles.total * blockIdx.x / gridDim.x), hi = (int)((int64_t)tiles.total * (blockIdx.x + 1) / gridDim.x);
+      const int lo = share_from(tiles.total, blockIdx.x, gridDim.x), hi = share_from(tiles.total, blockIdx.x + 1, gridDim.x);
       const int n = hi - lo > kg ? (hi - lo - kg + KW - 1) / KW : 0;  // this key group's tiles lo + kg + i KW
       // the queries' fragments
       uint32_t qf[kSteps][4];
@@ -220,8 +220,8 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
           a_b = id >= 0 ? __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float c = id >= 0 ? __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float cs = c == 0.f ? 0x1p-80f : c;  // a scale of 0 stands for values of 0, of their weight all the same
-          lc_b = log2f(cs);
-          ic_b = 1.f / cs;
+          lc_b = lg2_approx(cs);
+          ic_b = rcp_approx(cs);
         }
         if (mw == 0 && i + ST - 1 < n) issue(i + ST - 1);
         const int at = it0 + i, st = at % ST;
@@ -431,7 +431,7 @@ __global__ void __launch_bounds__(32 * W, 12 / W) k_kv8_eight(const __grid_const
       const int before = q.len - q.count;
       const KeyTiles units = key_tiles(before + r0 / a.group, before + (min(rows, r0 + kRows) - 1) / a.group, a.window, a.sinks);
       const int all = (units.total + 1) / 2;
-      const int lo = (int)((int64_t)all * blockIdx.x / gridDim.x), hi = (int)((int64_t)all * (blockIdx.x + 1) / gridDim.x);
+      const int lo = share_from(all, blockIdx.x, gridDim.x), hi = share_from(all, blockIdx.x + 1, gridDim.x);
       const int n = hi - lo > warp ? (hi - lo - warp + W - 1) / W : 0;  // this warp's stages lo + warp + W i
       const int32_t* table = a.b.table + (size_t)q.slot * a.b.table_width;
       // unit u of stage i in the list of units
@@ -522,8 +522,8 @@ __global__ void __launch_bounds__(32 * W, 12 / W) k_kv8_eight(const __grid_const
           a_b = id >= 0 ? __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float c = id >= 0 ? __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float cs = c == 0.f ? 0x1p-80f : c;  // a scale of 0 stands for values of 0, of their weight all the same
-          lc_b = log2f(cs);
-          ic_b = 1.f / cs;
+          lc_b = lg2_approx(cs);
+          ic_b = rcp_approx(cs);
         }
         const int at = it0 + i, st = at % ST;
         if (!__all_sync(0xffffffffu, mbar_wait(full + st, (uint32_t)(at / ST) & 1u))) {

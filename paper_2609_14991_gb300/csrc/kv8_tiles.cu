@@ -117,12 +117,6 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32
       "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
       : "memory");
 }
-__device__ __forceinline__ float lg2_approx(float x) {
-  float y;
-  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
@@ -211,8 +205,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     p.two = rows - p.row0 > 128;
     p.units = key_tiles(before + p.row0 / a.group, before + (min(rows, p.row0 + 256) - 1) / a.group, a.window, a.sinks);
     const int all = (p.units.total + kUnits - 1) / kUnits;
-    p.lo = (int)((int64_t)all * split / splits);
-    p.n = (int)((int64_t)all * (split + 1) / splits) - p.lo;
+    p.lo = share_from(all, split, splits);
+    p.n = share_from(all, split + 1, splits) - p.lo;
     p.steps = (min(p.units.total, (p.lo + p.n) * kUnits) - p.lo * kUnits + kStepUnits - 1) / kStepUnits;
     return p;
   };
@@ -231,6 +225,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     int mt = blockIdx.z;
     // (a warp of a row tile that has no rows must not arrive for the next one's queries early)
     const auto row_tile_end = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftWarps) : "memory"); };
+    // 16 bytes of a row of the warp's queries (later: results), in the 128-byte swizzle
+    constexpr int kRowLanes = DIM / 8, kRowsPer = 32 / kRowLanes;  // lanes per row of 16-bit values, rows of a warp's instruction
+    const auto chunk = [&](int row, int c) {
+      return reinterpret_cast<uint4*>(smem + S::kQ + tile * S::kTileBytes + (c >> 3) * S::kHalf + ((warp & 3) * 32 + row) * 128 + (((c ^ row) & 7) << 4));
+    };
+    const int step_tok = kRowsPer / a.group, step_h = kRowsPer % a.group;
     for (bool fine = true; mt < mts; mt += gridDim.z) {
       const Part pt = part_of(mt);
       const int row0 = pt.row0, lo = pt.lo, n = pt.n, steps = pt.steps;
@@ -243,40 +243,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
       }
       bool dead = false;
       const bool live = r < rows;
+      const int wr = row0 + (threadIdx.x & ~31);  // the warp's first row
       const int tok = min(r, rows - 1) / a.group, pos = before + tok;
+      // the first of this lane's rows where the warp goes through its rows with kRowLanes lanes each, and the next
+      const int own_tok = (wr + lane / kRowLanes) / a.group, own_h = head * a.group + (wr + lane / kRowLanes) % a.group;
+      const auto next_row = [&](int& t, int& h) {
+        t += step_tok;
+        h += step_h;
+        if (h >= (head + 1) * a.group) h -= a.group, ++t;
+      };
       // the row's queries as fp16, scaled by f into [2^14, 2^15)
       float rc = 0.f;
       if (steps > 0) {
-        float top = 0.f;
-        bool odd = false;
-        const uint16_t* src = a.q + (int64_t)(q.row0 + tok) * a.q_row + (int64_t)(head * a.group + min(r, rows - 1) % a.group) * a.q_head;
-        uint4 w[DIM / 8];
+        // the warp's rows one after the other, each with neighbouring lanes, to where their fp16 will stand (the
+        // last row tile's products have read the rows before these: its accumulators were waited for)
+        int ct = own_tok, ch = own_h;
 #pragma unroll
-        for (int i = 0; i < DIM / 8; ++i) w[i] = live ? __ldg(reinterpret_cast<const uint4*>(src) + i) : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kRowLanes; ++i) {
+          const int rw = i * kRowsPer + lane / kRowLanes;
+          const uint16_t* src = a.q + (int64_t)(q.row0 + ct) * a.q_row + (int64_t)ch * a.q_head + 8 * (lane % kRowLanes);
+          if (wr + rw < rows)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(chunk(rw, lane % kRowLanes))), "l"(src) : "memory");
+          else
+            *chunk(rw, lane % kRowLanes) = make_uint4(0, 0, 0, 0);
+          next_row(ct, ch);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        uint32_t top2 = 0;  // magnitudes compare as integers
 #pragma unroll
         for (int i = 0; i < DIM / 8; ++i) {
-          const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x = fabsf(wide16<BF16>(u[j] & 0xffffu)), y = fabsf(wide16<BF16>(u[j] >> 16));
-            top = fmaxf(top, fmaxf(x, y));
-            odd = odd || !(x + y <= INFINITY);
-          }
+          const uint4 w = *chunk(lane, i);
+          top2 = __vmaxu2(__vmaxu2(top2, __vmaxu2(w.x & 0x7fff7fffu, w.y & 0x7fff7fffu)), __vmaxu2(w.z & 0x7fff7fffu, w.w & 0x7fff7fffu));
         }
+        const float top = wide16<BF16>(max(top2 & 0xffffu, top2 >> 16));
         // (a negative scale's sign too, so that a larger product is a larger score)
-        const QueryScale qs = query_scale(odd ? INFINITY : top);
+        const QueryScale qs = query_scale(top);
         rc = qs.fine ? fabsf(a.scale) * kLog2e / qs.f : __uint_as_float(0x7fc00000u);
         const float f = a.scale < 0.f ? -qs.f : qs.f;
-        // the last row tile's products have read the rows before these: its accumulators were waited for
-        const int rr = threadIdx.x & 127;
-        unsigned char* dst = smem + S::kQ + tile * S::kTileBytes + rr * 128;
 #pragma unroll
         for (int i = 0; i < DIM / 8; ++i) {
-          const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+          const uint4 w = *chunk(lane, i);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
           uint32_t y[4];
 #pragma unroll
           for (int j = 0; j < 4; ++j) y[j] = narrow2<false>(wide16<BF16>(u[j] & 0xffffu) * f, wide16<BF16>(u[j] >> 16) * f);
-          *reinterpret_cast<uint4*>(dst + (i >> 3) * S::kHalf + (((i & 7) ^ (rr & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *chunk(lane, i) = make_uint4(y[0], y[1], y[2], y[3]);
         }
         fence_async_smem();
         __syncwarp();
@@ -286,7 +298,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         const uint32_t st = tmem + (uint32_t)(tile * 128) + ((uint32_t)((warp & 3) * 32) << 16);  // scores, then probabilities
         const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
         // positions that every row of the warp sees
-        const int wr = row0 + (threadIdx.x & ~31);
         const int all_to = before + min(wr, rows - 1) / a.group;
         const int all_from = a.window > 0 ? before + min(wr + 31, rows - 1) / a.group - a.window + 1 : 0;
         // ... and the units of the list, past the sinks, that hold nothing else
@@ -418,26 +429,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
         if (steps > 0 && !dead && !mbar_wait(o_full + tile, (uint32_t)done & 1u)) dead = true;
         fence_after();
         if (__any_sync(0xffffffffu, dead)) l = nan;
-        // a row's results: its own contiguous DIM values
+        // results, through shared memory: neighbouring lanes write a row
         const int h = head * a.group + min(r, rows - 1) % a.group;
         const size_t item = ((size_t)split * a.b.rows + q.row0 + tok) * a.heads + h;
         const float inv = 1.f / l;
+        if (splits == 1) {
 #pragma unroll
-        for (int ch = 0; ch < DIM / 32; ++ch) {
-          float v[32];
-          __syncwarp();
-          if (n > 0) tmem_ld32(ot + 32 * ch, v);
-          if (!live) continue;
-          if (splits == 1) {
-            uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)(q.row0 + tok) * a.out_row + (int64_t)h * a.out_head + 32 * ch);
+          for (int ch = 0; ch < DIM / 32; ++ch) {
+            float v[32];
+            tmem_ld32(ot + 32 * ch, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              dst[i] = make_uint4(narrow2<BF16>(v[8 * i] * inv, v[8 * i + 1] * inv), narrow2<BF16>(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
-                                  narrow2<BF16>(v[8 * i + 4] * inv, v[8 * i + 5] * inv), narrow2<BF16>(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
-          } else if (n > 0) {
-            float4* dst = reinterpret_cast<float4*>(a.part + item * DIM + 32 * ch);
+              *chunk(lane, 4 * ch + i) = make_uint4(narrow2<BF16>(v[8 * i] * inv, v[8 * i + 1] * inv), narrow2<BF16>(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
+                                                    narrow2<BF16>(v[8 * i + 4] * inv, v[8 * i + 5] * inv), narrow2<BF16>(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
+          }
+          __syncwarp();
+          int ct = own_tok, ch = own_h;
+#pragma unroll 8
+          for (int i = 0; i < kRowLanes; ++i) {
+            const int rw = i * kRowsPer + lane / kRowLanes;
+            if (wr + rw < rows)
+              *reinterpret_cast<uint4*>(a.out + (int64_t)(q.row0 + ct) * a.out_row + (int64_t)ch * a.out_head + 8 * (lane % kRowLanes)) = *chunk(rw, lane % kRowLanes);
+            next_row(ct, ch);
+          }
+        } else if (steps > 0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dst[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          for (int part = 0; part < 2; ++part) {  // half of the dimensions, fp32
+#pragma unroll
+            for (int ch = 0; ch < DIM / 64; ++ch) {
+              float v[32];
+              tmem_ld32(ot + part * (DIM / 2) + 32 * ch, v);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *chunk(lane, 8 * ch + i) = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            }
+            __syncwarp();
+            int ct = own_tok, ch = own_h;
+#pragma unroll 8
+            for (int i = 0; i < kRowLanes; ++i) {
+              const int rw = i * kRowsPer + lane / kRowLanes;
+              if (wr + rw < rows)
+                *reinterpret_cast<uint4*>(a.part + (((size_t)split * a.b.rows + q.row0 + ct) * a.heads + ch) * DIM + part * (DIM / 2) + 4 * (lane % kRowLanes)) =
+                    *chunk(rw, lane % kRowLanes);
+              next_row(ct, ch);
+            }
+            __syncwarp();
           }
         }
         if (splits > 1 && live) a.part_ml[item] = make_float2(m, l);
