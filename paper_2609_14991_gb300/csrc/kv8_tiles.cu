@@ -165,6 +165,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     return;
   }
 
+  // The softmax warps' queries and results pass through shared memory row by row, kRowLanes
+  // lanes each: 16 bytes of a row of the warp's, in the 128-byte swizzle
+  constexpr int kRowLanes = DIM / 8, kRowsPer = 32 / kRowLanes;
+  const auto chunk = [&](int row, int c) {
+    return reinterpret_cast<uint4*>(smem + S::kQ + (warp >> 2) * S::kTileBytes + (c >> 3) * S::kHalf + ((warp & 3) * 32 + row) * 128 + (((c ^ row) & 7) << 4));
+  };
+  const int step_tok = kRowsPer / a.group, step_h = kRowsPer % a.group;
+  const auto next_row = [&](int& t, int& h) {
+    t += step_tok;
+    h += step_h;
+    if (h >= (head + 1) * a.group) h -= a.group, ++t;
+  };
+  // Starts the copies of the warp's queries to where their fp16 will stand, and gives the token and
+  // head of the lane's first row.  (The products have read the last row tile's: its accumulators were waited for.)
+  const auto load_q = [&](int row0, int& own_tok, int& own_h) {
+    const int wr = row0 + (threadIdx.x & ~31), r = wr + lane / kRowLanes;
+    own_tok = r / a.group;
+    own_h = head * a.group + r - own_tok * a.group;
+    int t = own_tok, h = own_h;
+#pragma unroll
+    for (int i = 0; i < kRowLanes; ++i) {
+      const int rw = i * kRowsPer + lane / kRowLanes;
+      const uint16_t* src = a.q + (int64_t)(q.row0 + t) * a.q_row + (int64_t)h * a.q_head + 8 * (lane % kRowLanes);
+      if (wr + rw < rows)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(chunk(rw, lane % kRowLanes))), "l"(src) : "memory");
+      else
+        *chunk(rw, lane % kRowLanes) = make_uint4(0, 0, 0, 0);
+      next_row(t, h);
+    }
+  };
+  int first_tok = 0, first_h = 0;
+  if (warp < kSoftWarps) load_q((mts - 1 - (int)blockIdx.z) * 256, first_tok, first_h);
+
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i, kConvWarps);
@@ -205,8 +238,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     p.two = rows - p.row0 > 128;
     p.units = key_tiles(before + p.row0 / a.group, before + (min(rows, p.row0 + 256) - 1) / a.group, a.window, a.sinks);
     const int all = (p.units.total + kUnits - 1) / kUnits;
-    p.lo = share_from(all, split, splits);
-    p.n = share_from(all, split + 1, splits) - p.lo;
+    p.lo = splits == 1 ? 0 : share_from(all, split, splits);
+    p.n = (splits == 1 ? all : share_from(all, split + 1, splits)) - p.lo;
     p.steps = (min(p.units.total, (p.lo + p.n) * kUnits) - p.lo * kUnits + kStepUnits - 1) / kStepUnits;
     return p;
   };
@@ -222,15 +255,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int tile = warp >> 2;
     int at0 = 0, kt0 = 0, done = 0;  // the barriers' positions: steps, key tiles and row tiles with steps so far
-    int mt = blockIdx.z;
+    int mt = (int)blockIdx.z;
     // (a warp of a row tile that has no rows must not arrive for the next one's queries early)
     const auto row_tile_end = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftWarps) : "memory"); };
-    // 16 bytes of a row of the warp's queries (later: results), in the 128-byte swizzle
-    constexpr int kRowLanes = DIM / 8, kRowsPer = 32 / kRowLanes;  // lanes per row of 16-bit values, rows of a warp's instruction
-    const auto chunk = [&](int row, int c) {
-      return reinterpret_cast<uint4*>(smem + S::kQ + tile * S::kTileBytes + (c >> 3) * S::kHalf + ((warp & 3) * 32 + row) * 128 + (((c ^ row) & 7) << 4));
-    };
-    const int step_tok = kRowsPer / a.group, step_h = kRowsPer % a.group;
     for (bool fine = true; mt < mts; mt += gridDim.z) {
       const Part pt = part_of(mt);
       const int row0 = pt.row0, lo = pt.lo, n = pt.n, steps = pt.steps;
@@ -245,30 +272,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
       const bool live = r < rows;
       const int wr = row0 + (threadIdx.x & ~31);  // the warp's first row
       const int tok = min(r, rows - 1) / a.group, pos = before + tok;
-      // the first of this lane's rows where the warp goes through its rows with kRowLanes lanes each, and the next
-      const int own_tok = (wr + lane / kRowLanes) / a.group, own_h = head * a.group + (wr + lane / kRowLanes) % a.group;
-      const auto next_row = [&](int& t, int& h) {
-        t += step_tok;
-        h += step_h;
-        if (h >= (head + 1) * a.group) h -= a.group, ++t;
-      };
+      int own_tok, own_h;
+      if (mt == (int)blockIdx.z) own_tok = first_tok, own_h = first_h;
+      else load_q(row0, own_tok, own_h);
       // the row's queries as fp16, scaled by f into [2^14, 2^15)
       float rc = 0.f;
+      asm volatile("cp.async.wait_all;" ::: "memory");  // (before the next row tile's, also where nothing is to be done)
       if (steps > 0) {
-        // the warp's rows one after the other, each with neighbouring lanes, to where their fp16 will stand (the
-        // last row tile's products have read the rows before these: its accumulators were waited for)
-        int ct = own_tok, ch = own_h;
-#pragma unroll
-        for (int i = 0; i < kRowLanes; ++i) {
-          const int rw = i * kRowsPer + lane / kRowLanes;
-          const uint16_t* src = a.q + (int64_t)(q.row0 + ct) * a.q_row + (int64_t)ch * a.q_head + 8 * (lane % kRowLanes);
-          if (wr + rw < rows)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(chunk(rw, lane % kRowLanes))), "l"(src) : "memory");
-          else
-            *chunk(rw, lane % kRowLanes) = make_uint4(0, 0, 0, 0);
-          next_row(ct, ch);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
         uint32_t top2 = 0;  // magnitudes compare as integers
 #pragma unroll
