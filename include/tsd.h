@@ -597,7 +597,7 @@ TSD_API tsd_status tsd_encoder_launches_per_chunk(const tsd_encoder* enc, int32_
 #define TSD_F16 2
 
 /* From logits in memory: n rows of C elements of type dtype, row_stride
- * elements apart (any alignment of the element type).  1 <= n <= 2^30,
+ * elements apart (any alignment of the element type).  1 <= n <= 2^27,
  * 1 <= C <= 262144, row_stride >= C (or n = 1), temperature > 0 and finite.  A
  * row's results are the same bits whatever else is in the call. */
 TSD_API tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits, int32_t dtype, int64_t row_stride,
@@ -605,7 +605,8 @@ TSD_API tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits, in
                                     float* entropy, int32_t* alt_labels, float* alt_logp, void* cuda_stream);
 
 /* From a joint network's input rows: x = A[row] . Wt[label] (bf16 in, fp32
- * accumulate on the tensor cores); the logits are not stored.
+ * accumulate on the tensor cores).  A large call never stores its logits; one of fewer than
+ * two 256 x 256 tiles of them per two SMs keeps them in the workspace, where they stay in L2.
  *   A   bf16 [n][H], rows a_stride elements apart;
  *   Wt  bf16 [C][H] (W_out label-major), rows w_stride elements apart;
  * both 16-byte aligned with strides a multiple of 8.  H a multiple of 64 in

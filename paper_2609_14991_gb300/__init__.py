@@ -701,6 +701,7 @@ def _empty(n, dtype, dev, stream):
 
 
 _sizes = {}  # workspace bytes by call shape
+_MAX32 = 2 ** 31 - 1
 
 
 def _remember(key, bytes_):
@@ -771,8 +772,8 @@ def label_scores(logits, labels=None, k: int = 0, temperature: float = 1.0, out:
     or [n, m], -1 for none."""
     who = "label_scores"
     shape = logits.shape
-    if len(shape) != 2 or shape[0] < 1 or shape[1] < 1:
-        raise ValueError(f"{who}: logits must be [n, C]")
+    if len(shape) != 2 or not (1 <= shape[0] <= 1 << 27 and 1 <= shape[1] <= 262144):
+        raise ValueError(f"{who}: logits must be [n, C] with 1 <= n <= 2^27 and 1 <= C <= 262144")
     code = _dtype_code(logits)
     if code < 0:
         raise ValueError(f"{who}: logits must be float32, bfloat16 or float16")
@@ -788,7 +789,7 @@ def label_scores(logits, labels=None, k: int = 0, temperature: float = 1.0, out:
 
 def joint_label_scores(A, Wt, labels=None, k: int = 0, temperature: float = 1.0, out: Optional[LabelScores] = None,
                        stream=None) -> LabelScores:
-    """The same of the logits A . Wt^T, which stay on the chip
+    """The same of the logits A . Wt^T, which are not kept
     (``tsd_joint_label_scores``): A cuda bf16 [n, H], the joint network's input
     rows; Wt cuda bf16 (or int16 bit patterns) [C, H], W_out label-major.  Row
     strides a multiple of 8, H of 64."""
@@ -796,11 +797,11 @@ def joint_label_scores(A, Wt, labels=None, k: int = 0, temperature: float = 1.0,
 
     who = "joint_label_scores"
     sa, sw = A.shape, Wt.shape
-    if len(sa) != 2 or A.dtype != torch.bfloat16 or sa[0] < 1:
-        raise ValueError(f"{who}: A must be bf16 [n, H]")
+    if len(sa) != 2 or A.dtype != torch.bfloat16 or not 1 <= sa[0] <= 1 << 24:
+        raise ValueError(f"{who}: A must be bf16 [n, H] with 1 <= n <= 2^24")
     n, H = sa
-    if len(sw) != 2 or Wt.dtype not in (torch.bfloat16, torch.int16) or sw[1] != H or sw[0] < 1:
-        raise ValueError(f"{who}: Wt must be bf16 [C, H] with H = {H}")
+    if len(sw) != 2 or Wt.dtype not in (torch.bfloat16, torch.int16) or sw[1] != H or not 1 <= sw[0] <= 262144:
+        raise ValueError(f"{who}: Wt must be bf16 [C, H] with 1 <= C <= 262144 and H = {H}")
     C = sw[0]
     dev = _on_current(who, "A", A)
     if Wt.get_device() != dev:
@@ -891,7 +892,7 @@ class KV8Cache:
         if torch.cuda.current_device() != dev:
             raise ValueError(f"{who}: the cache is on another device than the current one")
         ts, n_slots = table.shape, self.n_slots
-        if table.dtype != i32 or len(ts) != 2 or ts[0] != n_slots or not table.is_contiguous():
+        if table.dtype != i32 or len(ts) != 2 or ts[0] != n_slots or ts[1] > _MAX32 or not table.is_contiguous():
             raise ValueError(f"{who}: table must be contiguous int32 [{n_slots}, width]")
         if lens.dtype != i32 or lens.shape != (n_slots,) or not lens.is_contiguous():
             raise ValueError(f"{who}: lens must be contiguous int32 [{n_slots}]")
@@ -906,10 +907,13 @@ class KV8Cache:
             if slots is not None and starts.shape[0] != n + 1:
                 raise ValueError(f"{who}: starts must have {n + 1} entries")
             n, pt = starts.shape[0] - 1, starts.data_ptr()
+        if n > 65535 or not 0 <= rows <= 1 << 22:
+            raise ValueError(f"{who}: at most 65535 sequences and 2^22 rows")
         if (table.get_device() != dev or lens.get_device() != dev or (ps is not None and slots.get_device() != dev)
                 or (pt is not None and starts.get_device() != dev)):
             raise ValueError(f"{who}: table, lens, slots and starts must be on the cache's device")
-        return KV8BatchC(n, ps, lens.data_ptr(), table.data_ptr(), ts[1], pt, rows, max_new or 0, max_len or 0)
+        return KV8BatchC(n, ps, lens.data_ptr(), table.data_ptr(), ts[1], pt, rows, min(max_new or 0, _MAX32),
+                         min(max_len or 0, _MAX32))
 
     def _rows(self, who, name, t, heads=None):
         """(rows, heads, distance of rows, distance of heads) of [rows, heads, dim]."""
@@ -964,6 +968,7 @@ class KV8Cache:
 
         who = "KV8Cache.attend"
         rows, heads, qr, qh = self._rows(who, "q", q)
+        window, sinks = min(window, _MAX32), min(sinks, _MAX32)  # no sequence is longer
         b = self._batch(who, table, lens, starts, slots, rows, max_new, max_len)
         pb = ctypes.byref(b)
         L = lib()

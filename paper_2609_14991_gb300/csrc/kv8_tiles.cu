@@ -12,8 +12,12 @@
 //   warps 8-15  turn the integers of the next key tile into fp16 in shared memory
 //               (128-byte swizzle; warps 8-11 keys, 12-15 values), once for both row
 //               tiles and all heads of a group;
-//   warp 16     issues the MMAs.
+//   warp 16     issues the MMAs;
+//   warp 17     puts each key tile's scales, and the value scales' logarithms and reciprocals,
+//               into shared memory for the softmax.
 // Registers go to where they are used (setmaxnreg): 144 for softmax, 72 for conversion.
+// Queries come and results leave through shared memory, a row's bytes by neighbouring
+// lanes; a CTA's first queries are on their way while it sets up.
 // Each row tile has two score buffers of 64 keys: the scores of step i + 2 are computed
 // as soon as the values' product of step i has read its probabilities, so the softmax
 // never waits for a product that waits for it.  (With one buffer of 128 keys a tile's
@@ -22,9 +26,13 @@
 // operand, so neither is transposed.  The maximum is looked for, and the accumulator rescaled in
 // TMEM, only in steps whose probabilities outgrow fp16.
 //
-// What bounds it at dim 128, per 128 keys: the MMAs take 2600 clocks (49 for 128 x 64 x
-// 16, whose operands come from shared memory at 128 bytes per clock, 65 for 128 x 128 x
-// 16 with A in TMEM), the hardware's 2^x 2048 (256 x 128 at 16 per clock).
+// Measured (16 query and 4 key heads of 128, bf16): 2000 clocks per step of 64 keys and 256
+// rows, of which the MMAs are 1300 (49 for 128 x 64 x 16, whose operands come from shared
+// memory at 128 bytes per clock, 65 for 128 x 128 x 16 with A in TMEM), and 16000 per CTA
+// before the first step and after the last: 4 ragged sequences of 4000 new tokens past 2000
+// take 248 us (0.50 of the MMAs' floor at the library's rate), one of 2432 past 16000 292
+// us (0.61).  A step's 2000 are the softmax's at dim 64 too (1930): two of its warps per scheduler
+// wait for scores, for TMEM and for one another's 2^x in turn, at half of the issue slots.
 #include <algorithm>
 #include <climits>
 

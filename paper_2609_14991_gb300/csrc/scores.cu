@@ -486,7 +486,7 @@ extern "C" tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits,
   clear_error();
   const char* who = "tsd_label_scores";
   if (!logits) return fail(TSD_EINVAL, "%s: NULL logits", who);
-  if (tsd_status st = label_check(who, n, 1 << 28, C, temperature, m, labels, k, logp, alt_labels, alt_logp)) return st;
+  if (tsd_status st = label_check(who, n, 1 << 27, C, temperature, m, labels, k, logp, alt_labels, alt_logp)) return st;
   if (dtype != TSD_F32 && dtype != TSD_BF16 && dtype != TSD_F16) return fail(TSD_EINVAL, "%s: unknown dtype %d", who, dtype);
   if (n > 1 && row_stride < C) return fail(TSD_EINVAL, "%s: row_stride=%lld below C=%d", who, (long long)row_stride, C);
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == TSD_F32 ? 4 : 2)) return fail(TSD_EINVAL, "%s: logits not aligned to their type", who);

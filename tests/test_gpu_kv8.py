@@ -389,6 +389,20 @@ def test_defaults_one_row_each_in_slot_order():
     assert torch.equal(out, ref[order])
 
 
+def test_sizes_past_32_bits():
+    """Windows and sinks that no sequence reaches are as none, and sizes that 32 bits would cut are refused."""
+    b = Batch(tsd, [90, 200], 1, 16, 64, seed=1)
+    b.append([90, 200])
+    a = b.args([3, 100])
+    q = b.rows(103, 2)
+    want = b.cache.attend(q, **a, max_new=100)
+    for window, sinks in ((2 ** 40, 0), (2 ** 32 + 5, 2 ** 32 + 1), (2 ** 31 - 1, 2 ** 31 - 1)):
+        assert torch.equal(b.cache.attend(q, **a, window=window, sinks=sinks, max_new=100), want)
+    assert torch.equal(b.cache.attend(q, **a, window=7, sinks=2 ** 33, max_new=2 ** 40), want)
+    with pytest.raises(ValueError, match="rows"):
+        b.cache.read(rows=2 ** 32 + 1, **a)
+
+
 def test_same_slot_twice_in_attention():
     b = Batch(tsd, [40, 50], 1, 16, 64, seed=1)
     b.append([40, 50])

@@ -27,7 +27,7 @@ def test_label_scores(L):
     def call(n=2, C=10, x=P, dtype=0, ld=10, t=1.0, m=1, labels=P, k=2, logp=P, ent=P, al=P, ap=P):
         return L.tsd_label_scores(n, C, x, dtype, ld, t, m, labels, k, logp, ent, al, ap, None)
 
-    for kw, word in [(dict(x=None), "logits"), (dict(n=0), "n=0"), (dict(n=-1), "n=-1"), (dict(C=0), "C=0"),
+    for kw, word in [(dict(x=None), "logits"), (dict(n=(1 << 27) + 1), "n="), (dict(n=0), "n=0"), (dict(n=-1), "n=-1"), (dict(C=0), "C=0"),
                      (dict(C=262145, ld=262145), "C=262145"), (dict(dtype=3), "dtype"), (dict(ld=9), "row_stride"),
                      (dict(t=0.0), "temperature"), (dict(t=float("inf")), "temperature"), (dict(t=-1.0), "temperature"),
                      (dict(t=float("nan")), "temperature"), (dict(t=1e-45), "temperature"), (dict(m=9), "m=9"), (dict(m=-1), "m=-1"), (dict(k=9), "k=9"),
@@ -106,6 +106,11 @@ def test_bindings_refuse_host_tensors():
         tsd.joint_label_scores(torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(3, 128, dtype=torch.bfloat16))
     with pytest.raises(ValueError, match="CUDA"):
         tsd.joint_label_scores(torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(3, 64, dtype=torch.bfloat16))
+    for n in (2 ** 27 + 1, 2 ** 32 + 2):  # the second would pass for 2 in 32 bits
+        with pytest.raises(ValueError, match="2\\^27"):
+            tsd.label_scores(torch.zeros(1, 1).expand(n, 1))
+        with pytest.raises(ValueError, match="2\\^24"):
+            tsd.joint_label_scores(torch.zeros(1, 64, dtype=torch.bfloat16).expand(n, 64), torch.zeros(3, 64, dtype=torch.bfloat16))
     k8, sc = torch.zeros(4, 2, 16, 64, dtype=torch.int8), torch.zeros(4, 2)
     tail = torch.zeros(3, 2, 2, 16, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="CUDA"):
