@@ -198,14 +198,13 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
   const float m = value_of(__reduce_max_sync(0xffffffffu, key));
   float bound = -INFINITY;
   if (k > 0) {
+    // the class's number in the lowest bits: no two are equal, and the bound is lower by a few steps at most
+    const int own = (key & -kClasses) | (lane & (kClasses - 1));
     int place = 0;
 #pragma unroll
-    for (int d = 1; d < kClasses; ++d) {
-      const int other = __shfl_xor_sync(0xffffffffu, key, d);
-      // of equal ones the lower lane's comes first: this one has d's highest bit where the partner is lower
-      place += other > key || (other == key && (lane & (1 << (31 - __clz(d)))) != 0) ? 1 : 0;
-    }
-    bound = value_of(__shfl_sync(0xffffffffu, key, __ffs(__ballot_sync(0xffffffffu, place == k - 1)) - 1));
+    for (int d = 1; d < kClasses; ++d) place += __shfl_xor_sync(0xffffffffu, own, d) > own ? 1 : 0;
+    const int kth = __shfl_sync(0xffffffffu, own, __ffs(__ballot_sync(0xffffffffu, place == k - 1)) - 1) & -kClasses;
+    bound = fmaxf(value_of(kth), -INFINITY);  // (a few steps below -inf is a NaN)
   }
 
   // sums: in pairs, a masked logit's exponent held finite (its term is 0 all the same)
@@ -315,31 +314,23 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
     if (k == 0) return;
     // the gathered eights' logits that reach the bound, with their labels
     int found = 0;
-    for (int base = 0; base < count; base += 32) {
-      const int at = base + lane;
-      float y[8];
-      int code = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = -INFINITY;
+    for (int base = 0; base < count; base += 4) {  // eight lanes per eight
+      const int at = base + (lane >> 3), j = lane & 7;
+      float y = -INFINITY;
+      int label = 0;
       if (at < count) {
-        const float4 x0 = sh.eight[at][0], x1 = sh.eight[at][1];
-        y[0] = x0.x, y[1] = x0.y, y[2] = x0.z, y[3] = x0.w, y[4] = x1.x, y[5] = x1.y, y[6] = x1.z, y[7] = x1.w;
-        code = sh.code[at];
+        const int code = sh.code[at], e = code % kEights * 8 + j;
+        y = reinterpret_cast<const float*>(sh.eight[at])[j];
+        label = code < 0 ? ~code : lead + (code / kEights + e / VE * G * CS) * VE + e % VE;
       }
-      const int first = code % kEights * 8, owner = code / kEights;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = y[j] >= bound && y[j] > -INFINITY;
-        const unsigned who = __ballot_sync(0xffffffffu, in);
-        if (in) {
-          const int to = found + __popc(who & ((1u << lane) - 1)), e = first + j;
-          if (to < kCap) {
-            sh.cv[to] = y[j];
-            sh.ci[to] = code < 0 ? ~code : lead + (owner + e / VE * G * CS) * VE + e % VE;
-          }
-        }
-        found += __popc(who);
+      const bool in = y >= bound && y > -INFINITY;
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      const int to = found + __popc(who & ((1u << lane) - 1));
+      if (in && to < kCap) {
+        sh.cv[to] = y;
+        sh.ci[to] = label;
       }
+      found += __popc(who);
     }
     __syncwarp();
     if (found <= 32) {  // a logit's place is the number of better ones
