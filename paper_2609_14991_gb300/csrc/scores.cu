@@ -131,6 +131,10 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
   const T* x = static_cast<const T*>(a.x) + row * a.ld;
   const int C = a.C, k = a.o.k;
 
+  // the given labels, on their way before the logits, and theirs after
+  const int given = rt < a.o.m ? __ldg(a.o.labels + row * a.o.m + rt) : -1;
+  float given_x = __uint_as_float(0x7fc00000u);
+
   // the logits: whole aligned vectors, and the ends one by one
   const int lead = min(C, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T));
   const int nvec = (C - lead) / VE, tail = C - lead - nvec * VE;
@@ -143,6 +147,7 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
       w[i] = make_uint4(0, 0, 0, 0);
       if (j < nvec) w[i] = __ldcs(reinterpret_cast<const uint4*>(x + lead) + j);
     }
+    if (given >= 0 && given < C) given_x = to_float(x[given]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       unpack<T>(w[i], v + i * VE);
@@ -151,13 +156,6 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
         for (int j = 0; j < VE; ++j) v[i * VE + j] = -INFINITY;
       }
     }
-  }
-  // the given labels' logits, on their way early
-  int given = -1;
-  float given_x = __uint_as_float(0x7fc00000u);
-  if (rt < a.o.m) {
-    given = __ldg(a.o.labels + row * a.o.m + rt);
-    if (given >= 0 && given < C) given_x = to_float(x[given]);
   }
   const int xi = rt < lead ? rt : rt < lead + tail ? nvec * VE + rt : -1;
   const float xv = xi >= 0 ? to_float(x[xi]) : -INFINITY;
