@@ -82,7 +82,7 @@ __device__ __forceinline__ QueryScale query_scale(float top) {
   return {__uint_as_float((uint32_t)(fine ? min(127 + 126, 127 + 14 - (ex - 127)) : 127) << 23), fine};
 }
 
-// Few rows per key head (kv8_rows.cu): row tiles of 8, 16 (two or four warps), 32 or 64, the
+// Few rows per key head (kv8_rows.cu): row tiles of 8, 16 (two or four warps) or 32, the
 // keys over `splits` CTAs.
 struct Kv8RowsPlan {
   int rows = 8, warps = 4, mtiles = 1, splits = 1;

@@ -6,8 +6,9 @@
 // mma.sync.m16n8k16 (fp16 in, fp32 out): tcgen05 takes 64 or 128 rows, and these are
 // few.  Up to 16 rows (k_kv8_eight) are one or two column tiles of eight: scores are
 // keys x rows, results dimensions x rows, so few products are spent on rows that are
-// not there.  More (k_kv8_rows) are row tiles of 16.  The keys and values are read once
-// for all rows of a CTA, whose four warps share the work as MW row tiles x 4 / MW key groups; a
+// not there.  More (k_kv8_rows) are two row tiles of 16 per CTA (four, with one key group, took 133
+// us where two take 82: 48 rows, 64 sequences past 2000 tokens).  The keys and values are read once
+// for all rows of a CTA, whose four warps share the work as two row tiles x two key groups; a
 // long context is split over CTAs too (partial results in the workspace, joined by
 // k_kv8_join).
 //
@@ -43,10 +44,11 @@ namespace {
 using namespace tc;
 
 constexpr int kTile = kKv8Unit;  // keys per tile
+constexpr int kRowTiles = 2;     // row tiles of 16 in a CTA of k_kv8_rows
 
-template <int DIM, int MW>
+template <int DIM>
 struct RowsShape {
-  static constexpr int kKeyGroups = 4 / MW;
+  static constexpr int kKeyGroups = 4 / kRowTiles;
   static constexpr int kStages = 8;
   static constexpr int kStageBytes = 2 * kTile * DIM;
   static constexpr int kRing = kKeyGroups * kStages * kStageBytes;
@@ -97,9 +99,9 @@ __device__ __forceinline__ void emit_row(const Kv8Attend& a, const Kv8Seq& q, in
   }
 }
 
-template <bool BF16, int DIM, int MW>
+template <bool BF16, int DIM>
 __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Attend a) {
-  using S = RowsShape<DIM, MW>;
+  using S = RowsShape<DIM>;
   constexpr int KW = S::kKeyGroups, ST = S::kStages;
   constexpr int kSteps = DIM / 16;  // k-steps of the scores' product
   constexpr int kCols = DIM / 8;    // column tiles of the values' product
@@ -109,11 +111,11 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
   float* s_out = reinterpret_cast<float*>(smem);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int mw = warp % MW, kg = warp / MW;
+  const int mw = warp % kRowTiles, kg = warp / kRowTiles;
   const int head = blockIdx.y % a.c.kv_heads, mt0 = blockIdx.y / a.c.kv_heads, mts = gridDim.y / a.c.kv_heads;
   const Kv8Seq q = kv8_seq(a.c, a.b, blockIdx.z);
   const int rows = q.count * a.group;
-  if (mt0 * 16 * MW >= rows) return;
+  if (mt0 * 16 * kRowTiles >= rows) return;
   uint64_t* full = bars + kg * ST;
   uint64_t* empty = bars + KW * ST + kg * ST;
   unsigned char* ring = smem + kg * ST * S::kStageBytes;
@@ -121,7 +123,7 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
   if (threadIdx.x == 0) {
     for (int i = 0; i < KW * ST; ++i) {
       mbar_init(bars + i, 1);
-      mbar_init(bars + KW * ST + i, MW);
+      mbar_init(bars + KW * ST + i, kRowTiles);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -129,8 +131,8 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
   int it0 = 0;  // tiles that this key group has taken so far (the ring's position)
   bool dead = false;  // a wait of this CTA ran out: NaN for its rows from there on
 
-  for (int mt = mt0; mt * 16 * MW < rows; mt += mts) {
-    const int r0 = mt * 16 * MW + mw * 16;  // this warp's first row
+  for (int mt = mt0; mt * 16 * kRowTiles < rows; mt += mts) {
+    const int r0 = mt * 16 * kRowTiles + mw * 16;  // this warp's first row
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     float o[kCols][4];
 #pragma unroll
@@ -138,8 +140,8 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
 
     if (q.ok && !dead) {
       const int before = q.len - q.count;
-      const int last_row = min(rows, (mt + 1) * 16 * MW) - 1;
-      const KeyTiles tiles = key_tiles(before + mt * 16 * MW / a.group, before + last_row / a.group, a.window, a.sinks);
+      const int last_row = min(rows, (mt + 1) * 16 * kRowTiles) - 1;
+      const KeyTiles tiles = key_tiles(before + mt * 16 * kRowTiles / a.group, before + last_row / a.group, a.window, a.sinks);
       const int lo = share_from(tiles.total, blockIdx.x, gridDim.x), hi = share_from(tiles.total, blockIdx.x + 1, gridDim.x);
       const int n = hi - lo > kg ? (hi - lo - kg + KW - 1) / KW : 0;  // this key group's tiles lo + kg + i KW
       // the queries' fragments
@@ -360,10 +362,10 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
     }
     __syncthreads();
     constexpr int kOct = DIM / 8;
-    for (int e = threadIdx.x; e < 16 * MW * kOct; e += 128) {
-      const int row = e / kOct, col = 8 * (e % kOct), r = mt * 16 * MW + row;
+    for (int e = threadIdx.x; e < 16 * kRowTiles * kOct; e += 128) {
+      const int row = e / kOct, col = 8 * (e % kOct), r = mt * 16 * kRowTiles + row;
       if (r >= rows) break;
-      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, 16 * MW, s_out + row * S::kOutStride + col, 16 * MW * S::kOutStride, KW);
+      emit_row<BF16, DIM>(a, q, r, head, col, s_ml + row, 16 * kRowTiles, s_out + row * S::kOutStride + col, 16 * kRowTiles * S::kOutStride, KW);
     }
     fence_async_smem();
     dead = __syncthreads_or(dead);  // then the ring is written again
@@ -718,12 +720,12 @@ __global__ void __launch_bounds__(128) k_kv8_join(const __grid_constant__ Kv8Att
   for (int j = 0; j < kN; j += 2) dst[j / 2] = narrow2<BF16>(acc[j] * inv, acc[j + 1] * inv);
 }
 
-template <bool BF16, int DIM, int MW>
+template <bool BF16, int DIM>
 cudaError_t launch_rows(const Kv8Attend& a, int splits, int mtiles, cudaStream_t s) {
-  using S = RowsShape<DIM, MW>;
-  const cudaError_t e = smem_opt_in<k_kv8_rows<BF16, DIM, MW>>(S::kSmem);
+  using S = RowsShape<DIM>;
+  const cudaError_t e = smem_opt_in<k_kv8_rows<BF16, DIM>>(S::kSmem);
   if (e != cudaSuccess) return e;
-  k_kv8_rows<BF16, DIM, MW><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, S::kSmem, s>>>(a);
+  k_kv8_rows<BF16, DIM><<<dim3(splits, mtiles * a.c.kv_heads, a.b.n), 128, S::kSmem, s>>>(a);
   return cudaGetLastError();
 }
 
@@ -742,8 +744,7 @@ cudaError_t launch_dim(const Kv8Attend& a, const Kv8RowsPlan& p, cudaStream_t s)
     return p.rows == 8 ? launch_eight<BF16, DIM, 1, 2>(a, p.splits, p.mtiles, s) : launch_eight<BF16, DIM, 2, 2>(a, p.splits, p.mtiles, s);
   return p.rows == 8    ? launch_eight<BF16, DIM, 1, 4>(a, p.splits, p.mtiles, s)
          : p.rows == 16 ? launch_eight<BF16, DIM, 2, 4>(a, p.splits, p.mtiles, s)
-         : p.rows == 32 ? launch_rows<BF16, DIM, 2>(a, p.splits, p.mtiles, s)
-                        : launch_rows<BF16, DIM, 4>(a, p.splits, p.mtiles, s);
+                        : launch_rows<BF16, DIM>(a, p.splits, p.mtiles, s);
 }
 
 template <bool BF16, int DIM>
@@ -768,7 +769,7 @@ Kv8RowsPlan kv8_rows_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, i
   const int group = heads / c.kv_heads;
   const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
   const int64_t rows = (int64_t)most * group;
-  p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  p.rows = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   const int64_t mtiles = (rows + p.rows - 1) / p.rows;
   p.mtiles = (int)std::min<int64_t>(mtiles, std::max(1, 65535 / c.kv_heads));
   const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);

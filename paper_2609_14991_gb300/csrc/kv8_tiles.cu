@@ -707,7 +707,10 @@ cudaError_t launch(const Kv8Attend& a, const Kv8TilesPlan& p, cudaStream_t s) {
 bool kv8_tiles_plan(const tsd_kv8& c, const tsd_kv8_batch& b, int heads, int window, int sinks, int sms, Kv8TilesPlan* p) {
   const int group = heads / c.kv_heads;
   const int most = std::max(1, b.max_new ? std::min(b.max_new, b.rows) : (b.rows + b.n - 1) / b.n);
-  if ((int64_t)most * group < 96) return false;
+  // Rows from which a tile of 256 pays although most of it is empty; here and with kv8_rows.cu, dim 128, us: 4 sequences of 4
+  // key heads past 2000 tokens 21 and 20 at 48 rows, 23 and 23 at 64, 21 and 29 at 96; 60 past 300 27 and 22, 27 and 26, 29 and
+  // 37; 64 past 2000 64 and 82, 65 and 105, 64 and 140.  (Dim 64: 60 past 300 22 and 16, 23 and 17, 25 and 24.)
+  if ((int64_t)most * group <= 48) return false;
   p->mtiles = (int)std::min<int64_t>(((int64_t)most * group + 255) / 256, 65535);
   const int64_t cap = std::min<int64_t>(b.max_len ? b.max_len : INT64_MAX, (int64_t)b.table_width * c.block);
   const int64_t keys = window > 0 ? std::min<int64_t>(cap, (int64_t)window + sinks + most) : cap;

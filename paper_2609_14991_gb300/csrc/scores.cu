@@ -424,8 +424,10 @@ cudaError_t launch(const RowsArgs& a, bool after, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, k_label_rows<T, G, CS, E>, a);
 }
 
-// The fewest threads that hold a row in 32 registers each (64 above 8 x 512 x 32; 8 for
-// rows of a few vectors, where 32 would be mostly empty).
+// The fewest threads that hold a row in 32 registers each: with twice as many, half of which
+// idle, 16384 rows of 4097 take 94 us and not 51, of 1500 44 and not 31 (200 rows of 4097, a
+// wave at most: 4.9 and 4.7).  64 registers above 8 x 512 x 32; 8 for rows of at most a warp's worth of
+// them (16384 x 120: 11 us, with 32 15).
 template <typename T>
 cudaError_t launch_type(const RowsArgs& a, bool after, cudaStream_t s) {
   const int vecs = a.C / (16 / (int)sizeof(T)) + 1;  // most whole vectors, with one of the ends
