@@ -494,7 +494,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         else
           asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(map_rank(smem_u32(acce + ab), 0)) : "memory");
       }
-      if (K == kStore) continue;
+      if (K == kStore) {
+        if (!ok && part == 0 && row < a.n) a.logits[(int64_t)row * a.ld + n0] = __uint_as_float(0x7fc00000u);
+        continue;
+      }
       if (t + 1 == last || (t + 1) / a.Nt != mt) {
         // the row tile's last tile here: join the parts of each row and leave the result
         if (!ok) s = __uint_as_float(0x7fc00000u);

@@ -255,10 +255,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
   // next one's keys and values are converted while the softmax ends this one.  A wait
   // that runs out ends its role; the others' waits on it run out in turn, and the rows from
   // there on say NaN.
-  if (warp > kScaleWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    return;
-  }
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int tile = warp >> 2;
@@ -569,122 +565,124 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
       at0 += n;
       if (__any_sync(0xffffffffu, dead)) break;
     }
-  } else if (warp == kScaleWarp) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    int at0 = 0;
-    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
-      const Part pt = part_of(mt);
-      const int lo = pt.lo, n = pt.n;
-      bool dead = false;
-      // lane u < 8: unit u of the tile: its scales, loaded a tile ahead, from the block read two ahead
-      const auto block_of = [&](int j) {
-        const int u = (lo + j) * kUnits + lane;
-        return lane < kUnits && u < pt.units.total && j < n ? __ldg(table + (pt.units.token(u) >> shift)) : -1;
-      };
-      float ka, vc;
-      const auto fetch = [&](int id) {
-        ka = vc = __uint_as_float(0x7fc00000u);
-        if (id >= 0 && id < a.c.n_blocks) {
-          ka = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
-          vc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
-        }
-      };
-      fetch(block_of(0));
-      int id1 = block_of(1);
-#pragma unroll 1
-      for (int j = 0; j < n; ++j) {
-        const int at = at0 + j;
-        if (at >= 2 && !mbar_wait(v_empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
-          dead = true;
-          break;
-        }
-        const float y = vc == 0.f ? 0x1p-80f : vc;
-        float* to = scales + 3 * kUnits * (at & 1) + lane;
-        if (lane < kUnits) {
-          to[0] = ka;
-          to[kUnits] = lg2_approx(y);  // 2^-22 of the value: 2^-17 at a scale of 2^-32, an fp16 weight rounds by 2^-11
-          to[2 * kUnits] = rcp_approx(y);
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(v_full + (at & 1));
-        fetch(id1);
-        id1 = block_of(j + 2);
-      }
-      at0 += n;
-      if (__any_sync(0xffffffffu, dead)) break;
-    }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));
-    int at0 = 0, tile_at[2] = {0, 0}, mi = 0;  // key tiles, steps of the row tiles, row tiles with steps
-    for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
-      const Part pt = part_of(mt);
-      const int steps = pt.steps, tiles = pt.two ? 2 : 1;
-      if (steps == 0) continue;
-      bool dead = false;
-      if (elect()) {
-      bool ok = mbar_wait(q_full, (uint32_t)mi & 1u);
-      const uint32_t sq = smem_u32(smem + S::kQ), sk = smem_u32(smem + S::kK), sv = smem_u32(smem + S::kV);
-      // step i's products; a key tile's stage is free once its last step's of all row tiles are done
-      const auto scores = [&](int t, int i) {
-        const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
-        const uint32_t qa = sq + t * S::kTileBytes, kb = sk + stage * S::kTileBytes + (i & 1) * (kStep * 128);
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));  // one instruction for the whole warpgroup
+    if (warp > kScaleWarp) return;
+    if (warp == kScaleWarp) {
+      int at0 = 0;
+      for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
+        const Part pt = part_of(mt);
+        const int lo = pt.lo, n = pt.n;
+        bool dead = false;
+        // lane u < 8: unit u of the tile: its scales, loaded a tile ahead, from the block read two ahead
+        const auto block_of = [&](int j) {
+          const int u = (lo + j) * kUnits + lane;
+          return lane < kUnits && u < pt.units.total && j < n ? __ldg(table + (pt.units.token(u) >> shift)) : -1;
+        };
+        float ka, vc;
+        const auto fetch = [&](int id) {
+          ka = vc = __uint_as_float(0x7fc00000u);
+          if (id >= 0 && id < a.c.n_blocks) {
+            ka = __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head);
+            vc = __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head);
+          }
+        };
+        fetch(block_of(0));
+        int id1 = block_of(1);
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) {
+          const int at = at0 + j;
+          if (at >= 2 && !mbar_wait(v_empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
+            dead = true;
+            break;
+          }
+          const float y = vc == 0.f ? 0x1p-80f : vc;
+          float* to = scales + 3 * kUnits * (at & 1) + lane;
+          if (lane < kUnits) {
+            to[0] = ka;
+            to[kUnits] = lg2_approx(y);  // 2^-22 of the value: 2^-17 at a scale of 2^-32, an fp16 weight rounds by 2^-11
+            to[2 * kUnits] = rcp_approx(y);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(v_full + (at & 1));
+          fetch(id1);
+          id1 = block_of(j + 2);
+        }
+        at0 += n;
+        if (__any_sync(0xffffffffu, dead)) break;
+      }
+    } else {
+      int at0 = 0, tile_at[2] = {0, 0}, mi = 0;  // key tiles, steps of the row tiles, row tiles with steps
+      for (int mt = blockIdx.z; mt < mts; mt += gridDim.z) {
+        const Part pt = part_of(mt);
+        const int steps = pt.steps, tiles = pt.two ? 2 : 1;
+        if (steps == 0) continue;
+        bool dead = false;
+        if (elect()) {
+          bool ok = mbar_wait(q_full, (uint32_t)mi & 1u);
+          const uint32_t sq = smem_u32(smem + S::kQ), sk = smem_u32(smem + S::kK), sv = smem_u32(smem + S::kV);
+          // step i's products; a key tile's stage is free once its last step's of all row tiles are done
+          const auto scores = [&](int t, int i) {
+            const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
+            const uint32_t qa = sq + t * S::kTileBytes, kb = sk + stage * S::kTileBytes + (i & 1) * (kStep * 128);
 #pragma unroll
-        for (int kk = 0; kk < DIM / 16; ++kk)
-          mma_f16_ss(tmem + t * 128 + buf * kStep, sw128_desc(qa + (kk >> 2) * S::kHalf) + 2 * (kk & 3), sw128_desc(kb + (kk >> 2) * S::kHalf) + 2 * (kk & 3),
-                     idesc_f16(128, kStep, false), kk > 0);
-        mma_commit(s_full + 2 * t + buf);
-        if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(k_empty + stage);
-      };
-      const auto values = [&](int t, int i) {
-        const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
-        const uint32_t vb = sv + stage * S::kTileBytes + (i & 1) * (kStep * 128);
+            for (int kk = 0; kk < DIM / 16; ++kk)
+              mma_f16_ss(tmem + t * 128 + buf * kStep, sw128_desc(qa + (kk >> 2) * S::kHalf) + 2 * (kk & 3), sw128_desc(kb + (kk >> 2) * S::kHalf) + 2 * (kk & 3),
+                         idesc_f16(128, kStep, false), kk > 0);
+            mma_commit(s_full + 2 * t + buf);
+            if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(k_empty + stage);
+          };
+          const auto values = [&](int t, int i) {
+            const int stage = (at0 + (i >> 1)) & 1, buf = (tile_at[t] + i) & 1;
+            const uint32_t vb = sv + stage * S::kTileBytes + (i & 1) * (kStep * 128);
 #pragma unroll
-        for (int kk = 0; kk < kStep / 16; ++kk)
-          mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + buf * kStep + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true),
-                     i > 0 || kk > 0);
-        mma_commit(o_done + t);
-        if (i == steps - 1) mma_commit(o_full + t);
-        if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(v_empty + stage);
-      };
-      const auto have = [&](uint64_t* full, int i) {
-        const int at = at0 + (i >> 1);
-        const bool there = mbar_wait(full + (at & 1), (uint32_t)(at >> 1) & 1u);
-        fence_after();
-        return there;
-      };
-      if (ok) ok = have(k_full, 0);
-      for (int i = 0; i < min(2, steps) && ok; ++i)
-        for (int t = 0; t < tiles; ++t) scores(t, i);
-      for (int i = 0; i < steps && ok; ++i) {
-        if ((i & 1) == 0) ok = have(v_full, i);
-        for (int t = 0; t < tiles && ok; ++t) {
-          const int at = tile_at[t] + i;
-          ok = mbar_wait(p_full + 2 * t + (at & 1), (uint32_t)(at >> 1) & 1u);
-          if (!ok) break;
-          fence_after();
-          values(t, i);
-          if (i + 2 < steps) {
-            if (t == 0 && (i & 1) == 0) ok = have(k_full, i + 2);
-            if (ok) scores(t, i + 2);
+            for (int kk = 0; kk < kStep / 16; ++kk)
+              mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + buf * kStep + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true),
+                         i > 0 || kk > 0);
+            mma_commit(o_done + t);
+            if (i == steps - 1) mma_commit(o_full + t);
+            if (t == tiles - 1 && ((i & 1) || i == steps - 1)) mma_commit(v_empty + stage);
+          };
+          const auto have = [&](uint64_t* full, int i) {
+            const int at = at0 + (i >> 1);
+            const bool there = mbar_wait(full + (at & 1), (uint32_t)(at >> 1) & 1u);
+            fence_after();
+            return there;
+          };
+          if (ok) ok = have(k_full, 0);
+          for (int i = 0; i < min(2, steps) && ok; ++i)
+            for (int t = 0; t < tiles; ++t) scores(t, i);
+          for (int i = 0; i < steps && ok; ++i) {
+            if ((i & 1) == 0) ok = have(v_full, i);
+            for (int t = 0; t < tiles && ok; ++t) {
+              const int at = tile_at[t] + i;
+              ok = mbar_wait(p_full + 2 * t + (at & 1), (uint32_t)(at >> 1) & 1u);
+              if (!ok) break;
+              fence_after();
+              values(t, i);
+              if (i + 2 < steps) {
+                if (t == 0 && (i & 1) == 0) ok = have(k_full, i + 2);
+                if (ok) scores(t, i + 2);
+              }
+            }
+          }
+          if (!ok) {  // the rows say NaN, once their own waits have run out; what was issued ends first
+            mma_commit(drain);
+            mbar_wait(drain, 0);
+            dead = true;
           }
         }
+        __syncwarp();
+        ++mi;
+        at0 += pt.n;
+        tile_at[0] += steps;
+        if (pt.two) tile_at[1] += steps;
+        if (__any_sync(0xffffffffu, dead)) break;
       }
-      if (!ok) {  // the rows say NaN, once their own waits have run out; what was issued ends first
-        mma_commit(drain);
-        mbar_wait(drain, 0);
-        dead = true;
-      }
-      }
-      __syncwarp();
-      ++mi;
-      at0 += pt.n;
-      tile_at[0] += steps;
-      if (pt.two) tile_at[1] += steps;
-      if (__any_sync(0xffffffffu, dead)) break;
+      asm volatile("bar.sync 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");  // the accumulators have been read
+      fence_after();
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
-    asm volatile("bar.sync 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");  // the accumulators have been read
-    fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
 }
 
