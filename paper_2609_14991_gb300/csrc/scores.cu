@@ -6,8 +6,8 @@
 //   S = sum 2^d_i,  E = sum 2^d_i d_i,
 //   log p(l) = (x_l - m) / T - ln S,   entropy = ln S - ln 2 E / S.
 // x_i - m is formed first (exact or rounded once), so a row's offset costs no
-// precision.  A row stays in registers (32 or 64 logits per thread): 32 to 512 threads
-// per row, above 16384 logits a cluster of 2 to 8 CTAs of 512 that exchange
+// precision.  A row stays in registers as it came (32 logits per thread, 64 of long 16-bit rows): 32 to 512
+// threads per row, above 16384 logits (32768 of 16 bits) a cluster of 2 to 8 CTAs of 512 that exchange
 // through distributed shared memory.  The k largest: the threads form 16 groups (per CTA); the
 // k-th largest of the groups' maxima is a bound that at least k logits reach and few pass
 // (about 11 of random ones for 8; the least of eight classes' maxima let 22 pass, which took 1.4 times as long in all).  Threads that hold one
@@ -61,26 +61,29 @@ __device__ __forceinline__ float to_float(T v) {
   return (float)v;
 }
 
-// eight (16-bit) or four (fp32) consecutive logits
+// eight consecutive logits from their words
 template <typename T>
-__device__ __forceinline__ void unpack(uint4 w, float* v) {
+__device__ __forceinline__ void unpack(const uint32_t* w, float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
-    v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
   } else {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-        v[2 * i] = __uint_as_float(u[i] << 16);
-        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        v[2 * i] = __uint_as_float(w[i] << 16);
+        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
       } else {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
         v[2 * i] = f.x;
         v[2 * i + 1] = f.y;
       }
     }
   }
 }
+// -inf in every place of a word
+template <typename T>
+constexpr uint32_t kNoneWord = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, __nv_bfloat16>::value ? 0xff80ff80u : 0xfc00fc00u;
 
 // order-preserving int of a float (-0 and 0 alike, no NaN)
 __device__ __forceinline__ int order_of(float x) {
@@ -99,7 +102,7 @@ __device__ __forceinline__ void warp_best(float& v, int& i) {
 }
 
 template <typename T, int G, int CS, int E>
-__global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 32 ? 128 : G)) k_label_rows(const __grid_constant__ RowsArgs a) {
+__global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1024 / (G == 32 ? 128 : G)) k_label_rows(const __grid_constant__ RowsArgs a) {
   constexpr int VE = 16 / sizeof(T), NV = E / VE;
   constexpr int kWarps = G / 32;
   constexpr int kLanes = G / kGroups;  // threads of a group
@@ -138,40 +141,29 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
   // the logits: whole aligned vectors, and the ends one by one
   const int lead = min(C, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int)sizeof(T));
   const int nvec = (C - lead) / VE, tail = C - lead - nvec * VE;
-  float v[E];
-  {
-    uint4 w[NV];
+  constexpr int kWords = 2 * sizeof(T);  // of eight logits
+  uint32_t held[E / 8 * kWords];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int j = rt + i * G * CS;
-      w[i] = make_uint4(0, 0, 0, 0);
-      if (j < nvec) w[i] = __ldcs(reinterpret_cast<const uint4*>(x + lead) + j);
-    }
-    if (given >= 0 && given < C) given_x = to_float(x[given]);
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      unpack<T>(w[i], v + i * VE);
-      if ((i + 1) * G * CS > nvec && rt + i * G * CS >= nvec) {  // the first test is the row's: most vectors skip the second
-#pragma unroll
-        for (int j = 0; j < VE; ++j) v[i * VE + j] = -INFINITY;
-      }
-    }
+  for (int i = 0; i < NV; ++i) {
+    const int j = rt + i * G * CS;
+    uint4 w = make_uint4(kNoneWord<T>, kNoneWord<T>, kNoneWord<T>, kNoneWord<T>);
+    if (j < nvec) w = __ldcs(reinterpret_cast<const uint4*>(x + lead) + j);
+    held[4 * i] = w.x, held[4 * i + 1] = w.y, held[4 * i + 2] = w.z, held[4 * i + 3] = w.w;
   }
+  if (given >= 0 && given < C) given_x = to_float(x[given]);
   const int xi = rt < lead ? rt : rt < lead + tail ? nvec * VE + rt : -1;
   const float xv = xi >= 0 ? to_float(x[xi]) : -INFINITY;
   const auto label_of = [&](int e) { return lead + (rt + e / VE * G * CS) * VE + e % VE; };
 
-  // maxima: of eight logits each, the thread's, the groups'
-  float sub[kEights];
-#pragma unroll
-  for (int i = 0; i < kEights; ++i) {
-    sub[i] = v[i * 8];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) sub[i] = fmaxf(sub[i], v[i * 8 + j]);
-  }
+  // maxima: the thread's, the groups'
+  const auto largest = [](const float (&v)[8]) { return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7]))); };
   float mine = xv;
 #pragma unroll
-  for (int i = 0; i < kEights; ++i) mine = fmaxf(mine, sub[i]);
+  for (int i = 0; i < kEights; ++i) {
+    float v[8];
+    unpack<T>(held + i * kWords, v);
+    mine = fmaxf(mine, largest(v));
+  }
   if (!(mine >= -INFINITY)) mine = INFINITY;  // NaN alone: the sums say so
   float gm = mine;
 #pragma unroll
@@ -205,20 +197,34 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
     bound = fmaxf(value_of(kth), -INFINITY);  // (a few steps below -inf is a NaN)
   }
 
+  // (unpacked anew, not kept unpacked since the maxima: that took registers there are not)
+  const auto forget = [&]() {
+    if constexpr (E > 32 && sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < E / 8 * kWords; ++i) asm volatile("" : "+r"(held[i]));
+    }
+  };
+  forget();
+
   // sums: in pairs, a masked logit's exponent held finite (its term is 0 all the same)
   const float ms = m == -INFINITY ? 0.f : m, c = a.o.inv_temp * kLog2e;
   uint64_t s2 = 0, e2 = 0;
   const uint64_t nm = pair_of(-ms, -ms), cc = pair_of(c, c);
 #pragma unroll
-  for (int e = 0; e < E; e += 2) {
-    const uint64_t d = mul2(add2(pair_of(v[e], v[e + 1]), nm), cc);
-    float d0, d1;
-    unpair(d, d0, d1);
-    d0 = max_nan(d0, -1e30f);
-    d1 = max_nan(d1, -1e30f);
-    const uint64_t p = pair_of(ex2_approx(d0), ex2_approx(d1));
-    s2 = add2(s2, p);
-    e2 = fma2(p, pair_of(d0, d1), e2);
+  for (int i = 0; i < kEights; ++i) {
+    float v[8];
+    unpack<T>(held + i * kWords, v);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const uint64_t d = mul2(add2(pair_of(v[e], v[e + 1]), nm), cc);
+      float d0, d1;
+      unpair(d, d0, d1);
+      d0 = max_nan(d0, -1e30f);
+      d1 = max_nan(d1, -1e30f);
+      const uint64_t p = pair_of(ex2_approx(d0), ex2_approx(d1));
+      s2 = add2(s2, p);
+      e2 = fma2(p, pair_of(d0, d1), e2);
+    }
   }
   float S, E2;
   {
@@ -237,18 +243,22 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
   if (lane == 0) peer(0)->sums[rank * kWarps + warp] = make_float2(S, E2);
 
   // gather the eights with a logit that reaches the bound
+  forget();
   constexpr int kMine = RowShared<CS>::kEights / CS;
   if (k > 0 && mine >= bound && mine > -INFINITY) {
 #pragma unroll
-    for (int i = 0; i < kEights; ++i)
-      if (sub[i] >= bound) {
+    for (int i = 0; i < kEights; ++i) {
+      float v[8];
+      unpack<T>(held + i * kWords, v);
+      if (largest(v) >= bound) {
         const int at = atomicAdd(&sh.count, 1);
         if (at < kMine) {
-          sh.eight[at][0] = make_float4(v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3]);
-          sh.eight[at][1] = make_float4(v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]);
+          sh.eight[at][0] = make_float4(v[0], v[1], v[2], v[3]);
+          sh.eight[at][1] = make_float4(v[4], v[5], v[6], v[7]);
           sh.code[at] = rt * kEights + i;
         }
       }
+    }
     if (xv >= bound && xi >= 0) {
       const int at = atomicAdd(&sh.count, 1);
       if (at < kMine) {
@@ -379,7 +389,12 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E > 32 ? 1 : 1024 / (G == 3
       for (int i = t; i < C; i += alone ? 32 : G) look(to_float(x[i]), i);
     } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) look(v[e], label_of(e));
+      for (int i = 0; i < kEights; ++i) {
+        float v[8];
+        unpack<T>(held + i * kWords, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) look(v[j], label_of(8 * i + j));
+      }
       if (xi >= 0) look(xv, xi);
     }
     warp_best(bv, bi);
@@ -427,7 +442,9 @@ cudaError_t launch(const RowsArgs& a, bool after, cudaStream_t s) {
 // The fewest threads that hold a row in 32 registers each: with twice as many, half of which
 // idle, 16384 rows of 4097 take 94 us and not 51, of 1500 44 and not 31 (200 rows of 4097, a
 // wave at most: 4.9 and 4.7).  64 registers above 8 x 512 x 32; 8 for rows of at most a warp's worth of
-// them (16384 x 120: 11 us, with 32 15).
+// them (16384 x 120: 11 us, with 32 15).  Rows of 16 bits above 16384 pack 64 logits into 32 registers, half as many
+// CTAs: 96 x 131073 20 us and 24, 300 x 60000 21 and 30, 2000 x 20000 60 and 79; where all fit at once anyway
+// they wait longer for each other's sums, 1 x 131073 8.2 and 7.2.
 template <typename T>
 cudaError_t launch_type(const RowsArgs& a, bool after, cudaStream_t s) {
   const int vecs = a.C / (16 / (int)sizeof(T)) + 1;  // most whole vectors, with one of the ends
@@ -439,9 +456,12 @@ cudaError_t launch_type(const RowsArgs& a, bool after, cudaStream_t s) {
   if (v <= 128 * per) return launch<T, 128, 1, 32>(a, after, s);
   if (v <= 256 * per) return launch<T, 256, 1, 32>(a, after, s);
   if (v <= 512 * per) return launch<T, 512, 1, 32>(a, after, s);
-  if (v <= 1024 * per) return launch<T, 512, 2, 32>(a, after, s);
-  if (v <= 2048 * per) return launch<T, 512, 4, 32>(a, after, s);
-  if (v <= 4096 * per) return launch<T, 512, 8, 32>(a, after, s);
+  constexpr int kE = sizeof(T) == 4 ? 32 : 64;  // 16-bit logits stay packed: as many registers for twice as many
+  const int most = v * (16 / (int)sizeof(T)) / kE;  // threads that hold the row
+  if (kE > 32 && most <= 512) return launch<T, 512, 1, kE>(a, after, s);
+  if (most <= 1024) return launch<T, 512, 2, kE>(a, after, s);
+  if (most <= 2048) return launch<T, 512, 4, kE>(a, after, s);
+  if (most <= 4096) return launch<T, 512, 8, kE>(a, after, s);
   return launch<T, 512, 8, 64>(a, after, s);
 }
 
