@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
         }
         if (mw == 0 && i + ST - 1 < n) issue(i + ST - 1);
         const int at = it0 + i, st = at % ST;
-        if (!mbar_wait(full + st, (uint32_t)(at / ST) & 1u)) {
+        if (!__all_sync(0xffffffffu, mbar_wait(full + st, (uint32_t)(at / ST) & 1u))) {
           // what is still in flight lands before anything reuses the ring
           for (int j = at + 1; j < min(it0 + n, at + ST); ++j) mbar_wait(full + j % ST, (uint32_t)(j / ST) & 1u);
           expired = true;

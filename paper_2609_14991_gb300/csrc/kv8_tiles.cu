@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
 #pragma unroll 1
       for (int j = 0; j < n; ++j) {
         const int at = at0 + j, id = block_of(j + 2);
-        if (at >= 2 && !mbar_wait(empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
+        if (at >= 2 && !__all_sync(0xffffffffu, mbar_wait(empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u))) {
           dead = true;
           break;
         }
@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
 #pragma unroll 1
         for (int j = 0; j < n; ++j) {
           const int at = at0 + j;
-          if (at >= 2 && !mbar_wait(v_empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u)) {
+          if (at >= 2 && !__all_sync(0xffffffffu, mbar_wait(v_empty + (at & 1), (uint32_t)((at >> 1) - 1) & 1u))) {
             dead = true;
             break;
           }
