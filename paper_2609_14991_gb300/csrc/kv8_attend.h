@@ -2,6 +2,7 @@
 #pragma once
 
 #include "kv8.h"
+#include "kv8_keys.h"
 
 namespace tsd {
 
@@ -39,29 +40,6 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b) {
   }
   const __half2 v = __floats2half2_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&v);
-}
-
-constexpr int kKv8Unit = 16;  // tokens that are sure to share a block
-
-// The key tiles that rows at positions pos0 .. pos1 see: first those of the
-// sinks before the window, then the window's.
-struct KeyTiles {
-  int sink, from, total;  // sink tiles 0 .. sink-1, then tiles from, from + 1, ..
-  __device__ __forceinline__ int token(int j) const { return kKv8Unit * (j < sink ? j : from + j - sink); }
-};
-__device__ __forceinline__ KeyTiles key_tiles(int pos0, int pos1, int window, int sinks) {
-  const int first = window > 0 ? max(0, pos0 - window + 1) : 0;
-  KeyTiles k;
-  k.sink = (min(sinks, first) + kKv8Unit - 1) / kKv8Unit;
-  k.from = max(k.sink, first / kKv8Unit);
-  k.total = k.sink + pos1 / kKv8Unit + 1 - k.from;
-  return k;
-}
-
-// Where share i of `parts` even shares of `all` begins.
-__device__ __forceinline__ int share_from(int all, int i, int parts) {
-  const int each = all / parts;
-  return i * each + min(i, all - each * parts);
 }
 
 __device__ __forceinline__ float lg2_approx(float x) {

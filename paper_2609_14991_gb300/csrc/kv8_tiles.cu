@@ -245,10 +245,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
     p.row0 = (mts - 1 - mt) * 256;  // the later rows see the most keys: they go first, of all heads and sequences
     p.two = rows - p.row0 > 128;
     p.units = key_tiles(before + p.row0 / a.group, before + (min(rows, p.row0 + 256) - 1) / a.group, a.window, a.sinks);
-    const int all = (p.units.total + kUnits - 1) / kUnits;
-    p.lo = splits == 1 ? 0 : share_from(all, split, splits);
-    p.n = (splits == 1 ? all : share_from(all, split + 1, splits)) - p.lo;
-    p.steps = (min(p.units.total, (p.lo + p.n) * kUnits) - p.lo * kUnits + kStepUnits - 1) / kStepUnits;
+    const KeyShare share = key_share(p.units.total, kUnits, kStepUnits, split, splits);
+    p.lo = share.lo, p.n = share.n, p.steps = share.steps;
     return p;
   };
   // Every role walks the row tiles by itself (each has registers of its own number), so the

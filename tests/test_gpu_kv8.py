@@ -189,6 +189,35 @@ def test_row_tiles(heads, kv, counts, past, window, sinks, dim, dtype):
         b.check_attend(counts, heads, window=window, sinks=sinks, **kw)
 
 
+@pytest.mark.parametrize("past", [9, 10, 16])
+def test_row_tiles_with_empty_shares_of_keys(past):
+    """More shares than a row tile has key tiles, its units 1 more than whole key tiles; a CTA takes several row tiles."""
+    b = Batch(tsd, [past + 1000], 1, 16, 64, seed=past, spare_width=512)
+    b.append([past])
+    b.append([1000])
+    b.check_attend([1000], 2, max_new=96)
+
+
+def test_a_short_sequence_beside_a_prompt_takes_no_time():
+    """A sequence with fewer key tiles than a prompt's are shared out to: its empty shares wait for nothing."""
+    b = Batch(tsd, [2000, 9], 1, 16, 64, seed=2)
+    b.append([2000, 9])
+    q, both = b.rows(2009, 1), b.args([2000, 9])
+    alone = {**both, "slots": both["slots"][:1].contiguous(), "starts": both["starts"][:2].contiguous()}
+    ms = []
+    for rows, a in ((2000, alone), (2009, both)):
+        times = []
+        for _ in range(8):
+            x, y = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            x.record()
+            b.cache.attend(q[:rows], **a, max_new=2000, max_len=2000)
+            y.record()
+            y.synchronize()
+            times.append(x.elapsed_time(y))
+        ms.append(min(times))
+    assert ms[1] < ms[0] + 0.1, ms
+
+
 def test_row_tiles_of_spoilt_rows_and_blocks():
     """NaN reaches the rows that see it in the tiled form too, and a bad sequence is all NaN."""
     b = Batch(tsd, [400, 300], 1, 16, 64, seed=3)
