@@ -24,7 +24,7 @@
 // softmax, 3700 clocks, and its products, 1600, took turns.)  Keys are the K-major B
 // operand of the scores; the same layout of the values is read as an MN-major B
 // operand, so neither is transposed.  The maximum is looked for, and the accumulator rescaled in
-// TMEM, only in steps whose probabilities outgrow fp16.
+// TMEM, only in steps whose probabilities outgrow fp16, and in which a row sees its first key.
 //
 // Measured (16 query and 4 key heads of 128, bf16): 2000 clocks per step of 64 keys and 256
 // rows, of which the MMAs are 1300 (49 for 128 x 64 x 16, whose operands come from shared
@@ -353,7 +353,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
           // Probabilities relative to the maximum so far, without looking for this step's:
           // one that a score has outgrown shows in the sum, and the step is taken again from
           // its scores, which the probabilities have not replaced yet.  (Sums up to 2^15:
-          // no probability then reaches fp16's largest.)
+          // no probability then reaches fp16's largest.)  A row that has seen nothing (its
+          // window begins later) has no maximum: relative to -1e30 a key that it sees now
+          // has outgrown anything, and a masked one still adds 0.
           uint32_t y[kStep / 2];
           float more;
           bool look = i == 0;
@@ -395,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_kv8_tiles(const __grid_constant
                 }
               }
             }
-            const float ref = m == -INFINITY ? 0.f : m - 7.f;
+            const float ref = m > -INFINITY ? m - 7.f : look ? 0.f : -1e30f;
             more = 0.f;
             float whole_sum = 0.f;
             const auto unit = [&](const uint32_t (&raw)[kUnit], int u) {
