@@ -11,9 +11,9 @@
 // through distributed shared memory.  The k largest: the threads form 16 groups (per CTA); the
 // k-th largest of the groups' maxima is a bound that at least k logits reach and few pass
 // (about 11 of random ones for 8; the least of eight classes' maxima let 22 pass, which took 1.4 times as long in all).  Threads that hold one
-// leave it with its seven neighbours; one warp picks and orders.  If more
-// than the gathering holds reach it (many equal logits), k rounds of a maximum over
-// the whole row take its place.
+// leave it with its seven neighbours; one warp picks and orders, in k rounds of a
+// maximum where more than 32 reach it.  If the gathering has no room for them (many equal
+// logits), those rounds go over the whole row, by all threads of its CTA.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1
     bound = fmaxf(value_of(kth), -INFINITY);  // (a few steps below -inf is a NaN)
   }
 
-  // (unpacked anew, not kept unpacked since the maxima: that took registers there are not)
+  // (unpacked anew each time, not kept unpacked since the maxima: that took registers there are not)
   const auto forget = [&]() {
     if constexpr (E > 32 && sizeof(T) == 2) {
 #pragma unroll
@@ -318,25 +318,24 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1
   if (t == 0 && a.o.entropy) a.o.entropy[row] = sums.entropy;
 
   // the k best in order
-  if (!over) {
+  if (!over) {  // the first warp alone: all that reach the bound are in the gathered eights
     if (k == 0) return;
-    // the gathered eights' logits that reach the bound, with their labels
+    const auto label_at = [&](int at, int j) {
+      const int code = sh.code[at], e = code % kEights * 8 + j;
+      return code < 0 ? ~code : lead + (code / kEights + e / VE * G * CS) * VE + e % VE;
+    };
+    const auto logit_at = [&](int at, int j) { return reinterpret_cast<const float*>(sh.eight[at])[j]; };
+    // those logits, with their labels
     int found = 0;
     for (int base = 0; base < count; base += 4) {  // eight lanes per eight
       const int at = base + (lane >> 3), j = lane & 7;
-      float y = -INFINITY;
-      int label = 0;
-      if (at < count) {
-        const int code = sh.code[at], e = code % kEights * 8 + j;
-        y = reinterpret_cast<const float*>(sh.eight[at])[j];
-        label = code < 0 ? ~code : lead + (code / kEights + e / VE * G * CS) * VE + e % VE;
-      }
+      const float y = at < count ? logit_at(at, j) : -INFINITY;
       const bool in = y >= bound && y > -INFINITY;
       const unsigned who = __ballot_sync(0xffffffffu, in);
       const int to = found + __popc(who & ((1u << lane) - 1));
       if (in && to < kCap) {
         sh.cv[to] = y;
-        sh.ci[to] = label;
+        sh.ci[to] = label_at(at, j);
       }
       found += __popc(who);
     }
@@ -351,29 +350,29 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1
       if (lane >= found && lane < k) label_alternative(a.o, row, lane, sums, -INFINITY, -1);  // fewer than k
       return;
     }
-    over = found > kCap;
-    if (!over) {
-      float pv = INFINITY;
-      int pi = -1;
-      for (int r = 0; r < k; ++r) {
-        float bv = -INFINITY;
-        int bi = 0x7fffffff;
-        for (int i = lane; i < found; i += 32) {
-          const float y = sh.cv[i];
-          const int l = sh.ci[i];
-          if (before(pv, pi, y, l) && before(y, l, bv, bi)) bv = y, bi = l;
-        }
-        warp_best(bv, bi);
-        if (lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
-        pv = bv;
-        pi = bi;
+    // more: k rounds of the best one after the last, in the list or, where it has no room, in the eights
+    float pv = INFINITY;
+    int pi = -1;
+    for (int r = 0; r < k; ++r) {
+      float bv = -INFINITY;
+      int bi = 0x7fffffff;
+      const auto look = [&](float y, int l) {
+        if (y > -INFINITY && before(pv, pi, y, l) && before(y, l, bv, bi)) bv = y, bi = l;
+      };
+      if (found <= kCap) {
+        for (int i = lane; i < found; i += 32) look(sh.cv[i], sh.ci[i]);
+      } else {
+        for (int i = lane; i < 8 * count; i += 32) look(logit_at(i >> 3, i & 7), label_at(i >> 3, i & 7));
       }
-      return;
+      warp_best(bv, bi);
+      if (lane == 0) label_alternative(a.o, row, r, sums, bv, bi);
+      pv = bv;
+      pi = bi;
     }
+    return;
   }
-  // Many equal logits: a maximum over the whole row per round, by all threads where the
-  // eights had no room, by one warp from memory where their logits had none.
-  const bool alone = count <= kMine;
+  // Many equal logits, for whose eights there was no room: a maximum over the whole row per
+  // round, by all threads of the (first) CTA; a cluster's from memory.
   float pv = INFINITY;
   int pi = -1;
   for (int r = 0; r < k; ++r) {
@@ -385,9 +384,10 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1
         bi = i;
       }
     };
-    if (CS > 1 || alone) {  // the first CTA, or its first warp
-      for (int i = t; i < C; i += alone ? 32 : G) look(to_float(x[i]), i);
+    if constexpr (CS > 1) {
+      for (int i = t; i < C; i += G) look(to_float(x[i]), i);
     } else {
+      forget();
 #pragma unroll
       for (int i = 0; i < kEights; ++i) {
         float v[8];
@@ -398,7 +398,7 @@ __global__ void __launch_bounds__(G == 32 ? 128 : G, E * sizeof(T) > 128 ? 1 : 1
       if (xi >= 0) look(xv, xi);
     }
     warp_best(bv, bi);
-    if (!alone) {
+    if constexpr (kWarps > 1) {
       if (lane == 0) {
         sh.best_v[warp] = bv;
         sh.best_i[warp] = bi;
