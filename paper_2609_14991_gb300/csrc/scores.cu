@@ -457,11 +457,11 @@ cudaError_t launch_type(const RowsArgs& a, bool after, cudaStream_t s) {
   if (v <= 256 * per) return launch<T, 256, 1, 32>(a, after, s);
   if (v <= 512 * per) return launch<T, 512, 1, 32>(a, after, s);
   constexpr int kE = sizeof(T) == 4 ? 32 : 64;  // 16-bit logits stay packed: as many registers for twice as many
-  const int most = v * (16 / (int)sizeof(T)) / kE;  // threads that hold the row
-  if (kE > 32 && most <= 512) return launch<T, 512, 1, kE>(a, after, s);
-  if (most <= 1024) return launch<T, 512, 2, kE>(a, after, s);
-  if (most <= 2048) return launch<T, 512, 4, kE>(a, after, s);
-  if (most <= 4096) return launch<T, 512, 8, kE>(a, after, s);
+  constexpr int kPer = kE / (16 / (int)sizeof(T));  // whole vectors per thread
+  if (kE > 32 && v <= 512 * kPer) return launch<T, 512, 1, kE>(a, after, s);
+  if (v <= 2 * 512 * kPer) return launch<T, 512, 2, kE>(a, after, s);
+  if (v <= 4 * 512 * kPer) return launch<T, 512, 4, kE>(a, after, s);
+  if (v <= 8 * 512 * kPer) return launch<T, 512, 8, kE>(a, after, s);
   return launch<T, 512, 8, 64>(a, after, s);
 }
 

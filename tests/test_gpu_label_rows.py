@@ -1,4 +1,5 @@
-"""label_scores on long rows: equal best logits, few and many, spread and close together."""
+"""label_scores on long rows: equal best logits, few and many, spread and close together; rows
+around the most that each variant holds."""
 import math
 
 import pytest
@@ -62,3 +63,28 @@ def test_joint_equal_best_logits():
         x = A.double() @ W.double().t()
         got = tsd.joint_label_scores(A.to(DEV), W.to(torch.bfloat16).to(DEV), k=8)
         lu.assert_scores(got, lu.oracle(x, None, 8), n, float(x.max() - x.min()))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("threads", [32, 64, 128, 256, 512, 1024, 2048, 4096])
+def test_rows_around_what_a_variant_holds(threads, dtype):
+    """Aligned rows of as many whole vectors as that many threads hold (in 8, 32 and 64 logits each), up
+    to eight more, and the vectors' ends: the largest logit in the last whole vector, the next in the end."""
+    size = torch.finfo(TYPES[dtype]).bits // 8
+    vec = 16 // size
+    for each in (8, 32, 64):
+        full = threads * each
+        for C in sorted({full + d for d in (-vec, -1, 0, 1)} | {full + d * vec + e for d in range(1, 9) for e in (0, vec - 1)}):
+            if C > 262144:
+                continue
+            x = (torch.randn(2, -(-C // vec) * vec, device=DEV)).to(TYPES[dtype])[:, :C]
+            assert x.data_ptr() % 16 == 0 and x.stride(0) % vec == 0
+            last = C // vec * vec - 1
+            x[0, last], x[0, last - vec + 1], x[1, C - 1], x[1, 0] = 20.0, 18.0, 20.0, 19.0
+            got = tsd.label_scores(x, torch.tensor([[last], [C - 1]], dtype=torch.int32, device=DEV), k=2)
+            lp = torch.log_softmax(x.double(), 1)
+            top = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :2]
+            assert torch.equal(got.alt_labels, top.to(torch.int32)), C
+            # a logarithm of a sum near 1 and a difference of logits below 32: see assert_scores
+            assert float((got.alt_logp - torch.gather(lp, 1, top)).abs().max()) < 8e-6 + 3 * 2 ** -24 * 32, C
+            assert torch.equal(got.logp[:, 0], got.alt_logp[:, 0]), C
