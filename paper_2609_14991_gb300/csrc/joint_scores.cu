@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float all = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
           if (__any_sync(0xffffffffu, all > m)) {
             const float to = fmaxf(m, all);
-            const float d = m == -INFINITY ? 0.f : (m - to) * c, w = ex2_approx(d);
+            const float d = growth(m, to, c), w = ex2_approx(d);
             e = w * fmaf(d, s, e);
             s *= w;
             m = to;
@@ -528,8 +528,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int p = 1; p < S::kParts; ++p) {
             const float to = fmaxf(m, of[p].x);
-            const float d0 = m == -INFINITY ? 0.f : (m - to) * c, w0 = ex2_approx(d0);
-            const float d1 = of[p].x == -INFINITY ? 0.f : (of[p].x - to) * c, w1 = ex2_approx(d1);
+            const float d0 = growth(m, to, c), w0 = ex2_approx(d0);
+            const float d1 = growth(of[p].x, to, c), w1 = ex2_approx(d1);
             e = w0 * fmaf(d0, s, e) + w1 * fmaf(d1, of[p].y, of[p].z);
             s = w0 * s + w1 * of[p].y;
             m = to;
@@ -603,8 +603,8 @@ __global__ void __launch_bounds__(128) k_joint_scores_join(const __grid_constant
   };
   const auto join = [&](float om, float os, float oe) {
     const float to = fmaxf(m, om);
-    const float d0 = m == -INFINITY ? 0.f : (m - to) * c, x0 = ex2_approx(d0);
-    const float d1 = om == -INFINITY ? 0.f : (om - to) * c, x1 = ex2_approx(d1);
+    const float d0 = growth(m, to, c), x0 = ex2_approx(d0);
+    const float d1 = growth(om, to, c), x1 = ex2_approx(d1);
     e = x0 * fmaf(d0, s, e) + x1 * fmaf(d1, os, oe);
     s = x0 * s + x1 * os;
     m = to;

@@ -30,6 +30,11 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return r;
 }
 
+// The exponent of a running sum whose maximum grows from m to `to`.  Held finite: the
+// weight 2^d of a far lower maximum (labels masked by the type's lowest value) is 0, and E's
+// share, d S times it, is not to be infinity times 0.
+__device__ __forceinline__ float growth(float m, float to, float c) { return m == -INFINITY ? 0.f : max_nan((m - to) * c, -1e30f); }
+
 // What a row's scores are made of.
 struct RowScore {
   float m, ln_s, entropy;

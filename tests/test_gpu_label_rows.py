@@ -88,3 +88,50 @@ def test_rows_around_what_a_variant_holds(threads, dtype):
             # a logarithm of a sum near 1 and a difference of logits below 32: see assert_scores
             assert float((got.alt_logp - torch.gather(lp, 1, top)).abs().max()) < 8e-6 + 3 * 2 ** -24 * 32, C
             assert torch.equal(got.logp[:, 0], got.alt_logp[:, 0]), C
+
+
+@pytest.mark.parametrize("n,C", [(3, 700), (5000, 2100), (129, 40001), (260, 30000)])
+@pytest.mark.parametrize("temperature", [1.0, 0.1])
+def test_joint_masks_of_the_types_lowest_value(n, C, temperature):
+    """Labels ruled out by a column of bf16's lowest value, in half of the rows: runs of them and single ones
+    (stored and kept logits).  Their weight is 0, and the others' scores are those of a row without them."""
+    H, low = 64, torch.finfo(torch.bfloat16).min
+    g = torch.Generator().manual_seed(C)
+    A = ((torch.relu(torch.randn(n, H, generator=g) * 1.4).clamp(max=7.9) * 16).round() / 16)
+    W = ((torch.randn(C, H, generator=g) * 0.07).clamp(-0.24, 0.24) * 256).round() / 256
+    off = torch.rand(C, generator=g) < 0.1
+    off[:300] = True  # whole tiles' parts from the first label on
+    off[C // 2:C // 2 + 64] = True
+    off[C - 5:] = True
+    A[:, 0] = (torch.arange(n) % 3 != 1).float()
+    W[:, 0] = off * low
+    A, W = A.to(torch.bfloat16).to(DEV), W.to(torch.bfloat16).to(DEV)
+    lab = torch.stack([torch.randint(0, C, (n,), generator=g), torch.full((n,), 7)], 1).to(torch.int32).to(DEV)
+    x = A.double() @ W.double().t()
+    lp = torch.log_softmax(x / temperature, 1)
+    fine = x > -1e30
+    spread = float((x[fine].max() - x[fine].min())) / temperature
+    tol = 8e-6 + 3 * 2 ** -24 * spread  # as in assert_scores
+    for k in (0, 4, 8):
+        got = tsd.joint_label_scores(A, W, lab, k=k, temperature=temperature)
+        assert float((got.entropy + (lp.exp() * lp).sum(1)).abs().max()) < 3 * tol, k
+        want = torch.gather(lp, 1, lab.long())
+        seen = torch.gather(fine, 1, lab.long())
+        assert float((got.logp - want)[seen].abs().max()) < tol
+        assert bool((got.logp[~seen] < -1e38).all())
+        top = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+        assert torch.equal(got.alt_labels, top.to(torch.int32))
+        assert k == 0 or float((got.alt_logp - torch.gather(lp, 1, top)).abs().max()) < tol
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("C", [40, 1025, 9000, 50000])
+def test_masks_of_the_types_lowest_value(C, dtype):
+    low = torch.finfo(TYPES[dtype]).min
+    x = torch.randn(4, C, device=DEV).to(TYPES[dtype])
+    x[1, : C // 2], x[2, 1:], x[3, ::3] = low, low, low
+    lp = torch.log_softmax(x.double(), 1)
+    got = tsd.label_scores(x, k=3)
+    assert float((got.entropy + (lp.exp() * lp).sum(1)).abs().max()) < 3 * (8e-6 + 3 * 2 ** -24 * 16)
+    top = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :3]
+    assert torch.equal(got.alt_labels, top.to(torch.int32))
