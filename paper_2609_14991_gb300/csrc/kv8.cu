@@ -10,6 +10,7 @@
 #include <climits>
 
 #include "kv8.h"
+#include "kv8_keys.h"
 #include "tc_common.cuh"
 
 namespace tsd {
@@ -279,8 +280,7 @@ extern "C" tsd_status tsd_kv8_append(const tsd_kv8* cache, const tsd_kv8_batch* 
   if (tsd_status st = kv8_check_rows("tsd_kv8_append", "k", k, k_row, k_head)) return st;
   if (tsd_status st = kv8_check_rows("tsd_kv8_append", "v", v, v_row, v_head)) return st;
   AppendArgs a{*cache, *batch, {static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v)}, {k_row, v_row}, {k_head, v_head}};
-  const int most = batch->max_new ? (batch->max_new < batch->rows ? batch->max_new : batch->rows) : batch->rows;
-  const int64_t blocks = ((int64_t)most + 2 * cache->block - 2) / cache->block;
+  const int64_t blocks = append_blocks(batch->n, batch->rows, batch->starts != nullptr, batch->max_new, cache->block);
   const dim3 grid((unsigned)blocks, 1, batch->n);
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   if (cache->dtype == TSD_BF16) launch_append_type<true>(a, grid, s);

@@ -1,6 +1,8 @@
 // Which keys of the 8-bit paged cache a tile of query rows sees, and how they are dealt
-// out to CTAs (kv8_rows.cu, kv8_tiles.cu).
+// out to CTAs (kv8_rows.cu, kv8_tiles.cu); how many CTAs an append takes (kv8.cu).
 #pragma once
+
+#include <cstdint>
 
 #ifdef __CUDACC__
 #define TSD_HD __host__ __device__
@@ -46,6 +48,16 @@ TSD_HD inline KeyShare key_share(int units, int tile_units, int step_units, int 
   const int from = s.lo * tile_units, to = from + s.n * tile_units, end = units < to ? units : to;
   s.steps = end > from ? (end - from + step_units - 1) / step_units : 0;  // (an empty share begins past the last unit)
   return s;
+}
+
+// Blocks of a sequence that an append's launch has CTAs for (a CTA takes more in turn): all that
+// max_new rows may touch; one row's without starts; else sixteen times the mean's, so that a launch
+// grows with its rows and sequences and not with their product (1024 x 1, 8 heads of 128: 65 us, with
+// CTAs for all rows in each 168; a prompt of 4000 beside 63 x 1: 25 and 41).
+inline int64_t append_blocks(int n, int rows, bool starts, int max_new, int block) {
+  const int64_t mean = ((int64_t)rows + n - 1) / n;
+  const int64_t most = max_new ? max_new : !starts ? 1 : 16 * mean;
+  return ((most < rows ? most : rows) + 2 * block - 2) / block;
 }
 
 }  // namespace tsd

@@ -23,6 +23,23 @@ def test_append_holds_the_rounded_tokens(block, dim, dtype):
     b.check_held()
 
 
+@pytest.mark.parametrize("rows", [[3000] + [1] * 40, [1] * 50, [0] * 30 + [700]])
+def test_append_without_bounds(rows):
+    """A prompt among single tokens, and single tokens with and without starts, no bound given."""
+    b = Batch(tsd, [x + 20 for x in rows], 1, 16, 64, seed=len(rows), spare_slots=0)
+    b.append([17] * len(rows))
+    b.append(rows)
+    b.check_held()
+    if max(rows) == 1:
+        k, a = b.rows(len(rows), 1), b.args(rows)
+        a["lens"] += 1
+        b.cache.append(k, k, a["table"], a["lens"], slots=a["slots"])
+        for i, s in enumerate(b.slots):
+            b.len[i] += 1
+            b.model.append(s, k[i:i + 1], k[i:i + 1])
+        b.check_held()
+
+
 @pytest.mark.parametrize("block", [16, 64])
 def test_append_does_not_depend_on_the_splits(block):
     lens = [2 * block + 7, 5, block, 150]
