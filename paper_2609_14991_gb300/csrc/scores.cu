@@ -478,8 +478,8 @@ tsd_status label_check(const char* who, int32_t n, int32_t most_n, int32_t C, fl
                        const int32_t* labels, int32_t k, const float* logp, const int32_t* alt_labels, const float* alt_logp) {
   if (n < 1 || n > most_n) return fail(TSD_EINVAL, "%s: n=%d outside [1, %d]", who, n, most_n);
   if (C < 1 || C > 262144) return fail(TSD_EINVAL, "%s: C=%d outside [1, 262144]", who, C);
-  if (!(temperature > 0.f) || temperature > 3.4e38f || !(1.f / temperature <= 3.4e38f))
-    return fail(TSD_EINVAL, "%s: temperature=%g must be positive and finite, as its reciprocal", who, (double)temperature);
+  if (!(temperature > 0.f) || temperature > 3.4e38f || !(1.f / temperature * kLog2e <= 3.4e38f))  // the exponents' factor
+    return fail(TSD_EINVAL, "%s: temperature=%g must be positive and finite, as log2(e) over it", who, (double)temperature);
   if (m < 0 || m > kMaxGiven) return fail(TSD_EINVAL, "%s: m=%d outside [0, %d]", who, m, kMaxGiven);
   if (k < 0 || k > kMaxAlt) return fail(TSD_EINVAL, "%s: k=%d outside [0, %d]", who, k, kMaxAlt);
   if (m > 0 && (!labels || !logp)) return fail(TSD_EINVAL, "%s: NULL labels or logp with m=%d", who, m);

@@ -121,3 +121,11 @@ def test_bindings_refuse_host_tensors():
         tsd.KV8Cache(k8.float(), k8, sc, sc, tail, tail)
     with pytest.raises(ValueError, match="block"):
         tsd.KV8Cache(torch.zeros(4, 2, 8, 64, dtype=torch.int8), k8, sc, sc, torch.zeros(3, 2, 2, 8, 64, dtype=torch.bfloat16), tail)
+
+
+def test_temperatures_whose_exponent_factor_overflows(L):
+    """log2(e) / T has to be finite too: with an infinite factor a difference of 0 would be NaN."""
+    for t in (2.95e-39, 3.5e-39, 4.2e-39):
+        st = L.tsd_label_scores(2, 10, P, 0, 10, t, 1, P, 2, P, P, P, P, None)
+        refused(L, st, "temperature")
+        refused(L, L.tsd_joint_label_scores(2, 64, 10, P, 64, P, 64, t, 0, None, 0, P, P, P, P, P, 1 << 30, None), "temperature")
