@@ -86,6 +86,7 @@ struct ScoreShape {
   static constexpr int kSmem = kBarOff + 512 + 1024;
   static_assert((2 * kStages + 5) * 8 + 4 <= 512, "barrier area");
   static_assert(kSmem <= 227 * 1024 && kStages >= 4, "shared memory per CTA");
+  static_assert(K <= 0 || (kParts == 4 && kCols == 64), "lists of four parts, of eight groups of eight each");
 };
 
 constexpr float kLowest = -3.402823466e38f;  // finite: masked logits (-inf) stay below it
@@ -187,20 +188,19 @@ __device__ __forceinline__ void merge_top(float (&a)[K], const float (&b)[K]) {
       }
 }
 
-// Enters N group maxima (8 or 4) into the list of the K largest.
-template <int K, int N>
-__device__ __forceinline__ void enter(float (&kept)[K], const float (&groups)[N]) {
-  constexpr int M = N > K ? N : K;
-  float x[M];
+// Enters eight group maxima into the list of the K largest (K 4 or 8).
+template <int K>
+__device__ __forceinline__ void enter(float (&kept)[K], const float (&groups)[8]) {
+  float x[8];
 #pragma unroll
-  for (int i = 0; i < M; ++i) x[i] = i < N ? groups[i] : -INFINITY;
+  for (int i = 0; i < 8; ++i) x[i] = groups[i];
   // bitonic sort, descending
 #pragma unroll
-  for (int w = 2; w <= M; w <<= 1)
+  for (int w = 2; w <= 8; w <<= 1)
 #pragma unroll
     for (int d = w / 2; d > 0; d >>= 1)
 #pragma unroll
-      for (int i = 0; i < M; ++i)
+      for (int i = 0; i < 8; ++i)
         if (!(i & d)) {
           const float hi = fmaxf(x[i], x[i + d]), lo = fminf(x[i], x[i + d]);
           const bool down = (i & w) == 0;
@@ -213,25 +213,23 @@ __device__ __forceinline__ void enter(float (&kept)[K], const float (&groups)[N]
   merge_top<K>(kept, b);
 }
 
-// The K-th largest of the parts' lists ([part][K / 4][128], this thread's row).
-template <int K, int PARTS>
+// The K-th largest of the four parts' lists ([part][K / 4][128], this thread's row).
+template <int K>
 __device__ __forceinline__ float row_bound(const float4* shown) {
-  float a[PARTS][K];
+  float a[4][K];
 #pragma unroll
-  for (int p = 0; p < PARTS; ++p)
+  for (int p = 0; p < 4; ++p)
 #pragma unroll
     for (int j = 0; j < K; j += 4) {
       float4 x;  // another warp may be writing it
       asm volatile("ld.volatile.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(smem_u32(shown + (p * (K / 4) + j / 4) * 128)));
       a[p][j] = x.x, a[p][j + 1] = x.y, a[p][j + 2] = x.z, a[p][j + 3] = x.w;
     }
-  if constexpr (PARTS == 4) {
-    merge_top<K>(a[0], a[1]);
-    merge_top<K>(a[2], a[3]);
-  }
+  merge_top<K>(a[0], a[1]);
+  merge_top<K>(a[2], a[3]);
   float least = INFINITY;
 #pragma unroll
-  for (int i = 0; i < K; ++i) least = fminf(least, fmaxf(a[0][i], a[PARTS / 2][K - 1 - i]));
+  for (int i = 0; i < K; ++i) least = fminf(least, fmaxf(a[0][i], a[2][K - 1 - i]));
   return least;
 }
 
@@ -459,14 +457,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float4 x = shown[(part * (K / 4) + j / 4) * 128];
             kept[j] = x.x, kept[j + 1] = x.y, kept[j + 2] = x.z, kept[j + 3] = x.w;
           }
-          enter<K, S::kCols / 8>(kept, groups);
+          enter<K>(kept, groups);
 #pragma unroll
           for (int j = 0; j < K; j += 4) shown[(part * (K / 4) + j / 4) * 128] = make_float4(kept[j], kept[j + 1], kept[j + 2], kept[j + 3]);
         }
         // in step on a row tile's first tile; later the others' lists may be a tile old, or half
         // of each: every entry only grows, so the bound, which serves the next tile, holds all the same
         if (opening) bar();
-        bound = fmaxf(bound, row_bound<K, S::kParts>(shown));
+        bound = fmaxf(bound, row_bound<K>(shown));
         gate = fmaxf(gate, bound);
         if (live && opening) {  // the first tile's logits again, now that there is a bound
 #pragma unroll
@@ -505,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int64_t at = (int64_t)row * a.segs + seg;
         if constexpr (K > 0) {
           bar();  // every part's last list is there
-          bound = row_bound<K, S::kParts>(shown);
+          bound = row_bound<K>(shown);
           cnt = make_room<K>(buf, cnt, bound, gate, 4 * K / S::kParts).cnt;
           bar();  // the lists have been read: the sums take their place
         }

@@ -26,13 +26,6 @@ struct AppendArgs {
   int64_t row[2], head[2];
 };
 
-// 16-bit float pattern (bf16 or fp16) to fp32
-template <bool BF16>
-__device__ __forceinline__ float wide(uint32_t u) {
-  if (BF16) return __uint_as_float(u << 16);
-  return __half2float(__ushort_as_half((unsigned short)u));
-}
-
 // Eight quotients x / s rounded to nearest even, as bytes (|x / s| below 127.5, s >
 // 2^-40).  r = x (1 / s) is off by less than 2^-15; adding 1.5 * 2^23 leaves its nearest
 // integer in the low bits.  Only a quotient that near to a half needs more: the exact side
@@ -125,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 8) k_kv8_append(const __grid_constan
 #pragma unroll
       for (int i = 0; i < T / 32; ++i) top = max(top, mine[i]);
     }
-    const float big = wide<BF16>(top);
+    const float big = wide16<BF16>(top);
     const bool fine = big <= kKv8Most;  // false for NaN and infinity
     const float s = fmaxf(big, kKv8Least) * (1.f / 127.f), inv = 1.f / s;
     if (id >= 0 && id < a.c.n_blocks) {
@@ -138,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, 8) k_kv8_append(const __grid_constan
         if (fine) {
           float v[8];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) v[2 * j] = wide<BF16>(w[j] & 0xffffu), v[2 * j + 1] = BF16 ? __uint_as_float(w[j] & 0xffff0000u) : wide<BF16>(w[j] >> 16);
+          for (int j = 0; j < 4; ++j) v[2 * j] = wide16<BF16>(w[j] & 0xffffu), v[2 * j + 1] = BF16 ? __uint_as_float(w[j] & 0xffff0000u) : wide16<BF16>(w[j] >> 16);
           y = round8(v, s, inv);
         }
         *reinterpret_cast<uint2*>(out + (size_t)(t + i * T) * 8) = y;

@@ -36,6 +36,13 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const tsd_kv8& c, const tsd_kv8_batch&
   return s;
 }
 
+// 16-bit float pattern (bf16 or fp16) to fp32
+template <bool BF16>
+__device__ __forceinline__ float wide16(uint32_t u) {
+  if (BF16) return __uint_as_float(u << 16);
+  return __half2float(__ushort_as_half((unsigned short)u));
+}
+
 // Checks shared by the entry points (before any device work).
 tsd_status kv8_check(const char* who, const tsd_kv8* c, const tsd_kv8_batch* b);
 tsd_status kv8_check_rows(const char* who, const char* what, const void* p, int64_t row, int64_t head);

@@ -27,12 +27,6 @@ __device__ __forceinline__ uint32_t int_half2(uint32_t x) {
 }
 
 template <bool BF16>
-__device__ __forceinline__ float wide16(uint32_t u) {
-  if (BF16) return __uint_as_float(u << 16);
-  return __half2float(__ushort_as_half((unsigned short)u));
-}
-
-template <bool BF16>
 __device__ __forceinline__ uint32_t narrow2(float a, float b) {
   if (BF16) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
