@@ -637,9 +637,11 @@ TSD_API tsd_status tsd_joint_label_scores(int32_t n, int32_t H, int32_t C, const
  * reciprocal), a the largest magnitude among its tokens, at least 2^-32;
  * q = x / scale, the exact quotient rounded to nearest even.  While a block is filling it is
  * rounded again from the unrounded tokens, so what a sequence's blocks hold does not depend
- * on how its tokens were split into calls.  A block and head with a NaN, an
- * infinity or a magnitude above 2^60 gets scale NaN: every query that sees
- * one of its tokens has a NaN result for the heads that read it. */
+ * on how its tokens were split into calls.  Tokens are taken back by lowering a length before
+ * the next append: to any multiple of block, and into a block b as long as no append since b's
+ * tokens were put there has reached block b + 2, whose originals take the place of b's.
+ * A block and head with a NaN, an infinity or a magnitude above 2^60 gets scale NaN: every
+ * query that sees one of its tokens has a NaN result for the heads that read it. */
 typedef struct {
   void *k, *v;
   float *k_scale, *v_scale;

@@ -839,7 +839,10 @@ class KV8Cache:
     sequences; None: slots 0 .. n-1) and starts int32 [n + 1] (their rows; None:
     one row each).  max_new and max_len bound a sequence's rows and tokens; they
     size launches only.  Everything is read on the device, so a call captured
-    into a graph can be replayed with other lengths, tables and rows."""
+    into a graph can be replayed with other lengths, tables and rows.
+
+    Tokens are taken back by lowering a length: to a multiple of block, or into
+    a block b while no append since its tokens' has reached block b + 2."""
 
     def __init__(self, k, v, k_scale, v_scale, k_tail, v_tail):
         import torch

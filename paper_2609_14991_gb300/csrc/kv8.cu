@@ -6,7 +6,7 @@
 // copies of its tokens (the tail) and the new ones: what the cache holds then
 // does not depend on the calls' splits, and the attention kernels read one
 // format.  Two blocks of originals per slot cost 2 x block tokens of 16 bits
-// per head and let a caller take back up to a block of tokens.
+// per head and let a caller take tokens back into the block before the last.
 #include <climits>
 
 #include "kv8.h"

@@ -132,6 +132,18 @@ def test_appending_again_from_an_earlier_length():
         b.check_held()
 
 
+def test_taking_back_again_and_again():
+    """Within the last two blocks reached, to multiples of the block further back, and on from there."""
+    b = Batch(tsd, [90], 1, 16, 64, seed=8)
+    s = b.slots[0]
+    b.append([50])  # block 3
+    for to, new in ((40, 3), (33, 1), (34, 13), (45, 30), (64, 2), (50, 9), (32, 1), (33, 20), (16, 5), (21, 30), (0, 3), (2, 40)):
+        b.len[0] = to
+        b.model.k[s], b.model.v[s] = b.model.k[s][:to], b.model.v[s][:to]
+        b.append([new])
+        b.check_held()
+
+
 def test_reads_a_part_and_leaves_rows_behind():
     b = Batch(tsd, [90, 20, 0], 2, 16, 128, seed=8)
     b.append([90, 20, 0])

@@ -26,6 +26,8 @@ def check(b, counts, heads, window, sinks, q, scale=None, **kw):
     out = b.cache.attend(q, **b.args(counts), window=window, sinks=sinks, scale=scale, **kw).double()
     g, at = heads // b.heads, 0
     for i, c in enumerate(counts):
+        if not c:
+            continue
         L = b.len[i]
         k, v = (b.model.held(x, b.slots[i]).cuda() for x in "kv")
         key, pos = torch.arange(L, device="cuda"), torch.arange(L - c, L, device="cuda")[:, None]
