@@ -698,7 +698,8 @@ TSD_API tsd_status tsd_kv8_read(const tsd_kv8* cache, const tsd_kv8_batch* batch
  * strides in elements, a multiple of 8, 16-byte aligned; out may not overlap q.
  * Products take fp16 operands (queries scaled by a power of two per row, the
  * 8-bit integers as they are, probabilities rounded to fp16) and accumulate in
- * fp32, as do the softmax's statistics.  workspace: device memory of at least
+ * fp32, as do the softmax's statistics.  What is rounded is a probability times its value's
+ * scale: to 11 bits down to 2^-21 of the row's largest, below that to multiples of 2^-31 of it.  workspace: device memory of at least
  * tsd_kv8_attend_workspace() bytes (may be 0), 16-byte aligned, for this call alone. */
 TSD_API tsd_status tsd_kv8_attend_workspace(const tsd_kv8* cache, const tsd_kv8_batch* batch, int32_t heads,
                                             int32_t window, int32_t sinks, int64_t* bytes);

@@ -67,8 +67,9 @@ __device__ __forceinline__ uint2 round8(const float (&x)[8], float s, float inv)
 // (32 in the smallest blocks), so a unit is a warp, two or four, and CTAs of 128 threads hold 4, 2 or 1.  A
 // thread holds its elements as packed 16-bit vectors: one read, the largest
 // magnitude from the patterns (they order as integers without the sign, NaN
-// and infinity above every number), one write.  Bound by memory: 2 bytes in, 1 out
-// per element.
+// and infinity above every number), one write.  Bound by the rounding's instructions in
+// prompts (66% of issue slots; 6 ragged ones of 4000, 8 heads of 128: 26.5 us, where 2 bytes in and 1 out
+// per element take 15), by its dependent loads in single tokens (256: 10 us).
 template <bool BF16, int BLOCK, int DIM>
 __global__ void __launch_bounds__(kThreads, 8) k_kv8_append(const __grid_constant__ AppendArgs a) {
   constexpr int T = BLOCK * DIM / 64 < 32 ? 32 : BLOCK * DIM / 64;  // threads per unit
@@ -167,7 +168,7 @@ __device__ __forceinline__ int seq_of(const tsd_kv8_batch& b, int r, int lane) {
 }
 
 // One warp per row: its keys or its values, all heads.  Bound by the writes (4 bytes an
-// element): 106 MB of them and 26 read, 31 us.  All keys, then all values, written past the caches, with two loads
+// element): 134 MB of them and 34 read, 31 us.  All keys, then all values, written past the caches, with two loads
 // ahead: both by one warp 33.6, without the hint 34.4, with eight loads ahead 53.
 template <int DIM>
 __global__ void __launch_bounds__(256) k_kv8_read(const __grid_constant__ tsd_kv8 c, const __grid_constant__ tsd_kv8_batch b,

@@ -18,8 +18,9 @@
 //   out = sum_j 2^(s_j - m) v_j  /  sum_j 2^(s_j - m) / c_b,
 // so a value's scale is an addend of the exponent and the integers go into the
 // products as they are (exact in fp16, as is every query within 2^28 of its
-// row's largest).  Probabilities are rounded to fp16 (half a step 2^-11), as
-// multiples of 2^(m - 7): down to 2^-31 of the largest they are not flushed.  The maximum
+// row's largest).  The weights 2^(s_j - m), with their value's scale in them, are rounded to fp16
+// (half a step 2^-11) as multiples of 2^(m - 7): below 2^-21 of the largest to multiples of 2^-31
+// of it, so a block whose values are 2^21 times smaller than another's counts more coarsely.  The maximum
 // follows only when a score passes it by more than 2^8, which fp16 still holds:
 // most tiles need no exchange between lanes.
 //
@@ -222,6 +223,8 @@ __global__ void __launch_bounds__(128) k_kv8_rows(const __grid_constant__ Kv8Att
           a_b = id >= 0 ? __ldg(a.c.k_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float c = id >= 0 ? __ldg(a.c.v_scale + (size_t)id * a.c.kv_heads + head) : nan;
           const float cs = c == 0.f ? 0x1p-80f : c;  // a scale of 0 stands for values of 0, of their weight all the same
+          // (approximate: 2^-22 of the logarithm is 2^-17 at a scale of 2^-32, where a weight in fp16 rounds by
+          // 2^-11; 2^-23 of the reciprocal)
           lc_b = lg2_approx(cs);
           ic_b = rcp_approx(cs);
         }

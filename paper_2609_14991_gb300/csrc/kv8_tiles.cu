@@ -1,7 +1,7 @@
 // Attention over the 8-bit paged cache with many query rows per key head:
 // prompts (tsd.h: tsd_kv8_attend).
 //
-// The mathematics is kv8_rows.cu's; the products run on tcgen05 (fp16 in, fp32
+// The mathematics is kv8_rows.cu's, but for when the maximum follows (below); the products run on tcgen05 (fp16 in, fp32
 // accumulate in TMEM).  A CTA takes 256 rows of a sequence and key head (row =
 // token * group + head of the group) as two tiles of 128, and the keys they see in
 // tiles of 128, 64 at a time:
