@@ -708,6 +708,74 @@ TSD_API tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* bat
                                   int64_t out_row, int64_t out_head, void* workspace, int64_t workspace_bytes,
                                   void* cuda_stream);
 
+/* ------------------------------------------------------------------------
+ * A decoder layer around that cache (an attention decoder or a neural LM;
+ * the paper has no counterpart): rotary positions of queries and keys.  All pointers are
+ * device memory unless said otherwise; calls are asynchronous on
+ * cuda_stream, allocate nothing and can be captured into a graph: lengths,
+ * positions and rows are read on the device. */
+
+/* Rotary positions.  Pair i of the first `rot` dimensions of a head at position p, (a, b),
+ * becomes  magnitude * (a cos(p f_i) - b sin(p f_i), b cos(p f_i) + a sin(p f_i));
+ * the other dimensions stay as they are.  Pairs are (i, i + rot / 2), or neighbours
+ * (2i, 2i + 1) if interleaved.  With g_i = base^(-2i / rot) the frequencies are
+ *   PLAIN   f_i = g_i                        (factor, original, low, high not used)
+ *   LINEAR  f_i = g_i / factor
+ *   BASE    g_i of the base  base * factor^(rot / (rot - 2))  (rot 2: base)
+ *   RAMP    f_i = c_i g_i + (1 - c_i) g_i / factor, c_i = the turns that g_i makes
+ *           in `original` positions, mapped from [low, high] to [0, 1] and clamped. */
+#define TSD_ROTARY_PLAIN 0
+#define TSD_ROTARY_LINEAR 1
+#define TSD_ROTARY_BASE 2
+#define TSD_ROTARY_RAMP 3
+typedef struct {
+  int32_t rot;      /* turned dimensions: even, 2..1024 */
+  int32_t scaling;  /* one of the above */
+  double base, factor, original, low, high;
+} tsd_rotary_cfg;
+
+/* Host only, no device work: the rot / 2 frequencies as 64-bit fractions of a turn per
+ * position, frac(f_i / (2 pi)) * 2^64, into host memory.  An angle is a product
+ * of the position and one of them, exact mod 2^64, so far positions lose nothing.  TSD_EINVAL: sizes and
+ * values out of range, a frequency above 2^52. */
+TSD_API tsd_status tsd_rotary_turns(const tsd_rotary_cfg* cfg, uint64_t* turns);
+
+typedef struct {
+  const uint64_t* turns; /* device [rot / 2]: tsd_rotary_turns's */
+  int32_t dim, rot;      /* head dimension 2..1024; turned ones, even, at most dim */
+  int32_t interleaved;
+  int32_t dtype;         /* TSD_F32, TSD_BF16 or TSD_F16; angles and products are fp32, rounded once */
+  float magnitude;
+} tsd_rotary;
+
+/* The rows' positions: positions[r], any 32-bit integer (a negative one turns back), or (positions
+ * NULL) those of a cache's call (tsd_kv8_batch): sequence i of n in slot slots[i] (NULL: i) holds
+ * lens[slot] tokens, and rows starts[i] .. starts[i+1] (NULL: one row each) are its last ones.
+ * Rows behind the last sequence's are not read or written; rows of a sequence whose
+ * slot, length or rows are out of range become NaN. */
+typedef struct {
+  int32_t rows;             /* 1..2^22 */
+  const int32_t* positions; /* [rows] or NULL */
+  int32_t n;                /* 1..65535 */
+  const int32_t* slots;     /* [n] or NULL */
+  const int32_t* lens;      /* [n_slots] */
+  const int32_t* starts;    /* [n + 1] or NULL */
+  int32_t n_slots;
+} tsd_rotary_rows;
+
+/* Queries or keys: rows x heads x dim, strides in elements (any alignment of the element
+ * type; at multiples of 16 bytes accesses are wide).  out may be x with the same strides; else they do not overlap. */
+typedef struct {
+  const void* x;
+  void* out;
+  int64_t row, head, out_row, out_head;
+  int32_t heads; /* 1..1024 */
+} tsd_rotary_heads;
+
+/* Turns queries and (k not NULL) keys in one launch. */
+TSD_API tsd_status tsd_rotary_apply(const tsd_rotary* rotary, const tsd_rotary_rows* rows, const tsd_rotary_heads* q,
+                                    const tsd_rotary_heads* k, void* cuda_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -73,6 +73,24 @@ class KV8BatchC(ctypes.Structure):
                 ("rows", _i32), ("max_new", _i32), ("max_len", _i32)]
 
 
+class RotaryCfgC(ctypes.Structure):
+    _fields_ = [("rot", _i32), ("scaling", _i32)] + [(n, ctypes.c_double) for n in ("base", "factor", "original", "low", "high")]
+
+
+class RotaryC(ctypes.Structure):
+    _fields_ = [("turns", _vp), ("dim", _i32), ("rot", _i32), ("interleaved", _i32), ("dtype", _i32), ("magnitude", _f32)]
+
+
+class RotaryRowsC(ctypes.Structure):
+    _fields_ = [("rows", _i32), ("positions", _vp), ("n", _i32), ("slots", _vp), ("lens", _vp), ("starts", _vp),
+                ("n_slots", _i32)]
+
+
+class RotaryHeadsC(ctypes.Structure):
+    _fields_ = [("x", _vp), ("out", _vp), ("row", _i64), ("head", _i64), ("out_row", _i64), ("out_head", _i64),
+                ("heads", _i32)]
+
+
 SIGNATURES = {
     "tsd_last_error": ([], ctypes.c_char_p),
     "tsd_version": ([], ctypes.c_char_p),
@@ -134,6 +152,8 @@ SIGNATURES = {
     "tsd_kv8_attend_workspace": ([_P(KV8C), _P(KV8BatchC), _i32, _i32, _i32, _P(_i64)], _i32),
     "tsd_kv8_attend": ([_P(KV8C), _P(KV8BatchC), _i32, _vp, _i64, _i64, _f32, _i32, _i32, _vp, _i64, _i64, _vp, _i64,
                         _vp], _i32),
+    "tsd_rotary_turns": ([_P(RotaryCfgC), _vp], _i32),
+    "tsd_rotary_apply": ([_P(RotaryC), _P(RotaryRowsC), _P(RotaryHeadsC), _P(RotaryHeadsC), _vp], _i32),
 }
 
 _lib = None
@@ -998,3 +1018,111 @@ class KV8Cache:
         if st:
             _check(st)
         return out
+
+
+# ---------------------------------------------------------------- a decoder layer around the cache
+
+_SCALINGS = {None: 0, "linear": 1, "base": 2, "ramp": 3}
+
+
+class Rotary:
+    """Rotary positions of heads of `dim` (``tsd_rotary_apply``): the first `rot`
+    dimensions (None: all) are turned in pairs (i, i + rot / 2) (layout "half") or of
+    neighbours ("interleaved") by position * base^(-2i / rot).  scaling stretches the
+    positions by `factor`: "linear" (every frequency divided), "base" (a larger base),
+    "ramp" (divided where a pair makes `low` turns or fewer in `original` positions,
+    kept from `high` on, linearly between).  Results are times `magnitude`.
+
+    The handle holds the frequencies on the device (current one if None)."""
+
+    def __init__(self, dim: int, rot: Optional[int] = None, layout: str = "half", base: float = 10000.0,
+                 scaling: Optional[str] = None, factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                 high: float = 32.0, magnitude: float = 1.0, device=None):
+        import torch
+
+        rot = dim if rot is None else rot
+        if not 2 <= dim <= 1024 or not 2 <= rot <= dim or rot % 2:
+            raise ValueError("Rotary: 2 <= rot <= dim <= 1024, rot even")
+        if layout not in ("half", "interleaved"):
+            raise ValueError("Rotary: layout is 'half' or 'interleaved'")
+        if scaling not in _SCALINGS:
+            raise ValueError("Rotary: scaling is None, 'linear', 'base' or 'ramp'")
+        turns = np.zeros(rot // 2, dtype=np.uint64)
+        cfg = RotaryCfgC(rot, _SCALINGS[scaling], base, factor, original, low, high)
+        _check(lib().tsd_rotary_turns(ctypes.byref(cfg), turns.ctypes.data))
+        device = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
+        self.dim, self.rot, self.layout, self.magnitude = dim, rot, layout, magnitude
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
+        self._dev = self.turns.get_device()
+        self._c = [ctypes.byref(RotaryC(self.turns.data_ptr(), dim, rot, layout == "interleaved", code, magnitude))
+                   for code in range(3)]  # by element type
+
+    def _heads(self, name, t, out, rows, dtype, stream):
+        """(result, tsd_rotary_heads) of queries or keys [rows, heads, dim]."""
+        s, d = t.shape, t.stride()
+        if len(s) != 3 or s[0] != rows or s[2] != self.dim or t.dtype != dtype:
+            raise ValueError(f"Rotary: {name} must be {dtype} [{rows}, heads, {self.dim}]")
+        if t.get_device() != self._dev:
+            raise ValueError(f"Rotary: {name} must be on the handle's device")
+        if out is None:
+            out = _empty(s, dtype, self._dev, stream)
+            o = (s[1] * s[2], s[2], 1)
+        else:
+            o = out.stride()
+            if out.shape != s or out.dtype != dtype or out.get_device() != self._dev:
+                raise ValueError(f"Rotary: the result of {name} must be {dtype} {list(s)} on the handle's device")
+        if d[2] != 1 or o[2] != 1:
+            raise ValueError(f"Rotary: {name}'s last dimension must be adjacent")
+        return out, RotaryHeadsC(t.data_ptr(), out.data_ptr(), d[0], d[1], o[0], o[1], s[1])
+
+    def __call__(self, q, k=None, positions=None, lens=None, starts=None, slots=None, out=None, stream=None):
+        """q [rows, heads, dim] and k [rows, kv heads, dim] (float32, bfloat16 or
+        float16) turned: their results, or q's alone if k is None.  positions: int32
+        [rows]; or a cache's lens, starts and slots as KV8Cache's calls take them (the rows are
+        their sequences' last tokens).  out: tensors for the results (a pair, or q's); q and k
+        themselves turn in place."""
+        import torch
+
+        rows, dtype, i32, dev = q.shape[0], q.dtype, torch.int32, self._dev
+        code = _dtype_code(q)
+        if code < 0:
+            raise ValueError("Rotary: q must be float32, bfloat16 or float16")
+        if torch.cuda.current_device() != dev:
+            raise ValueError("Rotary: the handle is on another device than the current one")
+        if not 1 <= rows <= 1 << 22:
+            raise ValueError("Rotary: 1 to 2^22 rows")
+        if (positions is None) == (lens is None) or (positions is not None and (starts is not None or slots is not None)):
+            raise ValueError("Rotary: positions, or lens with starts and slots")
+        n, n_slots, ptr = rows, 0, [None] * 4
+        for j, (name, t) in enumerate((("positions", positions), ("slots", slots), ("lens", lens), ("starts", starts))):
+            if t is None:
+                continue
+            if t.dtype != i32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != dev:
+                raise ValueError(f"Rotary: {name} must be contiguous int32 on the handle's device")
+            ptr[j] = t.data_ptr()
+        if positions is not None:
+            if positions.shape[0] != rows:
+                raise ValueError(f"Rotary: positions must have {rows} entries")
+        else:
+            n_slots = lens.shape[0]
+            if slots is not None:
+                n = slots.shape[0]
+            if starts is not None:
+                if starts.shape[0] < 2 or (slots is not None and starts.shape[0] != n + 1):
+                    raise ValueError("Rotary: starts must have n + 1 entries")
+                n = starts.shape[0] - 1
+            elif n != rows:
+                raise ValueError("Rotary: without starts there is one row per sequence")
+            if not 1 <= n <= 65535:
+                raise ValueError("Rotary: at most 65535 sequences")
+        oq, ok = (out, None) if k is None or out is None else out
+        oq, hq = self._heads("q", q, oq, rows, dtype, stream)
+        hk = None
+        if k is not None:
+            ok, hk = self._heads("k", k, ok, rows, dtype, stream)
+            hk = ctypes.byref(hk)
+        r = RotaryRowsC(rows, ptr[0], n, ptr[1], ptr[2], ptr[3], n_slots)
+        st = lib().tsd_rotary_apply(self._c[code], ctypes.byref(r), ctypes.byref(hq), hk, _raw_stream(stream, dev))
+        if st:
+            _check(st)
+        return oq if k is None else (oq, ok)

@@ -11,6 +11,7 @@
 
 #include "kv8.h"
 #include "kv8_keys.h"
+#include "seq.h"
 #include "tc_common.cuh"
 
 namespace tsd {
@@ -152,21 +153,6 @@ __global__ void __launch_bounds__(kThreads, 8) k_kv8_append(const __grid_constan
   }
 }
 
-// The sequence that holds a warp's row r: the last i with starts[i] <= r; -1: none.  Each
-// round takes 32 probes at once.
-__device__ __forceinline__ int seq_of(const tsd_kv8_batch& b, int r, int lane) {
-  if (!b.starts) return r < b.n ? r : -1;
-  int lo = 0, hi = b.n + 1;  // starts[lo] <= r < starts[hi], where both hold
-  do {
-    const int step = (hi - lo + 31) / 32, at = lo + step * lane;
-    const unsigned below = __ballot_sync(0xffffffffu, at < hi && __ldg(b.starts + at) <= r);
-    if (!below) return -1;
-    lo += step * (31 - __clz(below));
-    hi = min(lo + step, hi);
-  } while (hi - lo > 1);
-  return lo < b.n ? lo : -1;
-}
-
 // One warp per row: its keys or its values, all heads.  Bound by the writes (4 bytes an
 // element): 134 MB of them and 34 read, 31 us.  All keys, then all values, written past the caches, with two loads
 // ahead: both by one warp 33.6, without the hint 34.4, with eight loads ahead 53.
@@ -175,7 +161,7 @@ __global__ void __launch_bounds__(256) k_kv8_read(const __grid_constant__ tsd_kv
                                                   float* k_out, float* v_out) {
   const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (r >= b.rows) return;
-  const int i = seq_of(b, r, lane);
+  const int i = seq_of(b.starts, b.n, r, lane);
   if (i < 0) return;  // behind the last sequence
   const Kv8Seq q = kv8_seq(c, b, i);
   if (r < q.row0 || r >= q.row0 + q.count) return;

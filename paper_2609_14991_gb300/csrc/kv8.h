@@ -2,9 +2,7 @@
 // append, read and attention kernels.
 #pragma once
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
+#include "elem.cuh"
 #include "internal.h"
 
 namespace tsd {
@@ -34,13 +32,6 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const tsd_kv8& c, const tsd_kv8_batch&
   s.row0 = r0;
   s.count = r1 - r0;
   return s;
-}
-
-// 16-bit float pattern (bf16 or fp16) to fp32
-template <bool BF16>
-__device__ __forceinline__ float wide16(uint32_t u) {
-  if (BF16) return __uint_as_float(u << 16);
-  return __half2float(__ushort_as_half((unsigned short)u));
 }
 
 // Checks shared by the entry points (before any device work).

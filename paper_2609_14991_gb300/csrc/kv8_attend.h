@@ -26,16 +26,6 @@ __device__ __forceinline__ uint32_t int_half2(uint32_t x) {
   return r;
 }
 
-template <bool BF16>
-__device__ __forceinline__ uint32_t narrow2(float a, float b) {
-  if (BF16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&v);
-  }
-  const __half2 v = __floats2half2_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
-}
-
 __device__ __forceinline__ float lg2_approx(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -1,0 +1,115 @@
+"""Rotary positions refuse bad
+arguments before any device work, and the host's frequencies are the formula's (no GPU)."""
+import ctypes
+import math
+from decimal import Decimal, getcontext
+
+import numpy as np
+import pytest
+
+import paper_2609_14991_gb300 as tsd
+from paper_2609_14991_gb300 import _build
+
+torch = pytest.importorskip("torch")
+P = 256  # a non-NULL, aligned address; never dereferenced
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+
+
+@pytest.fixture(scope="module")
+def L():
+    _build.build()
+    return tsd.lib()
+
+
+def refused(L, st, word):
+    assert st == tsd.TSD_EINVAL
+    msg = L.tsd_last_error().decode()
+    assert word in msg, msg
+
+
+def cfg(rot=64, scaling=0, base=10000.0, factor=8.0, original=4096.0, low=1.0, high=32.0):
+    return tsd.RotaryCfgC(rot, scaling, base, factor, original, low, high)
+
+
+def turns_of(L, c):
+    t = np.zeros(c.rot // 2, dtype=np.uint64)
+    assert L.tsd_rotary_turns(ctypes.byref(c), t.ctypes.data) == 0, L.tsd_last_error()
+    return t
+
+
+def frequency(c, i):
+    half = c.rot // 2
+    base = c.base * (c.factor ** (half / (half - 1)) if c.scaling == 2 and half > 1 else 1)
+    f = base ** (-i / half)
+    if c.scaling == 1:
+        f /= c.factor
+    if c.scaling == 3:
+        keep = min(1.0, max(0.0, (c.original * f / (2 * math.pi) - c.low) / (c.high - c.low)))
+        f = f * keep + f / c.factor * (1 - keep)
+    return f
+
+
+@pytest.mark.parametrize("rot", [2, 4, 64, 128, 1024])
+@pytest.mark.parametrize("scaling", [0, 1, 2, 3])
+@pytest.mark.parametrize("base", [10000.0, 500000.0, 0.5])
+def test_turns(L, rot, scaling, base):
+    """Fractions of a turn, mod 2^64: the power is good to a few units of 2^-53 of itself (2^-49 is
+    allowed), the rest to two units."""
+    getcontext().prec = 60
+    c = cfg(rot, scaling, base)
+    for i, t in enumerate(turns_of(L, c)):
+        f = frequency(c, i)
+        want = (Decimal(f) / (2 * PI)) * 2 ** 64 % 2 ** 64
+        off = abs((Decimal(int(t)) - want + 2 ** 63) % 2 ** 64 - 2 ** 63)
+        assert off <= Decimal(f) / 6 * 2 ** 15 + 2, (i, f, off)
+
+
+def test_turns_refusals(L):
+    t = np.zeros(512, dtype=np.uint64)
+    for kw, word in [(dict(rot=0), "rot=0"), (dict(rot=3), "rot=3"), (dict(rot=1026), "rot=1026"), (dict(base=0.0), "base"),
+                     (dict(base=-1.0), "base"), (dict(base=math.inf), "base"), (dict(base=math.nan), "base"), (dict(scaling=4), "scaling"),
+                     (dict(scaling=-1), "scaling"), (dict(scaling=1, factor=0.0), "factor"), (dict(scaling=2, factor=math.inf), "factor"),
+                     (dict(scaling=3, original=0.0), "ramp"), (dict(scaling=3, low=2.0, high=2.0), "ramp"),
+                     (dict(scaling=3, high=math.nan), "ramp"), (dict(base=1e-300), "2^52"), (dict(scaling=1, factor=1e-300), "2^52")]:
+        refused(L, L.tsd_rotary_turns(ctypes.byref(cfg(**kw)), t.ctypes.data), word)
+    refused(L, L.tsd_rotary_turns(None, t.ctypes.data), "NULL")
+    refused(L, L.tsd_rotary_turns(ctypes.byref(cfg()), None), "NULL")
+
+
+def test_rotary_refusals(L):
+    def call(rot=(), rows=(), q=(), k=(), with_k=True):
+        r = dict(turns=P, dim=64, rot=64, interleaved=0, dtype=1, magnitude=1.0)
+        w = dict(rows=3, positions=None, n=2, slots=P, lens=P, starts=P, n_slots=4)
+        h = dict(x=P, out=P, row=512, head=64, out_row=512, out_head=64, heads=8)
+        h2 = {**h, "x": 2 * P, "out": 2 * P}
+        a, b = tsd.RotaryC(*{**r, **dict(rot)}.values()), tsd.RotaryRowsC(*{**w, **dict(rows)}.values())
+        c, d = tsd.RotaryHeadsC(*{**h, **dict(q)}.values()), tsd.RotaryHeadsC(*{**h2, **dict(k)}.values())
+        return L.tsd_rotary_apply(ctypes.byref(a), ctypes.byref(b), ctypes.byref(c), ctypes.byref(d) if with_k else None, None)
+
+    for kw, word in [(dict(turns=None), "turns"), (dict(turns=P + 4), "turns"), (dict(dim=1), "dim=1"), (dict(dim=1026), "dim=1026"),
+                     (dict(rot=66), "rot=66"), (dict(rot=0), "rot=0"), (dict(rot=7), "rot=7"), (dict(dtype=3), "dtype"),
+                     (dict(magnitude=math.inf), "magnitude"), (dict(magnitude=math.nan), "magnitude")]:
+        refused(L, call(rot=kw.items()), word)
+    for kw, word in [(dict(rows=0), "rows=0"), (dict(rows=(1 << 22) + 1), "rows="), (dict(positions=P), "positions, or"),
+                     (dict(lens=None), "NULL positions"), (dict(n=0), "n=0"), (dict(n=65536), "n=65536"), (dict(n_slots=0), "n_slots=0"),
+                     (dict(starts=None), "starts is NULL")]:
+        refused(L, call(rows=kw.items()), word)
+    for kw, word in [(dict(x=None), "NULL"), (dict(out=None), "NULL"), (dict(heads=0), "heads=0"), (dict(heads=1025), "heads=1025"),
+                     (dict(x=P + 1), "aligned"), (dict(row=-1), "strides"), (dict(out_head=1 << 41), "strides"),
+                     (dict(out_row=63), "overlap"), (dict(out_head=0), "overlap"), (dict(row=1024), "in place"), (dict(head=72), "in place")]:
+        refused(L, call(q=kw.items()), word)
+        refused(L, call(k=kw.items()), word)
+    refused(L, call(q=dict(out=2 * P).items()), "queries and keys overlap")
+    refused(L, call(k=dict(out=P).items()), "queries and keys overlap")
+    refused(L, L.tsd_rotary_apply(None, None, None, None, None), "NULL")
+
+
+def test_bindings_refuse():
+    with pytest.raises(ValueError, match="rot"):
+        tsd.Rotary(64, 66, device="cpu")
+    with pytest.raises(ValueError, match="layout"):
+        tsd.Rotary(64, layout="other", device="cpu")
+    with pytest.raises(ValueError, match="scaling"):
+        tsd.Rotary(64, scaling="other", device="cpu")
+    with pytest.raises(tsd.TsdError, match="factor"):
+        tsd.Rotary(64, scaling="linear", factor=0.0, device="cpu")
