@@ -710,7 +710,8 @@ TSD_API tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* bat
 
 /* ------------------------------------------------------------------------
  * A decoder layer around that cache (an attention decoder or a neural LM;
- * the paper has no counterpart): rotary positions of queries and keys.  All pointers are
+ * the paper has no counterpart): rotary positions of queries and keys, norms
+ * around a block.  All pointers are
  * device memory unless said otherwise; calls are asynchronous on
  * cuda_stream, allocate nothing and can be captured into a graph: lengths,
  * positions and rows are read on the device. */
@@ -775,6 +776,33 @@ typedef struct {
 /* Turns queries and (k not NULL) keys in one launch. */
 TSD_API tsd_status tsd_rotary_apply(const tsd_rotary* rotary, const tsd_rotary_rows* rows, const tsd_rotary_heads* q,
                                     const tsd_rotary_heads* k, void* cuda_stream);
+
+/* Norms around a block: of n rows of d elements
+ *   r = x + scale * gate (.) post(y),   h = norm(r)
+ * with  RMS    v / sqrt(mean(v^2) + eps) * weight + bias
+ *       LAYER  (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) * weight + bias. */
+#define TSD_NORM_NONE 0
+#define TSD_NORM_RMS 1
+#define TSD_NORM_LAYER 2
+typedef struct {
+  int32_t kind;
+  float eps;                  /* finite, 0 or more */
+  const float *weight, *bias; /* [d] each; NULL: 1 and 0 */
+} tsd_norm;
+
+/*   x, r     the residual stream before and after, of type x_dtype: dtype's or TSD_F32;
+ *   y        the block's output, of type dtype (TSD_F32, TSD_BF16 or TSD_F16); NULL: none, then
+ *            r is not written and h = norm(x), with no gate and no post;
+ *   gate     of type dtype, NULL: 1; gate_row 0: one row for all;
+ *   post, norm  NULL or kind NONE: post(y) = y, and h is not written.
+ * Row strides in elements, at least d; any alignment of the element types (sixteen-byte accesses
+ * where pointers are 16-byte aligned and d and strides multiples of 8).  r may be x, and h may be y
+ * (without y: x), with the same strides; other overlaps are not allowed.  Everything between is fp32 and rounded once: h comes of
+ * the unrounded r.  1 <= n <= 2^27, 1 <= d <= 16384.  A row's results are the same bits whatever else is in the call. */
+TSD_API tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int32_t x_dtype, int64_t x_row, const void* y,
+                                     int32_t dtype, int64_t y_row, const tsd_norm* post, const void* gate,
+                                     int64_t gate_row, float scale, const tsd_norm* norm, void* r, int64_t r_row,
+                                     void* h, int64_t h_row, void* cuda_stream);
 
 #ifdef __cplusplus
 }

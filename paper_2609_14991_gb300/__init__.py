@@ -91,6 +91,10 @@ class RotaryHeadsC(ctypes.Structure):
                 ("heads", _i32)]
 
 
+class NormC(ctypes.Structure):
+    _fields_ = [("kind", _i32), ("eps", _f32), ("weight", _vp), ("bias", _vp)]
+
+
 SIGNATURES = {
     "tsd_last_error": ([], ctypes.c_char_p),
     "tsd_version": ([], ctypes.c_char_p),
@@ -154,6 +158,8 @@ SIGNATURES = {
                         _vp], _i32),
     "tsd_rotary_turns": ([_P(RotaryCfgC), _vp], _i32),
     "tsd_rotary_apply": ([_P(RotaryC), _P(RotaryRowsC), _P(RotaryHeadsC), _P(RotaryHeadsC), _vp], _i32),
+    "tsd_residual_norm": ([_i32, _i32, _vp, _i32, _i64, _vp, _i32, _i64, _P(NormC), _vp, _i64, _f32, _P(NormC), _vp, _i64,
+                           _vp, _i64, _vp], _i32),
 }
 
 _lib = None
@@ -1126,3 +1132,93 @@ class Rotary:
         if st:
             _check(st)
         return oq if k is None else (oq, ok)
+
+
+_NORMS = {None: 0, "rms": 1, "layer": 2}
+
+
+def _norm_arg(who, what, kind, weight, bias, d, eps, dev):
+    import torch
+
+    if kind is None:
+        if weight is not None or bias is not None:
+            raise ValueError(f"{who}: {what} is None, but has a weight or a bias")
+        return None
+    ptr = []
+    for t in (weight, bias):
+        if t is not None and (t.dtype != torch.float32 or t.shape != (d,) or not t.is_contiguous() or t.get_device() != dev):
+            raise ValueError(f"{who}: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
+        ptr.append(t.data_ptr() if t is not None else None)
+    return ctypes.byref(NormC(_NORMS[kind], eps, ptr[0], ptr[1]))
+
+
+def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None, post: Optional[str] = None,
+                  post_weight=None, post_bias=None, gate=None, scale: float = 1.0, eps: float = 1e-5, out=None,
+                  stream=None):
+    """(h, r): r = x + scale * gate * post(y), a block's output y normed, gated and
+    added to the residual stream x, and h = norm(r), the next block's input
+    (``tsd_residual_norm``).  norm and post: "rms", "layer" or None (no h; y as it is).
+    x, y: cuda [n, d], any row stride; y float32, bfloat16 or float16, x the same or
+    float32.  gate: y's type, [d] or [n, d].  Weights and biases: float32 [d].  y None:
+    h = norm(x) of x's type, and r is x.  out: (h, r) to write; r may be x and h may be y."""
+    import torch
+
+    who = "residual_norm"
+    shape = x.shape
+    if len(shape) != 2 or not (1 <= shape[0] <= 1 << 27 and 1 <= shape[1] <= 16384):
+        raise ValueError(f"{who}: x must be [n, d] with 1 <= n <= 2^27 and 1 <= d <= 16384")
+    if norm not in _NORMS or post not in _NORMS:
+        raise ValueError(f"{who}: norms are 'rms', 'layer' or None")
+    n, d = shape
+    x_code = _dtype_code(x)
+    src = x if y is None else y
+    code, dtype = (x_code, x.dtype) if y is None else (_dtype_code(y), y.dtype)
+    if code < 0 or (x_code != code and x_code != 0):
+        raise ValueError(f"{who}: y must be float32, bfloat16 or float16 and x of the same type or float32")
+    dev = _on_current(who, "x", x)
+    xr = _row_stride(who, "x", x, shape)
+    yp, yr, gp, gr = None, 0, None, 0
+    if y is not None:
+        if y.shape != shape or y.get_device() != dev:
+            raise ValueError(f"{who}: y must be {list(shape)} on x's device")
+        yp, yr = y.data_ptr(), _row_stride(who, "y", y, shape)
+        if gate is not None:
+            if gate.dtype != dtype or gate.get_device() != dev or (gate.shape != (d,) and gate.shape != shape):
+                raise ValueError(f"{who}: gate must be {dtype} [{d}] or {list(shape)} on x's device")
+            if gate.dim() == 1:
+                if gate.stride(0) != 1 and d > 1:
+                    raise ValueError(f"{who}: gate must be adjacent")
+            else:
+                gr = _row_stride(who, "gate", gate, shape)
+            gp = gate.data_ptr()
+    elif gate is not None or post is not None or norm is None:
+        raise ValueError(f"{who}: without y there is a norm, and no gate or post")
+    pn = _norm_arg(who, "norm", norm, weight, bias, d, eps, dev)
+    pp = _norm_arg(who, "post", post, post_weight, post_bias, d, eps, dev)
+    h = r = None
+    if out is not None:
+        h, r = out
+    hp, hr, rp, rr = None, 0, None, 0
+    if norm is not None:
+        if h is None:
+            h, hr = _empty(shape, dtype, dev, stream), d
+        else:
+            if h.shape != shape or h.dtype != dtype or h.get_device() != dev:
+                raise ValueError(f"{who}: out's h must be {dtype} {list(shape)} on x's device")
+            hr = _row_stride(who, "out's h", h, shape)
+        hp = h.data_ptr()
+    if y is None:
+        r = x
+    else:
+        if r is None:
+            r, rr = _empty(shape, x.dtype, dev, stream), d
+        else:
+            if r.shape != shape or r.dtype != x.dtype or r.get_device() != dev:
+                raise ValueError(f"{who}: out's r must be {x.dtype} {list(shape)} on x's device")
+            rr = _row_stride(who, "out's r", r, shape)
+        rp = r.data_ptr()
+    st = lib().tsd_residual_norm(n, d, x.data_ptr(), x_code, xr, yp, code, yr, pp, gp, gr, scale, pn, rp, rr, hp, hr,
+                                 _raw_stream(stream, dev))
+    if st:
+        _check(st)
+    return h, r

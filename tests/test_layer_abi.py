@@ -1,4 +1,4 @@
-"""Rotary positions refuse bad
+"""Rotary positions and residual norms refuse bad
 arguments before any device work, and the host's frequencies are the formula's (no GPU)."""
 import ctypes
 import math
@@ -104,7 +104,26 @@ def test_rotary_refusals(L):
     refused(L, L.tsd_rotary_apply(None, None, None, None, None), "NULL")
 
 
+def test_residual_norm_refusals(L):
+    norm = lambda **kw: ctypes.byref(tsd.NormC(*{**dict(kind=1, eps=1e-5, weight=P, bias=None), **kw}.values()))  # noqa: E731
+
+    def call(n=3, d=16, x=P, xt=1, xr=16, y=2 * P, yt=1, yr=16, post=None, gate=None, gr=0, scale=1.0, nm=norm(), r=P, rr=16, h=2 * P, hr=16):
+        return L.tsd_residual_norm(n, d, x, xt, xr, y, yt, yr, post, gate, gr, scale, nm, r, rr, h, hr, None)
+
+    for kw, word in [(dict(n=0), "n=0"), (dict(n=(1 << 27) + 1), "n="), (dict(d=0), "d=0"), (dict(d=16385, xr=16385), "d=16385"),
+                     (dict(yt=3), "dtype"), (dict(yt=-1), "dtype"), (dict(xt=2), "dtype"), (dict(yt=0), "dtype"), (dict(x=None), "NULL x"),
+                     (dict(x=P + 1), "aligned"), (dict(xr=15), "x overlap"), (dict(yr=15), "y overlap"), (dict(r=None), "NULL r"),
+                     (dict(h=None), "NULL h"), (dict(hr=15), "h overlap"), (dict(gate=P, gr=15), "gate overlap"), (dict(gate=P + 1), "gate"),
+                     (dict(scale=math.inf), "scale"), (dict(scale=math.nan), "scale"), (dict(nm=norm(kind=3)), "kind 3"),
+                     (dict(post=norm(kind=-1)), "kind -1"), (dict(nm=norm(eps=-1.0)), "eps"), (dict(post=norm(eps=math.nan)), "eps"),
+                     (dict(nm=norm(weight=P + 2)), "weight"), (dict(y=None, gate=P), "without y"), (dict(y=None, post=norm()), "without y"),
+                     (dict(y=None, nm=None), "without y"), (dict(h=P), "overlap"), (dict(r=2 * P), "overlap"), (dict(r=3 * P, h=P), "overlap"),
+                     (dict(xr=32), "overlap"), (dict(yr=32), "overlap"), (dict(y=None, xr=32, h=P), "overlap"), (dict(r=3 * P, h=3 * P), "overlap")]:
+        refused(L, call(**kw), word)
+
+
 def test_bindings_refuse():
+    bf = torch.bfloat16
     with pytest.raises(ValueError, match="rot"):
         tsd.Rotary(64, 66, device="cpu")
     with pytest.raises(ValueError, match="layout"):
@@ -113,3 +132,8 @@ def test_bindings_refuse():
         tsd.Rotary(64, scaling="other", device="cpu")
     with pytest.raises(tsd.TsdError, match="factor"):
         tsd.Rotary(64, scaling="linear", factor=0.0, device="cpu")
+    x = torch.zeros(2, 16, dtype=bf)
+    for kw, word in [(dict(x=x.view(-1)), "n, d"), (dict(x=x, norm="other"), "norms are"), (dict(x=x.double()), "float32"), (dict(x=x, y=x.half()), "same type"),
+                     (dict(x=x), "CUDA"), (dict(x=torch.zeros(1, 16385)), "16384"), (dict(x=torch.zeros(1, 1).expand(2 ** 27 + 1, 1)), "2\\^27")]:
+        with pytest.raises(ValueError, match=word):
+            tsd.residual_norm(**kw)
