@@ -711,7 +711,7 @@ TSD_API tsd_status tsd_kv8_attend(const tsd_kv8* cache, const tsd_kv8_batch* bat
 /* ------------------------------------------------------------------------
  * A decoder layer around that cache (an attention decoder or a neural LM;
  * the paper has no counterpart): rotary positions of queries and keys, norms
- * around a block.  All pointers are
+ * around a block, attention over an encoder's states.  All pointers are
  * device memory unless said otherwise; calls are asynchronous on
  * cuda_stream, allocate nothing and can be captured into a graph: lengths,
  * positions and rows are read on the device. */
@@ -803,6 +803,37 @@ TSD_API tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int32_
                                      int32_t dtype, int64_t y_row, const tsd_norm* post, const void* gate,
                                      int64_t gate_row, float scale, const tsd_norm* norm, void* r, int64_t r_row,
                                      void* h, int64_t h_row, void* cuda_stream);
+
+/* Attention over an encoder's states: keys and values of n_sources sources (utterances) of up
+ * to `frames` frames, projected once per utterance.  Strides in elements, multiples of 8, 16-byte aligned, so both may stand
+ * in one projection's output.  What lies past a source's length is never used. */
+typedef struct {
+  const void *k, *v;                    /* dtype [n_sources][frames][kv_heads][dim] */
+  int64_t k_source, k_frame, k_head, v_source, v_frame, v_head;
+  const int32_t* lens;                  /* [n_sources] frames of each, 0..frames; NULL: all of them */
+  int32_t dtype;                        /* TSD_BF16 or TSD_F16: states, queries, results */
+  int32_t n_sources, frames, kv_heads, dim; /* frames 1..2^30, kv_heads 1..1024, dim 64 or 128 */
+} tsd_states;
+
+/* The sequences of a call.  Rows starts[i] .. starts[i+1] (NULL: one each) attend over source sources[i] (NULL:
+ * i; sequences may share one).  The hypotheses of an utterance as one sequence share its reads.
+ * Rows behind the last sequence's are not read or written.  A row whose source has no frames
+ * gives 0; rows of a sequence whose source, length or rows are out of range give NaN. */
+typedef struct {
+  int32_t n;              /* 1..65535 */
+  const int32_t* sources; /* [n] or NULL */
+  const int32_t* starts;  /* [n + 1] or NULL */
+  int32_t rows;           /* rows of the row arrays, 1..2^22 */
+  int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches; results do not depend on it being right */
+} tsd_cross_batch;
+
+/*   out[row][h] = sum_j p_j v_j,  p = softmax_j(scale * q[row][h] . k_j)  over its source's frames j.
+ * heads: query heads, a multiple of kv_heads, at most 64 per kv head and 1024; query head h reads kv head
+ * h / (heads / kv_heads).  q and out: row and head strides in elements, a multiple of 8, 16-byte aligned; out
+ * may not overlap the inputs.  Products take the states' type and accumulate in fp32, as do the softmax's statistics. */
+TSD_API tsd_status tsd_cross_attend(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads, const void* q,
+                                    int64_t q_row, int64_t q_head, float scale, void* out, int64_t out_row, int64_t out_head,
+                                    void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -95,6 +95,15 @@ class NormC(ctypes.Structure):
     _fields_ = [("kind", _i32), ("eps", _f32), ("weight", _vp), ("bias", _vp)]
 
 
+class StatesC(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp)] + [(n, _i64) for n in ("k_source", "k_frame", "k_head", "v_source", "v_frame", "v_head")] + [
+        ("lens", _vp), ("dtype", _i32), ("n_sources", _i32), ("frames", _i32), ("kv_heads", _i32), ("dim", _i32)]
+
+
+class CrossBatchC(ctypes.Structure):
+    _fields_ = [("n", _i32), ("sources", _vp), ("starts", _vp), ("rows", _i32), ("max_rows", _i32)]
+
+
 SIGNATURES = {
     "tsd_last_error": ([], ctypes.c_char_p),
     "tsd_version": ([], ctypes.c_char_p),
@@ -160,6 +169,7 @@ SIGNATURES = {
     "tsd_rotary_apply": ([_P(RotaryC), _P(RotaryRowsC), _P(RotaryHeadsC), _P(RotaryHeadsC), _vp], _i32),
     "tsd_residual_norm": ([_i32, _i32, _vp, _i32, _i64, _vp, _i32, _i64, _P(NormC), _vp, _i64, _f32, _P(NormC), _vp, _i64,
                            _vp, _i64, _vp], _i32),
+    "tsd_cross_attend": ([_P(StatesC), _P(CrossBatchC), _i32, _vp, _i64, _i64, _f32, _vp, _i64, _i64, _vp], _i32),
 }
 
 _lib = None
@@ -1222,3 +1232,84 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
     if st:
         _check(st)
     return h, r
+
+
+class CrossStates:
+    """Keys and values of encoder states that a decoder attends over
+    (``tsd_states``), over tensors of the caller's: k, v bf16 or fp16 [n_sources, frames,
+    kv_heads, dim] (dim 64 or 128, any strides that are multiples of 8), lens int32
+    [n_sources], the frames of each (None: all).  Lengths are read on the device."""
+
+    def __init__(self, k, v, lens=None):
+        import torch
+
+        code = _dtype_code(k)
+        if k.dim() != 4 or code not in (1, 2):
+            raise ValueError("CrossStates: k must be bf16 or fp16 [n_sources, frames, kv_heads, dim]")
+        if v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError(f"CrossStates: v must be {k.dtype} {list(k.shape)}")
+        n, frames, heads, dim = k.shape
+        if dim not in (64, 128) or not 1 <= heads <= 1024 or not 1 <= frames <= 1 << 30 or not 1 <= n <= _MAX32:
+            raise ValueError("CrossStates: dim is 64 or 128, 1 to 1024 kv_heads, 1 to 2^30 frames, a source at least")
+        if not k.is_cuda or v.device != k.device or (lens is not None and lens.device != k.device):
+            raise ValueError("CrossStates: k, v and lens must be CUDA tensors on one device")
+        if lens is not None and (lens.dtype != torch.int32 or lens.shape != (n,) or not lens.is_contiguous()):
+            raise ValueError(f"CrossStates: lens must be contiguous int32 [{n}]")
+        for name, t in (("k", k), ("v", v)):
+            if t.stride(3) != 1 or any(x % 8 for x in t.stride()[:3]) or t.data_ptr() % 16:
+                raise ValueError(f"CrossStates: {name}'s last dimension must be adjacent, its strides multiples of 8, 16-byte aligned")
+        self.k, self.v, self.lens = k, v, lens
+        self.n_sources, self.frames, self.kv_heads, self.dim, self.dtype = n, frames, heads, dim, k.dtype
+        self._dev = k.get_device()
+        self._c = StatesC(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3],
+                          lens.data_ptr() if lens is not None else None, code, n, frames, heads, dim)
+        self._pc = ctypes.byref(self._c)
+
+    def attend(self, q, starts=None, sources=None, scale: Optional[float] = None, out=None,
+               max_rows: Optional[int] = None, stream=None):
+        """Attention of queries [rows, heads, dim] over the states (``tsd_cross_attend``).
+        Rows starts[i] .. starts[i + 1] (int32 [n + 1]; None: one row each) attend over source
+        sources[i] (int32 [n]; None: i): an utterance's hypotheses in one sequence
+        share its reads.  max_rows, the most rows of a sequence, sizes launches only.
+        scale: 1 / sqrt(dim) if None."""
+        import torch
+
+        who, dev, i32 = "CrossStates.attend", self._dev, torch.int32
+        s = q.shape
+        if len(s) != 3 or q.dtype != self.dtype or s[2] != self.dim:
+            raise ValueError(f"{who}: q must be {self.dtype} [rows, heads, {self.dim}]")
+        if torch.cuda.current_device() != dev or q.get_device() != dev:
+            raise ValueError(f"{who}: q must be on the states' device, the current one")
+        rows, heads = s[0], s[1]
+        if not 1 <= rows <= 1 << 22:
+            raise ValueError(f"{who}: 1 to 2^22 rows")
+        n, ps, pt = rows, None, None
+        if sources is not None:
+            if sources.dtype != i32 or sources.dim() != 1 or not sources.is_contiguous() or sources.get_device() != dev:
+                raise ValueError(f"{who}: sources must be contiguous int32 [n] on the states' device")
+            n, ps = sources.shape[0], sources.data_ptr()
+        if starts is not None:
+            if starts.dtype != i32 or starts.dim() != 1 or not starts.is_contiguous() or starts.get_device() != dev:
+                raise ValueError(f"{who}: starts must be contiguous int32 [n + 1] on the states' device")
+            if starts.shape[0] < 2 or (sources is not None and starts.shape[0] != n + 1):
+                raise ValueError(f"{who}: starts must have n + 1 entries")
+            n, pt = starts.shape[0] - 1, starts.data_ptr()
+        if n > 65535:
+            raise ValueError(f"{who}: at most 65535 sequences")
+        d = q.stride()
+        if out is None:
+            out = _empty(s, self.dtype, dev, stream)
+            o = (heads * self.dim, self.dim, 1)
+        else:
+            o = out.stride()
+            if out.shape != s or out.dtype != self.dtype or out.get_device() != dev:
+                raise ValueError(f"{who}: out must be {self.dtype} {list(s)} on the states' device")
+        if d[2] != 1 or o[2] != 1:
+            raise ValueError(f"{who}: the last dimension of q and out must be adjacent")
+        b = CrossBatchC(n, ps, pt, rows, min(max_rows or 0, _MAX32))
+        st = lib().tsd_cross_attend(self._pc, ctypes.byref(b), heads, q.data_ptr(), d[0], d[1],
+                                    self.dim ** -0.5 if scale is None else scale, out.data_ptr(), o[0], o[1],
+                                    _raw_stream(stream, dev))
+        if st:
+            _check(st)
+        return out

@@ -1,4 +1,4 @@
-"""Rotary positions and residual norms refuse bad
+"""Rotary positions, residual norms and attention over encoder states refuse bad
 arguments before any device work, and the host's frequencies are the formula's (no GPU)."""
 import ctypes
 import math
@@ -122,6 +122,28 @@ def test_residual_norm_refusals(L):
         refused(L, call(**kw), word)
 
 
+def test_cross_refusals(L):
+    def call(s=(), b=(), heads=4, q=P, qr=256, qh=64, scale=0.1, out=P, orow=256, oh=64):
+        x = dict(k=P, v=P, ks=4096, kf=128, kh=64, vs=4096, vf=128, vh=64, lens=P, dtype=1, n_sources=3, frames=32, kv_heads=2, dim=64)
+        w = dict(n=2, sources=P, starts=P, rows=5, max_rows=0)
+        x, w = tsd.StatesC(*{**x, **dict(s)}.values()), tsd.CrossBatchC(*{**w, **dict(b)}.values())
+        return L.tsd_cross_attend(ctypes.byref(x), ctypes.byref(w), heads, q, qr, qh, scale, out, orow, oh, None)
+
+    for kw, word in [(dict(k=None), "NULL k"), (dict(v=None), "NULL v"), (dict(k=P + 8), "aligned"), (dict(kf=127), "aligned"), (dict(vh=4), "aligned"),
+                     (dict(ks=-4096), "range"), (dict(vs=1 << 37), "range"), (dict(dtype=0), "dtype"), (dict(dim=96), "dim=96"),
+                     (dict(kv_heads=0), "kv_heads=0"), (dict(n_sources=0), "n_sources=0"), (dict(frames=0), "frames=0"),
+                     (dict(frames=(1 << 30) + 1), "frames=")]:
+        refused(L, call(s=kw.items()), word)
+    for kw, word in [(dict(n=0), "n=0"), (dict(n=65536), "n=65536"), (dict(rows=0), "rows=0"), (dict(rows=(1 << 22) + 1), "rows="),
+                     (dict(starts=None), "starts is NULL"), (dict(n=4, sources=None), "sources is NULL"), (dict(max_rows=-1), "max_rows")]:
+        refused(L, call(b=kw.items()), word)
+    for kw, word in [(dict(heads=0), "heads=0"), (dict(heads=3), "heads=3"), (dict(heads=130), "heads=130"), (dict(q=None), "NULL q"),
+                     (dict(out=None), "NULL out"), (dict(qr=250), "aligned"), (dict(out=P + 2), "aligned"), (dict(oh=-64), "range"),
+                     (dict(scale=math.inf), "scale"), (dict(scale=math.nan), "scale"), (dict(orow=56), "overlap"), (dict(oh=0), "overlap")]:
+        refused(L, call(**kw), word)
+    refused(L, L.tsd_cross_attend(None, None, 4, P, 256, 64, 0.1, P, 256, 64, None), "NULL")
+
+
 def test_bindings_refuse():
     bf = torch.bfloat16
     with pytest.raises(ValueError, match="rot"):
@@ -137,3 +159,7 @@ def test_bindings_refuse():
                      (dict(x=x), "CUDA"), (dict(x=torch.zeros(1, 16385)), "16384"), (dict(x=torch.zeros(1, 1).expand(2 ** 27 + 1, 1)), "2\\^27")]:
         with pytest.raises(ValueError, match=word):
             tsd.residual_norm(**kw)
+    k = torch.zeros(2, 5, 1, 64, dtype=bf)
+    for a, word in [((k.float(), k), "bf16"), ((k, k[:1]), "v must"), ((k, k.half()), "v must"), ((k[..., :32], k[..., :32]), "dim is"), ((k, k), "CUDA")]:
+        with pytest.raises(ValueError, match=word):
+            tsd.CrossStates(*a)
