@@ -827,13 +827,17 @@ typedef struct {
   int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches; results do not depend on it being right */
 } tsd_cross_batch;
 
+/* Device memory that tsd_cross_attend needs for such calls (their pointers are not read): 0 or 16-byte aligned. */
+TSD_API tsd_status tsd_cross_attend_workspace(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads,
+                                              int64_t* bytes);
+
 /*   out[row][h] = sum_j p_j v_j,  p = softmax_j(scale * q[row][h] . k_j)  over its source's frames j.
  * heads: query heads, a multiple of kv_heads, at most 64 per kv head and 1024; query head h reads kv head
  * h / (heads / kv_heads).  q and out: row and head strides in elements, a multiple of 8, 16-byte aligned; out
  * may not overlap the inputs.  Products take the states' type and accumulate in fp32, as do the softmax's statistics. */
 TSD_API tsd_status tsd_cross_attend(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads, const void* q,
                                     int64_t q_row, int64_t q_head, float scale, void* out, int64_t out_row, int64_t out_head,
-                                    void* cuda_stream);
+                                    void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 #ifdef __cplusplus
 }

@@ -169,7 +169,8 @@ SIGNATURES = {
     "tsd_rotary_apply": ([_P(RotaryC), _P(RotaryRowsC), _P(RotaryHeadsC), _P(RotaryHeadsC), _vp], _i32),
     "tsd_residual_norm": ([_i32, _i32, _vp, _i32, _i64, _vp, _i32, _i64, _P(NormC), _vp, _i64, _f32, _P(NormC), _vp, _i64,
                            _vp, _i64, _vp], _i32),
-    "tsd_cross_attend": ([_P(StatesC), _P(CrossBatchC), _i32, _vp, _i64, _i64, _f32, _vp, _i64, _i64, _vp], _i32),
+    "tsd_cross_attend_workspace": ([_P(StatesC), _P(CrossBatchC), _i32, _P(_i64)], _i32),
+    "tsd_cross_attend": ([_P(StatesC), _P(CrossBatchC), _i32, _vp, _i64, _i64, _f32, _vp, _i64, _i64, _vp, _i64, _vp], _i32),
 }
 
 _lib = None
@@ -1264,6 +1265,7 @@ class CrossStates:
         self._c = StatesC(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3],
                           lens.data_ptr() if lens is not None else None, code, n, frames, heads, dim)
         self._pc = ctypes.byref(self._c)
+        self._flat = k.stride(1) < dim or v.stride(1) < dim  # frames overlap
 
     def attend(self, q, starts=None, sources=None, scale: Optional[float] = None, out=None,
                max_rows: Optional[int] = None, stream=None):
@@ -1307,9 +1309,16 @@ class CrossStates:
         if d[2] != 1 or o[2] != 1:
             raise ValueError(f"{who}: the last dimension of q and out must be adjacent")
         b = CrossBatchC(n, ps, pt, rows, min(max_rows or 0, _MAX32))
-        st = lib().tsd_cross_attend(self._pc, ctypes.byref(b), heads, q.data_ptr(), d[0], d[1],
-                                    self.dim ** -0.5 if scale is None else scale, out.data_ptr(), o[0], o[1],
-                                    _raw_stream(stream, dev))
+        pb, L = ctypes.byref(b), lib()
+        key = (who, dev, self.dim, self.kv_heads, self.frames, self._flat, n, rows, heads, max_rows, pt is None)
+        need = _sizes.get(key)
+        if need is None:
+            x = _i64()
+            _check(L.tsd_cross_attend_workspace(self._pc, pb, heads, ctypes.byref(x)))
+            need = _remember(key, x.value)
+        ws = _empty(need, torch.uint8, dev, stream).data_ptr() if need else None
+        st = L.tsd_cross_attend(self._pc, pb, heads, q.data_ptr(), d[0], d[1], self.dim ** -0.5 if scale is None else scale,
+                                out.data_ptr(), o[0], o[1], ws, need, _raw_stream(stream, dev))
         if st:
             _check(st)
         return out

@@ -43,4 +43,12 @@ struct CrossRowsPlan {
 CrossRowsPlan cross_rows_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, int sms);
 cudaError_t cross_rows_launch(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s);
 
+// Many (cross_tiles.cu); false: they are few.  bytes of workspace.
+struct CrossTilesPlan {
+  int ctas = 1;
+  int64_t bytes = 0;
+};
+bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, int sms, CrossTilesPlan* p);
+cudaError_t cross_tiles_launch(const CrossAttend& a, const CrossTilesPlan& p, void* workspace, cudaStream_t s);
+
 }  // namespace tsd

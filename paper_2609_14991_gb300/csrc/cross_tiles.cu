@@ -1,0 +1,680 @@
+// Attention over an encoder's states with many query rows per key head: whole
+// transcripts, n-best lists (tsd.h: tsd_cross_attend).
+//
+// The mathematics is cross_rows.cu's; the products run on tcgen05 (16-bit in, fp32 accumulate in
+// TMEM).  A unit is 256 rows of a sequence and key head (row = token * group + head of the
+// group), two row tiles of 128, over the frames of its source, 128 at a time:
+//   warps 0-7   softmax: a thread is a row (warps 0-3 tile 0, 4-7 tile 1), so its maximum
+//               and sum need no exchange.  Reads its 128 scores from TMEM and leaves the weights
+//               in their place, as the values' product's A operand, in the states' type (the
+//               product wants one type for both; half a step of bf16 is 2^-8 of a weight, and the
+//               sum that divides them is of unrounded ones);
+//   warp 8      copies keys and values, a ring of tiles by TMA (128-byte swizzle);
+//   warp 9      issues the MMAs;
+//   warp 10     zeroes what stands behind a source's length in its last tile of values: a
+//               weight of 0 does not make a NaN or infinity 0.
+// While one row tile's scores are with the softmax, the other's products run.  Keys are the K-major B
+// operand of the scores; the same layout of the values is read as an MN-major B
+// operand, so neither is transposed.  The maximum is looked for, and the accumulator rescaled in
+// TMEM, only in steps whose weights outgrow fp16 relative to the one so far.
+//
+// Work: every unit has its tiles of frames in one line of all sequences, weighted by what they
+// cost, and each CTA takes an equal share of that line, so ragged sequences and few
+// long ones fill the device alike.  A unit that several CTAs share leaves its parts in the workspace, which a
+// second kernel joins in their order.
+#include <algorithm>
+#include <climits>
+
+#include "cross.h"
+#include "launch.h"
+#include "tc_attend.cuh"
+
+namespace tsd {
+
+namespace {
+
+using namespace tc;
+
+constexpr int kFrames = 128;  // per tile
+constexpr int kUnitRows = 256;
+constexpr int kSoftWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kFixWarp = 10;
+constexpr int kThreads = 384;  // whole warpgroups: the last warp has no work
+constexpr int kSoftRegs = 208, kOtherRegs = 80, kLaunchRegs = 168;
+static_assert(32 * kSoftWarps * kSoftRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
+
+template <int DIM>
+struct TilesShape {
+  static constexpr int kHalf = 128 * 128;                // 128 rows of 64 elements
+  static constexpr int kTileBytes = kHalf * (DIM / 64);  // a row tile's queries, or a tile of keys or values
+  static constexpr int kStages = DIM == 128 ? 4 : 8;
+  static constexpr int kQ = 0;
+  static constexpr int kRing = 2 * kTileBytes;
+  static constexpr int kBar = kRing + kStages * kTileBytes;
+  static constexpr int kSmem = kBar + 512 + 1024;
+  static constexpr int kO = 256;  // TMEM: the row tiles' scores at 0 and 128; accumulators from here
+};
+
+static_assert(TilesShape<64>::kStages % 2 == 0 && TilesShape<128>::kStages % 2 == 0, "keys in even stages, values in odd ones");
+
+// What a unit and its tiles cost, in fifths of a tile of two row tiles.
+constexpr int kPad = 5, kTwo = 5, kOne = 3, kLeast = 20;
+
+struct TilesArgs {
+  CrossAttend a;
+  float* part;      // [2 * CTAs][kUnitRows][DIM]: a unit begun by an earlier CTA; one that the next CTAs go on with
+  float2* part_ml;  // (maximum, sum) of those rows
+  int4* joins;      // [2 * CTAs]: the second one's place
+  int k_heads, k_sources, v_heads, v_sources;  // 0: the coordinate is 0 (stride 0)
+};
+
+struct Line {
+  int kv, group;
+  __device__ __forceinline__ int units(const CrossSeq& q) const { return (int)(((int64_t)q.count * group + kUnitRows - 1) / kUnitRows); }
+  static __device__ __forceinline__ int tiles(const CrossSeq& q) { return max(1, (q.len + kFrames - 1) / kFrames); }
+  __device__ __forceinline__ bool two(const CrossSeq& q, int u) const { return (int64_t)q.count * group - (int64_t)u * kUnitRows > 128; }
+  static __device__ __forceinline__ int64_t unit(int tiles, bool two) { return kPad + (int64_t)tiles * (two ? kTwo : kOne); }
+  __device__ __forceinline__ int64_t head(const CrossSeq& q) const {
+    const int n = units(q), t = tiles(q);
+    return n ? (n - 1) * unit(t, true) + unit(t, two(q, n - 1)) : 0;
+  }
+  __device__ __forceinline__ int64_t seq(const CrossSeq& q) const { return kv * head(q); }
+};
+
+// One CTA's share of a unit.
+struct Part {
+  CrossSeq q;
+  int head, row0;   // row0: of the sequence's count * group
+  int lo, hi, all;  // tiles of frames lo .. hi - 1 of all
+  int n;            // those to compute (0 where a row sees nothing)
+  int64_t at;       // the unit's place in the line
+  bool two;
+};
+
+// The parts of a CTA in order, the same for each of its warps: places lo .. hi - 1 of the line, from sequence i
+// (which begins at place `at`) on.  A warp holds 32 sequences at a time.
+struct Walk {
+  const CrossAttend& a;
+  Line line;
+  int64_t at, lo, hi, next_unit;
+  int lane, base, i, head, u, units, tiles;
+  CrossSeq w, q;
+  __device__ __forceinline__ Walk(const CrossAttend& args, int64_t place, int64_t from, int64_t to, int seq)
+      : a(args), line{args.s.kv_heads, args.group}, at(place), lo(from), hi(to), lane(threadIdx.x & 31), base(seq), i(seq) {
+    window();
+    take();
+    if (units == 0) return;  // (a share begins inside a sequence)
+    const int64_t per = line.head(q);
+    head = (int)min((lo - at) / per, (int64_t)line.kv - 1);
+    at += head * per;
+    u = (int)min((lo - at) / Line::unit(tiles, true), (int64_t)units - 1);
+    at += u * Line::unit(tiles, true);
+  }
+  __device__ __forceinline__ void window() {
+    w.source = w.len = w.row0 = w.count = 0, w.ok = false;
+    if (base + lane < a.b.n) w = cross_seq(a.s, a.b, base + lane);
+  }
+  __device__ __forceinline__ void take() {
+    const int l = i - base;
+    q.source = __shfl_sync(0xffffffffu, w.source, l);
+    q.len = __shfl_sync(0xffffffffu, w.len, l);
+    q.row0 = __shfl_sync(0xffffffffu, w.row0, l);
+    q.count = __shfl_sync(0xffffffffu, w.count, l);
+    q.ok = __shfl_sync(0xffffffffu, (int)w.ok, l);
+    units = line.units(q), tiles = Line::tiles(q), head = 0, u = 0;
+  }
+  __device__ __forceinline__ bool sequence() {  // the next one with rows
+    while (true) {
+      const unsigned some = __ballot_sync(0xffffffffu, w.count > 0 && base + lane > i);
+      if (some) {
+        i = base + __ffs(some) - 1;
+        take();
+        return true;
+      }
+      base += 32;
+      i = base - 1;
+      if (base >= a.b.n) return false;
+      window();
+    }
+  }
+  __device__ __forceinline__ bool next(Part& p) {
+    while (at < hi) {
+      if (u >= units) {
+        u = 0;
+        if (++head >= line.kv && !sequence()) return false;
+      }
+      if (units == 0) return false;
+      p.q = q, p.head = head, p.row0 = u * kUnitRows, p.at = at, p.all = tiles;
+      p.two = line.two(q, u);
+      const int cost = p.two ? kTwo : kOne;
+      const auto first = [&](int64_t place) {  // the first tile that begins there or later
+        const int64_t x = place - at - kPad;
+        return x <= 0 ? 0 : (int)min((x + cost - 1) / cost, (int64_t)tiles);
+      };
+      p.lo = first(lo), p.hi = first(hi);
+      at += Line::unit(tiles, p.two);
+      ++u;
+      p.n = q.ok && q.len > 0 ? p.hi - p.lo : 0;
+      if (p.hi > p.lo) return true;
+    }
+    return false;
+  }
+};
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+               : "memory");
+}
+
+template <bool BF16, int DIM>
+__global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_constant__ TilesArgs args, const __grid_constant__ CUtensorMap k_map,
+                                                             const __grid_constant__ CUtensorMap v_map) {
+  using S = TilesShape<DIM>;
+  constexpr int ST = S::kStages;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ int64_t s_sums[kThreads / 32], s_place;
+  __shared__ int s_seq;
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBar);
+  uint64_t *full = bars, *empty = bars + ST, *v_ready = bars + 2 * ST;  // the ring's stages; those of values past warp 10
+  uint64_t *s_full = v_ready + ST / 2, *p_full = s_full + 2, *o_full = s_full + 4;  // [2] row tiles
+  uint64_t *q_full = s_full + 6, *drain = s_full + 7;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 8);
+  const CrossAttend& a = args.a;
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const Line line{a.s.kv_heads, a.group};
+
+  // The line's length and this CTA's share: a thread's run of sequences, then the threads'.
+  const int run = (a.b.n + kThreads - 1) / kThreads, run0 = min((int)threadIdx.x * run, a.b.n), run1 = min(run0 + run, a.b.n);
+  int64_t mine = 0;
+  for (int i = run0; i < run1; ++i) mine += line.seq(cross_seq(a.s, a.b, i));
+  int64_t upto = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += x;
+  }
+  if (lane == 31) s_sums[warp] = upto;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < ST; ++i) {
+      mbar_init(full + i, 1);
+      mbar_init(empty + i, 1);
+    }
+    for (int i = 0; i < ST / 2; ++i) mbar_init(v_ready + i, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 4);
+      mbar_init(o_full + i, 1);
+    }
+    mbar_init(q_full, kSoftWarps);
+    mbar_init(drain, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) {
+    const int64_t x = s_sums[i];
+    if (i < warp) upto += x;
+    total += x;
+  }
+  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kLeast);
+  const int64_t lo = share * blockIdx.x, hi = min(lo + share, total);
+  if (lo >= hi) {
+    if (args.joins && threadIdx.x == 0) args.joins[2 * blockIdx.x + 1].x = -1;
+    return;
+  }
+  if (upto - mine <= lo && lo < upto) {
+    int64_t x = upto - mine;
+    for (int i = run0; i < run1; ++i) {
+      const int64_t y = line.seq(cross_seq(a.s, a.b, i));
+      if (lo < x + y) {
+        s_seq = i, s_place = x;
+        break;
+      }
+      x += y;
+    }
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  __syncthreads();
+  fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk walk(a, s_place, lo, hi, s_seq);
+  Part p;
+  // A wait that runs out ends its role; the others' waits on it run out in turn, and the
+  // rows from there on say NaN.
+  if (warp < kSoftWarps) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    const int tile = warp >> 2;
+    // Queries and results pass through shared memory row by row, kRowLanes lanes each: 16
+    // bytes of a row of the warp's, in the 128-byte swizzle
+    constexpr int kRowLanes = DIM / 8, kRowsPer = 32 / kRowLanes;
+    const auto chunk = [&](int row, int c) {
+      return reinterpret_cast<uint4*>(smem + S::kQ + tile * S::kTileBytes + (c >> 3) * S::kHalf + ((warp & 3) * 32 + row) * 128 + (((c ^ row) & 7) << 4));
+    };
+    const int step_tok = kRowsPer / a.group, step_h = kRowsPer % a.group;
+    const uint32_t st = tmem + (uint32_t)(tile * 128) + ((uint32_t)((warp & 3) * 32) << 16);  // scores, then weights
+    const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
+    const float c = a.scale * kLog2e;
+    const uint64_t c2 = pair_of(c, c);
+    const float nan = __uint_as_float(0x7fc00000u);
+    int at0 = 0, done = 0;  // steps and parts of this row tile so far
+    bool fine = true, join = false;
+    // (a warp of a row tile that has no rows must not arrive for the next one's queries early)
+    const auto row_tile_end = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftWarps) : "memory"); };
+    while (walk.next(p)) {
+      const int rows = p.q.count * a.group, r = p.row0 + threadIdx.x, wr = p.row0 + (threadIdx.x & ~31);
+      const bool whole_unit = p.lo == 0 && p.hi == p.all;
+      const int slot = 2 * (int)blockIdx.x + (p.lo == 0 ? 1 : 0);
+      if (!whole_unit && p.lo == 0) {
+        join = true;
+        if (threadIdx.x == 0) {  // (an exact division: this CTA's share is followed by whole ones)
+          const int64_t last = (p.at + kPad + (int64_t)(p.all - 1) * (p.two ? kTwo : kOne)) / share;
+          args.joins[slot - 1] = make_int4(p.q.row0, rows, p.row0, p.head);
+          args.joins[slot].x = (int)min(last, (int64_t)gridDim.x - 1);
+        }
+      }
+      if (p.n == 0 || !fine) {
+        if (r < rows) {
+          const int tok = p.q.row0 + r / a.group, h = p.head * a.group + r % a.group;
+          const uint32_t x = p.q.ok && fine ? 0u : BF16 ? 0x7fc07fc0u : 0x7e007e00u;
+          if (whole_unit) {
+            uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head);
+            for (int i = 0; i < DIM / 8; ++i) dst[i] = make_uint4(x, x, x, x);
+          } else {
+            args.part_ml[(size_t)slot * kUnitRows + threadIdx.x] = make_float2(0.f, nan);
+          }
+        }
+        if (p.n > 0) row_tile_end();
+        continue;
+      }
+      // the rows that a lane copies, from the first on
+      const int r0 = wr + lane / kRowLanes, tok0 = r0 / a.group, h0 = p.head * a.group + r0 - tok0 * a.group;
+      const auto next_row = [&](int& t, int& h) {
+        t += step_tok;
+        h += step_h;
+        if (h >= (p.head + 1) * a.group) h -= a.group, ++t;
+      };
+      {
+        int t = tok0, h = h0;
+#pragma unroll
+        for (int i = 0; i < kRowLanes; ++i) {
+          const int rw = i * kRowsPer + lane / kRowLanes;
+          const uint16_t* src = a.q + (int64_t)(p.q.row0 + t) * a.q_row + (int64_t)h * a.q_head + 8 * (lane % kRowLanes);
+          if (wr + rw < rows)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(chunk(rw, lane % kRowLanes))), "l"(src) : "memory");
+          else
+            *chunk(rw, lane % kRowLanes) = make_uint4(0, 0, 0, 0);
+          next_row(t, h);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(q_full);
+      }
+      bool dead = false;
+      if (tile == 0 || p.two) {
+        float m = -INFINITY, l = 0.f;
+#pragma unroll 1
+        for (int j = 0; j < p.n; ++j) {
+          if (!__all_sync(0xffffffffu, mbar_wait(s_full + tile, (uint32_t)(at0 + j) & 1u))) {
+            dead = true;
+            break;
+          }
+          fence_after();
+          const int left = p.q.len - (p.lo + j) * kFrames;  // frames from here on
+          const bool whole = left >= kFrames;
+          // Weights relative to the maximum so far, without looking for this step's: one
+          // that a score has outgrown shows in the sum, and the step is taken again from its
+          // scores, which the weights have not replaced yet.  (Sums up to 2^15: no weight then
+          // reaches fp16's largest.)
+          uint32_t y[kFrames / 2];
+          float sum;
+          bool look = j == 0;
+#pragma unroll 1
+          while (true) {
+            if (look) {
+              float top = -INFINITY;
+#pragma unroll
+              for (int h = 0; h < 4; ++h) {
+                float v[32];
+                tmem_ld32(st + 32 * h, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) {
+                  const float x = whole || 32 * h + e < left ? v[e] * c : -INFINITY;
+                  top = fmaxf(top, x);
+                }
+              }
+              const float x = fmaxf(m, top);
+              const float w = x == m ? 1.f : ex2_approx(m - x);
+              m = x;
+              l *= w;
+              if (j > 0) {  // (this step's scores came after the last step's values: they are in the accumulator)
+#pragma unroll 1
+                for (int ch = 0; ch < DIM / 16; ++ch) {
+                  float o[16];
+                  tmem_ld16(ot + 16 * ch, o);
+                  uint32_t z[16];
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * w);
+                  tmem_st16(ot + 16 * ch, z);
+                }
+              }
+            }
+            const float ref = m > -INFINITY ? m - 7.f : 0.f;
+            const uint64_t ref2 = pair_of(-ref, -ref);
+            uint64_t sums = 0;
+            uint32_t raw[2][16];  // 16 scores are on their way while the ones before are worked on
+            tmem_ld16_begin(st, raw[0]);
+#pragma unroll
+            for (int b = 0; b < kFrames / 16; ++b) {
+              tmem_ld16_wait(raw[b & 1]);
+              if (b + 1 < kFrames / 16) tmem_ld16_begin(st + 16 * (b + 1), raw[(b + 1) & 1]);
+              float x[16];
+#pragma unroll
+              for (int e = 0; e < 16; e += 2)
+                unpair(fma2(pair_of(__uint_as_float(raw[b & 1][e]), __uint_as_float(raw[b & 1][e + 1])), c2, ref2), x[e], x[e + 1]);
+              if (!whole)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                  if (16 * b + e >= left) x[e] = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < 16; e += 2) {
+                const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
+                sums = add2(sums, pair_of(p0, p1));
+                y[8 * b + e / 2] = narrow2<BF16>(p0, p1);
+              }
+            }
+            float s0, s1;
+            unpair(sums, s0, s1);
+            sum = s0 + s1;
+            if (look || !__any_sync(0xffffffffu, sum > 32768.f)) break;
+            look = true;
+          }
+          l += sum;
+          tmem_st32(st, *reinterpret_cast<const uint32_t(*)[32]>(y));
+          tmem_st32(st + 32, *reinterpret_cast<const uint32_t(*)[32]>(y + 32));
+          tmem_st_wait();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(p_full + tile);
+        }
+        if (!dead && !mbar_wait(o_full + tile, (uint32_t)done & 1u)) dead = true;
+        fence_after();
+        dead = __any_sync(0xffffffffu, dead);
+        if (dead) l = nan;
+        // results, through shared memory: neighbouring lanes write a row
+        if (whole_unit) {
+          const float inv = 1.f / l;
+#pragma unroll
+          for (int ch = 0; ch < DIM / 32; ++ch) {
+            float v[32];
+            tmem_ld32(ot + 32 * ch, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *chunk(lane, 4 * ch + i) = make_uint4(narrow2<BF16>(v[8 * i] * inv, v[8 * i + 1] * inv), narrow2<BF16>(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
+                                                    narrow2<BF16>(v[8 * i + 4] * inv, v[8 * i + 5] * inv), narrow2<BF16>(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
+          }
+          __syncwarp();
+          int t = tok0, h = h0;
+#pragma unroll 8
+          for (int i = 0; i < kRowLanes; ++i) {
+            const int rw = i * kRowsPer + lane / kRowLanes;
+            if (wr + rw < rows)
+              *reinterpret_cast<uint4*>(a.out + (int64_t)(p.q.row0 + t) * a.out_row + (int64_t)h * a.out_head + 8 * (lane % kRowLanes)) = *chunk(rw, lane % kRowLanes);
+            next_row(t, h);
+          }
+          __syncwarp();
+        } else {
+          float* to = args.part + ((size_t)slot * kUnitRows + (threadIdx.x & ~31)) * DIM + 4 * (lane % kRowLanes);
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {  // half of the dimensions, fp32
+#pragma unroll
+            for (int ch = 0; ch < DIM / 64; ++ch) {
+              float v[32];
+              tmem_ld32(ot + half * (DIM / 2) + 32 * ch, v);
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                *chunk(lane, 8 * ch + i) = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            }
+            __syncwarp();
+#pragma unroll 8
+            for (int i = 0; i < kRowLanes; ++i) {
+              const int rw = i * kRowsPer + lane / kRowLanes;
+              if (wr + rw < rows) *reinterpret_cast<uint4*>(to + (size_t)rw * DIM + half * (DIM / 2)) = *chunk(rw, lane % kRowLanes);
+            }
+            __syncwarp();
+          }
+          args.part_ml[(size_t)slot * kUnitRows + threadIdx.x] = make_float2(m, l);
+        }
+        at0 += p.n;
+        ++done;
+      }
+      fence_before();
+      fine = !dead;
+      row_tile_end();
+    }
+    if (threadIdx.x == 0 && args.joins && !join) args.joins[2 * blockIdx.x + 1].x = -1;
+    asm volatile("bar.arrive 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");
+    return;
+  }
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));  // one instruction for the whole warpgroup
+  if (warp == kTmaWarp) {
+    uint32_t at = 0;  // tiles through the ring, keys and values
+    bool dead = false;
+    while (!dead && walk.next(p)) {
+      if (elect()) {
+        for (int j = 0; j < p.n && !dead; ++j) {
+#pragma unroll
+          for (int kind = 0; kind < 2 && !dead; ++kind, ++at) {
+            const int s = at % ST;
+            if (at >= ST && !mbar_wait(empty + s, (at / ST - 1) & 1u)) {
+              dead = true;
+              break;
+            }
+            mbar_expect_tx(full + s, S::kTileBytes);
+#pragma unroll
+            for (int h = 0; h < DIM / 64; ++h)
+              tma_load_4d(smem_u32(smem + S::kRing + s * S::kTileBytes + h * S::kHalf), kind ? &v_map : &k_map, full + s, 64 * h, (p.lo + j) * kFrames,
+                          kind ? p.head * args.v_heads : p.head * args.k_heads, kind ? p.q.source * args.v_sources : p.q.source * args.k_sources);
+          }
+        }
+        if (dead)  // what is on its way ends first
+          for (uint32_t i = at - min(at, (uint32_t)ST); i < at; ++i) mbar_wait(full + i % ST, (i / ST) & 1u);
+      }
+      dead = __any_sync(0xffffffffu, dead);
+      at = __reduce_max_sync(0xffffffffu, at);
+    }
+  } else if (warp == kFixWarp) {
+    uint32_t at = 0;
+    bool dead = false;
+    while (!dead && walk.next(p)) {
+      const bool fix = p.hi == p.all && p.q.len % 16;
+      for (int j = 0; j < p.n && !dead; ++j, at += 2) {
+        const uint32_t v = at + 1;
+        if (!__all_sync(0xffffffffu, mbar_wait(full + v % ST, (v / ST) & 1u))) {
+          dead = true;
+          break;
+        }
+        if (fix && j == p.n - 1) {
+          const int from = p.q.len - (p.all - 1) * kFrames, to = (from + 15) & ~15;
+          unsigned char* tile = smem + S::kRing + (v % ST) * S::kTileBytes;
+          for (int i = lane; i < (to - from) * (DIM / 8); i += 32) {
+            const int f = from + i / (DIM / 8), c = i % (DIM / 8);
+            *reinterpret_cast<uint4*>(tile + (c >> 3) * S::kHalf + f * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async_smem();
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(v_ready + v % ST / 2);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    uint32_t at0 = 0, parts = 0, tile_at[2] = {0, 0};
+    bool dead = false;
+    while (!dead && walk.next(p)) {
+      if (p.n == 0) continue;
+      const int n = p.n, tiles = p.two ? 2 : 1;
+      const bool ends = p.hi == p.all;
+      const int rest = p.q.len - (p.all - 1) * kFrames;  // of the last tile
+      if (elect()) {
+        const uint32_t sq = smem_u32(smem + S::kQ), ring = smem_u32(smem + S::kRing);
+        bool ok = mbar_wait(q_full, parts & 1u);
+        const auto have = [&](uint32_t at) {
+          const bool there = mbar_wait(full + at % ST, (at / ST) & 1u);
+          fence_after();
+          return there;
+        };
+        const auto scores = [&](int t, int j) {
+          const uint32_t at = at0 + 2 * (uint32_t)j, qa = sq + t * S::kTileBytes, kb = ring + (at % ST) * S::kTileBytes;
+#pragma unroll
+          for (int kk = 0; kk < DIM / 16; ++kk)
+            mma_f16_ss(tmem + t * 128, sw128_desc(qa + (kk >> 2) * S::kHalf) + 2 * (kk & 3), sw128_desc(kb + (kk >> 2) * S::kHalf) + 2 * (kk & 3),
+                       idesc_f16(128, kFrames, false, BF16), kk > 0);
+          mma_commit(s_full + t);
+          if (t == tiles - 1) mma_commit(empty + at % ST);
+        };
+        const auto values = [&](int t, int j) {
+          const uint32_t at = at0 + 2 * (uint32_t)j + 1, vb = ring + (at % ST) * S::kTileBytes;
+          const int steps = ends && j == n - 1 ? (rest + 15) / 16 : kFrames / 16;  // frames behind the length stay out
+#pragma unroll
+          for (int kk = 0; kk < kFrames / 16; ++kk)
+            if (kk < steps)
+              mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true, BF16), j > 0 || kk > 0);
+          if (j == n - 1) mma_commit(o_full + t);
+          if (t == tiles - 1) mma_commit(empty + at % ST);
+        };
+        if (ok) ok = have(at0);
+        for (int t = 0; t < tiles && ok; ++t) scores(t, 0);
+        for (int j = 0; j < n && ok; ++j) {
+          for (int t = 0; t < tiles && ok; ++t) {
+            ok = mbar_wait(p_full + t, (tile_at[t] + j) & 1u);
+            if (ok && t == 0) ok = have(at0 + 2 * j + 1);
+            if (ok && t == 0) ok = mbar_wait(v_ready + (at0 + 2 * j + 1) % ST / 2, ((at0 + 2 * j + 1) / ST) & 1u);
+            if (!ok) break;
+            fence_after();
+            values(t, j);
+            if (j + 1 < n) {
+              if (t == 0) ok = have(at0 + 2 * j + 2);
+              if (ok) scores(t, j + 1);
+            }
+          }
+        }
+        if (!ok) {  // the rows say NaN, once their own waits have run out; what was issued ends first
+          mma_commit(drain);
+          mbar_wait(drain, 0);
+          dead = true;
+        }
+      }
+      __syncwarp();
+      ++parts;
+      at0 += 2 * (uint32_t)n;
+      tile_at[0] += n;
+      if (p.two) tile_at[1] += n;
+      dead = __any_sync(0xffffffffu, dead);
+    }
+    asm volatile("bar.sync 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");  // the accumulators have been read
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  }
+}
+
+// The units that several CTAs share: block (c, y) takes kJoinRows rows of the one that CTA c began.
+constexpr int kJoinRows = 16, kJoinWarps = 4;
+
+template <bool BF16, int DIM>
+__global__ void __launch_bounds__(32 * kJoinWarps) k_cross_join(const __grid_constant__ TilesArgs args) {
+  const int c = blockIdx.x, last = __ldg(&args.joins[2 * c + 1].x);
+  if (last < 0) return;
+  const CrossAttend& a = args.a;
+  const int4 place = __ldg(args.joins + 2 * c);  // the sequence's first row, its rows * group, the unit's first, key head
+  constexpr int kLanes = DIM / 4, kPer = 32 / kLanes;  // lanes per row, rows per warp
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = last - c + 1;
+  const auto slot = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)); };
+#pragma unroll
+  for (int i = 0; i < kJoinRows / (kJoinWarps * kPer); ++i) {
+    const int rr = blockIdx.y * kJoinRows + (i * kJoinWarps + warp) * kPer + lane / kLanes, r = place.z + rr;
+    if (r >= place.y) continue;
+    float top = -INFINITY;
+    for (int k = 0; k < parts; ++k) top = fmaxf(top, __ldg(&args.part_ml[slot(k) * kUnitRows + rr].x));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < parts; ++k) {
+      const float2 x = __ldg(args.part_ml + slot(k) * kUnitRows + rr);
+      const float4 v = __ldg(reinterpret_cast<const float4*>(args.part + (slot(k) * kUnitRows + rr) * DIM) + lane % kLanes);
+      const float f = x.x == top ? 1.f : ex2_approx(x.x - top);  // (top -inf: every score is, and 0 / 0 is the result)
+      sum = fmaf(f, x.y, sum);
+      acc.x = fmaf(f, v.x, acc.x), acc.y = fmaf(f, v.y, acc.y), acc.z = fmaf(f, v.z, acc.z), acc.w = fmaf(f, v.w, acc.w);
+    }
+    const float inv = 1.f / sum;
+    const int tok = place.x + r / a.group, h = place.w * a.group + r % a.group;
+    *reinterpret_cast<uint2*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + 4 * (lane % kLanes)) =
+        make_uint2(narrow2<BF16>(acc.x * inv, acc.y * inv), narrow2<BF16>(acc.z * inv, acc.w * inv));
+  }
+}
+
+// Keys or values as [sources][heads][frames][dim], a dimension of stride 0 as one of size 1.
+bool make_states_map(CUtensorMap* m, const tsd_states& s, const void* base, int64_t source, int64_t frame, int64_t head) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn || frame < s.dim) return false;
+  const auto stride = [&](int64_t x, int64_t size) { return (cuuint64_t)(size > 1 && x ? x : s.dim) * 2; };
+  const cuuint64_t dims[4] = {(cuuint64_t)s.dim, (cuuint64_t)s.frames, (cuuint64_t)(head ? s.kv_heads : 1), (cuuint64_t)(source ? s.n_sources : 1)};
+  const cuuint64_t strides[3] = {stride(frame, s.frames), stride(head, s.kv_heads), stride(source, s.n_sources)};
+  const cuuint32_t box[4] = {64, kFrames, 1, 1}, es[4] = {1, 1, 1, 1};
+  return fn(m, s.dtype == TSD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <bool BF16, int DIM>
+cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
+  using S = TilesShape<DIM>;
+  static const bool enough = [] {  // setmaxnreg waits for registers that the launch did not bring
+    cudaFuncAttributes at{};
+    return cudaFuncGetAttributes(&at, k_cross_tiles<BF16, DIM>) == cudaSuccess && at.numRegs >= kLaunchRegs;
+  }();
+  if (!enough) return cudaErrorLaunchOutOfResources;
+  const cudaError_t e = smem_opt_in<k_cross_tiles<BF16, DIM>>(S::kSmem);
+  if (e != cudaSuccess) return e;
+  k_cross_tiles<BF16, DIM><<<p.ctas, kThreads, S::kSmem, s>>>(args, k, v);
+  if (p.bytes > 0) k_cross_join<BF16, DIM><<<dim3(p.ctas, kUnitRows / kJoinRows), 32 * kJoinWarps, 0, s>>>(args);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, int sms, CrossTilesPlan* p) {
+  const int group = heads / s.kv_heads;
+  const int64_t most = std::max<int64_t>(1, b.max_rows ? std::min(b.max_rows, b.rows) : !b.starts ? 1 : ((int64_t)b.rows + b.n - 1) / b.n);
+  if (most * group <= 48 || s.k_frame < s.dim || s.v_frame < s.dim) return false;
+  const int64_t tiles = ((int64_t)s.frames + kFrames - 1) / kFrames;
+  const int64_t units = s.kv_heads * (((int64_t)b.rows * group + kUnitRows - 1) / kUnitRows + b.n);  // at most
+  const double line = (double)units * (double)(kPad + tiles * kTwo);
+  p->ctas = (int)std::max(1.0, std::min((double)sms, std::ceil(line / kLeast)));
+  // one tile of frames is never shared
+  p->bytes = tiles > 1 && p->ctas > 1 ? (int64_t)p->ctas * 2 * (kUnitRows * (s.dim * 4 + 8) + 16) : 0;
+  return true;
+}
+
+cudaError_t cross_tiles_launch(const CrossAttend& a, const CrossTilesPlan& p, void* workspace, cudaStream_t s) {
+  const bool bf = a.s.dtype == TSD_BF16;
+  CUtensorMap k, v;
+  if (!make_states_map(&k, a.s, a.s.k, a.s.k_source, a.s.k_frame, a.s.k_head) || !make_states_map(&v, a.s, a.s.v, a.s.v_source, a.s.v_frame, a.s.v_head))
+    return cudaErrorInvalidValue;
+  TilesArgs t{};
+  t.a = a;
+  if (p.bytes > 0) {
+    t.part = static_cast<float*>(workspace);
+    t.part_ml = reinterpret_cast<float2*>(t.part + (size_t)2 * p.ctas * kUnitRows * a.s.dim);
+    t.joins = reinterpret_cast<int4*>(t.part_ml + (size_t)2 * p.ctas * kUnitRows);
+  }
+  t.k_heads = a.s.k_head != 0, t.k_sources = a.s.k_source != 0, t.v_heads = a.s.v_head != 0, t.v_sources = a.s.v_source != 0;
+  return a.s.dim == 64 ? (bf ? launch<true, 64>(t, p, k, v, s) : launch<false, 64>(t, p, k, v, s))
+                       : (bf ? launch<true, 128>(t, p, k, v, s) : launch<false, 128>(t, p, k, v, s));
+}
+
+}  // namespace tsd

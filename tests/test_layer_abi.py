@@ -123,11 +123,11 @@ def test_residual_norm_refusals(L):
 
 
 def test_cross_refusals(L):
-    def call(s=(), b=(), heads=4, q=P, qr=256, qh=64, scale=0.1, out=P, orow=256, oh=64):
+    def call(s=(), b=(), heads=4, q=P, qr=256, qh=64, scale=0.1, out=P, orow=256, oh=64, ws=None, nws=0):
         x = dict(k=P, v=P, ks=4096, kf=128, kh=64, vs=4096, vf=128, vh=64, lens=P, dtype=1, n_sources=3, frames=32, kv_heads=2, dim=64)
         w = dict(n=2, sources=P, starts=P, rows=5, max_rows=0)
         x, w = tsd.StatesC(*{**x, **dict(s)}.values()), tsd.CrossBatchC(*{**w, **dict(b)}.values())
-        return L.tsd_cross_attend(ctypes.byref(x), ctypes.byref(w), heads, q, qr, qh, scale, out, orow, oh, None)
+        return L.tsd_cross_attend(ctypes.byref(x), ctypes.byref(w), heads, q, qr, qh, scale, out, orow, oh, ws, nws, None)
 
     for kw, word in [(dict(k=None), "NULL k"), (dict(v=None), "NULL v"), (dict(k=P + 8), "aligned"), (dict(kf=127), "aligned"), (dict(vh=4), "aligned"),
                      (dict(ks=-4096), "range"), (dict(vs=1 << 37), "range"), (dict(dtype=0), "dtype"), (dict(dim=96), "dim=96"),
@@ -141,7 +141,10 @@ def test_cross_refusals(L):
                      (dict(out=None), "NULL out"), (dict(qr=250), "aligned"), (dict(out=P + 2), "aligned"), (dict(oh=-64), "range"),
                      (dict(scale=math.inf), "scale"), (dict(scale=math.nan), "scale"), (dict(orow=56), "overlap"), (dict(oh=0), "overlap")]:
         refused(L, call(**kw), word)
-    refused(L, L.tsd_cross_attend(None, None, 4, P, 256, 64, 0.1, P, 256, 64, None), "NULL")
+    refused(L, L.tsd_cross_attend(None, None, 4, P, 256, 64, 0.1, P, 256, 64, None, 0, None), "NULL")
+    need = ctypes.c_int64()
+    refused(L, L.tsd_cross_attend_workspace(None, None, 4, ctypes.byref(need)), "NULL")
+    refused(L, L.tsd_cross_attend_workspace(None, None, 4, None), "NULL")
 
 
 def test_bindings_refuse():
