@@ -39,7 +39,7 @@ constexpr int kFrames = 128;  // per tile
 constexpr int kUnitRows = 256;
 constexpr int kSoftWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kFixWarp = 10;
 constexpr int kThreads = 384;  // whole warpgroups: the last warp has no work
-constexpr int kSoftRegs = 208, kOtherRegs = 80, kLaunchRegs = 168;
+constexpr int kSoftRegs = 192, kOtherRegs = 120, kLaunchRegs = 168;
 static_assert(32 * kSoftWarps * kSoftRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
 
 template <int DIM>
@@ -177,9 +177,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBar);
   uint64_t *full = bars, *empty = bars + ST, *v_ready = bars + 2 * ST;  // the ring's stages; those of values past warp 10
-  uint64_t *s_full = v_ready + ST / 2, *p_full = s_full + 2, *o_full = s_full + 4;  // [2] row tiles
-  uint64_t *q_full = s_full + 6, *drain = s_full + 7;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 8);
+  uint64_t *s_full = v_ready + ST / 2, *o_half = s_full + 2, *o_full = s_full + 4, *p_full = s_full + 6;  // [2] row tiles; [2][2] and halves of a step
+  uint64_t *q_full = s_full + 10, *drain = s_full + 11;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 12);
   const CrossAttend& a = args.a;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const Line line{a.s.kv_heads, a.group};
@@ -203,9 +203,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     for (int i = 0; i < ST / 2; ++i) mbar_init(v_ready + i, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(s_full + i, 1);
-      mbar_init(p_full + i, 4);
+      mbar_init(o_half + i, 1);
       mbar_init(o_full + i, 1);
     }
+    for (int i = 0; i < 4; ++i) mbar_init(p_full + i, 4);
     mbar_init(q_full, kSoftWarps);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -328,80 +329,102 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
           fence_after();
           const int left = p.q.len - (p.lo + j) * kFrames;  // frames from here on
           const bool whole = left >= kFrames;
-          // Weights relative to the maximum so far, without looking for this step's: one
-          // that a score has outgrown shows in the sum, and the step is taken again from its
+          // 64 frames, then 64: the first ones' values' product runs while the others' weights are
+          // made.  Weights are relative to the maximum so far, without looking for that of these 64: one
+          // that a score has outgrown shows in the sum, and they are taken again from their
           // scores, which the weights have not replaced yet.  (Sums up to 2^15: no weight then
           // reaches fp16's largest.)
-          uint32_t y[kFrames / 2];
-          float sum;
-          bool look = j == 0;
+          uint32_t raw[2][32];  // 32 scores are on their way while the ones before are worked on
+          tmem_ld32_begin(st, raw[0]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h == 1 && left <= 64) {  // nothing to see: no product reads these weights
+              tmem_ld32_wait(raw[0]);
+              break;
+            }
+            uint32_t y[32];
+            float sum;
+            bool look = h == 0 && j == 0;
 #pragma unroll 1
-          while (true) {
-            if (look) {
-              float top = -INFINITY;
+            while (true) {
+              if (look) {
+                float top = -INFINITY;
+                tmem_ld32_wait(raw[0]);
 #pragma unroll
-              for (int h = 0; h < 4; ++h) {
-                float v[32];
-                tmem_ld32(st + 32 * h, v);
+                for (int b = 0; b < 2; ++b) {
+                  float v[32];
+                  tmem_ld32(st + 64 * h + 32 * b, v);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                  const float x = whole || 32 * h + e < left ? v[e] * c : -INFINITY;
-                  top = fmaxf(top, x);
+                  for (int e = 0; e < 32; ++e) {
+                    const float x = whole || 64 * h + 32 * b + e < left ? v[e] * c : -INFINITY;
+                    top = fmaxf(top, x);
+                  }
+                }
+                const float x = fmaxf(m, top);
+                const float w = x == m ? 1.f : ex2_approx(m - x);
+                m = x;
+                l *= w;
+                if (j > 0 || h > 0) {
+                  // the last step's values are in the accumulator (this one's scores came after them); the first 64's
+                  if (h == 1 && !__all_sync(0xffffffffu, mbar_wait(o_half + tile, (uint32_t)(at0 + j) & 1u))) {
+                    dead = true;
+                    break;
+                  }
+                  fence_after();
+#pragma unroll 1
+                  for (int ch = 0; ch < DIM / 16; ++ch) {
+                    float o[16];
+                    tmem_ld16(ot + 16 * ch, o);
+                    uint32_t z[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * w);
+                    tmem_st16(ot + 16 * ch, z);
+                  }
+                }
+                tmem_ld32_begin(st + 64 * h, raw[0]);
+              }
+              const float ref = m > -INFINITY ? m - 7.f : 0.f;
+              const uint64_t ref2 = pair_of(-ref, -ref);
+              uint64_t sums[4] = {0, 0, 0, 0};
+#pragma unroll
+              for (int b = 0; b < 2; ++b) {
+                tmem_ld32_wait(raw[b]);
+                if (b == 0) tmem_ld32_begin(st + 64 * h + 32, raw[1]);
+                else if (h == 0) tmem_ld32_begin(st + 64, raw[0]);
+                float x[32];
+#pragma unroll
+                for (int e = 0; e < 32; e += 2)
+                  unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x[e], x[e + 1]);
+                if (!whole)
+#pragma unroll
+                  for (int e = 0; e < 32; ++e)
+                    if (64 * h + 32 * b + e >= left) x[e] = -INFINITY;
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) {
+                  const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
+                  sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
+                  y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
                 }
               }
-              const float x = fmaxf(m, top);
-              const float w = x == m ? 1.f : ex2_approx(m - x);
-              m = x;
-              l *= w;
-              if (j > 0) {  // (this step's scores came after the last step's values: they are in the accumulator)
-#pragma unroll 1
-                for (int ch = 0; ch < DIM / 16; ++ch) {
-                  float o[16];
-                  tmem_ld16(ot + 16 * ch, o);
-                  uint32_t z[16];
-#pragma unroll
-                  for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(o[e] * w);
-                  tmem_st16(ot + 16 * ch, z);
-                }
-              }
+              float s0, s1;
+              unpair(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), s0, s1);
+              sum = s0 + s1;
+              if (look || !__any_sync(0xffffffffu, sum > 32768.f)) break;
+              look = true;
             }
-            const float ref = m > -INFINITY ? m - 7.f : 0.f;
-            const uint64_t ref2 = pair_of(-ref, -ref);
-            uint64_t sums = 0;
-            uint32_t raw[2][16];  // 16 scores are on their way while the ones before are worked on
-            tmem_ld16_begin(st, raw[0]);
-#pragma unroll
-            for (int b = 0; b < kFrames / 16; ++b) {
-              tmem_ld16_wait(raw[b & 1]);
-              if (b + 1 < kFrames / 16) tmem_ld16_begin(st + 16 * (b + 1), raw[(b + 1) & 1]);
-              float x[16];
-#pragma unroll
-              for (int e = 0; e < 16; e += 2)
-                unpair(fma2(pair_of(__uint_as_float(raw[b & 1][e]), __uint_as_float(raw[b & 1][e + 1])), c2, ref2), x[e], x[e + 1]);
-              if (!whole)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                  if (16 * b + e >= left) x[e] = -INFINITY;
-#pragma unroll
-              for (int e = 0; e < 16; e += 2) {
-                const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
-                sums = add2(sums, pair_of(p0, p1));
-                y[8 * b + e / 2] = narrow2<BF16>(p0, p1);
-              }
-            }
-            float s0, s1;
-            unpair(sums, s0, s1);
-            sum = s0 + s1;
-            if (look || !__any_sync(0xffffffffu, sum > 32768.f)) break;
-            look = true;
+            if (dead) break;
+            l += sum;
+            tmem_st32(st + 32 * h, y);
+            tmem_st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 2 * tile + h);
           }
-          l += sum;
-          tmem_st32(st, *reinterpret_cast<const uint32_t(*)[32]>(y));
-          tmem_st32(st + 32, *reinterpret_cast<const uint32_t(*)[32]>(y + 32));
-          tmem_st_wait();
-          fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(p_full + tile);
+          if (dead) break;
+          if (left <= 64) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_full + 2 * tile + 1);
+          }
         }
         if (!dead && !mbar_wait(o_full + tile, (uint32_t)done & 1u)) dead = true;
         fence_after();
@@ -538,13 +561,19 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
           mma_commit(s_full + t);
           if (t == tiles - 1) mma_commit(empty + at % ST);
         };
-        const auto values = [&](int t, int j) {
+        const auto values = [&](int t, int j, int h) {
           const uint32_t at = at0 + 2 * (uint32_t)j + 1, vb = ring + (at % ST) * S::kTileBytes;
           const int steps = ends && j == n - 1 ? (rest + 15) / 16 : kFrames / 16;  // frames behind the length stay out
 #pragma unroll
-          for (int kk = 0; kk < kFrames / 16; ++kk)
+          for (int k = 0; k < kFrames / 32; ++k) {
+            const int kk = h * (kFrames / 32) + k;
             if (kk < steps)
               mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true, BF16), j > 0 || kk > 0);
+          }
+          if (h == 0) {
+            mma_commit(o_half + t);
+            return;
+          }
           if (j == n - 1) mma_commit(o_full + t);
           if (t == tiles - 1) mma_commit(empty + at % ST);
         };
@@ -552,12 +581,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
         for (int t = 0; t < tiles && ok; ++t) scores(t, 0);
         for (int j = 0; j < n && ok; ++j) {
           for (int t = 0; t < tiles && ok; ++t) {
-            ok = mbar_wait(p_full + t, (tile_at[t] + j) & 1u);
+            ok = mbar_wait(p_full + 2 * t, (tile_at[t] + j) & 1u);
             if (ok && t == 0) ok = have(at0 + 2 * j + 1);
             if (ok && t == 0) ok = mbar_wait(v_ready + (at0 + 2 * j + 1) % ST / 2, ((at0 + 2 * j + 1) / ST) & 1u);
             if (!ok) break;
             fence_after();
-            values(t, j);
+            values(t, j, 0);
+            ok = mbar_wait(p_full + 2 * t + 1, (tile_at[t] + j) & 1u);
+            if (!ok) break;
+            fence_after();
+            values(t, j, 1);
             if (j + 1 < n) {
               if (t == 0) ok = have(at0 + 2 * j + 2);
               if (ok) scores(t, j + 1);
