@@ -78,7 +78,8 @@ extern "C" tsd_status tsd_cross_attend(const tsd_states* states, const tsd_cross
   a.scale = scale;
   cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
   CrossTilesPlan p;
-  if (cross_tiles_plan(s, b, heads, sms, &p)) {
+  // (queries that share memory are no tensor that TMA takes)
+  if ((heads == 1 || q_head > 0) && (b.rows == 1 || q_row > 0) && cross_tiles_plan(s, b, heads, sms, &p)) {
     if (p.bytes > 0 && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
       return fail(TSD_EINVAL, "tsd_cross_attend: workspace of %lld bytes, %lld needed (16-byte aligned)", (long long)workspace_bytes, (long long)p.bytes);
     TSD_CUDA(cross_tiles_launch(a, p, workspace, stream));

@@ -23,7 +23,7 @@
 // long ones fill the device alike.  A unit that several CTAs share leaves its parts in the workspace, which a
 // second kernel joins in their order.
 #include <algorithm>
-#include <climits>
+#include <type_traits>
 
 #include "cross.h"
 #include "launch.h"
@@ -36,7 +36,7 @@ namespace {
 using namespace tc;
 
 constexpr int kFrames = 128;  // per tile
-constexpr int kUnitRows = 256;
+constexpr int kUnitRows = 256;  // of which a row tile takes whole tokens' heads: 128 / group tokens
 constexpr int kSoftWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kFixWarp = 10;
 constexpr int kThreads = 384;  // whole warpgroups: the last warp has no work
 constexpr int kSoftRegs = 192, kOtherRegs = 120, kLaunchRegs = 168;
@@ -49,15 +49,16 @@ struct TilesShape {
   static constexpr int kStages = DIM == 128 ? 4 : 8;
   static constexpr int kQ = 0;
   static constexpr int kRing = 2 * kTileBytes;
-  static constexpr int kBar = kRing + kStages * kTileBytes;
+  static constexpr int kKnown = kRing + kStages * kTileBytes;  // sequences of a small call
+  static constexpr int kBar = kKnown + kThreads * (int)sizeof(CrossSeq);
   static constexpr int kSmem = kBar + 512 + 1024;
   static constexpr int kO = 256;  // TMEM: the row tiles' scores at 0 and 128; accumulators from here
 };
 
 static_assert(TilesShape<64>::kStages % 2 == 0 && TilesShape<128>::kStages % 2 == 0, "keys in even stages, values in odd ones");
 
-// What a unit and its tiles cost, in fifths of a tile of two row tiles.
-constexpr int kPad = 5, kTwo = 5, kOne = 3, kLeast = 20;
+// What a unit and its tiles cost, in sixteenths of a tile of two row tiles.
+constexpr int kPad = 32, kTwo = 16, kOne = 15, kLeast = 64;
 
 struct TilesArgs {
   CrossAttend a;
@@ -65,13 +66,20 @@ struct TilesArgs {
   float2* part_ml;  // (maximum, sum) of those rows
   int4* joins;      // [2 * CTAs]: the second one's place
   int k_heads, k_sources, v_heads, v_sources;  // 0: the coordinate is 0 (stride 0)
+  int tokens;       // of a row tile
+  bool wide;        // results allow 32-byte stores
 };
 
+// a / b; mostly small numbers
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
+
 struct Line {
-  int kv, group;
-  __device__ __forceinline__ int units(const CrossSeq& q) const { return (int)(((int64_t)q.count * group + kUnitRows - 1) / kUnitRows); }
+  int kv, tokens;  // key heads; tokens of a row tile
+  __device__ __forceinline__ int units(const CrossSeq& q) const { return (q.count + 2 * tokens - 1) / (2 * tokens); }
   static __device__ __forceinline__ int tiles(const CrossSeq& q) { return max(1, (q.len + kFrames - 1) / kFrames); }
-  __device__ __forceinline__ bool two(const CrossSeq& q, int u) const { return (int64_t)q.count * group - (int64_t)u * kUnitRows > 128; }
+  __device__ __forceinline__ bool two(const CrossSeq& q, int u) const { return q.count - 2 * u * tokens > tokens; }
   static __device__ __forceinline__ int64_t unit(int tiles, bool two) { return kPad + (int64_t)tiles * (two ? kTwo : kOne); }
   __device__ __forceinline__ int64_t head(const CrossSeq& q) const {
     const int n = units(q), t = tiles(q);
@@ -83,7 +91,7 @@ struct Line {
 // One CTA's share of a unit.
 struct Part {
   CrossSeq q;
-  int head, row0;   // row0: of the sequence's count * group
+  int head, tok0;   // the key head; the unit's first token
   int lo, hi, all;  // tiles of frames lo .. hi - 1 of all
   int n;            // those to compute (0 where a row sees nothing)
   int64_t at;       // the unit's place in the line
@@ -94,24 +102,25 @@ struct Part {
 // (which begins at place `at`) on.  A warp holds 32 sequences at a time.
 struct Walk {
   const CrossAttend& a;
+  const CrossSeq* known;  // [n], or NULL: in the call's arrays
   Line line;
-  int64_t at, lo, hi, next_unit;
+  int64_t at, lo, hi;
   int lane, base, i, head, u, units, tiles;
   CrossSeq w, q;
-  __device__ __forceinline__ Walk(const CrossAttend& args, int64_t place, int64_t from, int64_t to, int seq)
-      : a(args), line{args.s.kv_heads, args.group}, at(place), lo(from), hi(to), lane(threadIdx.x & 31), base(seq), i(seq) {
+  __device__ __forceinline__ Walk(const CrossAttend& args, const Line& l, const CrossSeq* sequences, int64_t place, int64_t from, int64_t to, int seq)
+      : a(args), known(sequences), line(l), at(place), lo(from), hi(to), lane(threadIdx.x & 31), base(seq), i(seq) {
     window();
     take();
     if (units == 0) return;  // (a share begins inside a sequence)
     const int64_t per = line.head(q);
-    head = (int)min((lo - at) / per, (int64_t)line.kv - 1);
+    head = (int)min(quotient(lo - at, per), (int64_t)line.kv - 1);
     at += head * per;
-    u = (int)min((lo - at) / Line::unit(tiles, true), (int64_t)units - 1);
+    u = (int)min(quotient(lo - at, Line::unit(tiles, true)), (int64_t)units - 1);
     at += u * Line::unit(tiles, true);
   }
   __device__ __forceinline__ void window() {
     w.source = w.len = w.row0 = w.count = 0, w.ok = false;
-    if (base + lane < a.b.n) w = cross_seq(a.s, a.b, base + lane);
+    if (base + lane < a.b.n) w = known ? known[base + lane] : cross_seq(a.s, a.b, base + lane);
   }
   __device__ __forceinline__ void take() {
     const int l = i - base;
@@ -143,12 +152,14 @@ struct Walk {
         if (++head >= line.kv && !sequence()) return false;
       }
       if (units == 0) return false;
-      p.q = q, p.head = head, p.row0 = u * kUnitRows, p.at = at, p.all = tiles;
+      p.q = q, p.head = head, p.tok0 = 2 * u * line.tokens, p.at = at, p.all = tiles;
       p.two = line.two(q, u);
-      const int cost = p.two ? kTwo : kOne;
       const auto first = [&](int64_t place) {  // the first tile that begins there or later
         const int64_t x = place - at - kPad;
-        return x <= 0 ? 0 : (int)min((x + cost - 1) / cost, (int64_t)tiles);
+        if (x <= 0) return 0;
+        if (x >= (int64_t)tiles * (p.two ? kTwo : kOne)) return tiles;
+        const uint32_t y = (uint32_t)x;
+        return (int)(p.two ? (y + kTwo - 1) / kTwo : (y + kOne - 1) / kOne);
       };
       p.lo = first(lo), p.hi = first(hi);
       at += Line::unit(tiles, p.two);
@@ -160,6 +171,24 @@ struct Walk {
   }
 };
 
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+               : "memory");
+}
+
+// Eight words at a 16-byte, or (wide) 32-byte boundary: the lanes' rows lie apart, and a whole sector goes out at once.
+__device__ __forceinline__ void store32(uint16_t* to, const uint32_t (&z)[8], bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]), "r"(z[4]), "r"(z[5]),
+                 "r"(z[6]), "r"(z[7])
+                 : "memory");
+  } else {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(z[0], z[1], z[2], z[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(z[4], z[5], z[6], z[7]);
+  }
+}
+
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int x, int y, int z, int w) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
                "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
@@ -167,8 +196,8 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 }
 
 template <bool BF16, int DIM>
-__global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_constant__ TilesArgs args, const __grid_constant__ CUtensorMap k_map,
-                                                             const __grid_constant__ CUtensorMap v_map) {
+__global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_constant__ TilesArgs args, const __grid_constant__ CUtensorMap q_map,
+                                                             const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
   using S = TilesShape<DIM>;
   constexpr int ST = S::kStages;
   extern __shared__ unsigned char smem_raw[];
@@ -178,16 +207,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBar);
   uint64_t *full = bars, *empty = bars + ST, *v_ready = bars + 2 * ST;  // the ring's stages; those of values past warp 10
   uint64_t *s_full = v_ready + ST / 2, *o_half = s_full + 2, *o_full = s_full + 4, *p_full = s_full + 6;  // [2] row tiles; [2][2] and halves of a step
-  uint64_t *q_full = s_full + 10, *drain = s_full + 11;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 12);
+  uint64_t *q_full = s_full + 10, *q_empty = s_full + 11, *drain = s_full + 12;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 13);
   const CrossAttend& a = args.a;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
-  const Line line{a.s.kv_heads, a.group};
+  const Line line{a.s.kv_heads, args.tokens};
 
   // The line's length and this CTA's share: a thread's run of sequences, then the threads'.
   const int run = (a.b.n + kThreads - 1) / kThreads, run0 = min((int)threadIdx.x * run, a.b.n), run1 = min(run0 + run, a.b.n);
+  CrossSeq* known = run == 1 ? reinterpret_cast<CrossSeq*>(smem + S::kKnown) : nullptr;
   int64_t mine = 0;
-  for (int i = run0; i < run1; ++i) mine += line.seq(cross_seq(a.s, a.b, i));
+  for (int i = run0; i < run1; ++i) {
+    const CrossSeq q = cross_seq(a.s, a.b, i);
+    if (known) known[i] = q;
+    mine += line.seq(q);
+  }
   int64_t upto = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -195,6 +229,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     if (lane >= o) upto += x;
   }
   if (lane == 31) s_sums[warp] = upto;
+  if (warp == kTmaWarp && lane < 3)
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0 ? &q_map : lane == 1 ? &k_map : &v_map)) : "memory");
   if (threadIdx.x == 0) {
     for (int i = 0; i < ST; ++i) {
       mbar_init(full + i, 1);
@@ -207,7 +243,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
       mbar_init(o_full + i, 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(p_full + i, 4);
-    mbar_init(q_full, kSoftWarps);
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -219,7 +256,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     if (i < warp) upto += x;
     total += x;
   }
-  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kLeast);
+  const int64_t share = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kLeast);
   const int64_t lo = share * blockIdx.x, hi = min(lo + share, total);
   if (lo >= hi) {
     if (args.joins && threadIdx.x == 0) args.joins[2 * blockIdx.x + 1].x = -1;
@@ -228,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   if (upto - mine <= lo && lo < upto) {
     int64_t x = upto - mine;
     for (int i = run0; i < run1; ++i) {
-      const int64_t y = line.seq(cross_seq(a.s, a.b, i));
+      const int64_t y = known ? mine : line.seq(cross_seq(a.s, a.b, i));
       if (lo < x + y) {
         s_seq = i, s_place = x;
         break;
@@ -244,20 +281,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk walk(a, s_place, lo, hi, s_seq);
+  Walk walk(a, line, known, s_place, lo, hi, s_seq);
   Part p;
   // A wait that runs out ends its role; the others' waits on it run out in turn, and the
   // rows from there on say NaN.
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int tile = warp >> 2;
-    // Queries and results pass through shared memory row by row, kRowLanes lanes each: 16
-    // bytes of a row of the warp's, in the 128-byte swizzle
-    constexpr int kRowLanes = DIM / 8, kRowsPer = 32 / kRowLanes;
-    const auto chunk = [&](int row, int c) {
-      return reinterpret_cast<uint4*>(smem + S::kQ + tile * S::kTileBytes + (c >> 3) * S::kHalf + ((warp & 3) * 32 + row) * 128 + (((c ^ row) & 7) << 4));
-    };
-    const int step_tok = kRowsPer / a.group, step_h = kRowsPer % a.group;
+    const int row = threadIdx.x % 128, row_tok = tile * args.tokens + row / a.group, row_h = row % a.group;  // the thread's, of a unit
+    const bool used = row < args.tokens * a.group;
     const uint32_t st = tmem + (uint32_t)(tile * 128) + ((uint32_t)((warp & 3) * 32) << 16);  // scores, then weights
     const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
     const float c = a.scale * kLog2e;
@@ -265,57 +297,30 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     const float nan = __uint_as_float(0x7fc00000u);
     int at0 = 0, done = 0;  // steps and parts of this row tile so far
     bool fine = true, join = false;
-    // (a warp of a row tile that has no rows must not arrive for the next one's queries early)
-    const auto row_tile_end = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * kSoftWarps) : "memory"); };
     while (walk.next(p)) {
-      const int rows = p.q.count * a.group, r = p.row0 + threadIdx.x, wr = p.row0 + (threadIdx.x & ~31);
+      const int tok = p.tok0 + row_tok;
+      const bool live = used && tok < p.q.count;
+      uint16_t* const dst = a.out + (int64_t)(p.q.row0 + tok) * a.out_row + (int64_t)(p.head * a.group + row_h) * a.out_head;
       const bool whole_unit = p.lo == 0 && p.hi == p.all;
       const int slot = 2 * (int)blockIdx.x + (p.lo == 0 ? 1 : 0);
       if (!whole_unit && p.lo == 0) {
         join = true;
         if (threadIdx.x == 0) {  // (an exact division: this CTA's share is followed by whole ones)
-          const int64_t last = (p.at + kPad + (int64_t)(p.all - 1) * (p.two ? kTwo : kOne)) / share;
-          args.joins[slot - 1] = make_int4(p.q.row0, rows, p.row0, p.head);
+          const int64_t last = quotient(p.at + kPad + (int64_t)(p.all - 1) * (p.two ? kTwo : kOne), share);
+          args.joins[slot - 1] = make_int4(p.q.row0, p.q.count, p.tok0, p.head);
           args.joins[slot].x = (int)min(last, (int64_t)gridDim.x - 1);
         }
       }
       if (p.n == 0 || !fine) {
-        if (r < rows) {
-          const int tok = p.q.row0 + r / a.group, h = p.head * a.group + r % a.group;
+        if (live) {
           const uint32_t x = p.q.ok && fine ? 0u : BF16 ? 0x7fc07fc0u : 0x7e007e00u;
           if (whole_unit) {
-            uint4* dst = reinterpret_cast<uint4*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head);
-            for (int i = 0; i < DIM / 8; ++i) dst[i] = make_uint4(x, x, x, x);
+            for (int i = 0; i < DIM / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(x, x, x, x);
           } else {
             args.part_ml[(size_t)slot * kUnitRows + threadIdx.x] = make_float2(0.f, nan);
           }
         }
-        if (p.n > 0) row_tile_end();
         continue;
-      }
-      // the rows that a lane copies, from the first on
-      const int r0 = wr + lane / kRowLanes, tok0 = r0 / a.group, h0 = p.head * a.group + r0 - tok0 * a.group;
-      const auto next_row = [&](int& t, int& h) {
-        t += step_tok;
-        h += step_h;
-        if (h >= (p.head + 1) * a.group) h -= a.group, ++t;
-      };
-      {
-        int t = tok0, h = h0;
-#pragma unroll
-        for (int i = 0; i < kRowLanes; ++i) {
-          const int rw = i * kRowsPer + lane / kRowLanes;
-          const uint16_t* src = a.q + (int64_t)(p.q.row0 + t) * a.q_row + (int64_t)h * a.q_head + 8 * (lane % kRowLanes);
-          if (wr + rw < rows)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(chunk(rw, lane % kRowLanes))), "l"(src) : "memory");
-          else
-            *chunk(rw, lane % kRowLanes) = make_uint4(0, 0, 0, 0);
-          next_row(t, h);
-        }
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(q_full);
       }
       bool dead = false;
       if (tile == 0 || p.two) {
@@ -386,30 +391,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
               const float ref = m > -INFINITY ? m - 7.f : 0.f;
               const uint64_t ref2 = pair_of(-ref, -ref);
               uint64_t sums[4] = {0, 0, 0, 0};
+              const auto weigh = [&](auto masked) {  // a branch for the whole of it: masks in all steps cost 250 clocks
 #pragma unroll
-              for (int b = 0; b < 2; ++b) {
-                tmem_ld32_wait(raw[b]);
-                if (b == 0) tmem_ld32_begin(st + 64 * h + 32, raw[1]);
-                else if (h == 0) tmem_ld32_begin(st + 64, raw[0]);
-                float x[32];
+                for (int b = 0; b < 2; ++b) {
+                  tmem_ld32_wait(raw[b]);
+                  if (b == 0) tmem_ld32_begin(st + 64 * h + 32, raw[1]);
+                  else if (h == 0) tmem_ld32_begin(st + 64, raw[0]);
+                  float x[32];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2)
-                  unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x[e], x[e + 1]);
-                if (!whole)
+                  for (int e = 0; e < 32; e += 2)
+                    unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x[e], x[e + 1]);
+                  if constexpr (decltype(masked)::value)
 #pragma unroll
-                  for (int e = 0; e < 32; ++e)
-                    if (64 * h + 32 * b + e >= left) x[e] = -INFINITY;
+                    for (int e = 0; e < 32; ++e)
+                      if (64 * h + 32 * b + e >= left) x[e] = -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                  const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
-                  sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
-                  y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
+                  for (int e = 0; e < 32; e += 2) {
+                    const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
+                    sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
+                    y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
+                  }
                 }
-              }
+              };
+              if (whole) weigh(std::false_type{});
+              else weigh(std::true_type{});
               float s0, s1;
               unpair(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), s0, s1);
               sum = s0 + s1;
-              if (look || !__any_sync(0xffffffffu, sum > 32768.f)) break;
+              if (look || !__any_sync(0xffffffffu, live && sum > 32768.f)) break;
               look = true;
             }
             if (dead) break;
@@ -430,56 +439,39 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
         fence_after();
         dead = __any_sync(0xffffffffu, dead);
         if (dead) l = nan;
-        // results, through shared memory: neighbouring lanes write a row
+        // results: a thread its row
         if (whole_unit) {
           const float inv = 1.f / l;
 #pragma unroll
           for (int ch = 0; ch < DIM / 32; ++ch) {
             float v[32];
             tmem_ld32(ot + 32 * ch, v);
+            if (live)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *chunk(lane, 4 * ch + i) = make_uint4(narrow2<BF16>(v[8 * i] * inv, v[8 * i + 1] * inv), narrow2<BF16>(v[8 * i + 2] * inv, v[8 * i + 3] * inv),
-                                                    narrow2<BF16>(v[8 * i + 4] * inv, v[8 * i + 5] * inv), narrow2<BF16>(v[8 * i + 6] * inv, v[8 * i + 7] * inv));
+              for (int i = 0; i < 2; ++i) {
+                uint32_t z[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = narrow2<BF16>(v[16 * i + 2 * e] * inv, v[16 * i + 2 * e + 1] * inv);
+                store32(dst + 32 * ch + 16 * i, z, args.wide);
+              }
           }
-          __syncwarp();
-          int t = tok0, h = h0;
-#pragma unroll 8
-          for (int i = 0; i < kRowLanes; ++i) {
-            const int rw = i * kRowsPer + lane / kRowLanes;
-            if (wr + rw < rows)
-              *reinterpret_cast<uint4*>(a.out + (int64_t)(p.q.row0 + t) * a.out_row + (int64_t)h * a.out_head + 8 * (lane % kRowLanes)) = *chunk(rw, lane % kRowLanes);
-            next_row(t, h);
+        } else {  // [DIM / 4][rows] of four: neighbouring lanes write a column
+          float4* to = reinterpret_cast<float4*>(args.part) + (size_t)slot * (DIM / 4) * kUnitRows + threadIdx.x;
+#pragma unroll
+          for (int ch = 0; ch < DIM / 32; ++ch) {
+            float v[32];
+            tmem_ld32(ot + 32 * ch, v);
+            if (live)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) to[(8 * ch + i) * kUnitRows] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           }
-          __syncwarp();
-        } else {
-          float* to = args.part + ((size_t)slot * kUnitRows + (threadIdx.x & ~31)) * DIM + 4 * (lane % kRowLanes);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {  // half of the dimensions, fp32
-#pragma unroll
-            for (int ch = 0; ch < DIM / 64; ++ch) {
-              float v[32];
-              tmem_ld32(ot + half * (DIM / 2) + 32 * ch, v);
-#pragma unroll
-              for (int i = 0; i < 8; ++i)
-                *chunk(lane, 8 * ch + i) = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-            }
-            __syncwarp();
-#pragma unroll 8
-            for (int i = 0; i < kRowLanes; ++i) {
-              const int rw = i * kRowsPer + lane / kRowLanes;
-              if (wr + rw < rows) *reinterpret_cast<uint4*>(to + (size_t)rw * DIM + half * (DIM / 2)) = *chunk(rw, lane % kRowLanes);
-            }
-            __syncwarp();
-          }
-          args.part_ml[(size_t)slot * kUnitRows + threadIdx.x] = make_float2(m, l);
+          if (live) args.part_ml[(size_t)slot * kUnitRows + threadIdx.x] = make_float2(m, l);
         }
         at0 += p.n;
         ++done;
       }
       fence_before();
       fine = !dead;
-      row_tile_end();
     }
     if (threadIdx.x == 0 && args.joins && !join) args.joins[2 * blockIdx.x + 1].x = -1;
     asm volatile("bar.arrive 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");
@@ -487,10 +479,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   }
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));  // one instruction for the whole warpgroup
   if (warp == kTmaWarp) {
-    uint32_t at = 0;  // tiles through the ring, keys and values
+    uint32_t at = 0, parts = 0;  // tiles through the ring, keys and values; parts with any
     bool dead = false;
     while (!dead && walk.next(p)) {
       if (elect()) {
+        bool asked = false;
         for (int j = 0; j < p.n && !dead; ++j) {
 #pragma unroll
           for (int kind = 0; kind < 2 && !dead; ++kind, ++at) {
@@ -504,11 +497,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
             for (int h = 0; h < DIM / 64; ++h)
               tma_load_4d(smem_u32(smem + S::kRing + s * S::kTileBytes + h * S::kHalf), kind ? &v_map : &k_map, full + s, 64 * h, (p.lo + j) * kFrames,
                           kind ? p.head * args.v_heads : p.head * args.k_heads, kind ? p.q.source * args.v_sources : p.q.source * args.k_sources);
+            if (j == 0 && kind == 0) {  // the queries, once the last part's have been used
+              if (parts > 0 && !mbar_wait(q_empty, (parts - 1) & 1u)) {
+                dead = true;
+                ++at;
+                break;
+              }
+              const int tiles = p.two ? 2 : 1;
+              mbar_expect_tx(q_full, tiles * (DIM / 64) * args.tokens * a.group * 128);
+              for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                for (int h = 0; h < DIM / 64; ++h)
+                  tma_load_3d(smem_u32(smem + S::kQ + t * S::kTileBytes + h * S::kHalf), &q_map, q_full, 64 * h, p.head * a.group,
+                              p.q.row0 + p.tok0 + t * args.tokens);
+              asked = true;
+            }
           }
         }
-        if (dead)  // what is on its way ends first
+        if (dead) {  // what is on its way ends first
           for (uint32_t i = at - min(at, (uint32_t)ST); i < at; ++i) mbar_wait(full + i % ST, (i / ST) & 1u);
+          if (asked) mbar_wait(q_full, parts & 1u);
+        }
       }
+      parts += p.n > 0;
       dead = __any_sync(0xffffffffu, dead);
       at = __reduce_max_sync(0xffffffffu, at);
     }
@@ -560,6 +571,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                        idesc_f16(128, kFrames, false, BF16), kk > 0);
           mma_commit(s_full + t);
           if (t == tiles - 1) mma_commit(empty + at % ST);
+          if (t == tiles - 1 && j == n - 1) mma_commit(q_empty);
         };
         const auto values = [&](int t, int j, int h) {
           const uint32_t at = at0 + 2 * (uint32_t)j + 1, vb = ring + (at % ST) * S::kTileBytes;
@@ -616,39 +628,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   }
 }
 
-// The units that several CTAs share: block (c, y) takes kJoinRows rows of the one that CTA c began.
-constexpr int kJoinRows = 16, kJoinWarps = 4;
-
+// The units that several CTAs share: blocks (c, ..) take the one that CTA c began.
+// A warp takes 32 rows and 16 of their dimensions.
 template <bool BF16, int DIM>
-__global__ void __launch_bounds__(32 * kJoinWarps) k_cross_join(const __grid_constant__ TilesArgs args) {
-  const int c = blockIdx.x, last = __ldg(&args.joins[2 * c + 1].x);
-  if (last < 0) return;
+__global__ void __launch_bounds__(2 * DIM) k_cross_join(const __grid_constant__ TilesArgs args) {
+  const int c = blockIdx.x, warp = threadIdx.x >> 5, rr = blockIdx.y * 32 + (threadIdx.x & 31), row = rr % 128;
   const CrossAttend& a = args.a;
-  const int4 place = __ldg(args.joins + 2 * c);  // the sequence's first row, its rows * group, the unit's first, key head
-  constexpr int kLanes = DIM / 4, kPer = 32 / kLanes;  // lanes per row, rows per warp
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = last - c + 1;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int4 place = args.joins[2 * c];  // the sequence's first row and its tokens, the unit's first token, the key head
+  const int parts = args.joins[2 * c + 1].x - c + 1, tok = place.z + rr / 128 * args.tokens + row / a.group;
+  if (parts < 2 || row >= args.tokens * a.group || tok >= place.y) return;
   const auto slot = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)); };
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int k = 0; k < parts; ++k) top = fmaxf(top, args.part_ml[slot(k) * kUnitRows + rr].x);
+  float acc[16], sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kJoinRows / (kJoinWarps * kPer); ++i) {
-    const int rr = blockIdx.y * kJoinRows + (i * kJoinWarps + warp) * kPer + lane / kLanes, r = place.z + rr;
-    if (r >= place.y) continue;
-    float top = -INFINITY;
-    for (int k = 0; k < parts; ++k) top = fmaxf(top, __ldg(&args.part_ml[slot(k) * kUnitRows + rr].x));
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+  for (int e = 0; e < 16; ++e) acc[e] = 0.f;
 #pragma unroll 2
-    for (int k = 0; k < parts; ++k) {
-      const float2 x = __ldg(args.part_ml + slot(k) * kUnitRows + rr);
-      const float4 v = __ldg(reinterpret_cast<const float4*>(args.part + (slot(k) * kUnitRows + rr) * DIM) + lane % kLanes);
-      const float f = x.x == top ? 1.f : ex2_approx(x.x - top);  // (top -inf: every score is, and 0 / 0 is the result)
-      sum = fmaf(f, x.y, sum);
-      acc.x = fmaf(f, v.x, acc.x), acc.y = fmaf(f, v.y, acc.y), acc.z = fmaf(f, v.z, acc.z), acc.w = fmaf(f, v.w, acc.w);
+  for (int k = 0; k < parts; ++k) {
+    const float2 x = args.part_ml[slot(k) * kUnitRows + rr];
+    const float4* from = reinterpret_cast<const float4*>(args.part) + (slot(k) * (DIM / 4) + 4 * warp) * kUnitRows + rr;
+    const float f = x.x == top ? 1.f : ex2_approx(x.x - top);  // (top -inf: every score is, and 0 / 0 is the result)
+    sum = fmaf(f, x.y, sum);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 v = from[i * kUnitRows];
+      acc[4 * i] = fmaf(f, v.x, acc[4 * i]), acc[4 * i + 1] = fmaf(f, v.y, acc[4 * i + 1]);
+      acc[4 * i + 2] = fmaf(f, v.z, acc[4 * i + 2]), acc[4 * i + 3] = fmaf(f, v.w, acc[4 * i + 3]);
     }
-    const float inv = 1.f / sum;
-    const int tok = place.x + r / a.group, h = place.w * a.group + r % a.group;
-    *reinterpret_cast<uint2*>(a.out + (int64_t)tok * a.out_row + (int64_t)h * a.out_head + 4 * (lane % kLanes)) =
-        make_uint2(narrow2<BF16>(acc.x * inv, acc.y * inv), narrow2<BF16>(acc.z * inv, acc.w * inv));
   }
+  const float inv = 1.f / sum;
+  uint32_t z[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z[e] = narrow2<BF16>(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+  store32(a.out + (int64_t)(place.x + tok) * a.out_row + (int64_t)(place.w * a.group + row % a.group) * a.out_head + 16 * warp, z, args.wide);
 }
 
 // Keys or values as [sources][heads][frames][dim], a dimension of stride 0 as one of size 1.
@@ -663,8 +677,19 @@ bool make_states_map(CUtensorMap* m, const tsd_states& s, const void* base, int6
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Queries as [rows][heads][dim], in boxes of a row tile's tokens and a key head's heads.
+bool make_queries_map(CUtensorMap* m, const CrossAttend& a, int tokens) {
+  const EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)a.s.dim, (cuuint64_t)a.heads, (cuuint64_t)a.b.rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)(a.heads > 1 ? a.q_head : a.s.dim) * 2, (cuuint64_t)(a.b.rows > 1 ? a.q_row : a.s.dim) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)tokens}, es[3] = {1, 1, 1};
+  return fn(m, a.s.dtype == TSD_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t*>(a.q), dims, strides, box, es,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <bool BF16, int DIM>
-cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
+cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, cudaStream_t s) {
   using S = TilesShape<DIM>;
   static const bool enough = [] {  // setmaxnreg waits for registers that the launch did not bring
     cudaFuncAttributes at{};
@@ -673,9 +698,19 @@ cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtenso
   if (!enough) return cudaErrorLaunchOutOfResources;
   const cudaError_t e = smem_opt_in<k_cross_tiles<BF16, DIM>>(S::kSmem);
   if (e != cudaSuccess) return e;
-  k_cross_tiles<BF16, DIM><<<p.ctas, kThreads, S::kSmem, s>>>(args, k, v);
-  if (p.bytes > 0) k_cross_join<BF16, DIM><<<dim3(p.ctas, kUnitRows / kJoinRows), 32 * kJoinWarps, 0, s>>>(args);
-  return cudaGetLastError();
+  k_cross_tiles<BF16, DIM><<<p.ctas, kThreads, S::kSmem, s>>>(args, q, k, v);
+  const cudaError_t launched = cudaGetLastError();
+  if (launched != cudaSuccess || p.bytes == 0) return launched;
+  cudaLaunchConfig_t c{};
+  c.gridDim = dim3((unsigned)p.ctas, kUnitRows / 32);
+  c.blockDim = 2 * DIM;
+  c.stream = s;
+  cudaLaunchAttribute at{};  // its blocks come while the last CTAs end, and wait for them
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = &at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, k_cross_join<BF16, DIM>, args);
 }
 
 }  // namespace
@@ -685,7 +720,7 @@ bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, 
   const int64_t most = std::max<int64_t>(1, b.max_rows ? std::min(b.max_rows, b.rows) : !b.starts ? 1 : ((int64_t)b.rows + b.n - 1) / b.n);
   if (most * group <= 48 || s.k_frame < s.dim || s.v_frame < s.dim) return false;
   const int64_t tiles = ((int64_t)s.frames + kFrames - 1) / kFrames;
-  const int64_t units = s.kv_heads * (((int64_t)b.rows * group + kUnitRows - 1) / kUnitRows + b.n);  // at most
+  const int64_t units = s.kv_heads * ((int64_t)b.rows / (2 * (128 / group)) + b.n);  // at most
   const double line = (double)units * (double)(kPad + tiles * kTwo);
   p->ctas = (int)std::max(1.0, std::min((double)sms, std::ceil(line / kLeast)));
   // one tile of frames is never shared
@@ -695,8 +730,9 @@ bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, 
 
 cudaError_t cross_tiles_launch(const CrossAttend& a, const CrossTilesPlan& p, void* workspace, cudaStream_t s) {
   const bool bf = a.s.dtype == TSD_BF16;
-  CUtensorMap k, v;
-  if (!make_states_map(&k, a.s, a.s.k, a.s.k_source, a.s.k_frame, a.s.k_head) || !make_states_map(&v, a.s, a.s.v, a.s.v_source, a.s.v_frame, a.s.v_head))
+  const int tokens = 128 / a.group;
+  CUtensorMap q, k, v;
+  if (!make_queries_map(&q, a, tokens) || !make_states_map(&k, a.s, a.s.k, a.s.k_source, a.s.k_frame, a.s.k_head) || !make_states_map(&v, a.s, a.s.v, a.s.v_source, a.s.v_frame, a.s.v_head))
     return cudaErrorInvalidValue;
   TilesArgs t{};
   t.a = a;
@@ -705,9 +741,11 @@ cudaError_t cross_tiles_launch(const CrossAttend& a, const CrossTilesPlan& p, vo
     t.part_ml = reinterpret_cast<float2*>(t.part + (size_t)2 * p.ctas * kUnitRows * a.s.dim);
     t.joins = reinterpret_cast<int4*>(t.part_ml + (size_t)2 * p.ctas * kUnitRows);
   }
+  t.tokens = tokens;
+  t.wide = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.out_row % 16 == 0 && a.out_head % 16 == 0;
   t.k_heads = a.s.k_head != 0, t.k_sources = a.s.k_source != 0, t.v_heads = a.s.v_head != 0, t.v_sources = a.s.v_source != 0;
-  return a.s.dim == 64 ? (bf ? launch<true, 64>(t, p, k, v, s) : launch<false, 64>(t, p, k, v, s))
-                       : (bf ? launch<true, 128>(t, p, k, v, s) : launch<false, 128>(t, p, k, v, s));
+  return a.s.dim == 64 ? (bf ? launch<true, 64>(t, p, q, k, v, s) : launch<false, 64>(t, p, q, k, v, s))
+                       : (bf ? launch<true, 128>(t, p, q, k, v, s) : launch<false, 128>(t, p, q, k, v, s));
 }
 
 }  // namespace tsd
