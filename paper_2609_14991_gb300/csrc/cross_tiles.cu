@@ -640,12 +640,12 @@ __global__ void __launch_bounds__(2 * DIM) k_cross_join(const __grid_constant__ 
   if (parts < 2 || row >= args.tokens * a.group || tok >= place.y) return;
   const auto slot = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)); };
   float top = -INFINITY;
-#pragma unroll 4
+#pragma unroll 8
   for (int k = 0; k < parts; ++k) top = fmaxf(top, args.part_ml[slot(k) * kUnitRows + rr].x);
   float acc[16], sum = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 2
+#pragma unroll 4
   for (int k = 0; k < parts; ++k) {
     const float2 x = args.part_ml[slot(k) * kUnitRows + rr];
     const float4* from = reinterpret_cast<const float4*>(args.part) + (slot(k) * (DIM / 4) + 4 * warp) * kUnitRows + rr;
