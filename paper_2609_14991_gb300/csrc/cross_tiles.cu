@@ -12,7 +12,8 @@
 //   warp 8      copies keys and values, a ring of tiles by TMA (128-byte swizzle);
 //   warp 9      issues the MMAs;
 //   warp 10     zeroes what stands behind a source's length in its last tile of values: a
-//               weight of 0 does not make a NaN or infinity 0.
+//               weight of 0 does not make a NaN or infinity 0;
+//   warp 11     says which parts of the work are this CTA's.
 // While one row tile's scores are with the softmax, the other's products run.  Keys are the K-major B
 // operand of the scores; the same layout of the values is read as an MN-major B
 // operand, so neither is transposed.  The maximum is looked for, and the accumulator rescaled in
@@ -38,7 +39,8 @@ using namespace tc;
 constexpr int kFrames = 128;  // per tile
 constexpr int kUnitRows = 256;  // of which a row tile takes whole tokens' heads: 128 / group tokens
 constexpr int kSoftWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kFixWarp = 10;
-constexpr int kThreads = 384;  // whole warpgroups: the last warp has no work
+constexpr int kPlanWarp = 11, kReaders = 11;  // the warps that follow its parts
+constexpr int kThreads = 384, kPlanned = 4;
 constexpr int kSoftRegs = 192, kOtherRegs = 120, kLaunchRegs = 168;
 static_assert(32 * kSoftWarps * kSoftRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
 
@@ -50,7 +52,8 @@ struct TilesShape {
   static constexpr int kQ = 0;
   static constexpr int kRing = 2 * kTileBytes;
   static constexpr int kKnown = kRing + kStages * kTileBytes;  // sequences of a small call
-  static constexpr int kBar = kKnown + kThreads * (int)sizeof(CrossSeq);
+  static constexpr int kParts = kKnown + kThreads * (int)sizeof(CrossSeq);
+  static constexpr int kBar = kParts + kPlanned * 48;
   static constexpr int kSmem = kBar + 512 + 1024;
   static constexpr int kO = 256;  // TMEM: the row tiles' scores at 0 and 128; accumulators from here
 };
@@ -58,7 +61,7 @@ struct TilesShape {
 static_assert(TilesShape<64>::kStages % 2 == 0 && TilesShape<128>::kStages % 2 == 0, "keys in even stages, values in odd ones");
 
 // What a unit and its tiles cost, in sixteenths of a tile of two row tiles.
-constexpr int kPad = 32, kTwo = 16, kOne = 15, kLeast = 64;
+constexpr int kPad = 26, kTwo = 16, kOne = 15, kLeast = 64;
 
 struct TilesArgs {
   CrossAttend a;
@@ -89,17 +92,18 @@ struct Line {
 };
 
 // One CTA's share of a unit.
-struct Part {
-  CrossSeq q;
-  int head, tok0;   // the key head; the unit's first token
-  int lo, hi, all;  // tiles of frames lo .. hi - 1 of all
-  int n;            // those to compute (0 where a row sees nothing)
-  int64_t at;       // the unit's place in the line
-  bool two;
+struct alignas(16) Part {
+  int row0, count, head, tok0;  // the sequence's rows; the key head; the unit's first token
+  int source, len, lo, hi;      // tiles of frames lo .. hi - 1 ...
+  int all, n, what, last;       // ... of all; those to compute (0: a row sees nothing; -1: no part, the last one was); the CTA of the unit's last tile
+  static constexpr int kTwo = 1, kOk = 2;  // `what`: two row tiles; the sequence is in range
+  __device__ __forceinline__ bool two() const { return what & kTwo; }
+  __device__ __forceinline__ bool ok() const { return what & kOk; }
 };
+static_assert(sizeof(Part) == 48, "");
 
-// The parts of a CTA in order, the same for each of its warps: places lo .. hi - 1 of the line, from sequence i
-// (which begins at place `at`) on.  A warp holds 32 sequences at a time.
+// The parts of a CTA in order: places lo .. hi - 1 of the line, from sequence i (which begins at place `at`)
+// on.  A warp holds 32 sequences at a time.
 struct Walk {
   const CrossAttend& a;
   const CrossSeq* known;  // [n], or NULL: in the call's arrays
@@ -145,26 +149,28 @@ struct Walk {
       window();
     }
   }
-  __device__ __forceinline__ bool next(Part& p) {
+  __device__ __forceinline__ bool next(Part& p, int64_t share, int ctas) {
     while (at < hi) {
       if (u >= units) {
         u = 0;
         if (++head >= line.kv && !sequence()) return false;
       }
       if (units == 0) return false;
-      p.q = q, p.head = head, p.tok0 = 2 * u * line.tokens, p.at = at, p.all = tiles;
-      p.two = line.two(q, u);
+      const bool two = line.two(q, u);
       const auto first = [&](int64_t place) {  // the first tile that begins there or later
         const int64_t x = place - at - kPad;
         if (x <= 0) return 0;
-        if (x >= (int64_t)tiles * (p.two ? kTwo : kOne)) return tiles;
+        if (x >= (int64_t)tiles * (two ? kTwo : kOne)) return tiles;
         const uint32_t y = (uint32_t)x;
-        return (int)(p.two ? (y + kTwo - 1) / kTwo : (y + kOne - 1) / kOne);
+        return (int)(two ? (y + kTwo - 1) / kTwo : (y + kOne - 1) / kOne);
       };
-      p.lo = first(lo), p.hi = first(hi);
-      at += Line::unit(tiles, p.two);
+      p.row0 = q.row0, p.count = q.count, p.head = head, p.tok0 = 2 * u * line.tokens;
+      p.source = q.source, p.len = q.len, p.lo = first(lo), p.hi = first(hi);
+      p.all = tiles, p.n = q.ok && q.len > 0 ? p.hi - p.lo : 0, p.what = (two ? Part::kTwo : 0) | (q.ok ? Part::kOk : 0);
+      p.last = 0;
+      if (p.lo == 0 && p.hi > 0 && p.hi < tiles) p.last = (int)min(quotient(at + kPad + (int64_t)(tiles - 1) * (two ? kTwo : kOne), share), (int64_t)ctas - 1);
+      at += Line::unit(tiles, two);
       ++u;
-      p.n = q.ok && q.len > 0 ? p.hi - p.lo : 0;
       if (p.hi > p.lo) return true;
     }
     return false;
@@ -201,14 +207,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   using S = TilesShape<DIM>;
   constexpr int ST = S::kStages;
   extern __shared__ unsigned char smem_raw[];
-  __shared__ int64_t s_sums[kThreads / 32], s_place;
-  __shared__ int s_seq;
+  __shared__ int64_t s_sums[kThreads / 32], s_upto[kThreads];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::kBar);
   uint64_t *full = bars, *empty = bars + ST, *v_ready = bars + 2 * ST;  // the ring's stages; those of values past warp 10
   uint64_t *s_full = v_ready + ST / 2, *o_half = s_full + 2, *o_full = s_full + 4, *p_full = s_full + 6;  // [2] row tiles; [2][2] and halves of a step
   uint64_t *q_full = s_full + 10, *q_empty = s_full + 11, *drain = s_full + 12;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(s_full + 13);
+  uint64_t *part_full = s_full + 13, *part_empty = part_full + kPlanned;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(part_empty + kPlanned);
+  Part* plan = reinterpret_cast<Part*>(smem + S::kParts);
   const CrossAttend& a = args.a;
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const Line line{a.s.kv_heads, args.tokens};
@@ -228,6 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
+  s_upto[threadIdx.x] = upto;
   if (lane == 31) s_sums[warp] = upto;
   if (warp == kTmaWarp && lane < 3)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(lane == 0 ? &q_map : lane == 1 ? &k_map : &v_map)) : "memory");
@@ -243,35 +251,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
       mbar_init(o_full + i, 1);
     }
     for (int i = 0; i < 4; ++i) mbar_init(p_full + i, 4);
+    for (int i = 0; i < kPlanned; ++i) {
+      mbar_init(part_full + i, 1);
+      mbar_init(part_empty + i, kReaders);
+    }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int i = 0; i < kThreads / 32; ++i) {
-    const int64_t x = s_sums[i];
-    if (i < warp) upto += x;
-    total += x;
-  }
-  const int64_t share = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kLeast);
-  const int64_t lo = share * blockIdx.x, hi = min(lo + share, total);
-  if (lo >= hi) {
-    if (args.joins && threadIdx.x == 0) args.joins[2 * blockIdx.x + 1].x = -1;
-    return;
-  }
-  if (upto - mine <= lo && lo < upto) {
-    int64_t x = upto - mine;
-    for (int i = run0; i < run1; ++i) {
-      const int64_t y = known ? mine : line.seq(cross_seq(a.s, a.b, i));
-      if (lo < x + y) {
-        s_seq = i, s_place = x;
-        break;
-      }
-      x += y;
-    }
   }
   if (warp == kMmaWarp) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
@@ -281,10 +268,29 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   __syncthreads();
   fence_after();
   const uint32_t tmem = *tmem_slot;
-  Walk walk(a, line, known, s_place, lo, hi, s_seq);
+  int64_t total = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 32; ++i) total += s_sums[i];
+  const int64_t share = max(quotient(total + gridDim.x - 1, gridDim.x), (int64_t)kLeast);
+  const int64_t lo = share * blockIdx.x, hi = min(lo + share, total);
+  if (lo >= hi) {
+    if (args.joins && threadIdx.x == 0) args.joins[2 * blockIdx.x + 1].x = -1;
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    return;
+  }
   Part p;
-  // A wait that runs out ends its role; the others' waits on it run out in turn, and the
-  // rows from there on say NaN.
+  int seen = 0;
+  const auto next = [&] {  // the next part; false: there is none
+    const int s = seen % kPlanned;
+    if (!__all_sync(0xffffffffu, mbar_wait(part_full + s, (uint32_t)(seen / kPlanned) & 1u, 16 * kWaitNs))) return false;
+    p = plan[s];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(part_empty + s);
+    ++seen;
+    return p.n >= 0;
+  };
+  // A wait that runs out ends what its role does (it goes on to follow the parts); the others' waits on it
+  // run out in turn, and the rows from there on say NaN.
   if (warp < kSoftWarps) {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     const int tile = warp >> 2;
@@ -292,28 +298,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     const bool used = row < args.tokens * a.group;
     const uint32_t st = tmem + (uint32_t)(tile * 128) + ((uint32_t)((warp & 3) * 32) << 16);  // scores, then weights
     const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
-    const float c = a.scale * kLog2e;
+    // (not 0: what no row may see is an infinite score; the least factor leaves the others 0)
+    const float c = a.scale * kLog2e == 0.f ? 0x1p-120f : a.scale * kLog2e;
     const uint64_t c2 = pair_of(c, c);
     const float nan = __uint_as_float(0x7fc00000u);
     int at0 = 0, done = 0;  // steps and parts of this row tile so far
     bool fine = true, join = false;
-    while (walk.next(p)) {
+    while (next()) {
       const int tok = p.tok0 + row_tok;
-      const bool live = used && tok < p.q.count;
-      uint16_t* const dst = a.out + (int64_t)(p.q.row0 + tok) * a.out_row + (int64_t)(p.head * a.group + row_h) * a.out_head;
+      const bool live = used && tok < p.count;
+      uint16_t* const dst = a.out + (int64_t)(p.row0 + tok) * a.out_row + (int64_t)(p.head * a.group + row_h) * a.out_head;
       const bool whole_unit = p.lo == 0 && p.hi == p.all;
       const int slot = 2 * (int)blockIdx.x + (p.lo == 0 ? 1 : 0);
       if (!whole_unit && p.lo == 0) {
         join = true;
-        if (threadIdx.x == 0) {  // (an exact division: this CTA's share is followed by whole ones)
-          const int64_t last = quotient(p.at + kPad + (int64_t)(p.all - 1) * (p.two ? kTwo : kOne), share);
-          args.joins[slot - 1] = make_int4(p.q.row0, p.q.count, p.tok0, p.head);
-          args.joins[slot].x = (int)min(last, (int64_t)gridDim.x - 1);
+        if (threadIdx.x == 0) {
+          args.joins[slot - 1] = make_int4(p.row0, p.count, p.tok0, p.head);
+          args.joins[slot].x = p.last;
         }
       }
       if (p.n == 0 || !fine) {
         if (live) {
-          const uint32_t x = p.q.ok && fine ? 0u : BF16 ? 0x7fc07fc0u : 0x7e007e00u;
+          const uint32_t x = p.ok() && fine ? 0u : BF16 ? 0x7fc07fc0u : 0x7e007e00u;
           if (whole_unit) {
             for (int i = 0; i < DIM / 8; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(x, x, x, x);
           } else {
@@ -323,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
         continue;
       }
       bool dead = false;
-      if (tile == 0 || p.two) {
+      if (tile == 0 || p.two()) {
         float m = -INFINITY, l = 0.f;
 #pragma unroll 1
         for (int j = 0; j < p.n; ++j) {
@@ -332,8 +338,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
             break;
           }
           fence_after();
-          const int left = p.q.len - (p.lo + j) * kFrames;  // frames from here on
-          const bool whole = left >= kFrames;
+          const int left = p.len - (p.lo + j) * kFrames;  // frames from here on
+          if (left < kFrames) {  // the last tile: what lies behind the length becomes a score that gives weight 0
+            const float none = c < 0.f ? INFINITY : -INFINITY;
+#pragma unroll 1
+            for (int b = left / 16; b < kFrames / 16; ++b) {
+              float v[16];
+              tmem_ld16(st + 16 * b, v);
+              uint32_t z[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(16 * b + e < left ? v[e] : none);
+              tmem_st16(st + 16 * b, z);
+            }
+            tmem_st_wait();
+          }
           // 64 frames, then 64: the first ones' values' product runs while the others' weights are
           // made.  Weights are relative to the maximum so far, without looking for that of these 64: one
           // that a score has outgrown shows in the sum, and they are taken again from their
@@ -341,10 +359,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
           // reaches fp16's largest.)
           uint32_t raw[2][32];  // 32 scores are on their way while the ones before are worked on
           tmem_ld32_begin(st, raw[0]);
-#pragma unroll
+#pragma unroll 1
           for (int h = 0; h < 2; ++h) {
             if (h == 1 && left <= 64) {  // nothing to see: no product reads these weights
               tmem_ld32_wait(raw[0]);
+              __syncwarp();
+              if (lane == 0) mbar_arrive(p_full + 2 * tile + 1);
               break;
             }
             uint32_t y[32];
@@ -360,10 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                   float v[32];
                   tmem_ld32(st + 64 * h + 32 * b, v);
 #pragma unroll
-                  for (int e = 0; e < 32; ++e) {
-                    const float x = whole || 64 * h + 32 * b + e < left ? v[e] * c : -INFINITY;
-                    top = fmaxf(top, x);
-                  }
+                  for (int e = 0; e < 32; ++e) top = fmaxf(top, v[e] * c);
                 }
                 const float x = fmaxf(m, top);
                 const float w = x == m ? 1.f : ex2_approx(m - x);
@@ -391,30 +408,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
               const float ref = m > -INFINITY ? m - 7.f : 0.f;
               const uint64_t ref2 = pair_of(-ref, -ref);
               uint64_t sums[4] = {0, 0, 0, 0};
-              const auto weigh = [&](auto masked) {  // a branch for the whole of it: masks in all steps cost 250 clocks
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                  tmem_ld32_wait(raw[b]);
-                  if (b == 0) tmem_ld32_begin(st + 64 * h + 32, raw[1]);
-                  else if (h == 0) tmem_ld32_begin(st + 64, raw[0]);
-                  float x[32];
+              for (int b = 0; b < 2; ++b) {
+                tmem_ld32_wait(raw[b]);
+                if (b == 0) tmem_ld32_begin(st + 64 * h + 32, raw[1]);
+                else if (h == 0) tmem_ld32_begin(st + 64, raw[0]);
 #pragma unroll
-                  for (int e = 0; e < 32; e += 2)
-                    unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x[e], x[e + 1]);
-                  if constexpr (decltype(masked)::value)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                      if (64 * h + 32 * b + e >= left) x[e] = -INFINITY;
-#pragma unroll
-                  for (int e = 0; e < 32; e += 2) {
-                    const float p0 = ex2_approx(x[e]), p1 = ex2_approx(x[e + 1]);
-                    sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
-                    y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
-                  }
+                for (int e = 0; e < 32; e += 2) {
+                  float x0, x1;
+                  unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x0, x1);
+                  const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+                  sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
+                  y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
                 }
-              };
-              if (whole) weigh(std::false_type{});
-              else weigh(std::true_type{});
+              }
               float s0, s1;
               unpair(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), s0, s1);
               sum = s0 + s1;
@@ -430,10 +437,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
             if (lane == 0) mbar_arrive(p_full + 2 * tile + h);
           }
           if (dead) break;
-          if (left <= 64) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full + 2 * tile + 1);
-          }
         }
         if (!dead && !mbar_wait(o_full + tile, (uint32_t)done & 1u)) dead = true;
         fence_after();
@@ -481,8 +484,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   if (warp == kTmaWarp) {
     uint32_t at = 0, parts = 0;  // tiles through the ring, keys and values; parts with any
     bool dead = false;
-    while (!dead && walk.next(p)) {
-      if (elect()) {
+    while (next()) {
+      if (!dead && elect()) {
         bool asked = false;
         for (int j = 0; j < p.n && !dead; ++j) {
 #pragma unroll
@@ -496,20 +499,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
 #pragma unroll
             for (int h = 0; h < DIM / 64; ++h)
               tma_load_4d(smem_u32(smem + S::kRing + s * S::kTileBytes + h * S::kHalf), kind ? &v_map : &k_map, full + s, 64 * h, (p.lo + j) * kFrames,
-                          kind ? p.head * args.v_heads : p.head * args.k_heads, kind ? p.q.source * args.v_sources : p.q.source * args.k_sources);
+                          kind ? p.head * args.v_heads : p.head * args.k_heads, kind ? p.source * args.v_sources : p.source * args.k_sources);
             if (j == 0 && kind == 0) {  // the queries, once the last part's have been used
               if (parts > 0 && !mbar_wait(q_empty, (parts - 1) & 1u)) {
                 dead = true;
                 ++at;
                 break;
               }
-              const int tiles = p.two ? 2 : 1;
+              const int tiles = p.two() ? 2 : 1;
               mbar_expect_tx(q_full, tiles * (DIM / 64) * args.tokens * a.group * 128);
               for (int t = 0; t < tiles; ++t)
 #pragma unroll
                 for (int h = 0; h < DIM / 64; ++h)
                   tma_load_3d(smem_u32(smem + S::kQ + t * S::kTileBytes + h * S::kHalf), &q_map, q_full, 64 * h, p.head * a.group,
-                              p.q.row0 + p.tok0 + t * args.tokens);
+                              p.row0 + p.tok0 + t * args.tokens);
               asked = true;
             }
           }
@@ -526,8 +529,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   } else if (warp == kFixWarp) {
     uint32_t at = 0;
     bool dead = false;
-    while (!dead && walk.next(p)) {
-      const bool fix = p.hi == p.all && p.q.len % 16;
+    while (next()) {
+      const bool fix = p.hi == p.all && p.len % 16;
       for (int j = 0; j < p.n && !dead; ++j, at += 2) {
         const uint32_t v = at + 1;
         if (!__all_sync(0xffffffffu, mbar_wait(full + v % ST, (v / ST) & 1u))) {
@@ -535,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
           break;
         }
         if (fix && j == p.n - 1) {
-          const int from = p.q.len - (p.all - 1) * kFrames, to = (from + 15) & ~15;
+          const int from = p.len - (p.all - 1) * kFrames, to = (from + 15) & ~15;
           unsigned char* tile = smem + S::kRing + (v % ST) * S::kTileBytes;
           for (int i = lane; i < (to - from) * (DIM / 8); i += 32) {
             const int f = from + i / (DIM / 8), c = i % (DIM / 8);
@@ -550,11 +553,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
   } else if (warp == kMmaWarp) {
     uint32_t at0 = 0, parts = 0, tile_at[2] = {0, 0};
     bool dead = false;
-    while (!dead && walk.next(p)) {
-      if (p.n == 0) continue;
-      const int n = p.n, tiles = p.two ? 2 : 1;
+    while (next()) {
+      if (p.n == 0 || dead) continue;
+      const int n = p.n, tiles = p.two() ? 2 : 1;
       const bool ends = p.hi == p.all;
-      const int rest = p.q.len - (p.all - 1) * kFrames;  // of the last tile
+      const int rest = p.len - (p.all - 1) * kFrames;  // of the last tile
       if (elect()) {
         const uint32_t sq = smem_u32(smem + S::kQ), ring = smem_u32(smem + S::kRing);
         bool ok = mbar_wait(q_full, parts & 1u);
@@ -619,44 +622,90 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
       ++parts;
       at0 += 2 * (uint32_t)n;
       tile_at[0] += n;
-      if (p.two) tile_at[1] += n;
+      if (p.two()) tile_at[1] += n;
       dead = __any_sync(0xffffffffu, dead);
     }
     asm volatile("bar.sync 2, %0;" ::"n"(32 * (kSoftWarps + 1)) : "memory");  // the accumulators have been read
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  } else if (warp == kPlanWarp) {
+    // the thread whose run of sequences holds place lo, among the warps' sums, then among a warp's threads
+    int64_t place = 0, sum = s_sums[0];
+    int w = 0;
+    while (place + sum <= lo) place += sum, sum = s_sums[++w];
+    const int first = __ffs(__ballot_sync(0xffffffffu, place + s_upto[32 * w + lane] > lo)) - 1;
+    if (first > 0) place += s_upto[32 * w + first - 1];
+    int i = (32 * w + first) * run;
+    if (run > 1)
+      while (true) {
+        const int64_t x = line.seq(cross_seq(a.s, a.b, i));
+        if (lo < place + x || i + 1 >= a.b.n) break;
+        place += x, ++i;
+      }
+    Walk walk(a, line, known, place, lo, hi, i);
+    bool more = true;
+    for (int n = 0; more; ++n) {
+      const int s = n % kPlanned;
+      more = walk.next(p, share, gridDim.x);
+      if (!more) p.n = -1;
+      if (n >= kPlanned && !__all_sync(0xffffffffu, mbar_wait(part_empty + s, (uint32_t)(n / kPlanned - 1) & 1u, 8 * kWaitNs))) break;
+      if (lane == 0) {
+        plan[s] = p;
+        mbar_arrive(part_full + s);
+      }
+      __syncwarp();
+    }
   }
 }
 
 // The units that several CTAs share: blocks (c, ..) take the one that CTA c began.
 // A warp takes 32 rows and 16 of their dimensions.
 template <bool BF16, int DIM>
-__global__ void __launch_bounds__(2 * DIM) k_cross_join(const __grid_constant__ TilesArgs args) {
-  const int c = blockIdx.x, warp = threadIdx.x >> 5, rr = blockIdx.y * 32 + (threadIdx.x & 31), row = rr % 128;
+__global__ void __launch_bounds__(DIM) k_cross_join(const __grid_constant__ TilesArgs args) {
+  const int c = blockIdx.x, warp = blockIdx.z * (DIM / 32) + (threadIdx.x >> 5), rr = blockIdx.y * 32 + (threadIdx.x & 31), row = rr % 128;
   const CrossAttend& a = args.a;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int4 place = args.joins[2 * c];  // the sequence's first row and its tokens, the unit's first token, the key head
   const int parts = args.joins[2 * c + 1].x - c + 1, tok = place.z + rr / 128 * args.tokens + row / a.group;
   if (parts < 2 || row >= args.tokens * a.group || tok >= place.y) return;
   const auto slot = [&](int k) { return (size_t)(k == 0 ? 2 * c + 1 : 2 * (c + k)); };
+  // (kAtOnce parts' loads are on their way together; one that is not there has weight 0)
+  constexpr int kAtOnce = 4;
   float top = -INFINITY;
-#pragma unroll 8
-  for (int k = 0; k < parts; ++k) top = fmaxf(top, args.part_ml[slot(k) * kUnitRows + rr].x);
+  for (int k0 = 0; k0 < parts; k0 += 2 * kAtOnce) {
+    float x[2 * kAtOnce];
+#pragma unroll
+    for (int k = 0; k < 2 * kAtOnce; ++k) x[k] = k0 + k < parts ? args.part_ml[slot(k0 + k) * kUnitRows + rr].x : -INFINITY;
+#pragma unroll
+    for (int k = 0; k < 2 * kAtOnce; ++k) top = fmaxf(top, x[k]);
+  }
   float acc[16], sum = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const float2 x = args.part_ml[slot(k) * kUnitRows + rr];
-    const float4* from = reinterpret_cast<const float4*>(args.part) + (slot(k) * (DIM / 4) + 4 * warp) * kUnitRows + rr;
-    const float f = x.x == top ? 1.f : ex2_approx(x.x - top);  // (top -inf: every score is, and 0 / 0 is the result)
-    sum = fmaf(f, x.y, sum);
+  for (int k0 = 0; k0 < parts; k0 += kAtOnce) {
+    float2 x[kAtOnce];
+    float4 v[kAtOnce][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 v = from[i * kUnitRows];
-      acc[4 * i] = fmaf(f, v.x, acc[4 * i]), acc[4 * i + 1] = fmaf(f, v.y, acc[4 * i + 1]);
-      acc[4 * i + 2] = fmaf(f, v.z, acc[4 * i + 2]), acc[4 * i + 3] = fmaf(f, v.w, acc[4 * i + 3]);
+    for (int k = 0; k < kAtOnce; ++k) {
+      x[k] = make_float2(0.f, 0.f);
+      if (k0 + k < parts) {
+        const size_t at = slot(k0 + k);
+        x[k] = args.part_ml[at * kUnitRows + rr];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[k][i] = reinterpret_cast<const float4*>(args.part)[(at * (DIM / 4) + 4 * warp + i) * kUnitRows + rr];
+      }
     }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k)
+      if (k0 + k < parts) {
+        const float f = x[k].x == top ? 1.f : ex2_approx(x[k].x - top);  // (top -inf: every score is, and 0 / 0 is the result)
+        sum = fmaf(f, x[k].y, sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          acc[4 * i] = fmaf(f, v[k][i].x, acc[4 * i]), acc[4 * i + 1] = fmaf(f, v[k][i].y, acc[4 * i + 1]);
+          acc[4 * i + 2] = fmaf(f, v[k][i].z, acc[4 * i + 2]), acc[4 * i + 3] = fmaf(f, v[k][i].w, acc[4 * i + 3]);
+        }
+      }
   }
   const float inv = 1.f / sum;
   uint32_t z[8];
@@ -702,8 +751,8 @@ cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtenso
   const cudaError_t launched = cudaGetLastError();
   if (launched != cudaSuccess || p.bytes == 0) return launched;
   cudaLaunchConfig_t c{};
-  c.gridDim = dim3((unsigned)p.ctas, kUnitRows / 32);
-  c.blockDim = 2 * DIM;
+  c.gridDim = dim3((unsigned)p.ctas, kUnitRows / 32, 2);
+  c.blockDim = DIM;
   c.stream = s;
   cudaLaunchAttribute at{};  // its blocks come while the last CTAs end, and wait for them
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
