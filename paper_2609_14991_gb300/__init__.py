@@ -711,12 +711,16 @@ def _dtype_code(t) -> int:
     return _DTYPE.get(t.dtype, -1)
 
 
-def _on_current(who, name, t):
-    """The current device's index, which t has to be on."""
+def _current_device():
     import torch
 
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _on_current(who, name, t):
+    """The current device's index, which t has to be on."""
     dev = t.get_device()
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current_device():
         raise ValueError(f"{who}: {name} must be a CUDA tensor on the current device")
     return dev
 
@@ -731,12 +735,22 @@ def _empty(n, dtype, dev, stream):
     """n elements that the caching allocator gives out for the call's stream."""
     import torch
 
+    device = _devices.get(dev)  # (a device by its number takes torch 3 us more)
+    if device is None:
+        device = _devices[dev] = torch.device("cuda", dev)
     if stream is None:
-        return torch.empty(n, dtype=dtype, device=dev)
+        return torch.empty(n, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=dtype, device=dev)
+        return torch.empty(n, dtype=dtype, device=device)
 
 
+def _workspace(n, dev, stream):
+    import torch
+
+    return _empty(n, torch.uint8, dev, stream)
+
+
+_devices = {}  # by number
 _sizes = {}  # workspace bytes by call shape
 _MAX32 = 2 ** 31 - 1
 
@@ -1076,21 +1090,29 @@ class Rotary:
 
     def _heads(self, name, t, out, rows, dtype, stream):
         """(result, tsd_rotary_heads) of queries or keys [rows, heads, dim]."""
-        s, d = t.shape, t.stride()
+        s, d, dev = t.shape, t.stride(), self._dev
         if len(s) != 3 or s[0] != rows or s[2] != self.dim or t.dtype != dtype:
             raise ValueError(f"Rotary: {name} must be {dtype} [{rows}, heads, {self.dim}]")
-        if t.get_device() != self._dev:
+        if t.get_device() != dev:
             raise ValueError(f"Rotary: {name} must be on the handle's device")
+        heads = s[1]
         if out is None:
-            out = _empty(s, dtype, self._dev, stream)
-            o = (s[1] * s[2], s[2], 1)
+            out = _empty(s, dtype, dev, stream)
+            out_head, out_row, last = self.dim, heads * self.dim, 1
         else:
-            o = out.stride()
-            if out.shape != s or out.dtype != dtype or out.get_device() != self._dev:
+            out_row, out_head, last = out.stride() if out.dim() == 3 else (0, 0, 0)
+            if out.shape != s or out.dtype != dtype or out.get_device() != dev:
                 raise ValueError(f"Rotary: the result of {name} must be {dtype} {list(s)} on the handle's device")
-        if d[2] != 1 or o[2] != 1:
+        if d[2] != 1 or last != 1:
             raise ValueError(f"Rotary: {name}'s last dimension must be adjacent")
-        return out, RotaryHeadsC(t.data_ptr(), out.data_ptr(), d[0], d[1], o[0], o[1], s[1])
+        return out, RotaryHeadsC(t.data_ptr(), out.data_ptr(), d[0], d[1], out_row, out_head, heads)
+
+    def _ints(self, name, t):
+        import torch
+
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
+            raise ValueError(f"Rotary: {name} must be contiguous int32 on the handle's device")
+        return t.data_ptr(), t.shape[0]
 
     def __call__(self, q, k=None, positions=None, lens=None, starts=None, slots=None, out=None, stream=None):
         """q [rows, heads, dim] and k [rows, kv heads, dim] (float32, bfloat16 or
@@ -1098,48 +1120,46 @@ class Rotary:
         [rows]; or a cache's lens, starts and slots as KV8Cache's calls take them (the rows are
         their sequences' last tokens).  out: tensors for the results (a pair, or q's); q and k
         themselves turn in place."""
-        import torch
-
-        rows, dtype, i32, dev = q.shape[0], q.dtype, torch.int32, self._dev
+        rows, dtype, dev = q.shape[0], q.dtype, self._dev
         code = _dtype_code(q)
         if code < 0:
             raise ValueError("Rotary: q must be float32, bfloat16 or float16")
-        if torch.cuda.current_device() != dev:
+        if _current_device() != dev:
             raise ValueError("Rotary: the handle is on another device than the current one")
         if not 1 <= rows <= 1 << 22:
             raise ValueError("Rotary: 1 to 2^22 rows")
-        if (positions is None) == (lens is None) or (positions is not None and (starts is not None or slots is not None)):
-            raise ValueError("Rotary: positions, or lens with starts and slots")
-        n, n_slots, ptr = rows, 0, [None] * 4
-        for j, (name, t) in enumerate((("positions", positions), ("slots", slots), ("lens", lens), ("starts", starts))):
-            if t is None:
-                continue
-            if t.dtype != i32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != dev:
-                raise ValueError(f"Rotary: {name} must be contiguous int32 on the handle's device")
-            ptr[j] = t.data_ptr()
         if positions is not None:
-            if positions.shape[0] != rows:
+            if lens is not None or starts is not None or slots is not None:
+                raise ValueError("Rotary: positions, or lens with starts and slots")
+            at, m = self._ints("positions", positions)
+            if m != rows:
                 raise ValueError(f"Rotary: positions must have {rows} entries")
+            r = RotaryRowsC(rows, at)
+        elif lens is None:
+            raise ValueError("Rotary: positions, or lens with starts and slots")
         else:
-            n_slots = lens.shape[0]
+            at, n_slots = self._ints("lens", lens)
+            n, at_slots, at_starts = rows, None, None
             if slots is not None:
-                n = slots.shape[0]
+                at_slots, n = self._ints("slots", slots)
             if starts is not None:
-                if starts.shape[0] < 2 or (slots is not None and starts.shape[0] != n + 1):
+                at_starts, m = self._ints("starts", starts)
+                if m < 2 or (slots is not None and m != n + 1):
                     raise ValueError("Rotary: starts must have n + 1 entries")
-                n = starts.shape[0] - 1
+                n = m - 1
             elif n != rows:
                 raise ValueError("Rotary: without starts there is one row per sequence")
             if not 1 <= n <= 65535:
                 raise ValueError("Rotary: at most 65535 sequences")
-        oq, ok = (out, None) if k is None or out is None else out
-        oq, hq = self._heads("q", q, oq, rows, dtype, stream)
-        hk = None
-        if k is not None:
+            r = RotaryRowsC(rows, None, n, at_slots, at, at_starts, n_slots)
+        if k is None:
+            oq, hq = self._heads("q", q, out, rows, dtype, stream)
+            ok = hk = None
+        else:
+            oq, ok = (None, None) if out is None else out
+            oq, hq = self._heads("q", q, oq, rows, dtype, stream)
             ok, hk = self._heads("k", k, ok, rows, dtype, stream)
-            hk = ctypes.byref(hk)
-        r = RotaryRowsC(rows, ptr[0], n, ptr[1], ptr[2], ptr[3], n_slots)
-        st = lib().tsd_rotary_apply(self._c[code], ctypes.byref(r), ctypes.byref(hq), hk, _raw_stream(stream, dev))
+        st = lib().tsd_rotary_apply(self._c[code], r, hq, hk, _raw_stream(stream, dev))
         if st:
             _check(st)
         return oq if k is None else (oq, ok)
@@ -1148,19 +1168,24 @@ class Rotary:
 _NORMS = {None: 0, "rms": 1, "layer": 2}
 
 
-def _norm_arg(who, what, kind, weight, bias, d, eps, dev):
+def _norm_arg(what, kind, weight, bias, d, eps, dev):
     import torch
 
     if kind is None:
         if weight is not None or bias is not None:
-            raise ValueError(f"{who}: {what} is None, but has a weight or a bias")
+            raise ValueError(f"residual_norm: {what} is None, but has a weight or a bias")
         return None
-    ptr = []
-    for t in (weight, bias):
-        if t is not None and (t.dtype != torch.float32 or t.shape != (d,) or not t.is_contiguous() or t.get_device() != dev):
-            raise ValueError(f"{who}: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
-        ptr.append(t.data_ptr() if t is not None else None)
-    return ctypes.byref(NormC(_NORMS[kind], eps, ptr[0], ptr[1]))
+    w = b = None
+    f32 = torch.float32
+    if weight is not None:
+        if weight.dtype != f32 or weight.shape != (d,) or not weight.is_contiguous() or weight.get_device() != dev:
+            raise ValueError(f"residual_norm: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
+        w = weight.data_ptr()
+    if bias is not None:
+        if bias.dtype != f32 or bias.shape != (d,) or not bias.is_contiguous() or bias.get_device() != dev:
+            raise ValueError(f"residual_norm: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
+        b = bias.data_ptr()
+    return NormC(_NORMS[kind], eps, w, b)
 
 
 def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None, post: Optional[str] = None,
@@ -1172,8 +1197,6 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
     x, y: cuda [n, d], any row stride; y float32, bfloat16 or float16, x the same or
     float32.  gate: y's type, [d] or [n, d].  Weights and biases: float32 [d].  y None:
     h = norm(x) of x's type, and r is x.  out: (h, r) to write; r may be x and h may be y."""
-    import torch
-
     who = "residual_norm"
     shape = x.shape
     if len(shape) != 2 or not (1 <= shape[0] <= 1 << 27 and 1 <= shape[1] <= 16384):
@@ -1182,7 +1205,6 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
         raise ValueError(f"{who}: norms are 'rms', 'layer' or None")
     n, d = shape
     x_code = _dtype_code(x)
-    src = x if y is None else y
     code, dtype = (x_code, x.dtype) if y is None else (_dtype_code(y), y.dtype)
     if code < 0 or (x_code != code and x_code != 0):
         raise ValueError(f"{who}: y must be float32, bfloat16 or float16 and x of the same type or float32")
@@ -1204,8 +1226,8 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
             gp = gate.data_ptr()
     elif gate is not None or post is not None or norm is None:
         raise ValueError(f"{who}: without y there is a norm, and no gate or post")
-    pn = _norm_arg(who, "norm", norm, weight, bias, d, eps, dev)
-    pp = _norm_arg(who, "post", post, post_weight, post_bias, d, eps, dev)
+    pn = _norm_arg("norm", norm, weight, bias, d, eps, dev)
+    pp = _norm_arg("post", post, post_weight, post_bias, d, eps, dev)
     h = r = None
     if out is not None:
         h, r = out
@@ -1267,6 +1289,13 @@ class CrossStates:
         self._pc = ctypes.byref(self._c)
         self._flat = k.stride(1) < dim or v.stride(1) < dim  # frames overlap
 
+    def _ints(self, name, size, t):
+        import torch
+
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
+            raise ValueError(f"CrossStates.attend: {name} must be contiguous int32 [{size}] on the states' device")
+        return t.shape[0], t.data_ptr()
+
     def attend(self, q, starts=None, sources=None, scale: Optional[float] = None, out=None,
                max_rows: Optional[int] = None, stream=None):
         """Attention of queries [rows, heads, dim] over the states (``tsd_cross_attend``).
@@ -1274,28 +1303,23 @@ class CrossStates:
         sources[i] (int32 [n]; None: i): an utterance's hypotheses in one sequence
         share its reads.  max_rows, the most rows of a sequence, sizes launches only.
         scale: 1 / sqrt(dim) if None."""
-        import torch
-
-        who, dev, i32 = "CrossStates.attend", self._dev, torch.int32
+        who, dev = "CrossStates.attend", self._dev
         s = q.shape
         if len(s) != 3 or q.dtype != self.dtype or s[2] != self.dim:
             raise ValueError(f"{who}: q must be {self.dtype} [rows, heads, {self.dim}]")
-        if torch.cuda.current_device() != dev or q.get_device() != dev:
+        if _current_device() != dev or q.get_device() != dev:
             raise ValueError(f"{who}: q must be on the states' device, the current one")
         rows, heads = s[0], s[1]
         if not 1 <= rows <= 1 << 22:
             raise ValueError(f"{who}: 1 to 2^22 rows")
         n, ps, pt = rows, None, None
         if sources is not None:
-            if sources.dtype != i32 or sources.dim() != 1 or not sources.is_contiguous() or sources.get_device() != dev:
-                raise ValueError(f"{who}: sources must be contiguous int32 [n] on the states' device")
-            n, ps = sources.shape[0], sources.data_ptr()
+            n, ps = self._ints("sources", "n", sources)
         if starts is not None:
-            if starts.dtype != i32 or starts.dim() != 1 or not starts.is_contiguous() or starts.get_device() != dev:
-                raise ValueError(f"{who}: starts must be contiguous int32 [n + 1] on the states' device")
-            if starts.shape[0] < 2 or (sources is not None and starts.shape[0] != n + 1):
+            m, pt = self._ints("starts", "n + 1", starts)
+            if m < 2 or (sources is not None and m != n + 1):
                 raise ValueError(f"{who}: starts must have n + 1 entries")
-            n, pt = starts.shape[0] - 1, starts.data_ptr()
+            n = m - 1
         if n > 65535:
             raise ValueError(f"{who}: at most 65535 sequences")
         d = q.stride()
@@ -1309,16 +1333,17 @@ class CrossStates:
         if d[2] != 1 or o[2] != 1:
             raise ValueError(f"{who}: the last dimension of q and out must be adjacent")
         b = CrossBatchC(n, ps, pt, rows, min(max_rows or 0, _MAX32))
-        pb, L = ctypes.byref(b), lib()
+        L = lib()
         key = (who, dev, self.dim, self.kv_heads, self.frames, self._flat, n, rows, heads, max_rows, pt is None)
         need = _sizes.get(key)
         if need is None:
             x = _i64()
-            _check(L.tsd_cross_attend_workspace(self._pc, pb, heads, ctypes.byref(x)))
+            _check(L.tsd_cross_attend_workspace(self._pc, b, heads, ctypes.byref(x)))
             need = _remember(key, x.value)
-        ws = _empty(need, torch.uint8, dev, stream).data_ptr() if need else None
-        st = L.tsd_cross_attend(self._pc, pb, heads, q.data_ptr(), d[0], d[1], self.dim ** -0.5 if scale is None else scale,
-                                out.data_ptr(), o[0], o[1], ws, need, _raw_stream(stream, dev))
+        ws = _workspace(need, dev, stream) if need else None
+        st = L.tsd_cross_attend(self._pc, b, heads, q.data_ptr(), d[0], d[1], self.dim ** -0.5 if scale is None else scale,
+                                out.data_ptr(), o[0], o[1], ws.data_ptr() if need else None, need,
+                                _raw_stream(stream, dev))
         if st:
             _check(st)
         return out
