@@ -599,7 +599,8 @@ TSD_API tsd_status tsd_encoder_launches_per_chunk(const tsd_encoder* enc, int32_
 /* From logits in memory: n rows of C elements of type dtype, row_stride
  * elements apart (any alignment of the element type).  1 <= n <= 2^27,
  * 1 <= C <= 262144, row_stride >= C (or n = 1), temperature > 0 and finite, as
- * log2(e) / temperature in fp32.  A row's results are the same bits whatever else is in the call. */
+ * log2(e) / temperature in fp32.  A row's results do not depend on the
+ * other rows; their last bits may on where it stands (mod 8 elements). */
 TSD_API tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits, int32_t dtype, int64_t row_stride,
                                     float temperature, int32_t m, const int32_t* labels, int32_t k, float* logp,
                                     float* entropy, int32_t* alt_labels, float* alt_logp, void* cuda_stream);
@@ -752,8 +753,8 @@ typedef struct {
 /* The rows' positions: positions[r], any 32-bit integer (a negative one turns back), or (positions
  * NULL) those of a cache's call (tsd_kv8_batch): sequence i of n in slot slots[i] (NULL: i) holds
  * lens[slot] tokens, and rows starts[i] .. starts[i+1] (NULL: one row each) are its last ones.
- * Rows behind the last sequence's are not read or written; rows of a sequence whose
- * slot, length or rows are out of range become NaN. */
+ * Rows behind the last sequence's have no results; those of a sequence whose
+ * slot, length or rows are out of range are NaN. */
 typedef struct {
   int32_t rows;             /* 1..2^22 */
   const int32_t* positions; /* [rows] or NULL */
@@ -795,10 +796,11 @@ typedef struct {
  *            r is not written and h = norm(x), with no gate and no post;
  *   gate     of type dtype, NULL: 1; gate_row 0: one row for all;
  *   post, norm  NULL or kind NONE: post(y) = y, and h is not written.
- * Row strides in elements, at least d; any alignment of the element types (sixteen-byte accesses
- * where pointers are 16-byte aligned and d and strides multiples of 8).  r may be x, and h may be y
+ * Row strides in elements, at least d; any alignment of the element types (accesses are
+ * wide where all row arrays stand equally off a multiple of eight elements, as contiguous ones do).  r may be x, and h may be y
  * (without y: x), with the same strides; other overlaps are not allowed.  Everything between is fp32 and rounded once: h comes of
- * the unrounded r.  1 <= n <= 2^27, 1 <= d <= 16384.  A row's results are the same bits whatever else is in the call. */
+ * the unrounded r.  1 <= n <= 2^27, 1 <= d <= 16384.  A row's results do not depend on the
+ * other rows; their last bits may on where it stands (mod 8 elements). */
 TSD_API tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int32_t x_dtype, int64_t x_row, const void* y,
                                      int32_t dtype, int64_t y_row, const tsd_norm* post, const void* gate,
                                      int64_t gate_row, float scale, const tsd_norm* norm, void* r, int64_t r_row,

@@ -61,6 +61,15 @@ struct Eight {
 #pragma unroll
     for (int i = 0; i < kWords / 4; ++i) reinterpret_cast<uint4*>(p)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
   }
+  // at a 32-byte boundary where there are 32 bytes: whole sectors at once
+  __device__ __forceinline__ void store_even(typename Elem<DT>::Raw* p) const {
+    if constexpr (DT == TSD_F32)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]),
+                   "r"(w[6]), "r"(w[7])
+                   : "memory");
+    else
+      store(p);
+  }
   __device__ __forceinline__ void get(float* x) const {
     if constexpr (DT == TSD_F32) {
 #pragma unroll

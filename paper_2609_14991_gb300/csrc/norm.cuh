@@ -1,0 +1,306 @@
+// A block's output normed, gated and added to the residual stream, and the next
+// block's norm (tsd.h: tsd_residual_norm):
+//   r = x + scale g (.) post(y),   h = norm(r)
+// in one pass: a row stays in registers from its loads to its stores, statistics
+// are fp32 sums over deviations from a mean known before (layer) or squares (rms),
+// and h is computed from r before r is rounded.  Reads x, y (and g), writes r and h:
+// bound by memory.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+#include <type_traits>
+
+#include "elem.cuh"
+#include "launch.h"
+#include "norm.h"
+
+namespace tsd {
+
+namespace {
+
+constexpr int kMaxSmem = 227 * 1024 - 512;  // of a CTA, dynamic
+constexpr int kRingBytes = 128 * 1024;      // of an SM for rows on their way; the rest caches weights
+
+// Sum over the row's THREADS threads (a power of two; above a warp: the whole CTA; the warp's lanes are all here).
+// s_part: two places that sums take in turn, so that one barrier serves for each.
+template <int THREADS>
+__device__ __forceinline__ float row_sum(float v, float (*s_part)[32], int& turn) {
+#pragma unroll
+  for (int o = THREADS < 32 ? THREADS / 2 : 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if constexpr (THREADS > 32) {
+    float* part = s_part[turn ^= 1];
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[threadIdx.x & (THREADS / 32 - 1)];
+#pragma unroll
+    for (int o = THREADS / 64; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  return v;
+}
+
+// A thread's elements of a row.  EVEN: groups of eight that begin at a multiple of eight elements in memory, the row's
+// first one `shift` elements into its first group; else every THREADS-th element.
+template <int THREADS, int CHUNKS, bool EVEN>
+struct Places {
+  static constexpr int N = 8 * CHUNKS;
+  int t, d, shift;
+  __device__ __forceinline__ int first(int c) const { return (c * THREADS + t) * 8 - shift; }  // EVEN: a group's first element
+  __device__ __forceinline__ int at(int i) const { return EVEN ? first(i / 8) + i % 8 : i * THREADS + t; }
+  __device__ __forceinline__ bool whole(int c) const { return first(c) >= 0 && first(c) + 8 <= d; }
+  __device__ __forceinline__ bool some(int c) const { return first(c) < d; }  // (the first group always has some)
+  __device__ __forceinline__ bool has(int i) const { return (unsigned)at(i) < (unsigned)d; }
+
+  // eight elements (group c's) of an array that stands anywhere; 0 past the row
+  template <int DT>
+  __device__ __forceinline__ void load(const void* base, int c, float* v) const {
+    const typename Elem<DT>::Raw* p = static_cast<const typename Elem<DT>::Raw*>(base);
+    if (EVEN && shift == 0 && d % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0) {
+      Eight<DT> x;
+#pragma unroll
+      for (int i = 0; i < Eight<DT>::kWords; ++i) x.w[i] = 0;
+      if (some(c)) x.load(p + first(c));
+      x.get(v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = has(8 * c + i) ? Elem<DT>::wide(p[at(8 * c + i)]) : 0.f;
+    }
+  }
+  template <int DT>
+  __device__ __forceinline__ void store(void* base, int64_t row, int c, const float* v) const {
+    typename Elem<DT>::Raw* p = static_cast<typename Elem<DT>::Raw*>(base) + row;
+    if (EVEN && whole(c)) {
+      Eight<DT> x;
+      x.put(v);
+      x.store_even(p + first(c));
+    } else if (!EVEN || some(c)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (has(8 * c + j)) p[at(8 * c + j)] = Elem<DT>::narrow(v[j]);
+    }
+  }
+};
+
+// The first half of a norm: v <- v or (layer) its deviations from the mean, and the factor 1 / sqrt(mean square + eps);
+// elements past the row are 0 and stay out of the sums.
+template <int THREADS, int CHUNKS, bool EVEN>
+__device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, float* v, float (*s_part)[32], int& turn) {
+  constexpr int N = 8 * CHUNKS;
+  if (k.kind == TSD_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s += v[i];
+    const float mean = row_sum<THREADS>(s, s_part, turn) / pl.d;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = pl.has(i) ? v[i] - mean : 0.f;
+  }
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
+  return 1.f / sqrtf(row_sum<THREADS>(s, s_part, turn) / pl.d + k.eps);
+}
+// The second, for group c
+template <int THREADS, int CHUNKS, bool EVEN>
+__device__ __forceinline__ void scaled(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, float inv, float* v) {
+  float w[8];
+  if (k.weight) {
+    pl.template load<TSD_F32>(k.weight, c, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= inv * w[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= inv;
+  }
+  if (k.bias) {
+    pl.template load<TSD_F32>(k.bias, c, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += w[i];
+  }
+}
+
+// A row array's groups of eight in shared memory, copied there asynchronously, 16 bytes at a time by neighbouring
+// lanes: a thread's own, or (fp32, whose groups take two) its warp's.
+template <int DT, int THREADS, int CHUNKS>
+struct Staged {
+  static constexpr int kUnits = DT == TSD_F32 ? 2 : 1;  // 16 bytes each
+  static constexpr int kBytes = kUnits * CHUNKS * THREADS * 16;
+  static constexpr int kLanes = THREADS < 32 ? THREADS : 32;  // of a row
+  template <class P>
+  static __device__ __forceinline__ void begin(unsigned char* to, const void* base, int64_t row, const P& pl) {
+    const typename Elem<DT>::Raw* p = static_cast<const typename Elem<DT>::Raw*>(base) + row;
+    constexpr int kPer = 8 / kUnits;
+    const int lane = pl.t % kLanes;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+      for (int u = 0; u < kUnits; ++u) {
+        const int unit = (c * THREADS + pl.t - lane) * kUnits + u * kLanes + lane, e = unit * kPer - pl.shift;
+        if (e > -kPer && e < pl.d)  // at least one of the row's elements: the 16 bytes around them
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + unit * 16)), "l"(p + e) : "memory");
+      }
+  }
+  template <class P>
+  static __device__ __forceinline__ void get(const unsigned char* from, const P& pl, int c, float* v) {
+    Eight<DT> x;
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const uint4 w = *reinterpret_cast<const uint4*>(from + ((c * THREADS + pl.t) * kUnits + u) * 16);
+      x.w[4 * u] = w.x, x.w[4 * u + 1] = w.y, x.w[4 * u + 2] = w.z, x.w[4 * u + 3] = w.w;
+    }
+    x.get(v);
+    if (!pl.whole(c))
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (!pl.has(8 * c + j)) v[j] = 0.f;
+  }
+};
+
+// Rows per CTA and CTAs per SM: those of a warp's lanes or part of them in CTAs of 128, wider ones a CTA's.
+constexpr int cta_threads(int per_row) { return per_row <= 32 ? 128 : per_row; }
+constexpr int ctas_per_sm(int per_row, int chunks) { return (chunks == 1 ? 1024 : per_row < 512 ? 768 : per_row) / cta_threads(per_row); }
+
+// A CTA goes from row to row.  EVEN: the next rows are on their way to shared memory, each warp's elements to its own
+// place, so no barrier guards them.
+template <int XT, int YT, int THREADS, int CHUNKS, bool EVEN>
+__global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHUNKS)) k_residual_norm(const __grid_constant__ NormArgs a) {
+  constexpr int kRows = cta_threads(THREADS) / THREADS, N = 8 * CHUNKS;
+  static_assert(kRows == 1 || THREADS <= 32, "several rows per CTA: a warp's lanes each, or part of them");
+  using X = Staged<XT, THREADS, CHUNKS>;
+  using Y = Staged<YT, THREADS, CHUNKS>;
+  extern __shared__ __align__(16) unsigned char s_ring[];
+  __shared__ float s_part[2][32];
+  int turn = 0;
+  Places<THREADS, CHUNKS, EVEN> pl{(int)threadIdx.x % THREADS, a.d, 0};
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  constexpr int kOfWarp = THREADS < 32 ? 32 / THREADS : 1;  // a warp's rows go together
+  const int sub = threadIdx.x / THREADS % kOfWarp;
+  int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
+  unsigned char* ring = s_ring + threadIdx.x / THREADS * a.depth * a.slot;
+  const auto shift_of = [&](int64_t r) { return EVEN ? (int)((a.base + r * a.stride) & 7) : 0; };
+  const auto fetch = [&](int slot, int64_t r) {
+    if constexpr (EVEN) {
+      if (r < a.n) {
+        const Places<THREADS, CHUNKS, true> at{pl.t, a.d, shift_of(r)};
+        unsigned char* to = ring + slot * a.slot;
+        X::begin(to, a.x, r * a.x_row, at);
+        if (a.y) Y::begin(to + X::kBytes, a.y, r * a.y_row, at);
+        if (a.gate && a.gate_row) Y::begin(to + X::kBytes + Y::kBytes, a.gate, r * a.gate_row, at);
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+  };
+  if constexpr (EVEN)
+    for (int i = 0; i < a.depth; ++i) fetch(i, row + i * step);
+  for (int slot = 0; row - sub < a.n; row += step) {  // (all lanes of a warp, all warps of a row)
+    const bool live = kOfWarp == 1 || row < a.n;
+    // One array of the row's values at a time stays in registers; what each group of eight takes besides comes when it is
+    // its turn.
+    float v[N];
+    const bool gate_rows = a.gate && a.gate_row;
+    pl.shift = shift_of(row);
+    const unsigned char* from = ring + slot * a.slot;
+    if constexpr (EVEN) {
+      if (a.depth >= 4) asm volatile("cp.async.wait_group 3;" ::: "memory");
+      else if (a.depth == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+      else if (a.depth == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+      else asm volatile("cp.async.wait_group 0;" ::: "memory");
+      __syncwarp();
+    }
+    const auto get_x = [&](int c, float* to) {
+      if constexpr (EVEN) X::get(from, pl, c, to);
+      else if (live) pl.template load<XT>(static_cast<const typename Elem<XT>::Raw*>(a.x) + row * a.x_row, c, to);
+    };
+    if (a.y) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        if constexpr (EVEN) Y::get(from + X::kBytes, pl, c, v + 8 * c);
+        else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.y) + row * a.y_row, c, v + 8 * c);
+      }
+      float inv = 1.f;
+      if (a.post.kind != TSD_NORM_NONE) inv = statistics(a.post, pl, v, s_part, turn);
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        float* z = v + 8 * c;
+        if (a.post.kind != TSD_NORM_NONE) scaled(a.post, pl, c, inv, z);
+        if (a.gate) {
+          float g[8];
+          if (!gate_rows) pl.template load<YT>(a.gate, c, g);
+          else if constexpr (EVEN) Y::get(from + X::kBytes + Y::kBytes, pl, c, g);
+          else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.gate) + row * a.gate_row, c, g);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) z[i] *= g[i];
+        }
+        float x[8];
+        get_x(c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = fmaf(a.scale, z[i], x[i]);
+        if (live) pl.template store<XT>(a.r, row * a.r_row, c, z);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) get_x(c, v + 8 * c);
+    }
+    if constexpr (EVEN) {
+      __syncwarp();  // the slot has been read
+      fetch(slot, row + a.depth * step);
+      slot = slot + 1 == a.depth ? 0 : slot + 1;
+    }
+    if (a.norm.kind != TSD_NORM_NONE) {
+      const float inv = statistics(a.norm, pl, v, s_part, turn);
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        scaled(a.norm, pl, c, inv, v + 8 * c);
+        if (live) pl.template store<YT>(a.h, row * a.h_row, c, v + 8 * c);
+      }
+    }
+  }
+}
+
+template <int XT, int YT, bool EVEN>
+cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
+  const auto go = [&](auto threads, auto chunks) {
+    constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
+    constexpr int kRows = cta_threads(T) / T;
+    int per_sm = ctas_per_sm(T, C);
+    if (EVEN) {
+      a.slot = Staged<XT, T, C>::kBytes + ((a.y ? 1 : 0) + (a.gate && a.gate_row ? 1 : 0)) * Staged<YT, T, C>::kBytes;
+      a.depth = std::min(std::max(kRingBytes / (per_sm * kRows * a.slot), 1), 4);
+      per_sm = std::max(1, std::min(per_sm, kMaxSmem / (a.depth * kRows * a.slot)));
+      const cudaError_t e = smem_opt_in<k_residual_norm<XT, YT, T, C, EVEN>>(kMaxSmem);
+      if (e != cudaSuccess) return e;
+    }
+    const int ctas = std::min((a.n + kRows - 1) / kRows, sms * per_sm);
+    k_residual_norm<XT, YT, T, C, EVEN><<<(unsigned)ctas, cta_threads(T), (size_t)a.depth * kRows * a.slot, s>>>(a);
+    return cudaGetLastError();
+  };
+  using std::integral_constant;
+  const int d = a.d + (EVEN && (a.base || a.stride) ? 7 : 0);  // (with the elements that a row's first group may begin before it)
+  // Up to 32 elements per thread: what each thread does besides (the sums' joins, the root) then weighs little.  Few rows:
+  // as many threads as a row has groups.  200 x 777 with norms on both sides: 4.0 us, with 32 threads per row 7.8.
+  if constexpr (EVEN)
+    if (a.n <= 6 * sms && d > 256) {
+      if (d <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+      if (d <= 1024) return go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+      if (d <= 2048) return go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+      if (d <= 4096) return go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+      if (d <= 8192) return go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+    }
+  if (d <= 64) return go(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+  if (d <= 128) return go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+  if (d <= 256) return go(integral_constant<int, 16>{}, integral_constant<int, 2>{});
+  if (d <= 512) return go(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+  if (d <= 1024) return go(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+  if (d <= 2048) return go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  if (d <= 4096) return go(integral_constant<int, 128>{}, integral_constant<int, 4>{});
+  if (d <= 8192) return go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+  return go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+}
+
+}  // namespace
+
+template <int XT, int YT>
+cudaError_t norm_launch(const NormArgs& a, bool even, int sms, cudaStream_t s) {
+  return even ? launch<XT, YT, true>(a, sms, s) : launch<XT, YT, false>(a, sms, s);
+}
+
+}  // namespace tsd

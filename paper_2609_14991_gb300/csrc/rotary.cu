@@ -83,10 +83,61 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
   constexpr int kWide = 16 / (int)sizeof(Raw);
   constexpr int kTurn = WIDE ? kWide : PAIRS ? 2 : 1;  // elements (of each half) of a turned item
   constexpr int kPass = WIDE ? kWide : 1;              // ... of one that stays as it is
+  constexpr int kAtOnce = PAIRS ? 4 : 2;               // items of a thread on their way together
   __shared__ alignas(16) float2 s_turn[kMaxAngles];
   __shared__ int s_pos[kMaxRows], s_state[kMaxRows];  // state: 0 a row of no sequence, 1 turned, 2 NaN
   const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned turned = (PAIRS ? a.rot : half) / kTurn, per_head = turned + (a.dim - a.rot) / kPass, per_row = per_head * a.heads;
+  const unsigned total = per_row * rows;
+  // a thread's items, kThreads apart: row, head (queries', then keys') and place in the head
+  struct Item {
+    unsigned r, h, at;
+  };
+  unsigned i = threadIdx.x;
+  Item next{i / per_row, 0, 0};
+  next.h = (i - next.r * per_row) / per_head;
+  next.at = i - next.r * per_row - next.h * per_head;
+  const unsigned step_h = kThreads / per_head, step_at = kThreads % per_head;
+  const auto advance = [&] {
+    next.at += step_at;
+    next.h += step_h;
+    if (next.at >= per_head) next.at -= per_head, ++next.h;
+    while (next.h >= (unsigned)a.heads) next.h -= a.heads, ++next.r;
+  };
+  const auto place = [&](const Item& t, bool out) {
+    const bool key = t.h >= (unsigned)a.heads_q;
+    const HeadRows& x = key ? a.k : a.q;
+    const int64_t row = row0 + (int)t.r, head = key ? t.h - a.heads_q : t.h;
+    return out ? row * x.out_row + head * x.out_head : row * x.row + head * x.head;
+  };
+  const auto base = [&](const Item& t, bool out) {
+    const HeadRows& x = t.h >= (unsigned)a.heads_q ? a.k : a.q;
+    return (out ? static_cast<Raw*>(x.out) : static_cast<Raw*>(const_cast<void*>(x.x))) + place(t, out);
+  };
+  Item items[kAtOnce];
+  Some<DT, kTurn, WIDE> v[kAtOnce], z[PAIRS ? 1 : kAtOnce];
+  static_assert(kPass <= kTurn, "");
+  const auto fetch = [&] {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      items[u] = next;
+      if (i + u * kThreads < total) {
+        const Raw* x = base(next, false);
+        if (next.at >= turned) {
+          Some<DT, kPass, WIDE> w;
+          w.load(x + a.rot + (next.at - turned) * kPass);
+#pragma unroll
+          for (int j = 0; j < kPass; ++j) v[u].x[j] = w.x[j];
+        } else {
+          v[u].load(x + next.at * kTurn);
+          if constexpr (!PAIRS) z[u].load(x + half + next.at * kTurn);
+        }
+      }
+      advance();
+    }
+  };
+  fetch();  // the first items are on their way while positions and angles are found
   if (warp < rows) {
     const int r = row0 + warp;
     int pos = 0, state = 1;
@@ -108,58 +159,53 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
     if (lane == 0) s_pos[warp] = pos, s_state[warp] = state;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
-    const int r = i / half;
-    if (s_state[r] == 1) s_turn[i] = turn_of(s_pos[r], __ldg(a.turns + (i - r * half)), a.magnitude);
+  for (int j = threadIdx.x; j < rows * half; j += kThreads) {
+    const int r = j / half;
+    if (s_state[r] == 1) s_turn[j] = turn_of(s_pos[r], __ldg(a.turns + (j - r * half)), a.magnitude);
   }
   __syncthreads();
-  const unsigned turned = (PAIRS ? a.rot : half) / kTurn, per_head = turned + (a.dim - a.rot) / kPass, per_row = per_head * a.heads;
-  for (unsigned i = threadIdx.x; i < per_row * rows; i += kThreads) {
-    const unsigned r = i / per_row, in_row = i - r * per_row, h = in_row / per_head, item = in_row - h * per_head;
-    const int state = s_state[r];
-    if (state == 0) continue;
-    const bool key = (int)h >= a.heads_q;
-    const HeadRows& t = key ? a.k : a.q;
-    const int64_t row = row0 + (int)r, head = key ? (int)h - a.heads_q : (int)h;
-    const Raw* x = static_cast<const Raw*>(t.x) + row * t.row + head * t.head;
-    Raw* out = static_cast<Raw*>(t.out) + row * t.out_row + head * t.out_head;
-    const Raw nan = Elem<DT>::narrow(__uint_as_float(0x7fc00000u));
-    if (item >= turned) {
-      const int at = a.rot + (int)(item - turned) * kPass;
-      if (state == 1 && x + at == out + at) continue;
-      Some<DT, kPass, WIDE> v;
-      v.load(x + at);
-      if (state == 2)
+  const Raw nan = Elem<DT>::narrow(__uint_as_float(0x7fc00000u));
+  for (; i < total; i += kAtOnce * kThreads) {
 #pragma unroll
-        for (int j = 0; j < kPass; ++j) v.x[j] = nan;
-      v.store(out + at);
-    } else if constexpr (PAIRS) {
-      const float2* turn = s_turn + r * half + item * (kTurn / 2);
-      Some<DT, kTurn, WIDE> v;
-      v.load(x + item * kTurn);
+    for (int u = 0; u < kAtOnce; ++u) {
+      const Item& t = items[u];
+      if (i + u * kThreads >= total) break;
+      const int state = s_state[t.r];
+      if (state == 0) continue;
+      Raw* out = base(t, true);
+      if (t.at >= turned) {
+        const unsigned at = a.rot + (t.at - turned) * kPass;
+        if (state == 1 && out == base(t, false)) continue;
+        Some<DT, kPass, WIDE> w;
 #pragma unroll
-      for (int j = 0; j < kTurn; j += 2) {
-        const float2 cs = turn[j / 2];
-        const float u = Elem<DT>::wide(v.x[j]), w = Elem<DT>::wide(v.x[j + 1]);
-        v.x[j] = state == 2 ? nan : Elem<DT>::narrow(u * cs.x - w * cs.y);
-        v.x[j + 1] = state == 2 ? nan : Elem<DT>::narrow(w * cs.x + u * cs.y);
+        for (int j = 0; j < kPass; ++j) w.x[j] = state == 2 ? nan : v[u].x[j];
+        w.store(out + at);
+      } else if constexpr (PAIRS) {
+        const float2* turn = s_turn + t.r * half + t.at * (kTurn / 2);
+#pragma unroll
+        for (int j = 0; j < kTurn; j += 2) {
+          const float2 cs = turn[j / 2];
+          const float x = Elem<DT>::wide(v[u].x[j]), y = Elem<DT>::wide(v[u].x[j + 1]);
+          v[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(x * cs.x - y * cs.y);
+          v[u].x[j + 1] = state == 2 ? nan : Elem<DT>::narrow(y * cs.x + x * cs.y);
+        }
+        v[u].store(out + t.at * kTurn);
+      } else {
+        const float2* turn = s_turn + t.r * half + t.at * kTurn;
+#pragma unroll
+        for (int j = 0; j < kTurn; ++j) {
+          const float2 cs = turn[j];
+          const float x = Elem<DT>::wide(v[u].x[j]), y = Elem<DT>::wide(z[u].x[j]);
+          v[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(x * cs.x - y * cs.y);
+          z[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(y * cs.x + x * cs.y);
+        }
+        v[u].store(out + t.at * kTurn);
+        z[u].store(out + half + t.at * kTurn);
       }
-      v.store(out + item * kTurn);
-    } else {
-      const float2* turn = s_turn + r * half + item * kTurn;
-      Some<DT, kTurn, WIDE> v, z;
-      v.load(x + item * kTurn);
-      z.load(x + half + item * kTurn);
-#pragma unroll
-      for (int j = 0; j < kTurn; ++j) {
-        const float2 cs = turn[j];
-        const float u = Elem<DT>::wide(v.x[j]), w = Elem<DT>::wide(z.x[j]);
-        v.x[j] = state == 2 ? nan : Elem<DT>::narrow(u * cs.x - w * cs.y);
-        z.x[j] = state == 2 ? nan : Elem<DT>::narrow(w * cs.x + u * cs.y);
-      }
-      v.store(out + item * kTurn);
-      z.store(out + half + item * kTurn);
     }
+    i += kAtOnce * kThreads;
+    fetch();
+    i -= kAtOnce * kThreads;
   }
 }
 
