@@ -11,6 +11,7 @@
 // heads, which follow 16 bytes (of each half) at a time.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "elem.cuh"
 #include "internal.h"
@@ -24,6 +25,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxRows = 8;        // rows of a CTA
 constexpr int kMaxAngles = 2048;   // ... and their angles
+constexpr int kStaged = 24 * 1024; // bytes of heads that a CTA stages
 
 struct HeadRows {
   const void* x;
@@ -36,7 +38,8 @@ struct RotaryArgs {
   const int32_t *positions, *slots, *lens, *starts;
   int n, n_slots, rows;
   int rot, dim, heads_q, heads;  // heads: of queries and keys
-  int per_cta;                   // rows of a CTA
+  int per_cta, heads_cta;        // rows of a CTA, and (staged) heads
+  bool pairs;                    // neighbours are a pair
   float magnitude;
   HeadRows q, k;
 };
@@ -53,91 +56,14 @@ __device__ __forceinline__ float2 turn_of(int p, unsigned long long t, float m) 
   return make_float2((quarter + 1) & 2 ? -x : x, quarter & 2 ? -y : y);
 }
 
-// V adjacent elements; WIDE: by one access
-template <int DT, int V, bool WIDE>
-struct Some {
-  using Raw = typename Elem<DT>::Raw;
-  Raw x[V];
-  __device__ __forceinline__ void load(const Raw* p) {
-    if constexpr (WIDE) {
-      static_assert(sizeof(x) == 16);
-      *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(p);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) x[i] = p[i];
-    }
-  }
-  __device__ __forceinline__ void store(Raw* p) const {
-    if constexpr (WIDE) {
-      *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(x);
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) p[i] = x[i];
-    }
-  }
+// Rows row0 .. row0 + rows - 1 of a CTA: positions, states and angles in shared memory.
+struct Turns {
+  float2 cs[kMaxAngles];               // [rows][rot / 2] (cosine, sine)
+  int pos[kMaxRows], state[kMaxRows];  // state: 0 a row of no sequence, 1 turned, 2 NaN
 };
 
-template <int DT, bool PAIRS, bool WIDE>  // PAIRS: neighbours are a pair
-__global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ RotaryArgs a) {
-  using Raw = typename Elem<DT>::Raw;
-  constexpr int kWide = 16 / (int)sizeof(Raw);
-  constexpr int kTurn = WIDE ? kWide : PAIRS ? 2 : 1;  // elements (of each half) of a turned item
-  constexpr int kPass = WIDE ? kWide : 1;              // ... of one that stays as it is
-  constexpr int kAtOnce = PAIRS ? 4 : 2;               // items of a thread on their way together
-  __shared__ alignas(16) float2 s_turn[kMaxAngles];
-  __shared__ int s_pos[kMaxRows], s_state[kMaxRows];  // state: 0 a row of no sequence, 1 turned, 2 NaN
-  const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const unsigned turned = (PAIRS ? a.rot : half) / kTurn, per_head = turned + (a.dim - a.rot) / kPass, per_row = per_head * a.heads;
-  const unsigned total = per_row * rows;
-  // a thread's items, kThreads apart: row, head (queries', then keys') and place in the head
-  struct Item {
-    unsigned r, h, at;
-  };
-  unsigned i = threadIdx.x;
-  Item next{i / per_row, 0, 0};
-  next.h = (i - next.r * per_row) / per_head;
-  next.at = i - next.r * per_row - next.h * per_head;
-  const unsigned step_h = kThreads / per_head, step_at = kThreads % per_head;
-  const auto advance = [&] {
-    next.at += step_at;
-    next.h += step_h;
-    if (next.at >= per_head) next.at -= per_head, ++next.h;
-    while (next.h >= (unsigned)a.heads) next.h -= a.heads, ++next.r;
-  };
-  const auto place = [&](const Item& t, bool out) {
-    const bool key = t.h >= (unsigned)a.heads_q;
-    const HeadRows& x = key ? a.k : a.q;
-    const int64_t row = row0 + (int)t.r, head = key ? t.h - a.heads_q : t.h;
-    return out ? row * x.out_row + head * x.out_head : row * x.row + head * x.head;
-  };
-  const auto base = [&](const Item& t, bool out) {
-    const HeadRows& x = t.h >= (unsigned)a.heads_q ? a.k : a.q;
-    return (out ? static_cast<Raw*>(x.out) : static_cast<Raw*>(const_cast<void*>(x.x))) + place(t, out);
-  };
-  Item items[kAtOnce];
-  Some<DT, kTurn, WIDE> v[kAtOnce], z[PAIRS ? 1 : kAtOnce];
-  static_assert(kPass <= kTurn, "");
-  const auto fetch = [&] {
-#pragma unroll
-    for (int u = 0; u < kAtOnce; ++u) {
-      items[u] = next;
-      if (i + u * kThreads < total) {
-        const Raw* x = base(next, false);
-        if (next.at >= turned) {
-          Some<DT, kPass, WIDE> w;
-          w.load(x + a.rot + (next.at - turned) * kPass);
-#pragma unroll
-          for (int j = 0; j < kPass; ++j) v[u].x[j] = w.x[j];
-        } else {
-          v[u].load(x + next.at * kTurn);
-          if constexpr (!PAIRS) z[u].load(x + half + next.at * kTurn);
-        }
-      }
-      advance();
-    }
-  };
-  fetch();  // the first items are on their way while positions and angles are found
+__device__ __forceinline__ void find_turns(const RotaryArgs& a, int row0, int rows, Turns& s) {
+  const int half = a.rot / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (warp < rows) {
     const int r = row0 + warp;
     int pos = 0, state = 1;
@@ -156,69 +82,192 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
         }
       }
     }
-    if (lane == 0) s_pos[warp] = pos, s_state[warp] = state;
+    if (lane == 0) s.pos[warp] = pos, s.state[warp] = state;
   }
   __syncthreads();
-  for (int j = threadIdx.x; j < rows * half; j += kThreads) {
-    const int r = j / half;
-    if (s_state[r] == 1) s_turn[j] = turn_of(s_pos[r], __ldg(a.turns + (j - r * half)), a.magnitude);
+  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+    const int r = i / half;
+    if (s.state[r] == 1) s.cs[i] = turn_of(s.pos[r], __ldg(a.turns + (i - r * half)), a.magnitude);
   }
   __syncthreads();
-  const Raw nan = Elem<DT>::narrow(__uint_as_float(0x7fc00000u));
+}
+
+// A thread's items, kThreads apart, of rows x heads x per_head: row, head (queries', then keys') and place in the head.
+struct Items {
+  unsigned heads, per_head, r, h, at, step_h, step_at;
+  __device__ __forceinline__ Items(unsigned hs, unsigned per) : heads(hs), per_head(per) {
+    const unsigned i = threadIdx.x, per_row = heads * per_head;
+    r = i / per_row;
+    h = (i - r * per_row) / per_head;
+    at = i - r * per_row - h * per_head;
+    step_h = kThreads / per_head;
+    step_at = kThreads - step_h * per_head;
+  }
+  __device__ __forceinline__ void advance() {
+    at += step_at;
+    h += step_h;
+    if (at >= per_head) at -= per_head, ++h;
+    while (h >= heads) h -= heads, ++r;
+  }
+};
+
+template <class Raw>
+__device__ __forceinline__ Raw* head_at(const RotaryArgs& a, int row, unsigned h, bool out) {
+  const bool key = h >= (unsigned)a.heads_q;
+  const HeadRows& x = key ? a.k : a.q;
+  const int64_t head = key ? h - a.heads_q : h;
+  return out ? static_cast<Raw*>(x.out) + row * x.out_row + head * x.out_head : static_cast<Raw*>(const_cast<void*>(x.x)) + row * x.row + head * x.head;
+}
+
+// (a, b) turned
+__device__ __forceinline__ float2 turn(float a, float b, float2 cs) { return make_float2(a * cs.x - b * cs.y, b * cs.x + a * cs.y); }
+
+// 16 bytes at a time: both halves of a pair (PAIRS: neighbours) begin at 16-byte boundaries.
+template <int DT, bool PAIRS>
+__global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ RotaryArgs a) {
+  using Raw = typename Elem<DT>::Raw;
+  constexpr int kPer = 16 / (int)sizeof(Raw);  // elements of 16 bytes
+  constexpr int kAtOnce = 2;                   // items of a thread on their way together
+  __shared__ Turns s;
+  const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
+  const unsigned turned = (PAIRS ? a.rot : half) / kPer, per_head = turned + (a.dim - a.rot) / kPer, total = per_head * a.heads * rows;
+  Items next(a.heads, per_head);
+  struct Item {
+    unsigned r, h, at;
+    uint4 v, z;
+  } items[kAtOnce];
+  unsigned i = threadIdx.x;
+  const auto fetch = [&](unsigned first) {
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      Item& t = items[u];
+      t.r = next.r, t.h = next.h, t.at = next.at;
+      if (first + u * kThreads < total) {
+        const Raw* x = head_at<Raw>(a, row0 + (int)t.r, t.h, false);
+        t.v = *reinterpret_cast<const uint4*>(t.at < turned ? x + t.at * kPer : x + a.rot + (t.at - turned) * kPer);
+        if (!PAIRS && t.at < turned) t.z = *reinterpret_cast<const uint4*>(x + half + t.at * kPer);
+      }
+      next.advance();
+    }
+  };
+  fetch(i);  // the first items are on their way while positions and angles are found
+  find_turns(a, row0, rows, s);
+  const uint32_t nan = DT == TSD_F32 ? 0x7fc00000u : DT == TSD_BF16 ? 0x7fc07fc0u : 0x7e007e00u;
   for (; i < total; i += kAtOnce * kThreads) {
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      const Item& t = items[u];
+      Item& t = items[u];
       if (i + u * kThreads >= total) break;
-      const int state = s_state[t.r];
+      const int state = s.state[t.r];
       if (state == 0) continue;
-      Raw* out = base(t, true);
+      Raw* out = head_at<Raw>(a, row0 + (int)t.r, t.h, true);
+      if (state == 2) t.v = t.z = make_uint4(nan, nan, nan, nan);
       if (t.at >= turned) {
-        const unsigned at = a.rot + (t.at - turned) * kPass;
-        if (state == 1 && out == base(t, false)) continue;
-        Some<DT, kPass, WIDE> w;
-#pragma unroll
-        for (int j = 0; j < kPass; ++j) w.x[j] = state == 2 ? nan : v[u].x[j];
-        w.store(out + at);
-      } else if constexpr (PAIRS) {
-        const float2* turn = s_turn + t.r * half + t.at * (kTurn / 2);
-#pragma unroll
-        for (int j = 0; j < kTurn; j += 2) {
-          const float2 cs = turn[j / 2];
-          const float x = Elem<DT>::wide(v[u].x[j]), y = Elem<DT>::wide(v[u].x[j + 1]);
-          v[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(x * cs.x - y * cs.y);
-          v[u].x[j + 1] = state == 2 ? nan : Elem<DT>::narrow(y * cs.x + x * cs.y);
-        }
-        v[u].store(out + t.at * kTurn);
-      } else {
-        const float2* turn = s_turn + t.r * half + t.at * kTurn;
-#pragma unroll
-        for (int j = 0; j < kTurn; ++j) {
-          const float2 cs = turn[j];
-          const float x = Elem<DT>::wide(v[u].x[j]), y = Elem<DT>::wide(z[u].x[j]);
-          v[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(x * cs.x - y * cs.y);
-          z[u].x[j] = state == 2 ? nan : Elem<DT>::narrow(y * cs.x + x * cs.y);
-        }
-        v[u].store(out + t.at * kTurn);
-        z[u].store(out + half + t.at * kTurn);
+        if (state == 1 && out == head_at<Raw>(a, row0 + (int)t.r, t.h, false)) continue;  // in place
+        *reinterpret_cast<uint4*>(out + a.rot + (t.at - turned) * kPer) = t.v;
+        continue;
       }
+      const float2* cs = s.cs + t.r * half + t.at * (PAIRS ? kPer / 2 : kPer);
+      if (state == 1) {
+        uint32_t v[4] = {t.v.x, t.v.y, t.v.z, t.v.w}, z[4] = {t.z.x, t.z.y, t.z.z, t.z.w};
+        if constexpr (PAIRS && DT == TSD_F32) {
+#pragma unroll
+          for (int j = 0; j < 4; j += 2) {
+            const float2 y = turn(__uint_as_float(v[j]), __uint_as_float(v[j + 1]), cs[j / 2]);
+            v[j] = __float_as_uint(y.x), v[j + 1] = __float_as_uint(y.y);
+          }
+        } else if constexpr (PAIRS) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 x = Elem<DT>::wide_pair(v[j]), y = turn(x.x, x.y, cs[j]);
+            v[j] = narrow2<Elem<DT>::kBf16>(y.x, y.y);
+          }
+        } else if constexpr (DT == TSD_F32) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y = turn(__uint_as_float(v[j]), __uint_as_float(z[j]), cs[j]);
+            v[j] = __float_as_uint(y.x), z[j] = __float_as_uint(y.y);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 x = Elem<DT>::wide_pair(v[j]), y = Elem<DT>::wide_pair(z[j]);
+            const float4 c = *reinterpret_cast<const float4*>(cs + 2 * j);
+            const float2 p = turn(x.x, y.x, make_float2(c.x, c.y)), q = turn(x.y, y.y, make_float2(c.z, c.w));
+            v[j] = narrow2<Elem<DT>::kBf16>(p.x, q.x);
+            z[j] = narrow2<Elem<DT>::kBf16>(p.y, q.y);
+          }
+        }
+        t.v = make_uint4(v[0], v[1], v[2], v[3]), t.z = make_uint4(z[0], z[1], z[2], z[3]);
+      }
+      *reinterpret_cast<uint4*>(out + t.at * kPer) = t.v;
+      if (!PAIRS) *reinterpret_cast<uint4*>(out + half + t.at * kPer) = t.z;
     }
-    i += kAtOnce * kThreads;
-    fetch();
-    i -= kAtOnce * kThreads;
+    fetch(i + kAtOnce * kThreads);
+  }
+}
+
+// Any number of turned dimensions: heads through shared memory, where neighbouring lanes turn neighbouring pairs.  WIDE: heads begin
+// and end at 16-byte boundaries, and come and leave by them; else element by element.
+template <int DT, bool WIDE>
+__global__ void __launch_bounds__(kThreads) k_rotary_staged(const __grid_constant__ RotaryArgs a) {
+  using Raw = typename Elem<DT>::Raw;
+  constexpr int kPer = WIDE ? 16 / (int)sizeof(Raw) : 1;
+  using Unit = typename std::conditional<WIDE, uint4, Raw>::type;
+  __shared__ Turns s;
+  extern __shared__ __align__(16) unsigned char s_raw[];
+  Raw* const data = reinterpret_cast<Raw*>(s_raw);
+  const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
+  const unsigned head0 = blockIdx.y * a.heads_cta, heads = min(a.heads_cta, a.heads - (int)head0), per_head = a.dim / kPer, total = per_head * heads * rows;
+  {
+    Items t(heads, per_head);
+    for (unsigned i = threadIdx.x; i < total; i += kThreads, t.advance()) {
+      const Raw* x = head_at<Raw>(a, row0 + (int)t.r, head0 + t.h, false) + t.at * kPer;
+      if constexpr (WIDE)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(data + i * kPer)), "l"(x) : "memory");
+      else
+        data[i] = *x;
+    }
+    if constexpr (WIDE) asm volatile("cp.async.wait_all;" ::: "memory");
+  }
+  find_turns(a, row0, rows, s);
+  {
+    Items t(heads, half);
+    for (unsigned i = threadIdx.x; i < half * heads * rows; i += kThreads, t.advance()) {
+      if (s.state[t.r] != 1) continue;
+      Raw* x = data + (t.r * heads + t.h) * a.dim;
+      Raw &u = x[a.pairs ? 2 * t.at : t.at], &w = x[a.pairs ? 2 * t.at + 1 : half + t.at];
+      const float2 y = turn(Elem<DT>::wide(u), Elem<DT>::wide(w), s.cs[t.r * half + t.at]);
+      u = Elem<DT>::narrow(y.x), w = Elem<DT>::narrow(y.y);
+    }
+  }
+  __syncthreads();
+  Items t(heads, per_head);
+  for (unsigned i = threadIdx.x; i < total; i += kThreads, t.advance()) {
+    const int state = s.state[t.r];
+    if (state == 0) continue;
+    Unit v = reinterpret_cast<const Unit*>(data)[i];
+    if (state == 2) {
+      const Raw nan = Elem<DT>::narrow(__uint_as_float(0x7fc00000u));
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) reinterpret_cast<Raw*>(&v)[j] = nan;
+    }
+    *reinterpret_cast<Unit*>(head_at<Raw>(a, row0 + (int)t.r, head0 + t.h, true) + t.at * kPer) = v;
   }
 }
 
 template <int DT>
-void launch(const RotaryArgs& a, bool pairs, bool wide, cudaStream_t s) {
+void launch(const RotaryArgs& a, bool direct, bool wide, cudaStream_t s) {
   const unsigned grid = (unsigned)((a.rows + a.per_cta - 1) / a.per_cta);
-  if (pairs) {
-    if (wide) k_rotary<DT, true, true><<<grid, kThreads, 0, s>>>(a);
-    else k_rotary<DT, true, false><<<grid, kThreads, 0, s>>>(a);
-  } else {
-    if (wide) k_rotary<DT, false, true><<<grid, kThreads, 0, s>>>(a);
-    else k_rotary<DT, false, false><<<grid, kThreads, 0, s>>>(a);
+  if (direct) {
+    if (a.pairs) k_rotary<DT, true><<<grid, kThreads, 0, s>>>(a);
+    else k_rotary<DT, false><<<grid, kThreads, 0, s>>>(a);
+    return;
   }
+  const dim3 g(grid, (unsigned)((a.heads + a.heads_cta - 1) / a.heads_cta));
+  const size_t bytes = (size_t)a.per_cta * a.heads_cta * a.dim * sizeof(typename Elem<DT>::Raw);
+  if (wide) k_rotary_staged<DT, true><<<g, kThreads, bytes, s>>>(a);
+  else k_rotary_staged<DT, false><<<g, kThreads, bytes, s>>>(a);
 }
 
 tsd_status check_heads(const char* what, const tsd_rotary_heads& t, int size, int rows, int dim) {
@@ -307,15 +356,17 @@ extern "C" tsd_status tsd_rotary_apply(const tsd_rotary* rotary, const tsd_rotar
   if (k) a.k = {k->x, k->out, k->row, k->head, k->out_row, k->out_head};
   int sms = 0;
   TSD_CUDA(device_sms(&sms));
-  // rows of a CTA: enough for its threads, but no fewer CTAs than twelve per SM
-  const int64_t per_row = (int64_t)a.heads * c.dim;
-  a.per_cta = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxRows, kMaxAngles / (c.rot / 2), 16384 / per_row, a.rows / (12 * sms)}));
+  a.pairs = c.interleaved;
   const int v = 16 / size;
-  const bool wide = is_wide(*q, v) && (!k || is_wide(*k, v)) && (c.interleaved ? c.rot : c.rot / 2) % v == 0 && c.dim % v == 0;
+  const bool wide = is_wide(*q, v) && (!k || is_wide(*k, v)) && c.dim % v == 0, direct = wide && (c.interleaved ? c.rot : c.rot / 2) % v == 0;
+  // rows of a CTA: a few items for each of its threads, but no fewer CTAs than four per SM
+  const int64_t per_row = (int64_t)a.heads * c.dim, most = direct ? 16384 : kStaged / size;
+  a.per_cta = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxRows, kMaxAngles / (c.rot / 2), most / per_row, a.rows / (4 * sms)}));
+  a.heads_cta = (int)std::min<int64_t>(a.heads, std::max<int64_t>(1, most / c.dim));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (c.dtype == TSD_F32) launch<TSD_F32>(a, c.interleaved, wide, s);
-  else if (c.dtype == TSD_BF16) launch<TSD_BF16>(a, c.interleaved, wide, s);
-  else launch<TSD_F16>(a, c.interleaved, wide, s);
+  if (c.dtype == TSD_F32) launch<TSD_F32>(a, direct, wide, s);
+  else if (c.dtype == TSD_BF16) launch<TSD_BF16>(a, direct, wide, s);
+  else launch<TSD_F16>(a, direct, wide, s);
   TSD_CUDA(cudaGetLastError());
   return TSD_OK;
 }
