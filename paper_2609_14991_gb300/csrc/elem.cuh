@@ -37,12 +37,32 @@ struct Elem {  // 16-bit floats
   static __device__ __forceinline__ Raw narrow(float x) { return (Raw)narrow2<kBf16>(x, 0.f); }
   // two elements as they lie in a 32-bit word
   static __device__ __forceinline__ float2 wide_pair(uint32_t w) { return make_float2(wide16<kBf16>(w & 0xffffu), wide16<kBf16>(w >> 16)); }
+  // the eight of four words
+  static __device__ __forceinline__ void wide4(const uint32_t (&w)[4], float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = wide_pair(w[i]);
+      x[2 * i] = v.x, x[2 * i + 1] = v.y;
+    }
+  }
+  static __device__ __forceinline__ void narrow4(const float (&x)[8], uint32_t (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = narrow2<kBf16>(x[2 * i], x[2 * i + 1]);
+  }
 };
 template <>
 struct Elem<TSD_F32> {
   using Raw = float;
   static __device__ __forceinline__ float wide(Raw x) { return x; }
   static __device__ __forceinline__ Raw narrow(float x) { return x; }
+  static __device__ __forceinline__ void wide4(const uint32_t (&w)[4], float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+  }
+  static __device__ __forceinline__ void narrow4(const float (&x)[4], uint32_t (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+  }
 };
 
 // Eight adjacent elements, 16-byte aligned, as they came from memory.

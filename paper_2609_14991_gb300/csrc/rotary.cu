@@ -22,7 +22,7 @@ namespace tsd {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kDirect = 128, kThreads = 256;  // of a CTA: 16 bytes at a time straight through, staged
 constexpr int kMaxRows = 8;        // rows of a CTA
 constexpr int kMaxAngles = 2048;   // ... and their angles
 constexpr int kStaged = 24 * 1024; // bytes of heads that a CTA stages
@@ -58,14 +58,16 @@ __device__ __forceinline__ float2 turn_of(int p, unsigned long long t, float m) 
 
 // Rows row0 .. row0 + rows - 1 of a CTA: positions, states and angles in shared memory.
 struct Turns {
-  float2 cs[kMaxAngles];               // [rows][rot / 2] (cosine, sine)
+  alignas(16) float2 cs[kMaxAngles];   // [rows][rot / 2] (cosine, sine), in an order of the kernel's
   int pos[kMaxRows], state[kMaxRows];  // state: 0 a row of no sequence, 1 turned, 2 NaN
 };
 
-__device__ __forceinline__ void find_turns(const RotaryArgs& a, int row0, int rows, Turns& s) {
-  const int half = a.rot / 2, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp < rows) {
-    const int r = row0 + warp;
+// PLACE: where the cosine and the sine of pair i of a row stand among the row's floats
+template <int THREADS, class PLACE>
+__device__ __forceinline__ void find_turns(const RotaryArgs& a, int row0, int rows, Turns& s, PLACE place) {
+  const int half = a.rot / 2, lane = threadIdx.x & 31;
+  for (int w = threadIdx.x >> 5; w < rows; w += THREADS / 32) {
+    const int r = row0 + w;
     int pos = 0, state = 1;
     if (a.positions) {
       pos = __ldg(a.positions + r);
@@ -82,17 +84,23 @@ __device__ __forceinline__ void find_turns(const RotaryArgs& a, int row0, int ro
         }
       }
     }
-    if (lane == 0) s.pos[warp] = pos, s.state[warp] = state;
+    if (lane == 0) s.pos[w] = pos, s.state[w] = state;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * half; i += kThreads) {
+  for (int i = threadIdx.x; i < rows * half; i += THREADS) {
     const int r = i / half;
-    if (s.state[r] == 1) s.cs[i] = turn_of(s.pos[r], __ldg(a.turns + (i - r * half)), a.magnitude);
+    if (s.state[r] == 1) {
+      const float2 cs = turn_of(s.pos[r], __ldg(a.turns + (i - r * half)), a.magnitude);
+      const int2 at = place(i - r * half);
+      float* to = reinterpret_cast<float*>(s.cs) + 2 * r * half;
+      to[at.x] = cs.x, to[at.y] = cs.y;
+    }
   }
   __syncthreads();
 }
 
-// A thread's items, kThreads apart, of rows x heads x per_head: row, head (queries', then keys') and place in the head.
+// A thread's items, THREADS apart, of rows x heads x per_head: row, head (queries', then keys') and place in the head.
+template <int THREADS>
 struct Items {
   unsigned heads, per_head, r, h, at, step_h, step_at;
   __device__ __forceinline__ Items(unsigned hs, unsigned per) : heads(hs), per_head(per) {
@@ -100,8 +108,8 @@ struct Items {
     r = i / per_row;
     h = (i - r * per_row) / per_head;
     at = i - r * per_row - h * per_head;
-    step_h = kThreads / per_head;
-    step_at = kThreads - step_h * per_head;
+    step_h = THREADS / per_head;
+    step_at = THREADS - step_h * per_head;
   }
   __device__ __forceinline__ void advance() {
     at += step_at;
@@ -122,16 +130,18 @@ __device__ __forceinline__ Raw* head_at(const RotaryArgs& a, int row, unsigned h
 // (a, b) turned
 __device__ __forceinline__ float2 turn(float a, float b, float2 cs) { return make_float2(a * cs.x - b * cs.y, b * cs.x + a * cs.y); }
 
-// 16 bytes at a time: both halves of a pair (PAIRS: neighbours) begin at 16-byte boundaries.
+// Twice 16 bytes at a time: halves of a head's turned dimensions begin at 16-byte boundaries.  An item is 16 bytes of
+// the first half and those of the second (PAIRS: neighbours are pairs, in each of both), or such of the other dimensions.
 template <int DT, bool PAIRS>
-__global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ RotaryArgs a) {
+__global__ void __launch_bounds__(kDirect) k_rotary(const __grid_constant__ RotaryArgs a) {
   using Raw = typename Elem<DT>::Raw;
   constexpr int kPer = 16 / (int)sizeof(Raw);  // elements of 16 bytes
   constexpr int kAtOnce = 2;                   // items of a thread on their way together
   __shared__ Turns s;
   const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
-  const unsigned turned = (PAIRS ? a.rot : half) / kPer, per_head = turned + (a.dim - a.rot) / kPer, total = per_head * a.heads * rows;
-  Items next(a.heads, per_head);
+  const unsigned turned = half / kPer, rest = (a.dim - a.rot) / kPer, twice = rest % 2 ? 0 : rest / 2;  // (an odd rest: one by one)
+  const unsigned per_head = turned + (twice ? twice : rest), total = per_head * a.heads * rows;
+  Items<kDirect> next(a.heads, per_head);
   struct Item {
     unsigned r, h, at;
     uint4 v, z;
@@ -142,68 +152,77 @@ __global__ void __launch_bounds__(kThreads) k_rotary(const __grid_constant__ Rot
     for (int u = 0; u < kAtOnce; ++u) {
       Item& t = items[u];
       t.r = next.r, t.h = next.h, t.at = next.at;
-      if (first + u * kThreads < total) {
+      if (first + u * kDirect < total) {
         const Raw* x = head_at<Raw>(a, row0 + (int)t.r, t.h, false);
-        t.v = *reinterpret_cast<const uint4*>(t.at < turned ? x + t.at * kPer : x + a.rot + (t.at - turned) * kPer);
-        if (!PAIRS && t.at < turned) t.z = *reinterpret_cast<const uint4*>(x + half + t.at * kPer);
+        if (t.at >= turned) x += a.rot - half;  // (turned * kPer is half)
+        t.v = *reinterpret_cast<const uint4*>(x + t.at * kPer);
+        if (t.at < turned || twice) t.z = *reinterpret_cast<const uint4*>(x + (t.at < turned ? turned : twice) * kPer + t.at * kPer);
       }
       next.advance();
     }
   };
   fetch(i);  // the first items are on their way while positions and angles are found
-  find_turns(a, row0, rows, s);
+  // Four floats (of two pairs) of an item stand among those of the others of the head, so that neighbouring lanes read
+  // neighbouring ones: (c0, c1, s0, s1), PAIRS (c0, s0, c1, s1).
+  constexpr int kPairs = PAIRS ? kPer / 2 : kPer;  // of 16 bytes
+  find_turns<kDirect>(a, row0, rows, s, [&](int i) {
+    const int second = PAIRS && i >= half / 2, k = second ? i - half / 2 : i;
+    const int item = k / kPairs, j = k % kPairs, at = 4 * ((second * (kPairs / 2) + j / 2) * (int)turned + item);
+    return PAIRS ? make_int2(at + 2 * (j & 1), at + 2 * (j & 1) + 1) : make_int2(at + (j & 1), at + 2 + (j & 1));
+  });
   const uint32_t nan = DT == TSD_F32 ? 0x7fc00000u : DT == TSD_BF16 ? 0x7fc07fc0u : 0x7e007e00u;
-  for (; i < total; i += kAtOnce * kThreads) {
+  for (; i < total; i += kAtOnce * kDirect) {
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
       Item& t = items[u];
-      if (i + u * kThreads >= total) break;
+      if (i + u * kDirect >= total) break;
       const int state = s.state[t.r];
       if (state == 0) continue;
       Raw* out = head_at<Raw>(a, row0 + (int)t.r, t.h, true);
       if (state == 2) t.v = t.z = make_uint4(nan, nan, nan, nan);
       if (t.at >= turned) {
         if (state == 1 && out == head_at<Raw>(a, row0 + (int)t.r, t.h, false)) continue;  // in place
-        *reinterpret_cast<uint4*>(out + a.rot + (t.at - turned) * kPer) = t.v;
+        out += a.rot - half + t.at * kPer;
+        *reinterpret_cast<uint4*>(out) = t.v;
+        if (twice) *reinterpret_cast<uint4*>(out + twice * kPer) = t.z;
         continue;
       }
-      const float2* cs = s.cs + t.r * half + t.at * (PAIRS ? kPer / 2 : kPer);
+      const float4* cs = reinterpret_cast<const float4*>(s.cs + t.r * half) + t.at;
       if (state == 1) {
         uint32_t v[4] = {t.v.x, t.v.y, t.v.z, t.v.w}, z[4] = {t.z.x, t.z.y, t.z.z, t.z.w};
-        if constexpr (PAIRS && DT == TSD_F32) {
+        if constexpr (PAIRS) {
 #pragma unroll
-          for (int j = 0; j < 4; j += 2) {
-            const float2 y = turn(__uint_as_float(v[j]), __uint_as_float(v[j + 1]), cs[j / 2]);
-            v[j] = __float_as_uint(y.x), v[j + 1] = __float_as_uint(y.y);
-          }
-        } else if constexpr (PAIRS) {
+          for (int k = 0; k < 2; ++k) {
+            uint32_t(&w)[4] = k ? z : v;
+            float x[kPer];
+            Elem<DT>::wide4(w, x);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 x = Elem<DT>::wide_pair(v[j]), y = turn(x.x, x.y, cs[j]);
-            v[j] = narrow2<Elem<DT>::kBf16>(y.x, y.y);
-          }
-        } else if constexpr (DT == TSD_F32) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 y = turn(__uint_as_float(v[j]), __uint_as_float(z[j]), cs[j]);
-            v[j] = __float_as_uint(y.x), z[j] = __float_as_uint(y.y);
+            for (int j = 0; j < kPer; j += 4) {
+              const float4 c = cs[(k * (kPairs / 2) + j / 4) * turned];
+              const float2 p = turn(x[j], x[j + 1], make_float2(c.x, c.y)), q = turn(x[j + 2], x[j + 3], make_float2(c.z, c.w));
+              x[j] = p.x, x[j + 1] = p.y, x[j + 2] = q.x, x[j + 3] = q.y;
+            }
+            Elem<DT>::narrow4(x, w);
           }
         } else {
+          float x[kPer], y[kPer];
+          Elem<DT>::wide4(v, x);
+          Elem<DT>::wide4(z, y);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float2 x = Elem<DT>::wide_pair(v[j]), y = Elem<DT>::wide_pair(z[j]);
-            const float4 c = *reinterpret_cast<const float4*>(cs + 2 * j);
-            const float2 p = turn(x.x, y.x, make_float2(c.x, c.y)), q = turn(x.y, y.y, make_float2(c.z, c.w));
-            v[j] = narrow2<Elem<DT>::kBf16>(p.x, q.x);
-            z[j] = narrow2<Elem<DT>::kBf16>(p.y, q.y);
+          for (int j = 0; j < kPer; j += 2) {
+            const float4 c = cs[j / 2 * turned];
+            const float2 p = turn(x[j], y[j], make_float2(c.x, c.z)), q = turn(x[j + 1], y[j + 1], make_float2(c.y, c.w));
+            x[j] = p.x, y[j] = p.y, x[j + 1] = q.x, y[j + 1] = q.y;
           }
+          Elem<DT>::narrow4(x, v);
+          Elem<DT>::narrow4(y, z);
         }
         t.v = make_uint4(v[0], v[1], v[2], v[3]), t.z = make_uint4(z[0], z[1], z[2], z[3]);
       }
       *reinterpret_cast<uint4*>(out + t.at * kPer) = t.v;
-      if (!PAIRS) *reinterpret_cast<uint4*>(out + half + t.at * kPer) = t.z;
+      *reinterpret_cast<uint4*>(out + half + t.at * kPer) = t.z;
     }
-    fetch(i + kAtOnce * kThreads);
+    fetch(i + kAtOnce * kDirect);
   }
 }
 
@@ -220,7 +239,7 @@ __global__ void __launch_bounds__(kThreads) k_rotary_staged(const __grid_constan
   const int half = a.rot / 2, row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
   const unsigned head0 = blockIdx.y * a.heads_cta, heads = min(a.heads_cta, a.heads - (int)head0), per_head = a.dim / kPer, total = per_head * heads * rows;
   {
-    Items t(heads, per_head);
+    Items<kThreads> t(heads, per_head);
     for (unsigned i = threadIdx.x; i < total; i += kThreads, t.advance()) {
       const Raw* x = head_at<Raw>(a, row0 + (int)t.r, head0 + t.h, false) + t.at * kPer;
       if constexpr (WIDE)
@@ -230,9 +249,9 @@ __global__ void __launch_bounds__(kThreads) k_rotary_staged(const __grid_constan
     }
     if constexpr (WIDE) asm volatile("cp.async.wait_all;" ::: "memory");
   }
-  find_turns(a, row0, rows, s);
+  find_turns<kThreads>(a, row0, rows, s, [](int i) { return make_int2(2 * i, 2 * i + 1); });
   {
-    Items t(heads, half);
+    Items<kThreads> t(heads, half);
     for (unsigned i = threadIdx.x; i < half * heads * rows; i += kThreads, t.advance()) {
       if (s.state[t.r] != 1) continue;
       Raw* x = data + (t.r * heads + t.h) * a.dim;
@@ -242,7 +261,7 @@ __global__ void __launch_bounds__(kThreads) k_rotary_staged(const __grid_constan
     }
   }
   __syncthreads();
-  Items t(heads, per_head);
+  Items<kThreads> t(heads, per_head);
   for (unsigned i = threadIdx.x; i < total; i += kThreads, t.advance()) {
     const int state = s.state[t.r];
     if (state == 0) continue;
@@ -260,8 +279,8 @@ template <int DT>
 void launch(const RotaryArgs& a, bool direct, bool wide, cudaStream_t s) {
   const unsigned grid = (unsigned)((a.rows + a.per_cta - 1) / a.per_cta);
   if (direct) {
-    if (a.pairs) k_rotary<DT, true><<<grid, kThreads, 0, s>>>(a);
-    else k_rotary<DT, false><<<grid, kThreads, 0, s>>>(a);
+    if (a.pairs) k_rotary<DT, true><<<grid, kDirect, 0, s>>>(a);
+    else k_rotary<DT, false><<<grid, kDirect, 0, s>>>(a);
     return;
   }
   const dim3 g(grid, (unsigned)((a.heads + a.heads_cta - 1) / a.heads_cta));
@@ -358,9 +377,9 @@ extern "C" tsd_status tsd_rotary_apply(const tsd_rotary* rotary, const tsd_rotar
   TSD_CUDA(device_sms(&sms));
   a.pairs = c.interleaved;
   const int v = 16 / size;
-  const bool wide = is_wide(*q, v) && (!k || is_wide(*k, v)) && c.dim % v == 0, direct = wide && (c.interleaved ? c.rot : c.rot / 2) % v == 0;
+  const bool wide = is_wide(*q, v) && (!k || is_wide(*k, v)) && c.dim % v == 0, direct = wide && c.rot / 2 % v == 0;
   // rows of a CTA: a few items for each of its threads, but no fewer CTAs than four per SM
-  const int64_t per_row = (int64_t)a.heads * c.dim, most = direct ? 16384 : kStaged / size;
+  const int64_t per_row = (int64_t)a.heads * c.dim, most = direct ? 8192 : kStaged / size;
   a.per_cta = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxRows, kMaxAngles / (c.rot / 2), most / per_row, a.rows / (4 * sms)}));
   a.heads_cta = (int)std::min<int64_t>(a.heads, std::max<int64_t>(1, most / c.dim));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
