@@ -14,10 +14,17 @@
 #include "elem.cuh"
 #include "launch.h"
 #include "norm.h"
+#include "tc_common.cuh"
 
 namespace tsd {
 
 namespace {
+
+using tc::add2;
+using tc::fma2;
+using tc::mul2;
+using tc::pair_of;
+using tc::unpair;
 
 constexpr int kMaxSmem = 227 * 1024 - 512;  // of a CTA, dynamic
 constexpr int kRingBytes = 128 * 1024;      // of an SM for rows on their way; the rest caches weights
@@ -51,70 +58,99 @@ struct Places {
   __device__ __forceinline__ bool some(int c) const { return first(c) < d; }  // (the first group always has some)
   __device__ __forceinline__ bool has(int i) const { return (unsigned)at(i) < (unsigned)d; }
 
-  // eight elements (group c's) of an array that stands anywhere; 0 past the row
+  // Eight elements (group c's), as pairs, of an array that stands anywhere; 0 past the row
   template <int DT>
-  __device__ __forceinline__ void load(const void* base, int c, float* v) const {
+  __device__ __forceinline__ void load(const void* base, int c, uint64_t* v) const {
     const typename Elem<DT>::Raw* p = static_cast<const typename Elem<DT>::Raw*>(base);
+    float x[8];
     if (EVEN && shift == 0 && d % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0) {
-      Eight<DT> x;
+      Eight<DT> y;
 #pragma unroll
-      for (int i = 0; i < Eight<DT>::kWords; ++i) x.w[i] = 0;
-      if (some(c)) x.load(p + first(c));
-      x.get(v);
+      for (int i = 0; i < Eight<DT>::kWords; ++i) y.w[i] = 0;
+      if (some(c)) y.load(p + first(c));
+      y.get(x);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = has(8 * c + i) ? Elem<DT>::wide(p[at(8 * c + i)]) : 0.f;
+      for (int i = 0; i < 8; ++i) x[i] = has(8 * c + i) ? Elem<DT>::wide(p[at(8 * c + i)]) : 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pair_of(x[2 * i], x[2 * i + 1]);
   }
   template <int DT>
-  __device__ __forceinline__ void store(void* base, int64_t row, int c, const float* v) const {
+  __device__ __forceinline__ void store(void* base, int64_t row, int c, const uint64_t* v) const {
     typename Elem<DT>::Raw* p = static_cast<typename Elem<DT>::Raw*>(base) + row;
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpair(v[i], x[2 * i], x[2 * i + 1]);
     if (EVEN && whole(c)) {
-      Eight<DT> x;
-      x.put(v);
-      x.store_even(p + first(c));
+      Eight<DT> y;
+      y.put(x);
+      y.store_even(p + first(c));
     } else if (!EVEN || some(c)) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (has(8 * c + j)) p[at(8 * c + j)] = Elem<DT>::narrow(v[j]);
+        if (has(8 * c + j)) p[at(8 * c + j)] = Elem<DT>::narrow(x[j]);
+    }
+  }
+  // group c's elements past the row become 0
+  __device__ __forceinline__ void trim(int c, uint64_t* v) const {
+    if (EVEN && whole(c)) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      unpair(v[i], a, b);
+      v[i] = pair_of(has(8 * c + 2 * i) ? a : 0.f, has(8 * c + 2 * i + 1) ? b : 0.f);
     }
   }
 };
 
+__device__ __forceinline__ float both(uint64_t v) {
+  float a, b;
+  unpair(v, a, b);
+  return a + b;
+}
+
 // The first half of a norm: v <- v or (layer) its deviations from the mean, and the factor 1 / sqrt(mean square + eps);
 // elements past the row are 0 and stay out of the sums.
 template <int THREADS, int CHUNKS, bool EVEN>
-__device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, float* v, float (*s_part)[32], int& turn) {
-  constexpr int N = 8 * CHUNKS;
+__device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, uint64_t* v, float (*s_part)[32], int& turn) {
+  constexpr int N = 4 * CHUNKS;
   if (k.kind == TSD_NORM_LAYER) {
-    float s = 0.f;
+    uint64_t s = v[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += v[i];
-    const float mean = row_sum<THREADS>(s, s_part, turn) / pl.d;
+    for (int i = 1; i < N; ++i) s = add2(s, v[i]);
+    const float mean = row_sum<THREADS>(both(s), s_part, turn) / pl.d;
+    const uint64_t m2 = pair_of(-mean, -mean);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = pl.has(i) ? v[i] - mean : 0.f;
+    for (int i = 0; i < N; ++i) v[i] = add2(v[i], m2);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) pl.trim(c, v + 4 * c);
   }
-  float s = 0.f;
+  uint64_t s = mul2(v[0], v[0]);
 #pragma unroll
-  for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
-  return 1.f / sqrtf(row_sum<THREADS>(s, s_part, turn) / pl.d + k.eps);
+  for (int i = 1; i < N; ++i) s = fma2(v[i], v[i], s);
+  return 1.f / sqrtf(row_sum<THREADS>(both(s), s_part, turn) / pl.d + k.eps);
 }
-// The second, for group c
+// The second, for group c, but for that factor: v <- v * weight
 template <int THREADS, int CHUNKS, bool EVEN>
-__device__ __forceinline__ void scaled(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, float inv, float* v) {
-  float w[8];
-  if (k.weight) {
-    pl.template load<TSD_F32>(k.weight, c, w);
+__device__ __forceinline__ void weighed(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, uint64_t* v) {
+  if (!k.weight) return;
+  uint64_t w[4];
+  pl.template load<TSD_F32>(k.weight, c, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= inv * w[i];
+  for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], w[i]);
+}
+// ... and v <- v * factor + bias
+template <int THREADS, int CHUNKS, bool EVEN>
+__device__ __forceinline__ void scaled(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, uint64_t factor, uint64_t* v) {
+  if (k.bias) {
+    uint64_t b[4];
+    pl.template load<TSD_F32>(k.bias, c, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = fma2(v[i], factor, b[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= inv;
-  }
-  if (k.bias) {
-    pl.template load<TSD_F32>(k.bias, c, w);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += w[i];
+    for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], factor);
   }
 }
 
@@ -140,18 +176,18 @@ struct Staged {
       }
   }
   template <class P>
-  static __device__ __forceinline__ void get(const unsigned char* from, const P& pl, int c, float* v) {
+  static __device__ __forceinline__ void get(const unsigned char* from, const P& pl, int c, uint64_t* v) {
     Eight<DT> x;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       const uint4 w = *reinterpret_cast<const uint4*>(from + ((c * THREADS + pl.t) * kUnits + u) * 16);
       x.w[4 * u] = w.x, x.w[4 * u + 1] = w.y, x.w[4 * u + 2] = w.z, x.w[4 * u + 3] = w.w;
     }
-    x.get(v);
-    if (!pl.whole(c))
+    float y[8];
+    x.get(y);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (!pl.has(8 * c + j)) v[j] = 0.f;
+    for (int i = 0; i < 4; ++i) v[i] = pair_of(y[2 * i], y[2 * i + 1]);
+    pl.trim(c, v);
   }
 };
 
@@ -163,7 +199,7 @@ constexpr int ctas_per_sm(int per_row, int chunks) { return (chunks == 1 ? 1024 
 // place, so no barrier guards them.
 template <int XT, int YT, int THREADS, int CHUNKS, bool EVEN>
 __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHUNKS)) k_residual_norm(const __grid_constant__ NormArgs a) {
-  constexpr int kRows = cta_threads(THREADS) / THREADS, N = 8 * CHUNKS;
+  constexpr int kRows = cta_threads(THREADS) / THREADS;
   static_assert(kRows == 1 || THREADS <= 32, "several rows per CTA: a warp's lanes each, or part of them");
   using X = Staged<XT, THREADS, CHUNKS>;
   using Y = Staged<YT, THREADS, CHUNKS>;
@@ -195,7 +231,7 @@ __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHU
     const bool live = kOfWarp == 1 || row < a.n;
     // One array of the row's values at a time stays in registers; what each group of eight takes besides comes when it is
     // its turn.
-    float v[N];
+    uint64_t v[4 * CHUNKS];
     const bool gate_rows = a.gate && a.gate_row;
     pl.shift = shift_of(row);
     const unsigned char* from = ring + slot * a.slot;
@@ -206,39 +242,48 @@ __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHU
       else asm volatile("cp.async.wait_group 0;" ::: "memory");
       __syncwarp();
     }
-    const auto get_x = [&](int c, float* to) {
+    const auto get_x = [&](int c, uint64_t* to) {
       if constexpr (EVEN) X::get(from, pl, c, to);
       else if (live) pl.template load<XT>(static_cast<const typename Elem<XT>::Raw*>(a.x) + row * a.x_row, c, to);
     };
     if (a.y) {
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        if constexpr (EVEN) Y::get(from + X::kBytes, pl, c, v + 8 * c);
-        else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.y) + row * a.y_row, c, v + 8 * c);
+        if constexpr (EVEN) Y::get(from + X::kBytes, pl, c, v + 4 * c);
+        else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.y) + row * a.y_row, c, v + 4 * c);
       }
-      float inv = 1.f;
-      if (a.post.kind != TSD_NORM_NONE) inv = statistics(a.post, pl, v, s_part, turn);
+      float factor = a.scale;  // what a gated output takes besides: scale, and the norm's factor where no bias comes between
+      uint64_t inv = 0;
+      const bool post = a.post.kind != TSD_NORM_NONE;
+      if (post) {
+        const float f = statistics(a.post, pl, v, s_part, turn);
+        if (a.post.bias) inv = pair_of(f, f);
+        else factor *= f;
+      }
+      const uint64_t factor2 = pair_of(factor, factor);
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        float* z = v + 8 * c;
-        if (a.post.kind != TSD_NORM_NONE) scaled(a.post, pl, c, inv, z);
-        if (a.gate) {
-          float g[8];
-          if (!gate_rows) pl.template load<YT>(a.gate, c, g);
-          else if constexpr (EVEN) Y::get(from + X::kBytes + Y::kBytes, pl, c, g);
-          else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.gate) + row * a.gate_row, c, g);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) z[i] *= g[i];
+        uint64_t* z = v + 4 * c;
+        if (post) {
+          weighed(a.post, pl, c, z);
+          if (a.post.bias) scaled(a.post, pl, c, inv, z);
         }
-        float x[8];
+        uint64_t x[4];
+        if (a.gate) {
+          if (!gate_rows) pl.template load<YT>(a.gate, c, x);
+          else if constexpr (EVEN) Y::get(from + X::kBytes + Y::kBytes, pl, c, x);
+          else if (live) pl.template load<YT>(static_cast<const typename Elem<YT>::Raw*>(a.gate) + row * a.gate_row, c, x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[i] = mul2(z[i], x[i]);
+        }
         get_x(c, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) z[i] = fmaf(a.scale, z[i], x[i]);
+        for (int i = 0; i < 4; ++i) z[i] = fma2(z[i], factor2, x[i]);
         if (live) pl.template store<XT>(a.r, row * a.r_row, c, z);
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) get_x(c, v + 8 * c);
+      for (int c = 0; c < CHUNKS; ++c) get_x(c, v + 4 * c);
     }
     if constexpr (EVEN) {
       __syncwarp();  // the slot has been read
@@ -246,11 +291,13 @@ __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHU
       slot = slot + 1 == a.depth ? 0 : slot + 1;
     }
     if (a.norm.kind != TSD_NORM_NONE) {
-      const float inv = statistics(a.norm, pl, v, s_part, turn);
+      const float f = statistics(a.norm, pl, v, s_part, turn);
+      const uint64_t inv = pair_of(f, f);
 #pragma unroll
       for (int c = 0; c < CHUNKS; ++c) {
-        scaled(a.norm, pl, c, inv, v + 8 * c);
-        if (live) pl.template store<YT>(a.h, row * a.h_row, c, v + 8 * c);
+        weighed(a.norm, pl, c, v + 4 * c);
+        scaled(a.norm, pl, c, inv, v + 4 * c);
+        if (live) pl.template store<YT>(a.h, row * a.h_row, c, v + 4 * c);
       }
     }
   }
@@ -269,7 +316,10 @@ cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
       const cudaError_t e = smem_opt_in<k_residual_norm<XT, YT, T, C, EVEN>>(kMaxSmem);
       if (e != cudaSuccess) return e;
     }
-    const int ctas = std::min((a.n + kRows - 1) / kRows, sms * per_sm);
+    // Many rows: two per CTA and as many CTAs as that takes, which reads and writes memory more evenly than CTAs that stay (16384 x
+    // 2048: 43 us, 47), but for one or two wide ones per SM (4000 x 12000 with norms on both sides: 173 us, 155).
+    const int groups = (a.n + kRows - 1) / kRows, stay = sms * per_sm;
+    const int ctas = per_sm > 2 && groups > 2 * stay ? (groups + 1) / 2 : std::min(groups, stay);
     k_residual_norm<XT, YT, T, C, EVEN><<<(unsigned)ctas, cta_threads(T), (size_t)a.depth * kRows * a.slot, s>>>(a);
     return cudaGetLastError();
   };
