@@ -767,7 +767,15 @@ cudaError_t launch(const TilesArgs& args, const CrossTilesPlan& p, const CUtenso
 bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, int sms, CrossTilesPlan* p) {
   const int group = heads / s.kv_heads;
   const int64_t most = std::max<int64_t>(1, b.max_rows ? std::min(b.max_rows, b.rows) : !b.starts ? 1 : ((int64_t)b.rows + b.n - 1) / b.n);
-  if (most * group <= 48 || s.k_frame < s.dim || s.v_frame < s.dim) return false;
+  if (s.k_frame < s.dim || s.v_frame < s.dim) return false;
+  // cross_rows.cu's time grows with its units of 16 rows, each of which reads the frames again (0.016 us + 0.047 us per 1000 frames at dim 128,
+  // half of that at 64), this kernel's starts at 7 to 13 us.  Here and there, us, dim 128: 64 sources of 100 frames, 8 key heads: 20 rows
+  // 14 and 23, 64 rows 14 and 46; 4 of 300, 4 key heads: 64 rows 12 and 10, 500 rows 17 and 20; one of 12000, one key head: 40
+  // rows 17 and 24.  Dim 64, 64 of 400, 8 key heads: 20 rows 28 and 23, 40 rows 28 and 31.
+  const int64_t sixteens = (most * group + 15) / 16;
+  if (sixteens < 2) return false;
+  const bool much = sixteens > (s.dim == 64 ? 2 : 1) && b.n * s.kv_heads * sixteens * (s.frames + 330) >= (s.dim == 64 ? 350000 : 200000);
+  if (!much && s.frames <= 8000) return false;
   const int64_t tiles = ((int64_t)s.frames + kFrames - 1) / kFrames;
   const int64_t units = s.kv_heads * ((int64_t)b.rows / (2 * (128 / group)) + b.n);  // at most
   const double line = (double)units * (double)(kPad + tiles * kTwo);
