@@ -829,7 +829,8 @@ typedef struct {
   int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches; results do not depend on it being right */
 } tsd_cross_batch;
 
-/* Device memory that tsd_cross_attend needs for such calls (their pointers are not read): 0 or 16-byte aligned. */
+/* Bytes of device memory, 16-byte aligned, that such a call of tsd_cross_attend needs for itself alone (may be 0; the structs'
+ * pointers are not read). */
 TSD_API tsd_status tsd_cross_attend_workspace(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads,
                                               int64_t* bytes);
 

@@ -405,7 +405,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                 }
                 tmem_ld32_begin(st + 64 * h, raw[0]);
               }
-              const float ref = m > -INFINITY ? m - 7.f : 0.f;
+              // (no maximum yet, every score so far -inf: relative to -1e30 any other has outgrown it)
+              const float ref = m > -INFINITY ? m - 7.f : look ? 0.f : -1e30f;
               const uint64_t ref2 = pair_of(-ref, -ref);
               uint64_t sums[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -774,7 +775,7 @@ bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, 
   // rows 17 and 24.  Dim 64, 64 of 400, 8 key heads: 20 rows 28 and 23, 40 rows 28 and 31.
   const int64_t sixteens = (most * group + 15) / 16;
   if (sixteens < 2) return false;
-  const bool much = sixteens > (s.dim == 64 ? 2 : 1) && b.n * s.kv_heads * sixteens * (s.frames + 330) >= (s.dim == 64 ? 350000 : 200000);
+  const bool much = sixteens > (s.dim == 64 ? 2 : 1) && (double)b.n * s.kv_heads * sixteens * (s.frames + 330.0) >= (s.dim == 64 ? 350e3 : 200e3);
   if (!much && s.frames <= 8000) return false;
   const int64_t tiles = ((int64_t)s.frames + kFrames - 1) / kFrames;
   const int64_t units = s.kv_heads * ((int64_t)b.rows / (2 * (128 / group)) + b.n);  // at most

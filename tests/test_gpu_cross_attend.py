@@ -67,6 +67,11 @@ def starts_of(counts):
     return ints([sum(counts[:i]) for i in range(len(counts) + 1)])
 
 
+def for_many_rows(n, kv, rows, frames, dim):
+    """A call's sizes (rows: tokens * heads of a group) are those of the kernel for many rows per key head."""
+    assert frames > 8000 or n * kv * (-(-rows // 16)) * (frames + 330) >= (350e3 if dim == 64 else 200e3)
+
+
 LENGTHS = [0, 1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 191, 192, 193, 255, 256, 257, 300]
 
 
@@ -77,6 +82,8 @@ def test_lengths(dtype, dim, rows):
     """Every end of a step or tile; what lies behind a source's length is NaN."""
     k, v = make(len(LENGTHS), 300, 2, dim, dtype, seed=rows, poison=math.nan, lens=LENGTHS)
     counts = [rows] * len(LENGTHS)
+    if rows == 130:
+        for_many_rows(len(LENGTHS), 2, 2 * rows, 300, dim)
     q = queries(sum(counts), 4, dim, dtype)
     out = tsd.CrossStates(k, v, ints(LENGTHS)).attend(q, starts=starts_of(counts), max_rows=rows)
     check(out, k, v, LENGTHS, q, counts, fine=rows < 16)
@@ -84,9 +91,11 @@ def test_lengths(dtype, dim, rows):
 
 
 @pytest.mark.parametrize("poison", [math.inf, -math.inf, 6e4])
-@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("rows", [1, 1500])
 def test_what_lies_behind(poison, rows):
     lens = [1, 33, 130, 200]
+    if rows > 1:
+        for_many_rows(4, 1, 2 * rows, 200, 64)
     k, v = make(4, 200, 1, 64, HF, seed=3, poison=poison, lens=lens)
     q = queries(4 * rows, 2, 64, HF)
     out = tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of([rows] * 4), max_rows=rows)
@@ -103,12 +112,23 @@ def test_groups_and_ragged_rows(group, kv, counts):
     check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max(counts)), k, v, lens, q, counts)
 
 
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 7, 16, 17, 33, 43, 64])
+@pytest.mark.parametrize("dtype,dim", [(BF, 64), (HF, 128)])
+def test_groups_of_many_rows(group, dtype, dim):
+    counts, lens = [600 // group + 1, 0, 300 // group + 1, 1], [400, 399, 131, 0]
+    for_many_rows(4, 4, max(counts) * group, 400, dim)
+    k, v = make(4, 400, 4, dim, dtype, seed=group, poison=math.nan, lens=lens)
+    q = queries(sum(counts), 4 * group, dim, dtype)
+    check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max(counts)), k, v, lens, q, counts)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("counts", [[127], [128], [129], [255], [256], [257], [1, 511, 0, 513], [700, 3]])
 def test_row_tiles(dim, counts):
-    lens = [90, 400, 1, 333][:len(counts)]
-    k, v = make(len(counts), 400, 2, dim, seed=sum(counts))
-    q = queries(sum(counts), 2, dim)
+    lens = [1490, 400, 1, 1333][:len(counts)]
+    for_many_rows(len(counts), 32, max(counts), 1500, dim)
+    k, v = make(len(counts), 1500, 32, dim, seed=sum(counts))
+    q = queries(sum(counts), 32, dim)
     check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max(counts)), k, v, lens, q, counts)
 
 
@@ -116,15 +136,18 @@ def test_row_tiles(dim, counts):
 def test_results_do_not_depend_on_the_bound(max_rows):
     """Rows without a bound, with one too low and with one too high."""
     counts, lens = [1, 300, 20, 0, 2], [500, 77, 300, 9, 1]
-    k, v = make(5, 500, 2, 64, seed=9)
-    q = queries(sum(counts), 4, 64)
+    for_many_rows(5, 4, 300 * 2, 500, 64)
+    k, v = make(5, 500, 4, 64, seed=9)
+    q = queries(sum(counts), 8, 64)
     check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max_rows), k, v, lens, q, counts)
 
 
-@pytest.mark.parametrize("rows", [1, 60])
+@pytest.mark.parametrize("rows", [1, 100])
 @pytest.mark.parametrize("frames", [1, 5000, 40001])
 def test_long_sources(rows, frames):
     lens = [frames, max(1, frames // 3)]
+    if rows > 1 and frames > 1:
+        for_many_rows(2, 1, 4 * rows, frames, 128)
     k, v = make(2, frames, 1, 128, seed=frames)
     q = queries(2 * rows, 4, 128)
     check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of([rows] * 2), max_rows=rows), k, v, lens, q, [rows] * 2)
@@ -137,9 +160,11 @@ def test_without_lengths_and_starts():
     check(tsd.CrossStates(k, v).attend(q[:2], sources=ints([2, 2])), k, v, None, q, [1] * 2, [2, 2], fine=True)
 
 
-@pytest.mark.parametrize("rows", [2, 150])
+@pytest.mark.parametrize("rows", [2, 1200])
 def test_shared_sources(rows):
     """Sequences over one source, in any order; and their rows as one sequence."""
+    if rows > 2:
+        for_many_rows(4, 2, rows, 333, 64)
     lens, sources = [40, 333], [1, 0, 1, 1]
     k, v = make(2, 333, 2, 64, seed=2)
     q = queries(4 * rows, 2, 64)
@@ -148,9 +173,11 @@ def test_shared_sources(rows):
     check(s.attend(q, starts=starts_of([4 * rows]), sources=ints([1]), max_rows=4 * rows), k, v, lens, q, [4 * rows], [1])
 
 
-@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("rows", [1, 2500])
 @pytest.mark.parametrize("bad", ["source", "negative source", "long", "negative", "rows", "backwards"])
 def test_sequences_out_of_range_are_nan(bad, rows):
+    if rows > 1:
+        for_many_rows(3, 2, rows, 90, 64)
     lens, sources, at = [30, 60, 90], [2, 1, 0], [0, rows, 2 * rows, 3 * rows]
     if bad == "source":
         sources[1] = 3
@@ -177,8 +204,10 @@ def test_sequences_out_of_range_are_nan(bad, rows):
         check(out[part], k, v, lens, q[part], [rows], [sources[i]])
 
 
-@pytest.mark.parametrize("counts", [[1, 1], [3, 200]])
+@pytest.mark.parametrize("counts", [[1, 1], [3, 9000]])
 def test_rows_behind_the_last_sequence_stay(counts):
+    if sum(counts) > 2:
+        for_many_rows(2, 2, sum(counts) // 2, 100, 64)
     k, v = make(2, 100, 2, 64)
     q = queries(sum(counts) + 5, 2, 64)
     out = torch.full_like(q, 7.0)
@@ -187,10 +216,12 @@ def test_rows_behind_the_last_sequence_stay(counts):
     assert bool((out[sum(counts):] == 7).all())
 
 
-@pytest.mark.parametrize("rows", [1, 140])
+@pytest.mark.parametrize("rows", [1, 2100])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_layouts(rows, dim):
     """Keys and values in one projection's rows; heads before frames; frames before sources; shared heads; queries and results likewise."""
+    if rows > 1:
+        for_many_rows(3, 2, rows, 150, dim)
     n, frames, kv, lens = 3, 150, 2, [150, 20, 99]
     counts = [rows] * n
     qkv = queries(n * rows, 6, dim)
@@ -208,9 +239,11 @@ def test_layouts(rows, dim):
         check(out, k, v, lens, q, counts)
 
 
-@pytest.mark.parametrize("rows", [1, 80])
+@pytest.mark.parametrize("rows", [1, 4000])
 def test_far_sources(rows):
     """Offsets past 2^32 elements."""
+    if rows > 1:
+        for_many_rows(3, 1, 2 * rows, 70, 64)
     frames, far = 70, 2 ** 31 + 64
     buf = torch.zeros(2 * far + frames * 64, dtype=BF, device="cuda")
     k = buf.as_strided((3, frames, 1, 64), (far, 64, 64, 1))
@@ -221,17 +254,21 @@ def test_far_sources(rows):
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.2, 1.0, 3.0])
-@pytest.mark.parametrize("rows", [2, 100])
+@pytest.mark.parametrize("rows", [2, 3000])
 def test_scales(scale, rows):
+    if rows > 2:
+        for_many_rows(2, 1, 2 * rows, 200, 64)
     k, v = make(2, 200, 1, 64, HF, seed=7)
     q = queries(2 * rows, 2, 64, HF)
     check(tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * 2), max_rows=rows, scale=scale), k, v, None, q, [rows] * 2, scale=scale)
 
 
-@pytest.mark.parametrize("rows", [1, 100])
+@pytest.mark.parametrize("rows", [1, 8000])
 @pytest.mark.parametrize("rising", [False, True])
 def test_maxima_that_move(rows, rising):
     """Scores that rise or fall by hundreds along the frames: each row's maximum follows."""
+    if rows > 1:
+        for_many_rows(1, 1, rows, 400, 64)
     frames = 400
     k, v = make(1, frames, 1, 64, HF, seed=8)
     ramp = torch.linspace(-200, 200, frames, device="cuda")
@@ -242,9 +279,11 @@ def test_maxima_that_move(rows, rising):
     check(tsd.CrossStates(k, v).attend(q, starts=starts_of([rows]), max_rows=rows, scale=1.0), k, v, None, q, [rows], scale=1.0)
 
 
-@pytest.mark.parametrize("rows", [1, 100])
+@pytest.mark.parametrize("rows", [1, 1700])
 def test_values_at_the_ends(rows):
     """A NaN or infinite key or value reaches the rows of its source and head alone; one frame's result is its values."""
+    if rows > 1:
+        for_many_rows(4, 2, rows, 100, 64)
     k, v = make(4, 100, 2, 64, HF, seed=5)
     k[0, 99, 0, 3] = math.nan
     v[1, 50, 1, 7] = math.inf
@@ -258,8 +297,30 @@ def test_values_at_the_ends(rows):
     assert bool(torch.isfinite(out[3]).all())
 
 
-@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("rows", [2, 700])
+@pytest.mark.parametrize("hidden", [1, 130, 600])
+def test_frames_of_infinite_scores(rows, hidden):
+    """Frames whose scores are -inf, the first of a source among them, weigh nothing; where all are, the result is NaN, as the formula's."""
+    n, frames, kv = 4, 700, 4
+    if rows > 2:
+        for_many_rows(n, kv, rows, frames, 64)
+    k, v = make(n, frames, kv, 64, HF, seed=hidden)
+    q = queries(n * rows, kv, 64, HF)
+    q[:, :, 5] = q[:, :, 5].abs() + 0.5
+    k[:, :hidden, :, 5] = -math.inf
+    k[3, :, 1, 5] = -math.inf
+    out = tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * n), max_rows=rows)
+    bad = out.view(n, rows, kv, 64)[3, :, 1]
+    assert bool(torch.isnan(bad).all())
+    out.view(n, rows, kv, 64)[3, :, 1] = 0
+    k[3, hidden:, 1, 5], v[3, hidden:, 1] = 0, 0
+    check(out, k[:, hidden:], v[:, hidden:], None, q, [rows] * n)
+
+
+@pytest.mark.parametrize("rows", [1, 1200])
 def test_a_replayed_graph_follows_lengths_and_sources(rows):
+    if rows > 1:
+        for_many_rows(2, 2, 2 * rows, 300, 64)
     k, v = make(3, 300, 2, 64, seed=11)
     lens, sources = ints([5, 6, 7]), ints([0, 1])
     s = tsd.CrossStates(k, v, lens)
@@ -277,8 +338,10 @@ def test_a_replayed_graph_follows_lengths_and_sources(rows):
         assert torch.equal(out, s.attend(q, starts=at, sources=sources, max_rows=rows))  # and run to run
 
 
-@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("rows", [1, 200])
 def test_two_streams_at_once(rows):
+    if rows > 1:
+        for_many_rows(2, 2, 2 * rows, 3000, 128)
     k, v = make(2, 3000, 2, 128, seed=12)
     s = tsd.CrossStates(k, v)
     q, at = queries(2 * rows, 4, 128), starts_of([rows] * 2)
