@@ -85,6 +85,56 @@ def test_widths(d, dtype, x_dtype):
     check(x, y, "rms", "rms", None, 1.0, None, None, None, None, 1e-6, h, r)
 
 
+@pytest.mark.parametrize("d", [1, 7, 8, 33, 64, 65, 128, 129, 256, 257, 505, 512, 513, 1017, 1024, 1025, 2041, 2048, 2049, 4089, 4097, 8192, 8193, 16376, 16378, 16384])
+@pytest.mark.parametrize("dtype,x_dtype", [(HF, HF), (BF, FL)])
+def test_widths_of_many_rows(d, dtype, x_dtype):
+    """Enough rows for as few threads per row as any number takes; odd widths, whose rows stand off multiples of eight elements."""
+    x, y, (w, b, pw, pb), gt = make(1003, d, dtype, x_dtype, "rows" if d % 2 else "channels", seed=d)
+    h, r = tsd.residual_norm(x, y, norm="layer", weight=w, bias=b, post="rms", post_weight=pw, gate=gt, scale=0.7)
+    check(x, y, "layer", "rms", gt, 0.7, w, b, pw, None, 1e-5, h, r)
+    h, r = tsd.residual_norm(x, y, norm="rms", post="layer", post_weight=pw, post_bias=pb)
+    check(x, y, "rms", "layer", None, 1.0, None, None, pw, pb, 1e-5, h, r)
+
+
+@pytest.mark.parametrize("n,d", [(40001, 33), (40001, 64), (20011, 200), (20001, 500), (9001, 1000), (9001, 1024), (5003, 1537), (5003, 2048), (3001, 4001), (1999, 6001)])
+@pytest.mark.parametrize("dtype,x_dtype", [(BF, BF), (HF, FL)])
+def test_many_rows(n, d, dtype, x_dtype):
+    """More rows than the device holds at once, an odd number of them; in place with the same bits."""
+    x, y, (w, b, pw, _), gt = make(n, d, dtype, x_dtype, "rows", seed=n)
+    h, r = tsd.residual_norm(x, y, norm="layer", weight=w, bias=b, post="rms", post_weight=pw, gate=gt)
+    check(x, y, "layer", "rms", gt, 1.0, w, b, pw, None, 1e-5, h, r)
+    tsd.residual_norm(x, y, norm="layer", weight=w, bias=b, post="rms", post_weight=pw, gate=gt, out=(y, x))
+    assert torch.equal(x, r) and torch.equal(y, h)
+
+
+@pytest.mark.parametrize("d", [40, 333, 3000, 9000])
+@pytest.mark.parametrize("n", [3, 2000])
+def test_arrays_that_stand_apart(d, n):
+    """Row arrays each off by another number of elements, and with other distances of rows."""
+    x, y, (w, b, pw, _), gt = make(n, d, BF, FL, "rows", seed=d)
+    def apart(t, shift, pad):  # noqa: E306
+        v = torch.full((n * (d + pad) + 16,), 9.0, dtype=t.dtype, device="cuda")[shift:shift + n * (d + pad)].view(n, d + pad)[:, :d]
+        v.copy_(t)
+        return v
+    h, r = apart(y, 5, 7), apart(x, 2, 1)
+    tsd.residual_norm(apart(x, 1, 3), apart(y, 3, 0), norm="layer", weight=w, bias=b, post="rms", post_weight=pw, gate=apart(gt, 0, 2), scale=0.3, out=(h, r))
+    check(x, y, "layer", "rms", gt, 0.3, w, b, pw, None, 1e-5, h, r)
+    # ... and alike, but off a multiple of eight
+    h, r = apart(y, 3, 5), apart(x, 3, 5)
+    tsd.residual_norm(apart(x, 3, 5), apart(y, 3, 5), norm="layer", weight=w, bias=b, gate=apart(gt, 3, 5), out=(h, r))
+    check(x, y, "layer", None, gt, 1.0, w, b, None, None, 1e-5, h, r)
+
+
+@pytest.mark.parametrize("shift", [1, 4])
+def test_weights_at_any_float(shift):
+    x, y, (w, b, _, _), gt = make(1200, 512, BF, BF, "channels", seed=2)
+    w2, b2 = (torch.cat([torch.zeros(shift, device="cuda"), t])[shift:] for t in (w, b))
+    g2 = torch.cat([torch.zeros(shift, dtype=BF, device="cuda"), gt])[shift:]
+    for n in (3, 1200):
+        h, r = tsd.residual_norm(x[:n], y[:n], norm="layer", weight=w2, bias=b2, gate=g2)
+        check(x[:n], y[:n], "layer", None, gt, 1.0, w, b, None, None, 1e-5, h, r)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 127, 1000])
 @pytest.mark.parametrize("d", [64, 512, 1536])
 def test_rows(n, d):

@@ -82,6 +82,23 @@ def test_given_positions(dtype, layout, dim, rot):
     assert a is q2 and torch.equal(q2, oq) and torch.equal(k2, ok)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("dim,rot", [(80, 26), (128, 100), (64, 2), (72, 72), (72, 64), (96, 80), (37, 36)])
+@pytest.mark.parametrize("heads,kv,rows", [(5, 2, 9), (170, 11, 3), (1, 1, 4000), (700, 1, 1)])
+def test_parts_of_heads(dtype, layout, dim, rot, heads, kv, rows):
+    """Turned parts that do not end at 16 bytes; heads of a row that several CTAs take; what is not turned, an odd number of times 16 bytes."""
+    pos = [(i * 7919) % 100000 for i in range(rows)]
+    r = tsd.Rotary(dim, rot, layout=layout)
+    q, k = rand(rows, heads, dim, dtype=dtype), rand(rows, kv, dim, dtype=dtype, seed=1)
+    p = torch.tensor(pos, dtype=torch.int32, device="cuda")
+    oq, ok = r(q, k, positions=p)
+    check(oq, q, pos, rot, layout)
+    check(ok, k, pos, rot, layout)
+    r(q, k, positions=p, out=(q, k))
+    assert torch.equal(q, oq) and torch.equal(k, ok)
+
+
 @pytest.mark.parametrize("pos", [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 12345, 10 ** 9])
 def test_farthest_positions(pos):
     r = tsd.Rotary(64, base=500000.0)
