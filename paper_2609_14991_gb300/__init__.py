@@ -698,7 +698,22 @@ class Encoder:
 # itself (four views of one buffer take twice as long: 11.6 and 5.9 us) and
 # remember a shape's workspace size.
 
+# What a call needs of torch, bound at the first one: a module's attribute at a time would take each
+# call a microsecond more.
 _DTYPE = None  # element type -> the library's number
+_F32 = _I32 = _U8 = _new_empty = _get_device = _get_raw_stream = None
+_devices = {}  # by number (a device given as one takes torch.empty 3 us more)
+
+
+def _bind_torch():
+    global _DTYPE, _F32, _I32, _U8, _new_empty, _get_device, _get_raw_stream
+    import torch
+
+    torch.cuda.init()
+    _F32, _I32, _U8, _new_empty = torch.float32, torch.int32, torch.uint8, torch.empty
+    _get_device, _get_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    for i in range(torch.cuda.device_count()):
+        _devices[i] = torch.device("cuda", i)
 
 
 def _dtype_code(t) -> int:
@@ -712,9 +727,9 @@ def _dtype_code(t) -> int:
 
 
 def _current_device():
-    import torch
-
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+    if _get_device is None:
+        _bind_torch()
+    return _get_device()
 
 
 def _on_current(who, name, t):
@@ -726,31 +741,29 @@ def _on_current(who, name, t):
 
 
 def _raw_stream(stream, dev) -> int:
-    import torch
-
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _get_raw_stream is None:
+        _bind_torch()
+    return _get_raw_stream(dev)
 
 
 def _empty(n, dtype, dev, stream):
     """n elements that the caching allocator gives out for the call's stream."""
+    if _new_empty is None:
+        _bind_torch()
+    if stream is None:
+        return _new_empty(n, dtype=dtype, device=_devices[dev])
     import torch
 
-    device = _devices.get(dev)  # (a device by its number takes torch 3 us more)
-    if device is None:
-        device = _devices[dev] = torch.device("cuda", dev)
-    if stream is None:
-        return torch.empty(n, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(n, dtype=dtype, device=device)
+        return _new_empty(n, dtype=dtype, device=_devices[dev])
 
 
 def _workspace(n, dev, stream):
-    import torch
-
-    return _empty(n, torch.uint8, dev, stream)
+    return _empty(n, _U8, dev, stream)
 
 
-_devices = {}  # by number
 _sizes = {}  # workspace bytes by call shape
 _MAX32 = 2 ** 31 - 1
 
@@ -943,7 +956,7 @@ class KV8Cache:
         import torch
 
         i32, dev = torch.int32, self._dev
-        if torch.cuda.current_device() != dev:
+        if _current_device() != dev:
             raise ValueError(f"{who}: the cache is on another device than the current one")
         ts, n_slots = table.shape, self.n_slots
         if table.dtype != i32 or len(ts) != 2 or ts[0] != n_slots or ts[1] > _MAX32 or not table.is_contiguous():
@@ -1108,9 +1121,7 @@ class Rotary:
         return out, RotaryHeadsC(t.data_ptr(), out.data_ptr(), d[0], d[1], out_row, out_head, heads)
 
     def _ints(self, name, t):
-        import torch
-
-        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
+        if t.dtype != _I32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
             raise ValueError(f"Rotary: {name} must be contiguous int32 on the handle's device")
         return t.data_ptr(), t.shape[0]
 
@@ -1169,23 +1180,19 @@ _NORMS = {None: 0, "rms": 1, "layer": 2}
 
 
 def _norm_arg(what, kind, weight, bias, d, eps, dev):
-    import torch
-
     if kind is None:
         if weight is not None or bias is not None:
             raise ValueError(f"residual_norm: {what} is None, but has a weight or a bias")
         return None
-    w = b = None
-    f32 = torch.float32
-    if weight is not None:
-        if weight.dtype != f32 or weight.shape != (d,) or not weight.is_contiguous() or weight.get_device() != dev:
-            raise ValueError(f"residual_norm: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
-        w = weight.data_ptr()
-    if bias is not None:
-        if bias.dtype != f32 or bias.shape != (d,) or not bias.is_contiguous() or bias.get_device() != dev:
-            raise ValueError(f"residual_norm: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
-        b = bias.data_ptr()
+    w = None if weight is None else _vector(what, weight, d, dev)
+    b = None if bias is None else _vector(what, bias, d, dev)
     return NormC(_NORMS[kind], eps, w, b)
+
+
+def _vector(what, t, d, dev):
+    if t.dtype != _F32 or t.shape != (d,) or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"residual_norm: weights and biases of {what} must be contiguous float32 [{d}] on x's device")
+    return t.data_ptr()
 
 
 def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None, post: Optional[str] = None,
@@ -1204,13 +1211,19 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
     if norm not in _NORMS or post not in _NORMS:
         raise ValueError(f"{who}: norms are 'rms', 'layer' or None")
     n, d = shape
-    x_code = _dtype_code(x)
-    code, dtype = (x_code, x.dtype) if y is None else (_dtype_code(y), y.dtype)
+    x_code = code = _dtype_code(x)
+    x_type = dtype = x.dtype
+    if y is not None:
+        dtype = y.dtype
+        if dtype != x_type:
+            code = _dtype_code(y)
     if code < 0 or (x_code != code and x_code != 0):
         raise ValueError(f"{who}: y must be float32, bfloat16 or float16 and x of the same type or float32")
     dev = _on_current(who, "x", x)
     xr = _row_stride(who, "x", x, shape)
-    yp, yr, gp, gr = None, 0, None, 0
+    yp = gp = rp = hp = None
+    yr = gr = rr = hr = 0
+    h, r = (None, None) if out is None else out
     if y is not None:
         if y.shape != shape or y.get_device() != dev:
             raise ValueError(f"{who}: y must be {list(shape)} on x's device")
@@ -1228,10 +1241,6 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
         raise ValueError(f"{who}: without y there is a norm, and no gate or post")
     pn = _norm_arg("norm", norm, weight, bias, d, eps, dev)
     pp = _norm_arg("post", post, post_weight, post_bias, d, eps, dev)
-    h = r = None
-    if out is not None:
-        h, r = out
-    hp, hr, rp, rr = None, 0, None, 0
     if norm is not None:
         if h is None:
             h, hr = _empty(shape, dtype, dev, stream), d
@@ -1244,10 +1253,10 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
         r = x
     else:
         if r is None:
-            r, rr = _empty(shape, x.dtype, dev, stream), d
+            r, rr = _empty(shape, x_type, dev, stream), d
         else:
-            if r.shape != shape or r.dtype != x.dtype or r.get_device() != dev:
-                raise ValueError(f"{who}: out's r must be {x.dtype} {list(shape)} on x's device")
+            if r.shape != shape or r.dtype != x_type or r.get_device() != dev:
+                raise ValueError(f"{who}: out's r must be {x_type} {list(shape)} on x's device")
             rr = _row_stride(who, "out's r", r, shape)
         rp = r.data_ptr()
     st = lib().tsd_residual_norm(n, d, x.data_ptr(), x_code, xr, yp, code, yr, pp, gp, gr, scale, pn, rp, rr, hp, hr,
@@ -1290,9 +1299,7 @@ class CrossStates:
         self._flat = k.stride(1) < dim or v.stride(1) < dim  # frames overlap
 
     def _ints(self, name, size, t):
-        import torch
-
-        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
+        if t.dtype != _I32 or t.dim() != 1 or not t.is_contiguous() or t.get_device() != self._dev:
             raise ValueError(f"CrossStates.attend: {name} must be contiguous int32 [{size}] on the states' device")
         return t.shape[0], t.data_ptr()
 
