@@ -36,6 +36,7 @@ namespace cg = cooperative_groups;
 constexpr int kWarps = 4;
 constexpr int kTile = 16;  // frames per step of a warp
 constexpr int kRows = 16;  // rows per CTA
+constexpr int kMaxSplits = 8;
 
 template <int DIM>
 struct RowsShape {
@@ -45,7 +46,7 @@ struct RowsShape {
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kOutStride = DIM + 4;
   static constexpr int kOut = kWarps * kRows * kOutStride * 4;
-  static constexpr int kMl = kRing > kOut ? kRing : kOut;  // [warps + 1][rows] (maximum, sum), then [rows] weights
+  static constexpr int kMl = kRing > kOut ? kRing : kOut;  // [warps + 1][rows] (maximum, sum): the warps', the CTA's
   static constexpr int kSmem = kMl + (kWarps + 1) * kRows * 8;
 };
 
@@ -72,7 +73,7 @@ __device__ __forceinline__ void copy_wait() {
 }
 
 template <bool BF16, int DIM>
-__global__ void __launch_bounds__(32 * kWarps) k_cross_rows(const __grid_constant__ CrossAttend a) {
+__global__ void __launch_bounds__(32 * kWarps, DIM == 128 ? 2 : 3) k_cross_rows(const __grid_constant__ CrossAttend a) {
   using S = RowsShape<DIM>;
   constexpr int ST = S::kStages, kChunks = DIM / 8;  // 16-byte chunks of a frame
   constexpr int kSteps = DIM / 16, kCols = DIM / 8;
@@ -230,46 +231,68 @@ __global__ void __launch_bounds__(32 * kWarps) k_cross_rows(const __grid_constan
             *reinterpret_cast<float4*>(dst + 4) = make_float4(o[8 * u + 4][2 * h + e], o[8 * u + 5][2 * h + e], o[8 * u + 6][2 * h + e], o[8 * u + 7][2 * h + e]);
           }
     }
-    // A row's parts are joined by the CTA of the cluster that takes its dimensions: each CTA reads
-    // all CTAs' warps.
-    if (splits > 1) cluster.sync();
-    else __syncthreads();
-    const int vecs = kRows * (DIM / 4);
+    // The warps' shares are joined in place of the first's, then (splits) the CTAs' by the CTA of the cluster that takes the row's
+    // dimensions, all of them read at once.
+    __syncthreads();
+    const int vecs = min(kRows, rows - r0) * (DIM / 4);
+    const bool seen = q.ok && q.len > 0;
+    struct Share {
+      float top, sum;
+      float4 acc;
+      __device__ __forceinline__ void add(float2 ml, float4 v) {  // (top is known; -inf: every score is, and 0 / 0 is the result)
+        const float f = ml.x == top ? 1.f : ex2_approx(ml.x - top);
+        sum = fmaf(f, ml.y, sum);
+        acc.x = fmaf(f, v.x, acc.x), acc.y = fmaf(f, v.y, acc.y), acc.z = fmaf(f, v.z, acc.z), acc.w = fmaf(f, v.w, acc.w);
+      }
+    };
+    const auto own = [&](int rr, int col) {
+      Share x{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) x.top = fmaxf(x.top, s_ml[w * kRows + rr].x);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) x.add(s_ml[w * kRows + rr], *reinterpret_cast<const float4*>(s_out + (w * kRows + rr) * S::kOutStride + col));
+      return x;
+    };
+    if (splits > 1) {
+      if (seen)
+        for (int i = threadIdx.x; i < vecs; i += 32 * kWarps) {
+          const int rr = i / (DIM / 4), col = 4 * (i % (DIM / 4));
+          const Share x = own(rr, col);
+          *reinterpret_cast<float4*>(s_out + rr * S::kOutStride + col) = x.acc;
+          if (col == 0) s_ml[kWarps * kRows + rr] = make_float2(x.top, x.sum);
+        }
+      cluster.sync();
+    }
     for (int i = split * 32 * kWarps + threadIdx.x; i < vecs; i += splits * 32 * kWarps) {
       const int rr = i / (DIM / 4), col = 4 * (i % (DIM / 4)), r = r0 + rr;
-      if (r >= rows) continue;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      float sum = 0.f;
-      if (q.ok && q.len > 0) {
-        float top = -INFINITY;
-        bool any = false;
-        for (int k = 0; k < splits; ++k) {
-          const float2* ml = splits > 1 ? cluster.map_shared_rank(s_ml, k) : s_ml;
+      Share x{0.f, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      if (!q.ok) {
+        x.sum = __uint_as_float(0x7fc00000u);
+      } else if (!seen) {
+        x.sum = 1.f;
+      } else if (splits == 1) {
+        x = own(rr, col);
+      } else {
+        float2 ml[kMaxSplits];
+        float4 v[kMaxSplits];
 #pragma unroll
-          for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml[w * kRows + rr].x);
-        }
-        for (int k = 0; k < splits; ++k) {
-          const float2* ml = splits > 1 ? cluster.map_shared_rank(s_ml, k) : s_ml;
-          const float* src = splits > 1 ? cluster.map_shared_rank(s_out, k) : s_out;
-#pragma unroll
-          for (int w = 0; w < kWarps; ++w) {
-            const float2 x = ml[w * kRows + rr];
-            if (x.x == -INFINITY && x.y == 0.f) continue;  // no frames
-            any = true;
-            const float f = x.x == -INFINITY ? 1.f : ex2_approx(x.x - top);
-            const float4 v = *reinterpret_cast<const float4*>(src + (w * kRows + rr) * S::kOutStride + col);
-            sum = fmaf(f, x.y, sum);
-            acc.x = fmaf(f, v.x, acc.x), acc.y = fmaf(f, v.y, acc.y), acc.z = fmaf(f, v.z, acc.z), acc.w = fmaf(f, v.w, acc.w);
+        for (int k = 0; k < kMaxSplits; ++k)
+          if (k < splits) {
+            ml[k] = cluster.map_shared_rank(s_ml, k)[kWarps * kRows + rr];
+            v[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(s_out, k) + rr * S::kOutStride + col);
           }
-        }
-        const float inv = any ? 1.f / sum : __uint_as_float(0x7fc00000u);
-        acc.x *= inv, acc.y *= inv, acc.z *= inv, acc.w *= inv;
-      } else if (!q.ok) {
-        acc.x = acc.y = acc.z = acc.w = __uint_as_float(0x7fc00000u);
+        x.top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kMaxSplits; ++k)
+          if (k < splits) x.top = fmaxf(x.top, ml[k].x);
+#pragma unroll
+        for (int k = 0; k < kMaxSplits; ++k)
+          if (k < splits) x.add(ml[k], v[k]);
       }
+      const float inv = 1.f / x.sum;
       const int tok = q.row0 + r / a.group, hd = head * a.group + r % a.group;
       *reinterpret_cast<uint2*>(a.out + (int64_t)tok * a.out_row + (int64_t)hd * a.out_head + col) =
-          make_uint2(narrow2<BF16>(acc.x, acc.y), narrow2<BF16>(acc.z, acc.w));
+          make_uint2(narrow2<BF16>(x.acc.x * inv, x.acc.y * inv), narrow2<BF16>(x.acc.z * inv, x.acc.w * inv));
     }
     if (splits > 1) cluster.sync();  // the others have read this CTA's shares
     else __syncthreads();
@@ -301,9 +324,10 @@ CrossRowsPlan cross_rows_plan(const tsd_states& s, const tsd_cross_batch& b, int
   const int group = heads / s.kv_heads;
   const int64_t most = std::max<int64_t>(1, b.max_rows ? std::min(b.max_rows, b.rows) : !b.starts ? 1 : ((int64_t)b.rows + b.n - 1) / b.n);
   p.mtiles = (int)std::min<int64_t>((most * group + kRows - 1) / kRows, 65535);
-  // few row tiles: a source's frames over up to eight CTAs, a step for each warp at least
+  // Few row tiles: a source's frames over up to eight CTAs, two steps for each warp at least (one row, 8 key heads, dim 64, us: over 375
+  // frames 5.2 with two steps or more, over 750 5.6 with two, 6.4 with four, over 3000 6.7 and 8.7 with six).
   const int64_t units = (int64_t)b.n * s.kv_heads * p.mtiles, slots = (s.dim == 128 ? 2 : 3) * (int64_t)sms;
-  while (p.splits < 8 && units * p.splits * 2 <= slots && (int64_t)p.splits * 2 * kWarps * kTile <= s.frames) p.splits *= 2;
+  while (p.splits < kMaxSplits && units * p.splits * 2 <= slots && (int64_t)p.splits * 2 * kWarps * kTile * 2 <= s.frames) p.splits *= 2;
   return p;
 }
 
