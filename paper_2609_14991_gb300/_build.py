@@ -25,7 +25,7 @@ CHECKS_LIB_PATH = os.path.join(PKG, "libtsd_checks.so")
 
 SOURCES = ["tables.cpp", "arpa.cpp", "decoder.cu", "row_pass.cu", "row_fused.cu", "row_stream.cu", "chunk_cluster.cu", "joint_simt.cu", "joint_tc.cu", "joint_greedy.cu", "noalloc.cu", "row_beam.cu", "row_pruned.cu", "gemm_tc.cu", "encoder.cu", "encoder_gemm.cu",
            "scores.cu", "joint_scores.cu", "kv8.cu", "kv8_attend.cu", "kv8_rows.cu", "kv8_tiles.cu",
-           "rotary.cu", "norm.cu", "norm_f32.cu", "norm_bf16.cu", "norm_f16.cu", "cross.cu", "cross_rows.cu", "cross_tiles.cu"]
+           "rotary.cu", "norm.cu", "norm_f32.cu", "norm_bf16.cu", "norm_f16.cu", "norm_f32_bf16.cu", "norm_f32_f16.cu", "cross.cu", "cross_rows.cu", "cross_tiles.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

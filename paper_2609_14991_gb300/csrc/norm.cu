@@ -75,13 +75,19 @@ extern "C" tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int
   a.base = off(a.x, x_size);
   a.stride = (int)(x_row % 8);
   const auto alike = [&](const void* p, int64_t row, int bytes) { return !p || (off(p, bytes) == a.base && (n == 1 || row % 8 == a.stride)); };
-  const bool even = alike(a.y, a.y_row, size) && alike(a.r, a.r_row, x_size) && alike(a.h, a.h_row, size) && (!a.gate_row || alike(a.gate, a.gate_row, size)) &&
-                    d + (a.base || a.stride ? 7 : 0) <= kMaxWidth;
+  const bool even = alike(a.y, a.y_row, size) && alike(a.r, a.r_row, x_size) && alike(a.h, a.h_row, size) && (!a.gate_row || alike(a.gate, a.gate_row, size));
+  const auto aligned = [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; };
+  NormHow how = NormHow::kApart;
+  if (even && a.base == 0 && (n == 1 || a.stride == 0) && d % 8 == 0 && aligned(a.post.weight) && aligned(a.post.bias) && aligned(a.norm.weight) &&
+      aligned(a.norm.bias) && aligned(a.gate))
+    how = NormHow::kWhole;
+  else if (even && d + 7 <= kMaxWidth)
+    how = NormHow::kShifted;
   int sms = 0;
   TSD_CUDA(device_sms(&sms));
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  if (dtype == TSD_F32) TSD_CUDA((norm_launch<TSD_F32, TSD_F32>(a, even, sms, s)));
-  else if (dtype == TSD_BF16) TSD_CUDA((x_dtype == TSD_F32 ? norm_launch<TSD_F32, TSD_BF16>(a, even, sms, s) : norm_launch<TSD_BF16, TSD_BF16>(a, even, sms, s)));
-  else TSD_CUDA((x_dtype == TSD_F32 ? norm_launch<TSD_F32, TSD_F16>(a, even, sms, s) : norm_launch<TSD_F16, TSD_F16>(a, even, sms, s)));
+  if (dtype == TSD_F32) TSD_CUDA((norm_launch<TSD_F32, TSD_F32>(a, how, sms, s)));
+  else if (dtype == TSD_BF16) TSD_CUDA((x_dtype == TSD_F32 ? norm_launch<TSD_F32, TSD_BF16>(a, how, sms, s) : norm_launch<TSD_BF16, TSD_BF16>(a, how, sms, s)));
+  else TSD_CUDA((x_dtype == TSD_F32 ? norm_launch<TSD_F32, TSD_F16>(a, how, sms, s) : norm_launch<TSD_F16, TSD_F16>(a, how, sms, s)));
   return TSD_OK;
 }

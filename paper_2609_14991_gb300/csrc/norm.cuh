@@ -46,29 +46,61 @@ __device__ __forceinline__ float row_sum(float v, float (*s_part)[32], int& turn
   return v;
 }
 
-// A thread's elements of a row.  EVEN: groups of eight that begin at a multiple of eight elements in memory, the row's
-// first one `shift` elements into its first group; else every THREADS-th element.
-template <int THREADS, int CHUNKS, bool EVEN>
+// A thread's elements of a row: groups of eight, THREADS of them apart, or (apart) every THREADS-th element.
+template <int THREADS, int CHUNKS, NormHow HOW>
 struct Places {
-  static constexpr int N = 8 * CHUNKS;
+  static constexpr bool EVEN = HOW != NormHow::kApart;
   int t, d, shift;
-  __device__ __forceinline__ int first(int c) const { return (c * THREADS + t) * 8 - shift; }  // EVEN: a group's first element
+  __device__ __forceinline__ int first(int c) const { return (c * THREADS + t) * 8 - (HOW == NormHow::kShifted ? shift : 0); }  // a group's first element
   __device__ __forceinline__ int at(int i) const { return EVEN ? first(i / 8) + i % 8 : i * THREADS + t; }
-  __device__ __forceinline__ bool whole(int c) const { return first(c) >= 0 && first(c) + 8 <= d; }
   __device__ __forceinline__ bool some(int c) const { return first(c) < d; }  // (the first group always has some)
-  __device__ __forceinline__ bool has(int i) const { return (unsigned)at(i) < (unsigned)d; }
+  __device__ __forceinline__ bool whole(int c) const { return HOW == NormHow::kWhole ? some(c) : first(c) >= 0 && first(c) + 8 <= d; }
+  __device__ __forceinline__ bool has(int i) const { return HOW == NormHow::kWhole ? some(i / 8) : (unsigned)at(i) < (unsigned)d; }
 
   // Eight elements (group c's), as pairs, of an array that stands anywhere; 0 past the row
   template <int DT>
   __device__ __forceinline__ void load(const void* base, int c, uint64_t* v) const {
     const typename Elem<DT>::Raw* p = static_cast<const typename Elem<DT>::Raw*>(base);
     float x[8];
-    if (EVEN && shift == 0 && d % 8 == 0 && reinterpret_cast<uintptr_t>(base) % 16 == 0) {
+    if (HOW == NormHow::kWhole) {
       Eight<DT> y;
 #pragma unroll
       for (int i = 0; i < Eight<DT>::kWords; ++i) y.w[i] = 0;
       if (some(c)) y.load(p + first(c));
       y.get(x);
+    } else if (EVEN && reinterpret_cast<uintptr_t>(base) % 16 == 0) {
+      // 16 bytes at a time: the group lies in them from element `over` on, alike for all groups of the row
+      constexpr int kPer = DT == TSD_F32 ? 4 : 8, kPieces = 8 / kPer + 1;
+      const int over = -shift & (kPer - 1), begin = first(c) - over;
+      uint32_t w[4 * kPieces];
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u) {
+        const int e = begin + u * kPer;
+        uint4 y = make_uint4(0, 0, 0, 0);
+        if (e >= 0 && e < d && (u + 1 < kPieces || over)) y = __ldg(reinterpret_cast<const uint4*>(p + e));
+        w[4 * u] = y.x, w[4 * u + 1] = y.y, w[4 * u + 2] = y.z, w[4 * u + 3] = y.w;
+      }
+      if constexpr (DT == TSD_F32) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (over == m)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[m + i]);
+      } else {
+        uint32_t y[5] = {0, 0, 0, 0, 0}, z[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (over / 2 == m)
+#pragma unroll
+            for (int i = 0; i < 5; ++i) y[i] = m + i < 8 ? w[m + i] : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] = over & 1 ? __funnelshift_r(y[i], y[i + 1], 16) : y[i];
+        Elem<DT>::wide4(z, x);
+      }
+      if (!whole(c))
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (!has(8 * c + i)) x[i] = 0.f;
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = has(8 * c + i) ? Elem<DT>::wide(p[at(8 * c + i)]) : 0.f;
@@ -86,7 +118,7 @@ struct Places {
       Eight<DT> y;
       y.put(x);
       y.store_even(p + first(c));
-    } else if (!EVEN || some(c)) {
+    } else if (HOW != NormHow::kWhole && (!EVEN || some(c))) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (has(8 * c + j)) p[at(8 * c + j)] = Elem<DT>::narrow(x[j]);
@@ -112,8 +144,8 @@ __device__ __forceinline__ float both(uint64_t v) {
 
 // The first half of a norm: v <- v or (layer) its deviations from the mean, and the factor 1 / sqrt(mean square + eps);
 // elements past the row are 0 and stay out of the sums.
-template <int THREADS, int CHUNKS, bool EVEN>
-__device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, uint64_t* v, float (*s_part)[32], int& turn) {
+template <int THREADS, int CHUNKS, NormHow HOW>
+__device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, HOW>& pl, uint64_t* v, float (*s_part)[32], int& turn) {
   constexpr int N = 4 * CHUNKS;
   if (k.kind == TSD_NORM_LAYER) {
     uint64_t s = v[0];
@@ -132,8 +164,8 @@ __device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THRE
   return 1.f / sqrtf(row_sum<THREADS>(both(s), s_part, turn) / pl.d + k.eps);
 }
 // The second, for group c, but for that factor: v <- v * weight
-template <int THREADS, int CHUNKS, bool EVEN>
-__device__ __forceinline__ void weighed(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, uint64_t* v) {
+template <int THREADS, int CHUNKS, NormHow HOW>
+__device__ __forceinline__ void weighed(const tsd_norm& k, const Places<THREADS, CHUNKS, HOW>& pl, int c, uint64_t* v) {
   if (!k.weight) return;
   uint64_t w[4];
   pl.template load<TSD_F32>(k.weight, c, w);
@@ -141,8 +173,8 @@ __device__ __forceinline__ void weighed(const tsd_norm& k, const Places<THREADS,
   for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], w[i]);
 }
 // ... and v <- v * factor + bias
-template <int THREADS, int CHUNKS, bool EVEN>
-__device__ __forceinline__ void scaled(const tsd_norm& k, const Places<THREADS, CHUNKS, EVEN>& pl, int c, uint64_t factor, uint64_t* v) {
+template <int THREADS, int CHUNKS, NormHow HOW>
+__device__ __forceinline__ void scaled(const tsd_norm& k, const Places<THREADS, CHUNKS, HOW>& pl, int c, uint64_t factor, uint64_t* v) {
   if (k.bias) {
     uint64_t b[4];
     pl.template load<TSD_F32>(k.bias, c, b);
@@ -195,28 +227,29 @@ struct Staged {
 constexpr int cta_threads(int per_row) { return per_row <= 32 ? 128 : per_row; }
 constexpr int ctas_per_sm(int per_row, int chunks) { return (chunks == 1 ? 1024 : per_row < 512 ? 768 : per_row) / cta_threads(per_row); }
 
-// A CTA goes from row to row.  EVEN: the next rows are on their way to shared memory, each warp's elements to its own
+// A CTA goes from row to row.  Where they stand in groups of eight the next rows are on their way to shared memory, each warp's elements to its own
 // place, so no barrier guards them.
-template <int XT, int YT, int THREADS, int CHUNKS, bool EVEN>
+template <int XT, int YT, int THREADS, int CHUNKS, NormHow HOW>
 __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHUNKS)) k_residual_norm(const __grid_constant__ NormArgs a) {
   constexpr int kRows = cta_threads(THREADS) / THREADS;
+  constexpr bool EVEN = HOW != NormHow::kApart;
   static_assert(kRows == 1 || THREADS <= 32, "several rows per CTA: a warp's lanes each, or part of them");
   using X = Staged<XT, THREADS, CHUNKS>;
   using Y = Staged<YT, THREADS, CHUNKS>;
   extern __shared__ __align__(16) unsigned char s_ring[];
   __shared__ float s_part[2][32];
   int turn = 0;
-  Places<THREADS, CHUNKS, EVEN> pl{(int)threadIdx.x % THREADS, a.d, 0};
+  Places<THREADS, CHUNKS, HOW> pl{(int)threadIdx.x % THREADS, a.d, 0};
   const int64_t step = (int64_t)gridDim.x * kRows;
   constexpr int kOfWarp = THREADS < 32 ? 32 / THREADS : 1;  // a warp's rows go together
   const int sub = threadIdx.x / THREADS % kOfWarp;
   int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / THREADS;
   unsigned char* ring = s_ring + threadIdx.x / THREADS * a.depth * a.slot;
-  const auto shift_of = [&](int64_t r) { return EVEN ? (int)((a.base + r * a.stride) & 7) : 0; };
+  const auto shift_of = [&](int64_t r) { return HOW == NormHow::kShifted ? (int)((a.base + r * a.stride) & 7) : 0; };
   const auto fetch = [&](int slot, int64_t r) {
     if constexpr (EVEN) {
       if (r < a.n) {
-        const Places<THREADS, CHUNKS, true> at{pl.t, a.d, shift_of(r)};
+        const Places<THREADS, CHUNKS, HOW> at{pl.t, a.d, shift_of(r)};
         unsigned char* to = ring + slot * a.slot;
         X::begin(to, a.x, r * a.x_row, at);
         if (a.y) Y::begin(to + X::kBytes, a.y, r * a.y_row, at);
@@ -303,8 +336,9 @@ __global__ void __launch_bounds__(cta_threads(THREADS), ctas_per_sm(THREADS, CHU
   }
 }
 
-template <int XT, int YT, bool EVEN>
+template <int XT, int YT, NormHow HOW>
 cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
+  constexpr bool EVEN = HOW != NormHow::kApart;
   const auto go = [&](auto threads, auto chunks) {
     constexpr int T = decltype(threads)::value, C = decltype(chunks)::value;
     constexpr int kRows = cta_threads(T) / T;
@@ -313,18 +347,18 @@ cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
       a.slot = Staged<XT, T, C>::kBytes + ((a.y ? 1 : 0) + (a.gate && a.gate_row ? 1 : 0)) * Staged<YT, T, C>::kBytes;
       a.depth = std::min(std::max(kRingBytes / (per_sm * kRows * a.slot), 1), 4);
       per_sm = std::max(1, std::min(per_sm, kMaxSmem / (a.depth * kRows * a.slot)));
-      const cudaError_t e = smem_opt_in<k_residual_norm<XT, YT, T, C, EVEN>>(kMaxSmem);
+      const cudaError_t e = smem_opt_in<k_residual_norm<XT, YT, T, C, HOW>>(kMaxSmem);
       if (e != cudaSuccess) return e;
     }
     // Many rows: two per CTA and as many CTAs as that takes, which reads and writes memory more evenly than CTAs that stay (16384 x
     // 2048: 43 us, 47), but for one or two wide ones per SM (4000 x 12000 with norms on both sides: 173 us, 155).
     const int groups = (a.n + kRows - 1) / kRows, stay = sms * per_sm;
     const int ctas = per_sm > 2 && groups > 2 * stay ? (groups + 1) / 2 : std::min(groups, stay);
-    k_residual_norm<XT, YT, T, C, EVEN><<<(unsigned)ctas, cta_threads(T), (size_t)a.depth * kRows * a.slot, s>>>(a);
+    k_residual_norm<XT, YT, T, C, HOW><<<(unsigned)ctas, cta_threads(T), (size_t)a.depth * kRows * a.slot, s>>>(a);
     return cudaGetLastError();
   };
   using std::integral_constant;
-  const int d = a.d + (EVEN && (a.base || a.stride) ? 7 : 0);  // (with the elements that a row's first group may begin before it)
+  const int d = a.d + (HOW == NormHow::kShifted ? 7 : 0);  // (with the elements that a row's first group may begin before it)
   // Up to 32 elements per thread: what each thread does besides (the sums' joins, the root) then weighs little.  Few rows:
   // as many threads as a row has groups.  200 x 777 with norms on both sides: 4.0 us, with 32 threads per row 7.8.
   if constexpr (EVEN)
@@ -349,8 +383,8 @@ cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
 }  // namespace
 
 template <int XT, int YT>
-cudaError_t norm_launch(const NormArgs& a, bool even, int sms, cudaStream_t s) {
-  return even ? launch<XT, YT, true>(a, sms, s) : launch<XT, YT, false>(a, sms, s);
+cudaError_t norm_launch(const NormArgs& a, NormHow how, int sms, cudaStream_t s) {
+  return how == NormHow::kWhole ? launch<XT, YT, NormHow::kWhole>(a, sms, s) : how == NormHow::kShifted ? launch<XT, YT, NormHow::kShifted>(a, sms, s) : launch<XT, YT, NormHow::kApart>(a, sms, s);
 }
 
 }  // namespace tsd

@@ -3,7 +3,6 @@
 
 namespace tsd {
 
-template cudaError_t norm_launch<TSD_F16, TSD_F16>(const NormArgs&, bool, int, cudaStream_t);
-template cudaError_t norm_launch<TSD_F32, TSD_F16>(const NormArgs&, bool, int, cudaStream_t);
+template cudaError_t norm_launch<TSD_F16, TSD_F16>(const NormArgs&, NormHow, int, cudaStream_t);
 
 }  // namespace tsd

@@ -3,6 +3,6 @@
 
 namespace tsd {
 
-template cudaError_t norm_launch<TSD_F32, TSD_F32>(const NormArgs&, bool, int, cudaStream_t);
+template cudaError_t norm_launch<TSD_F32, TSD_F32>(const NormArgs&, NormHow, int, cudaStream_t);
 
 }  // namespace tsd
