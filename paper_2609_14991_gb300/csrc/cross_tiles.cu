@@ -23,6 +23,12 @@
 // cost, and each CTA takes an equal share of that line, so ragged sequences and few
 // long ones fill the device alike.  A unit that several CTAs share leaves its parts in the workspace, which a
 // second kernel joins in their order.
+//
+// A step of two row tiles and 128 frames takes 1.40 us at dim 128 (0.96 of the library's product rate): the products' 2048 clocks and
+// shared memory's as many (operands 1536, copies 512) do not overlap wholly.  Dim 64: 1.36 us, the softmax's 1850 clocks
+// for a row tile and what its products leave between.  6 ragged texts of up to 1100 tokens, 16 heads, over up to 9000 frames,
+// 4 key heads of 128: 150 us, 1.40 PFLOP/s.  What a unit takes besides its tiles, 2.2 us: first maximum, last products,
+// results (64 KB at 64 bytes per clock, 128 where it is shared).
 #include <algorithm>
 #include <type_traits>
 

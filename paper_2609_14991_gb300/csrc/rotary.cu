@@ -6,9 +6,11 @@
 // fp32 p f_i is off by 0.06 rad at p = 10^6).  What is left of an eighth of a turn
 // goes through sincospif in fp32, its quarter turns are swaps and signs.
 //
-// Reads and writes each element once: bound by memory.  A CTA takes a few rows: one
+// Reads and writes each element once: bound by memory, and by the instructions of half-words.  A CTA takes a few rows: one
 // sine and cosine per row and pair, kept in shared memory for all query and key
-// heads, which follow 16 bytes (of each half) at a time.
+// heads, which follow 16 bytes (of each half) at a time.  16500 rows of 18 heads (128 wide, bf16, half layout): 28 us, 0.80 of the
+// copy rate; CTAs of 256 threads and twice the rows 31, of 64 and half 35; half of the head turned, interleaved, fp16: 29.  Parts of a
+// head that 16 bytes do not divide go through shared memory: 26 of 80, 16500 rows: 26 us, 0.54.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
