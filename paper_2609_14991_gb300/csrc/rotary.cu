@@ -10,7 +10,7 @@
 // sine and cosine per row and pair, kept in shared memory for all query and key
 // heads, which follow 16 bytes (of each half) at a time.  16500 rows of 18 heads (128 wide, bf16, half layout): 28 us, 0.80 of the
 // copy rate; CTAs of 256 threads and twice the rows 31, of 64 and half 35; half of the head turned, interleaved, fp16: 29.  Parts of a
-// head that 16 bytes do not divide go through shared memory: 26 of 80, 16500 rows: 26 us, 0.54.
+// head that 16 bytes do not divide go through shared memory: 26 of 80, 16500 rows: 24 us, 0.59.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -26,7 +26,7 @@ namespace {
 
 constexpr int kDirect = 128, kThreads = 256;  // of a CTA: 16 bytes at a time straight through, staged
 constexpr int kMaxRows = 8;        // rows of a CTA
-constexpr int kMaxAngles = 2048;   // ... and their angles
+constexpr int kMaxAngles = 512;    // ... and their angles
 constexpr int kStaged = 24 * 1024; // bytes of heads that a CTA stages
 
 struct HeadRows {
