@@ -837,7 +837,8 @@ TSD_API tsd_status tsd_cross_attend_workspace(const tsd_states* states, const ts
 /*   out[row][h] = sum_j p_j v_j,  p = softmax_j(scale * q[row][h] . k_j)  over its source's frames j.
  * heads: query heads, a multiple of kv_heads, at most 64 per kv head and 1024; query head h reads kv head
  * h / (heads / kv_heads).  q and out: row and head strides in elements, a multiple of 8, 16-byte aligned; out
- * may not overlap the inputs.  Products take the states' type and accumulate in fp32, as do the softmax's statistics. */
+ * may not overlap the inputs.  Products take the states' type and accumulate in fp32, as do the softmax's statistics; what is rounded is
+ * a weight of the values' product: to 16 bits, with many rows per kv head to the states' type. */
 TSD_API tsd_status tsd_cross_attend(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads, const void* q,
                                     int64_t q_row, int64_t q_head, float scale, void* out, int64_t out_row, int64_t out_head,
                                     void* workspace, int64_t workspace_bytes, void* cuda_stream);

@@ -233,10 +233,32 @@ def test_layouts(rows, dim):
         orders.append(tuple(t.permute(order).contiguous().permute(back) for t in (a, b)))
     orders.append(tuple(t[:, :, :1].expand(n, frames, kv, dim) for t in (a, b)))
     orders.append(tuple(t[:1].expand(n, frames, kv, dim) for t in (a, b)))
+    orders.append(tuple(t[:, :1].expand(n, frames, kv, dim) for t in (a, b)))
     for k, v in orders:
         out = torch.empty(2, n * rows, dim, dtype=BF, device="cuda").transpose(0, 1)
         tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=rows, out=out)
         check(out, k, v, lens, q, counts)
+
+
+@pytest.mark.parametrize("rows", [2, 2100])
+def test_queries_that_share_memory(rows):
+    """One row for all tokens, one head for all heads; odd distances of heads and rows."""
+    n, lens = 3, [150, 20, 99]
+    k, v = make(n, 150, 2, 64, seed=14)
+    s, at = tsd.CrossStates(k, v, ints(lens)), starts_of([rows] * n)
+    buf = queries(n * rows, 5, 72)
+    for q in (queries(1, 4, 64).expand(n * rows, 4, 64), queries(n * rows, 1, 64).expand(n * rows, 4, 64), buf[:, 1:, 8:]):
+        check(s.attend(q, starts=at, max_rows=rows), k, v, lens, q, [rows] * n)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_wide_groups_of_single_rows(dtype):
+    """A token per sequence whose group alone is many rows, without starts."""
+    n, lens = 64, [(i * 53) % 301 for i in range(64)]
+    for_many_rows(n, 4, 64, 300, 64)
+    k, v = make(n, 300, 4, 64, dtype, seed=15, poison=math.nan, lens=lens)
+    q = queries(n, 256, 64, dtype)
+    check(tsd.CrossStates(k, v, ints(lens)).attend(q), k, v, lens, q, [1] * n)
 
 
 @pytest.mark.parametrize("rows", [1, 4000])
