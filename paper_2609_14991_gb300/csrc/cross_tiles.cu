@@ -25,8 +25,8 @@
 // second kernel joins in their order.
 //
 // A step of two row tiles and 128 frames takes 1.40 us at dim 128 (0.96 of the library's product rate): the products' 2048 clocks and
-// shared memory's as many (operands 1536, copies 512) do not overlap wholly.  Dim 64: 1.36 us, the softmax's 1850 clocks
-// for a row tile and what its products leave between.  6 ragged texts of up to 1100 tokens, 16 heads, over up to 9000 frames,
+// shared memory's as many (operands 1536, copies 512) do not overlap wholly.  Dim 64: 1.36 us, a values' product whose
+// weights come from TMEM takes 65 clocks at any width, and the softmax 1300 a row tile.  6 ragged texts of up to 1100 tokens, 16 heads, over up to 9000 frames,
 // 4 key heads of 128: 150 us, 1.40 PFLOP/s.  What a unit takes besides its tiles, 2.2 us: first maximum, last products,
 // results (64 KB at 64 bytes per clock, 128 where it is shared).
 #include <algorithm>

@@ -1,4 +1,5 @@
 """Attention over an encoder's states on the GPU against 64 bits."""
+import ctypes
 import math
 
 import pytest
@@ -400,6 +401,14 @@ def test_binding_refusals():
                      (dict(q=q, out=q[:1].expand(2, 4, 64)), "overlap")]:
         with pytest.raises(tsd.TsdError, match=word):
             s.attend(**kw)
+    big = tsd.CrossStates(*make(4, 700, 4, 64))
+    x = queries(2800, 4, 64)
+    batch, need = tsd.CrossBatchC(4, None, starts_of([700] * 4).data_ptr(), 2800, 700), ctypes.c_int64()
+    for_many_rows(4, 4, 700, 700, 64)
+    assert tsd.lib().tsd_cross_attend_workspace(big._pc, batch, 4, ctypes.byref(need)) == 0 and need.value > 0
+    for space, size in ((None, need.value), (x.data_ptr(), need.value - 1), (x.data_ptr() + 8, need.value)):  # refused, not written
+        assert tsd.lib().tsd_cross_attend(big._pc, batch, 4, x.data_ptr(), 256, 64, 0.1, x.data_ptr(), 256, 64, space, size, None) == tsd.TSD_EINVAL
+        assert b"workspace" in tsd.lib().tsd_last_error()
     for args, word in [((k, v, i2.long()), "lens"), ((k, v, i2[:1]), "lens"), ((k, v, i2.cpu()), "one device"), ((k, v.cpu()), "one device"),
                        ((torch.cat([k, k], 3)[..., ::2], v), "adjacent"),
                        ((torch.zeros(2, 20, 2, 68, dtype=BF, device="cuda")[..., :64], v), "multiples of 8"),
