@@ -38,7 +38,7 @@ __device__ __forceinline__ CrossSeq cross_seq(const tsd_states& s, const tsd_cro
 
 // Few rows per key head (cross_rows.cu): row tiles of 16, the frames of one over a cluster.
 struct CrossRowsPlan {
-  int mtiles = 1, splits = 1;
+  int mtiles = 1, splits = 1, warps = 4;  // of a CTA
 };
 CrossRowsPlan cross_rows_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, int sms);
 cudaError_t cross_rows_launch(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s);

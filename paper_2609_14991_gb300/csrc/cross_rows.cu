@@ -37,21 +37,20 @@ namespace {
 using namespace tc;
 namespace cg = cooperative_groups;
 
-constexpr int kWarps = 4;
 constexpr int kTile = 16;  // frames per step of a warp
 constexpr int kRows = 16;  // rows per CTA
 constexpr int kMaxSplits = 8;
 
-template <int DIM>
+template <int DIM, int WARPS>
 struct RowsShape {
   static constexpr int kStages = DIM == 128 ? 3 : 4;
   static constexpr int kHalf = kTile * DIM * 2;     // a step's keys, or its values
   static constexpr int kStageBytes = 2 * kHalf;
-  static constexpr int kRing = kWarps * kStages * kStageBytes;
+  static constexpr int kRing = WARPS * kStages * kStageBytes;
   static constexpr int kOutStride = DIM + 4;
-  static constexpr int kOut = kWarps * kRows * kOutStride * 4;
+  static constexpr int kOut = WARPS * kRows * kOutStride * 4;
   static constexpr int kMl = kRing > kOut ? kRing : kOut;  // [warps + 1][rows] (maximum, sum): the warps', the CTA's
-  static constexpr int kSmem = kMl + (kWarps + 1) * kRows * 8;
+  static constexpr int kSmem = kMl + (WARPS + 1) * kRows * 8;
 };
 
 template <bool BF16>
@@ -76,9 +75,9 @@ __device__ __forceinline__ void copy_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-template <bool BF16, int DIM>
-__global__ void __launch_bounds__(32 * kWarps, DIM == 128 ? 2 : 3) k_cross_rows(const __grid_constant__ CrossAttend a) {
-  using S = RowsShape<DIM>;
+template <bool BF16, int DIM, int kWarps>
+__global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k_cross_rows(const __grid_constant__ CrossAttend a) {
+  using S = RowsShape<DIM, kWarps>;
   constexpr int ST = S::kStages, kChunks = DIM / 8;  // 16-byte chunks of a frame
   constexpr int kSteps = DIM / 16, kCols = DIM / 8;
   extern __shared__ __align__(128) unsigned char smem[];
@@ -303,10 +302,10 @@ __global__ void __launch_bounds__(32 * kWarps, DIM == 128 ? 2 : 3) k_cross_rows(
   }
 }
 
-template <bool BF16, int DIM>
+template <bool BF16, int DIM, int kWarps>
 cudaError_t launch(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s) {
-  using S = RowsShape<DIM>;
-  const cudaError_t e = smem_opt_in<k_cross_rows<BF16, DIM>>(S::kSmem);
+  using S = RowsShape<DIM, kWarps>;
+  const cudaError_t e = smem_opt_in<k_cross_rows<BF16, DIM, kWarps>>(S::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t c{};
   c.gridDim = dim3((unsigned)(a.s.kv_heads * p.mtiles * p.splits), (unsigned)a.b.n);
@@ -318,7 +317,12 @@ cudaError_t launch(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s)
   at.val.clusterDim.x = (unsigned)p.splits, at.val.clusterDim.y = 1, at.val.clusterDim.z = 1;
   c.attrs = &at;
   c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, k_cross_rows<BF16, DIM>, a);
+  return cudaLaunchKernelEx(&c, k_cross_rows<BF16, DIM, kWarps>, a);
+}
+
+template <bool BF16, int DIM>
+cudaError_t launch_warps(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s) {
+  return p.warps == 2 ? launch<BF16, DIM, 2>(a, p, s) : launch<BF16, DIM, 4>(a, p, s);
 }
 
 }  // namespace
@@ -331,13 +335,20 @@ CrossRowsPlan cross_rows_plan(const tsd_states& s, const tsd_cross_batch& b, int
   // Few row tiles: a source's frames over up to eight CTAs, two steps for each warp at least (one row, 8 key heads, dim 64, us: over 375
   // frames 5.2 with two steps or more, over 750 5.6 with two, 6.4 with four, over 3000 6.7 and 8.7 with six).
   const int64_t units = (int64_t)b.n * s.kv_heads * p.mtiles, slots = (s.dim == 128 ? 2 : 3) * (int64_t)sms;
-  while (p.splits < kMaxSplits && units * p.splits * 2 <= slots && (int64_t)p.splits * 2 * kWarps * kTile * 2 <= s.frames) p.splits *= 2;
+  while (p.splits < kMaxSplits && units * p.splits * 2 <= slots && (int64_t)p.splits * 2 * 4 * kTile * 2 <= s.frames) p.splits *= 2;
+  // More than the device holds at once, of four warps each, but not of two: one turn instead of one and a part, in which few would
+  // read (64 sources of 1500 frames, 8 rows, 8 key heads, dim 64: 35 us, 44; 128: 62, 65.  Two turns of two are worse than more of
+  // four where sources are long: 16 heads, ragged: 58, 48; 160 of 1500, 8 heads: 93, 76.)  Of short sources a CTA's start, join and
+  // end are a good part, and more of them at once hide it (300 sources, 8 heads, dim 64, of 60 frames: 12.8 us, 18.6; 200: 27.4, 32.5;
+  // 375: 42.6, 45.2; 500: 53.2, 55.3.  Dim 128, 60: 18.4, 27.6; 375: 73, 78.  160 sources, dim 128: 375: 48.5, 46.8; 500: 60.6, 59.4;
+  // 750: 87.8, 83.7.)
+  if (units > slots && (units <= 2 * slots || s.frames <= 400)) p.warps = 2;
   return p;
 }
 
 cudaError_t cross_rows_launch(const CrossAttend& a, const CrossRowsPlan& p, cudaStream_t s) {
   const bool bf = a.s.dtype == TSD_BF16;
-  return a.s.dim == 64 ? (bf ? launch<true, 64>(a, p, s) : launch<false, 64>(a, p, s)) : (bf ? launch<true, 128>(a, p, s) : launch<false, 128>(a, p, s));
+  return a.s.dim == 64 ? (bf ? launch_warps<true, 64>(a, p, s) : launch_warps<false, 64>(a, p, s)) : (bf ? launch_warps<true, 128>(a, p, s) : launch_warps<false, 128>(a, p, s));
 }
 
 }  // namespace tsd

@@ -385,6 +385,15 @@ def test_many_sequences():
     check(tsd.CrossStates(k, v, ints(lens)).attend(q), k, v, lens, q, [1] * n, fine=True)
 
 
+@pytest.mark.parametrize("dtype,dim,n", [(BF, 64, 600), (HF, 64, 2000), (BF, 128, 400), (HF, 128, 1300)])
+@pytest.mark.parametrize("rows,group", [(1, 1), (3, 5)])
+def test_more_units_than_the_device_holds(dtype, dim, n, rows, group):
+    lens = [(i * 37) % 301 for i in range(n)]
+    k, v = make(n, 300, 1, dim, dtype, seed=n, poison=math.nan, lens=lens)
+    q = queries(n * rows, group, dim, dtype)
+    check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of([rows] * n), max_rows=rows), k, v, lens, q, [rows] * n, fine=True)
+
+
 def test_binding_refusals():
     k, v = make(2, 20, 2, 64)
     s = tsd.CrossStates(k, v)
