@@ -826,7 +826,7 @@ typedef struct {
   const int32_t* sources; /* [n] or NULL */
   const int32_t* starts;  /* [n + 1] or NULL */
   int32_t rows;           /* rows of the row arrays, 1..2^22 */
-  int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches; results do not depend on it being right */
+  int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches and picks the kernel.  Results need not it to be right, their last bits may follow it */
 } tsd_cross_batch;
 
 /* Bytes of device memory, 16-byte aligned, that such a call of tsd_cross_attend needs for itself alone (may be 0; the structs'
@@ -838,7 +838,7 @@ TSD_API tsd_status tsd_cross_attend_workspace(const tsd_states* states, const ts
  * heads: query heads, a multiple of kv_heads, at most 64 per kv head and 1024; query head h reads kv head
  * h / (heads / kv_heads).  q and out: row and head strides in elements, a multiple of 8, 16-byte aligned; out
  * may not overlap the inputs.  Products take the states' type and accumulate in fp32, as do the softmax's statistics; what is rounded is
- * a weight of the values' product: to 16 bits, with many rows per kv head to the states' type. */
+ * a weight of the values' product: to 16 bits (with fp16 states no finer than 2^-32 of the row's largest). */
 TSD_API tsd_status tsd_cross_attend(const tsd_states* states, const tsd_cross_batch* batch, int32_t heads, const void* q,
                                     int64_t q_row, int64_t q_head, float scale, void* out, int64_t out_row, int64_t out_head,
                                     void* workspace, int64_t workspace_bytes, void* cuda_stream);

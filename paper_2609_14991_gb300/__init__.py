@@ -1308,7 +1308,7 @@ class CrossStates:
         """Attention of queries [rows, heads, dim] over the states (``tsd_cross_attend``).
         Rows starts[i] .. starts[i + 1] (int32 [n + 1]; None: one row each) attend over source
         sources[i] (int32 [n]; None: i): an utterance's hypotheses in one sequence
-        share its reads.  max_rows, the most rows of a sequence, sizes launches only.
+        share its reads.  max_rows, the most rows of a sequence, sizes launches (last bits may follow it).
         scale: 1 / sqrt(dim) if None."""
         who, dev = "CrossStates.attend", self._dev
         s = q.shape

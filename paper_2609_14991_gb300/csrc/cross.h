@@ -6,6 +6,11 @@
 
 namespace tsd {
 
+// A weight goes into the values' product as the sum of two 16-bit floats, hi = round(w f) and round(w - hi): half a step of the
+// second is at most 2^-16 w.  f is below 1, so neither is negative or (a rest of 0) makes a value's infinity a NaN.
+template <bool BF16>
+constexpr float kFirstPart = BF16 ? 255.f / 256 : 31.f / 32;
+
 struct CrossAttend {
   tsd_states s;
   tsd_cross_batch b;

@@ -6,9 +6,9 @@
 // group), two row tiles of 128, over the frames of its source, 128 at a time:
 //   warps 0-7   softmax: a thread is a row (warps 0-3 tile 0, 4-7 tile 1), so its maximum
 //               and sum need no exchange.  Reads its 128 scores from TMEM and leaves the weights
-//               in their place, as the values' product's A operand, in the states' type (the
-//               product wants one type for both; half a step of bf16 is 2^-8 of a weight, and the
-//               sum that divides them is of unrounded ones);
+//               in their place, as the values' product's A operands: the product wants the states'
+//               type, 8 or 11 bits of a weight, so a weight is a sum of two (cross.h), 16 bits, whose products
+//               run one after the other;
 //   warp 8      copies keys and values, a ring of tiles by TMA (128-byte swizzle);
 //   warp 9      issues the MMAs;
 //   warp 10     zeroes what stands behind a source's length in its last tile of values: a
@@ -24,11 +24,11 @@
 // long ones fill the device alike.  A unit that several CTAs share leaves its parts in the workspace, which a
 // second kernel joins in their order.
 //
-// A step of two row tiles and 128 frames takes 1.40 us at dim 128 (0.96 of the library's product rate): the products' 2048 clocks and
-// shared memory's as many (operands 1536, copies 512) do not overlap wholly.  Dim 64: 1.36 us, a values' product whose
+// A step of two row tiles and 128 frames takes 1.80 us at dim 128, its three products (scores, values with both parts of the weights)
+// at 2.1 PFLOP/s, above the library's rate: they bound it (with weights of 8 bits, two products, 1.39 us).  Dim 64: 1.66 us, a values' product whose
 // weights come from TMEM takes 65 clocks at any width, and the softmax 1300 a row tile.  6 ragged texts of up to 1100 tokens, 16 heads, over up to 9000 frames,
-// 4 key heads of 128: 150 us, 1.40 PFLOP/s.  What a unit takes besides its tiles, 2.2 us: first maximum, last products,
-// results (64 KB at 64 bytes per clock, 128 where it is shared).
+// 4 key heads of 128: 194 us.  What a unit takes besides its tiles: first maximum, last products, results (64 KB at 64 bytes per
+// clock, 128 where it is shared).
 #include <algorithm>
 #include <type_traits>
 
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
     // (not 0: what no row may see is an infinite score; the least factor leaves the others 0)
     const float c = a.scale * kLog2e == 0.f ? 0x1p-120f : a.scale * kLog2e;
-    const uint64_t c2 = pair_of(c, c);
+    const uint64_t c2 = pair_of(c, c), minus = pair_of(-1.f, -1.f), first2 = pair_of(kFirstPart<BF16>, kFirstPart<BF16>);
     const float nan = __uint_as_float(0x7fc00000u);
     int at0 = 0, done = 0;  // steps and parts of this row tile so far
     bool fine = true, join = false;
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
               if (lane == 0) mbar_arrive(p_full + 2 * tile + 1);
               break;
             }
-            uint32_t y[32];
+            uint32_t y[32], rest[32];  // the weights' two parts
             float sum;
             bool look = h == 0 && j == 0;
 #pragma unroll 1
@@ -426,7 +426,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                   unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x0, x1);
                   const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                   sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
-                  y[16 * b + e / 2] = narrow2<BF16>(p0, p1);
+                  float w0, w1;
+                  unpair(mul2(pair_of(p0, p1), first2), w0, w1);
+                  const uint32_t w = narrow2<BF16>(w0, w1);
+                  y[16 * b + e / 2] = w;
+                  float r0, r1;
+                  unpair(fma2(pair_of(wide16<BF16>(w & 0xffffu), wide16<BF16>(w >> 16)), minus, pair_of(p0, p1)), r0, r1);
+                  rest[16 * b + e / 2] = narrow2<BF16>(r0, r1);
                 }
               }
               float s0, s1;
@@ -437,7 +443,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
             }
             if (dead) break;
             l += sum;
-            tmem_st32(st + 32 * h, y);
+            tmem_st32(st + 64 * h, y);
+            tmem_st32(st + 64 * h + 32, rest);
             tmem_st_wait();
             fence_before();
             __syncwarp();
@@ -589,8 +596,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
 #pragma unroll
           for (int k = 0; k < kFrames / 32; ++k) {
             const int kk = h * (kFrames / 32) + k;
-            if (kk < steps)
-              mma_f16_ts(tmem + S::kO + t * DIM, tmem + t * 128 + 8 * kk, sw128_mn_desc(vb + kk * 2048, S::kHalf), idesc_f16(128, DIM, true, BF16), j > 0 || kk > 0);
+            if (kk < steps) {
+              const uint32_t w = tmem + t * 128 + 64 * h + 8 * k;
+              const uint64_t v = sw128_mn_desc(vb + kk * 2048, S::kHalf);
+              mma_f16_ts(tmem + S::kO + t * DIM, w, v, idesc_f16(128, DIM, true, BF16), j > 0 || kk > 0);
+              mma_f16_ts(tmem + S::kO + t * DIM, w + 32, v, idesc_f16(128, DIM, true, BF16), true);
+            }
           }
           if (h == 0) {
             mma_commit(o_half + t);

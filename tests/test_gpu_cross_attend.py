@@ -424,3 +424,27 @@ def test_binding_refusals():
                        ((torch.zeros(k.numel() + 4, dtype=BF, device="cuda")[4:].view(k.shape), v), "16-byte")]:
         with pytest.raises(ValueError, match=word):
             tsd.CrossStates(*args)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("frames", [5, 33, 64, 100, 129])
+def test_weights_of_many_rows_keep_16_bits(dtype, dim, frames):
+    """Few frames whose values have either sign: what a weight loses is not averaged away, and the results are small beside it."""
+    n, kv, rows = 4, 4, 1100
+    for_many_rows(n, kv, rows, frames, dim)
+    lens = [frames, frames - 1, 2, 3]
+    k, v = make(n, frames, kv, dim, dtype, seed=frames)
+    v = torch.where(torch.arange(frames, device="cuda")[:, None, None] % 2 == 0, v.abs(), -v.abs())
+    q = queries(n * rows, kv, dim, dtype, seed=frames)
+    out = tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of([rows] * n), max_rows=rows)
+    check(out, k, v, lens, q, [rows] * n, fine=True)
+
+
+@pytest.mark.parametrize("max_rows", [None, 1, 300, 10 ** 9])
+def test_the_bound_moves_no_result_by_more_than_last_bits(max_rows):
+    """Whichever kernel a bound selects keeps 16 bits of a weight."""
+    counts, lens = [1, 300, 20, 0, 2], [500, 77, 300, 9, 1]
+    k, v = make(5, 500, 4, 64, seed=19)
+    q = queries(sum(counts), 8, 64)
+    check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max_rows), k, v, lens, q, counts, fine=True)
