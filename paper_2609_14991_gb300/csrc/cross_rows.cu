@@ -1,13 +1,14 @@
 // Attention over an encoder's states with few query rows per key head: a token of
 // each hypothesis of an utterance (tsd.h: tsd_cross_attend).
 //
-// Mathematics, per row: s_j = (scale log2 e) q . k_j, m >= max_j s_j - 8,
+// Mathematics, per row: s_j = (scale log2 e) q . k_j, m >= max_j s_j - 8 (fp16 states: 1),
 //   out = sum_j 2^(s_j - m) v_j / sum_j 2^(s_j - m)
-// in one pass over the frames; the maximum follows when a score passes it by more than
-// 2^8.  Rows (row = token * group + head of the group) are taken 16 at a time, as the
+// in one pass over the frames; the maximum follows when a score passes it by more.
+// Rows (row = token * group + head of the group) are taken 16 at a time, as the
 // rows of mma.sync.m16n8k16 (fp32 accumulate).  A weight goes into the values'
 // product as a sum of two 16-bit floats, so it keeps 16 bits or more: the products
-// are not what bounds this kernel.
+// are not what bounds this kernel.  fp16's end at 2^-24, and many frames far below a row's largest may be its result
+// (where that one's values are 0): fp16 weights are taken relative to m - 14.
 //
 // Layout: a warp has frames of its own, 16 at a time, in a ring of its own that it
 // fills with 16-byte asynchronous copies (frames past the length arrive as zeros), so
@@ -80,6 +81,8 @@ __global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k
   using S = RowsShape<DIM, kWarps>;
   constexpr int ST = S::kStages, kChunks = DIM / 8;  // 16-byte chunks of a frame
   constexpr int kSteps = DIM / 16, kCols = DIM / 8;
+  // (weights up to 2^(kUp + kLag), fp16's largest is below 2^16; one is good to 2^-25, 2^-39 of the row's largest)
+  constexpr float kUp = BF16 ? 0.f : 14.f, kLag = BF16 ? 8.f : 1.f;
   extern __shared__ __align__(128) unsigned char smem[];
   float* s_out = reinterpret_cast<float*>(smem);
   float2* s_ml = reinterpret_cast<float2*>(smem + S::kMl);
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k
               s[nt][2 * h + e] = v;
               top[h] = fmaxf(top[h], v);
             }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + 8.f || top[1] > m[1] + 8.f)) {
+        if (__any_sync(0xffffffffu, top[0] > m[0] + kLag || top[1] > m[1] + kLag)) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             float x = fmaxf(m[h], top[h]);
@@ -182,7 +185,7 @@ __global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k
         uint32_t p[4], rest[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float ref = m[h] == -INFINITY ? 0.f : m[h];
+          const float ref = m[h] == -INFINITY ? 0.f : m[h] - kUp;
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
             const float x = ex2_approx(s[nt][2 * h] - ref), y = ex2_approx(s[nt][2 * h + 1] - ref);

@@ -448,3 +448,27 @@ def test_the_bound_moves_no_result_by_more_than_last_bits(max_rows):
     k, v = make(5, 500, 4, 64, seed=19)
     q = queries(sum(counts), 8, 64)
     check(tsd.CrossStates(k, v, ints(lens)).attend(q, starts=starts_of(counts), max_rows=max_rows), k, v, lens, q, counts, fine=True)
+
+
+@pytest.mark.parametrize("rows", [1, 600])
+@pytest.mark.parametrize("gap", [14.0, 17.5, 20.6, 23.0, 25.2])
+def test_small_weights_of_fp16_states(rows, gap):
+    """Frames far below a row's largest, whose values are 0 (an attention sink): the small weights are the result.  Besides
+    check()'s bounds a weight is off by half fp16's smallest step, 2^-25, where the largest is 2^14 at least (many rows: 2^7)."""
+    n, kv, frames, every = 40, 4, 1500, 300
+    if rows > 1:
+        for_many_rows(n, kv, rows, frames, 64)
+    g = torch.Generator().manual_seed(int(gap))
+    k = torch.zeros(n, frames, kv, 64)
+    k[..., 0] = -gap + 0.25 * torch.rand(n, frames, kv, generator=g)
+    v = 0.5 + torch.rand(n, frames, kv, 64, generator=g)
+    k[:, 7::every], v[:, 7::every] = 0, 0
+    k, v = k.half().cuda(), v.half().cuda()
+    q = torch.zeros(n * rows, kv, 64, dtype=HF, device="cuda")
+    q[..., 0] = 1.0
+    out = tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * n), max_rows=rows, scale=math.log(2)).double()
+    want, mag, top = reference(k, v, None, q.view(n, rows, kv, 64)[:, 0], [1] * n, list(range(n)), math.log(2))
+    small = frames * 2.0 ** (-39 if rows == 1 else -32) * float(v.max()) / (frames // every)  # (the largest, of which there are as many, divide it)
+    tol = (2.0 ** -16 + 2.0 ** -14 + 2 * top * 2.0 ** -18) * mag + 2.0 ** -11 * want.abs() + 2.0 ** -25 + small
+    off = (out.view(n, rows, kv, 64) - want[:, None]).abs()
+    assert bool((off <= tol[:, None]).all()), float((off / tol[:, None]).max())
