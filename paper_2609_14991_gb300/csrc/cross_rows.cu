@@ -6,7 +6,7 @@
 // in one pass over the frames; the maximum follows when a score passes it by more.
 // Rows (row = token * group + head of the group) are taken 16 at a time, as the
 // rows of mma.sync.m16n8k16 (fp32 accumulate).  A weight goes into the values'
-// product as a sum of two 16-bit floats, so it keeps 16 bits or more: the products
+// product as a sum of two 16-bit floats (cross.h), so it keeps 16 bits: the products
 // are not what bounds this kernel.  fp16's end at 2^-24, and many frames far below a row's largest may be its result
 // (where that one's values are 0): fp16 weights are taken relative to m - 14.
 //
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k
           for (int nt = 0; nt < 2; ++nt) {
             const float x = ex2_approx(s[nt][2 * h] - ref), y = ex2_approx(s[nt][2 * h + 1] - ref);
             l[h] += x + y;
-            const uint32_t w = narrow2<BF16>(x, y);
+            const uint32_t w = narrow2<BF16>(x * kFirstPart<BF16>, y * kFirstPart<BF16>);
             p[2 * nt + h] = w;
             rest[2 * nt + h] = narrow2<BF16>(x - wide16<BF16>(w & 0xffffu), y - wide16<BF16>(w >> 16));
           }

@@ -472,3 +472,19 @@ def test_small_weights_of_fp16_states(rows, gap):
     tol = (2.0 ** -16 + 2.0 ** -14 + 2 * top * 2.0 ** -18) * mag + 2.0 ** -11 * want.abs() + 2.0 ** -25 + small
     off = (out.view(n, rows, kv, 64) - want[:, None]).abs()
     assert bool((off <= tol[:, None]).all()), float((off / tol[:, None]).max())
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [1, 1700])
+def test_an_infinite_value_is_infinite_in_the_result(dtype, rows):
+    """A visible frame with a value of inf, and one of -inf: the results of that dimension are they, as the formula's."""
+    if rows > 1:
+        for_many_rows(4, 2, rows, 100, 64)
+    k, v = make(4, 100, 2, 64, dtype, seed=5)
+    k *= 0.25
+    v[0, 3, 0, 9], v[1, 50, 1, 7] = math.inf, -math.inf
+    q = queries(4 * rows, 2, 64, dtype)
+    out = tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * 4), max_rows=rows).view(4, rows, 2, 64)
+    assert bool((out[0, :, 0, 9] == math.inf).all()) and bool((out[1, :, 1, 7] == -math.inf).all())
+    out[0, :, 0, 9], out[1, :, 1, 7] = 0, 0
+    assert bool(torch.isfinite(out).all())
