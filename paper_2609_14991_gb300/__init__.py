@@ -710,10 +710,13 @@ def _bind_torch():
     import torch
 
     torch.cuda.init()
-    _F32, _I32, _U8, _new_empty = torch.float32, torch.int32, torch.uint8, torch.empty
-    _get_device, _get_raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     for i in range(torch.cuda.device_count()):
         _devices[i] = torch.device("cuda", i)
+    _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
+    # last, what is looked at for whether all is bound: other threads' first calls may come meanwhile
+    _get_raw_stream = torch._C._cuda_getCurrentRawStream
+    _new_empty = torch.empty
+    _get_device = torch._C._cuda_getDevice
 
 
 def _dtype_code(t) -> int:

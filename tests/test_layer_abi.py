@@ -1,7 +1,9 @@
 """Rotary positions, residual norms and attention over encoder states refuse bad
 arguments before any device work, and the host's frequencies are the formula's (no GPU)."""
+import concurrent.futures
 import ctypes
 import math
+import threading
 from decimal import Decimal, getcontext
 
 import numpy as np
@@ -166,3 +168,36 @@ def test_bindings_refuse():
     for a, word in [((k.float(), k), "bf16"), ((k, k[:1]), "v must"), ((k, k.half()), "v must"), ((k[..., :32], k[..., :32]), "dim is"), ((k, k), "CUDA")]:
         with pytest.raises(ValueError, match=word):
             tsd.CrossStates(*a)
+
+
+def test_a_first_call_beside_another_threads_first_call(monkeypatch):
+    """What the bindings keep of torch is complete before a thread can find it (torch's calls are replaced: no GPU)."""
+    inside, done, first = threading.Event(), threading.Event(), threading.Lock()
+
+    def device_count():
+        if first.acquire(blocking=False):  # the thread that came first waits here until the other's call has ended
+            inside.set()
+            done.wait(5)
+        return 2
+
+    for name in ("_new_empty", "_get_device", "_get_raw_stream", "_F32", "_I32", "_U8"):
+        monkeypatch.setattr(tsd, name, None)
+    monkeypatch.setattr(tsd, "_devices", {})
+    monkeypatch.setattr(torch.cuda, "init", lambda: None)
+    monkeypatch.setattr(torch.cuda, "device_count", device_count)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: 7 + dev, raising=False)
+    monkeypatch.setattr(torch, "empty", lambda n, dtype, device: (n, dtype, device))
+
+    def calls():
+        return tsd._current_device(), tsd._empty(3, torch.float32, 1, None), tsd._workspace(5, 0, None), tsd._raw_stream(None, 1)
+
+    with concurrent.futures.ThreadPoolExecutor(2) as ex:
+        a = ex.submit(calls)
+        assert inside.wait(5)
+        b = ex.submit(calls)
+        try:
+            got = b.result(5)
+        finally:
+            done.set()
+        assert got == a.result(5) == (1, (3, torch.float32, torch.device("cuda", 1)), (5, torch.uint8, torch.device("cuda", 0)), 8)
