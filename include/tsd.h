@@ -799,8 +799,8 @@ typedef struct {
  * Row strides in elements, at least d; any alignment of the element types (accesses are
  * wide where all row arrays stand equally off a multiple of eight elements, as contiguous ones do).  r may be x, and h may be y
  * (without y: x), with the same strides; other overlaps are not allowed.  Everything between is fp32 and rounded once: h comes of
- * the unrounded r.  1 <= n <= 2^27, 1 <= d <= 16384.  A row's results do not depend on the
- * other rows; their last bits may on where it stands (mod 8 elements). */
+ * the unrounded r.  1 <= n <= 2^27, 1 <= d <= 16384.  A row's results are the same bits whatever
+ * else is in the call; the last ones may depend on where its arrays stand, and on whether the call's row arrays stand alike (mod 8 elements). */
 TSD_API tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int32_t x_dtype, int64_t x_row, const void* y,
                                      int32_t dtype, int64_t y_row, const tsd_norm* post, const void* gate,
                                      int64_t gate_row, float scale, const tsd_norm* norm, void* r, int64_t r_row,

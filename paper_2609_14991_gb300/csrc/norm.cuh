@@ -32,21 +32,45 @@ using tc::unpair;
 constexpr int kMaxSmem = 227 * 1024 - 512;  // of a CTA, dynamic
 constexpr int kRingBytes = 128 * 1024;      // of an SM for rows on their way; the rest caches weights
 
-// Sum over the row's THREADS threads (a power of two; above a warp: the whole CTA; the warp's lanes are all here).
+// Sum over a row of its groups' sums v (group c * THREADS + t is thread t's c-th; THREADS a power of two; above a warp: the whole CTA;
+// the warp's lanes are all here).  Always in the same order, so that a row's bits do not depend on how many threads the call's size
+// gives it: 32 groups that follow each other by halves, then those sums by halves; groups that a row does not have are 0.
 // s_part: two places that sums take in turn, so that one barrier serves for each.
-template <int THREADS>
-__device__ __forceinline__ float row_sum(float v, float (*s_part)[32], int& turn) {
+template <int THREADS, int CHUNKS>
+__device__ __forceinline__ float row_sum(const float (&v)[CHUNKS], float (*s_part)[32], int& turn) {
+  static_assert(CHUNKS <= 2 || (CHUNKS == 4 && THREADS >= 32), "");
+  const auto swap = [](float x, int o) { return __shfl_xor_sync(0xffffffffu, x, o); };
+  float s;
+  if constexpr (CHUNKS == 1 || THREADS < 32) {  // (two groups of fewer lanes than a warp's: halves of 32)
+    s = v[0];
+    if constexpr (CHUNKS == 2) s += v[1];
 #pragma unroll
-  for (int o = THREADS < 32 ? THREADS / 2 : 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = THREADS < 32 ? THREADS / 2 : 16; o; o >>= 1) s += swap(s, o);
+  } else {
+    // a lane goes on with half of the sums: the other half's of its partner for its own
+    const int lane = threadIdx.x & 31;
+    const bool high = lane & 16;
+    s = (high ? v[CHUNKS / 2] : v[0]) + swap(high ? v[0] : v[CHUNKS / 2], 16);
+    if constexpr (CHUNKS == 4) {
+      const float z = (high ? v[3] : v[1]) + swap(high ? v[1] : v[3], 16);
+      s = (lane & 8 ? z : s) + swap(lane & 8 ? s : z, 8);
+    } else {
+      s += swap(s, 8);
+    }
+#pragma unroll
+    for (int o = 4; o; o >>= 1) s += swap(s, o);
+    s += swap(s, 16);
+    if constexpr (CHUNKS == 4) s += swap(s, 8);
+  }
   if constexpr (THREADS > 32) {
     float* part = s_part[turn ^= 1];
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
     __syncthreads();
-    v = part[threadIdx.x & (THREADS / 32 - 1)];
+    s = part[threadIdx.x & (THREADS / 32 - 1)];
 #pragma unroll
-    for (int o = THREADS / 64; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    for (int o = THREADS / 64; o; o >>= 1) s += swap(s, o);
   }
-  return v;
+  return s;
 }
 
 // A thread's elements of a row: groups of eight, THREADS of them apart, or (apart) every THREADS-th element.
@@ -150,21 +174,25 @@ __device__ __forceinline__ float both(uint64_t v) {
 template <int THREADS, int CHUNKS, NormHow HOW>
 __device__ __forceinline__ float statistics(const tsd_norm& k, const Places<THREADS, CHUNKS, HOW>& pl, uint64_t* v, float (*s_part)[32], int& turn) {
   constexpr int N = 4 * CHUNKS;
+  float sum[CHUNKS];  // of groups of eight
   if (k.kind == TSD_NORM_LAYER) {
-    uint64_t s = v[0];
 #pragma unroll
-    for (int i = 1; i < N; ++i) s = add2(s, v[i]);
-    const float mean = row_sum<THREADS>(both(s), s_part, turn) / pl.d;
+    for (int c = 0; c < CHUNKS; ++c) sum[c] = both(add2(add2(v[4 * c], v[4 * c + 1]), add2(v[4 * c + 2], v[4 * c + 3])));
+    const float mean = row_sum<THREADS, CHUNKS>(sum, s_part, turn) / pl.d;
     const uint64_t m2 = pair_of(-mean, -mean);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = add2(v[i], m2);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) pl.trim(c, v + 4 * c);
   }
-  uint64_t s = mul2(v[0], v[0]);
 #pragma unroll
-  for (int i = 1; i < N; ++i) s = fma2(v[i], v[i], s);
-  return 1.f / sqrtf(row_sum<THREADS>(both(s), s_part, turn) / pl.d + k.eps);
+  for (int c = 0; c < CHUNKS; ++c) {
+    uint64_t s = mul2(v[4 * c], v[4 * c]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = fma2(v[4 * c + i], v[4 * c + i], s);
+    sum[c] = both(s);
+  }
+  return 1.f / sqrtf(row_sum<THREADS, CHUNKS>(sum, s_part, turn) / pl.d + k.eps);
 }
 // The second, for group c, but for that factor: v <- v * weight
 template <int THREADS, int CHUNKS, NormHow HOW>

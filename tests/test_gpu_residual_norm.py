@@ -250,3 +250,29 @@ def test_binding_refusals():
         tsd.residual_norm(x, y, eps=-1.0)
     with pytest.raises(tsd.TsdError, match="scale"):
         tsd.residual_norm(x, y, scale=float("inf"))
+
+
+@pytest.mark.parametrize("d", [64, 200, 264, 512, 520, 1000, 1024, 1536, 2048, 4096, 5000, 8184, 8192, 12000])
+@pytest.mark.parametrize("norm,post", [("rms", "layer"), ("layer", "rms")])
+def test_bits_do_not_depend_on_other_rows(d, norm, post):
+    """Rows alone, in calls of some and of more than the device holds at once: in fp32, after a norm on both sides, bit by bit."""
+    n = 1200
+    x, y, (w, b, pw, pb), gt = make(n, d, FL, FL, "channels", seed=d)
+    kw = dict(norm=norm, weight=w, bias=b, post=post, post_weight=pw, post_bias=pb if post == "layer" else None, gate=gt, scale=0.7)
+    h, r = tsd.residual_norm(x, y, **kw)
+    for a, c in [(0, 1), (1199, 1200), (500, 503), (100, 300), (0, 900), (250, 1199)]:
+        h2, r2 = tsd.residual_norm(x[a:c], y[a:c], **kw)
+        assert torch.equal(h2, h[a:c]) and torch.equal(r2, r[a:c]), (a, c)
+
+
+@pytest.mark.parametrize("d", [63, 249, 257, 505, 777, 1017, 1021, 2043, 4095, 8191])
+def test_bits_of_odd_widths_do_not_depend_on_other_rows(d):
+    """The same of rows that stand off multiples of eight elements, where all arrays of the calls stand alike."""
+    n = 1200
+    x, y, (w, b, pw, _), gt = make(n, d, FL, FL, "rows", seed=d)
+    kw = dict(norm="layer", weight=w, bias=b, post="rms", post_weight=pw)
+    h, r = tsd.residual_norm(x, y, gate=gt, **kw)
+    for a, c in [(0, 1), (7, 8), (8, 9), (1199, 1200), (500, 503), (100, 300), (251, 1199)]:
+        h2, r2 = torch.zeros_like(h), torch.zeros_like(r)
+        tsd.residual_norm(x[a:c], y[a:c], gate=gt[a:c], out=(h2[a:c], r2[a:c]), **kw)
+        assert torch.equal(h2[a:c], h[a:c]) and torch.equal(r2[a:c], r[a:c]), (a, c)
