@@ -599,8 +599,8 @@ TSD_API tsd_status tsd_encoder_launches_per_chunk(const tsd_encoder* enc, int32_
 /* From logits in memory: n rows of C elements of type dtype, row_stride
  * elements apart (any alignment of the element type).  1 <= n <= 2^27,
  * 1 <= C <= 262144, row_stride >= C (or n = 1), temperature > 0 and finite, as
- * log2(e) / temperature in fp32.  A row's results do not depend on the
- * other rows; their last bits may on where it stands (mod 8 elements). */
+ * log2(e) / temperature in fp32.  A row's results are the same bits whatever
+ * else is in the call; the last ones may depend on where it stands (mod 16 bytes). */
 TSD_API tsd_status tsd_label_scores(int32_t n, int32_t C, const void* logits, int32_t dtype, int64_t row_stride,
                                     float temperature, int32_t m, const int32_t* labels, int32_t k, float* logp,
                                     float* entropy, int32_t* alt_labels, float* alt_logp, void* cuda_stream);

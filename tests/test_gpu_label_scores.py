@@ -143,6 +143,20 @@ def test_rows_do_not_depend_on_the_call():
         assert torch.equal(one.alt_labels[0], all_.alt_labels[r]) and torch.equal(one.alt_logp[0], all_.alt_logp[r])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("C,n", [(37, 2000), (263, 700), (1031, 1300), (4099, 400), (20001, 40), (70001, 9)])
+def test_bits_do_not_depend_on_other_rows(C, n, dtype):
+    """Rows of any alignment, alone and a few of them at a time, at the addresses that they have in a large call."""
+    x = rows(n, C, dtype, C, offset=3)
+    lab = given(n, 2, C, C).to(DEV)
+    all_ = tsd.label_scores(x, lab, k=5, temperature=0.9)
+    for a, b in [(0, 1), (1, 2), (n - 1, n), (3, 8), (n // 2, n)]:
+        some = tsd.label_scores(x[a:b], lab[a:b], k=5, temperature=0.9)
+        for name in ("logp", "entropy", "alt_labels", "alt_logp"):
+            one, other = getattr(some, name), getattr(all_, name)[a:b]
+            assert torch.equal(torch.nan_to_num(one, nan=7.0), torch.nan_to_num(other, nan=7.0)), (name, a, b)  # (NaN: a label outside the row)
+
+
 # ---------------------------------------------------------------- from joint rows
 
 def joint_inputs(n, H, C, seed, lda=None, ldw=None):
