@@ -1,4 +1,5 @@
 // The entry point of norms around a block (tsd.h: tsd_residual_norm); norm.cuh has the kernel.
+#include <algorithm>
 #include <cmath>
 
 #include "internal.h"
@@ -22,6 +23,27 @@ tsd_status check_norm(const char* what, const tsd_norm* k) {
   if (!(k->eps >= 0.f && std::isfinite(k->eps))) return fail(TSD_EINVAL, "tsd_residual_norm: %s needs a finite eps of 0 or more", what);
   if (reinterpret_cast<uintptr_t>(k->weight) % 4 || reinterpret_cast<uintptr_t>(k->bias) % 4)
     return fail(TSD_EINVAL, "tsd_residual_norm: %s's weight or bias is not aligned", what);
+  return TSD_OK;
+}
+
+// Whether `bytes` at p lie in one of n rows of `width` bytes, `row` apart from `base` on (at least `width`, or there is one).
+bool in_rows(const void* p, int64_t bytes, const void* base, int64_t row, int64_t width, int n) {
+  const int64_t at = reinterpret_cast<intptr_t>(p) - reinterpret_cast<intptr_t>(base);
+  if (at + bytes <= 0) return false;
+  if (at < 0 || n == 1) return at < width;
+  const int64_t i = std::min<int64_t>(at / row, n - 1);  // the last row that begins at p or before it
+  return at < i * row + width || (i + 1 < n && at + bytes > (i + 1) * row);
+}
+
+// Results (NULL: none) over the gate or over a norm's weight or bias.
+tsd_status check_vectors(const char* what, const void* to, int64_t row, int64_t width, int n, int d, const NormArgs& a, const void* gate, int64_t gate_row,
+                         int size) {
+  if (!to) return TSD_OK;
+  if (gate && (gate_row ? gate == to : in_rows(gate, (int64_t)d * size, to, row, width, n))) return fail(TSD_EINVAL, "tsd_residual_norm: %s and the gate overlap", what);
+  for (const tsd_norm* k : {&a.post, &a.norm}) {
+    if (k->weight && in_rows(k->weight, 4ll * d, to, row, width, n)) return fail(TSD_EINVAL, "tsd_residual_norm: %s and a weight overlap", what);
+    if (k->bias && in_rows(k->bias, 4ll * d, to, row, width, n)) return fail(TSD_EINVAL, "tsd_residual_norm: %s and a bias overlap", what);
+  }
   return TSD_OK;
 }
 
@@ -67,6 +89,9 @@ extern "C" tsd_status tsd_residual_norm(int32_t n, int32_t d, const void* x, int
   if ((y && a.norm.kind != TSD_NORM_NONE && (h == r || h == x)) || (y && r == y) || (y && moved(x, x_row, r, r_row)) ||
       (a.norm.kind != TSD_NORM_NONE && moved(src, src_row, h, h_row)))
     return fail(TSD_EINVAL, "tsd_residual_norm: results overlap each other or another input");
+  // what other rows read, or read later, is not written
+  if (tsd_status st = check_vectors("r", y ? r : nullptr, r_row * x_size, (int64_t)d * x_size, n, d, a, gate, gate_row, size)) return st;
+  if (tsd_status st = check_vectors("h", a.norm.kind != TSD_NORM_NONE ? h : nullptr, h_row * size, (int64_t)d * size, n, d, a, gate, gate_row, size)) return st;
   a.n = n, a.d = d, a.x = x, a.x_row = x_row, a.scale = scale;
   if (y) a.y = y, a.y_row = y_row, a.gate = gate, a.gate_row = gate ? gate_row : 0, a.r = r, a.r_row = r_row;
   if (a.norm.kind != TSD_NORM_NONE) a.h = h, a.h_row = h_row;

@@ -124,6 +124,29 @@ def test_residual_norm_refusals(L):
         refused(L, call(**kw), word)
 
 
+def test_residual_norm_refuses_results_over_what_other_rows_read(L):
+    """A gate, weights or biases in the memory of r or h: rows would race for them."""
+    F = 1 << 20
+    norm = lambda **kw: ctypes.byref(tsd.NormC(*{**dict(kind=1, eps=1e-5, weight=F, bias=None), **kw}.values()))  # noqa: E731
+
+    def call(n=3, d=16, x=P, xr=40, y=4096, yr=40, post=None, gate=None, gr=0, nm=norm(), r=8192, rr=40, h=16384, hr=40, xt=1):
+        return L.tsd_residual_norm(n, d, x, xt, xr, y, 1, yr, post, gate, gr, 1.0, nm, r, rr, h, hr, None)
+
+    for gr in (0, 40):
+        refused(L, call(gate=8192, gr=gr), "gate")
+        refused(L, call(gate=16384, gr=gr), "gate")
+        refused(L, call(gate=P, gr=gr, r=P), "gate")     # x in place, and the gate is x
+        refused(L, call(gate=4096, gr=gr, h=4096), "gate")  # likewise y
+    for at, word in [(8192 + 30, "gate"), (8192 - 30, "gate"), (8192 + 2 * 80, "gate"), (16384 + 80 + 30, "gate"), (16384 + 2 * 80 - 2, "gate")]:
+        refused(L, call(gate=at), word)
+    for at in (8192, 8192 - 60, 8192 + 28, 8192 + 2 * 80 + 28, 16384, 16384 + 80):
+        refused(L, call(nm=norm(weight=at)), "weight")
+        refused(L, call(nm=norm(bias=at)), "bias")
+        refused(L, call(post=norm(weight=at)), "weight")
+        refused(L, call(post=norm(bias=at)), "bias")
+    refused(L, call(y=None, nm=norm(weight=16384 + 4)), "weight")
+
+
 def test_cross_refusals(L):
     def call(s=(), b=(), heads=4, q=P, qr=256, qh=64, scale=0.1, out=P, orow=256, oh=64, ws=None, nws=0):
         x = dict(k=P, v=P, ks=4096, kf=128, kh=64, vs=4096, vf=128, vh=64, lens=P, dtype=1, n_sources=3, frames=32, kv_heads=2, dim=64)
