@@ -1206,7 +1206,8 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
     (``tsd_residual_norm``).  norm and post: "rms", "layer" or None (no h; y as it is).
     x, y: cuda [n, d], any row stride; y float32, bfloat16 or float16, x the same or
     float32.  gate: y's type, [d] or [n, d].  Weights and biases: float32 [d].  y None:
-    h = norm(x) of x's type, and r is x.  out: (h, r) to write; r may be x and h may be y."""
+    h = norm(x) of x's type, and r is x.  out: (h, r) to write, None for what the call has not or
+    shall allocate; r may be x and h may be y."""
     who = "residual_norm"
     shape = x.shape
     if len(shape) != 2 or not (1 <= shape[0] <= 1 << 27 and 1 <= shape[1] <= 16384):
@@ -1242,6 +1243,10 @@ def residual_norm(x, y=None, norm: Optional[str] = "rms", weight=None, bias=None
             gp = gate.data_ptr()
     elif gate is not None or post is not None or norm is None:
         raise ValueError(f"{who}: without y there is a norm, and no gate or post")
+    if norm is None and h is not None:
+        raise ValueError(f"{who}: without a norm there is no h to write")
+    if y is None and r is not None and r is not x:
+        raise ValueError(f"{who}: without y there is no r to write: it is x")
     pn = _norm_arg("norm", norm, weight, bias, d, eps, dev)
     pp = _norm_arg("post", post, post_weight, post_bias, d, eps, dev)
     if norm is not None:

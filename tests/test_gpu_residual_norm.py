@@ -276,3 +276,18 @@ def test_bits_of_odd_widths_do_not_depend_on_other_rows(d):
         h2, r2 = torch.zeros_like(h), torch.zeros_like(r)
         tsd.residual_norm(x[a:c], y[a:c], gate=gt[a:c], out=(h2[a:c], r2[a:c]), **kw)
         assert torch.equal(h2[a:c], h[a:c]) and torch.equal(r2[a:c], r[a:c]), (a, c)
+
+
+def test_results_that_a_call_does_not_write_are_refused():
+    x, y, (w, _, _, _), _ = make(4, 64, BF, BF)
+    h, r = torch.zeros_like(x), torch.zeros_like(x)
+    with pytest.raises(ValueError, match="no h to write"):
+        tsd.residual_norm(x, y, norm=None, out=(h, r))
+    with pytest.raises(ValueError, match="no r to write"):
+        tsd.residual_norm(x, weight=w, out=(h, r))
+    a, b = tsd.residual_norm(x, weight=w, out=(h, x))
+    assert a is h and b is x
+    check(x, None, "rms", None, None, 1.0, w, None, None, None, 1e-5, h, x)
+    a, b = tsd.residual_norm(x, y, norm=None, out=(None, r))
+    assert a is None and b is r
+    check(x, y, None, None, None, 1.0, None, None, None, None, 1e-5, None, r)
