@@ -306,7 +306,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     const uint32_t ot = tmem + (uint32_t)(S::kO + tile * DIM) + ((uint32_t)((warp & 3) * 32) << 16);
     // (not 0: what no row may see is an infinite score; the least factor leaves the others 0)
     const float c = a.scale * kLog2e == 0.f ? 0x1p-120f : a.scale * kLog2e;
-    const uint64_t c2 = pair_of(c, c), minus = pair_of(-1.f, -1.f), first2 = pair_of(kFirstPart<BF16>, kFirstPart<BF16>);
+    const float sign = c < 0.f ? -1.f : 1.f;
+    // A score is the product times c less the maximum's, rounded once: off by half a step of that maximum, above 2^26 (or below -2^26)
+    // more than an exponent should be.  There c is the next power of two, so that the maximum's own is 0: of such scores
+    // any two that differ do so by so much that the lower weighs nothing (by 4 at least, times c's change).
+    constexpr float kFar = 0x1p26f;
+    const float c_far = sign * __uint_as_float((__float_as_uint(fabsf(c)) + 0x7fffffu) & 0x7f800000u);
+    const uint64_t minus = pair_of(-1.f, -1.f), first2 = pair_of(kFirstPart<BF16>, kFirstPart<BF16>);
     const float nan = __uint_as_float(0x7fc00000u);
     int at0 = 0, done = 0;  // steps and parts of this row tile so far
     bool fine = true, join = false;
@@ -336,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
       }
       bool dead = false;
       if (tile == 0 || p.two()) {
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, factor = c;  // (of the row: c, or c_far as its maximum is)
 #pragma unroll 1
         for (int j = 0; j < p.n; ++j) {
           if (!__all_sync(0xffffffffu, mbar_wait(s_full + tile, (uint32_t)(at0 + j) & 1u))) {
@@ -346,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
           fence_after();
           const int left = p.len - (p.lo + j) * kFrames;  // frames from here on
           if (left < kFrames) {  // the last tile: what lies behind the length becomes a score that gives weight 0
-            const float none = c < 0.f ? INFINITY : -INFINITY;
+            const float none = sign * -INFINITY;
 #pragma unroll 1
             for (int b = left / 16; b < kFrames / 16; ++b) {
               float v[16];
@@ -386,11 +392,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                   float v[32];
                   tmem_ld32(st + 64 * h + 32 * b, v);
 #pragma unroll
-                  for (int e = 0; e < 32; ++e) top = fmaxf(top, v[e] * c);
+                  for (int e = 0; e < 32; ++e) top = fmaxf(top, v[e] * sign);
                 }
-                const float x = fmaxf(m, top);
-                const float w = x == m ? 1.f : ex2_approx(m - x);
-                m = x;
+                const float near = top * fabsf(c);
+                top = fabsf(near) < kFar ? near : top * fabsf(c_far);
+                float w = 1.f;
+                if (top > m) {
+                  w = ex2_approx(m - top);
+                  m = top;
+                  factor = fabsf(near) < kFar ? c : c_far;
+                }
                 l *= w;
                 if (j > 0 || h > 0) {
                   // the last step's values are in the accumulator (this one's scores came after them); the first 64's
@@ -411,10 +422,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                 }
                 tmem_ld32_begin(st + 64 * h, raw[0]);
               }
-              // (no maximum yet, every score so far -inf: relative to -1e30 any other has outgrown it)
-              const float ref = m > -INFINITY ? m - 7.f : look ? 0.f : -1e30f;
-              const uint64_t ref2 = pair_of(-ref, -ref);
-              uint64_t sums[4] = {0, 0, 0, 0};
+              // (no maximum yet, every score so far -inf: any other has outgrown the least number)
+              const float ref = m > -INFINITY ? m - 7.f : look ? 0.f : -3.4e38f;
+              const uint64_t ref2 = pair_of(-ref, -ref), c2 = pair_of(factor, factor);
+              uint64_t sums[2] = {0, 0};  // (four take registers that there are not: 205 us where two take 200, 6 x 1100 over 9000, fp16)
 #pragma unroll
               for (int b = 0; b < 2; ++b) {
                 tmem_ld32_wait(raw[b]);
@@ -425,7 +436,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                   float x0, x1;
                   unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x0, x1);
                   const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-                  sums[e / 2 & 3] = add2(sums[e / 2 & 3], pair_of(p0, p1));
+                  sums[e / 2 & 1] = add2(sums[e / 2 & 1], pair_of(p0, p1));
                   float w0, w1;
                   unpair(mul2(pair_of(p0, p1), first2), w0, w1);
                   const uint32_t w = narrow2<BF16>(w0, w1);
@@ -436,7 +447,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                 }
               }
               float s0, s1;
-              unpair(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), s0, s1);
+              unpair(add2(sums[0], sums[1]), s0, s1);
               sum = s0 + s1;
               if (look || !__any_sync(0xffffffffu, live && sum > 32768.f)) break;
               look = true;

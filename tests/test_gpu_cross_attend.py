@@ -488,3 +488,43 @@ def test_an_infinite_value_is_infinite_in_the_result(dtype, rows):
     assert bool((out[0, :, 0, 9] == math.inf).all()) and bool((out[1, :, 1, 7] == -math.inf).all())
     out[0, :, 0, 9], out[1, :, 1, 7] = 0, 0
     assert bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype,size", [(HF, 3000.0), (BF, 3000.0), (BF, 1e14)])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("rows", [2, 1500])
+def test_scores_of_any_finite_size(dtype, size, scale, rows):
+    """Scores up to 6e8 (1e30), of which each row's largest leaves the others nothing: the result is its frame's values."""
+    n, kv, frames = 4, 1, 200
+    if rows > 2:
+        for_many_rows(n, kv, 2 * rows, frames, 64)
+    g = torch.Generator().manual_seed(int(rows))
+    signs = torch.sign(torch.randn(64, generator=g))
+    size_of = torch.stack([torch.randperm(frames, generator=g).float() for _ in range(n)]) / frames
+    k = (size * size_of[:, :, None, None] * signs).to(dtype).cuda()
+    v = torch.randn(n, frames, kv, 64, generator=g).to(dtype).cuda()
+    q = (size * (0.5 + 0.5 * torch.rand(n * rows, 2, 1, generator=g)) * signs).to(dtype).cuda()
+    out = tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * n), max_rows=rows, scale=scale).view(n, rows * 2, 64)
+    for i in range(n):
+        size_in = k[i, :, 0].double() @ signs.double().cuda() * scale
+        assert int((size_in == size_in.max()).sum()) == 1
+        assert torch.equal(out[i], v[i, int(size_in.argmax()), 0].expand(2 * rows, 64))
+
+
+@pytest.mark.parametrize("rows", [2, 700])
+@pytest.mark.parametrize("hidden", [1, 130, 600])
+def test_very_low_scores_behind_infinite_ones(rows, hidden):
+    """Two frames of score -3e30 behind and before others of -inf weigh a half each."""
+    n, frames, kv = 4, 700, 4
+    if rows > 2:
+        for_many_rows(n, kv, rows, frames, 64)
+    _, v = make(n, frames, kv, 64, seed=hidden)
+    k = torch.zeros_like(v)
+    k[..., 5] = -math.inf
+    two = [hidden, 699]
+    k[:, two, :, 5] = -1e20
+    q = torch.zeros(n * rows, kv, 64, dtype=BF, device="cuda")
+    q[..., 5] = 3e10
+    out = tsd.CrossStates(k, v).attend(q, starts=starts_of([rows] * n), max_rows=rows, scale=1.0).view(n, rows, kv, 64)
+    want = v[:, two].double().mean(1)[:, None]
+    assert bool(((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -15 * v[:, two].double().abs().amax(1)[:, None]).all())
