@@ -67,7 +67,7 @@ struct TilesShape {
 static_assert(TilesShape<64>::kStages % 2 == 0 && TilesShape<128>::kStages % 2 == 0, "keys in even stages, values in odd ones");
 
 // What a unit and its tiles cost, in sixteenths of a tile of two row tiles.
-constexpr int kPad = 36, kTwo = 16, kOne = 15, kLeast = 64;
+constexpr int kPad = 27, kTwo = 16, kOne = 14, kLeast = 64;
 
 struct TilesArgs {
   CrossAttend a;
