@@ -27,7 +27,7 @@
 // A step of two row tiles and 128 frames takes 1.80 us at dim 128, its three products (scores, values with both parts of the weights)
 // at 2.1 PFLOP/s, above the library's rate: they bound it (with weights of 8 bits, two products, 1.39 us).  Dim 64: 1.66 us, a values' product whose
 // weights come from TMEM takes 65 clocks at any width, and the softmax 1300 a row tile.  6 ragged texts of up to 1100 tokens, 16 heads, over up to 9000 frames,
-// 4 key heads of 128: 194 us.  What a unit takes besides its tiles: first maximum, last products, results (64 KB at 64 bytes per
+// 4 key heads of 128: 194 us.  What a unit takes besides its tiles, 3.0 us: first maximum, last products, results (64 KB at 64 bytes per
 // clock, 128 where it is shared).
 #include <algorithm>
 #include <type_traits>
@@ -66,7 +66,8 @@ struct TilesShape {
 
 static_assert(TilesShape<64>::kStages % 2 == 0 && TilesShape<128>::kStages % 2 == 0, "keys in even stages, values in odd ones");
 
-// What a unit and its tiles cost, in sixteenths of a tile of two row tiles.
+// What a unit and its tiles cost, in sixteenths of a tile of two row tiles: 3.0 us, 1.80 and (one row tile) 1.60 at dim 128.  (A unit
+// of one row tile: 2.1 us; dim 64: 2.0, 1.66 and 1.38, 1.1.)
 constexpr int kPad = 27, kTwo = 16, kOne = 14, kLeast = 64;
 
 struct TilesArgs {
@@ -798,9 +799,11 @@ bool cross_tiles_plan(const tsd_states& s, const tsd_cross_batch& b, int heads, 
   const int64_t most = std::max<int64_t>(1, b.max_rows ? std::min(b.max_rows, b.rows) : !b.starts ? 1 : ((int64_t)b.rows + b.n - 1) / b.n);
   if (s.k_frame < s.dim || s.v_frame < s.dim) return false;
   // cross_rows.cu's time grows with its units of 16 rows, each of which reads the frames again (0.016 us + 0.047 us per 1000 frames at dim 128,
-  // half of that at 64), this kernel's starts at 7 to 13 us.  Here and there, us, dim 128: 64 sources of 100 frames, 8 key heads: 20 rows
-  // 14 and 23, 64 rows 14 and 46; 4 of 300, 4 key heads: 64 rows 12 and 10, 500 rows 17 and 20; one of 12000, one key head: 40
-  // rows 17 and 24.  Dim 64, 64 of 400, 8 key heads: 20 rows 28 and 23, 40 rows 28 and 31.
+  // half of that at 64), this kernel's starts at 9 to 15 us.  Here and there, us, ragged (from 0.4 of the sizes on), dim 128: 64 sources of 100 frames,
+  // 8 key heads: 20 rows 15 and 15, 64 rows 16 and 23; 4 of 300, 4 key heads: 64 rows 14 and 7, 500 rows 18 and 12; 24 of 500, 8: 24 rows 18 and
+  // 20; one of 9000, 4: 64 rows 20 and 23; one of 20000, 8: 17 rows 30 and 44.  Dim 64, 8 key heads, 64 of 400: 20 rows 24 and 16, 40 rows 24 and 21;
+  // 24 of 900: 48 rows 20 and 20; 2 of 15000: 40 rows 26 and 27; 32 of 300: 40 rows 16 and 11.  (From the bounds on to twice them
+  // the other kernel is often the faster one still.)
   const int64_t sixteens = (most * group + 15) / 16;
   if (sixteens < 2) return false;
   const bool much = sixteens > (s.dim == 64 ? 2 : 1) && (double)b.n * s.kv_heads * sixteens * (s.frames + 330.0) >= (s.dim == 64 ? 350e3 : 200e3);
