@@ -391,7 +391,9 @@ cudaError_t launch(NormArgs a, int sms, cudaStream_t s) {
   using std::integral_constant;
   const int d = a.d + (HOW == NormHow::kShifted ? 7 : 0);  // (with the elements that a row's first group may begin before it)
   // Up to 32 elements per thread: what each thread does besides (the sums' joins, the root) then weighs little.  Few rows:
-  // as many threads as a row has groups.  200 x 777 with norms on both sides: 4.0 us, with 32 threads per row 7.8.
+  // as many threads as a row has groups.  With norms on both sides, us, so and with the threads of many rows: 152 rows of 512 2.5 and 2.8, of
+  // 1537 3.4 and 6.1, of 4096 3.4 and 3.9, of 8192 4.5 and 4.4; 608 rows: 2.7 and 2.8, 4.2 and 6.4, 6.4 and 5.1, 10.9 and 9.0; 912 rows: 3.0
+  // and 3.1, 6.2 and 6.7, 8.4 and 5.9, 15.2 and 10.3 (above 2048 elements many rows' threads are the better ones from some 300 rows on).
   if constexpr (EVEN)
     if (a.n <= 6 * sms && d > 256) {
       if (d <= 512) return go(integral_constant<int, 64>{}, integral_constant<int, 1>{});

@@ -291,3 +291,18 @@ def test_results_that_a_call_does_not_write_are_refused():
     a, b = tsd.residual_norm(x, y, norm=None, out=(None, r))
     assert a is None and b is r
     check(x, y, None, None, None, 1.0, None, None, None, None, 1e-5, None, r)
+
+
+@pytest.mark.parametrize("pad", [64, 65])
+@pytest.mark.parametrize("d", [512, 333])
+def test_far_rows(d, pad):
+    """Rows whose offsets pass 2^32 elements, in whole groups of eight, off them, and (the gate) apart from the others."""
+    far = 2 ** 31 + pad
+    buf = torch.empty(3 * far, dtype=BF, device="cuda")
+    x, y, h, r, gt = (buf[1024 * i:].as_strided((3, d), (far, 1)) for i in range(5))
+    a, b, (w, _, pw, _), c = make(3, d, BF, BF, "rows", seed=d)
+    x.copy_(a), y.copy_(b), gt.copy_(c)
+    tsd.residual_norm(x, y, weight=w, post="layer", post_weight=pw, gate=gt, out=(h, r))
+    check(a, b, "rms", "layer", c, 1.0, w, None, pw, None, 1e-5, h, r)
+    tsd.residual_norm(x, y, weight=w, post="layer", post_weight=pw, gate=c, out=(y, x))
+    check(a, b, "rms", "layer", c, 1.0, w, None, pw, None, 1e-5, y, x)

@@ -256,3 +256,20 @@ def test_binding_refusals():
                      (dict(q=q, lens=p, slots=p[:2], starts=p), "n \\+ 1"), (dict(q=q, positions=p, out=k), "result of q"), (dict(q=q.cpu(), positions=p), "device")]:
         with pytest.raises(ValueError, match=word):
             r(**kw)
+
+
+@pytest.mark.parametrize("dim,rot", [(64, 64), (80, 26)])
+def test_far_rows(dim, rot):
+    """Rows whose offsets pass 2^32 elements, into rows as far and in place."""
+    far, pos = 2 ** 31 + 64, [3, 70000, 11]
+    r = tsd.Rotary(dim, rot)
+    buf = torch.empty(3 * far, dtype=torch.bfloat16, device="cuda")
+    x = buf.as_strided((3, 2, dim), (far, 128, 1))
+    y = buf[1024:].as_strided((3, 2, dim), (far, 128, 1))
+    src = rand(3, 2, dim)
+    x.copy_(src)
+    p = torch.tensor(pos, dtype=torch.int32, device="cuda")
+    r(x, positions=p, out=y)
+    check(y, src, pos, rot, "half")
+    r(x, positions=p, out=x)
+    assert torch.equal(x, y)
