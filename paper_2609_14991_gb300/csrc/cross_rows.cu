@@ -20,7 +20,7 @@
 // Warps, then the CTAs of a cluster (a long source's frames are dealt out to up to
 // eight), join their maxima, sums and results through shared memory.
 //
-// Bound by memory: 4 sources of 45000 frames, one row each, 8 key heads of 128: 87 us, 0.89 of the copy rate; 64 of 1500, 8
+// Bound by memory: 4 sources of 45000 frames, one row each, 8 key heads of 128: 88 us, 0.88 of the copy rate; 64 of 1500, 8
 // rows, 16 heads of 64: 48.5 us, 0.82.  Rings of three steps (dim 64: four): with one more per warp fewer CTAs fit an SM (139 and 52
 // us), with one less 102 and 49.  One row over 375 frames: 5.2 us, launch, length, frames and join one after the other.
 #include <cooperative_groups.h>

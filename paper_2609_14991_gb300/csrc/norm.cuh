@@ -4,7 +4,7 @@
 // in one pass: a row stays in registers from its loads to its stores, statistics
 // are fp32 sums over deviations from a mean known before (layer) or squares (rms),
 // and h is computed from r before r is rounded.  Reads x, y (and g), writes r and h:
-// bound by memory.  16384 x 4096, bf16, norms on both sides and a gate: 84 us, 0.94 of the copy rate; 7000 x 8192, one norm:
+// bound by memory.  16384 x 4096, bf16, norms on both sides and a gate: 89 us, 0.89 of the copy rate; 7000 x 8192, one norm:
 // 69 us, 0.97; 60000 x 256: 22 us, 0.81 (what a row takes besides its elements); 16384 x 3001: 84 us, 0.69 (weights from
 // the 16 bytes around them).  One array of a row is in registers at a time, in pairs: the others come from shared
 // memory or the L1 cache group by group, so that six CTAs of 128 rows' threads fit an SM.
