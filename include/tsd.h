@@ -826,7 +826,7 @@ typedef struct {
   const int32_t* sources; /* [n] or NULL */
   const int32_t* starts;  /* [n + 1] or NULL */
   int32_t rows;           /* rows of the row arrays, 1..2^22 */
-  int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches and picks the kernel.  Results need not it to be right, their last bits may follow it */
+  int32_t max_rows;       /* most rows of a sequence (0: unknown): sizes launches and picks the kernel; need not be right, only last bits of results may follow it */
 } tsd_cross_batch;
 
 /* Bytes of device memory, 16-byte aligned, that such a call of tsd_cross_attend needs for itself alone (may be 0; the structs'
