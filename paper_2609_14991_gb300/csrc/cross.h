@@ -3,13 +3,24 @@
 
 #include "elem.cuh"
 #include "internal.h"
+#include "tc_common.cuh"
 
 namespace tsd {
 
-// A weight goes into the values' product as the sum of two 16-bit floats, hi = round(w f) and round(w - hi): half a step of the
-// second is at most 2^-16 w.  f is below 1, so neither is negative or (a rest of 0) makes a value's infinity a NaN.
+// Two weights go into the values' product as the sum of two pairs of 16-bit floats, `first`, a little less than they, and what is left: within
+// 2^-16 of them.  Neither is negative or (but of a weight of 0) 0: that would make a value's infinity a NaN.
+// bf16: cut off, and 2^-20 more is left; fp16: 31/32 rounded.  (The cut part's numbers from its pair, not by masks: 195 us where
+// those take 200, 6 x 1100 over 9000.)
 template <bool BF16>
-constexpr float kFirstPart = BF16 ? 255.f / 256 : 31.f / 32;
+__device__ __forceinline__ void weight_parts(float a, float b, uint32_t& first, uint32_t& rest) {
+  const float scale = BF16 ? 1.f + 0x1p-20f : 31.f / 32;
+  const uint64_t w = tc::pair_of(a, b), scaled = tc::mul2(w, tc::pair_of(scale, scale));
+  float x, y;
+  tc::unpair(scaled, x, y);
+  first = BF16 ? __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632) : narrow2<BF16>(x, y);
+  tc::unpair(tc::fma2(tc::pair_of(wide16<BF16>(first & 0xffffu), wide16<BF16>(first >> 16)), tc::pair_of(-1.f, -1.f), BF16 ? scaled : w), x, y);
+  rest = narrow2<BF16>(x, y);
+}
 
 struct CrossAttend {
   tsd_states s;

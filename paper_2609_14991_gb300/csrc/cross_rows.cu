@@ -190,9 +190,7 @@ __global__ void __launch_bounds__(32 * kWarps, (DIM == 128 ? 8 : 12) / kWarps) k
           for (int nt = 0; nt < 2; ++nt) {
             const float x = ex2_approx(s[nt][2 * h] - ref), y = ex2_approx(s[nt][2 * h + 1] - ref);
             l[h] += x + y;
-            const uint32_t w = narrow2<BF16>(x * kFirstPart<BF16>, y * kFirstPart<BF16>);
-            p[2 * nt + h] = w;
-            rest[2 * nt + h] = narrow2<BF16>(x - wide16<BF16>(w & 0xffffu), y - wide16<BF16>(w >> 16));
+            weight_parts<BF16>(x, y, p[2 * nt + h], rest[2 * nt + h]);
           }
         }
         // values: frames 2t, 2t+1, 2t+8, 2t+9; eight dimensions from 64 u + 8 g

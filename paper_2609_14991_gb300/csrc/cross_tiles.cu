@@ -313,7 +313,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
     // any two that differ do so by so much that the lower weighs nothing (by 4 at least, times c's change).
     constexpr float kFar = 0x1p26f;
     const float c_far = sign * __uint_as_float((__float_as_uint(fabsf(c)) + 0x7fffffu) & 0x7f800000u);
-    const uint64_t minus = pair_of(-1.f, -1.f), first2 = pair_of(kFirstPart<BF16>, kFirstPart<BF16>);
     const float nan = __uint_as_float(0x7fc00000u);
     int at0 = 0, done = 0;  // steps and parts of this row tile so far
     bool fine = true, join = false;
@@ -438,13 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_cross_tiles(const __grid_consta
                   unpair(fma2(pair_of(__uint_as_float(raw[b][e]), __uint_as_float(raw[b][e + 1])), c2, ref2), x0, x1);
                   const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
                   sums[e / 2 & 1] = add2(sums[e / 2 & 1], pair_of(p0, p1));
-                  float w0, w1;
-                  unpair(mul2(pair_of(p0, p1), first2), w0, w1);
-                  const uint32_t w = narrow2<BF16>(w0, w1);
-                  y[16 * b + e / 2] = w;
-                  float r0, r1;
-                  unpair(fma2(pair_of(wide16<BF16>(w & 0xffffu), wide16<BF16>(w >> 16)), minus, pair_of(p0, p1)), r0, r1);
-                  rest[16 * b + e / 2] = narrow2<BF16>(r0, r1);
+                  weight_parts<BF16>(p0, p1, y[16 * b + e / 2], rest[16 * b + e / 2]);
                 }
               }
               float s0, s1;
